@@ -297,6 +297,180 @@ das_status das_kv_append_f8(const das_kv_cache_f8 *cache, const void *k_new, con
                             const int32_t *accepted, int W, int32_t *prefix_len,
                             int32_t *error_flag, void *stream);
 
+/*
+ * ---- Paged cache with block scales, and sampling ----------------------------
+ * The paper has no counterpart for what follows: its experiments decode one
+ * sequence greedily out of one contiguous cache.
+ */
+
+/* Tokens of one page, and of one block of a scale. */
+#define DAS_PAGE_TOKENS 64
+
+/*
+ * A depth-indexed cache in pages of 64 tokens, every depth held in 8 bits with
+ * a scale per (page, kv head):
+ *   k, v              device e4m3 (as in das_kv_cache_f8)
+ *                     [depths][layers][pages][kv_heads][64][head_dim]
+ *   k_scale, v_scale  device fp32 [depths][layers][pages][kv_heads], positive;
+ *                     the key (value) is its code times its page's scale
+ * A sequence's tokens 64 t .. 64 t + 63 are in page block_table[b][t]; the
+ * tables, of as many sequences as the caller has, are arguments of the calls.
+ * Places of a page past its sequence's length may hold anything.  k and v are
+ * 16-byte aligned; the caller owns the memory.
+ */
+typedef struct {
+    void *k;
+    void *v;
+    float *k_scale;
+    float *v_scale;
+    int depths, layers, pages, kv_heads, head_dim; /* head_dim: 64 or 128 */
+} das_kv_cache_paged;
+
+/*
+ * Block tables and slot maps from request lengths.  Request b holds
+ * seq_len[b] tokens in pages(seq_len[b]) pages, pages(n) = ceil(n / 64), the
+ * first entries of row b of block_table; grow[b] > 0 asks for that many tokens
+ * more, grow[b] < 0 gives the last -grow[b] back (all of them if fewer are
+ * held: the request has ended).  In request order
+ *   - the pages of table entries pages(new) .. pages(old) - 1 of every
+ *     request that shrinks are pushed on the stack of free pages;
+ *   - then every request that grows takes what it needs from the stack's top
+ *     into its next table entries.
+ * A request that asks for more is refused (keeps its length and pages; bit 0
+ * of error_flag is set) if its row is too short, if the pages that it and the
+ * growing requests before it need (those of too short a row aside) are more
+ * than there are and it needs any, or if their tokens are more than max_slots.
+ *   seq_len         device int32 [batch]
+ *   grow            device int32 [batch]
+ *   block_table     device int32 [batch][max_pages], changed in place; entries
+ *                   past a request's pages may hold anything
+ *   free_pages      device int32 [pages], changed in place: the stack
+ *   free_count      device int32 [1]: pages on the stack
+ *   slots           device int32 [max_slots]: the place page * 64 + i of every
+ *                   new token, request after request; -1 past the last
+ *   slot_start      device int32 [batch + 1]: where each request's begin
+ *   new_len         device int32 [batch]: the length after the call (may be
+ *                   seq_len itself)
+ *   new_free_count  device int32 [1] (may be free_count itself)
+ *   error_flag      device int32 [1]: bits are set, never cleared; bit 1: a
+ *                   length or a count was out of range and clamped
+ * With outputs apart from their inputs the call can be repeated and gives the
+ * same result: it changes only stack entries from free_count on, and table
+ * entries past the pages of old lengths.
+ * Requires batch >= 0, 1 <= max_pages, max_pages * 64 < 2^31, and
+ * pages * 64 < 2^31.
+ */
+das_status das_page_assign(const int32_t *seq_len, const int32_t *grow, int batch,
+                           int32_t *block_table, int max_pages, int32_t *free_pages, int pages,
+                           const int32_t *free_count, int32_t *slots, int max_slots,
+                           int32_t *slot_start, int32_t *new_len, int32_t *new_free_count,
+                           int32_t *error_flag, void *stream);
+
+/*
+ * Commit into a paged cache: the first n_b = slot_start[b + 1] - slot_start[b]
+ * of each sequence's W staged tokens are stored at slots[slot_start[b] ..] at
+ * every depth and layer (das_page_assign makes both; a sequence's slots run on
+ * within a page and start the next page at its first place).
+ * For each page, kv head, and keys and values apart: the scale is 2^e with the
+ * least e in [-40, 120] such that every finite new element is at most
+ * 448 * 2^e in size.  If the page already holds tokens before the first new
+ * one, it is the larger of that and its present scale, and the older codes
+ * are rounded again where the scale grew (exact unless a code becomes
+ * subnormal).  A code is the element / scale rounded to e4m3 (nearest, ties to
+ * even, +-448 at most; NaN stays NaN).
+ *   k_new, v_new  device bf16 [depths][layers][batch][W][kv_heads][head_dim]
+ *   slots         device int32 [max_slots]
+ *   slot_start    device int32 [batch + 1]
+ *   error_flag    device int32 [1]: bit 1 is set (never cleared) and the page
+ *                 left alone where a slot lies outside the cache, a page does
+ *                 not start at its first place, or n_b is not in 0..W
+ * Sequences do not share the pages that they write.  Requires W >= 1.
+ */
+das_status das_kv_append_paged(const das_kv_cache_paged *cache, const void *k_new,
+                               const void *v_new, int batch, int W, const int32_t *slots,
+                               int max_slots, const int32_t *slot_start, int32_t *error_flag,
+                               void *stream);
+
+/* Workspace bytes for das_mature_v_attention_paged (as das_workspace_size). */
+size_t das_workspace_size_paged(const das_kv_cache_paged *cache, int batch, int num_q_heads,
+                                int max_block);
+
+/*
+ * das_mature_v_attention over a paged cache (Eqs. 2-3 on the values that its
+ * codes and scales stand for): keys of key_depth, values of value_depth;
+ * key_depth = value_depth is the verify attention.  max_block = 1 with
+ * block_len 1 is the call for single tokens.
+ *   block_table  device int32 [batch][max_pages]; entries past a sequence's
+ *                ceil(prefix_len / 64) pages are not read
+ *   prefix_len   device int32 [batch], 0..64 max_pages
+ *   k_blk, v_blk device bf16 [batch][max_block][kv_heads][head_dim]
+ * All other arguments, results and limits as das_mature_v_attention.  Bit 2
+ * of the workspace's status word is set where a table entry is no page of the
+ * cache; its 64 tokens are then taken as masked.
+ */
+das_status das_mature_v_attention_paged(const das_kv_cache_paged *cache, int layer, int key_depth,
+                                        int value_depth, const int32_t *block_table, int max_pages,
+                                        const int32_t *prefix_len, const int32_t *block_len,
+                                        int batch, int max_block, const void *q, const void *k_blk,
+                                        const void *v_blk, int num_q_heads, float softmax_scale,
+                                        void *out, float *lse, void *workspace,
+                                        size_t workspace_bytes, void *stream);
+
+typedef enum { DAS_LOGITS_F32 = 0, DAS_LOGITS_BF16 = 1 } das_logits_type;
+
+/* Sampling parameters, each device memory of one value per sequence, or NULL. */
+typedef struct {
+    const float *temperature; /* NULL: 1; <= 0 or NaN: greedy (the first maximum) */
+    const int32_t *top_k;     /* NULL or <= 0: all tokens                         */
+    const float *top_p;       /* NULL, >= 1 or NaN: all tokens                    */
+    const float *min_p;       /* NULL, <= 0 or NaN: all tokens; 1 at most         */
+} das_sampling;
+
+/*
+ * One token drawn from every row of logits with the row's random number.
+ * With m the row's largest logit l_v (NaN counts as -inf) and T the
+ * temperature,
+ *   e_v = 1 if l_v = m, 0 if l_v = -inf, else exp((l_v - m) / T) in binary32,
+ *   w_v = e_v * 2^32 rounded to a whole number,
+ * tokens ordered by logit, largest first, equal ones by index:
+ *   top-k keeps the first top_k tokens,
+ *   top-p keeps the least number of those (one at least) whose w sum to at
+ *         least ceil(top_p * S), S the sum over what top-k kept,
+ *   min-p keeps those of them with e_v >= min_p.
+ * With R the sum of the kept w, the token is the least index v for which the
+ * kept w up to and including v sum to more than floor(u R) (products in
+ * binary64; u is clamped to [0, 1)), and its logprob (l_v - m) / T -
+ * ln(R / 2^32).  Greedy rows keep the first token alone.  All sums are of
+ * whole numbers, so the result does not depend on their order.  A row with no
+ * logit above -inf gives token -1 and logprob -inf.
+ *   logits    device fp32 or bf16, row (b, i) at element
+ *             (b * W + i) * row_stride, row_stride >= vocab
+ *   uniforms  device fp32 [B][W], in [0, 1)
+ *   tokens    device int32 [B][W]
+ *   logprobs  device fp32 [B][W], or NULL
+ * Requires 1 <= W <= 1024, 1 <= vocab < 2^31.
+ */
+das_status das_sample(const void *logits, das_logits_type type, int B, int W, int vocab,
+                      long long row_stride, const das_sampling *sampling, const float *uniforms,
+                      int32_t *tokens, float *logprobs, void *stream);
+
+/*
+ * Sampled acceptance of proposals that a drafter made without chance (as
+ * DAS drafting does): target_ids[b][i] is drawn from logits[b][i] as
+ * das_sample draws it, and proposals are accepted while they equal it, so
+ * that every emitted token is a draw from the target's own (truncated)
+ * distribution.  accepted, target_ids and next_token as das_greedy_accept;
+ *   committed  device int32 [B], or NULL: min(accepted + 1, W), the verifier
+ *              inputs to commit (grow of das_page_assign)
+ * At temperature 0 it is das_greedy_accept, except that a row with no logit
+ * above -inf gives -1, which no proposal equals.
+ */
+das_status das_sample_accept(const void *logits, das_logits_type type, const int32_t *draft_ids,
+                             int B, int W, int vocab, long long row_stride,
+                             const das_sampling *sampling, const float *uniforms,
+                             int32_t *accepted, int32_t *target_ids, int32_t *next_token,
+                             int32_t *committed, float *logprobs, void *stream);
+
 /* Static text for a status code. */
 const char *das_status_string(das_status s);
 

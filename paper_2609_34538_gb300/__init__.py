@@ -15,6 +15,15 @@ ABI in include/das.h:
     DepthKVCacheF8, das_mature_v_attention_f8, das_kv_append_f8
                             the cache variant with depths below R stored as
                             e4m3 (not in the paper)
+    PagedKVCache, das_page_assign, das_kv_append_paged,
+    das_mature_v_attention_paged
+                            a cache in pages of 64 tokens held as e4m3 with a
+                            scale per (page, kv head): block tables and slot
+                            maps, commit and attention (not in the paper)
+    das_sample, das_sample_accept
+                            sampling (temperature, top-k, top-p, min-p) from
+                            given random numbers, and acceptance against the
+                            draws (not in the paper)
     AttentionCall           the attention calls with arguments checked once, for
                             loops that call with the same tensors every step
     wave_widths, WaveRefinement
@@ -30,6 +39,8 @@ import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdas.so")
+
+PAGE_TOKENS = 64  # DAS_PAGE_TOKENS
 
 DAS_OK, DAS_ERR_INVALID_ARG, DAS_ERR_UNSUPPORTED, DAS_ERR_WORKSPACE, DAS_ERR_CUDA = range(5)
 
@@ -51,6 +62,17 @@ class das_kv_cache_f8(ctypes.Structure):
                 ("k_low", ctypes.c_void_p), ("v_low", ctypes.c_void_p), ("depths", ctypes.c_int),
                 ("layers", ctypes.c_int), ("batch", ctypes.c_int), ("capacity", ctypes.c_int),
                 ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int)]
+
+
+class das_kv_cache_paged(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("depths", ctypes.c_int), ("layers", ctypes.c_int),
+                ("pages", ctypes.c_int), ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int)]
+
+
+class das_sampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p),
+                ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p)]
 
 
 def _load():
@@ -83,6 +105,21 @@ def _load():
     lib.das_mature_v_attention_noalloc.restype = i
     lib.das_noalloc_status.argtypes = [p, p]
     lib.das_noalloc_status.restype = i
+    cpp, ll = ctypes.POINTER(das_kv_cache_paged), ctypes.c_longlong
+    lib.das_page_assign.argtypes = [p, p, i, p, i, p, i, p, p, i, p, p, p, p, p]
+    lib.das_page_assign.restype = i
+    lib.das_kv_append_paged.argtypes = [cpp, p, p, i, i, p, i, p, p, p]
+    lib.das_kv_append_paged.restype = i
+    lib.das_workspace_size_paged.argtypes = [cpp, i, i, i]
+    lib.das_workspace_size_paged.restype = sz
+    lib.das_mature_v_attention_paged.argtypes = [cpp, i, i, i, p, i, p, p, i, i, p, p, p, i, f, p,
+                                                 p, p, sz, p]
+    lib.das_mature_v_attention_paged.restype = i
+    sp = ctypes.POINTER(das_sampling)
+    lib.das_sample.argtypes = [p, i, i, i, i, ll, sp, p, p, p, p]
+    lib.das_sample.restype = i
+    lib.das_sample_accept.argtypes = [p, i, p, i, i, i, ll, sp, p, p, p, p, p, p, p]
+    lib.das_sample_accept.restype = i
     lib.das_status_string.argtypes = [i]
     lib.das_status_string.restype = ctypes.c_char_p
     return lib
@@ -465,3 +502,211 @@ def das_kv_append_f8(cache, k_new, v_new, accepted, prefix_len, error_flag, stre
     _check(LIB.das_kv_append_f8(ctypes.byref(cache.desc), _ptr(k_new), _ptr(v_new),
                                 _ptr(accepted), W, _ptr(prefix_len), _ptr(error_flag),
                                 _stream(stream)), "das_kv_append_f8")
+
+
+def _new(shape, dtype, device, stream):
+    """An uninitialised tensor for results written on `stream` (allocated there,
+    so that memory still in use on another stream is not handed out)."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _need_shape(t, dtype, name, shape):
+    _need(t, dtype, name, len(shape))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+class PagedKVCache:
+    """A depth-indexed cache in pages of 64 tokens, all depths as e4m3 codes with
+    a scale per (page, kv head): k, v uint8
+    [depths][layers][pages][kv_heads][64][head_dim], k_scale, v_scale fp32
+    [depths][layers][pages][kv_heads].  Which pages a sequence has is its row of
+    a block table (das_page_assign)."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        _need(k, torch.uint8, "k", 6)
+        _need(v, torch.uint8, "v", 6)
+        _need(k_scale, torch.float32, "k_scale", 4)
+        _need(v_scale, torch.float32, "v_scale", 4)
+        if k.shape != v.shape:
+            raise ValueError("k and v shapes differ")
+        R, L, N, H, page, D = k.shape
+        if page != PAGE_TOKENS:
+            raise ValueError(f"pages must have {PAGE_TOKENS} tokens, got {page}")
+        if tuple(k_scale.shape) != (R, L, N, H) or tuple(v_scale.shape) != (R, L, N, H):
+            raise ValueError("k_scale / v_scale must be [depths][layers][pages][kv_heads]")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.desc = das_kv_cache_paged(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
+                                       v_scale.data_ptr(), R, L, N, H, D)
+
+    @classmethod
+    def empty(cls, depths, layers, pages, kv_heads, head_dim, device="cuda"):
+        tiles = (depths, layers, pages, kv_heads)
+        codes = lambda: torch.empty(tiles + (PAGE_TOKENS, head_dim), dtype=torch.uint8,
+                                    device=device)
+        scales = lambda: torch.ones(tiles, dtype=torch.float32, device=device)
+        return cls(codes(), codes(), scales(), scales())
+
+    @property
+    def shape(self):
+        """(depths, layers, pages, kv_heads, head_dim)"""
+        d = self.desc
+        return (d.depths, d.layers, d.pages, d.kv_heads, d.head_dim)
+
+
+def das_page_assign(seq_len, grow, block_table, free_pages, free_count, slots, error_flag,
+                    new_len=None, new_free_count=None, slot_start=None, stream=None):
+    """Block tables and slot maps from request lengths: request b goes from
+    seq_len[b] to seq_len[b] + grow[b] tokens, giving pages back to the stack
+    free_pages[:free_count] or taking them from its top; block_table and
+    free_pages change in place, slots gets the places of all new tokens.
+    new_len and new_free_count may be seq_len and free_count themselves.
+    Returns (new_len, new_free_count, slot_start)."""
+    _need(seq_len, torch.int32, "seq_len", 1)
+    B = seq_len.numel()
+    _need_shape(grow, torch.int32, "grow", (B,))
+    _need(block_table, torch.int32, "block_table", 2)
+    if block_table.shape[0] != B:
+        raise ValueError("block_table must be [batch][max_pages]")
+    _need(free_pages, torch.int32, "free_pages", 1)
+    _need_shape(free_count, torch.int32, "free_count", (1,))
+    _need(slots, torch.int32, "slots", 1)
+    _need_shape(error_flag, torch.int32, "error_flag", (1,))
+    dev = seq_len.device
+    new_len = _new(B, torch.int32, dev, stream) if new_len is None else new_len
+    new_free_count = (_new(1, torch.int32, dev, stream) if new_free_count is None
+                      else new_free_count)
+    slot_start = _new(B + 1, torch.int32, dev, stream) if slot_start is None else slot_start
+    _need_shape(new_len, torch.int32, "new_len", (B,))
+    _need_shape(new_free_count, torch.int32, "new_free_count", (1,))
+    _need_shape(slot_start, torch.int32, "slot_start", (B + 1,))
+    _check(LIB.das_page_assign(
+        _ptr(seq_len), _ptr(grow), B, _ptr(block_table), block_table.shape[1], _ptr(free_pages),
+        free_pages.numel(), _ptr(free_count), _ptr(slots), slots.numel(), _ptr(slot_start),
+        _ptr(new_len), _ptr(new_free_count), _ptr(error_flag), _stream(stream)),
+        "das_page_assign")
+    return new_len, new_free_count, slot_start
+
+
+def das_kv_append_paged(cache, k_new, v_new, slots, slot_start, error_flag, stream=None):
+    """Commit into a PagedKVCache: the first slot_start[b + 1] - slot_start[b] of
+    each sequence's staged tokens, at every depth and layer, as e4m3 codes under
+    a power-of-two scale per (page, kv head)."""
+    _need(k_new, torch.bfloat16, "k_new", 6)
+    _need(v_new, torch.bfloat16, "v_new", 6)
+    R, L, _, H, D = cache.shape
+    B, W = k_new.shape[2:4]
+    if tuple(k_new.shape) != (R, L, B, W, H, D) or k_new.shape != v_new.shape:
+        raise ValueError("k_new / v_new must be [depths][layers][batch][W][kv_heads][head_dim]")
+    _need(slots, torch.int32, "slots", 1)
+    _need_shape(slot_start, torch.int32, "slot_start", (B + 1,))
+    _need_shape(error_flag, torch.int32, "error_flag", (1,))
+    _check(LIB.das_kv_append_paged(
+        ctypes.byref(cache.desc), _ptr(k_new), _ptr(v_new), B, W, _ptr(slots), slots.numel(),
+        _ptr(slot_start), _ptr(error_flag), _stream(stream)), "das_kv_append_paged")
+
+
+def new_workspace_paged(cache, batch, num_q_heads, max_block, device=None):
+    """Zeroed workspace for das_mature_v_attention_paged."""
+    n = int(LIB.das_workspace_size_paged(ctypes.byref(cache.desc), batch, num_q_heads, max_block))
+    if n == 0:
+        raise DasError(DAS_ERR_UNSUPPORTED, "das_workspace_size_paged")
+    return torch.zeros(n, dtype=torch.uint8, device=device or cache.k.device)
+
+
+def das_mature_v_attention_paged(cache, layer, key_depth, value_depth, block_table, prefix_len,
+                                 block_len, q, k_blk, v_blk, workspace, out=None, lse=None,
+                                 softmax_scale=0.0, stream=None):
+    """das_mature_v_attention over a PagedKVCache; key_depth = value_depth is the
+    verify attention.  Returns (out, lse)."""
+    _need(prefix_len, torch.int32, "prefix_len", 1)
+    _need(block_table, torch.int32, "block_table", 2)
+    _need(q, torch.bfloat16, "q", 4)
+    R, L, N, H, D = cache.shape
+    B, T, Hq, Dq = q.shape
+    if Dq != D or prefix_len.numel() != B or block_table.shape[0] != B:
+        raise ValueError("q / length / table shapes do not match the cache")
+    _need_shape(block_len, torch.int32, "block_len", (B,))
+    _need_shape(k_blk, torch.bfloat16, "k_blk", (B, T, H, D))
+    _need_shape(v_blk, torch.bfloat16, "v_blk", (B, T, H, D))
+    _need(workspace, torch.uint8, "workspace", 1)
+    out = _new(q.shape, torch.bfloat16, q.device, stream) if out is None else out
+    lse = _new((B, Hq, T), torch.float32, q.device, stream) if lse is None else lse
+    _need_shape(out, torch.bfloat16, "out", q.shape)
+    _need_shape(lse, torch.float32, "lse", (B, Hq, T))
+    _check(LIB.das_mature_v_attention_paged(
+        ctypes.byref(cache.desc), layer, key_depth, value_depth, _ptr(block_table),
+        block_table.shape[1], _ptr(prefix_len), _ptr(block_len), B, T, _ptr(q), _ptr(k_blk),
+        _ptr(v_blk), Hq, float(softmax_scale), _ptr(out), _ptr(lse), _ptr(workspace),
+        workspace.numel(), _stream(stream)), "das_mature_v_attention_paged")
+    return out, lse
+
+
+def _sampling_args(logits, uniforms, temperature, top_k, top_p, min_p):
+    """Checks shared by the sampling calls: (type, B, W, vocab, row stride, parameters).
+    Rows of the logits may be strided (a padded vocabulary)."""
+    if not isinstance(logits, torch.Tensor):
+        raise TypeError("logits must be a torch.Tensor")
+    if logits.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"logits must be float32 or bfloat16, got {logits.dtype}")
+    if not logits.is_cuda:
+        raise ValueError("logits must be on a CUDA device")
+    if logits.dim() != 3:
+        raise ValueError(f"logits must have 3 dims, got {tuple(logits.shape)}")
+    B, W, V = logits.shape
+    row = logits.stride(1) if W > 1 else logits.stride(0) if B > 1 else V
+    if (V > 1 and logits.stride(2) != 1) or (B > 1 and logits.stride(0) != W * row):
+        raise ValueError("logits must have contiguous rows at one stride")
+    _need_shape(uniforms, torch.float32, "uniforms", (B, W))
+    for t, dt, name in ((temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
+                        (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p")):
+        if t is not None:
+            _need_shape(t, dt, name, (B,))
+    params = das_sampling(_ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p))
+    return int(logits.dtype == torch.bfloat16), B, W, V, row, params
+
+
+def das_sample(logits, uniforms, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None,
+               logprobs=None, stream=None):
+    """One token from every row of logits [B][W][vocab] (fp32 or bf16) with the
+    row's random number in [0, 1); parameters are per sequence, None for none.
+    Returns (tokens, logprobs)."""
+    kind, B, W, V, row, params = _sampling_args(logits, uniforms, temperature, top_k, top_p, min_p)
+    dev = logits.device
+    tokens = _new((B, W), torch.int32, dev, stream) if tokens is None else tokens
+    logprobs = _new((B, W), torch.float32, dev, stream) if logprobs is None else logprobs
+    _need_shape(tokens, torch.int32, "tokens", (B, W))
+    _need_shape(logprobs, torch.float32, "logprobs", (B, W))
+    _check(LIB.das_sample(_ptr(logits), kind, B, W, V, row, ctypes.byref(params), _ptr(uniforms),
+                          _ptr(tokens), _ptr(logprobs), _stream(stream)), "das_sample")
+    return tokens, logprobs
+
+
+def das_sample_accept(logits, draft_ids, uniforms, temperature=None, top_k=None, top_p=None,
+                      min_p=None, accepted=None, target_ids=None, next_token=None, committed=None,
+                      logprobs=None, stream=None):
+    """Sampled acceptance: target_ids drawn as das_sample draws them, proposals
+    accepted while they equal them.  committed = min(accepted + 1, W).
+    Returns (accepted, target_ids, next_token, committed, logprobs)."""
+    kind, B, W, V, row, params = _sampling_args(logits, uniforms, temperature, top_k, top_p, min_p)
+    _need_shape(draft_ids, torch.int32, "draft_ids", (B, W))
+    dev = logits.device
+    new = lambda t, shape, dt: _new(shape, dt, dev, stream) if t is None else t
+    accepted = new(accepted, (B,), torch.int32)
+    target_ids = new(target_ids, (B, W), torch.int32)
+    next_token = new(next_token, (B,), torch.int32)
+    committed = new(committed, (B,), torch.int32)
+    logprobs = new(logprobs, (B, W), torch.float32)
+    _need_shape(accepted, torch.int32, "accepted", (B,))
+    _need_shape(target_ids, torch.int32, "target_ids", (B, W))
+    _need_shape(next_token, torch.int32, "next_token", (B,))
+    _need_shape(committed, torch.int32, "committed", (B,))
+    _need_shape(logprobs, torch.float32, "logprobs", (B, W))
+    _check(LIB.das_sample_accept(
+        _ptr(logits), kind, _ptr(draft_ids), B, W, V, row, ctypes.byref(params), _ptr(uniforms),
+        _ptr(accepted), _ptr(target_ids), _ptr(next_token), _ptr(committed), _ptr(logprobs),
+        _stream(stream)), "das_sample_accept")
+    return accepted, target_ids, next_token, committed, logprobs

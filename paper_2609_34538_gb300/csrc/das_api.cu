@@ -283,6 +283,70 @@ das_status attention_f8(const das_kv_cache_f8 *c, int layer, int key_depth, int 
                           lse, workspace, workspace_bytes, false, stream);
 }
 
+bool cache_paged_ok(const das_kv_cache_paged *c) {
+    return c && c->k && c->v && c->k_scale && c->v_scale && c->depths >= 1 && c->depths <= 63 &&
+           c->layers >= 1 && c->layers <= (1 << 20) && c->pages >= 1 && c->pages < (1 << 25) &&
+           c->kv_heads >= 1 && c->kv_heads <= (1 << 20) &&
+           (c->head_dim == 64 || c->head_dim == 128) && aligned16(c->k) && aligned16(c->v);
+}
+
+das_status attention_paged(const das_kv_cache_paged *c, int layer, int key_depth, int value_depth,
+                           const int32_t *block_table, int max_pages, const int32_t *prefix_len,
+                           const int32_t *block_len, int batch, int max_block, const void *q,
+                           const void *k_blk, const void *v_blk, int num_q_heads,
+                           float softmax_scale, void *out, float *lse, void *workspace,
+                           size_t workspace_bytes, void *stream) {
+    if (c && c->head_dim != 64 && c->head_dim != 128) return DAS_ERR_UNSUPPORTED;
+    if (!cache_paged_ok(c) || layer < 0 || layer >= c->layers || key_depth < 1 ||
+        key_depth > c->depths || value_depth < 1 || value_depth > c->depths || !block_table ||
+        max_pages < 1 || max_pages >= (1 << 25) || !prefix_len || !block_len || batch < 1 || !q ||
+        !k_blk || !v_blk || !out || !lse || num_q_heads < 1 || max_block < 1 ||
+        num_q_heads % c->kv_heads != 0 || !aligned16(q) || !aligned16(k_blk) ||
+        !aligned16(v_blk) || !aligned16(out) || !isfinite(softmax_scale))
+        return DAS_ERR_INVALID_ARG;
+    const int G = num_q_heads / c->kv_heads;
+    if (max_block > kTileKeys || (long long)G * max_block > kMaxRows || batch > (1 << 20) ||
+        (long long)batch * c->kv_heads * G * max_block > 0x7fffffffLL)
+        return DAS_ERR_UNSUPPORTED;
+    const size_t need = das_workspace_size_paged(c, batch, num_q_heads, max_block);
+    if (need == 0) return DAS_ERR_CUDA;
+    if (!workspace || workspace_bytes < need ||
+        (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
+        return DAS_ERR_WORKSPACE;
+    const size_t slab_tiles = (size_t)c->pages * c->kv_heads;
+    const size_t slab_bytes = slab_tiles * DAS_PAGE_TOKENS * c->head_dim;
+    const size_t ks = (size_t)(key_depth - 1) * c->layers + layer;
+    const size_t vs = (size_t)(value_depth - 1) * c->layers + layer;
+    PagedAttnParams p = {};
+    p.k = static_cast<const uint8_t *>(c->k) + ks * slab_bytes;
+    p.v = static_cast<const uint8_t *>(c->v) + vs * slab_bytes;
+    p.k_scale = c->k_scale + ks * slab_tiles;
+    p.v_scale = c->v_scale + vs * slab_tiles;
+    p.table = block_table;
+    p.prefix_len = prefix_len;
+    p.block_len = block_len;
+    p.q = static_cast<const uint16_t *>(q);
+    p.k_blk = static_cast<const uint16_t *>(k_blk);
+    p.v_blk = static_cast<const uint16_t *>(v_blk);
+    p.out = static_cast<uint16_t *>(out);
+    p.lse = lse;
+    p.B = batch;
+    p.Hq = num_q_heads;
+    p.Hkv = c->kv_heads;
+    p.G = G;
+    p.max_block = max_block;
+    p.rows_max = G * max_block;
+    p.max_pages = max_pages;
+    p.pages = c->pages;
+    const double scale =
+        softmax_scale > 0.f ? (double)softmax_scale : 1.0 / sqrt((double)c->head_dim);
+    p.scale_log2 = (float)(scale * 1.4426950408889634);
+    return paged_attn_launch(p, c->head_dim, workspace, static_cast<cudaStream_t>(stream)) ==
+                   cudaSuccess
+               ? DAS_OK
+               : DAS_ERR_CUDA;
+}
+
 }  // namespace
 }  // namespace das
 
@@ -383,6 +447,107 @@ das_status das_kv_append_f8(const das_kv_cache_f8 *cache, const void *k_new, con
         return DAS_ERR_INVALID_ARG;
     return das::append_f8_launch(*cache, k_new, v_new, accepted, W, prefix_len, error_flag,
                                  static_cast<cudaStream_t>(stream)) == cudaSuccess
+               ? DAS_OK
+               : DAS_ERR_CUDA;
+}
+
+das_status das_page_assign(const int32_t *seq_len, const int32_t *grow, int batch,
+                           int32_t *block_table, int max_pages, int32_t *free_pages, int pages,
+                           const int32_t *free_count, int32_t *slots, int max_slots,
+                           int32_t *slot_start, int32_t *new_len, int32_t *new_free_count,
+                           int32_t *error_flag, void *stream) {
+    if (!free_count || !slot_start || !new_free_count || !error_flag || !free_pages || batch < 0 ||
+        (batch > 0 && (!seq_len || !grow || !block_table || !new_len)) || max_pages < 1 ||
+        max_pages >= (1 << 25) || pages < 1 || pages >= (1 << 25) || max_slots < 0 ||
+        (max_slots > 0 && !slots))
+        return DAS_ERR_INVALID_ARG;
+    const das::PageAssignArgs a = {seq_len,    grow,           block_table, free_pages,
+                                   free_count, slots,          slot_start,  new_len,
+                                   new_free_count, error_flag, batch,       max_pages,
+                                   pages,      max_slots};
+    return das::page_assign_launch(a, static_cast<cudaStream_t>(stream)) == cudaSuccess
+               ? DAS_OK
+               : DAS_ERR_CUDA;
+}
+
+das_status das_kv_append_paged(const das_kv_cache_paged *cache, const void *k_new,
+                               const void *v_new, int batch, int W, const int32_t *slots,
+                               int max_slots, const int32_t *slot_start, int32_t *error_flag,
+                               void *stream) {
+    if (cache && cache->head_dim != 64 && cache->head_dim != 128) return DAS_ERR_UNSUPPORTED;
+    if (!das::cache_paged_ok(cache) || !k_new || !v_new || batch < 0 || W < 1 || !slots ||
+        max_slots < 0 || !slot_start || !error_flag || !das::aligned16(k_new) ||
+        !das::aligned16(v_new))
+        return DAS_ERR_INVALID_ARG;
+    const long long pieces = ((long long)W + 2 * DAS_PAGE_TOKENS - 2) / DAS_PAGE_TOKENS;
+    if (W > (1 << 24) || pieces * cache->depths * cache->layers > 0x7fffffffLL / 2 ||
+        (double)pieces * cache->depths * cache->layers * batch * cache->kv_heads * 2 > 2147483647.0)
+        return DAS_ERR_UNSUPPORTED;
+    return das::append_paged_launch(*cache, k_new, v_new, batch, W, slots, max_slots, slot_start,
+                                    error_flag, static_cast<cudaStream_t>(stream)) == cudaSuccess
+               ? DAS_OK
+               : DAS_ERR_CUDA;
+}
+
+size_t das_workspace_size_paged(const das_kv_cache_paged *cache, int batch, int num_q_heads,
+                                int max_block) {
+    if (!cache || cache->kv_heads < 1 || batch < 1 || batch > (1 << 20) || num_q_heads < 1 ||
+        num_q_heads % cache->kv_heads != 0 || max_block < 1 ||
+        (cache->head_dim != 64 && cache->head_dim != 128))
+        return 0;
+    const int G = num_q_heads / cache->kv_heads;
+    if (max_block > das::kTileKeys || (long long)G * max_block > das::kMaxRows) return 0;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    return das::paged_workspace_bytes(dev, batch, cache->kv_heads, G * max_block, cache->head_dim);
+}
+
+das_status das_mature_v_attention_paged(const das_kv_cache_paged *cache, int layer, int key_depth,
+                                        int value_depth, const int32_t *block_table, int max_pages,
+                                        const int32_t *prefix_len, const int32_t *block_len,
+                                        int batch, int max_block, const void *q, const void *k_blk,
+                                        const void *v_blk, int num_q_heads, float softmax_scale,
+                                        void *out, float *lse, void *workspace,
+                                        size_t workspace_bytes, void *stream) {
+    return das::attention_paged(cache, layer, key_depth, value_depth, block_table, max_pages,
+                                prefix_len, block_len, batch, max_block, q, k_blk, v_blk,
+                                num_q_heads, softmax_scale, out, lse, workspace, workspace_bytes,
+                                stream);
+}
+
+static bool sample_args_ok(const das::SampleArgs &a, das_logits_type type) {
+    const uintptr_t elem = type == DAS_LOGITS_BF16 ? 2 : 4;
+    return (type == DAS_LOGITS_F32 || type == DAS_LOGITS_BF16) && a.logits && a.uniforms &&
+           a.tokens && a.B >= 0 && a.W >= 1 && a.W <= 1024 && a.vocab >= 1 &&
+           a.row_stride >= a.vocab && (long long)a.B * a.W <= 0x7fffffffLL / 8 &&
+           reinterpret_cast<uintptr_t>(a.logits) % elem == 0;
+}
+
+das_status das_sample(const void *logits, das_logits_type type, int B, int W, int vocab,
+                      long long row_stride, const das_sampling *sampling, const float *uniforms,
+                      int32_t *tokens, float *logprobs, void *stream) {
+    const das_sampling s = sampling ? *sampling : das_sampling{};
+    const das::SampleArgs a = {logits,     type == DAS_LOGITS_BF16, B, W, vocab, row_stride, s,
+                               uniforms, tokens, logprobs};
+    if (!sample_args_ok(a, type)) return DAS_ERR_INVALID_ARG;
+    return das::sample_launch(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? DAS_OK
+                                                                                   : DAS_ERR_CUDA;
+}
+
+das_status das_sample_accept(const void *logits, das_logits_type type, const int32_t *draft_ids,
+                             int B, int W, int vocab, long long row_stride,
+                             const das_sampling *sampling, const float *uniforms,
+                             int32_t *accepted, int32_t *target_ids, int32_t *next_token,
+                             int32_t *committed, float *logprobs, void *stream) {
+    const das_sampling s = sampling ? *sampling : das_sampling{};
+    const das::SampleArgs a = {logits,     type == DAS_LOGITS_BF16, B, W, vocab, row_stride, s,
+                               uniforms, target_ids, logprobs};
+    if (!sample_args_ok(a, type) || !draft_ids || !accepted || !next_token)
+        return DAS_ERR_INVALID_ARG;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (das::sample_launch(a, st) != cudaSuccess) return DAS_ERR_CUDA;
+    return das::sample_accept_launch(a, draft_ids, accepted, next_token, committed, st) ==
+                   cudaSuccess
                ? DAS_OK
                : DAS_ERR_CUDA;
 }

@@ -20,6 +20,11 @@ constexpr size_t kWorkspaceHeader = 256;
 // Bits of the workspace status word.
 constexpr int kStatusWaitTimeout = 1;
 constexpr int kStatusClamped = 2;
+constexpr int kStatusBadPage = 4;
+
+// Bits of the error flag of das_page_assign and das_kv_append_paged.
+constexpr int kFlagRefused = 1;
+constexpr int kFlagInvalid = 2;
 
 struct AttnParams {
     const int32_t *prefix_len;
@@ -82,5 +87,52 @@ cudaError_t append_launch(const das_kv_cache &c, const void *k_new, const void *
 cudaError_t append_f8_launch(const das_kv_cache_f8 &c, const void *k_new, const void *v_new,
                              const int32_t *accepted, int W, int32_t *prefix_len,
                              int32_t *error_flag, cudaStream_t stream);
+
+struct PageAssignArgs {
+    const int32_t *seq_len, *grow;
+    int32_t *table, *free_pages;
+    const int32_t *free_count;
+    int32_t *slots, *slot_start, *new_len, *new_free_count, *error_flag;
+    int batch, max_pages, pages, max_slots;
+};
+cudaError_t page_assign_launch(const PageAssignArgs &a, cudaStream_t stream);
+
+cudaError_t append_paged_launch(const das_kv_cache_paged &c, const void *k_new, const void *v_new,
+                                int batch, int W, const int32_t *slots, int max_slots,
+                                const int32_t *slot_start, int32_t *error_flag,
+                                cudaStream_t stream);
+
+struct PagedAttnParams {
+    const uint8_t *k, *v;                 // the slabs read: e4m3 [pages][Hkv][64][D]
+    const float *k_scale, *v_scale;       // [pages][Hkv]
+    const int32_t *table;                 // [B][max_pages]
+    const int32_t *prefix_len, *block_len;
+    const uint16_t *q, *k_blk, *v_blk;    // bf16
+    uint16_t *out;
+    float *lse;
+    float *part_o, *part_lse;             // [slots][rows_max][D], [slots][rows_max]
+    int32_t *status;
+    int B, Hq, Hkv, G, max_block, rows_max, max_pages, pages;
+    float scale_log2;
+    int num_ctas;
+};
+size_t paged_workspace_bytes(int device, int batch, int kv_heads, int rows_max, int head_dim);
+cudaError_t paged_attn_launch(PagedAttnParams &p, int head_dim, void *workspace,
+                              cudaStream_t stream);
+
+struct SampleArgs {
+    const void *logits;
+    bool bf16;
+    int B, W, vocab;
+    long long row_stride;
+    das_sampling sampling;
+    const float *uniforms;
+    int32_t *tokens;
+    float *logprobs;
+};
+cudaError_t sample_launch(const SampleArgs &a, cudaStream_t stream);
+// the acceptance that follows sample_launch: from tokens (= target_ids) and draft ids
+cudaError_t sample_accept_launch(const SampleArgs &a, const int32_t *draft, int32_t *accepted,
+                                 int32_t *next_token, int32_t *committed, cudaStream_t stream);
 
 }  // namespace das

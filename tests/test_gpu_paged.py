@@ -1,0 +1,395 @@
+"""Page assignment, the commit into the paged block-scaled cache and attention
+over it, against plain references in 64 bits (tests/paged_ref.py)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_34538_gb300 as das
+from tests import paged_ref as ref
+from tests.gpu_util import assert_close, dev_i32
+
+pytestmark = pytest.mark.gpu
+PAGE = 64
+
+
+def bf16(x):
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).to(torch.bfloat16).cuda()
+
+
+def f64(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+# ---- page assignment --------------------------------------------------------------
+
+def random_pool(rng, B, rows, spare, max_len):
+    """Lengths, a table and a free stack over disjoint pages; unused entries are garbage."""
+    seq = rng.integers(0, min(max_len, rows * PAGE) + 1, B)
+    have = -(-seq // PAGE)
+    pages = int(have.sum()) + spare
+    ids = rng.permutation(max(pages, 1))
+    table = rng.integers(-5, 1 << 30, (B, rows))
+    at = 0
+    for b in range(B):
+        table[b, :have[b]] = ids[at:at + have[b]]
+        at += have[b]
+    free = np.full(max(pages, 1), -7)
+    free[:spare] = ids[at:at + spare]
+    return seq, table, free, spare
+
+
+def check_assign(seq, grow, table, free, count, max_slots, in_place=False):
+    want = ref.page_assign(seq, grow, table, free, count, max_slots)
+    d = [dev_i32(x) for x in (seq, grow, table, free, [count])]
+    slots = torch.full((max_slots,), 12345, dtype=torch.int32, device="cuda")
+    flag = dev_i32([0])
+    out = dict(new_len=d[0], new_free_count=d[4]) if in_place else {}
+    for _ in range(1 if in_place else 2):   # with outputs apart the call can be repeated
+        n, c, start = das.das_page_assign(d[0], d[1], d[2], d[3], d[4], slots, flag, **out)
+    new_len, t, stack, cnt, sl, st, fl = want
+    assert n.tolist() == new_len and c.tolist() == [cnt] and start.tolist() == st
+    assert slots.tolist() == [int(x) for x in sl] + [-1] * (max_slots - len(sl))
+    assert d[2].cpu().numpy().tolist() == t.tolist()
+    assert d[3][:cnt].tolist() == [int(x) for x in stack]
+    assert flag.item() == fl
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("B,rows,spare,max_len,max_grow,max_slots", [
+    (1, 1, 1, 0, 64, 64), (1, 3, 0, 130, 2, 2), (3, 4, 2, 200, 80, 400), (16, 40, 20, 2000, 17, 300),
+    (40, 9, 30, 500, 300, 3000), (300, 3, 5, 192, 40, 2000), (1500, 4, 700, 256, 90, 40000),
+    (2050, 2, 2000, 128, 128, 65), (7, 100, 650, 0, 6400, 20000)])
+def test_assign_matches_one_request_after_the_other(B, rows, spare, max_len, max_grow, max_slots, in_place):
+    rng = np.random.default_rng(B * 7 + rows)
+    seq, table, free, count = random_pool(rng, B, rows, spare, max_len)
+    grow = rng.integers(-max_grow, max_grow + 1, B)
+    grow[rng.random(B) < 0.15] = -(1 << 30)
+    check_assign(seq, grow, table, free, count, max_slots, in_place)
+
+
+def test_assign_no_request_and_no_growth():
+    check_assign(np.zeros(0, int), np.zeros(0, int), np.zeros((0, 1), int), np.array([4, 3]), 2, 5)
+    check_assign(np.array([64, 0, 1]), np.zeros(3, int), np.array([[0], [9], [1]]), np.array([2, 0]), 1, 0)
+
+
+def test_assign_flags_values_out_of_range():
+    table, free, flag = dev_i32([[0, 1], [2, 3]]), dev_i32([4, 5]), dev_i32([0])
+    slots = dev_i32([0] * 8)
+    n, c, start = das.das_page_assign(dev_i32([-5, 10 ** 9]), dev_i32([3, 1]), table, free, dev_i32([99]), slots, flag)
+    # -5 counts as 0 tokens, 1e9 as the row's 128 (no room for another), 99 free pages as the pool's 2;
+    # page 5 is none of those 2, so its tokens get no place
+    assert n.tolist() == [3, 128] and c.tolist() == [1] and start.tolist() == [0, 3, 3]
+    assert slots.tolist() == [-1] * 8
+    assert flag.item() == 3
+    flag.zero_()
+    n, c, start = das.das_page_assign(dev_i32([-5, 10 ** 9]), dev_i32([3, 0]), table, dev_i32([1, 0]), dev_i32([99]),
+                                      slots, flag)
+    assert n.tolist() == [3, 128] and c.tolist() == [1] and start.tolist() == [0, 3, 3]
+    assert slots.tolist() == [0, 1, 2] + [-1] * 5 and flag.item() == 2
+
+
+# ---- commit -----------------------------------------------------------------------
+
+def append_case(rng, R, L, H, D, first, n, W, N, amp=lambda b, t: 1.0):
+    codes = rng.integers(0, 127, (R, L, N, H, PAGE, D)).astype(np.uint8)
+    scales = 2.0 ** rng.integers(-12, 3, (R, L, N, H))
+    B = len(n)
+    x = rng.normal(0, 1, (R, L, B, W, H, D))
+    for b in range(B):
+        for t in range(W):
+            x[:, :, b, t] *= amp(b, t)
+    ids, slots, start = list(rng.permutation(N)), [], [0]
+    for b in range(B):
+        pg = [ids.pop() for _ in range(-(-(first[b] + n[b]) // PAGE))]
+        slots += [pg[(first[b] + j) // PAGE] * PAGE + (first[b] + j) % PAGE for j in range(n[b])]
+        start.append(len(slots))
+    return codes, scales, x, slots, start
+
+
+def run_append(codes, scales, x, slots, start, flag=None, repeat=1):
+    dev = lambda a, dt: torch.from_numpy(np.ascontiguousarray(a)).to(dt).cuda()
+    cache = das.PagedKVCache(dev(codes, torch.uint8), dev(codes[..., ::-1], torch.uint8),
+                             dev(scales, torch.float32), dev(2 * scales, torch.float32))
+    flag = dev_i32([0]) if flag is None else flag
+    k, v = bf16(x), bf16(-3 * x)
+    for _ in range(repeat):
+        das.das_kv_append_paged(cache, k, v, dev_i32(slots if len(slots) else [0]), dev_i32(start), flag)
+    return cache, f64(k), f64(v), flag
+
+
+def same_codes(got, want):
+    """Equal codes; a NaN may carry either sign."""
+    got = got.cpu().numpy()
+    nan = (want & 127) == 127
+    return np.array_equal(got[~nan], want[~nan]) and np.all((got[nan] & 127) == 127)
+
+
+@pytest.mark.parametrize("repeat", [1, 2])
+@pytest.mark.parametrize("R,L,H,D,first,n,W", [
+    (1, 1, 1, 64, [0], [1], 1), (2, 2, 3, 64, [5], [16], 16), (3, 1, 2, 128, [63, 0, 32], [1, 64, 33], 64),
+    (1, 2, 8, 128, [10, 62], [200, 3], 201), (2, 1, 1, 128, [1, 0, 7], [0, 5, 0], 9), (1, 1, 5, 64, [33], [95], 95)])
+def test_append_codes_and_scales(R, L, H, D, first, n, W, repeat):
+    rng = np.random.default_rng(D + W + H)
+    # later tokens of a sequence are larger, so that scales of started pages have to grow for some
+    case = append_case(rng, R, L, H, D, first, n, W, 12, amp=lambda b, t: 2.0 ** (-6 + 9 * ((b + t) % 3)))
+    codes, scales, x, slots, start = case
+    cache, k, v, flag = run_append(*case, repeat=repeat)
+    wk, wks = ref.append(codes, scales, k, slots, start)
+    wv, wvs = ref.append(codes[..., ::-1], 2 * scales, v, slots, start)
+    assert same_codes(cache.k, wk) and same_codes(cache.v, wv)
+    assert np.array_equal(cache.k_scale.cpu().numpy(), wks) and np.array_equal(cache.v_scale.cpu().numpy(), wvs)
+    assert flag.item() == 0
+
+
+def test_append_extreme_values():
+    rng = np.random.default_rng(3)
+    codes, scales, x, slots, start = append_case(rng, 1, 1, 7, 64, [9], [20], 20, 2)
+    x[..., 0, :] *= 0.0                                   # all zero: the least scale
+    x[..., 1, :] *= 2.0 ** 100
+    x[..., 2, :] *= 2.0 ** -60
+    x[..., 3, 5] = np.inf
+    x[..., 4, 6] = np.nan
+    x[..., 5, :] = 448.0                                   # a scale of exactly 1
+    x[..., 6, :] = np.sign(x[..., 6, :]) * np.inf
+    scales[:, :, :, 2] = 2.0 ** -41                        # held scales below the least
+    cache, k, v, flag = run_append(codes, scales, x, slots, start)
+    wk, wks = ref.append(codes, scales, k, slots, start)
+    assert same_codes(cache.k, wk) and np.array_equal(cache.k_scale.cpu().numpy(), wks)
+    assert flag.item() == 0
+
+
+def test_append_held_scales_that_are_no_powers_of_two():
+    rng = np.random.default_rng(4)
+    codes, scales, x, slots, start = append_case(rng, 1, 1, 4, 128, [30], [10], 10, 2)
+    scales = np.float32(scales * rng.uniform(1, 2, scales.shape)).astype(np.float64)
+    cache, k, _, _ = run_append(codes, scales, x, slots, start)
+    wk, wks = ref.append(codes, scales, k, slots, start)
+    assert np.array_equal(cache.k_scale.cpu().numpy().astype(np.float64), wks)
+    # binary32 quotients differ from exact ones by 2^-24: only an exact half-way case could round apart
+    assert (cache.k.cpu().numpy() != wk).mean() < 1e-3
+
+
+def test_append_leaves_what_it_refuses():
+    rng = np.random.default_rng(5)
+    codes, scales, x, slots, start = append_case(rng, 1, 1, 2, 64, [60, 0, 0, 0], [8, 4, 4, 4], 8, 8)
+    slots = list(slots)
+    slots[start[0] + 4] += 1                               # a second page that does not start at its first place
+    slots[start[1]:start[2]] = [-1] * 4                    # no place
+    slots[start[2]:start[3]] = [8 * PAGE + i for i in range(4)]  # a page past the pool
+    cache, k, _, flag = run_append(codes, scales, x, slots, start)
+    wk, wks = ref.append(codes, scales, k[:, :, :1], slots[:4], [0, 4])
+    last = start[3]
+    wk, wks = ref.append(wk, wks, k[:, :, 3:], slots[last:], [0, 4])
+    assert flag.item() == 2
+    assert same_codes(cache.k, wk) and np.array_equal(cache.k_scale.cpu().numpy(), wks)
+    # counts past W, and starts past the slots, write nothing
+    for bad in ([0, 9, 9, 9, 9], [0, 0, 0, 0, 999], [4, 2, 2, 2, 2], [-3, -1, 0, 0, 0]):
+        cache, k, _, flag = run_append(codes, scales, x, slots, bad)
+        assert flag.item() == 2 and same_codes(cache.k, codes)
+
+
+# ---- attention --------------------------------------------------------------------
+
+def attention_case(rng, D, Hq, Hkv, Tm, P, T, rows=None, amp=1.0, poison=True):
+    """A two-depth cache: keys read at depth 1, values at depth 2; what no call may use is NaN."""
+    B = len(P)
+    need = [-(-p // PAGE) for p in P]
+    rows = max(1, max(need)) if rows is None else rows
+    N = sum(need) + 2
+    ids = rng.permutation(N)
+    table = np.full((B, rows), -1)
+    shape = (N, Hkv, PAGE, D)
+    kc, vc = ref.to_e4m3(rng.normal(0, 60, shape)), ref.to_e4m3(rng.normal(0, 60, shape))
+    ks, vs = (2.0 ** rng.integers(-8, -4, (N, Hkv)) for _ in range(2))
+    ks = ks * amp
+    at = 0
+    used = np.zeros((N, PAGE), bool)
+    for b in range(B):
+        table[b, :need[b]] = ids[at:at + need[b]]
+        for t in range(need[b]):
+            used[table[b, t], :min(PAGE, P[b] - t * PAGE)] = True
+        at += need[b]
+    if poison:
+        for c in (kc, vc):
+            c[np.broadcast_to(~used[:, None, :, None], shape)] = 0x7F
+        ks[~used.any(1)] = np.nan
+        vs[~used.any(1)] = np.nan
+    f = lambda *s: rng.normal(0, 1, s)
+    q, kb, vb = f(B, Tm, Hq, D), f(B, Tm, Hkv, D), f(B, Tm, Hkv, D)
+    if poison:
+        for b in range(B):
+            q[b, T[b]:], kb[b, T[b]:], vb[b, T[b]:] = np.nan, np.nan, np.nan
+    return kc, ks, vc, vs, table, np.array(P), np.array(T), q, kb, vb
+
+
+def run_attention(kc, ks, vc, vs, table, P, T, q, kb, vb, scale=0.0, stream=None, status=0, masked=(), where=""):
+    other = np.full_like(kc, 0x7F)                          # the depths that are not read: NaN
+    dev = lambda a, dt: torch.from_numpy(np.ascontiguousarray(a)).to(dt).cuda()
+    cache = das.PagedKVCache(dev(np.stack([kc, other])[:, None], torch.uint8),
+                             dev(np.stack([other, vc])[:, None], torch.uint8),
+                             dev(np.stack([ks, ks * np.nan])[:, None], torch.float32),
+                             dev(np.stack([vs * np.nan, vs])[:, None], torch.float32))
+    B, Tm, Hq, D = q.shape
+    ws = das.new_workspace_paged(cache, B, Hq, Tm)
+    qd, kbd, vbd = bf16(q), bf16(kb), bf16(vb)
+    torch.cuda.synchronize()
+    out, lse = das.das_mature_v_attention_paged(cache, 0, 1, 2, dev_i32(table), dev_i32(P), dev_i32(T), qd, kbd, vbd,
+                                                ws, softmax_scale=scale, stream=stream)
+    torch.cuda.synchronize()
+    assert das.workspace_status(ws) == status
+    Pc, Tc = np.clip(P, 0, table.shape[1] * PAGE), np.clip(T, 0, Tm)
+    o, l = ref.attention(kc, np.float32(ks), vc, np.float32(vs), table, Pc, Tc, f64(qd), f64(kbd), f64(vbd),
+                         scale=scale or None, masked=masked)
+    assert_close(f64(out), o, lse.cpu().numpy(), l, where=where)
+    for b in range(B):
+        assert not out[b, Tc[b]:].any() and torch.isneginf(lse[b, :, Tc[b]:]).all()
+    return out, lse
+
+
+SHAPES = [  # D, Hq, Hkv, max_block, prefix lengths, block lengths
+    (64, 4, 4, 4, [256], [4]), (64, 1, 1, 1, [0], [1]), (64, 1, 1, 1, [1], [1]), (128, 1, 1, 1, [63], [1]),
+    (128, 2, 2, 1, [64, 65], [1, 1]), (128, 8, 2, 16, [127, 0, 128], [16, 3, 0]), (128, 5, 1, 12, [1000], [11]),
+    (64, 10, 2, 12, [129, 700], [12, 1]), (128, 32, 8, 8, [300, 64, 1, 449], [8, 7, 1, 0]),
+    (128, 1, 1, 64, [190], [64]), (64, 8, 1, 8, [4097], [8]), (128, 32, 32, 1, [513], [1]),
+    (128, 4, 4, 16, [2000, 5], [16, 16]), (128, 6, 2, 9, [320] * 5, [9, 8, 7, 6, 5]),
+    (128, 4, 2, 16, [0] * 40, list(range(16)) * 2 + [16] * 8), (64, 2, 1, 32, list(range(0, 99, 3)), [32] * 33),
+    (128, 16, 4, 4, [640, 64, 1], [4, 4, 4]), (128, 3, 1, 21, [777], [20]), (64, 64, 1, 1, [130, 3], [1, 0])]
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=[str(s)[:60] for s in SHAPES])
+def test_attention_matches_64_bits(shape):
+    D, Hq, Hkv, Tm, P, T = shape
+    rng = np.random.default_rng(D + Hq + Tm + len(P))
+    run_attention(*attention_case(rng, D, Hq, Hkv, Tm, P, T), where=str(shape)[:60])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Tm", [1, 7, 16])
+def test_attention_sharp_and_rising_scores(D, Tm):
+    """Maxima that keep moving along the prefix, weights of one key near 1."""
+    rng = np.random.default_rng(D + Tm)
+    c = list(attention_case(rng, D, 4, 2, Tm, [1500, 700], [Tm, max(1, Tm - 1)]))
+    for b in range(2):                                      # scores grow page by page
+        for t in range(-(-int(c[5][b]) // PAGE)):
+            c[1][c[4][b, t]] = 2.0 ** (-9 + min(t, 6))
+    run_attention(*c, scale=0.5, where="rising")
+    c[1] = np.where(np.isnan(c[1]), c[1], 2.0 ** -6)
+    run_attention(*c, scale=1.0, where="sharp")
+
+
+def test_attention_scales_far_apart():
+    """Value scales from 2^-40 to 2^30 in one sequence, scales that are no powers of two, zero pages."""
+    rng = np.random.default_rng(8)
+    c = list(attention_case(rng, 128, 4, 1, 8, [64 * 12 + 5], [8]))
+    pages = c[4][0]
+    c[3][pages, 0] = np.float32([1.0, 2.0 ** -40, 3.7e-3, 2.0 ** -20, 0.9, 1.1, 1e-6, 0.37, 0.01, 0.5, 2.0 ** -40, 0.3,
+                                 0.77])
+    c[1][pages, 0] = np.float32([2.0 ** -40, 0.011, 2.0 ** -8, 0.013, 1e-4, 2.0 ** -6, 0.02] + [0.015] * 6)
+    c[2][pages[10], 0] = 0
+    run_attention(*c, where="scales")
+    big = list(c)
+    big[3] = c[3] * 2.0 ** -3
+    run_attention(*big, where="scales / 8")
+
+
+def test_attention_only_small_values():
+    """A sequence whose every page has the least scale."""
+    rng = np.random.default_rng(9)
+    c = list(attention_case(rng, 64, 2, 2, 2, [100, 64], [0, 2]))
+    c[3] = np.where(np.isnan(c[3]), c[3], 2.0 ** -40)
+    c[9] = c[9] * 2.0 ** -36
+    run_attention(*c, where="small values")
+
+
+def test_attention_entries_that_are_no_pages_are_masked_and_flagged():
+    rng = np.random.default_rng(10)
+    c = list(attention_case(rng, 128, 4, 2, 4, [300, 200], [4, 4]))
+    c[4] = c[4].copy()
+    c[4][0, 2], c[4][1, 0] = -1, 10 ** 9
+    run_attention(*c, status=4, masked={(0, 2), (1, 0)}, where="bad pages")
+
+
+def test_attention_clamps_and_flags_lengths():
+    rng = np.random.default_rng(11)
+    c = list(attention_case(rng, 64, 2, 1, 4, [128, 64], [4, 4], rows=2, poison=False))
+    c[5], c[6] = np.array([10 ** 9, -3]), np.array([9, -1])
+    run_attention(*c, status=2, where="lengths")
+
+
+def test_attention_on_another_stream_and_twice():
+    rng = np.random.default_rng(12)
+    c = attention_case(rng, 128, 8, 2, 8, [500, 70], [8, 5])
+    a = run_attention(*c, stream=torch.cuda.Stream())
+    b = run_attention(*c)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_attention_offsets_past_32_bits():
+    """Pages whose codes lie more than 4 GiB into the cache."""
+    rng = np.random.default_rng(13)
+    D, H, P = 128, 8, 200
+    pages = (5 << 30) // (H * PAGE * D)
+    codes = torch.zeros((1, 1, pages, H, PAGE, D), dtype=torch.uint8, device="cuda")
+    scales = torch.ones((1, 1, pages, H), device="cuda")
+    ids = [pages - 1, 3, pages - 7, pages // 2 + 1]
+    part = ref.to_e4m3(rng.normal(0, 60, (4, H, PAGE, D)))
+    codes[0, 0, ids] = torch.from_numpy(part).cuda()
+    scales[0, 0, ids] = 2.0 ** -6
+    cache = das.PagedKVCache(codes, codes, scales, scales)
+    ws = das.new_workspace_paged(cache, 1, H, 4)
+    q, kb, vb = (bf16(rng.normal(0, 1, (1, 4, H, D))) for _ in range(3))
+    out, lse = das.das_mature_v_attention_paged(cache, 0, 1, 1, dev_i32([ids]), dev_i32([P]), dev_i32([4]), q, kb, vb, ws)
+    s = np.full((4, H), 2.0 ** -6)
+    o, l = ref.attention(part, s, part, s, np.array([[0, 1, 2, 3]]), [P], [4], f64(q), f64(kb), f64(vb))
+    assert_close(f64(out), o, lse.cpu().numpy(), l, where="far pages")
+    # the commit reaches them too (keys and values are one tensor here, so both get the same tokens)
+    flag = dev_i32([0])
+    das.das_kv_append_paged(cache, vb[None, None], vb[None, None], dev_i32([ids[0] * PAGE + i for i in range(4)]),
+                            dev_i32([0, 4]), flag)
+    got = ref.TABLE[codes[0, 0, ids[0], :, :4].cpu().numpy()] * scales[0, 0, ids[0]].cpu().numpy()[:, None, None]
+    assert flag.item() == 0 and np.abs(got - f64(vb)[0].transpose(1, 0, 2)).max() <= 4 * 2.0 ** -4
+
+
+# ---- together ---------------------------------------------------------------------
+
+def test_assign_append_attend():
+    """Prompts and steps of ragged requests; one ends and its pages serve another."""
+    rng = np.random.default_rng(14)
+    D, H, Hq, B, N, rows, R = 64, 2, 4, 3, 16, 6, 2
+    cache = das.PagedKVCache.empty(R, 1, N, H, D)
+    cache.k.fill_(0x7F)
+    cache.v.fill_(0x7F)
+    table, free, count = dev_i32(np.full((B, rows), -1)), dev_i32(rng.permutation(N)), dev_i32([N])
+    length, flag = dev_i32([0] * B), dev_i32([0])
+    ws = das.new_workspace_paged(cache, B, Hq, 4)
+    kept = [np.zeros((R, 2, 0, H, D)) for _ in range(B)]
+    for grow in ([130, 64, 1], [1, 3, 16], [-500, 2, 60], [200, 1, -20], [5, 1, 1]):
+        W = max(1, max(grow))
+        slots = torch.empty(max(1, sum(max(g, 0) for g in grow)), dtype=torch.int32, device="cuda")
+        _, _, start = das.das_page_assign(length, dev_i32(grow), table, free, count, slots, flag, new_len=length,
+                                          new_free_count=count)
+        kn, vn = (bf16(rng.normal(0, 1 + abs(grow[1]), (R, 1, B, W, H, D))) for _ in range(2))
+        das.das_kv_append_paged(cache, kn, vn, slots, start, flag)
+        for b, g in enumerate(grow):
+            new = np.stack([f64(kn)[:, 0, b], f64(vn)[:, 0, b]], 1)[:, :, :max(g, 0)]
+            kept[b] = np.concatenate([kept[b][:, :, :max(0, kept[b].shape[2] + min(g, 0))], new], 2)
+        assert length.tolist() == [x.shape[2] for x in kept] and flag.item() == 0
+        tb, P = table.cpu().numpy(), length.tolist()
+        k, v, ks, vs = (t.cpu().numpy() for t in (cache.k, cache.v, cache.k_scale, cache.v_scale))
+        for b in range(B):      # stored values: within an e4m3 rounding of the page's largest scale
+            for t in range(P[b]):
+                pg = tb[b, t // PAGE]
+                for which, (c, s) in enumerate(((k, ks), (v, vs))):
+                    x = kept[b][:, which, t]
+                    got = ref.TABLE[c[:, 0, pg, :, t % PAGE]] * s[:, 0, pg][..., None]
+                    # one rounding to 4 bits, and one more for a code that a grown scale made subnormal
+                    assert np.all(np.abs(got - x) <= np.abs(x) / 16 + s[:, 0, pg][..., None] * 2.0 ** -9)
+        q, kb, vb = bf16(rng.normal(0, 1, (B, 4, Hq, D))), *(bf16(rng.normal(0, 1, (B, 4, H, D))) for _ in range(2))
+        T = [4, 1, 2]
+        out, lse = das.das_mature_v_attention_paged(cache, 0, 1, 2, table, length, dev_i32(T), q, kb, vb, ws)
+        o, l = ref.attention(k[0, 0], ks[0, 0], v[1, 0], vs[1, 0], tb, P, T, f64(q), f64(kb), f64(vb))
+        # values grow with the step: compare relative to the largest
+        assert np.abs(f64(out) - o).max() <= 2.0 ** -7 * max(1.0, np.abs(o).max())
+        fin = np.isfinite(l)
+        assert np.abs(lse.cpu().numpy()[fin] - l[fin]).max() <= 1e-5 * max(10.0, np.abs(l[fin]).max())
+    assert das.workspace_status(ws) == 0

@@ -1,0 +1,82 @@
+"""What the paged-cache and sampling calls refuse on the host, without a GPU: status codes of the C
+ABI (addresses are never used, since the checks fail first) and exceptions of the binding."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2609_34538_gb300 as das
+
+L, A = das.LIB, ctypes.c_void_p(256)
+NULL = ctypes.c_void_p(0)
+BAD, UNSUPPORTED = das.DAS_ERR_INVALID_ARG, das.DAS_ERR_UNSUPPORTED
+
+
+def cache(k=256, v=256, ks=256, vs=256, depths=2, layers=1, pages=4, heads=2, dim=64):
+    return ctypes.byref(das.das_kv_cache_paged(k, v, ks, vs, depths, layers, pages, heads, dim))
+
+
+@pytest.mark.parametrize("change", [dict(batch=-1), dict(max_pages=0), dict(max_pages=1 << 25), dict(pages=0),
+                                    dict(pages=1 << 25), dict(max_slots=-1), dict(slots=NULL), dict(count=NULL),
+                                    dict(seq=NULL), dict(table=NULL), dict(flag=NULL)])
+def test_page_assign_refusals(change):
+    a = dict(batch=2, max_pages=4, pages=8, max_slots=16, slots=A, count=A, seq=A, table=A, flag=A) | change
+    assert L.das_page_assign(a["seq"], A, a["batch"], a["table"], a["max_pages"], A, a["pages"], a["count"], a["slots"],
+                             a["max_slots"], A, A, A, a["flag"], NULL) == BAD
+
+
+@pytest.mark.parametrize("change,code", [(dict(dim=96), UNSUPPORTED), (dict(k=0), BAD), (dict(v=8), BAD),
+                                         (dict(ks=0), BAD), (dict(depths=0), BAD), (dict(depths=64), BAD),
+                                         (dict(pages=0), BAD), (dict(pages=1 << 25), BAD), (dict(heads=0), BAD)])
+def test_cache_refusals(change, code):
+    c = cache(**change)
+    assert L.das_kv_append_paged(c, A, A, 1, 4, A, 4, A, A, NULL) == code
+    assert L.das_mature_v_attention_paged(c, 0, 1, 1, A, 4, A, A, 1, 1, A, A, A, 2, 0.0, A, A, A, 1 << 30, NULL) == code
+
+
+def test_append_refusals():
+    call = lambda c=cache(), k=A, batch=1, W=4, slots=A, n=4, start=A, flag=A: L.das_kv_append_paged(
+        c, k, A, batch, W, slots, n, start, flag, NULL)
+    assert call(c=None) == BAD and call(k=NULL) == BAD and call(k=ctypes.c_void_p(8)) == BAD
+    assert call(batch=-1) == BAD and call(W=0) == BAD and call(slots=NULL) == BAD and call(n=-1) == BAD
+    assert call(start=NULL) == BAD and call(flag=NULL) == BAD
+    assert call(W=1 << 25) == UNSUPPORTED and call(c=cache(depths=63, layers=4096, heads=128), batch=1 << 10) == UNSUPPORTED
+
+
+def test_attention_refusals():
+    def call(layer=0, kd=1, vd=1, rows=4, batch=1, T=1, Hq=2, q=A, scale=0.0, table=A):
+        return L.das_mature_v_attention_paged(cache(), layer, kd, vd, table, rows, A, A, batch, T, q, A, A, Hq, scale, A,
+                                              A, A, 1 << 30, NULL)
+    assert call(layer=1) == BAD and call(layer=-1) == BAD and call(kd=0) == BAD and call(vd=3) == BAD
+    assert call(rows=0) == BAD and call(batch=0) == BAD and call(T=0) == BAD and call(Hq=3) == BAD and call(Hq=0) == BAD
+    assert call(q=ctypes.c_void_p(264)) == BAD and call(scale=float("nan")) == BAD and call(table=NULL) == BAD
+    assert call(T=65) == UNSUPPORTED and call(T=33, Hq=4) == UNSUPPORTED and call(batch=(1 << 20) + 1) == UNSUPPORTED
+    size = L.das_workspace_size_paged
+    assert size(None, 1, 2, 1) == 0 and size(cache(dim=32), 1, 2, 1) == 0 and size(cache(), 0, 2, 1) == 0
+    assert size(cache(), 1, 3, 1) == 0 and size(cache(), 1, 2, 65) == 0
+
+
+def test_sample_refusals():
+    def call(logits=A, kind=0, B=1, W=1, V=10, stride=10, u=A, out=A):
+        return L.das_sample(logits, kind, B, W, V, stride, None, u, out, NULL, NULL)
+    assert call(logits=NULL) == BAD and call(kind=2) == BAD and call(B=-1) == BAD and call(W=0) == BAD
+    assert call(W=1025) == BAD and call(V=0) == BAD and call(stride=9) == BAD and call(u=NULL) == BAD
+    assert call(out=NULL) == BAD and call(logits=ctypes.c_void_p(258)) == BAD
+    assert call(logits=ctypes.c_void_p(257), kind=1) == BAD
+    accept = lambda draft=A, acc=A, nxt=A: L.das_sample_accept(A, 0, draft, 1, 1, 10, 10, None, A, acc, A, nxt, NULL, NULL,
+                                                               NULL)
+    assert accept(draft=NULL) == BAD and accept(acc=NULL) == BAD and accept(nxt=NULL) == BAD
+
+
+def test_binding_refuses_host_tensors_and_wrong_types():
+    i32, f32 = torch.zeros(2, dtype=torch.int32), torch.zeros((2, 2, 8))
+    with pytest.raises(ValueError, match="CUDA"):
+        das.das_page_assign(i32, i32, i32.view(2, 1), i32, i32[:1], i32, i32[:1])
+    with pytest.raises(TypeError, match="int32"):
+        das.das_page_assign(f32, i32, i32.view(2, 1), i32, i32[:1], i32, i32[:1])
+    with pytest.raises(ValueError, match="CUDA"):
+        das.das_sample(f32, f32[..., 0])
+    with pytest.raises(TypeError, match="float32 or bfloat16"):
+        das.das_sample(f32.double(), f32[..., 0])
+    with pytest.raises(TypeError, match="uint8"):
+        das.PagedKVCache(f32, f32, f32, f32)
