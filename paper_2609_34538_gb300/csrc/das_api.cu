@@ -31,8 +31,8 @@ bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 
 // Tensor map over `rank` dims (innermost first): bf16 elements with 128-byte
 // swizzle, or 8-bit (e4m3) elements without swizzle (their tiles are widened
-// by the kernel, which reads them row by row) or, with swizzle8, with 128-byte
-// swizzle (key tiles of 128-byte rows that the e4m3 MMAs read as they land).
+// by the kernel, which reads them row by row) or, with swizzle8, swizzled by
+// their row's 128 or 64 bytes (tiles that the e4m3 MMAs read as they land).
 bool encode_uncached(CUtensorMap *m, void *base, int rank, const cuuint64_t *dims,
                      const cuuint32_t *box, bool e4m3, bool swizzle8) {
     EncodeTiledFn fn = encode_fn();
@@ -53,7 +53,10 @@ bool encode_uncached(CUtensorMap *m, void *base, int rank, const cuuint64_t *dim
                                                             : CU_TENSOR_MAP_L2_PROMOTION_L2_64B;
     return fn(m, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
               (cuuint32_t)rank, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              e4m3 && !swizzle8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, promo,
+              e4m3 && !swizzle8 ? CU_TENSOR_MAP_SWIZZLE_NONE
+              : row_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                                : CU_TENSOR_MAP_SWIZZLE_128B,
+              promo,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -306,7 +309,8 @@ das_status attention_paged(const das_kv_cache_paged *c, int layer, int key_depth
         return DAS_ERR_INVALID_ARG;
     const int G = num_q_heads / c->kv_heads;
     if (max_block > kTileKeys || (long long)G * max_block > kMaxRows || batch > (1 << 20) ||
-        (long long)batch * c->kv_heads * G * max_block > 0x7fffffffLL)
+        (long long)batch * c->kv_heads * G * max_block > 0x7fffffffLL ||
+        (long long)c->pages * c->kv_heads > 0x7fffffffLL)
         return DAS_ERR_UNSUPPORTED;
     const size_t need = das_workspace_size_paged(c, batch, num_q_heads, max_block);
     if (need == 0) return DAS_ERR_CUDA;
@@ -318,8 +322,13 @@ das_status attention_paged(const das_kv_cache_paged *c, int layer, int key_depth
     const size_t ks = (size_t)(key_depth - 1) * c->layers + layer;
     const size_t vs = (size_t)(value_depth - 1) * c->layers + layer;
     PagedAttnParams p = {};
-    p.k = static_cast<const uint8_t *>(c->k) + ks * slab_bytes;
-    p.v = static_cast<const uint8_t *>(c->v) + vs * slab_bytes;
+    // a tile is one box of 64 rows of D bytes
+    const cuuint64_t dims[3] = {(cuuint64_t)c->head_dim, DAS_PAGE_TOKENS, (cuuint64_t)slab_tiles};
+    const cuuint32_t box[3] = {(cuuint32_t)c->head_dim, DAS_PAGE_TOKENS, 1};
+    CUtensorMap tm_k, tm_v;
+    if (!encode(&tm_k, static_cast<uint8_t *>(c->k) + ks * slab_bytes, 3, dims, box, true, true) ||
+        !encode(&tm_v, static_cast<uint8_t *>(c->v) + vs * slab_bytes, 3, dims, box, true, true))
+        return DAS_ERR_CUDA;
     p.k_scale = c->k_scale + ks * slab_tiles;
     p.v_scale = c->v_scale + vs * slab_tiles;
     p.table = block_table;
@@ -341,8 +350,8 @@ das_status attention_paged(const das_kv_cache_paged *c, int layer, int key_depth
     const double scale =
         softmax_scale > 0.f ? (double)softmax_scale : 1.0 / sqrt((double)c->head_dim);
     p.scale_log2 = (float)(scale * 1.4426950408889634);
-    return paged_attn_launch(p, c->head_dim, workspace, static_cast<cudaStream_t>(stream)) ==
-                   cudaSuccess
+    return paged_attn_launch(p, c->head_dim, tm_k, tm_v, workspace,
+                             static_cast<cudaStream_t>(stream)) == cudaSuccess
                ? DAS_OK
                : DAS_ERR_CUDA;
 }

@@ -103,7 +103,6 @@ cudaError_t append_paged_launch(const das_kv_cache_paged &c, const void *k_new, 
                                 cudaStream_t stream);
 
 struct PagedAttnParams {
-    const uint8_t *k, *v;                 // the slabs read: e4m3 [pages][Hkv][64][D]
     const float *k_scale, *v_scale;       // [pages][Hkv]
     const int32_t *table;                 // [B][max_pages]
     const int32_t *prefix_len, *block_len;
@@ -117,8 +116,10 @@ struct PagedAttnParams {
     int num_ctas;
 };
 size_t paged_workspace_bytes(int device, int batch, int kv_heads, int rows_max, int head_dim);
-cudaError_t paged_attn_launch(PagedAttnParams &p, int head_dim, void *workspace,
-                              cudaStream_t stream);
+// tm_k / tm_v map the slabs read, e4m3 [pages * Hkv][64][D], with a {D, 64, 1}
+// box and D-byte swizzle; carves the workspace into p's status and partials.
+cudaError_t paged_attn_launch(PagedAttnParams &p, int head_dim, const CUtensorMap &tm_k,
+                              const CUtensorMap &tm_v, void *workspace, cudaStream_t stream);
 
 struct SampleArgs {
     const void *logits;

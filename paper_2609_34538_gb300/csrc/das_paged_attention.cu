@@ -1,171 +1,970 @@
 // das_paged_attention.cu -- depth-asynchronous attention (Eqs. 2-3) over the
-// paged e4m3 cache with a scale per (page, kv head).
+// paged e4m3 cache with a scale per (page, kv head), on the 5th-generation
+// tensor cores of sm_103a with the codes as they are stored.
 //
-// Plain form: one CTA takes a range of the 64-key tiles of one (sequence, kv
-// head) pair (a tile is a page; the block's own keys are the last tile),
-// widens each tile to fp32 in shared memory and keeps the running maximum,
-// sum and output of every row in registers; merge_kernel combines the ranges.
+// The mathematics.  With s_j = scale ks(page) q . kc_j (base 2) and values
+// vs(page) vc_j, a running reference m over x_j = s_j + log2 vs and
+//     p_j = 2^(x_j - m + kHead),
+// O = sum_j p_j vc_j and l = sum_j p_j / vs give o = O / l and
+// lse = ln 2 (m - kHead + log2 l): a page's value scale is part of the weight
+// that its codes are multiplied with, so the products run on the codes alone.
+// m moves (O and l are rescaled) only when a tile's largest x exceeds it by
+// more than kWindow, so p < 2^(kHead + kWindow) = 256 fits e4m3.
+//
+// Both operands of an e4m3 product have 4 significant bits, which is too few
+// for queries and weights, so each is split into two rows of one M = 128
+// product (no second pass over the keys):
+//   queries  2^e q = hi + lo / 16, exact for elements down to about 2^-13 of
+//            the row's largest (a bf16 value has 8 significant bits); S = S_hi
+//            + S_lo / 16, added where the scores are read;
+//   weights  p = hi + lo / 16, off by at most 2^-9 of p (bf16 weights: 2^-8),
+//            finer than e4m3's least step alone by the factor 16; O = O_hi +
+//            O_lo / 16, added at the end of a segment.
+// Row r of the pair (r = i * G + g) has its hi part in TMEM lane
+// 32 (r / 16) + r % 16 and its lo part 16 lanes on, in the same warp's reach.
+//
+// Work split: every (sequence, kv head) pair owns one tile for each of its
+// ceil(P / 64) pages plus one for the block's own keys; all pairs' tiles are
+// one list, and CTA c of a persistent grid (one per SM) takes the c-th of C
+// equal ranges, cut into segments at pair boundaries.  A segment that is a
+// whole pair writes the output, others a partial (O / l, lse), which
+// paged_merge_kernel joins.
+//
+// One CTA = four softmax warps + one TMA warp + two MMA warps + four warps
+// that prepare each segment's queries (split) and block keys and values (bf16,
+// with rows past the block zero).  The block tile runs bf16 products: S with
+// M = 64 (the hi lanes), P V with P split into two bf16 parts.
+// Every wait is bounded (2 s); a time-out sets the status word and ends the
+// CTA's waits.  Tensor memory is freed before the CTA exits.
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "das_internal.h"
+#include "das_tcgen05.h"
 
 namespace das {
 namespace {
 
-constexpr int kThreads = 128;
+using namespace t5;
+
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kSoftWarps = 4;
+constexpr int kProducerWarp = 4;
+constexpr int kPvWarp = 5;
+constexpr int kSWarp = 6;
+constexpr int kQueryWarp0 = 7;
+constexpr int kQueryWarps = 4;
+constexpr int kThreads = (kQueryWarp0 + kQueryWarps) * 32;
+constexpr int kRows = 64;          // query rows per pair
+constexpr int kSBufs = 4;          // S buffers in tensor memory
+constexpr int kTmemCols = 512;     // S [0, 256), O [256, 256 + D), P 2 x 16 columns
+constexpr int kOCol = kSBufs * kTileKeys;
+constexpr int kPCol = 384;
+constexpr float kHead = 5.f, kWindow = 3.f;
+constexpr float kLoInv = 0.0625f;  // the lo rows hold 16 times the remainder
+constexpr uint32_t kLoLanes = 16u << 16;
 
-__device__ __forceinline__ float bf16(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
-__device__ __forceinline__ float e4m3(uint8_t x) {
-    uint32_t h;
-    asm("{\n .reg .b16 t;\n cvt.u16.u32 t, %1;\n cvt.rn.f16x2.e4m3x2 %0, t;\n}\n"
-        : "=r"(h)
-        : "r"((uint32_t)x));
-    float f;
-    asm("{\n .reg .b16 l, u;\n mov.b32 {l, u}, %1;\n cvt.f32.f16 %0, l;\n}\n" : "=f"(f) : "r"(h));
-    return f;
+// ---- tile list --------------------------------------------------------------------
+__device__ __forceinline__ int clamp_to(int v, int hi) { return v < 0 ? 0 : (v > hi ? hi : v); }
+__device__ __forceinline__ int prefix_of(const PagedAttnParams &p, int b) {
+    return clamp_to(__ldcg(p.prefix_len + b), p.max_pages * kTileKeys);
 }
-__device__ __forceinline__ int clamped(int v, int hi) { return v < 0 ? 0 : (v > hi ? hi : v); }
+__device__ __forceinline__ int block_of(const PagedAttnParams &p, int b) {
+    return clamp_to(__ldcg(p.block_len + b), p.max_block);
+}
+__device__ __forceinline__ int tiles_of(int P) { return (P + kTileKeys - 1) / kTileKeys + 1; }
 
-template <int D>
-__global__ void __launch_bounds__(kThreads) paged_attn_kernel(const PagedAttnParams p, int splits) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    extern __shared__ float sm[];
-    float *qs = sm, *kv = qs + 64 * (D + 1), *ps = kv + 64 * (D + 1);
-    const int s = blockIdx.x % splits, pair = blockIdx.x / splits;
-    const int b = pair / p.Hkv, h = pair % p.Hkv;
-    const int P = clamped(p.prefix_len[b], p.max_pages * 64), T = clamped(p.block_len[b], p.max_block);
-    if (s == 0 && threadIdx.x == 0 && (P != p.prefix_len[b] || T != p.block_len[b]))
-        atomicOr(p.status, kStatusClamped);
-    const int nt = (P + 63) / 64 + 1;
-    const int lo = (int)((long long)nt * s / splits), hi = (int)((long long)nt * (s + 1) / splits);
-    const int rows = p.G * T, row = threadIdx.x >> 1, half = threadIdx.x & 1;
-    const int irow = row / p.G;
-    for (int i = threadIdx.x; i < rows * D; i += kThreads) {
-        const int r = i / D, d = i % D;
-        qs[r * (D + 1) + d] = bf16(
-            p.q[(((size_t)b * p.max_block + r / p.G) * p.Hq + h * p.G + r % p.G) * D + d]);
+struct Walk {
+    int b, h, t, nt, P, T;
+};
+__device__ __forceinline__ void walk_load(const PagedAttnParams &p, Walk &w) {
+    if (w.b < p.B) {
+        w.P = prefix_of(p, w.b);
+        w.T = block_of(p, w.b);
+        w.nt = tiles_of(w.P);
     }
-    float m = -INFINITY, l = 0.f, acc[D / 2];
-    for (int d = 0; d < D / 2; ++d) acc[d] = 0.f;
-    for (int t = lo; t < hi; ++t) {
-        const bool blk = t == nt - 1;
-        int n = blk ? T : min(64, P - t * 64);
-        const int page = blk ? 0 : p.table[(size_t)b * p.max_pages + t];
-        if (page < 0 || page >= p.pages) {
-            if (threadIdx.x == 0) atomicOr(p.status, kStatusBadPage);
-            n = 0;
-        }
-        const size_t tile = n ? (size_t)page * p.Hkv + h : 0;
-        auto fill = [&](const uint8_t *codes, float scale, const uint16_t *own) {
-            __syncthreads();
-            for (int i = threadIdx.x; i < n * D; i += kThreads) {
-                const int j = i / D, d = i % D;
-                kv[j * (D + 1) + d] =
-                    blk ? bf16(own[(((size_t)b * p.max_block + j) * p.Hkv + h) * D + d])
-                        : e4m3(codes[tile * 64 * D + i]) * scale;
-            }
-            __syncthreads();
-        };
-        fill(p.k, p.k_scale[tile], p.k_blk);
-        const int lim = row < rows ? (blk ? min(n, irow + 1) : n) : 0;
-        float mt = m;
-        for (int j = half; j < lim; j += 2) {
-            float x = 0.f;
-            for (int d = 0; d < D; ++d) x += qs[row * (D + 1) + d] * kv[j * (D + 1) + d];
-            x *= p.scale_log2;
-            ps[row * 65 + j] = x;
-            mt = fmaxf(mt, x);
-        }
-        mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, 1));
-        const float alpha = m == -INFINITY ? 0.f : exp2f(m - mt);
-        m = mt;
-        l *= alpha;
-        for (int d = 0; d < D / 2; ++d) acc[d] *= alpha;
-        for (int j = half; j < lim; j += 2) {
-            const float w = exp2f(ps[row * 65 + j] - m);
-            ps[row * 65 + j] = w;
-            l += w;
-        }
-        fill(p.v, p.v_scale[tile], p.v_blk);
-        for (int j = 0; j < lim; ++j) {
-            const float w = ps[row * 65 + j];
+}
+__device__ __forceinline__ void walk_pair(const PagedAttnParams &p, Walk &w) {
+    w.t = 0;
+    if (++w.h == p.Hkv) {
+        w.h = 0;
+        ++w.b;
+        walk_load(p, w);
+    }
+}
+__device__ __forceinline__ void walk_next(const PagedAttnParams &p, Walk &w) {
+    if (++w.t == w.nt) walk_pair(p, w);
+}
+
+// Tile x of pair n has weighted position x + beta n; CTA c takes the tiles at
+// [c W / C, (c + 1) W / C).  A range that holds a block tile, which costs more
+// than its keys, so takes beta tiles fewer; beta = 0 with more pairs than
+// CTAs (nearly every range then holds one) or where a CTA could stay empty.
+constexpr int kBlockWeight = 3;
+struct Split {
+    long long N, W;
+    int beta;
+};
+__device__ __forceinline__ Split split_of(const PagedAttnParams &p, long long tiles) {
+    const long long pairs = (long long)p.B * p.Hkv;
+    Split s;
+    s.N = tiles;
+    s.beta = pairs <= p.num_ctas &&
+                     tiles + kBlockWeight * pairs >= (long long)(2 + kBlockWeight) * p.num_ctas
+                 ? kBlockWeight
+                 : 0;
+    s.W = tiles + s.beta * pairs;
+    return s;
+}
+__device__ __forceinline__ long long udiv(long long a, long long b) {
+    if ((((unsigned long long)a | (unsigned long long)b) >> 32) == 0)
+        return (long long)((uint32_t)a / (uint32_t)b);
+    return a / b;
+}
+// the CTA whose range holds weighted position q
+__device__ __forceinline__ int cta_of(long long q, const Split &s, int C) {
+    return (int)udiv((q + 1) * C - 1, s.W);
+}
+__device__ __forceinline__ int seq_tiles(const PagedAttnParams &p, int b) {
+    return b < p.B ? tiles_of(prefix_of(p, b)) : 0;
+}
+__device__ long long all_tiles(const PagedAttnParams &p) {  // whole warp
+    long long n = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 32)
+        n += (long long)__reduce_add_sync(kFull, (unsigned)seq_tiles(p, b0 + (threadIdx.x & 31))) *
+             p.Hkv;
+    return n;
+}
+
+// This CTA's number of tiles and its first one (a whole warp executes this).
+__device__ long long plan(const PagedAttnParams &p, Walk &w) {
+    const int lane = threadIdx.x & 31;
+    const Split sp = split_of(p, all_tiles(p));
+    const long long q[2] = {udiv((long long)blockIdx.x * sp.W, p.num_ctas),
+                            udiv(((long long)blockIdx.x + 1) * sp.W, p.num_ctas)};
+    long long at[2] = {sp.N, sp.N};
+    w = {0, 0, 0, 1, 0, 0};
+    int found = 0;
+    long long run_w = 0, run_t = 0;  // weighted positions / tiles before the chunk
+    for (int b0 = 0; b0 < p.B && found < 2; b0 += 32) {
+        const int nt = seq_tiles(p, b0 + lane), nseq = min(32, p.B - b0);
+        int inc = nt;
 #pragma unroll
-            for (int d = 0; d < D / 2; ++d) acc[d] += w * kv[j * (D + 1) + half + 2 * d];
+        for (int d = 1; d < 32; d <<= 1) {
+            const int u = __shfl_up_sync(kFull, inc, d);
+            if (lane >= d) inc += u;
         }
+        const long long after =
+            run_w + ((long long)inc + (long long)sp.beta * min(lane + 1, nseq)) * p.Hkv;
+        while (found < 2) {
+            const unsigned m = __ballot_sync(kFull, after > q[found]);
+            if (!m) break;
+            const int f = __ffs(m) - 1;
+            const int ntf = __shfl_sync(kFull, nt, f), before = __shfl_sync(kFull, inc, f) - ntf;
+            const long long off =
+                q[found] - run_w - ((long long)before + (long long)sp.beta * f) * p.Hkv;
+            int h = (int)udiv(off, ntf + sp.beta);
+            int t = (int)(off - (long long)h * (ntf + sp.beta));
+            if (t >= ntf) {  // in a block tile's extra weight: the next pair
+                t = 0;
+                ++h;
+            }
+            at[found] = run_t + (long long)before * p.Hkv + (long long)h * ntf + t;
+            if (found == 0) {
+                w.b = b0 + f;
+                w.h = h;
+                w.t = t;
+                if (h == p.Hkv) {
+                    w.h = 0;
+                    ++w.b;
+                }
+                walk_load(p, w);
+            }
+            ++found;
+        }
+        const int all = __shfl_sync(kFull, inc, 31);
+        run_w += ((long long)all + (long long)sp.beta * nseq) * p.Hkv;
+        run_t += (long long)all * p.Hkv;
     }
-    l += __shfl_xor_sync(0xffffffffu, l, 1);
-    if (row < p.rows_max) {
-        const size_t at = (size_t)blockIdx.x * p.rows_max + row;
-        const float inv = l > 0.f ? 1.f / l : 0.f;
-        for (int d = 0; d < D / 2; ++d) p.part_o[at * D + half + 2 * d] = acc[d] * inv;
-        if (half == 0) p.part_lse[at] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+    return max(0ll, at[1] - at[0]);
+}
+
+// ---- shared memory ------------------------------------------------------------------
+struct TileInfo {
+    float ks, lv, ivs;  // key scale, log2 and reciprocal of the value scale
+    int n;              // visible keys
+};
+
+template <int D>
+struct Layout {
+    static constexpr int kStages = 7;
+    static constexpr int kTile = kTileKeys * D;         // an e4m3 tile
+    static constexpr int kStage = 2 * kTile;            // keys, values
+    static constexpr int kQ8 = 2 * kRows * D;           // split queries [128 rows][D]
+    static constexpr int kBf = kTileKeys * D * 2;       // a bf16 tile or the bf16 queries
+    static constexpr int kPb = 2 * kRows * kTileKeys * 2;  // P of the block tile
+    static constexpr int kQ8Off = kStages * kStage;
+    static constexpr int kQbOff = kQ8Off + 2 * kQ8;
+    static constexpr int kKbOff = kQbOff + kBf;
+    static constexpr int kVbOff = kKbOff + kBf;
+    static constexpr int kPbOff = kVbOff + kBf;
+    static constexpr int kBarOff = kPbOff + kPb;
+    // full, empty [kStages], qready, qfree [2], bready, bfree, sready, sfree
+    // [kSBufs], pready, pvdone [2], drain [2]
+    static constexpr int kBars = 2 * kStages + 4 + 2 + 2 * kSBufs + 4 + 2;
+    static constexpr int kInfoOff = (kBarOff + kBars * 8 + 15) / 16 * 16;
+    static constexpr int kExpOff = kInfoOff + kStages * 16;
+    static constexpr int kMiscOff = kExpOff + 2 * kRows * 4;
+    static constexpr int kBytes = kMiscOff + 64 + 1024;  // + alignment slack
+    static constexpr uint32_t kSwizzle = D == 128 ? 2 : 4;  // 128- or 64-byte rows
+    static_assert(kTile % 1024 == 0 && kQ8Off % 1024 == 0 && kPbOff % 1024 == 0, "alignment");
+    static_assert(kBytes <= 232448, "shared memory per CTA");
+};
+
+// byte offset of 16-byte chunk c of row m: rows of D bytes, swizzled
+template <int D>
+__device__ __forceinline__ uint32_t chunk8(int m, int c) {
+    return m * D + ((D == 128 ? c ^ (m & 7) : c ^ ((m >> 1) & 3)) << 4);
+}
+// the same for 128-byte rows (bf16 panels of 64 columns)
+__device__ __forceinline__ uint32_t chunk16(int m, int c) { return m * 128 + ((c ^ (m & 7)) << 4); }
+__device__ __forceinline__ void st_shared(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w)
+                 : "memory");
+}
+
+// One segment's queries: thread ct of 128 takes half of row ct / 2, finds the
+// row's e = 7 - floor(log2 max |q|) (its largest element then scales into
+// [128, 256)), and writes 2^e q = hi + lo / 16 as two e4m3 rows.
+template <int D>
+__device__ __forceinline__ void split_queries(const PagedAttnParams &p, const Walk &w, uint32_t q8,
+                                              int *qexp, int ct) {
+    const int row = ct >> 1, half = ct & 1;
+    const bool live = row < p.G * w.T;
+    constexpr int kChunks = D / 16;  // 16-byte loads of half a row
+    uint4 x[kChunks];
+    if (live) {
+        const uint4 *src = reinterpret_cast<const uint4 *>(
+            p.q + (((size_t)w.b * p.max_block + row / p.G) * p.Hq + w.h * p.G + row % p.G) * D +
+            half * (D / 2));
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) x[i] = src[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) x[i] = make_uint4(0, 0, 0, 0);
+    }
+    uint32_t u[4 * kChunks];
+    float mx = 0.f;
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+        u[4 * i] = x[i].x;
+        u[4 * i + 1] = x[i].y;
+        u[4 * i + 2] = x[i].z;
+        u[4 * i + 3] = x[i].w;
+    }
+#pragma unroll
+    for (int i = 0; i < 4 * kChunks; ++i)
+        mx = fmaxf(mx, fmaxf(fabsf(__uint_as_float(u[i] << 16)),
+                             fabsf(__uint_as_float(u[i] & 0xffff0000u))));
+    mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, 1));
+    int e = 0;
+    if (mx > 0.f && mx <= 3.4e38f) {
+        e = 7 - ((int)((__float_as_uint(mx) >> 23) & 0xffu) - 127);
+        e = e < -120 ? -120 : (e > 120 ? 120 : e);
+    }
+    const float sc = __uint_as_float((uint32_t)(127 + e) << 23);
+    const int m = 32 * (row >> 4) + (row & 15);
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {  // 16 elements: 8 words in, 4 + 4 words out
+        uint32_t h[4], l[4];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t v = u[8 * c + j];
+            const float a = __uint_as_float(v << 16) * sc, b = __uint_as_float(v & 0xffff0000u) * sc;
+            const uint32_t hi = e4m3_f32(a, b);
+            float ha, hb;
+            unpack_f16(f16_e4m3(hi), ha, hb);
+            const uint32_t lo = e4m3_f32((a - ha) * 16.f, (b - hb) * 16.f);
+            h[j >> 1] = j & 1 ? h[j >> 1] | hi << 16 : hi;
+            l[j >> 1] = j & 1 ? l[j >> 1] | lo << 16 : lo;
+        }
+        const int chunk = half * (D / 32) + c;
+        st_shared(q8 + chunk8<D>(m, chunk), h[0], h[1], h[2], h[3]);
+        st_shared(q8 + chunk8<D>(m + 16, chunk), l[0], l[1], l[2], l[3]);
+    }
+    if (half == 0) qexp[row] = e;
+}
+
+// A pair's bf16 queries, block keys and block values: [64 rows][D] as D / 64
+// swizzled panels, rows past the block zero.
+template <int D>
+__device__ __forceinline__ void load_block(const PagedAttnParams &p, const Walk &w, uint32_t qb,
+                                           uint32_t kb, uint32_t vb, int ct) {
+    constexpr int kPerRow = D / 8;
+    const int rows = p.G * w.T;
+    for (int i = ct; i < kRows * kPerRow; i += kQueryWarps * 32) {
+        const int r = i / kPerRow, c = i % kPerRow;
+        const uint32_t at = (c >> 3) * (kRows * 128) + chunk16(r, c & 7);
+        uint4 q = make_uint4(0, 0, 0, 0), k = q, v = q;
+        if (r < rows)
+            q = *reinterpret_cast<const uint4 *>(
+                p.q + (((size_t)w.b * p.max_block + r / p.G) * p.Hq + w.h * p.G + r % p.G) * D +
+                c * 8);
+        if (r < w.T) {
+            const size_t s = (((size_t)w.b * p.max_block + r) * p.Hkv + w.h) * D + c * 8;
+            k = *reinterpret_cast<const uint4 *>(p.k_blk + s);
+            v = *reinterpret_cast<const uint4 *>(p.v_blk + s);
+        }
+        st_shared(qb + at, q.x, q.y, q.z, q.w);
+        st_shared(kb + at, k.x, k.y, k.z, k.w);
+        st_shared(vb + at, v.x, v.y, v.z, v.w);
     }
 }
 
 template <int D>
-__global__ void __launch_bounds__(D) paged_merge_kernel(const PagedAttnParams p, int splits) {
+__global__ void __launch_bounds__(kThreads, 1)
+    paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k,
+                      const __grid_constant__ CUtensorMap tm_v, const PagedAttnParams p) {
+    using Lt = Layout<D>;
+    constexpr int kStages = Lt::kStages;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                              ~uintptr_t(1023));
+    const uint32_t sbase = smem_u32(sm);
+    const uint32_t b_full = sbase + Lt::kBarOff, b_empty = b_full + 8 * kStages,
+                   b_qready = b_empty + 8 * kStages, b_qfree = b_qready + 16,
+                   b_bready = b_qfree + 16, b_bfree = b_bready + 8, b_sready = b_bfree + 8,
+                   b_sfree = b_sready + 8 * kSBufs, b_pready = b_sfree + 8 * kSBufs,
+                   b_pvdone = b_pready + 16, b_drain = b_pvdone + 16;
+    TileInfo *info = reinterpret_cast<TileInfo *>(sm + Lt::kInfoOff);
+    int *qexp = reinterpret_cast<int *>(sm + Lt::kExpOff);  // [2][kRows]
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(sm + Lt::kMiscOff);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(sm + Lt::kMiscOff + 4);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(b_full + 8 * s, 1);
+            mbar_init(b_empty + 8 * s, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(b_qready + 8 * i, kQueryWarps);
+            // the segment's last S, and every softmax warp once it has read e
+            mbar_init(b_qfree + 8 * i, 1 + kSoftWarps);
+            mbar_init(b_pready + 8 * i, kSoftWarps);
+            mbar_init(b_pvdone + 8 * i, 1);
+            mbar_init(b_drain + 8 * i, 1);
+        }
+        mbar_init(b_bready, kQueryWarps);
+        mbar_init(b_bfree, 1);
+        for (int i = 0; i < kSBufs; ++i) {
+            mbar_init(b_sready + 8 * i, 1);
+            mbar_init(b_sfree + 8 * i, kSoftWarps);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        *abort_flag = 0;
+    }
+    if (warp == 0) {
+        asm volatile(
+            "tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                smem_u32(const_cast<uint32_t *>(tmem_slot))),
+            "n"(kTmemCols));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (warp == kProducerWarp && elect_one()) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tm_k)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tm_v)) : "memory");
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    // every input (and the workspace) may be written by the previous kernel
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int row = blockIdx.x % p.rows_max, pair = blockIdx.x / p.rows_max;
-    const int b = pair / p.Hkv, h = pair % p.Hkv, d = threadIdx.x;
-    float M = -INFINITY, L = 0.f, o = 0.f;
-    const float *ls = p.part_lse + (size_t)pair * splits * p.rows_max + row;
-    for (int s = 0; s < splits; ++s) M = fmaxf(M, ls[(size_t)s * p.rows_max]);
-    for (int s = 0; s < splits; ++s) {
-        const float w = M == -INFINITY ? 0.f : expf(ls[(size_t)s * p.rows_max] - M);
-        L += w;
-        o += w * p.part_o[(((size_t)pair * splits + s) * p.rows_max + row) * D + d];
+    Walk w0;
+    const long long ntiles = plan(p, w0);
+    if (blockIdx.x == 0 && warp == 0)
+        for (int b = lane; b < p.B; b += 32)
+            if (p.prefix_len[b] != prefix_of(p, b) || p.block_len[b] != block_of(p, b))
+                atomicOr(p.status, kStatusClamped);
+
+    auto waits = [&](uint32_t bar, uint32_t parity) {
+        return wait(bar, parity, abort_flag, p.status);
+    };
+    long long issued = 0;  // tiles whose loads were issued (the producer's)
+    if (warp == kProducerWarp) {
+        // ================================ producer ===============================
+        // Stage s is reused once the P V that read it has completed.  Lane i
+        // holds page and scales of tile base + i of the segment.
+        uint64_t policy;
+        asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+        Walk w = w0;
+        int base = -1, page = -1;
+        float ks = 0.f, vs = 0.f;
+        bool ok = true;
+        for (long long j = 0; j < ntiles && ok; ++j, walk_next(p, w)) {
+            if (j == 0 || w.t == 0) base = -1;
+            if (w.t == w.nt - 1) continue;
+            if (base < 0 || w.t - base == 32) {
+                base = w.t;
+                const int t = base + lane;
+                page = t < w.nt - 1 ? p.table[(size_t)w.b * p.max_pages + t] : 0;
+                const bool good = page >= 0 && page < p.pages;
+                if (!good) atomicOr(p.status, kStatusBadPage);
+                const size_t tile = (size_t)(good ? page : 0) * p.Hkv + w.h;
+                if (!good) page = -1;
+                ks = p.k_scale[tile];
+                vs = fmaxf(p.v_scale[tile], 8.6736174e-19f);  // 2^-60: codes under a 0 scale vanish
+            }
+            const int s = (int)(issued % kStages);
+            if (issued >= kStages) ok = waits(b_empty + 8 * s, (uint32_t)((issued / kStages - 1) & 1));
+            const int pg = __shfl_sync(kFull, page, w.t - base);
+            const float k1 = __shfl_sync(kFull, ks, w.t - base);
+            const float v1 = __shfl_sync(kFull, vs, w.t - base);
+            if (!ok) break;
+            if (elect_one()) {
+                const uint32_t full = b_full + 8 * s, dst = sbase + s * Lt::kStage;
+                const int tile = (pg < 0 ? 0 : pg) * p.Hkv + w.h;
+                TileInfo ti;
+                ti.ks = k1;
+                ti.lv = log2f(v1);
+                ti.ivs = 1.f / v1;
+                ti.n = pg < 0 ? 0 : min(kTileKeys, w.P - w.t * kTileKeys);
+                info[s] = ti;
+                mbar_arrive_expect_tx(full, Lt::kStage);
+                tma_3d(dst, &tm_k, full, 0, 0, tile, policy);
+                tma_3d(dst + Lt::kTile, &tm_v, full, 0, 0, tile, policy);
+            }
+            __syncwarp();
+            ++issued;
+        }
+    } else if (warp == kSWarp) {
+        // =============================== S = Q K^T ===============================
+        const uint32_t id8 = idesc_e4m3(2 * kRows, kTileKeys, 0, 0);
+        const uint32_t idb = idesc_bf16(kRows, kTileKeys, 0, 0);
+        const uint64_t dq8 = sdesc(sbase + Lt::kQ8Off, 16, 8 * D, Lt::kSwizzle);
+        const uint64_t dk8 = sdesc(sbase, 16, 8 * D, Lt::kSwizzle);
+        const uint64_t dqb = sdesc(sbase + Lt::kQbOff, 16, 1024, 2);
+        const uint64_t dkb = sdesc(sbase + Lt::kKbOff, 16, 1024, 2);
+        Walk w = w0;
+        int seg = -1;
+        long long kp = 0, nblk = 0;
+        bool ok = true;
+        for (long long k = 0; k < ntiles && ok; ++k) {
+            if (k == 0 || w.t == 0) {
+                ++seg;
+                ok = waits(b_qready + 8 * (seg & 1), (uint32_t)((seg >> 1) & 1));
+            }
+            const bool blk = w.t == w.nt - 1;
+            const int s = (int)(kp % kStages);
+            ok = ok && (blk ? waits(b_bready, (uint32_t)(nblk & 1))
+                            : waits(b_full + 8 * s, (uint32_t)((kp / kStages) & 1)));
+            if (k >= kSBufs)
+                ok = ok && waits(b_sfree + 8 * (int)(k % kSBufs), (uint32_t)((k / kSBufs - 1) & 1));
+            if (!ok) break;
+            fence_after();
+            if (elect_one()) {
+                const uint32_t dS = tmem + (uint32_t)((k % kSBufs) * kTileKeys);
+                if (!blk) {
+                    const uint64_t a0 = dq8 + (uint64_t)(((seg & 1) * Lt::kQ8) >> 4);
+                    const uint64_t b0 = dk8 + (uint64_t)((s * Lt::kStage) >> 4);
+#pragma unroll
+                    for (int kk = 0; kk < D / 32; ++kk)
+                        mma_e4m3(dS, a0 + kk * 2, b0 + kk * 2, id8, kk > 0);
+                } else {
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const uint32_t off = ((kk >> 2) * (kRows * 128) + (kk & 3) * 32) >> 4;
+                        mma_bf16(dS, dqb + off, dkb + off, idb, kk > 0);
+                    }
+                }
+                mma_commit(b_sready + 8 * (int)(k % kSBufs));
+                if (blk || k + 1 == ntiles) mma_commit(b_qfree + 8 * (seg & 1));
+            }
+            __syncwarp();
+            if (blk) ++nblk;
+            else ++kp;
+            walk_next(p, w);
+        }
+    } else if (warp == kPvWarp) {
+        // ================================ O += P V ===============================
+        const uint32_t id8 = idesc_e4m3(2 * kRows, D, 0, 1);
+        const uint32_t idb = idesc_bf16(2 * kRows, D, 0, 1);
+        const uint64_t dv8 = sdesc(sbase + Lt::kTile, 8 * D, 8 * D, Lt::kSwizzle);
+        const uint64_t dpb = sdesc(sbase + Lt::kPbOff, 16, 1024, 2);
+        const uint64_t dvb = sdesc(sbase + Lt::kVbOff, kRows * 128, 1024, 2);
+        const uint32_t dO = tmem + kOCol;
+        Walk w = w0;
+        long long kp = 0;
+        bool ok = true;
+        for (long long k = 0; k < ntiles && ok; ++k) {
+            const bool first = k == 0 || w.t == 0, blk = w.t == w.nt - 1;
+            const int s = (int)(kp % kStages);
+            ok = waits(b_pready + 8 * (int)(k & 1), (uint32_t)((k >> 1) & 1));
+            if (!blk) ok = ok && waits(b_full + 8 * s, (uint32_t)((kp / kStages) & 1));
+            if (!ok) break;
+            fence_after();
+            if (elect_one()) {
+                if (!blk) {
+                    const uint32_t a0 = tmem + kPCol + (uint32_t)((k & 1) * 16);
+                    const uint64_t b0 = dv8 + (uint64_t)((s * Lt::kStage) >> 4);
+#pragma unroll
+                    for (int kk = 0; kk < 2; ++kk)
+                        mma_e4m3_ta(dO, a0 + kk * 8, b0 + (uint64_t)((kk * 32 * D) >> 4), id8,
+                                    !first || kk > 0);
+                } else {
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk)
+                        mma_bf16(dO, dpb + kk * 2, dvb + (uint64_t)((kk * 2048) >> 4), idb,
+                                 !first || kk > 0);
+                }
+                mma_commit(b_pvdone + 8 * (int)(k & 1));
+                mma_commit(blk ? b_bfree : b_empty + 8 * s);
+            }
+            __syncwarp();
+            if (!blk) ++kp;
+            walk_next(p, w);
+        }
+    } else if (warp >= kQueryWarp0) {
+        // ====================== queries, block keys and values ===================
+        const int ct = threadIdx.x - kQueryWarp0 * 32;
+        Walk w = w0;
+        long long left = ntiles, nblk = 0;
+        for (int seg = 0; left > 0; ++seg) {
+            const int q = seg & 1;
+            if (seg >= 2 && !waits(b_qfree + 8 * q, (uint32_t)(((seg >> 1) - 1) & 1))) break;
+            split_queries<D>(p, w, sbase + Lt::kQ8Off + q * Lt::kQ8, qexp + q * kRows, ct);
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(b_qready + 8 * q);
+            if (left >= w.nt - w.t) {  // the segment reaches the pair's block tile
+                if (nblk >= 1 && !waits(b_bfree, (uint32_t)((nblk - 1) & 1))) break;
+                load_block<D>(p, w, sbase + Lt::kQbOff, sbase + Lt::kKbOff, sbase + Lt::kVbOff, ct);
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_bready);
+                ++nblk;
+            }
+            left -= w.nt - w.t;
+            walk_pair(p, w);
+        }
+    } else {
+        // ================================ softmax ================================
+        // thread (warp, lane): row 16 warp + lane % 16, 32 of each tile's keys
+        const int row = warp * 16 + (lane & 15), half = lane >> 4;
+        const int key0 = 32 * half;
+        const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
+        Walk w = w0;
+        float m_ref = -INFINITY, l_sum = 0.f, row_scale = 1.f;
+        int seg = -1, irow = 0, rows_active = 0, seg_t = 0;
+        long long kp = 0;
+        for (long long k = 0; k < ntiles; ++k) {
+            const bool first = k == 0 || w.t == 0, blk = w.t == w.nt - 1;
+            const bool last = blk || k + 1 == ntiles;
+            if (first) {
+                ++seg;
+                seg_t = w.t;
+                m_ref = -INFINITY;
+                l_sum = 0.f;
+                rows_active = p.G * w.T;
+                irow = row / p.G;
+                const int q = seg & 1;
+                waits(b_qready + 8 * q, (uint32_t)((seg >> 1) & 1));
+                row_scale = p.scale_log2 *
+                            __uint_as_float((uint32_t)(127 - qexp[q * kRows + row]) << 23);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_qfree + 8 * q);
+            }
+            const int s = (int)(kp % kStages);
+            float scale = p.scale_log2, lv = 0.f, ivs = 1.f;
+            int n = w.T;
+            if (!blk) {
+                waits(b_full + 8 * s, (uint32_t)((kp / kStages) & 1));
+                const TileInfo ti = info[s];
+                scale = row_scale * ti.ks;
+                lv = ti.lv;
+                ivs = ti.ivs;
+                n = ti.n;
+            }
+            const bool ok_s =
+                waits(b_sready + 8 * (int)(k % kSBufs), (uint32_t)((k / kSBufs) & 1));
+            fence_after();
+            const uint32_t s_addr = lanes + (uint32_t)((k % kSBufs) * kTileKeys);
+            float v[32];
+            {
+                uint32_t a[32];
+                ld_half(s_addr, a);
+                if (!blk) {
+                    uint32_t c[32];
+                    ld_half(s_addr + kLoLanes, c);
+                    ld_wait(a);
+                    ld_wait(c);
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2)
+                        axpy2(v[j], v[j + 1], kLoInv, __uint_as_float(c[j]),
+                              __uint_as_float(c[j + 1]), __uint_as_float(a[j]),
+                              __uint_as_float(a[j + 1]));
+                } else {
+                    ld_wait(a);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(a[j]);
+                }
+            }
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(b_sfree + 8 * (int)(k % kSBufs));
+            const bool live = row < rows_active && ok_s;
+            if (blk || n < kTileKeys) {  // keys from lim on are hidden from this row
+                const int lim = !live ? 0 : (blk ? min(n, irow + 1) : n);
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (key0 + j >= lim) v[j] = -INFINITY;
+            }
+            float mt;
+            {
+                float x[11];
+#pragma unroll
+                for (int j = 0; j < 10; ++j) x[j] = max3(v[3 * j], v[3 * j + 1], v[3 * j + 2]);
+                x[10] = fmaxf(v[30], v[31]);
+                mt = fmaxf(max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]),
+                                max3(x[6], x[7], x[8])),
+                           fmaxf(x[9], x[10]));
+            }
+            mt = fmaxf(mt, __shfl_xor_sync(kFull, mt, 16));
+            // a masked score stays -inf under a scale of 0
+            mt = mt == -INFINITY ? -INFINITY : mt * scale + lv;
+            if (first) {
+                m_ref = mt;
+            } else {
+                const bool jump = live && mt > m_ref + kWindow;
+                if (__any_sync(kFull, jump)) {
+                    // O is stable once P V of tile k - 1 is done
+                    waits(b_pvdone + 8 * (int)((k - 1) & 1), (uint32_t)(((k - 1) >> 1) & 1));
+                    fence_after();
+                    const float alpha = jump ? ex2(m_ref - mt) : 1.f;  // from -inf: 0
+                    if (jump) {
+                        m_ref = mt;
+                        l_sum *= alpha;
+                    }
+                    // thread t holds lane t: row t % 16's hi or lo part, the same alpha
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 16) {
+                        uint32_t o[16];
+                        ld_lanes16(lanes + kOCol + c, o);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+                        st_lanes16(lanes + kOCol + c, o);
+                    }
+                    st_wait();
+                }
+            }
+            const float off = lv + kHead - (m_ref == -INFINITY ? 0.f : m_ref);
+            if (blk || n < kTileKeys) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    v[j] = v[j] == -INFINITY ? -INFINITY : v[j] * scale + off;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 32; j += 2)
+                    fma2(v[j], v[j + 1], v[j], v[j + 1], scale, off);
+            }
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = ex2(v[j]);
+            // P buffer (k & 1) is free once the P V of tile k - 2 is done
+            if (k >= 2) waits(b_pvdone + 8 * (int)(k & 1), (uint32_t)((k / 2 - 1) & 1));
+            fence_after();
+            if (!blk) {
+                uint32_t hi[8], lo[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    uint32_t h2[2], l2[2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t x = pack_f16(v[4 * j + 2 * i], v[4 * j + 2 * i + 1]);
+                        h2[i] = e4m3_f16(x);
+                        // (x - hi) * 16, both steps exact
+                        l2[i] = e4m3_f16(hmul2(hsub2(x, f16_e4m3(h2[i])), 0x4c004c00u));
+                    }
+                    hi[j] = h2[0] | h2[1] << 16;
+                    lo[j] = l2[0] | l2[1] << 16;
+                }
+                const uint32_t pa = lanes + kPCol + (uint32_t)((k & 1) * 16);
+                st_half(pa, hi);
+                st_half(pa + kLoLanes, lo);
+                st_wait();
+                // keys past the page's last token may hold anything: zero their value rows
+                if (n < kTileKeys) {
+                    const uint32_t vt = sbase + s * Lt::kStage + Lt::kTile + n * D;
+                    for (int i = threadIdx.x; i < (kTileKeys - n) * (D / 16); i += kSoftWarps * 32)
+                        st_shared(vt + i * 16, 0, 0, 0, 0);
+                    fence_async_smem();
+                }
+            } else {
+                const uint32_t pb = sbase + Lt::kPbOff;
+                const int m = 32 * warp + (lane & 15);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t h[4], l[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float x = v[8 * c + 2 * i], y = v[8 * c + 2 * i + 1];
+                        h[i] = pack_bf16(x, y);
+                        l[i] = pack_bf16((x - __uint_as_float(h[i] << 16)) * 16.f,
+                                         (y - __uint_as_float(h[i] & 0xffff0000u)) * 16.f);
+                    }
+                    st_shared(pb + chunk16(m, key0 / 8 + c), h[0], h[1], h[2], h[3]);
+                    st_shared(pb + chunk16(m + 16, key0 / 8 + c), l[0], l[1], l[2], l[3]);
+                }
+                fence_async_smem();
+            }
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(b_pready + 8 * (int)(k & 1));
+            {  // l: in binary32, of the weights before rounding
+                float t[16];
+#pragma unroll
+                for (int j = 0; j < 16; j += 2)
+                    add2(t[j], t[j + 1], v[j], v[j + 1], v[j + 16], v[j + 17]);
+#pragma unroll
+                for (int d = 8; d > 1; d >>= 1)
+#pragma unroll
+                    for (int j = 0; j < d; j += 2)
+                        add2(t[j], t[j + 1], t[j], t[j + 1], t[j + d], t[j + d + 1]);
+                l_sum += (t[0] + t[1]) * ivs;
+            }
+
+            if (last) {
+                // ---- end of a segment: O / l and lse ----
+                waits(b_pvdone + 8 * (int)(k & 1), (uint32_t)((k >> 1) & 1));
+                fence_after();
+                const bool whole = seg_t == 0 && blk, write = row < rows_active;
+                const float l = l_sum + __shfl_xor_sync(kFull, l_sum, 16);
+                const float inv = l > 0.f ? 1.f / l : 0.f;
+                const float lse = l > 0.f ? (m_ref - kHead + log2f(l)) * kLn2 : -INFINITY;
+                const int gq = w.h * p.G + row % p.G;
+                const size_t slot =
+                    ((size_t)(w.b * p.Hkv + w.h) + blockIdx.x) * p.rows_max + row;
+                uint16_t *orow = p.out + (((size_t)w.b * p.max_block + irow) * p.Hq + gq) * D;
+                float *prow = p.part_o + slot * D;
+#pragma unroll
+                for (int g = 0; g < D / 64; ++g) {
+                    uint32_t a[32], c[32];
+                    ld_half(lanes + kOCol + 64 * g, a);
+                    ld_half(lanes + kOCol + 64 * g + kLoLanes, c);
+                    ld_wait(a);
+                    ld_wait(c);
+                    float x[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        x[j] = (__uint_as_float(a[j]) + kLoInv * __uint_as_float(c[j])) * inv;
+                    const int d0 = 64 * g + 32 * half;
+                    if (write) {
+                        if (whole) {
+#pragma unroll
+                            for (int j = 0; j < 32; j += 8)
+                                *reinterpret_cast<uint4 *>(orow + d0 + j) = make_uint4(
+                                    pack_bf16(x[j], x[j + 1]), pack_bf16(x[j + 2], x[j + 3]),
+                                    pack_bf16(x[j + 4], x[j + 5]), pack_bf16(x[j + 6], x[j + 7]));
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 32; j += 4)
+                                *reinterpret_cast<float4 *>(prow + d0 + j) =
+                                    make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+                        }
+                    }
+                }
+                if (write && half == 0) {
+                    if (whole)
+                        p.lse[((size_t)w.b * p.Hq + gq) * p.max_block + irow] = lse;
+                    else
+                        p.part_lse[slot] = lse;
+                }
+                if (whole)  // rows past the block: 0 and lse -inf
+                    for (int i = threadIdx.x; i < (p.rows_max - rows_active) * (D / 8);
+                         i += kSoftWarps * 32) {
+                        const int r = rows_active + i / (D / 8), c = (i % (D / 8)) * 8;
+                        const int ii = r / p.G, gg = w.h * p.G + r % p.G;
+                        *reinterpret_cast<uint4 *>(
+                            p.out + (((size_t)w.b * p.max_block + ii) * p.Hq + gg) * D + c) =
+                            make_uint4(0, 0, 0, 0);
+                        if (c == 0) p.lse[((size_t)w.b * p.Hq + gg) * p.max_block + ii] = -INFINITY;
+                    }
+                fence_before();
+            }
+            if (!blk) ++kp;
+            walk_next(p, w);
+        }
     }
-    const int i = row / p.G, g = h * p.G + row % p.G;
-    const __nv_bfloat16 r = __float2bfloat16_rn(L > 0.f ? o / L : 0.f);
-    p.out[(((size_t)b * p.max_block + i) * p.Hq + g) * D + d] = __bfloat16_as_ushort(r);
-    if (d == 0)
-        p.lse[((size_t)b * p.Hq + g) * p.max_block + i] = L > 0.f ? M + logf(L) : -INFINITY;
+    if (warp == kSWarp || warp == kPvWarp) {
+        // every MMA that this warp issued is complete before tensor memory is
+        // freed (only a timed-out run can leave any in flight)
+        const uint32_t drain = b_drain + (warp == kSWarp ? 8 : 0);
+        if (elect_one()) mma_commit(drain);
+        __syncwarp();
+        const unsigned long long t0 = globaltimer();
+        while (!mbar_try_wait(drain, 0) && globaltimer() - t0 < kWaitNs) {
+        }
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (*abort_flag && warp == kProducerWarp && elect_one())  // copies in flight land before exit
+        for (long long j = issued - 1; j >= 0 && j >= issued - kStages; --j)
+            drain_wait(b_full + 8 * (int)(j % kStages), (uint32_t)((j / kStages) & 1));
+    if (warp == 0)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem),
+                     "n"(kTmemCols));
 }
 
-int splits_of(int device, int batch, int kv_heads) {
-    const int C = attn_grid_size(device);
-    return C <= 0 ? 0 : (int)std::max<long long>(1, 2ll * C / ((long long)batch * kv_heads));
+// ---- merge ------------------------------------------------------------------------
+// One warp per query row of a pair that was cut: with partials O_s / l_s and
+// lse_s, out = sum_s e^(lse_s - M) O_s / l_s / sum_s e^(lse_s - M) and
+// lse = M + ln of that sum.
+constexpr int kMergeWarps = 4;
+constexpr int kMergeLoads = 4;
+
+template <int D>
+__global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const PagedAttnParams p) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    constexpr int V = D / 32;
+    const int rblocks = (p.rows_max + kMergeWarps - 1) / kMergeWarps;
+    const int pair = blockIdx.x / rblocks, lane = threadIdx.x & 31;
+    const int row = (blockIdx.x % rblocks) * kMergeWarps + (threadIdx.x >> 5);
+    const int b = pair / p.Hkv, h = pair % p.Hkv;
+    long long total = 0, before = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 32) {
+        const int nt = seq_tiles(p, b0 + lane);
+        total += (long long)__reduce_add_sync(kFull, (unsigned)nt) * p.Hkv;
+        before += (long long)__reduce_add_sync(kFull, b0 + lane < b ? (unsigned)nt : 0u) * p.Hkv;
+    }
+    const Split sp = split_of(p, total);
+    const int nt = tiles_of(prefix_of(p, b));
+    const long long q0 = before + (long long)h * nt + (long long)sp.beta * pair;
+    const int c0 = cta_of(q0, sp, p.num_ctas);
+    // with fewer tiles than CTAs a tile is a CTA's own and the CTAs between are empty
+    const bool dense = sp.beta > 0 || sp.N >= p.num_ctas;
+    const int nseg = dense ? cta_of(q0 + nt - 1, sp, p.num_ctas) - c0 + 1 : nt;
+    if (nseg <= 1 || row >= p.rows_max) return;
+    const int i = row / p.G, g = h * p.G + row % p.G;
+    uint16_t *orow = p.out + (((size_t)b * p.max_block + i) * p.Hq + g) * D + V * lane;
+    float *lrow = p.lse + ((size_t)b * p.Hq + g) * p.max_block + i;
+    float M = -INFINITY, L = 0.f, acc[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) acc[v] = 0.f;
+    if (row < p.G * block_of(p, b)) {
+        for (int s0 = 0; s0 < nseg; s0 += kMergeLoads) {
+            float ls[kMergeLoads], o[kMergeLoads][V];
+#pragma unroll
+            for (int u = 0; u < kMergeLoads; ++u) {
+                ls[u] = -INFINITY;
+#pragma unroll
+                for (int v = 0; v < V; ++v) o[u][v] = 0.f;
+                if (s0 + u < nseg) {
+                    const int c = dense ? c0 + s0 + u : cta_of(q0 + s0 + u, sp, p.num_ctas);
+                    const size_t slot = ((size_t)pair + c) * p.rows_max + row;
+                    ls[u] = __ldcg(p.part_lse + slot);
+                    const float *src = p.part_o + slot * D + V * lane;
+#pragma unroll
+                    for (int v = 0; v < V; v += 2) {
+                        const float2 x = __ldcg(reinterpret_cast<const float2 *>(src + v));
+                        o[u][v] = x.x;
+                        o[u][v + 1] = x.y;
+                    }
+                }
+            }
+            float m = M;
+#pragma unroll
+            for (int u = 0; u < kMergeLoads; ++u) m = fmaxf(m, ls[u]);
+            if (m == -INFINITY) continue;
+            const float a = __expf(M - m);
+            L *= a;
+#pragma unroll
+            for (int v = 0; v < V; ++v) acc[v] *= a;
+#pragma unroll
+            for (int u = 0; u < kMergeLoads; ++u) {
+                const float x = __expf(ls[u] - m);
+                L += x;
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[v] += x * o[u][v];
+            }
+            M = m;
+        }
+    }
+    const float inv = L > 0.f ? 1.f / L : 0.f;
+#pragma unroll
+    for (int v = 0; v < V; v += 2)
+        *reinterpret_cast<uint32_t *>(orow + v) = pack_bf16(acc[v] * inv, acc[v + 1] * inv);
+    if (lane == 0) *lrow = L > 0.f ? M + __logf(L) : -INFINITY;
 }
+
 size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 
 template <int D>
-cudaError_t launch_d(const PagedAttnParams &p, int splits, cudaStream_t stream) {
-    constexpr int smem = (2 * 64 * (D + 1) + 64 * 65) * 4;
-    cudaError_t e = cudaFuncSetAttribute(paged_attn_kernel<D>,
-                                         cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+cudaError_t launch_d(const PagedAttnParams &p, const CUtensorMap &tm_k, const CUtensorMap &tm_v,
+                     cudaStream_t stream) {
+    constexpr int smem = Layout<D>::kBytes;
+    static std::atomic<bool> configured[64];  // the shared-memory opt-in, once per device
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    paged_attn_kernel<D><<<p.B * p.Hkv * splits, kThreads, smem, stream>>>(p, splits);
-    paged_merge_kernel<D><<<p.B * p.Hkv * p.rows_max, D, 0, stream>>>(p, splits);
-    return cudaGetLastError();
+    if (dev >= 64 || !configured[dev].load(std::memory_order_acquire)) {
+        e = cudaFuncSetAttribute(paged_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 smem);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) configured[dev].store(true, std::memory_order_release);
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)p.num_ctas);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, paged_attn_kernel<D>, tm_k, tm_v, p);
+    if (e != cudaSuccess) return e;
+    const long long rblocks = (p.rows_max + kMergeWarps - 1) / kMergeWarps;
+    cfg.gridDim = dim3((unsigned)((long long)p.B * p.Hkv * rblocks));
+    cfg.blockDim = dim3(kMergeWarps * 32);
+    cfg.dynamicSmemBytes = 0;
+    return cudaLaunchKernelEx(&cfg, paged_merge_kernel<D>, p);
 }
 
 }  // namespace
 
+// header | part_o [slots][rows_max][D] | part_lse [slots][rows_max], slots =
+// B * Hkv + C (a segment's slot is its pair + its CTA).
 size_t paged_workspace_bytes(int device, int batch, int kv_heads, int rows_max, int head_dim) {
-    const size_t slots = (size_t)batch * kv_heads * splits_of(device, batch, kv_heads);
-    if (slots == 0) return 0;
+    const int C = attn_grid_size(device);
+    if (C <= 0) return 0;
+    const size_t slots = (size_t)batch * kv_heads + (size_t)C;
     return kWorkspaceHeader + round256(slots * rows_max * head_dim * sizeof(float)) +
            round256(slots * rows_max * sizeof(float));
 }
 
-cudaError_t paged_attn_launch(PagedAttnParams &p, int head_dim, void *workspace,
-                              cudaStream_t stream) {
+cudaError_t paged_attn_launch(PagedAttnParams &p, int head_dim, const CUtensorMap &tm_k,
+                              const CUtensorMap &tm_v, void *workspace, cudaStream_t stream) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    const int splits = splits_of(dev, p.B, p.Hkv);
+    p.num_ctas = attn_grid_size(dev);
+    if (p.num_ctas <= 0) return cudaErrorInvalidDevice;
     uint8_t *ws = static_cast<uint8_t *>(workspace);
+    const size_t slots = (size_t)p.B * p.Hkv + (size_t)p.num_ctas;
     p.status = reinterpret_cast<int32_t *>(ws);
     p.part_o = reinterpret_cast<float *>(ws + kWorkspaceHeader);
     p.part_lse = reinterpret_cast<float *>(
-        ws + kWorkspaceHeader +
-        round256((size_t)p.B * p.Hkv * splits * p.rows_max * head_dim * sizeof(float)));
-    return head_dim == 128 ? launch_d<128>(p, splits, stream) : launch_d<64>(p, splits, stream);
+        ws + kWorkspaceHeader + round256(slots * p.rows_max * head_dim * sizeof(float)));
+    return head_dim == 128 ? launch_d<128>(p, tm_k, tm_v, stream)
+                           : launch_d<64>(p, tm_k, tm_v, stream);
 }
 
 }  // namespace das
