@@ -5,22 +5,34 @@
 // equal ones by index), so each is one threshold: a key (the logit's bits made
 // monotone) and how many of the tokens equal to it, lowest index first, stay.
 // The threshold is where a sum over keys >= t first reaches a target: a sum of
-// ones for top-k, of the whole-number weights for top-p.
+// ones for top-k, of the whole-number weights for top-p.  Nothing is sorted.
+//
+// sample_kernel: a cluster of CTAs holds a row in shared memory, read once.  A
+// threshold is found from a histogram of kBins bins in shared memory, over
+// the logits (top-k) or the exponents (top-p), summed over the cluster; what
+// falls into the threshold's bin, rarely more than some dozens, is compared
+// pair by pair, or binned again by its keys if it is more than kList.  The
+// token is found from sums over segments in index order.
 //
 // Every kernel here is launched as a programmatic dependent of the previous
 // kernel in the stream: it reads nothing before griddepcontrol.wait, and
 // every CTA executes that wait.
 #include <algorithm>
+#include <atomic>
+
+#include <cooperative_groups.h>
 
 #include "das_internal.h"
+
+namespace cg = cooperative_groups;
 
 namespace das {
 namespace {
 
 using u64 = unsigned long long;
-constexpr uint32_t kFull = 0xffffffffu;
-constexpr int kThreads = 1024;
+constexpr int kLongThreads = 1024;
 constexpr int kScanWarps = 4;
+constexpr uint32_t kFull = 0xffffffffu;
 
 // A logit as a key that compares like the number: -0 equals 0, NaN is -inf.
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -54,9 +66,660 @@ __device__ __forceinline__ T block_reduce(T v, T *sums, F f) {
     return v;
 }
 
-// One row by one CTA, reading it once for every step.
+// ---- a row in the shared memory of a cluster ---------------------------------------
+constexpr int kThreads = 1024, kWarps = kThreads / 32;
+static_assert(kWarps == 32, "a warp scans the warps' sums");
+constexpr int kMaxRowCtas = 8;                 // a portable cluster
+constexpr int kSliceBytes = 131072;            // logits per CTA, as they come
+constexpr int kMaxSegs = kSliceBytes / 2 / 128;  // of one warp's 32 groups of four
+constexpr int kBins = 2048;
+constexpr int kList = 256;
+constexpr int kCand = 2048;
+// exponents past the last bin have weights that round to 0: e^-23 < 2^-33
+constexpr float kNats = 23.f;
+constexpr uint32_t kOne = 0xffffffffu;  // stands for the weight 2^32
+
+struct Shared {
+    float cand[kCand];              // the candidates left by a small top-k,
+    int cand_at[kCand];             // in index order
+    uint32_t lo[kBins], hi[kBins];  // a bin's sum: lo + 2^16 hi
+    u64 scan[kWarps];
+    u64 seg[kMaxSegs];
+    u64 xch[2][3][kMaxRowCtas];  // values of every CTA of the cluster
+    uint32_t list[kList];  // the CTA's keys in a bin
+    uint2 all[kList];      // the cluster's, with their weights
+    uint32_t list_n, key_min, key_max;
+    int bin, where;
+    uint32_t cut;
+    u64 above, target, sum, equal;
+};
+
+__device__ __forceinline__ u64 wide(uint32_t w) { return (u64)w + (w == kOne); }
+
 template <bool BF16>
-__global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a, int slice, bool vec) {
+    __shared__ Shared s;
+    extern __shared__ uint4 held[];  // the CTA's logits in groups of four, padded with -inf
+    cg::cluster_group cluster = cg::this_cluster();
+    const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const size_t row = blockIdx.x / C;
+    const int b = (int)(row / a.W);
+    auto of = [&](int r) { return C > 1 ? cluster.map_shared_rank(&s, r) : &s; };
+    auto sync = [&] {  // the cluster's threads, or the CTA's
+        if (C > 1) cluster.sync();
+        else __syncthreads();
+    };
+    int turn = 0;
+    // Three values of each CTA to every CTA, in s.xch[returned]; two sets in
+    // turn, so that none is written while another CTA may still read it.
+    auto exchange = [&](u64 x, u64 y, u64 z) {  // the same in all threads
+        turn ^= 1;
+        if (tid < C) {
+            u64(*to)[kMaxRowCtas] = of(tid)->xch[turn];
+            to[0][rank] = x;
+            to[1][rank] = y;
+            to[2][rank] = z;
+        }
+        sync();
+        return turn;
+    };
+    auto warp_scan = [&](u64 v) {  // inclusive
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const u64 y = __shfl_up_sync(kFull, v, d);
+            if (lane >= d) v += y;
+        }
+        return v;
+    };
+    auto scan = [&](u64 v, u64 &total) {  // exclusive sum over the CTA
+        const u64 x = warp_scan(v);
+        if (lane == 31) s.scan[warp] = x;
+        __syncthreads();
+        const u64 sums = warp_scan(s.scan[lane]);  // by every warp for itself
+        total = __shfl_sync(kFull, sums, 31);
+        const u64 before = __shfl_sync(kFull, sums, warp > 0 ? warp - 1 : 0);
+        __syncthreads();
+        return (warp > 0 ? before : 0) + x - v;
+    };
+
+    if (tid == 0) {
+        s.key_max = 0;
+        s.key_min = kOne;
+    }
+    sync();  // every CTA of the cluster has started
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    float T = a.sampling.temperature ? a.sampling.temperature[b] : 1.f;
+    long long k = a.sampling.top_k ? a.sampling.top_k[b] : 0;
+    const float p = a.sampling.top_p ? a.sampling.top_p[b] : 1.f;
+    float floor_p = a.sampling.min_p ? a.sampling.min_p[b] : 0.f;
+    floor_p = floor_p > 0.f ? fminf(floor_p, 1.f) : 0.f;  // NaN: none
+    if (!(T > 0.f)) {
+        T = 1.f;
+        k = 1;
+    }
+    T = fminf(T, 3.4028234e38f);
+    if (k <= 0 || k > a.vocab) k = a.vocab;
+
+    // ---- the row: NaN as -inf, -0 as 0 ----
+    const int base = rank * slice, len = max(0, min(slice, a.vocab - base));
+    int groups = (len + 3) / 4;
+    bool few = false;  // whether the candidates alone are left
+    auto clean = [](float f) { return f == f ? f + 0.f : -INFINITY; };
+    float mine = -INFINITY;
+    {
+        const size_t at = row * (size_t)a.row_stride + base;
+#pragma unroll 4
+        for (int g = tid; g < groups; g += kThreads) {
+            const int i = 4 * g;
+            float f[4];
+            if (vec && i + 4 <= len) {
+                if (BF16) {
+                    const uint2 u = __ldcs(reinterpret_cast<const uint2 *>(
+                        static_cast<const uint16_t *>(a.logits) + at + i));
+                    f[0] = __uint_as_float(u.x << 16);
+                    f[1] = __uint_as_float(u.x & 0xffff0000u);
+                    f[2] = __uint_as_float(u.y << 16);
+                    f[3] = __uint_as_float(u.y & 0xffff0000u);
+                } else {
+                    const float4 u = __ldcs(reinterpret_cast<const float4 *>(
+                        static_cast<const float *>(a.logits) + at + i));
+                    f[0] = u.x;
+                    f[1] = u.y;
+                    f[2] = u.z;
+                    f[3] = u.w;
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    f[c] = -INFINITY;
+                    if (i + c < len)
+                        f[c] = BF16 ? __uint_as_float((uint32_t)static_cast<const uint16_t *>(
+                                                          a.logits)[at + i + c]
+                                                      << 16)
+                                    : static_cast<const float *>(a.logits)[at + i + c];
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                f[c] = clean(f[c]);
+                mine = fmaxf(mine, f[c]);
+            }
+            if (BF16)
+                reinterpret_cast<uint2 *>(held)[g] =
+                    make_uint2(__float_as_uint(f[0]) >> 16 | (__float_as_uint(f[1]) & 0xffff0000u),
+                               __float_as_uint(f[2]) >> 16 | (__float_as_uint(f[3]) & 0xffff0000u));
+            else
+                reinterpret_cast<float4 *>(held)[g] = make_float4(f[0], f[1], f[2], f[3]);
+        }
+    }
+    auto load4 = [&](int g, float (&l)[4]) {
+        if (g >= groups) {
+            l[0] = l[1] = l[2] = l[3] = -INFINITY;
+        } else if (BF16 && !few) {
+            const uint2 u = reinterpret_cast<const uint2 *>(held)[g];
+            l[0] = __uint_as_float(u.x << 16);
+            l[1] = __uint_as_float(u.x & 0xffff0000u);
+            l[2] = __uint_as_float(u.y << 16);
+            l[3] = __uint_as_float(u.y & 0xffff0000u);
+        } else {
+            const float4 u = few ? reinterpret_cast<const float4 *>(s.cand)[g]
+                                 : reinterpret_cast<const float4 *>(held)[g];
+            l[0] = u.x;
+            l[1] = u.y;
+            l[2] = u.z;
+            l[3] = u.w;
+        }
+    };
+    auto store4 = [&](int g, const float (&l)[4]) {
+        if (BF16 && !few)
+            reinterpret_cast<uint2 *>(held)[g] =
+                make_uint2(__float_as_uint(l[0]) >> 16 | (__float_as_uint(l[1]) & 0xffff0000u),
+                           __float_as_uint(l[2]) >> 16 | (__float_as_uint(l[3]) & 0xffff0000u));
+        else if (few)
+            reinterpret_cast<float4 *>(s.cand)[g] = make_float4(l[0], l[1], l[2], l[3]);
+        else
+            reinterpret_cast<float4 *>(held)[g] = make_float4(l[0], l[1], l[2], l[3]);
+    };
+
+    // ---- the largest logit m, and a logit that at least k are not below ----
+    // (the least over the cluster's warps of the ceil(k / warps)-th largest of
+    // the threads' largest)
+    float m, low = -INFINITY;
+    {
+        const uint32_t key = key_of(mine), top = __reduce_max_sync(kFull, key);
+        uint32_t nth = kKeyNone;
+        if (k < a.vocab) {
+            const long long n = (k + C * kWarps - 1) / (C * kWarps);
+            int above = 0;
+#pragma unroll
+            for (int d = 1; d < 32; ++d) {
+                const uint32_t o = __shfl_xor_sync(kFull, key, d);
+                above += o > key || (o == key && (lane ^ d) < lane);
+            }
+            nth = n <= 32 ? __reduce_max_sync(kFull, above == n - 1 ? key : 0u) : kKeyNone;
+        }
+        if (lane == 0) {
+            atomicMax(&s.key_max, top);
+            atomicMin(&s.key_min, nth);
+        }
+        __syncthreads();
+        const int t = exchange(s.key_max, s.key_min, 0);
+        uint32_t most = 0, least = kOne;
+        for (int r = 0; r < C; ++r) {
+            most = max(most, (uint32_t)s.xch[t][0][r]);
+            least = min(least, (uint32_t)s.xch[t][1][r]);
+        }
+        if (most <= kKeyNone) {  // the same in every CTA
+            if (rank == 0 && tid == 0) {
+                a.tokens[row] = -1;
+                if (a.logprobs) a.logprobs[row] = -INFINITY;
+            }
+            return;
+        }
+        m = logit_of(most);
+        low = logit_of(max(least, kKeyNone + 1));
+    }
+    if (m == INFINITY) {  // the infinite ones alone have weight, and the same
+        for (int g = tid; g < groups; g += kThreads) {
+            float l[4];
+            load4(g, l);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) l[i] = l[i] == INFINITY ? 0.f : -INFINITY;
+            store4(g, l);
+        }
+        m = 0.f;
+        low = -3.4028234e38f;
+    }
+
+    // ---- a small top-k leaves few candidates: those not below `low`, in index order ----
+    if (k < a.vocab && k <= kCand / 4) {
+        const int chunks = (groups + kThreads - 1) / kThreads;
+        for (int it = 0; it < chunks; ++it) {
+            float l[4];
+            load4(it * kThreads + tid, l);
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) n += l[i] >= low;
+            n = __reduce_add_sync(kFull, n);
+            if (lane == 0) s.seg[it * kWarps + warp] = n;
+        }
+        __syncthreads();
+        u64 n_all;
+        const u64 before = scan(tid < chunks * kWarps ? s.seg[tid] : 0, n_all);
+        // (a CTA has at most 512 segments)
+        if (tid < chunks * kWarps) s.seg[tid] = before;
+        const int t = exchange(n_all, 0, 0);
+        bool fit = true;  // in every CTA of the cluster, which all go one way
+        for (int r = 0; r < C; ++r) fit = fit && s.xch[t][0][r] <= kCand;
+        if (fit) {
+            for (int it = 0; it < chunks; ++it) {
+                const int g = it * kThreads + tid;
+                float l[4];
+                load4(g, l);
+                int n = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) n += l[i] >= low;
+                int at = n;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int y = __shfl_up_sync(kFull, at, d);
+                    if (lane >= d) at += y;
+                }
+                at += (int)s.seg[it * kWarps + warp] - n;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (l[i] >= low) {
+                        s.cand[at] = l[i];
+                        s.cand_at[at++] = base + 4 * g + i;
+                    }
+            }
+            few = true;
+            groups = ((int)n_all + 3) / 4;
+            if (tid < 4 * groups - (int)n_all) s.cand[n_all + tid] = -INFINITY;
+            __syncthreads();
+        }
+    }
+
+    // (l - m) / T as binary32 division rounds it.  With r = 1 / T rounded, q =
+    // rn(x r), the exact remainder x - q T and one more fused step give the
+    // quotient rounded to nearest (Markstein, 1990) unless T's significand is
+    // all ones; quotients below -100 have weight 0 and need no care.
+    const float rT = __frcp_rn(T);
+    const bool quick = T > 1e-18f && T < 1e18f && (__float_as_uint(T) & 0x7fffffu) != 0x7fffffu;
+    auto quick_e = [&](float l) {
+        const float d = l - m, q = d * rT;
+        return expf(q < -100.f ? -INFINITY : fmaf(fmaf(-q, T, d), rT, q));
+    };
+    auto es_of = [&](const float (&l)[4], float (&e)[4]) {  // four, so that their steps overlap
+        if (quick) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[i] = quick_e(l[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[i] = expf((l[i] - m) / T);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (l[i] == m) e[i] = 1.f;
+    };
+    auto code_of = [](float e) { return __float2uint_rn(e * 4294967296.f); };  // 2^32 saturates
+    auto weight = [&](float l) {
+        return l == m ? kOne : code_of(quick ? quick_e(l) : expf((l - m) / T));
+    };
+
+    // ---- the threshold of a sum over the logits from `from` up ----
+    // Finds the largest t with the sum of f over logits > t below the target
+    // (then s.above), leaves its key in s.cut and how many have it in s.equal;
+    // false if the sum of all is below the target, which thread 0 makes of it
+    // (s.target).
+    auto search = [&](auto weights, float from, float per_logit, auto target_of) {
+        constexpr bool kWeights = decltype(weights)::value;
+        float lo = from, hi = m;  // logits considered
+        u64 target = 0, above = 0;
+        for (int level = 0;; ++level) {
+            const uint32_t k_hi = key_of(hi);
+            const int shift = level ? max(0, 21 - __clz(k_hi - key_of(lo))) : 0;
+            // Bins in order of falling logits: of the first level by a linear map
+            // (adding 2^23 rounds to the whole number), of later ones by key.
+            auto linear = [&](float l) { return fminf((m - l) * per_logit, (float)(kBins - 1)) + 8388608.f; };
+            auto bin_of = [&](float l) {
+                return level ? (k_hi - key_of(l)) >> shift
+                             : __float_as_uint(linear(l)) & (2 * kBins - 1);
+            };
+            for (int i = tid; i < kBins; i += kThreads) {
+                s.lo[i] = 0;
+                if (kWeights) s.hi[i] = 0;
+            }
+            if (tid == 0) {
+                s.list_n = 0;
+                s.key_min = kOne;
+                s.key_max = 0;
+            }
+            __syncthreads();
+            for (int g = tid; g - lane < groups; g += kThreads) {
+                float l[4];
+                load4(g, l);
+                bool in[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) in[i] = l[i] >= lo && l[i] <= hi;
+                if (!__any_sync(kFull, in[0] | in[1] | in[2] | in[3])) continue;
+                uint32_t w[4];
+                if (kWeights) {
+                    float e[4];
+                    es_of(l, e);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        w[i] = code_of(e[i]);
+                        in[i] = in[i] && w[i];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (!in[i]) continue;
+                    const uint32_t bin = bin_of(l[i]);
+                    if (kWeights) {
+                        const u64 v = wide(w[i]);
+                        atomicAdd(&s.lo[bin], (uint32_t)v & 0xffffu);
+                        atomicAdd(&s.hi[bin], (uint32_t)(v >> 16));
+                    } else {
+                        atomicAdd(&s.lo[bin], 1u);
+                    }
+                }
+            }
+            sync();
+            // The bins' sums over the cluster: each CTA takes 1 / C of the bins,
+            // one or two a thread in order, and tells the others its total.
+            const int per_cta = kBins / C, per_thread = max(1, per_cta / kThreads);
+            u64 v[2] = {0, 0};
+            if (tid * per_thread < per_cta) {
+                const int i0 = rank * per_cta + tid * per_thread;
+                for (int r = 0; r < C; ++r) {
+                    const Shared *o = of(r);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        if (i < per_thread)
+                            v[i] += o->lo[i0 + i] + (kWeights ? (u64)o->hi[i0 + i] << 16 : 0);
+                }
+            }
+            u64 total;
+            u64 before = scan(v[0] + v[1], total);
+            if (C > 1) {
+                const int t = exchange(total, 0, 0);
+                total = 0;
+                for (int r = 0; r < C; ++r) {
+                    if (r < rank) before += s.xch[t][0][r];
+                    total += s.xch[t][0][r];
+                }
+            }
+            if (level == 0) {
+                if (tid == 0) s.target = target_of(total);
+                __syncthreads();
+                target = s.target;
+                if (target > total) return false;  // (the same in every CTA)
+            }
+            before += above;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                if (before < target && before + v[i] >= target)
+                    for (int r = 0; r < C; ++r) {
+                        Shared *o = of(r);
+                        o->bin = rank * per_cta + tid * per_thread + i;
+                        o->above = before;
+                    }
+                before += v[i];
+            }
+            sync();
+            const uint32_t bin = (uint32_t)s.bin;
+            above = s.above;
+            // what is in the bin
+            uint32_t kmin = kOne, kmax = 0;
+            const float in_bin = (float)bin + 8388608.f;
+            for (int g = tid; g < groups; g += kThreads) {
+                float l[4];
+                load4(g, l);
+                uint32_t in = 0;
+                if (level == 0) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        in |= (uint32_t)(linear(l[i]) == in_bin && l[i] >= lo) << i;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        in |= (uint32_t)(l[i] >= lo && l[i] <= hi && bin_of(l[i]) == bin) << i;
+                }
+                if (!in) continue;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (!(in >> i & 1)) continue;
+                    const uint32_t key = key_of(l[i]);
+                    kmin = min(kmin, key);
+                    kmax = max(kmax, key);
+                    const uint32_t n = atomicAdd(&s.list_n, 1u);
+                    if (n < kList) s.list[n] = key;
+                }
+            }
+            kmin = __reduce_min_sync(kFull, kmin);
+            kmax = __reduce_max_sync(kFull, kmax);
+            if (lane == 0 && kmax) {
+                atomicMin(&s.key_min, kmin);
+                atomicMax(&s.key_max, kmax);
+            }
+            __syncthreads();
+            const int t = exchange(s.list_n, s.key_min, s.key_max);
+            u64 n = 0;
+            for (int r = 0; r < C; ++r) {
+                n += s.xch[t][0][r];
+                kmin = min(kmin, (uint32_t)s.xch[t][1][r]);
+                kmax = max(kmax, (uint32_t)s.xch[t][2][r]);
+            }
+            if (kmin == kmax) {  // one key
+                if (tid == 0) {
+                    s.cut = kmin;
+                    s.above = above;
+                    s.equal = n;
+                }
+                break;
+            }
+            if (n <= kList) {
+                int at = 0;
+                for (int r = 0; r < C; ++r) {
+                    const Shared *o = of(r);
+                    const int nr = (int)s.xch[t][0][r];
+                    for (int i = tid; i < nr; i += kThreads) {
+                        const uint32_t key = o->list[i];
+                        s.all[at + i] = make_uint2(key, kWeights ? weight(logit_of(key)) : 1u);
+                    }
+                    at += nr;
+                }
+                __syncthreads();
+                if (tid < (int)n) {
+                    const uint32_t key = s.all[tid].x;
+                    u64 more = 0, equal = 0, count = 0;
+#pragma unroll 4
+                    for (int i = 0; i < (int)n; ++i) {
+                        const uint2 o = s.all[i];
+                        const u64 w = wide(o.y);
+                        if (o.x > key) more += w;
+                        if (o.x == key) {
+                            equal += w;
+                            ++count;
+                        }
+                    }
+                    // threads of equal keys write the same
+                    if (above + more < target && above + more + equal >= target) {
+                        s.cut = key;
+                        s.above = above + more;
+                        s.equal = count;
+                    }
+                }
+                break;
+            }
+            lo = logit_of(kmin);
+            hi = logit_of(kmax);
+            sync();  // lists and bins may be written again
+        }
+        sync();
+        return true;
+    };
+
+    // ---- kept: keys > cut, and the first `ties` of those equal to it ----
+    uint32_t cut = kKeyNone;
+    u64 ties = 0, equal = 0;  // of `equal` tokens equal to the cut `ties` stay
+    if (k < a.vocab) {
+        const float span = m - low;
+        const float per_logit = span > 0.f && span < 3e38f ? (kBins - 1) / span : 0.f;
+        if (search(std::false_type(), low, per_logit, [&](u64) { return (u64)k; })) {
+            cut = s.cut;
+            ties = (u64)k - s.above;
+            equal = s.equal;
+        }  // else fewer than k tokens are above -inf: all stay
+    }
+    if (p < 1.f) {
+        const u64 w_cut = ties ? wide(weight(logit_of(cut))) : 0;
+        const bool here = search(std::true_type(), logit_of(cut + 1), (kBins - 1) / kNats / T, [&](u64 total) {
+            s.sum = total;
+            const u64 all = total + ties * w_cut;
+            const double want = ceil((double)p * (double)all);
+            const u64 target = want < 1.0 ? 1 : (u64)want;
+            return target < all ? target : all;
+        });
+        if (here) {
+            cut = s.cut;
+            const u64 w = wide(weight(logit_of(cut)));
+            ties = (s.target - s.above + w - 1) / w;
+            equal = s.equal;
+        } else {  // it ends among the tokens equal to the top-k cut
+            ties = (s.target - s.sum + w_cut - 1) / w_cut;
+        }
+    }
+    // of the tokens equal to the cut the first `ties` in index order stay; the
+    // others are taken out
+    const float at_cut = logit_of(cut);
+    if (ties && ties < equal) {
+        for (int g0 = warp * 32; g0 < groups; g0 += kThreads) {
+            float l[4];
+            load4(g0 + lane, l);
+            uint32_t n = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) n += l[i] == at_cut;
+            n = __reduce_add_sync(kFull, n);
+            if (lane == 0) s.seg[g0 / 32] = n;
+        }
+        __syncthreads();
+        u64 here;
+        const u64 ex = scan(tid < (groups + 31) / 32 ? s.seg[tid] : 0, here);
+        if (tid < (groups + 31) / 32) s.seg[tid] = ex;
+        const int t = exchange(here, 0, 0);
+        u64 before = 0;
+        for (int r = 0; r < rank; ++r) before += s.xch[t][0][r];
+        const u64 left = ties > before ? ties - before : 0;
+        if (left < here) {
+            for (int g0 = warp * 32; g0 < groups; g0 += kThreads) {
+                const int g = g0 + lane;
+                const u64 end = g0 / 32 + 1 < (groups + 31) / 32 ? s.seg[g0 / 32 + 1] : here;
+                if (end <= left || end == s.seg[g0 / 32]) continue;  // all stay, or none is here
+                float l[4];
+                load4(g, l);
+                uint32_t c = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) c += l[i] == at_cut;
+                uint32_t at = c;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const uint32_t y = __shfl_up_sync(kFull, at, d);
+                    if (lane >= d) at += y;
+                }
+                u64 place = s.seg[g0 / 32] + at - c;
+                if (c) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (l[i] == at_cut && place++ >= left) l[i] = -INFINITY;
+                    store4(g, l);
+                }
+            }
+        }
+        __syncthreads();  // seg is written again
+    }
+    const float from = ties ? at_cut : logit_of(cut + 1);  // kept by top-k and top-p
+    auto kept = [&](const float (&l)[4], u64 (&w)[4]) {
+        float e[4];
+        es_of(l, e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = l[i] < from || e[i] < floor_p ? 0 : wide(code_of(e[i]));
+    };
+
+    // ---- the token at which the running sum in index order passes r ----
+    for (int g0 = warp * 32; g0 < groups; g0 += kThreads) {  // segments of 32 groups
+        float l[4];
+        load4(g0 + lane, l);
+        u64 sum = 0;
+        if (__any_sync(kFull, fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])) >= from)) {
+            u64 w[4];
+            kept(l, w);
+            sum = (w[0] + w[1]) + (w[2] + w[3]);
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(kFull, sum, d);
+        }
+        if (lane == 0) s.seg[g0 / 32] = sum;
+    }
+    __syncthreads();
+    const int segs = (groups + 31) / 32;
+    u64 mine_all;
+    const u64 seg = tid < segs ? s.seg[tid] : 0;
+    const u64 seg_before = scan(seg, mine_all);
+    u64 total = 0, before = 0;
+    {
+        const int t = exchange(mine_all, 0, 0);
+        for (int r = 0; r < C; ++r) {
+            if (r < rank) before += s.xch[t][0][r];
+            total += s.xch[t][0][r];
+        }
+    }
+    if (tid == 0) {
+        float u = a.uniforms[row];
+        if (!(u >= 0.f)) u = 0.f;
+        const u64 r = (u64)((double)u * (double)total);
+        s.target = r < total ? r : total - 1;
+    }
+    __syncthreads();
+    u64 r = s.target;
+    if (r < before || r >= before + mine_all) return;  // another CTA of the cluster has it
+    r -= before;
+    if (seg_before <= r && r < seg_before + seg) {
+        s.where = tid;
+        s.above = seg_before;
+    }
+    __syncthreads();
+    if (warp != 0) return;
+    r -= s.above;
+    const int g = s.where * 32 + lane;
+    float l[4];
+    load4(g, l);
+    u64 w[4];
+    kept(l, w);
+    const u64 inc = (w[0] + w[1]) + (w[2] + w[3]);
+    u64 at = warp_scan(inc) - inc;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (at <= r && r < at + w[i]) {
+            a.tokens[row] = few ? s.cand_at[4 * g + i] : base + 4 * g + i;
+            if (a.logprobs) {
+                const float z = l[i] == m ? 0.f : (l[i] - m) / T;
+                a.logprobs[row] = z - logf((float)((double)total * (1.0 / 4294967296.0)));
+            }
+        }
+        at += w[i];
+    }
+}
+
+// ---- longer rows --------------------------------------------------------------------
+// Rows of more than kMaxRowCtas * kMaxSlice logits: one CTA per row, which reads
+// the row (from L2 at best) for every step.
+template <bool BF16>
+__global__ void __launch_bounds__(kLongThreads) long_row_kernel(const SampleArgs a) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     __shared__ u64 sums[32];
@@ -85,7 +748,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
 
     auto add = [](u64 x, u64 y) { return x + y; };
     uint32_t mine = 0;
-    for (int i = tid; i < V; i += kThreads) mine = max(mine, key(i));
+    for (int i = tid; i < V; i += kLongThreads) mine = max(mine, key(i));
     const uint32_t top =
         (uint32_t)block_reduce<u64>(mine, sums, [](u64 x, u64 y) { return x > y ? x : y; });
     if (top <= kKeyNone) {
@@ -105,7 +768,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
         for (int shift = 24; shift >= 0; shift -= 8) {
             if (tid < 256) hist[tid] = 0;
             __syncthreads();
-            for (int i = tid; i < V; i += kThreads) {
+            for (int i = tid; i < V; i += kLongThreads) {
                 const uint32_t x = key(i);
                 if (x >= least && (shift == 24 || (x >> (shift + 8)) == (t >> (shift + 8))))
                     atomicAdd(&hist[(x >> shift) & 255], f(x));
@@ -126,7 +789,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     };
     auto count_equal = [&](uint32_t t) {
         u64 n = 0;
-        for (int i = tid; i < V; i += kThreads) n += key(i) == t;
+        for (int i = tid; i < V; i += kLongThreads) n += key(i) == t;
         return block_reduce<u64>(n, sums, add);
     };
 
@@ -141,7 +804,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     auto weight = [&](uint32_t x) { return w_of(e_of(x, top, m, T)); };
     if (p < 1.f) {
         u64 s = 0;
-        for (int i = tid; i < V; i += kThreads) {
+        for (int i = tid; i < V; i += kLongThreads) {
             const uint32_t x = key(i);
             if (x > cut) s += weight(x);
         }
@@ -166,7 +829,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     __syncthreads();
     if (count_equal(cut) > ties) {
         u64 seen = 0;
-        for (int i0 = 0; i0 < V; i0 += kThreads) {
+        for (int i0 = 0; i0 < V; i0 += kLongThreads) {
             const int i = i0 + tid;
             const bool eq = i < V && key(i) == cut;
             const unsigned bal = __ballot_sync(kFull, eq);
@@ -192,7 +855,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
         return floor_p > 0.f && !(e >= floor_p) ? 0 : w_of(e);
     };
     u64 total = 0;
-    for (int i = tid; i < V; i += kThreads) total += kept(i);
+    for (int i = tid; i < V; i += kLongThreads) total += kept(i);
     total = block_reduce<u64>(total, sums, add);
     float u = a.uniforms[row];
     if (!(u >= 0.f)) u = 0.f;
@@ -201,7 +864,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     // the token at which the running sum in index order passes r
     __shared__ int s_token;
     u64 seen = 0;
-    for (int i0 = 0; i0 < V; i0 += kThreads) {
+    for (int i0 = 0; i0 < V; i0 += kLongThreads) {
         const int i = i0 + tid;
         const u64 w = i < V ? kept(i) : 0;
         u64 x = w;
@@ -262,35 +925,70 @@ __global__ void __launch_bounds__(kScanWarps * 32)
 }
 
 template <typename... Params, typename... Args>
-cudaError_t launch_pdl(void (*kernel)(Params...), dim3 grid, dim3 block, cudaStream_t stream,
-                       Args... args) {
+cudaError_t launch_pdl(void (*kernel)(Params...), dim3 grid, dim3 block, unsigned cluster,
+                       size_t smem, cudaStream_t stream, Args... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
+
+template <bool BF16>
+cudaError_t sample_launch_t(const SampleArgs &a, cudaStream_t stream) {
+    const long long rows = (long long)a.B * a.W;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const int sms = attn_grid_size(dev);
+    if (sms <= 0) return cudaErrorInvalidDevice;
+    // CTAs per row: enough to hold the row, and as many as fill the SMs
+    constexpr int kMaxSlice = kSliceBytes / (BF16 ? 2 : 4);
+    const int hold = (int)(((long long)a.vocab + kMaxSlice - 1) / kMaxSlice);
+    if (hold > kMaxRowCtas)
+        return launch_pdl(long_row_kernel<BF16>, dim3((unsigned)rows), dim3(kLongThreads), 1, 0,
+                          stream, a);
+    int C = 1;  // a power of two: the bins divide by it
+    while (C < kMaxRowCtas && (C < hold || (rows * C * 2 <= sms && a.vocab > C * 4 * kThreads)))
+        C *= 2;
+    const int slice = ((a.vocab + C - 1) / C + 3) / 4 * 4;
+    const uintptr_t bytes = 4 * (BF16 ? 2 : 4);
+    const bool vec = a.row_stride % 4 == 0 && reinterpret_cast<uintptr_t>(a.logits) % bytes == 0;
+    const dim3 grid((unsigned)(rows * C)), block(kThreads);
+    const size_t smem = (size_t)slice * (BF16 ? 2 : 4);
+    static std::atomic<bool> configured[64];  // the shared-memory opt-in, once per device
+    if (dev >= 64 || !configured[dev].load(std::memory_order_acquire)) {
+        e = cudaFuncSetAttribute(sample_kernel<BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 kSliceBytes);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) configured[dev].store(true, std::memory_order_release);
+    }
+    return launch_pdl(sample_kernel<BF16>, grid, block, C, smem, stream, a, slice, vec);
 }
 
 }  // namespace
 
 cudaError_t sample_launch(const SampleArgs &a, cudaStream_t stream) {
-    const long long rows = (long long)a.B * a.W;
-    if (rows == 0) return cudaSuccess;
-    return a.bf16 ? launch_pdl(sample_kernel<true>, dim3((unsigned)rows), dim3(kThreads), stream, a)
-                  : launch_pdl(sample_kernel<false>, dim3((unsigned)rows), dim3(kThreads), stream, a);
+    if ((long long)a.B * a.W == 0) return cudaSuccess;
+    return a.bf16 ? sample_launch_t<true>(a, stream) : sample_launch_t<false>(a, stream);
 }
 
 cudaError_t sample_accept_launch(const SampleArgs &a, const int32_t *draft, int32_t *accepted,
                                  int32_t *next_token, int32_t *committed, cudaStream_t stream) {
     if (a.B == 0) return cudaSuccess;
     return launch_pdl(sample_accept_kernel, dim3((unsigned)((a.B + kScanWarps - 1) / kScanWarps)),
-                      dim3(kScanWarps * 32), stream, static_cast<const int32_t *>(a.tokens), draft,
-                      a.B, a.W, accepted, next_token, committed);
+                      dim3(kScanWarps * 32), 1, 0, stream, static_cast<const int32_t *>(a.tokens),
+                      draft, a.B, a.W, accepted, next_token, committed);
 }
 
 }  // namespace das

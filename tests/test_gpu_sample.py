@@ -184,3 +184,57 @@ def test_another_stream():
     s.synchronize()
     b = das.das_sample(logits, u)
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("B,W,V,dtype", [(1, 1, 300001, torch.float32), (1, 2, 600007, torch.bfloat16),
+                                         (1, 1, 262144, torch.float32), (40, 4, 70001, torch.bfloat16),
+                                         (160, 1, 33000, torch.float32)])
+def test_long_rows_and_many_rows(B, W, V, dtype):
+    """Rows past what a cluster holds, rows of several CTAs, and more rows than SMs."""
+    g = torch.Generator(device="cuda").manual_seed(V)
+    logits = (3 * torch.randn((B, W, V), generator=g, device="cuda")).to(dtype)
+    u = torch.rand((B, W), generator=g, device="cuda")
+    some = [0, B // 2, B - 1] if B > 2 else list(range(B))
+    par = ([0.8] * B, [0, 900, 40][:1] * B, [0.9] * B, [0.0] * B)
+    for k, p, m in ((0, 0.9, 0.0), (900, 0.95, 0.001), (40, 1.0, 0.0), (0, 1.0, 0.0)):
+        kw = dict(temperature=f32([0.8] * B), top_k=dev_i32([k] * B), top_p=f32([p] * B), min_p=f32([m] * B))
+        ids, logp = das.das_sample(logits, u, **kw)
+        part, part_u = logits[some].contiguous(), u[some].contiguous().cpu().numpy()
+        want = [[ref.sample_row(part[b, i].double().cpu().numpy(), e32(part[b, i].float(), float(np.float32(0.8))),
+                                float(np.float32(0.8)), k, float(np.float32(p)), float(np.float32(m)),
+                                part_u[b, i])[0] for i in range(W)] for b in range(len(some))]
+        assert ids[some].tolist() == want, (k, p, m)
+
+
+@pytest.mark.parametrize("kind", ["outlier", "lowest", "steps", "cluster", "half"])
+@pytest.mark.parametrize("filters", [(0, 0.7, 0.0), (37, 1.0, 0.0), (2500, 0.9, 0.0), (600, 0.5, 0.1)])
+def test_rows_that_crowd_one_bin(kind, filters):
+    """Distributions that leave many distinct logits in one bin of the first histogram."""
+    g = torch.Generator(device="cuda").manual_seed(7)
+    V = 20011
+    x = torch.randn((2, 3, V), generator=g, device="cuda")
+    if kind == "outlier":
+        x[..., 5] = 1e6
+        x[1] *= 1e-3
+    elif kind == "lowest":               # masked by the type's lowest value
+        x[..., ::3] = torch.finfo(torch.float32).min
+        x[1, :, 100:] = torch.finfo(torch.float32).min
+    elif kind == "steps":                # a few values only, next to each other
+        x = 1 + torch.randint(0, 300, x.shape, generator=g, device="cuda") * 2.0 ** -23
+    elif kind == "cluster":
+        x = 5 + x * 1e-5
+    else:                                # one half of the vocabulary is masked
+        x[..., : V // 2 + 7] = -torch.inf
+    k, p, m = filters
+    rng = np.random.default_rng(8)
+    check(x.contiguous(), rng.random((2, 3)), [1.0, 0.3], [k, k], [p, p], [m, m])
+
+
+@pytest.mark.parametrize("T", [float(np.nextafter(np.float32(2), np.float32(0))), 1e-19, 3e19, 1.0 / 3, 0.7 + 2 ** -24])
+def test_temperatures_whose_quotients_round_awkwardly(T):
+    g = torch.Generator(device="cuda").manual_seed(9)
+    scale = min(max(T, 1e-19), 1e19)
+    x = torch.randn((1, 8, 3001), generator=g, device="cuda") * 4 * scale
+    u = np.random.default_rng(10).random((1, 8))
+    check(x, u, [T], [0], [0.95], [0.0])
+    check(x, u, [T], [300], [1.0], [0.0])
