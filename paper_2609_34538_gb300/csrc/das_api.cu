@@ -310,7 +310,9 @@ das_status attention_paged(const das_kv_cache_paged *c, int layer, int key_depth
     const int G = num_q_heads / c->kv_heads;
     if (max_block > kTileKeys || (long long)G * max_block > kMaxRows || batch > (1 << 20) ||
         (long long)batch * c->kv_heads * G * max_block > 0x7fffffffLL ||
-        (long long)c->pages * c->kv_heads > 0x7fffffffLL)
+        (long long)c->pages * c->kv_heads > 0x7fffffffLL ||
+        // tiles of one CTA, if every table is full, are counted in 32 bits
+        (double)batch * c->kv_heads * (max_pages + 1.0) > 64.0 * (1 << 30))
         return DAS_ERR_UNSUPPORTED;
     const size_t need = das_workspace_size_paged(c, batch, num_q_heads, max_block);
     if (need == 0) return DAS_ERR_CUDA;

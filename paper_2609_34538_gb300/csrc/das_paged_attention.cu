@@ -30,8 +30,9 @@
 // whole pair writes the output, others a partial (O / l, lse), which
 // paged_merge_kernel joins.
 //
-// One CTA = four softmax warps + one TMA warp + two MMA warps + four warps
-// that prepare each segment's queries (split) and block keys and values (bf16,
+// One CTA = two groups of four softmax warps, which take turns at the tiles
+// (one warp per sub-partition left its latencies bare), + one TMA warp + two
+// MMA warps + four warps that prepare each segment's queries (split) and block keys and values (bf16,
 // with rows past the block zero).  The block tile runs bf16 products: S with
 // M = 64 (the hi lanes), P V with P split into two bf16 parts.
 // Every wait is bounded (2 s); a time-out sets the status word and ends the
@@ -50,18 +51,21 @@ namespace {
 using namespace t5;
 
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kSoftWarps = 4;
-constexpr int kProducerWarp = 4;
-constexpr int kPvWarp = 5;
-constexpr int kSWarp = 6;
-constexpr int kQueryWarp0 = 7;
+constexpr int kGroupWarps = 4;     // softmax warps of one group, a TMEM quadrant each
+constexpr int kGroups = 2;         // group g takes the tiles k with k % 2 = g
+constexpr int kSoftWarps = kGroups * kGroupWarps;
+constexpr int kProducerWarp = kSoftWarps;
+constexpr int kPvWarp = kProducerWarp + 1;
+constexpr int kSWarp = kPvWarp + 1;
+constexpr int kQueryWarp0 = kSWarp + 1;
 constexpr int kQueryWarps = 4;
 constexpr int kThreads = (kQueryWarp0 + kQueryWarps) * 32;
 constexpr int kRows = 64;          // query rows per pair
-constexpr int kSBufs = 4;          // S buffers in tensor memory
-constexpr int kTmemCols = 512;     // S [0, 256), O [256, 256 + D), P 2 x 16 columns
+constexpr int kSBufs = 3;          // S buffers in tensor memory
+constexpr int kTmemCols = 512;     // S [0, 192), each group's O, each group's P (16 columns)
 constexpr int kOCol = kSBufs * kTileKeys;
-constexpr int kPCol = 384;
+constexpr int kOStep = 128;
+constexpr int kPCol = kOCol + kGroups * kOStep;
 constexpr float kHead = 5.f, kWindow = 3.f;
 constexpr float kLoInv = 0.0625f;  // the lo rows hold 16 times the remainder
 constexpr uint32_t kLoLanes = 16u << 16;
@@ -139,7 +143,7 @@ __device__ long long all_tiles(const PagedAttnParams &p) {  // whole warp
 }
 
 // This CTA's number of tiles and its first one (a whole warp executes this).
-__device__ long long plan(const PagedAttnParams &p, Walk &w) {
+__device__ int plan(const PagedAttnParams &p, Walk &w) {
     const int lane = threadIdx.x & 31;
     const Split sp = split_of(p, all_tiles(p));
     const long long q[2] = {udiv((long long)blockIdx.x * sp.W, p.num_ctas),
@@ -188,8 +192,22 @@ __device__ long long plan(const PagedAttnParams &p, Walk &w) {
         run_w += ((long long)all + (long long)sp.beta * nseq) * p.Hkv;
         run_t += (long long)all * p.Hkv;
     }
-    return max(0ll, at[1] - at[0]);
+    return (int)max(0ll, at[1] - at[0]);  // the host admits no more than 2^30 a CTA
 }
+
+// A place in a ring of N and the parity of its present phase, kept by counting
+// (a 64-bit remainder is a long dependent sequence).
+template <int N>
+struct Ring {
+    int i = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next() {
+        if (++i == N) {
+            i = 0;
+            phase ^= 1;
+        }
+    }
+};
 
 // ---- shared memory ------------------------------------------------------------------
 struct TileInfo {
@@ -216,7 +234,8 @@ struct Layout {
     static constexpr int kBars = 2 * kStages + 4 + 2 + 2 * kSBufs + 4 + 2;
     static constexpr int kInfoOff = (kBarOff + kBars * 8 + 15) / 16 * 16;
     static constexpr int kExpOff = kInfoOff + kStages * 16;
-    static constexpr int kMiscOff = kExpOff + 2 * kRows * 4;
+    static constexpr int kMlOff = kExpOff + 2 * kRows * 4;  // (m, l) of each group's rows
+    static constexpr int kMiscOff = kMlOff + kGroups * kRows * 8;
     static constexpr int kBytes = kMiscOff + 64 + 1024;  // + alignment slack
     static constexpr uint32_t kSwizzle = D == 128 ? 2 : 4;  // 128- or 64-byte rows
     static_assert(kTile % 1024 == 0 && kQ8Off % 1024 == 0 && kPbOff % 1024 == 0, "alignment");
@@ -353,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(b_qready + 8 * i, kQueryWarps);
             // the segment's last S, and every softmax warp once it has read e
             mbar_init(b_qfree + 8 * i, 1 + kSoftWarps);
-            mbar_init(b_pready + 8 * i, kSoftWarps);
+            mbar_init(b_pready + 8 * i, kGroupWarps);
             mbar_init(b_pvdone + 8 * i, 1);
             mbar_init(b_drain + 8 * i, 1);
         }
@@ -361,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_init(b_bfree, 1);
         for (int i = 0; i < kSBufs; ++i) {
             mbar_init(b_sready + 8 * i, 1);
-            mbar_init(b_sfree + 8 * i, kSoftWarps);
+            mbar_init(b_sfree + 8 * i, kGroupWarps);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *abort_flag = 0;
@@ -386,7 +405,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     Walk w0;
-    const long long ntiles = plan(p, w0);
+    const int ntiles = plan(p, w0);
     if (blockIdx.x == 0 && warp == 0)
         for (int b = lane; b < p.B; b += 32)
             if (p.prefix_len[b] != prefix_of(p, b) || p.block_len[b] != block_of(p, b))
@@ -395,7 +414,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto waits = [&](uint32_t bar, uint32_t parity) {
         return wait(bar, parity, abort_flag, p.status);
     };
-    long long issued = 0;  // tiles whose loads were issued (the producer's)
+    int issued = 0;           // tiles whose loads were issued (the producer's)
+    Ring<kStages> st;         // the stage of the next page
     if (warp == kProducerWarp) {
         // ================================ producer ===============================
         // Stage s is reused once the P V that read it has completed.  Lane i
@@ -406,7 +426,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         int base = -1, page = -1;
         float ks = 0.f, vs = 0.f;
         bool ok = true;
-        for (long long j = 0; j < ntiles && ok; ++j, walk_next(p, w)) {
+        for (int j = 0; j < ntiles && ok; ++j, walk_next(p, w)) {
             if (j == 0 || w.t == 0) base = -1;
             if (w.t == w.nt - 1) continue;
             if (base < 0 || w.t - base == 32) {
@@ -420,8 +440,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 ks = p.k_scale[tile];
                 vs = fmaxf(p.v_scale[tile], 8.6736174e-19f);  // 2^-60: codes under a 0 scale vanish
             }
-            const int s = (int)(issued % kStages);
-            if (issued >= kStages) ok = waits(b_empty + 8 * s, (uint32_t)((issued / kStages - 1) & 1));
+            const int s = st.i;
+            if (issued >= kStages) ok = waits(b_empty + 8 * s, st.phase ^ 1);
             const int pg = __shfl_sync(kFull, page, w.t - base);
             const float k1 = __shfl_sync(kFull, ks, w.t - base);
             const float v1 = __shfl_sync(kFull, vs, w.t - base);
@@ -441,6 +461,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             __syncwarp();
             ++issued;
+            st.next();
         }
     } else if (warp == kSWarp) {
         // =============================== S = Q K^T ===============================
@@ -452,23 +473,22 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint64_t dkb = sdesc(sbase + Lt::kKbOff, 16, 1024, 2);
         Walk w = w0;
         int seg = -1;
-        long long kp = 0, nblk = 0;
+        uint32_t blk_phase = 0;
+        Ring<kSBufs> sb;
         bool ok = true;
-        for (long long k = 0; k < ntiles && ok; ++k) {
+        for (int k = 0; k < ntiles && ok; ++k) {
             if (k == 0 || w.t == 0) {
                 ++seg;
                 ok = waits(b_qready + 8 * (seg & 1), (uint32_t)((seg >> 1) & 1));
             }
             const bool blk = w.t == w.nt - 1;
-            const int s = (int)(kp % kStages);
-            ok = ok && (blk ? waits(b_bready, (uint32_t)(nblk & 1))
-                            : waits(b_full + 8 * s, (uint32_t)((kp / kStages) & 1)));
-            if (k >= kSBufs)
-                ok = ok && waits(b_sfree + 8 * (int)(k % kSBufs), (uint32_t)((k / kSBufs - 1) & 1));
+            const int s = st.i;
+            ok = ok && (blk ? waits(b_bready, blk_phase) : waits(b_full + 8 * s, st.phase));
+            if (k >= kSBufs) ok = ok && waits(b_sfree + 8 * sb.i, sb.phase ^ 1);
             if (!ok) break;
             fence_after();
             if (elect_one()) {
-                const uint32_t dS = tmem + (uint32_t)((k % kSBufs) * kTileKeys);
+                const uint32_t dS = tmem + (uint32_t)(sb.i * kTileKeys);
                 if (!blk) {
                     const uint64_t a0 = dq8 + (uint64_t)(((seg & 1) * Lt::kQ8) >> 4);
                     const uint64_t b0 = dk8 + (uint64_t)((s * Lt::kStage) >> 4);
@@ -482,12 +502,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                         mma_bf16(dS, dqb + off, dkb + off, idb, kk > 0);
                     }
                 }
-                mma_commit(b_sready + 8 * (int)(k % kSBufs));
+                mma_commit(b_sready + 8 * sb.i);
                 if (blk || k + 1 == ntiles) mma_commit(b_qfree + 8 * (seg & 1));
             }
             __syncwarp();
-            if (blk) ++nblk;
-            else ++kp;
+            if (blk) blk_phase ^= 1;
+            else st.next();
+            sb.next();
             walk_next(p, w);
         }
     } else if (warp == kPvWarp) {
@@ -497,15 +518,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint64_t dv8 = sdesc(sbase + Lt::kTile, 8 * D, 8 * D, Lt::kSwizzle);
         const uint64_t dpb = sdesc(sbase + Lt::kPbOff, 16, 1024, 2);
         const uint64_t dvb = sdesc(sbase + Lt::kVbOff, kRows * 128, 1024, 2);
-        const uint32_t dO = tmem + kOCol;
         Walk w = w0;
-        long long kp = 0;
+        int k_seg = 0;
         bool ok = true;
-        for (long long k = 0; k < ntiles && ok; ++k) {
-            const bool first = k == 0 || w.t == 0, blk = w.t == w.nt - 1;
-            const int s = (int)(kp % kStages);
-            ok = waits(b_pready + 8 * (int)(k & 1), (uint32_t)((k >> 1) & 1));
-            if (!blk) ok = ok && waits(b_full + 8 * s, (uint32_t)((kp / kStages) & 1));
+        for (int k = 0; k < ntiles && ok; ++k) {
+            if (w.t == 0) k_seg = k;
+            const bool first = k - k_seg < kGroups, blk = w.t == w.nt - 1;  // the group's first
+            const uint32_t dO = tmem + kOCol + (uint32_t)((k & 1) * kOStep);
+            const int s = st.i;
+            ok = waits(b_pready + 8 * (k & 1), (uint32_t)(k >> 1) & 1);
+            if (!blk) ok = ok && waits(b_full + 8 * s, st.phase);
             if (!ok) break;
             fence_after();
             if (elect_one()) {
@@ -522,18 +544,18 @@ __global__ void __launch_bounds__(kThreads, 1)
                         mma_bf16(dO, dpb + kk * 2, dvb + (uint64_t)((kk * 2048) >> 4), idb,
                                  !first || kk > 0);
                 }
-                mma_commit(b_pvdone + 8 * (int)(k & 1));
+                mma_commit(b_pvdone + 8 * (k & 1));
                 mma_commit(blk ? b_bfree : b_empty + 8 * s);
             }
             __syncwarp();
-            if (!blk) ++kp;
+            if (!blk) st.next();
             walk_next(p, w);
         }
     } else if (warp >= kQueryWarp0) {
         // ====================== queries, block keys and values ===================
         const int ct = threadIdx.x - kQueryWarp0 * 32;
         Walk w = w0;
-        long long left = ntiles, nblk = 0;
+        int left = ntiles, nblk = 0;
         for (int seg = 0; left > 0; ++seg) {
             const int q = seg & 1;
             if (seg >= 2 && !waits(b_qfree + 8 * q, (uint32_t)(((seg >> 1) - 1) & 1))) break;
@@ -554,24 +576,26 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
     } else {
         // ================================ softmax ================================
-        // thread (warp, lane): row 16 warp + lane % 16, 32 of each tile's keys
-        const int row = warp * 16 + (lane & 15), half = lane >> 4;
+        // Group g takes every second tile, with a reference, sums and an O of
+        // its own; the groups meet at the end of a segment.  Thread (warp,
+        // lane): row 16 (warp % 4) + lane % 16, 32 of a tile's keys.
+        const int group = warp / kGroupWarps, quad = warp % kGroupWarps;
+        const int row = quad * 16 + (lane & 15), half = lane >> 4;
         const int key0 = 32 * half;
-        const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
+        const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
+        const uint32_t o_col = lanes + kOCol + (uint32_t)(group * kOStep);
+        float2 *ml = reinterpret_cast<float2 *>(sm + Lt::kMlOff);
         Walk w = w0;
         float m_ref = -INFINITY, l_sum = 0.f, row_scale = 1.f;
-        int seg = -1, irow = 0, rows_active = 0, seg_t = 0;
-        long long kp = 0;
-        for (long long k = 0; k < ntiles; ++k) {
-            const bool first = k == 0 || w.t == 0, blk = w.t == w.nt - 1;
-            const bool last = blk || k + 1 == ntiles;
-            if (first) {
-                ++seg;
-                seg_t = w.t;
-                m_ref = -INFINITY;
-                l_sum = 0.f;
-                rows_active = p.G * w.T;
-                irow = row / p.G;
+        int k = 0, kp = 0;  // the next tile, and the pages before it
+        for (int seg = 0; k < ntiles; ++seg, walk_pair(p, w)) {
+            const int k_seg = k, k_end = min(ntiles, k + w.nt - w.t);
+            const bool has_blk = w.t + (k_end - k_seg) == w.nt;
+            const int rows_active = p.G * w.T, irow = row / p.G, seg_t = w.t;
+            const bool live = row < rows_active;
+            m_ref = -INFINITY;
+            l_sum = 0.f;
+            {
                 const int q = seg & 1;
                 waits(b_qready + 8 * q, (uint32_t)((seg >> 1) & 1));
                 row_scale = p.scale_log2 *
@@ -579,140 +603,164 @@ __global__ void __launch_bounds__(kThreads, 1)
                 __syncwarp();
                 if (lane == 0) mbar_arrive(b_qfree + 8 * q);
             }
-            const int s = (int)(kp % kStages);
-            float scale = p.scale_log2, lv = 0.f, ivs = 1.f;
-            int n = w.T;
-            if (!blk) {
-                waits(b_full + 8 * s, (uint32_t)((kp / kStages) & 1));
-                const TileInfo ti = info[s];
-                scale = row_scale * ti.ks;
-                lv = ti.lv;
-                ivs = ti.ivs;
-                n = ti.n;
-            }
-            const bool ok_s =
-                waits(b_sready + 8 * (int)(k % kSBufs), (uint32_t)((k / kSBufs) & 1));
-            fence_after();
-            const uint32_t s_addr = lanes + (uint32_t)((k % kSBufs) * kTileKeys);
-            float v[32];
-            {
-                uint32_t a[32];
-                ld_half(s_addr, a);
-                if (!blk) {
-                    uint32_t c[32];
-                    ld_half(s_addr + kLoLanes, c);
-                    ld_wait(a);
-                    ld_wait(c);
+            const int k_blk = has_blk ? k_end - 1 : k_end;  // pages are the tiles before it
+            // Weights of a tile from its scores v (hidden ones -inf), in e; moves the
+            // reference (and rescales O and l) where a score asks for it.  The
+            // exponentials are taken under the present reference while the maximum is
+            // found, and again in the rare tile that moves it.
+            auto weights_of = [&](float (&v)[32], float (&e)[32], float scale, float lv, bool hidden) {
+                auto exps = [&] {
+                    const float off = lv + kHead - (m_ref == -INFINITY ? 0.f : m_ref);
+                    if (hidden) {  // a hidden score stays -inf under a scale of 0
 #pragma unroll
-                    for (int j = 0; j < 32; j += 2)
-                        axpy2(v[j], v[j + 1], kLoInv, __uint_as_float(c[j]),
-                              __uint_as_float(c[j + 1]), __uint_as_float(a[j]),
-                              __uint_as_float(a[j + 1]));
-                } else {
-                    ld_wait(a);
+                        for (int j = 0; j < 32; ++j)
+                            e[j] = v[j] == -INFINITY ? -INFINITY : v[j] * scale + off;
+                    } else {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(a[j]);
-                }
-            }
-            fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(b_sfree + 8 * (int)(k % kSBufs));
-            const bool live = row < rows_active && ok_s;
-            if (blk || n < kTileKeys) {  // keys from lim on are hidden from this row
-                const int lim = !live ? 0 : (blk ? min(n, irow + 1) : n);
+                        for (int j = 0; j < 32; j += 2)
+                            fma2(e[j], e[j + 1], v[j], v[j + 1], scale, off);
+                    }
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (key0 + j >= lim) v[j] = -INFINITY;
-            }
-            float mt;
-            {
+                    for (int j = 0; j < 32; ++j) e[j] = ex2(e[j]);
+                };
+                exps();
                 float x[11];
 #pragma unroll
                 for (int j = 0; j < 10; ++j) x[j] = max3(v[3 * j], v[3 * j + 1], v[3 * j + 2]);
                 x[10] = fmaxf(v[30], v[31]);
-                mt = fmaxf(max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]),
-                                max3(x[6], x[7], x[8])),
-                           fmaxf(x[9], x[10]));
-            }
-            mt = fmaxf(mt, __shfl_xor_sync(kFull, mt, 16));
-            // a masked score stays -inf under a scale of 0
-            mt = mt == -INFINITY ? -INFINITY : mt * scale + lv;
-            if (first) {
-                m_ref = mt;
-            } else {
+                float mt = fmaxf(max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]),
+                                      max3(x[6], x[7], x[8])),
+                                 fmaxf(x[9], x[10]));
+                mt = fmaxf(mt, __shfl_xor_sync(kFull, mt, 16));
+                mt = mt == -INFINITY ? -INFINITY : mt * scale + lv;
                 const bool jump = live && mt > m_ref + kWindow;
                 if (__any_sync(kFull, jump)) {
-                    // O is stable once P V of tile k - 1 is done
-                    waits(b_pvdone + 8 * (int)((k - 1) & 1), (uint32_t)(((k - 1) >> 1) & 1));
-                    fence_after();
                     const float alpha = jump ? ex2(m_ref - mt) : 1.f;  // from -inf: 0
                     if (jump) {
                         m_ref = mt;
                         l_sum *= alpha;
                     }
-                    // thread t holds lane t: row t % 16's hi or lo part, the same alpha
+                    if (k - k_seg >= kGroups) {  // the group has an O here
+                        waits(b_pvdone + 8 * group, (uint32_t)((k / kGroups - 1) & 1));
+                        fence_after();
+                        // thread t holds lane t: row t % 16's hi or lo part, the same alpha
 #pragma unroll 1
-                    for (int c = 0; c < D; c += 16) {
-                        uint32_t o[16];
-                        ld_lanes16(lanes + kOCol + c, o);
+                        for (int c = 0; c < D; c += 16) {
+                            uint32_t o[16];
+                            ld_lanes16(o_col + c, o);
 #pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
-                        st_lanes16(lanes + kOCol + c, o);
+                            for (int j = 0; j < 16; ++j)
+                                o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+                            st_lanes16(o_col + c, o);
+                        }
+                        st_wait();
                     }
-                    st_wait();
+                    exps();
                 }
-            }
-            const float off = lv + kHead - (m_ref == -INFINITY ? 0.f : m_ref);
-            if (blk || n < kTileKeys) {
+            };
+            auto add_up = [&](const float (&e)[32], float ivs) {  // l, before any rounding
+                float x[16];
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    v[j] = v[j] == -INFINITY ? -INFINITY : v[j] * scale + off;
-            } else {
+                for (int j = 0; j < 16; j += 2) add2(x[j], x[j + 1], e[j], e[j + 1], e[j + 16], e[j + 17]);
+#pragma unroll
+                for (int d = 8; d > 1; d >>= 1)
+#pragma unroll
+                    for (int j = 0; j < d; j += 2)
+                        add2(x[j], x[j + 1], x[j], x[j + 1], x[j + d], x[j + d + 1]);
+                l_sum += (x[0] + x[1]) * ivs;
+            };
+            // the group's P and O are its own again once P V of tile k - 2 is done
+            auto wait_pv = [&] {
+                if (k >= kGroups) waits(b_pvdone + 8 * group, (uint32_t)((k / kGroups - 1) & 1));
+                fence_after();
+            };
+
+            for (k = k_seg + ((k_seg ^ group) & 1); k < k_blk; k += kGroups) {
+                const int kq = kp + (k - k_seg), s = kq % kStages;
+                // (a buffer's phase before this one, the other group's, is over: S
+                // are issued and committed in order, and this group has had tile k - 2)
+                const bool ok_s = waits(b_sready + 8 * (k % kSBufs), (uint32_t)(k / kSBufs) & 1);
+                fence_after();
+                const uint32_t s_addr = lanes + (uint32_t)((k % kSBufs) * kTileKeys);
+                uint32_t a[32], c[32];
+                ld_half(s_addr, a);
+                ld_half(s_addr + kLoLanes, c);
+                waits(b_full + 8 * s, (uint32_t)(kq / kStages) & 1);
+                const TileInfo ti = info[s];
+                const float scale = row_scale * ti.ks;
+                const int n = ti.n;
+                ld_wait(a);
+                ld_wait(c);
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_sfree + 8 * (k % kSBufs));
+                float v[32], e[32];
 #pragma unroll
                 for (int j = 0; j < 32; j += 2)
-                    fma2(v[j], v[j + 1], v[j], v[j + 1], scale, off);
-            }
+                    axpy2(v[j], v[j + 1], kLoInv, __uint_as_float(c[j]), __uint_as_float(c[j + 1]),
+                          __uint_as_float(a[j]), __uint_as_float(a[j + 1]));
+                if (n < kTileKeys || !ok_s) {
+                    const int lim = ok_s ? n : 0;
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = ex2(v[j]);
-            // P buffer (k & 1) is free once the P V of tile k - 2 is done
-            if (k >= 2) waits(b_pvdone + 8 * (int)(k & 1), (uint32_t)((k / 2 - 1) & 1));
-            fence_after();
-            if (!blk) {
+                    for (int j = 0; j < 32; ++j)
+                        if (key0 + j >= lim) v[j] = -INFINITY;
+                }
+                weights_of(v, e, scale, ti.lv, n < kTileKeys || !ok_s);
                 uint32_t hi[8], lo[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     uint32_t h2[2], l2[2];
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const uint32_t x = pack_f16(v[4 * j + 2 * i], v[4 * j + 2 * i + 1]);
+                        const uint32_t x = pack_f16(e[4 * j + 2 * i], e[4 * j + 2 * i + 1]);
                         h2[i] = e4m3_f16(x);
-                        // (x - hi) * 16, both steps exact
-                        l2[i] = e4m3_f16(hmul2(hsub2(x, f16_e4m3(h2[i])), 0x4c004c00u));
+                        // 16 (x - hi), exact
+                        l2[i] = e4m3_f16(hfma2(f16_e4m3(h2[i]), 0xcc00cc00u, hmul2(x, 0x4c004c00u)));
                     }
                     hi[j] = h2[0] | h2[1] << 16;
                     lo[j] = l2[0] | l2[1] << 16;
                 }
-                const uint32_t pa = lanes + kPCol + (uint32_t)((k & 1) * 16);
+                wait_pv();
+                const uint32_t pa = lanes + kPCol + (uint32_t)(group * 16);
                 st_half(pa, hi);
                 st_half(pa + kLoLanes, lo);
-                st_wait();
                 // keys past the page's last token may hold anything: zero their value rows
                 if (n < kTileKeys) {
                     const uint32_t vt = sbase + s * Lt::kStage + Lt::kTile + n * D;
-                    for (int i = threadIdx.x; i < (kTileKeys - n) * (D / 16); i += kSoftWarps * 32)
+                    for (int i = threadIdx.x % (kGroupWarps * 32); i < (kTileKeys - n) * (D / 16);
+                         i += kGroupWarps * 32)
                         st_shared(vt + i * 16, 0, 0, 0, 0);
                     fence_async_smem();
                 }
-            } else {
+                st_wait();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_pready + 8 * group);
+                add_up(e, ti.ivs);
+            }
+            if (has_blk && k == k_blk) {  // the block's own keys, bf16
+                const bool ok_s = waits(b_sready + 8 * (k % kSBufs), (uint32_t)(k / kSBufs) & 1);
+                fence_after();
+                uint32_t a[32];
+                ld_half(lanes + (uint32_t)((k % kSBufs) * kTileKeys), a);
+                ld_wait(a);
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_sfree + 8 * (k % kSBufs));
+                const int lim = live && ok_s ? min(w.T, irow + 1) : 0;  // the causal mask
+                float v[32], e[32];
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] = key0 + j < lim ? __uint_as_float(a[j]) : -INFINITY;
+                weights_of(v, e, p.scale_log2, 0.f, true);
+                wait_pv();
                 const uint32_t pb = sbase + Lt::kPbOff;
-                const int m = 32 * warp + (lane & 15);
+                const int m = 32 * quad + (lane & 15);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     uint32_t h[4], l[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float x = v[8 * c + 2 * i], y = v[8 * c + 2 * i + 1];
+                        const float x = e[8 * c + 2 * i], y = e[8 * c + 2 * i + 1];
                         h[i] = pack_bf16(x, y);
                         l[i] = pack_bf16((x - __uint_as_float(h[i] << 16)) * 16.f,
                                          (y - __uint_as_float(h[i] & 0xffff0000u)) * 16.f);
@@ -721,68 +769,90 @@ __global__ void __launch_bounds__(kThreads, 1)
                     st_shared(pb + chunk16(m + 16, key0 / 8 + c), l[0], l[1], l[2], l[3]);
                 }
                 fence_async_smem();
-            }
-            fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(b_pready + 8 * (int)(k & 1));
-            {  // l: in binary32, of the weights before rounding
-                float t[16];
-#pragma unroll
-                for (int j = 0; j < 16; j += 2)
-                    add2(t[j], t[j + 1], v[j], v[j + 1], v[j + 16], v[j + 17]);
-#pragma unroll
-                for (int d = 8; d > 1; d >>= 1)
-#pragma unroll
-                    for (int j = 0; j < d; j += 2)
-                        add2(t[j], t[j + 1], t[j], t[j + 1], t[j + d], t[j + d + 1]);
-                l_sum += (t[0] + t[1]) * ivs;
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_pready + 8 * group);
+                add_up(e, 1.f);
             }
 
-            if (last) {
-                // ---- end of a segment: O / l and lse ----
-                waits(b_pvdone + 8 * (int)(k & 1), (uint32_t)((k >> 1) & 1));
+            {
+                // ---- end of a segment: the groups' sums joined, O / l and lse ----
+                // group g's last tile here is the last one of its parity, if any
+                const int k_last = k_end - 1, kl = (k_last & 1) == group ? k_last : k_last - 1;
+                const bool any = kl >= k_seg;
+                if (any) waits(b_pvdone + 8 * group, (uint32_t)((kl / kGroups) & 1));
                 fence_after();
-                const bool whole = seg_t == 0 && blk, write = row < rows_active;
-                const float l = l_sum + __shfl_xor_sync(kFull, l_sum, 16);
+                const float lg = l_sum + __shfl_xor_sync(kFull, l_sum, 16);
+                if (half == 0) ml[group * kRows + row] = make_float2(any ? m_ref : -INFINITY, lg);
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                fence_after();
+                const float2 ml0 = ml[row], ml1 = ml[kRows + row];
+                const float M = fmaxf(ml0.x, ml1.x), M0 = M == -INFINITY ? 0.f : M;
+                const float s0 = ex2(ml0.x - M0), s1 = ex2(ml1.x - M0);  // 0 for a group without tiles
+                const float l = s0 * ml0.y + s1 * ml1.y;
                 const float inv = l > 0.f ? 1.f / l : 0.f;
-                const float lse = l > 0.f ? (m_ref - kHead + log2f(l)) * kLn2 : -INFINITY;
+                const float lse = l > 0.f ? (M - kHead + log2f(l)) * kLn2 : -INFINITY;
+                const bool whole = seg_t == 0 && has_blk;
+                const bool two = k_last > k_seg;  // both groups hold an O
                 const int gq = w.h * p.G + row % p.G;
                 const size_t slot =
                     ((size_t)(w.b * p.Hkv + w.h) + blockIdx.x) * p.rows_max + row;
                 uint16_t *orow = p.out + (((size_t)w.b * p.max_block + irow) * p.Hq + gq) * D;
                 float *prow = p.part_o + slot * D;
+                // group g writes columns [g D / 2, (g + 1) D / 2), 32 at a time
+                float x[D / 64][16];
+                const uint32_t o0 = lanes + kOCol + (uint32_t)((k_seg & 1) * kOStep);
+                const uint32_t o1 = lanes + kOCol + (uint32_t)((~k_seg & 1) * kOStep);
+                const float f0 = (k_seg & 1 ? s1 : s0) * inv, f1 = (k_seg & 1 ? s0 : s1) * inv;
 #pragma unroll
-                for (int g = 0; g < D / 64; ++g) {
-                    uint32_t a[32], c[32];
-                    ld_half(lanes + kOCol + 64 * g, a);
-                    ld_half(lanes + kOCol + 64 * g + kLoLanes, c);
+                for (int c = 0; c < D / 64; ++c) {
+                    const uint32_t col = (uint32_t)(group * (D / 2) + 32 * c);
+                    uint32_t a[16], e[16];
+                    ld_half(o0 + col, a);
+                    ld_half(o0 + col + kLoLanes, e);
                     ld_wait(a);
-                    ld_wait(c);
-                    float x[32];
+                    ld_wait(e);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        x[j] = (__uint_as_float(a[j]) + kLoInv * __uint_as_float(c[j])) * inv;
-                    const int d0 = 64 * g + 32 * half;
-                    if (write) {
-                        if (whole) {
+                    for (int j = 0; j < 16; ++j)
+                        x[c][j] = (__uint_as_float(a[j]) + kLoInv * __uint_as_float(e[j])) * f0;
+                    if (two) {
+                        ld_half(o1 + col, a);
+                        ld_half(o1 + col + kLoLanes, e);
+                        ld_wait(a);
+                        ld_wait(e);
 #pragma unroll
-                            for (int j = 0; j < 32; j += 8)
-                                *reinterpret_cast<uint4 *>(orow + d0 + j) = make_uint4(
-                                    pack_bf16(x[j], x[j + 1]), pack_bf16(x[j + 2], x[j + 3]),
-                                    pack_bf16(x[j + 4], x[j + 5]), pack_bf16(x[j + 6], x[j + 7]));
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 32; j += 4)
-                                *reinterpret_cast<float4 *>(prow + d0 + j) =
-                                    make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
-                        }
+                        for (int j = 0; j < 16; ++j)
+                            x[c][j] += (__uint_as_float(a[j]) + kLoInv * __uint_as_float(e[j])) * f1;
                     }
                 }
-                if (write && half == 0) {
-                    if (whole)
-                        p.lse[((size_t)w.b * p.Hq + gq) * p.max_block + irow] = lse;
-                    else
-                        p.part_lse[slot] = lse;
+                // both groups have read both O and ml: the next segment may write them
+                fence_before();
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                if (live) {
+#pragma unroll
+                    for (int c = 0; c < D / 64; ++c) {
+                        const int d0 = group * (D / 2) + 32 * c + 16 * half;
+                        if (whole) {
+#pragma unroll
+                            for (int j = 0; j < 16; j += 8)
+                                *reinterpret_cast<uint4 *>(orow + d0 + j) = make_uint4(
+                                    pack_bf16(x[c][j], x[c][j + 1]),
+                                    pack_bf16(x[c][j + 2], x[c][j + 3]),
+                                    pack_bf16(x[c][j + 4], x[c][j + 5]),
+                                    pack_bf16(x[c][j + 6], x[c][j + 7]));
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 16; j += 4)
+                                *reinterpret_cast<float4 *>(prow + d0 + j) = make_float4(
+                                    x[c][j], x[c][j + 1], x[c][j + 2], x[c][j + 3]);
+                        }
+                    }
+                    if (half == 0 && group == 0) {
+                        if (whole)
+                            p.lse[((size_t)w.b * p.Hq + gq) * p.max_block + irow] = lse;
+                        else
+                            p.part_lse[slot] = lse;
+                    }
                 }
                 if (whole)  // rows past the block: 0 and lse -inf
                     for (int i = threadIdx.x; i < (p.rows_max - rows_active) * (D / 8);
@@ -794,10 +864,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                             make_uint4(0, 0, 0, 0);
                         if (c == 0) p.lse[((size_t)w.b * p.Hq + gg) * p.max_block + ii] = -INFINITY;
                     }
-                fence_before();
             }
-            if (!blk) ++kp;
-            walk_next(p, w);
+            kp += k_blk - k_seg;
+            k = k_end;
         }
     }
     if (warp == kSWarp || warp == kPvWarp) {
@@ -814,8 +883,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncthreads();
     fence_after();
     if (*abort_flag && warp == kProducerWarp && elect_one())  // copies in flight land before exit
-        for (long long j = issued - 1; j >= 0 && j >= issued - kStages; --j)
-            drain_wait(b_full + 8 * (int)(j % kStages), (uint32_t)((j / kStages) & 1));
+        for (int j = issued - 1; j >= 0 && j >= issued - kStages; --j)
+            drain_wait(b_full + 8 * (j % kStages), (uint32_t)(j / kStages) & 1);
     if (warp == 0)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem),
                      "n"(kTmemCols));

@@ -307,9 +307,9 @@ __device__ __forceinline__ void unpack_f16(uint32_t h2, float &lo, float &hi) {
         : "=f"(lo), "=f"(hi)
         : "r"(h2));
 }
-__device__ __forceinline__ uint32_t hsub2(uint32_t a, uint32_t b) {
+__device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
     uint32_t d;
-    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
     return d;
 }
 __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
