@@ -9,7 +9,7 @@
 // lse = ln 2 (m - kHead + log2 l): a page's value scale is part of the weight
 // that its codes are multiplied with, so the products run on the codes alone.
 // m moves (O and l are rescaled) only when a tile's largest x exceeds it by
-// more than kWindow, so p < 2^(kHead + kWindow) = 256 fits e4m3.
+// more than kWindow, so p <= 2^(kHead + kWindow) = 256 fits e4m3.
 //
 // Both operands of an e4m3 product have 4 significant bits, which is too few
 // for queries and weights, so each is split into two rows of one M = 128
@@ -17,9 +17,9 @@
 //   queries  2^e q = hi + lo / 16, exact for elements down to about 2^-13 of
 //            the row's largest (a bf16 value has 8 significant bits); S = S_hi
 //            + S_lo / 16, added where the scores are read;
-//   weights  p = hi + lo / 16, off by at most 2^-9 of p (bf16 weights: 2^-8),
-//            finer than e4m3's least step alone by the factor 16; O = O_hi +
-//            O_lo / 16, added at the end of a segment.
+//   weights  p = hi + lo / 32, off by at most 2^-9 of p (bf16 weights: 2^-8)
+//            or 2^-15, where the reference's weight is 2^kHead; O = O_hi +
+//            O_lo / 32, added at the end of a segment.
 // Row r of the pair (r = i * G + g) has its hi part in TMEM lane
 // 32 (r / 16) + r % 16 and its lo part 16 lanes on, in the same warp's reach.
 //
@@ -66,8 +66,9 @@ constexpr int kTmemCols = 512;     // S [0, 192), each group's O, each group's P
 constexpr int kOCol = kSBufs * kTileKeys;
 constexpr int kOStep = 128;
 constexpr int kPCol = kOCol + kGroups * kOStep;
-constexpr float kHead = 5.f, kWindow = 3.f;
-constexpr float kLoInv = 0.0625f;  // the lo rows hold 16 times the remainder
+constexpr float kHead = 2.f, kWindow = 6.f, kMost = 256.f;  // 2^(kHead + kWindow) = kMost
+constexpr float kQLoInv = 1.f / 16.f, kPLoInv = 1.f / 32.f;
+constexpr uint32_t kPlusLo = 0x50005000u, kMinusLo = 0xd000d000u;  // f16x2 of 32, -32
 constexpr uint32_t kLoLanes = 16u << 16;
 
 // ---- tile list --------------------------------------------------------------------
@@ -604,10 +605,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (lane == 0) mbar_arrive(b_qfree + 8 * q);
             }
             const int k_blk = has_blk ? k_end - 1 : k_end;  // pages are the tiles before it
-            // Weights of a tile from its scores v (hidden ones -inf), in e; moves the
-            // reference (and rescales O and l) where a score asks for it.  The
-            // exponentials are taken under the present reference while the maximum is
-            // found, and again in the rare tile that moves it.
+            // Weights of a tile from its scores v (hidden ones -inf), in e, and their
+            // sum.  They are taken under the present reference; a thread whose 32
+            // weights sum to no more than kMost has none above it, and only where
+            // that fails is the row's maximum found, the reference moved if it asks
+            // for it (O and l rescaled) and the weights taken again.
             auto weights_of = [&](float (&v)[32], float (&e)[32], float scale, float lv, bool hidden) {
                 auto exps = [&] {
                     const float off = lv + kHead - (m_ref == -INFINITY ? 0.f : m_ref);
@@ -622,52 +624,50 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
 #pragma unroll
                     for (int j = 0; j < 32; ++j) e[j] = ex2(e[j]);
+                    float x[16];
+#pragma unroll
+                    for (int j = 0; j < 16; j += 2)
+                        add2(x[j], x[j + 1], e[j], e[j + 1], e[j + 16], e[j + 17]);
+#pragma unroll
+                    for (int d = 8; d > 1; d >>= 1)
+#pragma unroll
+                        for (int j = 0; j < d; j += 2)
+                            add2(x[j], x[j + 1], x[j], x[j + 1], x[j + d], x[j + d + 1]);
+                    return x[0] + x[1];
                 };
-                exps();
-                float x[11];
+                float sum = exps();
+                if (__any_sync(kFull, live && (m_ref == -INFINITY || !(sum <= kMost)))) {
+                    float mt = v[0];
 #pragma unroll
-                for (int j = 0; j < 10; ++j) x[j] = max3(v[3 * j], v[3 * j + 1], v[3 * j + 2]);
-                x[10] = fmaxf(v[30], v[31]);
-                float mt = fmaxf(max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]),
-                                      max3(x[6], x[7], x[8])),
-                                 fmaxf(x[9], x[10]));
-                mt = fmaxf(mt, __shfl_xor_sync(kFull, mt, 16));
-                mt = mt == -INFINITY ? -INFINITY : mt * scale + lv;
-                const bool jump = live && mt > m_ref + kWindow;
-                if (__any_sync(kFull, jump)) {
-                    const float alpha = jump ? ex2(m_ref - mt) : 1.f;  // from -inf: 0
-                    if (jump) {
-                        m_ref = mt;
-                        l_sum *= alpha;
-                    }
-                    if (k - k_seg >= kGroups) {  // the group has an O here
-                        waits(b_pvdone + 8 * group, (uint32_t)((k / kGroups - 1) & 1));
-                        fence_after();
-                        // thread t holds lane t: row t % 16's hi or lo part, the same alpha
-#pragma unroll 1
-                        for (int c = 0; c < D; c += 16) {
-                            uint32_t o[16];
-                            ld_lanes16(o_col + c, o);
-#pragma unroll
-                            for (int j = 0; j < 16; ++j)
-                                o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
-                            st_lanes16(o_col + c, o);
+                    for (int j = 1; j < 32; ++j) mt = fmaxf(mt, v[j]);
+                    mt = fmaxf(mt, __shfl_xor_sync(kFull, mt, 16));
+                    mt = mt == -INFINITY ? -INFINITY : mt * scale + lv;
+                    const bool jump = live && mt > m_ref + kWindow;
+                    if (__any_sync(kFull, jump)) {
+                        const float alpha = jump ? ex2(m_ref - mt) : 1.f;  // from -inf: 0
+                        if (jump) {
+                            m_ref = mt;
+                            l_sum *= alpha;
                         }
-                        st_wait();
+                        if (k - k_seg >= kGroups) {  // the group has an O here
+                            waits(b_pvdone + 8 * group, (uint32_t)((k / kGroups - 1) & 1));
+                            fence_after();
+                            // thread t holds lane t: row t % 16's hi or lo part, the same alpha
+#pragma unroll 1
+                            for (int c = 0; c < D; c += 16) {
+                                uint32_t o[16];
+                                ld_lanes16(o_col + c, o);
+#pragma unroll
+                                for (int j = 0; j < 16; ++j)
+                                    o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+                                st_lanes16(o_col + c, o);
+                            }
+                            st_wait();
+                        }
+                        sum = exps();
                     }
-                    exps();
                 }
-            };
-            auto add_up = [&](const float (&e)[32], float ivs) {  // l, before any rounding
-                float x[16];
-#pragma unroll
-                for (int j = 0; j < 16; j += 2) add2(x[j], x[j + 1], e[j], e[j + 1], e[j + 16], e[j + 17]);
-#pragma unroll
-                for (int d = 8; d > 1; d >>= 1)
-#pragma unroll
-                    for (int j = 0; j < d; j += 2)
-                        add2(x[j], x[j + 1], x[j], x[j + 1], x[j + d], x[j + d + 1]);
-                l_sum += (x[0] + x[1]) * ivs;
+                return sum;
             };
             // the group's P and O are its own again once P V of tile k - 2 is done
             auto wait_pv = [&] {
@@ -685,7 +685,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                 uint32_t a[32], c[32];
                 ld_half(s_addr, a);
                 ld_half(s_addr + kLoLanes, c);
+                // while the loads are on their way: the tile's numbers, and whether the
+                // group's P and O are its own again (once P V of tile k - 2 is done)
                 waits(b_full + 8 * s, (uint32_t)(kq / kStages) & 1);
+                const bool pv_early =
+                    k < kGroups ||
+                    mbar_try_wait(b_pvdone + 8 * group, (uint32_t)((k / kGroups - 1) & 1));
                 const TileInfo ti = info[s];
                 const float scale = row_scale * ti.ks;
                 const int n = ti.n;
@@ -697,7 +702,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 float v[32], e[32];
 #pragma unroll
                 for (int j = 0; j < 32; j += 2)
-                    axpy2(v[j], v[j + 1], kLoInv, __uint_as_float(c[j]), __uint_as_float(c[j + 1]),
+                    axpy2(v[j], v[j + 1], kQLoInv, __uint_as_float(c[j]), __uint_as_float(c[j + 1]),
                           __uint_as_float(a[j]), __uint_as_float(a[j + 1]));
                 if (n < kTileKeys || !ok_s) {
                     const int lim = ok_s ? n : 0;
@@ -705,22 +710,20 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int j = 0; j < 32; ++j)
                         if (key0 + j >= lim) v[j] = -INFINITY;
                 }
-                weights_of(v, e, scale, ti.lv, n < kTileKeys || !ok_s);
+                const float sum = weights_of(v, e, scale, ti.lv, n < kTileKeys || !ok_s);
                 uint32_t hi[8], lo[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    uint32_t h2[2], l2[2];
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const uint32_t x = pack_f16(e[4 * j + 2 * i], e[4 * j + 2 * i + 1]);
-                        h2[i] = e4m3_f16(x);
-                        // 16 (x - hi), exact
-                        l2[i] = e4m3_f16(hfma2(f16_e4m3(h2[i]), 0xcc00cc00u, hmul2(x, 0x4c004c00u)));
-                    }
-                    hi[j] = h2[0] | h2[1] << 16;
-                    lo[j] = l2[0] | l2[1] << 16;
+                    // 32 (x - hi), exact
+                    const uint32_t x = pack_f16(e[4 * j], e[4 * j + 1]);
+                    const uint32_t y = pack_f16(e[4 * j + 2], e[4 * j + 3]);
+                    hi[j] = e4m3x4_f16(x, y);
+                    uint32_t hx, hy;
+                    f16_e4m3x4(hi[j], hx, hy);
+                    lo[j] = e4m3x4_f16(hfma2(hx, kMinusLo, hmul2(x, kPlusLo)),
+                                       hfma2(hy, kMinusLo, hmul2(y, kPlusLo)));
                 }
-                wait_pv();
+                if (!pv_early) wait_pv();
                 const uint32_t pa = lanes + kPCol + (uint32_t)(group * 16);
                 st_half(pa, hi);
                 st_half(pa + kLoLanes, lo);
@@ -736,7 +739,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(b_pready + 8 * group);
-                add_up(e, ti.ivs);
+                l_sum += sum * ti.ivs;
             }
             if (has_blk && k == k_blk) {  // the block's own keys, bf16
                 const bool ok_s = waits(b_sready + 8 * (k % kSBufs), (uint32_t)(k / kSBufs) & 1);
@@ -751,7 +754,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 float v[32], e[32];
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] = key0 + j < lim ? __uint_as_float(a[j]) : -INFINITY;
-                weights_of(v, e, p.scale_log2, 0.f, true);
+                l_sum += weights_of(v, e, p.scale_log2, 0.f, true);
                 wait_pv();
                 const uint32_t pb = sbase + Lt::kPbOff;
                 const int m = 32 * quad + (lane & 15);
@@ -762,8 +765,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int i = 0; i < 4; ++i) {
                         const float x = e[8 * c + 2 * i], y = e[8 * c + 2 * i + 1];
                         h[i] = pack_bf16(x, y);
-                        l[i] = pack_bf16((x - __uint_as_float(h[i] << 16)) * 16.f,
-                                         (y - __uint_as_float(h[i] & 0xffff0000u)) * 16.f);
+                        l[i] = pack_bf16((x - __uint_as_float(h[i] << 16)) * 32.f,
+                                         (y - __uint_as_float(h[i] & 0xffff0000u)) * 32.f);
                     }
                     st_shared(pb + chunk16(m, key0 / 8 + c), h[0], h[1], h[2], h[3]);
                     st_shared(pb + chunk16(m + 16, key0 / 8 + c), l[0], l[1], l[2], l[3]);
@@ -772,7 +775,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                 fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(b_pready + 8 * group);
-                add_up(e, 1.f);
             }
 
             {
@@ -814,7 +816,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     ld_wait(e);
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
-                        x[c][j] = (__uint_as_float(a[j]) + kLoInv * __uint_as_float(e[j])) * f0;
+                        x[c][j] = (__uint_as_float(a[j]) + kPLoInv * __uint_as_float(e[j])) * f0;
                     if (two) {
                         ld_half(o1 + col, a);
                         ld_half(o1 + col + kLoLanes, e);
@@ -822,7 +824,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         ld_wait(e);
 #pragma unroll
                         for (int j = 0; j < 16; ++j)
-                            x[c][j] += (__uint_as_float(a[j]) + kLoInv * __uint_as_float(e[j])) * f1;
+                            x[c][j] += (__uint_as_float(a[j]) + kPLoInv * __uint_as_float(e[j])) * f1;
                     }
                 }
                 // both groups have read both O and ml: the next segment may write them

@@ -288,12 +288,20 @@ __device__ __forceinline__ uint32_t e4m3_f32(float lo, float hi) {
         : "f"(hi), "f"(lo));
     return r;
 }
-__device__ __forceinline__ uint32_t e4m3_f16(uint32_t h2) {
+// four f16 (two pairs) -> four e4m3 codes, and back
+__device__ __forceinline__ uint32_t e4m3x4_f16(uint32_t a, uint32_t b) {
     uint32_t r;
-    asm("{\n .reg .b16 t;\n cvt.rn.satfinite.e4m3x2.f16x2 t, %1;\n cvt.u32.u16 %0, t;\n}"
+    asm("{\n .reg .b16 l, u;\n cvt.rn.satfinite.e4m3x2.f16x2 l, %1;\n"
+        " cvt.rn.satfinite.e4m3x2.f16x2 u, %2;\n mov.b32 %0, {l, u};\n}"
         : "=r"(r)
-        : "r"(h2));
+        : "r"(a), "r"(b));
     return r;
+}
+__device__ __forceinline__ void f16_e4m3x4(uint32_t c, uint32_t &a, uint32_t &b) {
+    asm("{\n .reg .b16 l, u;\n mov.b32 {l, u}, %2;\n cvt.rn.f16x2.e4m3x2 %0, l;\n"
+        " cvt.rn.f16x2.e4m3x2 %1, u;\n}"
+        : "=r"(a), "=r"(b)
+        : "r"(c));
 }
 __device__ __forceinline__ uint32_t f16_e4m3(uint32_t c2) {
     uint32_t h;
