@@ -99,10 +99,6 @@ __device__ __forceinline__ void walk_pair(const PagedAttnParams &p, Walk &w) {
         walk_load(p, w);
     }
 }
-__device__ __forceinline__ void walk_next(const PagedAttnParams &p, Walk &w) {
-    if (++w.t == w.nt) walk_pair(p, w);
-}
-
 // Tile x of pair n has weighted position x + beta n; CTA c takes the tiles at
 // [c W / C, (c + 1) W / C).  A range that holds a block tile, which costs more
 // than its keys, so takes beta tiles fewer; beta = 0 with more pairs than
@@ -215,10 +211,11 @@ struct TileInfo {
     float ks, lv, ivs;  // key scale, log2 and reciprocal of the value scale
     int n;              // visible keys
 };
+constexpr int kInfos = 64;  // ring of the pages' numbers: 32 looked up, and those in the stages
 
 template <int D>
 struct Layout {
-    static constexpr int kStages = 7;
+    static constexpr int kStages = 8;
     static constexpr int kTile = kTileKeys * D;         // an e4m3 tile
     static constexpr int kStage = 2 * kTile;            // keys, values
     static constexpr int kQ8 = 2 * kRows * D;           // split queries [128 rows][D]
@@ -226,20 +223,22 @@ struct Layout {
     static constexpr int kPb = 2 * kRows * kTileKeys * 2;  // P of the block tile
     static constexpr int kQ8Off = kStages * kStage;
     static constexpr int kQbOff = kQ8Off + 2 * kQ8;
-    static constexpr int kKbOff = kQbOff + kBf;
+    // the block tile's P takes the place of its queries, which S is done with
+    static constexpr int kPbOff = kQbOff;
+    static constexpr int kKbOff = kQbOff + (kBf > kPb ? kBf : kPb);
     static constexpr int kVbOff = kKbOff + kBf;
-    static constexpr int kPbOff = kVbOff + kBf;
-    static constexpr int kBarOff = kPbOff + kPb;
+    static constexpr int kBarOff = kVbOff + kBf;
     // full, empty [kStages], qready, qfree [2], bready, bfree, sready, sfree
     // [kSBufs], pready, pvdone [2], drain [2]
     static constexpr int kBars = 2 * kStages + 4 + 2 + 2 * kSBufs + 4 + 2;
     static constexpr int kInfoOff = (kBarOff + kBars * 8 + 15) / 16 * 16;
-    static constexpr int kExpOff = kInfoOff + kStages * 16;
+    static constexpr int kExpOff = kInfoOff + kInfos * 16;
     static constexpr int kMlOff = kExpOff + 2 * kRows * 4;  // (m, l) of each group's rows
     static constexpr int kMiscOff = kMlOff + kGroups * kRows * 8;
     static constexpr int kBytes = kMiscOff + 64 + 1024;  // + alignment slack
     static constexpr uint32_t kSwizzle = D == 128 ? 2 : 4;  // 128- or 64-byte rows
     static_assert(kTile % 1024 == 0 && kQ8Off % 1024 == 0 && kPbOff % 1024 == 0, "alignment");
+    static_assert(kInfos >= 32 + kStages + 1, "tile numbers in use are not written over");
     static_assert(kBytes <= 232448, "shared memory per CTA");
 };
 
@@ -415,142 +414,177 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto waits = [&](uint32_t bar, uint32_t parity) {
         return wait(bar, parity, abort_flag, p.status);
     };
-    int issued = 0;           // tiles whose loads were issued (the producer's)
-    Ring<kStages> st;         // the stage of the next page
+    int issued = 0;  // tiles whose loads were issued (the producer's)
+    // The roles below walk the same segments: a run of pages of one pair, and the
+    // pair's block tile if the range reaches it.
     if (warp == kProducerWarp) {
         // ================================ producer ===============================
-        // Stage s is reused once the P V that read it has completed.  Lane i
-        // holds page and scales of tile base + i of the segment.
+        // Stage s is reused once the P V that read it has completed.  32 pages at a
+        // time, lane i looks up the i-th and writes its numbers to their ring; the
+        // next 32 are asked for when these are begun.
         uint64_t policy;
         asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
         Walk w = w0;
-        int base = -1, page = -1;
-        float ks = 0.f, vs = 0.f;
+        Ring<kStages> st;
         bool ok = true;
-        for (int j = 0; j < ntiles && ok; ++j, walk_next(p, w)) {
-            if (j == 0 || w.t == 0) base = -1;
-            if (w.t == w.nt - 1) continue;
-            if (base < 0 || w.t - base == 32) {
-                base = w.t;
-                const int t = base + lane;
-                page = t < w.nt - 1 ? p.table[(size_t)w.b * p.max_pages + t] : 0;
-                const bool good = page >= 0 && page < p.pages;
-                if (!good) atomicOr(p.status, kStatusBadPage);
-                const size_t tile = (size_t)(good ? page : 0) * p.Hkv + w.h;
-                if (!good) page = -1;
-                ks = p.k_scale[tile];
-                vs = fmaxf(p.v_scale[tile], 8.6736174e-19f);  // 2^-60: codes under a 0 scale vanish
+        for (int left = ntiles; left > 0 && ok; walk_pair(p, w)) {
+            const int n = min(left, w.nt - 1 - w.t);  // pages of the segment
+            const int32_t *row = p.table + (size_t)w.b * p.max_pages + w.t;
+            int page[2] = {0, 0};
+            float ks[2] = {0.f, 0.f}, vs[2] = {0.f, 0.f};
+            auto look_up = [&](int i0, int u) {
+                int pg = i0 + lane < n ? __ldg(row + i0 + lane) : 0;
+                if (pg < 0 || pg >= p.pages) {
+                    atomicOr(p.status, kStatusBadPage);
+                    pg = -1;
+                }
+                const size_t tile = (size_t)max(pg, 0) * p.Hkv + w.h;
+                page[u] = pg;
+                ks[u] = p.k_scale[tile];
+                vs[u] = p.v_scale[tile];
+            };
+            look_up(0, 0);
+            for (int i0 = 0; i0 < n && ok; i0 += 32) {
+                if (i0 + 32 < n) look_up(i0 + 32, 1);
+                {
+                    const float v = fmaxf(vs[0], 8.6736174e-19f);  // 2^-60: codes under a 0 scale vanish
+                    TileInfo ti;
+                    ti.ks = ks[0];
+                    ti.lv = log2f(v);
+                    ti.ivs = 1.f / v;
+                    ti.n = page[0] < 0 ? 0 : min(kTileKeys, w.P - (w.t + i0 + lane) * kTileKeys);
+                    if (i0 + lane < n) info[(issued + lane) % kInfos] = ti;
+                }
+                __syncwarp();
+                const int tile0 = max(page[0], 0) * p.Hkv + w.h, end = min(32, n - i0);
+                for (int i = 0; i < end; ++i) {
+                    const uint32_t full = b_full + 8 * st.i, dst = sbase + st.i * Lt::kStage;
+                    const int tile = __shfl_sync(kFull, tile0, i);
+                    if (issued >= kStages) ok = waits(b_empty + 8 * st.i, st.phase ^ 1);
+                    if (!ok) break;
+                    if (elect_one()) {
+                        mbar_arrive_expect_tx(full, Lt::kStage);
+                        tma_3d(dst, &tm_k, full, 0, 0, tile, policy);
+                        tma_3d(dst + Lt::kTile, &tm_v, full, 0, 0, tile, policy);
+                    }
+                    __syncwarp();
+                    ++issued;
+                    st.next();
+                }
+                page[0] = page[1];
+                ks[0] = ks[1];
+                vs[0] = vs[1];
             }
-            const int s = st.i;
-            if (issued >= kStages) ok = waits(b_empty + 8 * s, st.phase ^ 1);
-            const int pg = __shfl_sync(kFull, page, w.t - base);
-            const float k1 = __shfl_sync(kFull, ks, w.t - base);
-            const float v1 = __shfl_sync(kFull, vs, w.t - base);
-            if (!ok) break;
-            if (elect_one()) {
-                const uint32_t full = b_full + 8 * s, dst = sbase + s * Lt::kStage;
-                const int tile = (pg < 0 ? 0 : pg) * p.Hkv + w.h;
-                TileInfo ti;
-                ti.ks = k1;
-                ti.lv = log2f(v1);
-                ti.ivs = 1.f / v1;
-                ti.n = pg < 0 ? 0 : min(kTileKeys, w.P - w.t * kTileKeys);
-                info[s] = ti;
-                mbar_arrive_expect_tx(full, Lt::kStage);
-                tma_3d(dst, &tm_k, full, 0, 0, tile, policy);
-                tma_3d(dst + Lt::kTile, &tm_v, full, 0, 0, tile, policy);
-            }
-            __syncwarp();
-            ++issued;
-            st.next();
+            left -= w.nt - w.t;
         }
     } else if (warp == kSWarp) {
         // =============================== S = Q K^T ===============================
         const uint32_t id8 = idesc_e4m3(2 * kRows, kTileKeys, 0, 0);
         const uint32_t idb = idesc_bf16(kRows, kTileKeys, 0, 0);
-        const uint64_t dq8 = sdesc(sbase + Lt::kQ8Off, 16, 8 * D, Lt::kSwizzle);
         const uint64_t dk8 = sdesc(sbase, 16, 8 * D, Lt::kSwizzle);
-        const uint64_t dqb = sdesc(sbase + Lt::kQbOff, 16, 1024, 2);
-        const uint64_t dkb = sdesc(sbase + Lt::kKbOff, 16, 1024, 2);
         Walk w = w0;
-        int seg = -1;
-        uint32_t blk_phase = 0;
+        Ring<kStages> st;
         Ring<kSBufs> sb;
+        uint32_t blk_phase = 0;
+        int k = 0;
         bool ok = true;
-        for (int k = 0; k < ntiles && ok; ++k) {
-            if (k == 0 || w.t == 0) {
-                ++seg;
-                ok = waits(b_qready + 8 * (seg & 1), (uint32_t)((seg >> 1) & 1));
-            }
-            const bool blk = w.t == w.nt - 1;
-            const int s = st.i;
-            ok = ok && (blk ? waits(b_bready, blk_phase) : waits(b_full + 8 * s, st.phase));
+        auto buffer = [&] {  // the next S buffer is free
             if (k >= kSBufs) ok = ok && waits(b_sfree + 8 * sb.i, sb.phase ^ 1);
-            if (!ok) break;
             fence_after();
-            if (elect_one()) {
-                const uint32_t dS = tmem + (uint32_t)(sb.i * kTileKeys);
-                if (!blk) {
-                    const uint64_t a0 = dq8 + (uint64_t)(((seg & 1) * Lt::kQ8) >> 4);
-                    const uint64_t b0 = dk8 + (uint64_t)((s * Lt::kStage) >> 4);
+        };
+        for (int seg = 0; k < ntiles && ok; ++seg, walk_pair(p, w)) {
+            const int k_end = min(ntiles, k + w.nt - w.t);
+            const bool has_blk = w.t + (k_end - k) == w.nt;
+            const uint64_t dq8 =
+                sdesc(sbase + Lt::kQ8Off + (seg & 1) * Lt::kQ8, 16, 8 * D, Lt::kSwizzle);
+            ok = waits(b_qready + 8 * (seg & 1), (uint32_t)((seg >> 1) & 1));
+            for (const int k_blk = has_blk ? k_end - 1 : k_end; k < k_blk && ok; ++k) {
+                ok = waits(b_full + 8 * st.i, st.phase);
+                buffer();
+                if (!ok) break;
+                if (elect_one()) {
+                    const uint32_t dS = tmem + (uint32_t)(sb.i * kTileKeys);
+                    const uint64_t b0 = dk8 + (uint64_t)((st.i * Lt::kStage) >> 4);
 #pragma unroll
                     for (int kk = 0; kk < D / 32; ++kk)
-                        mma_e4m3(dS, a0 + kk * 2, b0 + kk * 2, id8, kk > 0);
-                } else {
+                        mma_e4m3(dS, dq8 + kk * 2, b0 + kk * 2, id8, kk > 0);
+                    mma_commit(b_sready + 8 * sb.i);
+                    if (k + 1 == k_end) mma_commit(b_qfree + 8 * (seg & 1));
+                }
+                __syncwarp();
+                st.next();
+                sb.next();
+            }
+            if (has_blk && ok) {
+                ok = waits(b_bready, blk_phase);
+                blk_phase ^= 1;
+                buffer();
+                if (!ok) break;
+                if (elect_one()) {
+                    const uint64_t dqb = sdesc(sbase + Lt::kQbOff, 16, 1024, 2);
+                    const uint64_t dkb = sdesc(sbase + Lt::kKbOff, 16, 1024, 2);
+                    const uint32_t dS = tmem + (uint32_t)(sb.i * kTileKeys);
 #pragma unroll
                     for (int kk = 0; kk < D / 16; ++kk) {
                         const uint32_t off = ((kk >> 2) * (kRows * 128) + (kk & 3) * 32) >> 4;
                         mma_bf16(dS, dqb + off, dkb + off, idb, kk > 0);
                     }
+                    mma_commit(b_sready + 8 * sb.i);
+                    mma_commit(b_qfree + 8 * (seg & 1));
                 }
-                mma_commit(b_sready + 8 * sb.i);
-                if (blk || k + 1 == ntiles) mma_commit(b_qfree + 8 * (seg & 1));
+                __syncwarp();
+                sb.next();
+                ++k;
             }
-            __syncwarp();
-            if (blk) blk_phase ^= 1;
-            else st.next();
-            sb.next();
-            walk_next(p, w);
         }
     } else if (warp == kPvWarp) {
         // ================================ O += P V ===============================
         const uint32_t id8 = idesc_e4m3(2 * kRows, D, 0, 1);
         const uint32_t idb = idesc_bf16(2 * kRows, D, 0, 1);
         const uint64_t dv8 = sdesc(sbase + Lt::kTile, 8 * D, 8 * D, Lt::kSwizzle);
-        const uint64_t dpb = sdesc(sbase + Lt::kPbOff, 16, 1024, 2);
-        const uint64_t dvb = sdesc(sbase + Lt::kVbOff, kRows * 128, 1024, 2);
         Walk w = w0;
-        int k_seg = 0;
+        Ring<kStages> st;
+        int k = 0;
         bool ok = true;
-        for (int k = 0; k < ntiles && ok; ++k) {
-            if (w.t == 0) k_seg = k;
-            const bool first = k - k_seg < kGroups, blk = w.t == w.nt - 1;  // the group's first
-            const uint32_t dO = tmem + kOCol + (uint32_t)((k & 1) * kOStep);
-            const int s = st.i;
-            ok = waits(b_pready + 8 * (k & 1), (uint32_t)(k >> 1) & 1);
-            if (!blk) ok = ok && waits(b_full + 8 * s, st.phase);
-            if (!ok) break;
-            fence_after();
-            if (elect_one()) {
-                if (!blk) {
+        for (; k < ntiles && ok; walk_pair(p, w)) {
+            const int k_seg = k, k_end = min(ntiles, k + w.nt - w.t);
+            const bool has_blk = w.t + (k_end - k) == w.nt;
+            for (const int k_blk = has_blk ? k_end - 1 : k_end; k < k_blk && ok; ++k) {
+                ok = waits(b_pready + 8 * (k & 1), (uint32_t)(k >> 1) & 1) &&
+                     waits(b_full + 8 * st.i, st.phase);
+                if (!ok) break;
+                fence_after();
+                if (elect_one()) {
+                    const uint32_t dO = tmem + kOCol + (uint32_t)((k & 1) * kOStep);
                     const uint32_t a0 = tmem + kPCol + (uint32_t)((k & 1) * 16);
-                    const uint64_t b0 = dv8 + (uint64_t)((s * Lt::kStage) >> 4);
-#pragma unroll
-                    for (int kk = 0; kk < 2; ++kk)
-                        mma_e4m3_ta(dO, a0 + kk * 8, b0 + (uint64_t)((kk * 32 * D) >> 4), id8,
-                                    !first || kk > 0);
-                } else {
+                    const uint64_t b0 = dv8 + (uint64_t)((st.i * Lt::kStage) >> 4);
+                    // (the group's first tile of the segment begins its O)
+                    mma_e4m3_ta(dO, a0, b0, id8, k - k_seg >= kGroups);
+                    mma_e4m3_ta(dO, a0 + 8, b0 + (uint64_t)((32 * D) >> 4), id8, 1);
+                    mma_commit(b_empty + 8 * st.i);
+                    mma_commit(b_pvdone + 8 * (k & 1));
+                }
+                __syncwarp();
+                st.next();
+            }
+            if (has_blk && ok) {
+                ok = waits(b_pready + 8 * (k & 1), (uint32_t)(k >> 1) & 1);
+                if (!ok) break;
+                fence_after();
+                if (elect_one()) {
+                    const uint64_t dpb = sdesc(sbase + Lt::kPbOff, 16, 1024, 2);
+                    const uint64_t dvb = sdesc(sbase + Lt::kVbOff, kRows * 128, 1024, 2);
+                    const uint32_t dO = tmem + kOCol + (uint32_t)((k & 1) * kOStep);
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk)
                         mma_bf16(dO, dpb + kk * 2, dvb + (uint64_t)((kk * 2048) >> 4), idb,
-                                 !first || kk > 0);
+                                 k - k_seg >= kGroups || kk > 0);
+                    mma_commit(b_pvdone + 8 * (k & 1));
+                    mma_commit(b_bfree);
                 }
-                mma_commit(b_pvdone + 8 * (k & 1));
-                mma_commit(blk ? b_bfree : b_empty + 8 * s);
+                __syncwarp();
+                ++k;
             }
-            __syncwarp();
-            if (!blk) st.next();
-            walk_next(p, w);
         }
     } else if (warp >= kQueryWarp0) {
         // ====================== queries, block keys and values ===================
@@ -691,7 +725,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const bool pv_early =
                     k < kGroups ||
                     mbar_try_wait(b_pvdone + 8 * group, (uint32_t)((k / kGroups - 1) & 1));
-                const TileInfo ti = info[s];
+                const TileInfo ti = info[kq % kInfos];
                 const float scale = row_scale * ti.ks;
                 const int n = ti.n;
                 ld_wait(a);

@@ -47,12 +47,14 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
     return ok != 0;
 }
 // Bounded wait; false after 2 s or once another thread of the CTA gave up.
+// The first try, which mostly succeeds or is woken, is all that is inlined:
+// the single-warp roles run at the pace of their instruction fetches.
 __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int *abort_flag,
                                        int32_t *status) {
     const unsigned long long t0 = globaltimer();
     for (uint32_t it = 1;; ++it) {
         if (mbar_try_wait(bar, parity)) return true;
-        if ((it & 63u) == 0) {
+        if ((it & 63u) == 0 || *abort_flag) {
             if (*abort_flag) return false;
             if (globaltimer() - t0 > kWaitNs) {
                 *abort_flag = 1;
@@ -64,11 +66,7 @@ __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile i
 }
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int *abort_flag,
                                      int32_t *status) {
-#pragma unroll 1
-    for (int i = 0; i < 8; ++i)
-        if (mbar_try_wait(bar, parity)) return true;
-    if (*abort_flag) return false;
-    return wait_slow(bar, parity, abort_flag, status);
+    return mbar_try_wait(bar, parity) || wait_slow(bar, parity, abort_flag, status);
 }
 // On the abort path only: at most 20 ms for copies in flight to land.
 __device__ __noinline__ void drain_wait(uint32_t bar, uint32_t parity) {
