@@ -138,8 +138,9 @@ def _check(code, what):
 
 
 def _stream(stream):
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    if stream is None:  # the raw handle: building a Stream object costs about as much as a launch
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream
 
 
 def _ptr(t):
@@ -514,9 +515,20 @@ def _new(shape, dtype, device, stream):
 
 
 def _need_shape(t, dtype, name, shape):
+    if (type(t) is torch.Tensor and t.dtype is dtype and t.is_cuda and t.shape == shape
+            and t.is_contiguous()):
+        return  # the usual case, without the calls below
     _need(t, dtype, name, len(shape))
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def _result(t, shape, dtype, name, device, stream):
+    """t if given (checked), else a new tensor."""
+    if t is None:
+        return _new(shape, dtype, device, stream)
+    _need_shape(t, dtype, name, shape)
+    return t
 
 
 class PagedKVCache:
@@ -541,6 +553,8 @@ class PagedKVCache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.desc = das_kv_cache_paged(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
                                        v_scale.data_ptr(), R, L, N, H, D)
+        self.ref = ctypes.byref(self.desc)
+        self.shape = (R, L, N, H, D)  # depths, layers, pages, kv_heads, head_dim
 
     @classmethod
     def empty(cls, depths, layers, pages, kv_heads, head_dim, device="cuda"):
@@ -549,12 +563,6 @@ class PagedKVCache:
                                     device=device)
         scales = lambda: torch.ones(tiles, dtype=torch.float32, device=device)
         return cls(codes(), codes(), scales(), scales())
-
-    @property
-    def shape(self):
-        """(depths, layers, pages, kv_heads, head_dim)"""
-        d = self.desc
-        return (d.depths, d.layers, d.pages, d.kv_heads, d.head_dim)
 
 
 def das_page_assign(seq_len, grow, block_table, free_pages, free_count, slots, error_flag,
@@ -576,13 +584,9 @@ def das_page_assign(seq_len, grow, block_table, free_pages, free_count, slots, e
     _need(slots, torch.int32, "slots", 1)
     _need_shape(error_flag, torch.int32, "error_flag", (1,))
     dev = seq_len.device
-    new_len = _new(B, torch.int32, dev, stream) if new_len is None else new_len
-    new_free_count = (_new(1, torch.int32, dev, stream) if new_free_count is None
-                      else new_free_count)
-    slot_start = _new(B + 1, torch.int32, dev, stream) if slot_start is None else slot_start
-    _need_shape(new_len, torch.int32, "new_len", (B,))
-    _need_shape(new_free_count, torch.int32, "new_free_count", (1,))
-    _need_shape(slot_start, torch.int32, "slot_start", (B + 1,))
+    new_len = _result(new_len, (B,), torch.int32, "new_len", dev, stream)
+    new_free_count = _result(new_free_count, (1,), torch.int32, "new_free_count", dev, stream)
+    slot_start = _result(slot_start, (B + 1,), torch.int32, "slot_start", dev, stream)
     _check(LIB.das_page_assign(
         _ptr(seq_len), _ptr(grow), B, _ptr(block_table), block_table.shape[1], _ptr(free_pages),
         free_pages.numel(), _ptr(free_count), _ptr(slots), slots.numel(), _ptr(slot_start),
@@ -605,7 +609,7 @@ def das_kv_append_paged(cache, k_new, v_new, slots, slot_start, error_flag, stre
     _need_shape(slot_start, torch.int32, "slot_start", (B + 1,))
     _need_shape(error_flag, torch.int32, "error_flag", (1,))
     _check(LIB.das_kv_append_paged(
-        ctypes.byref(cache.desc), _ptr(k_new), _ptr(v_new), B, W, _ptr(slots), slots.numel(),
+        cache.ref, _ptr(k_new), _ptr(v_new), B, W, _ptr(slots), slots.numel(),
         _ptr(slot_start), _ptr(error_flag), _stream(stream)), "das_kv_append_paged")
 
 
@@ -622,26 +626,26 @@ def das_mature_v_attention_paged(cache, layer, key_depth, value_depth, block_tab
                                  softmax_scale=0.0, stream=None):
     """das_mature_v_attention over a PagedKVCache; key_depth = value_depth is the
     verify attention.  Returns (out, lse)."""
-    _need(prefix_len, torch.int32, "prefix_len", 1)
     _need(block_table, torch.int32, "block_table", 2)
     _need(q, torch.bfloat16, "q", 4)
     R, L, N, H, D = cache.shape
     B, T, Hq, Dq = q.shape
-    if Dq != D or prefix_len.numel() != B or block_table.shape[0] != B:
-        raise ValueError("q / length / table shapes do not match the cache")
+    if Dq != D or block_table.shape[0] != B:
+        raise ValueError("q / table shapes do not match the cache")
+    _need_shape(prefix_len, torch.int32, "prefix_len", (B,))
     _need_shape(block_len, torch.int32, "block_len", (B,))
     _need_shape(k_blk, torch.bfloat16, "k_blk", (B, T, H, D))
     _need_shape(v_blk, torch.bfloat16, "v_blk", (B, T, H, D))
     _need(workspace, torch.uint8, "workspace", 1)
-    out = _new(q.shape, torch.bfloat16, q.device, stream) if out is None else out
-    lse = _new((B, Hq, T), torch.float32, q.device, stream) if lse is None else lse
-    _need_shape(out, torch.bfloat16, "out", q.shape)
-    _need_shape(lse, torch.float32, "lse", (B, Hq, T))
-    _check(LIB.das_mature_v_attention_paged(
-        ctypes.byref(cache.desc), layer, key_depth, value_depth, _ptr(block_table),
-        block_table.shape[1], _ptr(prefix_len), _ptr(block_len), B, T, _ptr(q), _ptr(k_blk),
-        _ptr(v_blk), Hq, float(softmax_scale), _ptr(out), _ptr(lse), _ptr(workspace),
-        workspace.numel(), _stream(stream)), "das_mature_v_attention_paged")
+    out = _result(out, q.shape, torch.bfloat16, "out", q.device, stream)
+    lse = _result(lse, (B, Hq, T), torch.float32, "lse", q.device, stream)
+    code = LIB.das_mature_v_attention_paged(
+        cache.ref, layer, key_depth, value_depth, block_table.data_ptr(), block_table.shape[1],
+        prefix_len.data_ptr(), block_len.data_ptr(), B, T, q.data_ptr(), k_blk.data_ptr(),
+        v_blk.data_ptr(), Hq, softmax_scale, out.data_ptr(), lse.data_ptr(), workspace.data_ptr(),
+        workspace.numel(), _stream(stream))
+    if code:
+        raise DasError(code, "das_mature_v_attention_paged")
     return out, lse
 
 
@@ -676,10 +680,8 @@ def das_sample(logits, uniforms, temperature=None, top_k=None, top_p=None, min_p
     Returns (tokens, logprobs)."""
     kind, B, W, V, row, params = _sampling_args(logits, uniforms, temperature, top_k, top_p, min_p)
     dev = logits.device
-    tokens = _new((B, W), torch.int32, dev, stream) if tokens is None else tokens
-    logprobs = _new((B, W), torch.float32, dev, stream) if logprobs is None else logprobs
-    _need_shape(tokens, torch.int32, "tokens", (B, W))
-    _need_shape(logprobs, torch.float32, "logprobs", (B, W))
+    tokens = _result(tokens, (B, W), torch.int32, "tokens", dev, stream)
+    logprobs = _result(logprobs, (B, W), torch.float32, "logprobs", dev, stream)
     _check(LIB.das_sample(_ptr(logits), kind, B, W, V, row, ctypes.byref(params), _ptr(uniforms),
                           _ptr(tokens), _ptr(logprobs), _stream(stream)), "das_sample")
     return tokens, logprobs
@@ -694,17 +696,11 @@ def das_sample_accept(logits, draft_ids, uniforms, temperature=None, top_k=None,
     kind, B, W, V, row, params = _sampling_args(logits, uniforms, temperature, top_k, top_p, min_p)
     _need_shape(draft_ids, torch.int32, "draft_ids", (B, W))
     dev = logits.device
-    new = lambda t, shape, dt: _new(shape, dt, dev, stream) if t is None else t
-    accepted = new(accepted, (B,), torch.int32)
-    target_ids = new(target_ids, (B, W), torch.int32)
-    next_token = new(next_token, (B,), torch.int32)
-    committed = new(committed, (B,), torch.int32)
-    logprobs = new(logprobs, (B, W), torch.float32)
-    _need_shape(accepted, torch.int32, "accepted", (B,))
-    _need_shape(target_ids, torch.int32, "target_ids", (B, W))
-    _need_shape(next_token, torch.int32, "next_token", (B,))
-    _need_shape(committed, torch.int32, "committed", (B,))
-    _need_shape(logprobs, torch.float32, "logprobs", (B, W))
+    accepted = _result(accepted, (B,), torch.int32, "accepted", dev, stream)
+    target_ids = _result(target_ids, (B, W), torch.int32, "target_ids", dev, stream)
+    next_token = _result(next_token, (B,), torch.int32, "next_token", dev, stream)
+    committed = _result(committed, (B,), torch.int32, "committed", dev, stream)
+    logprobs = _result(logprobs, (B, W), torch.float32, "logprobs", dev, stream)
     _check(LIB.das_sample_accept(
         _ptr(logits), kind, _ptr(draft_ids), B, W, V, row, ctypes.byref(params), _ptr(uniforms),
         _ptr(accepted), _ptr(target_ids), _ptr(next_token), _ptr(committed), _ptr(logprobs),
