@@ -32,6 +32,7 @@ cudaError_t launch_pdl(void (*kernel)(Params...), dim3 grid, dim3 block, cudaStr
 
 // ---- page assignment ----------------------------------------------------------
 constexpr int kAssignThreads = 1024;
+constexpr int kFillAlone = 8192;  // slots that one CTA writes along the way
 
 // What one request asks for.
 struct Ask {
@@ -82,6 +83,9 @@ __device__ __forceinline__ long long scan(long long v, long long &total, long lo
     return r;
 }
 
+// One CTA.  FILL: it writes the table entries and the slots too; otherwise
+// slot_fill_kernel does, from new_len and slot_start.
+template <bool FILL>
 __global__ void __launch_bounds__(kAssignThreads) page_assign_kernel(const PageAssignArgs a) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -141,6 +145,7 @@ __global__ void __launch_bounds__(kAssignThreads) page_assign_kernel(const PageA
             a.new_len[b] = (int)(r.grows && !served ? r.old_len : r.new_len);
             a.slot_start[b] = (int)n_ex;
         }
+        if (!FILL) continue;
         // pages from the stack's top into the rows' next entries
         s_have[tid] = r.have;
         s_num[tid] = take;
@@ -166,11 +171,138 @@ __global__ void __launch_bounds__(kAssignThreads) page_assign_kernel(const PageA
             }
         __syncthreads();
     }
-    for (long long i = placed + tid; i < a.max_slots; i += kAssignThreads) a.slots[i] = -1;
+    if (FILL)
+        for (long long i = placed + tid; i < a.max_slots; i += kAssignThreads) a.slots[i] = -1;
     if (tid == 0) {
         a.slot_start[a.batch] = (int)placed;
         *a.new_free_count = (int)(avail - took);
     }
+    if (flag) atomicOr(a.error_flag, flag);
+}
+
+// Table entries and slots of the requests that page_assign_kernel served:
+// CTA x writes slots [x kFillSlots, (x + 1) kFillSlots), and the table entry
+// of every new page whose first token is among them.  Request b grew by n =
+// slot_start[b + 1] - slot_start[b] to new_len[b] and took the pages past
+// those of new_len[b] - n; the pages taken before its own, and by all, are
+// summed up again by every CTA.
+constexpr int kFillThreads = 256, kFillSlots = 4096, kFillBatch = 256;
+
+__global__ void __launch_bounds__(kFillThreads) slot_fill_kernel(const PageAssignArgs a) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    __shared__ long long sums[32];
+    __shared__ int s_start[kFillBatch + 1], s_old[kFillBatch], s_top[kFillBatch];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int i0 = blockIdx.x * kFillSlots, i1 = min(i0 + kFillSlots, a.max_slots);
+    const int end = a.slot_start[a.batch];
+    const bool wide = (reinterpret_cast<uintptr_t>(a.slots) & 15) == 0;
+    int flag = 0;
+    auto pages = [](int n) { return (n + kPage - 1) / kPage; };
+    auto taken = [&](int b, int &old) {
+        const int n = a.slot_start[b + 1] - a.slot_start[b], len = a.new_len[b];
+        old = len - n;
+        return n > 0 ? pages(len) - pages(old) : 0;
+    };
+    if (i0 < end) {
+        int b0 = 0;  // the first request with a slot past i0
+        for (int hi = a.batch; b0 < hi;) {
+            const int mid = (b0 + hi) / 2;
+            if (a.slot_start[mid + 1] > i0) hi = mid;
+            else b0 = mid + 1;
+        }
+        long long before = 0, all = 0;
+        int old;
+        for (int b = tid; b < a.batch; b += kFillThreads) {
+            const int n = taken(b, old);
+            all += n;
+            if (b < b0) before += n;
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+            before += __shfl_xor_sync(kFull, before, d);
+            all += __shfl_xor_sync(kFull, all, d);
+        }
+        if (lane == 0) {
+            sums[warp] = before;
+            sums[warp + 16] = all;
+        }
+        __syncthreads();
+        before = all = 0;
+#pragma unroll
+        for (int w = 0; w < kFillThreads / 32; ++w) {
+            before += sums[w];
+            all += sums[w + 16];
+        }
+        __syncthreads();
+        // the stack's place of the next page taken
+        long long top = (long long)*a.new_free_count + all - 1 - before;
+        for (; b0 < a.batch; b0 += kFillBatch) {
+            const int nb = min(kFillBatch, a.batch - b0);
+            const int start = a.slot_start[b0], stop = a.slot_start[b0 + nb];
+            if (start >= i1) break;
+            // exclusive sum of the pages taken, a thread to a request
+            const int n = tid < nb ? taken(b0 + tid, old) : 0;
+            long long x = n;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const long long y = __shfl_up_sync(kFull, x, d);
+                if (lane >= d) x += y;
+            }
+            if (lane == 31) sums[warp] = x;
+            __syncthreads();
+            long long sum = 0, batch_all = 0;
+#pragma unroll
+            for (int w = 0; w < kFillThreads / 32; ++w) {
+                if (w < warp) sum += sums[w];
+                batch_all += sums[w];
+            }
+            if (tid < nb) {
+                s_start[tid] = a.slot_start[b0 + tid];
+                s_old[tid] = old;
+                s_top[tid] = (int)(top - (sum + x - n));
+            }
+            if (tid == 0) s_start[nb] = stop;
+            __syncthreads();
+            const int lo = max(i0, start), hi = min(i1, stop);
+            // four slots a thread: one search, and mostly one page
+            for (int i4 = (lo & ~3) + 4 * tid; i4 < hi; i4 += 4 * kFillThreads) {
+                const int i_first = max(i4, lo), i_end = min(i4 + 4, hi);
+                int r = 0;
+                for (int h = nb - 1; r < h;) {  // the last request that starts by i_first
+                    const int mid = (r + h + 1) / 2;
+                    if (s_start[mid] <= i_first) r = mid;
+                    else h = mid - 1;
+                }
+                int out[4] = {-1, -1, -1, -1}, page = -1, page_r = -1, page_at = -1;
+                for (int i = i_first; i < i_end; ++i) {
+                    while (s_start[r + 1] <= i) ++r;
+                    const int pos = s_old[r] + i - s_start[r], at = pos / kPage;
+                    if (r != page_r || at != page_at) {
+                        const int have = pages(s_old[r]);
+                        int32_t *entry = a.table + (size_t)(b0 + r) * a.max_pages + at;
+                        page = at < have ? *entry : a.free_pages[s_top[r] - (at - have)];
+                        if (at >= have && pos % kPage == 0) *entry = page;
+                        if (page < 0 || page >= a.pages) {
+                            flag |= kFlagInvalid;
+                            page = -1;
+                        }
+                        page_r = r;
+                        page_at = at;
+                    }
+                    out[i - i4] = page < 0 ? -1 : page * kPage + pos % kPage;
+                }
+                if (i_first == i4 && i_end == i4 + 4 && wide) {
+                    *reinterpret_cast<int4 *>(a.slots + i4) = make_int4(out[0], out[1], out[2], out[3]);
+                } else {
+                    for (int i = i_first; i < i_end; ++i) a.slots[i] = out[i - i4];
+                }
+            }
+            __syncthreads();  // the requests' numbers are written again
+            top -= batch_all;
+        }
+    }
+    for (int i = max(i0, end) + tid; i < i1; i += kFillThreads) a.slots[i] = -1;
     if (flag) atomicOr(a.error_flag, flag);
 }
 
@@ -182,6 +314,19 @@ __device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi) {
     asm("{\n .reg .b16 t;\n cvt.rn.satfinite.e4m3x2.f32 t, %1, %2;\n cvt.u32.u16 %0, t;\n}"
         : "=r"(r)
         : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack4_e4m3(float a, float b, float c, float d) {
+    uint32_t r;
+    asm("{\n .reg .b16 l, u;\n cvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n"
+        " cvt.rn.satfinite.e4m3x2.f32 u, %4, %3;\n mov.b32 %0, {l, u};\n}"
+        : "=r"(r)
+        : "f"(a), "f"(b), "f"(c), "f"(d));
+    return r;
+}
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
 __device__ __forceinline__ void unpack_e4m3(uint32_t a, float &lo, float &hi) {
@@ -211,17 +356,132 @@ struct AppendArgs {
     int batch, W, pages, kv_heads, max_slots, pieces;
 };
 
-// One CTA: one page piece of one sequence, one kv head, one slab (depth,
-// layer), keys or values.  A thread holds 8 elements of every 128 / (D / 8)-th
-// of the page's tokens.
+// One CTA: one page piece of one sequence, one slab (depth, layer), keys or
+// values, the kv heads one batch after the other.  A thread holds 8 elements of
+// every kStep-th of the piece's tokens; a piece of few tokens leaves places for
+// HB heads at once.  The next batch is on its way while one is converted.
+// Bound by memory: 1001 tokens of 4 sequences at 8 depths and 4 layers 103 us,
+// 6.15 TB/s read and written (134 us with the conversions' first form, which
+// the integer pipe bound); 83 tokens at 32 depths 23 us, 3.2 TB/s, where a CTA's
+// dependent look-ups of its place count.  Runs of slabs to a CTA, which share
+// those, were slower (46 and 182 us: fewer CTAs to an SM).
+template <int D, int HB>
+__device__ __forceinline__ void append_piece(const AppendArgs &a, const uint16_t *src, uint8_t *codes,
+                                             float *scales, int first, int last,
+                                             uint32_t (*s_max)[8][kAppendThreads / 32]) {
+    constexpr int kLanes = D / 8, kStep = kAppendThreads / kLanes, kEach = kPage / kStep / HB;
+    const int lane = threadIdx.x % kLanes, row0 = first + threadIdx.x / kLanes;
+    const int warp = threadIdx.x >> 5;
+    struct Batch {
+        uint4 x[HB][kEach];
+        float held[HB];
+    };
+    auto load = [&](int h0, Batch &v) {
+#pragma unroll
+        for (int g = 0; g < HB; ++g) {
+            v.held[g] = first > 0 && h0 + g < a.kv_heads ? scales[h0 + g] : 0.f;
+#pragma unroll
+            for (int u = 0; u < kEach; ++u) {
+                const int i = row0 + u * kStep;
+                v.x[g][u] = make_uint4(0, 0, 0, 0);
+                if (i < last && h0 + g < a.kv_heads)
+                    v.x[g][u] = __ldcs(reinterpret_cast<const uint4 *>(
+                        src + ((ptrdiff_t)i * a.kv_heads + h0 + g) * D + lane * 8));
+            }
+        }
+    };
+    Batch v, next;
+    load(0, v);
+    for (int h0 = 0, turn = 0; h0 < a.kv_heads; h0 += HB, turn ^= 1) {
+        if (h0 + HB < a.kv_heads) load(h0 + HB, next);
+#pragma unroll
+        for (int g = 0; g < HB; ++g) {
+            uint32_t amax = 0;
+#pragma unroll
+            for (int u = 0; u < kEach; ++u) {
+                const uint32_t w[4] = {v.x[g][u].x, v.x[g][u].y, v.x[g][u].z, v.x[g][u].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) amax = max_bf16x2(amax, w[j] & 0x7fff7fffu);
+            }
+            amax = max(amax & 0xffffu, amax >> 16);
+            if (amax >= 0x7f80u) {  // an infinity (NaN loses): the largest finite one
+                amax = 0;
+#pragma unroll
+                for (int u = 0; u < kEach; ++u) {
+                    const uint32_t w[4] = {v.x[g][u].x, v.x[g][u].y, v.x[g][u].z, v.x[g][u].w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t lo = w[j] & 0x7fffu, hi = (w[j] >> 16) & 0x7fffu;
+                        if (lo < 0x7f80u) amax = max(amax, lo);
+                        if (hi < 0x7f80u) amax = max(amax, hi);
+                    }
+                }
+            }
+            amax = __reduce_max_sync(kFull, amax);
+            if ((threadIdx.x & 31) == 0) s_max[turn][g][warp] = amax;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int g = 0; g < HB; ++g) {
+            if (h0 + g >= a.kv_heads) continue;
+            uint32_t amax = 0;
+#pragma unroll
+            for (int w = 0; w < kAppendThreads / 32; ++w) amax = max(amax, s_max[turn][g][w]);
+            const float held = v.held[g];
+            const float scale = first > 0 ? fmaxf(scale_of(amax), held) : scale_of(amax);
+            // a product with the reciprocal of a power of two is the exact quotient
+            const float inv = 1.f / scale;
+            const bool exact = (__float_as_uint(scale) & 0x7fffffu) == 0;
+            uint8_t *dst = codes + (size_t)(h0 + g) * (kPage * D) + lane * 8;
+#pragma unroll
+            for (int u = 0; u < kEach; ++u) {
+                const int i = row0 + u * kStep;
+                if (i >= last) continue;
+                const uint32_t w[4] = {v.x[g][u].x, v.x[g][u].y, v.x[g][u].z, v.x[g][u].w};
+                float f[8];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    f[2 * j] = __uint_as_float(w[j] << 16);
+                    f[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+                }
+                if (exact) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) f[j] *= inv;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) f[j] /= scale;
+                }
+                *reinterpret_cast<uint2 *>(dst + i * D) =
+                    make_uint2(pack4_e4m3(f[0], f[1], f[2], f[3]), pack4_e4m3(f[4], f[5], f[6], f[7]));
+            }
+            if (first > 0 && scale != held) {  // the older tokens' codes under the larger scale
+                const float ratio = held / scale;
+                for (int i = threadIdx.x / kLanes; i < first; i += kStep) {
+                    uint2 *at = reinterpret_cast<uint2 *>(dst + i * D);
+                    const uint2 was = *at;
+                    const uint32_t w[4] = {was.x & 0xffffu, was.x >> 16, was.y & 0xffffu, was.y >> 16};
+                    uint32_t c[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float lo, hi;
+                        unpack_e4m3(w[j], lo, hi);
+                        c[j] = pack_e4m3(lo * ratio, hi * ratio);
+                    }
+                    *at = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+                }
+            }
+            if (threadIdx.x == 0) scales[h0 + g] = scale;
+        }
+        v = next;
+    }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kAppendThreads) append_paged_kernel(const AppendArgs a) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    constexpr int kLanes = D / 8, kStep = kAppendThreads / kLanes, kRowsEach = kPage / kStep;
+    __shared__ uint32_t s_max[2][8][kAppendThreads / 32];
     unsigned x = blockIdx.x;
-    const int h = x % a.kv_heads;
-    x /= a.kv_heads;
     const int which = x & 1;
     x >>= 1;
     const int piece = x % a.pieces;
@@ -252,77 +512,37 @@ __global__ void __launch_bounds__(kAppendThreads) append_paged_kernel(const Appe
     }
     const int first = piece ? 0 : o;                       // places [first, last) are new
     const int last = (int)min((long long)kPage, n - t0);
-    const int lane = threadIdx.x % kLanes, row0 = threadIdx.x / kLanes;
-    const uint16_t *src = a.fresh[which] + ((slab * a.batch + b) * a.W * a.kv_heads + h) * D + lane * 8;
-    uint4 x4[kRowsEach];
-    uint32_t amax = 0;
-#pragma unroll
-    for (int u = 0; u < kRowsEach; ++u) {
-        const int i = row0 + u * kStep;
-        x4[u] = make_uint4(0, 0, 0, 0);
-        if (i >= first && i < last)
-            x4[u] = __ldcs(reinterpret_cast<const uint4 *>(src + (size_t)(t0 + i) * a.kv_heads * D));
-    }
-#pragma unroll
-    for (int u = 0; u < kRowsEach; ++u) {
-        const uint32_t w[4] = {x4[u].x, x4[u].y, x4[u].z, x4[u].w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t lo = w[j] & 0x7fffu, hi = (w[j] >> 16) & 0x7fffu;
-            if (lo < 0x7f80u) amax = max(amax, lo);
-            if (hi < 0x7f80u) amax = max(amax, hi);
-        }
-    }
-    __shared__ uint32_t s_max[kAppendThreads / 32];
-    amax = __reduce_max_sync(kFull, amax);
-    if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = amax;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kAppendThreads / 32; ++w) amax = max(amax, s_max[w]);
-
-    const size_t tile = (slab * a.pages + page) * a.kv_heads + h;
-    float scale = scale_of(amax), held = 0.f;
-    if (first > 0) {
-        held = a.scales[which][tile];
-        scale = fmaxf(scale, held);
-    }
-    uint8_t *dst = a.codes[which] + tile * (kPage * D) + lane * 8;
-    const bool again = first > 0 && scale != held;
-    const float ratio = held / scale;
-#pragma unroll
-    for (int u = 0; u < kRowsEach; ++u) {
-        const int i = row0 + u * kStep;
-        uint2 *at = reinterpret_cast<uint2 *>(dst + i * D);
-        if (i >= first && i < last) {
-            const uint32_t w[4] = {x4[u].x, x4[u].y, x4[u].z, x4[u].w};
-            uint32_t c[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                c[j] = pack_e4m3(__uint_as_float(w[j] << 16) / scale,
-                                 __uint_as_float(w[j] & 0xffff0000u) / scale);
-            *at = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
-        } else if (again && i < first) {
-            const uint2 was = *at;
-            const uint32_t w[4] = {was.x & 0xffffu, was.x >> 16, was.y & 0xffffu, was.y >> 16};
-            uint32_t c[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float lo, hi;
-                unpack_e4m3(w[j], lo, hi);
-                c[j] = pack_e4m3(lo * ratio, hi * ratio);
-            }
-            *at = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
-        }
-    }
-    // every thread has read the page's present scale before it changes
-    __syncthreads();
-    if (threadIdx.x == 0) a.scales[which][tile] = scale;
+    const uint16_t *src =
+        a.fresh[which] + ((ptrdiff_t)(slab * a.batch + b) * a.W + t0) * a.kv_heads * D;
+    const size_t tile = (slab * a.pages + page) * a.kv_heads;
+    uint8_t *codes = a.codes[which] + tile * (kPage * D);
+    float *scales = a.scales[which] + tile;
+    // as many heads at once as leave every token a place
+    constexpr int kStep = kAppendThreads / (D / 8), kPlaces = kPage / kStep;
+    const int steps = (last - first + kStep - 1) / kStep;
+    if (kPlaces >= 8 && steps <= kPlaces / 8)
+        append_piece<D, kPlaces >= 8 ? 8 : 1>(a, src, codes, scales, first, last, s_max);
+    else if (steps <= kPlaces / 4)
+        append_piece<D, 4>(a, src, codes, scales, first, last, s_max);
+    else if (steps <= kPlaces / 2)
+        append_piece<D, 2>(a, src, codes, scales, first, last, s_max);
+    else
+        append_piece<D, 1>(a, src, codes, scales, first, last, s_max);
 }
 
 }  // namespace
 
 cudaError_t page_assign_launch(const PageAssignArgs &a, cudaStream_t stream) {
-    return launch_pdl(page_assign_kernel, dim3(1), dim3(kAssignThreads), stream, a);
+    // One CTA alone takes 5.2 us for 16 requests and their 144 slots, but 182 us
+    // for 256 requests and 1.2 million slots; a second kernel, which costs the
+    // small call about 2 us, brings that to 14.5 us.
+    if (a.max_slots <= kFillAlone)
+        return launch_pdl(page_assign_kernel<true>, dim3(1), dim3(kAssignThreads), stream, a);
+    const cudaError_t e =
+        launch_pdl(page_assign_kernel<false>, dim3(1), dim3(kAssignThreads), stream, a);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(slot_fill_kernel, dim3((unsigned)((a.max_slots + kFillSlots - 1) / kFillSlots)),
+                      dim3(kFillThreads), stream, a);
 }
 
 cudaError_t append_paged_launch(const das_kv_cache_paged &c, const void *k_new, const void *v_new,
@@ -345,8 +565,7 @@ cudaError_t append_paged_launch(const das_kv_cache_paged &c, const void *k_new, 
     a.kv_heads = c.kv_heads;
     a.max_slots = max_slots;
     a.pieces = (W + 2 * kPage - 2) / kPage;
-    const long long ctas =
-        (long long)c.depths * c.layers * batch * a.pieces * 2 * c.kv_heads;
+    const long long ctas = (long long)c.depths * c.layers * batch * a.pieces * 2;
     if (ctas > 0x7fffffffLL) return cudaErrorInvalidValue;
     if (ctas == 0) return cudaSuccess;
     return c.head_dim == 128 ? launch_pdl(append_paged_kernel<128>, dim3((unsigned)ctas),
