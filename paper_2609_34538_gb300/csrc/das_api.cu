@@ -328,9 +328,13 @@ das_status attention_paged(const das_kv_cache_paged *c, int layer, int key_depth
     const cuuint64_t dims[3] = {(cuuint64_t)c->head_dim, DAS_PAGE_TOKENS, (cuuint64_t)slab_tiles};
     const cuuint32_t box[3] = {(cuuint32_t)c->head_dim, DAS_PAGE_TOKENS, 1};
     CUtensorMap tm_k, tm_v;
-    if (!encode(&tm_k, static_cast<uint8_t *>(c->k) + ks * slab_bytes, 3, dims, box, true, true) ||
-        !encode(&tm_v, static_cast<uint8_t *>(c->v) + vs * slab_bytes, 3, dims, box, true, true))
+    uint8_t *k_slab = static_cast<uint8_t *>(c->k) + ks * slab_bytes;
+    uint8_t *v_slab = static_cast<uint8_t *>(c->v) + vs * slab_bytes;
+    if (!encode(&tm_k, k_slab, 3, dims, box, true, true) ||
+        !encode(&tm_v, v_slab, 3, dims, box, true, true))
         return DAS_ERR_CUDA;
+    p.k = k_slab;
+    p.v = v_slab;
     p.k_scale = c->k_scale + ks * slab_tiles;
     p.v_scale = c->v_scale + vs * slab_tiles;
     p.table = block_table;

@@ -103,6 +103,7 @@ cudaError_t append_paged_launch(const das_kv_cache_paged &c, const void *k_new, 
                                 cudaStream_t stream);
 
 struct PagedAttnParams {
+    const uint8_t *k, *v;                 // the slabs read: e4m3 [pages][Hkv][64][D]
     const float *k_scale, *v_scale;       // [pages][Hkv]
     const int32_t *table;                 // [B][max_pages]
     const int32_t *prefix_len, *block_len;

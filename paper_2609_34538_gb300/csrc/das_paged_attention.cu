@@ -8,8 +8,9 @@
 // O = sum_j p_j vc_j and l = sum_j p_j / vs give o = O / l and
 // lse = ln 2 (m - kHead + log2 l): a page's value scale is part of the weight
 // that its codes are multiplied with, so the products run on the codes alone.
-// m moves (O and l are rescaled) only when a tile's largest x exceeds it by
-// more than kWindow, so p <= 2^(kHead + kWindow) = 256 fits e4m3.
+// m moves (O and l are rescaled) only when a thread's weights of a tile sum to
+// more than kMost = 256 and the tile's largest x exceeds m by more than kWindow,
+// so that no weight is above 256 and all fit e4m3.
 //
 // Both operands of an e4m3 product have 4 significant bits, which is too few
 // for queries and weights, so each is split into two rows of one M = 128
@@ -35,8 +36,12 @@
 // MMA warps + four warps that prepare each segment's queries (split) and block keys and values (bf16,
 // with rows past the block zero).  The block tile runs bf16 products: S with
 // M = 64 (the hi lanes), P V with P split into two bf16 parts.
-// Every wait is bounded (2 s); a time-out sets the status word and ends the
-// CTA's waits.  Tensor memory is freed before the CTA exits.
+// The kernel is launched as a programmatic dependent: barrier set-up, the
+// tensor-memory allocation, the plan (from lengths read before the dependency
+// wait, read again after it) and L2 prefetches of the first tiles and queries
+// overlap the previous kernel's tail; nothing read before the wait is used
+// unchecked.  Every wait is bounded (2 s); a time-out sets the status word and
+// ends the CTA's waits.  Tensor memory is freed before the CTA exits.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -66,10 +71,11 @@ constexpr int kTmemCols = 512;     // S [0, 192), each group's O, each group's P
 constexpr int kOCol = kSBufs * kTileKeys;
 constexpr int kOStep = 128;
 constexpr int kPCol = kOCol + kGroups * kOStep;
-constexpr float kHead = 2.f, kWindow = 6.f, kMost = 256.f;  // 2^(kHead + kWindow) = kMost
+constexpr float kHead = 2.f, kWindow = 3.f, kMost = 256.f;  // 2^(kHead + kWindow) <= kMost
 constexpr float kQLoInv = 1.f / 16.f, kPLoInv = 1.f / 32.f;
 constexpr uint32_t kPlusLo = 0x50005000u, kMinusLo = 0xd000d000u;  // f16x2 of 32, -32
 constexpr uint32_t kLoLanes = 16u << 16;
+constexpr int kPrefetch = 4;       // pages pulled into L2 before the dependency wait
 
 // ---- tile list --------------------------------------------------------------------
 __device__ __forceinline__ int clamp_to(int v, int hi) { return v < 0 ? 0 : (v > hi ? hi : v); }
@@ -81,13 +87,18 @@ __device__ __forceinline__ int block_of(const PagedAttnParams &p, int b) {
 }
 __device__ __forceinline__ int tiles_of(int P) { return (P + kTileKeys - 1) / kTileKeys + 1; }
 
+// The lengths of up to kLens sequences are kept in shared memory (prefixes,
+// then blocks); with more sequences, they are read where they are needed.
+constexpr int kLens = 32;
+
 struct Walk {
     int b, h, t, nt, P, T;
+    const int *lens;  // shared memory, or null
 };
 __device__ __forceinline__ void walk_load(const PagedAttnParams &p, Walk &w) {
     if (w.b < p.B) {
-        w.P = prefix_of(p, w.b);
-        w.T = block_of(p, w.b);
+        w.P = w.lens ? w.lens[w.b] : prefix_of(p, w.b);
+        w.T = w.lens ? w.lens[kLens + w.b] : block_of(p, w.b);
         w.nt = tiles_of(w.P);
     }
 }
@@ -131,26 +142,25 @@ __device__ __forceinline__ int cta_of(long long q, const Split &s, int C) {
 __device__ __forceinline__ int seq_tiles(const PagedAttnParams &p, int b) {
     return b < p.B ? tiles_of(prefix_of(p, b)) : 0;
 }
-__device__ long long all_tiles(const PagedAttnParams &p) {  // whole warp
-    long long n = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 32)
-        n += (long long)__reduce_add_sync(kFull, (unsigned)seq_tiles(p, b0 + (threadIdx.x & 31))) *
-             p.Hkv;
-    return n;
-}
 
 // This CTA's number of tiles and its first one (a whole warp executes this).
-__device__ int plan(const PagedAttnParams &p, Walk &w) {
+__device__ int plan(const PagedAttnParams &p, const int *lens, Walk &w) {
     const int lane = threadIdx.x & 31;
-    const Split sp = split_of(p, all_tiles(p));
+    auto tiles = [&](int b) {
+        return lens ? (b < p.B ? tiles_of(lens[b]) : 0) : seq_tiles(p, b);
+    };
+    long long all = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 32)
+        all += (long long)__reduce_add_sync(kFull, (unsigned)tiles(b0 + lane)) * p.Hkv;
+    const Split sp = split_of(p, all);
     const long long q[2] = {udiv((long long)blockIdx.x * sp.W, p.num_ctas),
                             udiv(((long long)blockIdx.x + 1) * sp.W, p.num_ctas)};
     long long at[2] = {sp.N, sp.N};
-    w = {0, 0, 0, 1, 0, 0};
+    w = {0, 0, 0, 1, 0, 0, lens};
     int found = 0;
     long long run_w = 0, run_t = 0;  // weighted positions / tiles before the chunk
     for (int b0 = 0; b0 < p.B && found < 2; b0 += 32) {
-        const int nt = seq_tiles(p, b0 + lane), nseq = min(32, p.B - b0);
+        const int nt = tiles(b0 + lane), nseq = min(32, p.B - b0);
         int inc = nt;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -185,9 +195,9 @@ __device__ int plan(const PagedAttnParams &p, Walk &w) {
             }
             ++found;
         }
-        const int all = __shfl_sync(kFull, inc, 31);
-        run_w += ((long long)all + (long long)sp.beta * nseq) * p.Hkv;
-        run_t += (long long)all * p.Hkv;
+        const int chunk = __shfl_sync(kFull, inc, 31);
+        run_w += ((long long)chunk + (long long)sp.beta * nseq) * p.Hkv;
+        run_t += (long long)chunk * p.Hkv;
     }
     return (int)max(0ll, at[1] - at[0]);  // the host admits no more than 2^30 a CTA
 }
@@ -234,7 +244,8 @@ struct Layout {
     static constexpr int kInfoOff = (kBarOff + kBars * 8 + 15) / 16 * 16;
     static constexpr int kExpOff = kInfoOff + kInfos * 16;
     static constexpr int kMlOff = kExpOff + 2 * kRows * 4;  // (m, l) of each group's rows
-    static constexpr int kMiscOff = kMlOff + kGroups * kRows * 8;
+    static constexpr int kLenOff = kMlOff + kGroups * kRows * 8;
+    static constexpr int kMiscOff = kLenOff + 2 * kLens * 4;
     static constexpr int kBytes = kMiscOff + 64 + 1024;  // + alignment slack
     static constexpr uint32_t kSwizzle = D == 128 ? 2 : 4;  // 128- or 64-byte rows
     static_assert(kTile % 1024 == 0 && kQ8Off % 1024 == 0 && kPbOff % 1024 == 0, "alignment");
@@ -392,6 +403,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             "n"(kTmemCols));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
+    int *len_sm = reinterpret_cast<int *>(sm + Lt::kLenOff);
+    const bool early = p.B <= kLens;
+    if (early && warp == kProducerWarp) {
+        len_sm[lane] = lane < p.B ? prefix_of(p, lane) : 0;
+        len_sm[kLens + lane] = lane < p.B ? block_of(p, lane) : 0;
+    }
     if (warp == kProducerWarp && elect_one()) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tm_k)) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tm_v)) : "memory");
@@ -401,11 +418,53 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_after();
     const uint32_t tmem = *tmem_slot;
 
+    Walk w0 = {0, 0, 0, 1, 0, 0, nullptr};
+    int ntiles = 0;
+    if (early) {
+        ntiles = plan(p, len_sm, w0);
+        // Into L2 while the kernels before this one finish: the range's first pages
+        // (if the table still says other pages after the wait, these were for
+        // nothing), their scales, and the first queries.
+        if (warp == kProducerWarp) {
+            if (lane < min(ntiles, w0.nt - 1 - w0.t) && lane < kPrefetch) {
+                const int pg = __ldcg(p.table + (size_t)w0.b * p.max_pages + w0.t + lane);
+                if (pg >= 0 && pg < p.pages) {
+                    const size_t tile = (size_t)pg * p.Hkv + w0.h;
+                    prefetch_bulk(p.k + tile * Lt::kTile, Lt::kTile);
+                    prefetch_bulk(p.v + tile * Lt::kTile, Lt::kTile);
+                    prefetch_line(p.k_scale + tile);
+                    prefetch_line(p.v_scale + tile);
+                }
+            }
+        } else if (warp >= kQueryWarp0 && ntiles > 0) {
+            const int r = threadIdx.x - kQueryWarp0 * 32;  // half a row of the first pair
+            if ((r >> 1) < p.G * w0.T)
+                prefetch_line(p.q + (((size_t)w0.b * p.max_block + (r >> 1) / p.G) * p.Hq +
+                                     w0.h * p.G + (r >> 1) % p.G) * D + (r & 1) * (D / 2));
+        }
+    }
     // every input (and the workspace) may be written by the previous kernel
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    Walk w0;
-    const int ntiles = plan(p, w0);
+    // (the producer's first look-up is on its way while the lengths are read again)
+    int page_early = 0;
+    const int n_early = early ? min(ntiles, w0.nt - 1 - w0.t) : 0;
+    if (warp == kProducerWarp && lane < n_early)
+        page_early = __ldcg(p.table + (size_t)w0.b * p.max_pages + w0.t + lane);
+    bool kept = false;  // whether the plan holds; the same in every warp
+    if (early) {
+        const int P1 = lane < p.B ? prefix_of(p, lane) : 0, T1 = lane < p.B ? block_of(p, lane) : 0;
+        kept = __all_sync(kFull, P1 == len_sm[lane] && T1 == len_sm[kLens + lane]);
+        if (!kept) {
+            __syncthreads();  // every warp has compared
+            if (warp == kProducerWarp) {
+                len_sm[lane] = P1;
+                len_sm[kLens + lane] = T1;
+            }
+            __syncthreads();
+        }
+    }
+    if (!kept) ntiles = plan(p, early ? len_sm : nullptr, w0);
     if (blockIdx.x == 0 && warp == 0)
         for (int b = lane; b < p.B; b += 32)
             if (p.prefix_len[b] != prefix_of(p, b) || p.block_len[b] != block_of(p, b))
@@ -424,58 +483,91 @@ __global__ void __launch_bounds__(kThreads, 1)
         // next 32 are asked for when these are begun.
         uint64_t policy;
         asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
-        Walk w = w0;
         Ring<kStages> st;
         bool ok = true;
-        for (int left = ntiles; left > 0 && ok; walk_pair(p, w)) {
-            const int n = min(left, w.nt - 1 - w.t);  // pages of the segment
-            const int32_t *row = p.table + (size_t)w.b * p.max_pages + w.t;
-            int page[2] = {0, 0};
-            float ks[2] = {0.f, 0.f}, vs[2] = {0.f, 0.f};
-            auto look_up = [&](int i0, int u) {
-                int pg = i0 + lane < n ? __ldg(row + i0 + lane) : 0;
-                if (pg < 0 || pg >= p.pages) {
-                    atomicOr(p.status, kStatusBadPage);
-                    pg = -1;
-                }
-                const size_t tile = (size_t)max(pg, 0) * p.Hkv + w.h;
-                page[u] = pg;
-                ks[u] = p.k_scale[tile];
-                vs[u] = p.v_scale[tile];
-            };
-            look_up(0, 0);
-            for (int i0 = 0; i0 < n && ok; i0 += 32) {
-                if (i0 + 32 < n) look_up(i0 + 32, 1);
-                {
-                    const float v = fmaxf(vs[0], 8.6736174e-19f);  // 2^-60: codes under a 0 scale vanish
-                    TileInfo ti;
-                    ti.ks = ks[0];
-                    ti.lv = log2f(v);
-                    ti.ivs = 1.f / v;
-                    ti.n = page[0] < 0 ? 0 : min(kTileKeys, w.P - (w.t + i0 + lane) * kTileKeys);
-                    if (i0 + lane < n) info[(issued + lane) % kInfos] = ti;
+        struct Chunk {
+            Walk w;         // the segment: its pair and first page
+            int left;       // tiles of the range from there on
+            int i0, n;      // the chunk's first page in the segment, the segment's pages
+            int page;       // lane i: page i0 + i, -1 if it is none
+            float ks, vs;   // its scales
+        };
+        auto begin = [&](Chunk &c) {  // at the next segment with pages, if there is one
+            c.i0 = 0;
+            for (;;) {
+                c.n = min(c.left, c.w.nt - 1 - c.w.t);
+                if (c.n > 0 || c.left <= 0) return;
+                c.left -= c.w.nt - c.w.t;
+                walk_pair(p, c.w);
+            }
+        };
+        auto look_up = [&](Chunk &c, bool have) {
+            const int i = c.i0 + lane;
+            if (!have)
+                c.page = i < c.n
+                             ? __ldcg(p.table + (size_t)c.w.b * p.max_pages + c.w.t + i)
+                             : 0;
+            if (c.page < 0 || c.page >= p.pages) {
+                atomicOr(p.status, kStatusBadPage);
+                c.page = -1;
+            }
+            const size_t tile = (size_t)max(c.page, 0) * p.Hkv + c.w.h;
+            c.ks = p.k_scale[tile];
+            c.vs = p.v_scale[tile];
+        };
+        auto load = [&](int tile) {
+            const uint32_t full = b_full + 8 * st.i, dst = sbase + st.i * Lt::kStage;
+            tma_3d(dst, &tm_k, full, 0, 0, tile, policy);
+            tma_3d(dst + Lt::kTile, &tm_v, full, 0, 0, tile, policy);
+        };
+        Chunk c = {w0, ntiles, 0, 0, page_early, 0.f, 0.f};
+        begin(c);
+        if (c.left > 0) look_up(c, kept && c.n == n_early && c.left == ntiles);
+        while (c.left > 0 && ok) {
+            const int tile0 = max(c.page, 0) * p.Hkv + c.w.h, end = min(32, c.n - c.i0);
+            // the range's first loads go before the scales are there (their bytes are
+            // announced below: a barrier's phase waits for that)
+            const int ahead = issued == 0 ? min(end, kStages) : 0;
+            for (int i = 0; i < ahead; ++i) {
+                const int tile = __shfl_sync(kFull, tile0, i);
+                if (elect_one()) load(tile);
+                __syncwarp();
+                st.next();
+            }
+            Chunk next = c;
+            next.i0 += 32;
+            if (next.i0 >= next.n) {
+                next.left -= next.w.nt - next.w.t;
+                walk_pair(p, next.w);
+                begin(next);
+            }
+            if (next.left > 0) look_up(next, false);
+            {
+                const float v = fmaxf(c.vs, 8.6736174e-19f);  // 2^-60: codes under a 0 scale vanish
+                TileInfo ti;
+                ti.ks = c.ks;
+                ti.lv = log2f(v);
+                ti.ivs = 1.f / v;
+                ti.n = c.page < 0 ? 0 : min(kTileKeys, c.w.P - (c.w.t + c.i0 + lane) * kTileKeys);
+                if (lane < end) info[(issued + lane) % kInfos] = ti;
+            }
+            __syncwarp();
+            if (lane < ahead) mbar_arrive_expect_tx(b_full + 8 * lane, Lt::kStage);
+            __syncwarp();
+            issued += ahead;
+            for (int i = ahead; i < end; ++i) {
+                const int tile = __shfl_sync(kFull, tile0, i);
+                if (issued >= kStages) ok = waits(b_empty + 8 * st.i, st.phase ^ 1);
+                if (!ok) break;
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(b_full + 8 * st.i, Lt::kStage);
+                    load(tile);
                 }
                 __syncwarp();
-                const int tile0 = max(page[0], 0) * p.Hkv + w.h, end = min(32, n - i0);
-                for (int i = 0; i < end; ++i) {
-                    const uint32_t full = b_full + 8 * st.i, dst = sbase + st.i * Lt::kStage;
-                    const int tile = __shfl_sync(kFull, tile0, i);
-                    if (issued >= kStages) ok = waits(b_empty + 8 * st.i, st.phase ^ 1);
-                    if (!ok) break;
-                    if (elect_one()) {
-                        mbar_arrive_expect_tx(full, Lt::kStage);
-                        tma_3d(dst, &tm_k, full, 0, 0, tile, policy);
-                        tma_3d(dst + Lt::kTile, &tm_v, full, 0, 0, tile, policy);
-                    }
-                    __syncwarp();
-                    ++issued;
-                    st.next();
-                }
-                page[0] = page[1];
-                ks[0] = ks[1];
-                vs[0] = vs[1];
+                ++issued;
+                st.next();
             }
-            left -= w.nt - w.t;
+            c = next;
         }
     } else if (warp == kSWarp) {
         // =============================== S = Q K^T ===============================
@@ -671,9 +763,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                 };
                 float sum = exps();
                 if (__any_sync(kFull, live && (m_ref == -INFINITY || !(sum <= kMost)))) {
-                    float mt = v[0];
+                    float x[11];
 #pragma unroll
-                    for (int j = 1; j < 32; ++j) mt = fmaxf(mt, v[j]);
+                    for (int j = 0; j < 10; ++j) x[j] = max3(v[3 * j], v[3 * j + 1], v[3 * j + 2]);
+                    x[10] = fmaxf(v[30], v[31]);
+                    float mt = fmaxf(max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]),
+                                          max3(x[6], x[7], x[8])),
+                                     fmaxf(x[9], x[10]));
                     mt = fmaxf(mt, __shfl_xor_sync(kFull, mt, 16));
                     mt = mt == -INFINITY ? -INFINITY : mt * scale + lv;
                     const bool jump = live && mt > m_ref + kWindow;
@@ -688,13 +784,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                             fence_after();
                             // thread t holds lane t: row t % 16's hi or lo part, the same alpha
 #pragma unroll 1
-                            for (int c = 0; c < D; c += 16) {
-                                uint32_t o[16];
-                                ld_lanes16(o_col + c, o);
+                            for (int c = 0; c < D; c += 32) {
+                                uint32_t o[32];
+                                ld_lanes32(o_col + c, o);
 #pragma unroll
-                                for (int j = 0; j < 16; ++j)
+                                for (int j = 0; j < 32; ++j)
                                     o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
-                                st_lanes16(o_col + c, o);
+                                st_lanes32(o_col + c, o);
                             }
                             st_wait();
                         }
@@ -930,13 +1026,16 @@ __global__ void __launch_bounds__(kThreads, 1)
 // One warp per query row of a pair that was cut: with partials O_s / l_s and
 // lse_s, out = sum_s e^(lse_s - M) O_s / l_s / sum_s e^(lse_s - M) and
 // lse = M + ln of that sum.
-constexpr int kMergeWarps = 4;
+// Two warps a CTA: its registers then fit beside an attention CTA's, so that
+// it waits for the attention grid on the SM and has the plan by then.
+constexpr int kMergeWarps = 2;
 constexpr int kMergeLoads = 4;
 
 template <int D>
 __global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const PagedAttnParams p) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // (the lengths may be read before the wait: the attention grid lets this one
+    // begin only after its own wait)
     constexpr int V = D / 32;
     const int rblocks = (p.rows_max + kMergeWarps - 1) / kMergeWarps;
     const int pair = blockIdx.x / rblocks, lane = threadIdx.x & 31;
@@ -955,6 +1054,8 @@ __global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const Pag
     // with fewer tiles than CTAs a tile is a CTA's own and the CTAs between are empty
     const bool dense = sp.beta > 0 || sp.N >= p.num_ctas;
     const int nseg = dense ? cta_of(q0 + nt - 1, sp, p.num_ctas) - c0 + 1 : nt;
+    const int rows_active = p.G * block_of(p, b);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     if (nseg <= 1 || row >= p.rows_max) return;
     const int i = row / p.G, g = h * p.G + row % p.G;
     uint16_t *orow = p.out + (((size_t)b * p.max_block + i) * p.Hq + g) * D + V * lane;
@@ -962,7 +1063,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const Pag
     float M = -INFINITY, L = 0.f, acc[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) acc[v] = 0.f;
-    if (row < p.G * block_of(p, b)) {
+    if (row < rows_active) {
         for (int s0 = 0; s0 < nseg; s0 += kMergeLoads) {
             float ls[kMergeLoads], o[kMergeLoads][V];
 #pragma unroll

@@ -85,6 +85,14 @@ __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap *map, uin
         : "memory");
 }
 
+// L2 prefetches (no shared memory, no barrier): 16-byte aligned bytes, a line.
+__device__ __forceinline__ void prefetch_bulk(const void *src, uint32_t bytes) {
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void prefetch_line(const void *src) {
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(src) : "memory");
+}
+
 // ---- tcgen05 --------------------------------------------------------------------
 // Shared-memory matrix descriptor: start, leading / stride byte offsets,
 // descriptor version 1, layout (2: 128-byte swizzle, 4: 64-byte swizzle).
@@ -187,7 +195,6 @@ __device__ __forceinline__ void ld_half(uint32_t a, uint32_t (&r)[32]) {
         : "r"(a)
         : "memory");
 }
-#undef DAS_R8
 // Waits for the warp's loads; the registers pass through the statement, so
 // that no use of them is moved before it.
 template <int N>
@@ -216,26 +223,28 @@ __device__ __forceinline__ void st_half(uint32_t a, const uint32_t (&r)[8]) {
 __device__ __forceinline__ void st_wait() {
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
-// All 32 lanes of the warp x 16 columns: thread t has lane (base + t).
-__device__ __forceinline__ void ld_lanes16(uint32_t a, uint32_t (&r)[16]) {
+// All 32 lanes of the warp x 32 columns: thread t has lane (base + t).
+__device__ __forceinline__ void ld_lanes32(uint32_t a, uint32_t (&r)[32]) {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,"
-        "%14,%15}, [%16];\ntcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
-          "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
+        "%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+        "tcgen05.wait::ld.sync.aligned;"
+        : DAS_R8(r, 0), DAS_R8(r, 8), DAS_R8(r, 16), DAS_R8(r, 24)
         : "r"(a)
         : "memory");
 }
-__device__ __forceinline__ void st_lanes16(uint32_t a, const uint32_t (&r)[16]) {
+#define DAS_I8(v, o)                                                                          \
+    "r"(v[o]), "r"(v[o + 1]), "r"(v[o + 2]), "r"(v[o + 3]), "r"(v[o + 4]), "r"(v[o + 5]),     \
+        "r"(v[o + 6]), "r"(v[o + 7])
+__device__ __forceinline__ void st_lanes32(uint32_t a, const uint32_t (&r)[32]) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,"
-        "%13,%14,%15,%16};" ::"r"(a),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
-        "r"(r[15])
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,"
+        "%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(a),
+        DAS_I8(r, 0), DAS_I8(r, 8), DAS_I8(r, 16), DAS_I8(r, 24)
         : "memory");
 }
+#undef DAS_I8
+#undef DAS_R8
 
 // ---- arithmetic -------------------------------------------------------------------
 __device__ __forceinline__ float ex2(float x) {
