@@ -111,10 +111,13 @@ __device__ __forceinline__ void walk_pair(const PagedAttnParams &p, Walk &w) {
     }
 }
 // Tile x of pair n has weighted position x + beta n; CTA c takes the tiles at
-// [c W / C, (c + 1) W / C).  A range that holds a block tile, which costs more
-// than its keys, so takes beta tiles fewer; beta = 0 with more pairs than
-// CTAs (nearly every range then holds one) or where a CTA could stay empty.
-constexpr int kBlockWeight = 3;
+// [c W / C, (c + 1) W / C).  The end of a pair (its block tile, the joining of
+// the groups, the next pair's start) costs a CTA about as much as nine pages, so
+// a range that holds one takes beta tiles fewer (weights 3, 5, 7, 9, 12: 54.6,
+// 53.7, 53.5, 52.8, 52.9 us for 4 x 32768 tokens, 44.0, 43.2, 43.4, 41.2, 41.1
+// for 16 ragged sequences); beta = 0 with more pairs than CTAs (nearly every
+// range then holds one) or where a CTA could stay empty.
+constexpr int kBlockWeight = 9;
 struct Split {
     long long N, W;
     int beta;
