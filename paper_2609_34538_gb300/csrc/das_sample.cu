@@ -19,6 +19,7 @@
 // every CTA executes that wait.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include <cooperative_groups.h>
 
@@ -71,7 +72,7 @@ constexpr int kThreads = 1024, kWarps = kThreads / 32;
 static_assert(kWarps == 32, "a warp scans the warps' sums");
 constexpr int kMaxRowCtas = 8;                 // a portable cluster
 constexpr int kSliceBytes = 131072;            // logits per CTA, as they come
-constexpr int kMaxSegs = kSliceBytes / 2 / 128;  // of one warp's 32 groups of four
+constexpr int kMaxSegs = kSliceBytes / 2 / 128 + 32;  // of one warp's 32 groups of four
 constexpr int kBins = 2048;
 constexpr int kList = 256;
 constexpr int kCand = 2048;
@@ -79,12 +80,13 @@ constexpr int kCand = 2048;
 constexpr float kNats = 23.f;
 constexpr uint32_t kOne = 0xffffffffu;  // stands for the weight 2^32
 
-struct Shared {
+struct alignas(16) Shared {
     float cand[kCand];              // the candidates left by a small top-k,
     int cand_at[kCand];             // in index order
-    uint32_t lo[kBins], hi[kBins];  // a bin's sum: lo + 2^16 hi
+    uint32_t hist[2 * kBins];       // bin i's sum: [2 i] + 2^16 [2 i + 1]
     u64 scan[kWarps];
     u64 seg[kMaxSegs];
+    uint32_t n_seg[kMaxSegs];
     u64 xch[2][3][kMaxRowCtas];  // values of every CTA of the cluster
     uint32_t list[kList];  // the CTA's keys in a bin
     uint2 all[kList];      // the cluster's, with their weights
@@ -97,7 +99,7 @@ struct Shared {
 __device__ __forceinline__ u64 wide(uint32_t w) { return (u64)w + (w == kOne); }
 
 template <bool BF16>
-__global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a, int slice, bool vec) {
+__global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a, int slice) {
     __shared__ Shared s;
     extern __shared__ uint4 held[];  // the CTA's logits in groups of four, padded with -inf
     cg::cluster_group cluster = cg::this_cluster();
@@ -164,56 +166,54 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
     if (k <= 0 || k > a.vocab) k = a.vocab;
 
     // ---- the row: NaN as -inf, -0 as 0 ----
+    // Groups of four lie as the vector loads do: the CTA's first token is number
+    // `shift` of group 0, and index `base` + 4 g + i - shift is token i of group g.
+    using Elem = std::conditional_t<BF16, uint16_t, float>;
     const int base = rank * slice, len = max(0, min(slice, a.vocab - base));
-    int groups = (len + 3) / 4;
+    const Elem *src = static_cast<const Elem *>(a.logits) + row * (size_t)a.row_stride + base;
+    const int shift = (int)(reinterpret_cast<uintptr_t>(src) / sizeof(Elem) & 3);
+    int groups = len ? (len + shift + 3) / 4 : 0;
     bool few = false;  // whether the candidates alone are left
-    auto clean = [](float f) { return f == f ? f + 0.f : -INFINITY; };
     float mine = -INFINITY;
-    {
-        const size_t at = row * (size_t)a.row_stride + base;
+    src -= shift;
 #pragma unroll 4
-        for (int g = tid; g < groups; g += kThreads) {
-            const int i = 4 * g;
-            float f[4];
-            if (vec && i + 4 <= len) {
-                if (BF16) {
-                    const uint2 u = __ldcs(reinterpret_cast<const uint2 *>(
-                        static_cast<const uint16_t *>(a.logits) + at + i));
-                    f[0] = __uint_as_float(u.x << 16);
-                    f[1] = __uint_as_float(u.x & 0xffff0000u);
-                    f[2] = __uint_as_float(u.y << 16);
-                    f[3] = __uint_as_float(u.y & 0xffff0000u);
-                } else {
-                    const float4 u = __ldcs(reinterpret_cast<const float4 *>(
-                        static_cast<const float *>(a.logits) + at + i));
-                    f[0] = u.x;
-                    f[1] = u.y;
-                    f[2] = u.z;
-                    f[3] = u.w;
-                }
+    for (int g = tid; g < groups; g += kThreads) {
+        float f[4];
+        if (4 * g >= shift && 4 * g + 4 <= len + shift) {
+            if constexpr (BF16) {
+                const uint2 u = __ldcs(reinterpret_cast<const uint2 *>(src) + g);
+                f[0] = __uint_as_float(u.x << 16);
+                f[1] = __uint_as_float(u.x & 0xffff0000u);
+                f[2] = __uint_as_float(u.y << 16);
+                f[3] = __uint_as_float(u.y & 0xffff0000u);
             } else {
+                const float4 u = __ldcs(reinterpret_cast<const float4 *>(src) + g);
+                f[0] = u.x;
+                f[1] = u.y;
+                f[2] = u.z;
+                f[3] = u.w;
+            }
+        } else {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    f[c] = -INFINITY;
-                    if (i + c < len)
-                        f[c] = BF16 ? __uint_as_float((uint32_t)static_cast<const uint16_t *>(
-                                                          a.logits)[at + i + c]
-                                                      << 16)
-                                    : static_cast<const float *>(a.logits)[at + i + c];
+            for (int i = 0; i < 4; ++i) {
+                f[i] = -INFINITY;
+                if (4 * g + i >= shift && 4 * g + i < len + shift) {
+                    if constexpr (BF16) f[i] = __uint_as_float((uint32_t)src[4 * g + i] << 16);
+                    else f[i] = src[4 * g + i];
                 }
             }
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                f[c] = clean(f[c]);
-                mine = fmaxf(mine, f[c]);
-            }
-            if (BF16)
-                reinterpret_cast<uint2 *>(held)[g] =
-                    make_uint2(__float_as_uint(f[0]) >> 16 | (__float_as_uint(f[1]) & 0xffff0000u),
-                               __float_as_uint(f[2]) >> 16 | (__float_as_uint(f[3]) & 0xffff0000u));
-            else
-                reinterpret_cast<float4 *>(held)[g] = make_float4(f[0], f[1], f[2], f[3]);
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[i] = f[i] == f[i] ? f[i] + 0.f : -INFINITY;
+            mine = fmaxf(mine, f[i]);
+        }
+        if (BF16)
+            reinterpret_cast<uint2 *>(held)[g] =
+                make_uint2(__float_as_uint(f[0]) >> 16 | (__float_as_uint(f[1]) & 0xffff0000u),
+                           __float_as_uint(f[2]) >> 16 | (__float_as_uint(f[3]) & 0xffff0000u));
+        else
+            reinterpret_cast<float4 *>(held)[g] = make_float4(f[0], f[1], f[2], f[3]);
     }
     auto load4 = [&](int g, float (&l)[4]) {
         if (g >= groups) {
@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
                 for (int i = 0; i < 4; ++i)
                     if (l[i] >= low) {
                         s.cand[at] = l[i];
-                        s.cand_at[at++] = base + 4 * g + i;
+                        s.cand_at[at++] = base + 4 * g + i - shift;
                     }
             }
             few = true;
@@ -346,12 +346,12 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
     // (l - m) / T as binary32 division rounds it.  With r = 1 / T rounded, q =
     // rn(x r), the exact remainder x - q T and one more fused step give the
     // quotient rounded to nearest (Markstein, 1990) unless T's significand is
-    // all ones; quotients below -100 have weight 0 and need no care.
+    // all ones; quotients below -100, whose weight is 0, need no care (but no NaN).
     const float rT = __frcp_rn(T);
     const bool quick = T > 1e-18f && T < 1e18f && (__float_as_uint(T) & 0x7fffffu) != 0x7fffffu;
     auto quick_e = [&](float l) {
-        const float d = l - m, q = d * rT;
-        return expf(q < -100.f ? -INFINITY : fmaf(fmaf(-q, T, d), rT, q));
+        const float d = l - m, q = fmaxf(d * rT, -100.f);
+        return expf(fmaf(fmaf(-q, T, d), rT, q));
     };
     auto es_of = [&](const float (&l)[4], float (&e)[4]) {  // four, so that their steps overlap
         if (quick) {
@@ -361,14 +361,9 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
 #pragma unroll
             for (int i = 0; i < 4; ++i) e[i] = expf((l[i] - m) / T);
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (l[i] == m) e[i] = 1.f;
     };
     auto code_of = [](float e) { return __float2uint_rn(e * 4294967296.f); };  // 2^32 saturates
-    auto weight = [&](float l) {
-        return l == m ? kOne : code_of(quick ? quick_e(l) : expf((l - m) / T));
-    };
+    auto weight = [&](float l) { return code_of(quick ? quick_e(l) : expf((l - m) / T)); };
 
     // ---- the threshold of a sum over the logits from `from` up ----
     // Finds the largest t with the sum of f over logits > t below the target
@@ -381,52 +376,59 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
         u64 target = 0, above = 0;
         for (int level = 0;; ++level) {
             const uint32_t k_hi = key_of(hi);
-            const int shift = level ? max(0, 21 - __clz(k_hi - key_of(lo))) : 0;
+            const int key_shift = level ? max(0, 21 - __clz(k_hi - key_of(lo))) : 0;
             // Bins in order of falling logits: of the first level by a linear map
             // (adding 2^23 rounds to the whole number), of later ones by key.
             auto linear = [&](float l) { return fminf((m - l) * per_logit, (float)(kBins - 1)) + 8388608.f; };
             auto bin_of = [&](float l) {
-                return level ? (k_hi - key_of(l)) >> shift
+                return level ? (k_hi - key_of(l)) >> key_shift
                              : __float_as_uint(linear(l)) & (2 * kBins - 1);
             };
-            for (int i = tid; i < kBins; i += kThreads) {
-                s.lo[i] = 0;
-                if (kWeights) s.hi[i] = 0;
-            }
+            for (int i = tid; i < kBins / 2; i += kThreads)
+                reinterpret_cast<uint4 *>(s.hist)[i] = make_uint4(0, 0, 0, 0);
             if (tid == 0) {
                 s.list_n = 0;
                 s.key_min = kOne;
                 s.key_max = 0;
             }
             __syncthreads();
-            for (int g = tid; g - lane < groups; g += kThreads) {
-                float l[4];
-                load4(g, l);
-                bool in[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) in[i] = l[i] >= lo && l[i] <= hi;
-                if (!__any_sync(kFull, in[0] | in[1] | in[2] | in[3])) continue;
-                uint32_t w[4];
+            // (the first level's code is apart: every logit of the row goes through it, at
+            // the pace of the integer pipe.  A bin's two sums are neighbours, and the
+            // sum's bits less those of 2^23 are the bin.)
+            auto add = [&](uint32_t *at, uint32_t code) {
                 if (kWeights) {
-                    float e[4];
-                    es_of(l, e);
+                    uint32_t low = code & 0xffffu, high = code >> 16;
+                    if (code == kOne) {
+                        low = 0;
+                        high = 0x10000u;
+                    }
+                    atomicAdd(at, low);
+                    atomicAdd(at + 1, high);
+                } else {
+                    atomicAdd(at, 1u);
+                }
+            };
+            if (level == 0) {
+                for (int g = tid; g - lane < groups; g += kThreads) {
+                    float l[4];
+                    load4(g, l);
+                    if (!__any_sync(kFull, fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])) >= lo)) continue;
+                    float e[4] = {0.f, 0.f, 0.f, 0.f};
+                    if (kWeights) es_of(l, e);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        w[i] = code_of(e[i]);
-                        in[i] = in[i] && w[i];
+                        const uint32_t bin = __float_as_uint(linear(l[i])) - 0x4b000000u;
+                        if (l[i] >= lo) add(s.hist + 2 * bin, code_of(e[i]));
                     }
                 }
+            } else {
+                for (int g = tid; g < groups; g += kThreads) {
+                    float l[4];
+                    load4(g, l);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (!in[i]) continue;
-                    const uint32_t bin = bin_of(l[i]);
-                    if (kWeights) {
-                        const u64 v = wide(w[i]);
-                        atomicAdd(&s.lo[bin], (uint32_t)v & 0xffffu);
-                        atomicAdd(&s.hi[bin], (uint32_t)(v >> 16));
-                    } else {
-                        atomicAdd(&s.lo[bin], 1u);
-                    }
+                    for (int i = 0; i < 4; ++i)
+                        if (l[i] >= lo && l[i] <= hi)
+                            add(s.hist + 2 * bin_of(l[i]), kWeights ? weight(l[i]) : 0u);
                 }
             }
             sync();
@@ -441,7 +443,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
                         if (i < per_thread)
-                            v[i] += o->lo[i0 + i] + (kWeights ? (u64)o->hi[i0 + i] << 16 : 0);
+                            v[i] += o->hist[2 * (i0 + i)] + ((u64)o->hist[2 * (i0 + i) + 1] << 16);
                 }
             }
             u64 total;
@@ -475,7 +477,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
             const uint32_t bin = (uint32_t)s.bin;
             above = s.above;
             // what is in the bin
-            uint32_t kmin = kOne, kmax = 0;
+            uint32_t kmin = kOne, kmax = 0, in_bin_n = 0;
             const float in_bin = (float)bin + 8388608.f;
             for (int g = tid; g < groups; g += kThreads) {
                 float l[4];
@@ -497,9 +499,17 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
                     const uint32_t key = key_of(l[i]);
                     kmin = min(kmin, key);
                     kmax = max(kmax, key);
-                    const uint32_t n = atomicAdd(&s.list_n, 1u);
-                    if (n < kList) s.list[n] = key;
+                    if (BF16 && !few) {  // mostly many of one key: counted, not listed
+                        ++in_bin_n;
+                    } else {
+                        const uint32_t n = atomicAdd(&s.list_n, 1u);
+                        if (n < kList) s.list[n] = key;
+                    }
                 }
+            }
+            if (BF16 && !few) {
+                in_bin_n = __reduce_add_sync(kFull, in_bin_n);
+                if (lane == 0 && in_bin_n) atomicAdd(&s.list_n, in_bin_n);
             }
             kmin = __reduce_min_sync(kFull, kmin);
             kmax = __reduce_max_sync(kFull, kmax);
@@ -523,7 +533,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
                 }
                 break;
             }
-            if (n <= kList) {
+            if (n <= kList && !(BF16 && !few)) {
                 int at = 0;
                 for (int r = 0; r < C; ++r) {
                     const Shared *o = of(r);
@@ -595,80 +605,74 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
             ties = (s.target - s.sum + w_cut - 1) / w_cut;
         }
     }
-    // of the tokens equal to the cut the first `ties` in index order stay; the
-    // others are taken out
+    // Of the tokens equal to the cut the first `ties` in index order stay.  Where
+    // that is not all of them, they are counted apart, and what stays of a segment's
+    // is added when the counts before it are known.
     const float at_cut = logit_of(cut);
-    if (ties && ties < equal) {
-        for (int g0 = warp * 32; g0 < groups; g0 += kThreads) {
-            float l[4];
-            load4(g0 + lane, l);
-            uint32_t n = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) n += l[i] == at_cut;
-            n = __reduce_add_sync(kFull, n);
-            if (lane == 0) s.seg[g0 / 32] = n;
-        }
-        __syncthreads();
-        u64 here;
-        const u64 ex = scan(tid < (groups + 31) / 32 ? s.seg[tid] : 0, here);
-        if (tid < (groups + 31) / 32) s.seg[tid] = ex;
-        const int t = exchange(here, 0, 0);
-        u64 before = 0;
-        for (int r = 0; r < rank; ++r) before += s.xch[t][0][r];
-        const u64 left = ties > before ? ties - before : 0;
-        if (left < here) {
-            for (int g0 = warp * 32; g0 < groups; g0 += kThreads) {
-                const int g = g0 + lane;
-                const u64 end = g0 / 32 + 1 < (groups + 31) / 32 ? s.seg[g0 / 32 + 1] : here;
-                if (end <= left || end == s.seg[g0 / 32]) continue;  // all stay, or none is here
-                float l[4];
-                load4(g, l);
-                uint32_t c = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) c += l[i] == at_cut;
-                uint32_t at = c;
-#pragma unroll
-                for (int d = 1; d < 32; d <<= 1) {
-                    const uint32_t y = __shfl_up_sync(kFull, at, d);
-                    if (lane >= d) at += y;
-                }
-                u64 place = s.seg[g0 / 32] + at - c;
-                if (c) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (l[i] == at_cut && place++ >= left) l[i] = -INFINITY;
-                    store4(g, l);
-                }
-            }
-        }
-        __syncthreads();  // seg is written again
-    }
-    const float from = ties ? at_cut : logit_of(cut + 1);  // kept by top-k and top-p
-    auto kept = [&](const float (&l)[4], u64 (&w)[4]) {
+    const bool part = ties && ties < equal;
+    const float from = ties && !part ? at_cut : logit_of(cut + 1);
+    // codes of a group's kept weights (those equal to the cut aside where `part`)
+    auto kept = [&](const float (&l)[4], uint32_t (&w)[4]) {
         float e[4];
         es_of(l, e);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = l[i] < from || e[i] < floor_p ? 0 : wide(code_of(e[i]));
+        for (int i = 0; i < 4; ++i) w[i] = l[i] >= from ? code_of(e[i]) : 0u;
+        if (floor_p > 0.f)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (!(e[i] >= floor_p)) w[i] = 0;
     };
+    uint32_t code_cut = 0;  // of a token equal to the cut
+    if (part) {
+        const float l[4] = {at_cut, at_cut, at_cut, at_cut};
+        float e[4];
+        es_of(l, e);
+        code_cut = floor_p > 0.f && !(e[0] >= floor_p) ? 0u : code_of(e[0]);
+    }
 
     // ---- the token at which the running sum in index order passes r ----
+    const int segs = (groups + 31) / 32;
     for (int g0 = warp * 32; g0 < groups; g0 += kThreads) {  // segments of 32 groups
         float l[4];
         load4(g0 + lane, l);
+        const float most = fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3]));
         u64 sum = 0;
-        if (__any_sync(kFull, fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])) >= from)) {
-            u64 w[4];
+        if (__any_sync(kFull, most >= from)) {
+            uint32_t w[4], low = 0, high = 0;
             kept(l, w);
-            sum = (w[0] + w[1]) + (w[2] + w[3]);
 #pragma unroll
-            for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(kFull, sum, d);
+            for (int i = 0; i < 4; ++i) {
+                low += w[i] & 0xffffu;
+                high += w[i] >> 16;
+            }
+            // the few weights of 2^32, which the code has as one less
+            const uint32_t ones = (w[0] == kOne) + (w[1] == kOne) + (w[2] == kOne) + (w[3] == kOne);
+            sum = __reduce_add_sync(kFull, low + ones) +
+                  ((u64)__reduce_add_sync(kFull, high) << 16);
         }
-        if (lane == 0) s.seg[g0 / 32] = sum;
+        uint32_t n = 0;
+        if (part) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) n += l[i] == at_cut;
+            n = __reduce_add_sync(kFull, n);
+        }
+        if (lane == 0) {
+            s.seg[g0 / 32] = sum;
+            s.n_seg[g0 / 32] = n;
+        }
     }
     __syncthreads();
-    const int segs = (groups + 31) / 32;
+    u64 seg = tid < segs ? s.seg[tid] : 0, ties_before = 0;
+    if (part) {
+        const u64 n = tid < segs ? s.n_seg[tid] : 0;
+        u64 here, before = 0;
+        ties_before = scan(n, here);
+        const int t = exchange(here, 0, 0);
+        for (int r = 0; r < rank; ++r) before += s.xch[t][0][r];
+        ties_before += before;
+        seg += (ties > ties_before ? min(n, ties - ties_before) : 0) * wide(code_cut);
+    }
     u64 mine_all;
-    const u64 seg = tid < segs ? s.seg[tid] : 0;
     const u64 seg_before = scan(seg, mine_all);
     u64 total = 0, before = 0;
     {
@@ -691,6 +695,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
     if (seg_before <= r && r < seg_before + seg) {
         s.where = tid;
         s.above = seg_before;
+        s.equal = ties_before;
     }
     __syncthreads();
     if (warp != 0) return;
@@ -698,20 +703,32 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
     const int g = s.where * 32 + lane;
     float l[4];
     load4(g, l);
-    u64 w[4];
-    kept(l, w);
-    const u64 inc = (w[0] + w[1]) + (w[2] + w[3]);
+    uint32_t code[4];
+    kept(l, code);
+    if (part) {
+        uint32_t n = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n += l[i] == at_cut;
+        u64 place = s.equal + warp_scan(n) - n;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (l[i] == at_cut && place++ < ties) code[i] = code_cut;
+    }
+    u64 inc = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) inc += wide(code[i]);
     u64 at = warp_scan(inc) - inc;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (at <= r && r < at + w[i]) {
-            a.tokens[row] = few ? s.cand_at[4 * g + i] : base + 4 * g + i;
+        const u64 w = wide(code[i]);
+        if (at <= r && r < at + w) {
+            a.tokens[row] = few ? s.cand_at[4 * g + i] : base + 4 * g + i - shift;
             if (a.logprobs) {
                 const float z = l[i] == m ? 0.f : (l[i] - m) / T;
                 a.logprobs[row] = z - logf((float)((double)total * (1.0 / 4294967296.0)));
             }
         }
-        at += w[i];
+        at += w;
     }
 }
 
@@ -962,18 +979,16 @@ cudaError_t sample_launch_t(const SampleArgs &a, cudaStream_t stream) {
     while (C < kMaxRowCtas && (C < hold || (rows * C * 2 <= sms && a.vocab > C * 4 * kThreads)))
         C *= 2;
     const int slice = ((a.vocab + C - 1) / C + 3) / 4 * 4;
-    const uintptr_t bytes = 4 * (BF16 ? 2 : 4);
-    const bool vec = a.row_stride % 4 == 0 && reinterpret_cast<uintptr_t>(a.logits) % bytes == 0;
     const dim3 grid((unsigned)(rows * C)), block(kThreads);
-    const size_t smem = (size_t)slice * (BF16 ? 2 : 4);
+    const size_t smem = (size_t)(slice + 4) * (BF16 ? 2 : 4);  // (a group more where rows begin within one)
     static std::atomic<bool> configured[64];  // the shared-memory opt-in, once per device
     if (dev >= 64 || !configured[dev].load(std::memory_order_acquire)) {
         e = cudaFuncSetAttribute(sample_kernel<BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 kSliceBytes);
+                                 kSliceBytes + 16);
         if (e != cudaSuccess) return e;
         if (dev < 64) configured[dev].store(true, std::memory_order_release);
     }
-    return launch_pdl(sample_kernel<BF16>, grid, block, C, smem, stream, a, slice, vec);
+    return launch_pdl(sample_kernel<BF16>, grid, block, C, smem, stream, a, slice);
 }
 
 }  // namespace
