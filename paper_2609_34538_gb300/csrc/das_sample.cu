@@ -83,7 +83,7 @@ constexpr uint32_t kOne = 0xffffffffu;  // stands for the weight 2^32
 struct alignas(16) Shared {
     float cand[kCand];              // the candidates left by a small top-k,
     int cand_at[kCand];             // in index order
-    uint32_t hist[2 * kBins];       // bin i's sum: [2 i] + 2^16 [2 i + 1]
+    uint32_t hist[2 * kBins];       // bin i's sum: [i] + 2^16 [kBins + i]
     u64 scan[kWarps];
     u64 seg[kMaxSegs];
     uint32_t n_seg[kMaxSegs];
@@ -393,8 +393,8 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
             }
             __syncthreads();
             // (the first level's code is apart: every logit of the row goes through it, at
-            // the pace of the integer pipe.  A bin's two sums are neighbours, and the
-            // sum's bits less those of 2^23 are the bin.)
+            // the pace of the integer pipe and of the shared-memory atomics, 3.4 wavefronts
+            // each.  The sum's bits less those of 2^23 are the bin.)
             auto add = [&](uint32_t *at, uint32_t code) {
                 if (kWeights) {
                     uint32_t low = code & 0xffffu, high = code >> 16;
@@ -403,7 +403,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
                         high = 0x10000u;
                     }
                     atomicAdd(at, low);
-                    atomicAdd(at + 1, high);
+                    atomicAdd(at + kBins, high);
                 } else {
                     atomicAdd(at, 1u);
                 }
@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const uint32_t bin = __float_as_uint(linear(l[i])) - 0x4b000000u;
-                        if (l[i] >= lo) add(s.hist + 2 * bin, code_of(e[i]));
+                        if (l[i] >= lo) add(s.hist + bin, code_of(e[i]));
                     }
                 }
             } else {
@@ -428,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         if (l[i] >= lo && l[i] <= hi)
-                            add(s.hist + 2 * bin_of(l[i]), kWeights ? weight(l[i]) : 0u);
+                            add(s.hist + bin_of(l[i]), kWeights ? weight(l[i]) : 0u);
                 }
             }
             sync();
@@ -443,7 +443,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
                         if (i < per_thread)
-                            v[i] += o->hist[2 * (i0 + i)] + ((u64)o->hist[2 * (i0 + i) + 1] << 16);
+                            v[i] += o->hist[i0 + i] + ((u64)o->hist[kBins + i0 + i] << 16);
                 }
             }
             u64 total;
