@@ -543,7 +543,7 @@ das_status das_sample(const void *logits, das_logits_type type, int B, int W, in
                       int32_t *tokens, float *logprobs, void *stream) {
     const das_sampling s = sampling ? *sampling : das_sampling{};
     const das::SampleArgs a = {logits,     type == DAS_LOGITS_BF16, B, W, vocab, row_stride, s,
-                               uniforms, tokens, logprobs};
+                               uniforms, tokens, logprobs, nullptr, nullptr, nullptr, nullptr};
     if (!sample_args_ok(a, type)) return DAS_ERR_INVALID_ARG;
     return das::sample_launch(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? DAS_OK
                                                                                    : DAS_ERR_CUDA;
@@ -556,11 +556,10 @@ das_status das_sample_accept(const void *logits, das_logits_type type, const int
                              int32_t *committed, float *logprobs, void *stream) {
     const das_sampling s = sampling ? *sampling : das_sampling{};
     const das::SampleArgs a = {logits,     type == DAS_LOGITS_BF16, B, W, vocab, row_stride, s,
-                               uniforms, target_ids, logprobs};
+                               uniforms, target_ids, logprobs, nullptr, nullptr, nullptr, nullptr};
     if (!sample_args_ok(a, type) || !draft_ids || !accepted || !next_token)
         return DAS_ERR_INVALID_ARG;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (das::sample_launch(a, st) != cudaSuccess) return DAS_ERR_CUDA;
     return das::sample_accept_launch(a, draft_ids, accepted, next_token, committed, st) ==
                    cudaSuccess
                ? DAS_OK

@@ -131,10 +131,13 @@ struct SampleArgs {
     const float *uniforms;
     int32_t *tokens;
     float *logprobs;
+    // with draft set (W = 1 only) the sampling kernel accepts too
+    const int32_t *draft;
+    int32_t *accepted, *next_token, *committed;
 };
 cudaError_t sample_launch(const SampleArgs &a, cudaStream_t stream);
-// the acceptance that follows sample_launch: from tokens (= target_ids) and draft ids
-cudaError_t sample_accept_launch(const SampleArgs &a, const int32_t *draft, int32_t *accepted,
+// sampling, and acceptance of draft ids against the tokens (= target_ids)
+cudaError_t sample_accept_launch(SampleArgs a, const int32_t *draft, int32_t *accepted,
                                  int32_t *next_token, int32_t *committed, cudaStream_t stream);
 
 }  // namespace das

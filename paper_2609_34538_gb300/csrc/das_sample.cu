@@ -72,7 +72,7 @@ constexpr int kThreads = 1024, kWarps = kThreads / 32;
 static_assert(kWarps == 32, "a warp scans the warps' sums");
 constexpr int kMaxRowCtas = 8;                 // a portable cluster
 constexpr int kSliceBytes = 131072;            // logits per CTA, as they come
-constexpr int kMaxSegs = kSliceBytes / 2 / 128 + 32;  // of one warp's 32 groups of four
+constexpr int kMaxSegs = kSliceBytes / 2 / 128;  // of one warp's 32 groups of four
 constexpr int kBins = 2048;
 constexpr int kList = 256;
 constexpr int kCand = 2048;
@@ -95,6 +95,15 @@ struct alignas(16) Shared {
     uint32_t cut;
     u64 above, target, sum, equal;
 };
+
+// With one proposal a sequence its acceptance needs no other row.
+__device__ __forceinline__ void accept_one(const SampleArgs &a, size_t row, int token) {
+    if (!a.draft) return;
+    const int d = a.draft[row];
+    a.accepted[row] = token >= 0 && d == token;
+    a.next_token[row] = token;  // the proposal itself, where it was accepted
+    if (a.committed) a.committed[row] = 1;
+}
 
 __device__ __forceinline__ u64 wide(uint32_t w) { return (u64)w + (w == kOne); }
 
@@ -274,6 +283,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
         }
         if (most <= kKeyNone) {  // the same in every CTA
             if (rank == 0 && tid == 0) {
+                accept_one(a, row, -1);
                 a.tokens[row] = -1;
                 if (a.logprobs) a.logprobs[row] = -INFINITY;
             }
@@ -295,43 +305,59 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
     }
 
     // ---- a small top-k leaves few candidates: those not below `low`, in index order ----
+    // Four bits of each group of a thread say which; their numbers, in eight bits of
+    // a word per round of groups, are summed over the warp for four rounds at once.
     if (k < a.vocab && k <= kCand / 4) {
-        const int chunks = (groups + kThreads - 1) / kThreads;
-        for (int it = 0; it < chunks; ++it) {
+        constexpr int kRounds = kSliceBytes / (BF16 ? 2 : 4) / 4 / kThreads;
+        static_assert(kRounds * 4 * kThreads * (BF16 ? 2 : 4) == kSliceBytes && kRounds % 8 == 0);
+        uint32_t hits[kRounds / 8], count[kRounds / 4];
+#pragma unroll
+        for (int i = 0; i < kRounds / 8; ++i) hits[i] = 0;
+#pragma unroll
+        for (int i = 0; i < kRounds / 4; ++i) count[i] = 0;
+#pragma unroll
+        for (int it = 0; it < kRounds; ++it) {
+            if (it * kThreads >= groups) continue;
             float l[4];
             load4(it * kThreads + tid, l);
-            int n = 0;
+            const uint32_t in = (uint32_t)(l[0] >= low) | (uint32_t)(l[1] >= low) << 1 |
+                                (uint32_t)(l[2] >= low) << 2 | (uint32_t)(l[3] >= low) << 3;
+            hits[it / 8] |= in << (it % 8 * 4);
+            count[it / 4] |= __popc(in) << (it % 4 * 8);
+        }
+        uint32_t before[kRounds / 4];  // exclusive, over the warp
 #pragma unroll
-            for (int i = 0; i < 4; ++i) n += l[i] >= low;
-            n = __reduce_add_sync(kFull, n);
-            if (lane == 0) s.seg[it * kWarps + warp] = n;
+        for (int i = 0; i < kRounds / 4; ++i) {
+            uint32_t x = count[i];
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const uint32_t y = __shfl_up_sync(kFull, x, d);
+                if (lane >= d) x += y;
+            }
+            before[i] = x - count[i];
+            if (lane == 31)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s.seg[(4 * i + j) * kWarps + warp] = x >> (8 * j) & 0xffu;
         }
         __syncthreads();
         u64 n_all;
-        const u64 before = scan(tid < chunks * kWarps ? s.seg[tid] : 0, n_all);
-        // (a CTA has at most 512 segments)
-        if (tid < chunks * kWarps) s.seg[tid] = before;
+        const u64 ex = scan(tid < kRounds * kWarps ? s.seg[tid] : 0, n_all);
+        if (tid < kRounds * kWarps) s.seg[tid] = ex;
         const int t = exchange(n_all, 0, 0);
         bool fit = true;  // in every CTA of the cluster, which all go one way
         for (int r = 0; r < C; ++r) fit = fit && s.xch[t][0][r] <= kCand;
         if (fit) {
-            for (int it = 0; it < chunks; ++it) {
+#pragma unroll
+            for (int it = 0; it < kRounds; ++it) {
+                uint32_t in = hits[it / 8] >> (it % 8 * 4) & 15u;
+                if (!in) continue;
                 const int g = it * kThreads + tid;
+                int at = (int)s.seg[it * kWarps + warp] + (int)(before[it / 4] >> (it % 4 * 8) & 0xffu);
                 float l[4];
                 load4(g, l);
-                int n = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) n += l[i] >= low;
-                int at = n;
-#pragma unroll
-                for (int d = 1; d < 32; d <<= 1) {
-                    const int y = __shfl_up_sync(kFull, at, d);
-                    if (lane >= d) at += y;
-                }
-                at += (int)s.seg[it * kWarps + warp] - n;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (l[i] >= low) {
+                    if (in >> i & 1) {
                         s.cand[at] = l[i];
                         s.cand_at[at++] = base + 4 * g + i - shift;
                     }
@@ -438,12 +464,20 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
             u64 v[2] = {0, 0};
             if (tid * per_thread < per_cta) {
                 const int i0 = rank * per_cta + tid * per_thread;
-                for (int r = 0; r < C; ++r) {
-                    const Shared *o = of(r);
+                if (C == 1) {
+                    const uint2 low = *reinterpret_cast<const uint2 *>(s.hist + i0);
+                    const uint2 high = *reinterpret_cast<const uint2 *>(s.hist + kBins + i0);
+                    v[0] = low.x + ((u64)high.x << 16);
+                    v[1] = low.y + ((u64)high.y << 16);
+                } else {  // (C >= 2: one bin a thread) all CTAs' on their way at once
+                    uint32_t low[kMaxRowCtas], high[kMaxRowCtas];
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        if (i < per_thread)
-                            v[i] += o->hist[i0 + i] + ((u64)o->hist[kBins + i0 + i] << 16);
+                    for (int r = 0; r < kMaxRowCtas; ++r) {
+                        low[r] = r < C ? of(r)->hist[i0] : 0u;
+                        high[r] = r < C && kWeights ? of(r)->hist[kBins + i0] : 0u;
+                    }
+#pragma unroll
+                    for (int r = 0; r < kMaxRowCtas; ++r) v[0] += low[r] + ((u64)high[r] << 16);
                 }
             }
             u64 total;
@@ -534,22 +568,18 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
                 break;
             }
             if (n <= kList && !(BF16 && !few)) {
-                int at = 0;
-                for (int r = 0; r < C; ++r) {
-                    const Shared *o = of(r);
-                    const int nr = (int)s.xch[t][0][r];
-                    for (int i = tid; i < nr; i += kThreads) {
-                        const uint32_t key = o->list[i];
-                        s.all[at + i] = make_uint2(key, kWeights ? weight(logit_of(key)) : 1u);
-                    }
-                    at += nr;
+                if (tid < (int)n) {
+                    int r = 0, at = tid;
+                    while (at >= (int)s.xch[t][0][r]) at -= (int)s.xch[t][0][r++];
+                    const uint32_t key = of(r)->list[at];
+                    s.all[tid] = make_uint2(key, kWeights ? weight(logit_of(key)) : 1u);
                 }
                 __syncthreads();
-                if (tid < (int)n) {
-                    const uint32_t key = s.all[tid].x;
+                if (tid - lane < 4 * (int)n) {  // four threads to an entry, each every fourth
+                    const uint32_t key = s.all[min(tid >> 2, (int)n - 1)].x;
                     u64 more = 0, equal = 0, count = 0;
 #pragma unroll 4
-                    for (int i = 0; i < (int)n; ++i) {
+                    for (int i = tid & 3; i < (int)n; i += 4) {
                         const uint2 o = s.all[i];
                         const u64 w = wide(o.y);
                         if (o.x > key) more += w;
@@ -557,6 +587,12 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
                             equal += w;
                             ++count;
                         }
+                    }
+#pragma unroll
+                    for (int d = 1; d < 4; d <<= 1) {
+                        more += __shfl_xor_sync(kFull, more, d);
+                        equal += __shfl_xor_sync(kFull, equal, d);
+                        count += __shfl_xor_sync(kFull, count, d);
                     }
                     // threads of equal keys write the same
                     if (above + more < target && above + more + equal >= target) {
@@ -723,6 +759,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
         const u64 w = wide(code[i]);
         if (at <= r && r < at + w) {
             a.tokens[row] = few ? s.cand_at[4 * g + i] : base + 4 * g + i - shift;
+            accept_one(a, row, few ? s.cand_at[4 * g + i] : base + 4 * g + i - shift);
             if (a.logprobs) {
                 const float z = l[i] == m ? 0.f : (l[i] - m) / T;
                 a.logprobs[row] = z - logf((float)((double)total * (1.0 / 4294967296.0)));
@@ -770,6 +807,7 @@ __global__ void __launch_bounds__(kLongThreads) long_row_kernel(const SampleArgs
         (uint32_t)block_reduce<u64>(mine, sums, [](u64 x, u64 y) { return x > y ? x : y; });
     if (top <= kKeyNone) {
         if (tid == 0) {
+            accept_one(a, row, -1);
             a.tokens[row] = -1;
             if (a.logprobs) a.logprobs[row] = -INFINITY;
         }
@@ -904,6 +942,7 @@ __global__ void __launch_bounds__(kLongThreads) long_row_kernel(const SampleArgs
     }
     if (tid == 0) {
         const int t = s_token;
+        accept_one(a, row, t);
         a.tokens[row] = t;
         if (a.logprobs) {
             const float l = logit_of(key(t));
@@ -970,7 +1009,7 @@ cudaError_t sample_launch_t(const SampleArgs &a, cudaStream_t stream) {
     const int sms = attn_grid_size(dev);
     if (sms <= 0) return cudaErrorInvalidDevice;
     // CTAs per row: enough to hold the row, and as many as fill the SMs
-    constexpr int kMaxSlice = kSliceBytes / (BF16 ? 2 : 4);
+    constexpr int kMaxSlice = kSliceBytes / (BF16 ? 2 : 4) - 4;  // (with the shift of a first group)
     const int hold = (int)(((long long)a.vocab + kMaxSlice - 1) / kMaxSlice);
     if (hold > kMaxRowCtas)
         return launch_pdl(long_row_kernel<BF16>, dim3((unsigned)rows), dim3(kLongThreads), 1, 0,
@@ -984,7 +1023,7 @@ cudaError_t sample_launch_t(const SampleArgs &a, cudaStream_t stream) {
     static std::atomic<bool> configured[64];  // the shared-memory opt-in, once per device
     if (dev >= 64 || !configured[dev].load(std::memory_order_acquire)) {
         e = cudaFuncSetAttribute(sample_kernel<BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 kSliceBytes + 16);
+                                 kSliceBytes);
         if (e != cudaSuccess) return e;
         if (dev < 64) configured[dev].store(true, std::memory_order_release);
     }
@@ -998,9 +1037,18 @@ cudaError_t sample_launch(const SampleArgs &a, cudaStream_t stream) {
     return a.bf16 ? sample_launch_t<true>(a, stream) : sample_launch_t<false>(a, stream);
 }
 
-cudaError_t sample_accept_launch(const SampleArgs &a, const int32_t *draft, int32_t *accepted,
+cudaError_t sample_accept_launch(SampleArgs a, const int32_t *draft, int32_t *accepted,
                                  int32_t *next_token, int32_t *committed, cudaStream_t stream) {
     if (a.B == 0) return cudaSuccess;
+    if (a.W == 1) {  // one kernel: the launch and the dependency cost 3 us
+        a.draft = draft;
+        a.accepted = accepted;
+        a.next_token = next_token;
+        a.committed = committed;
+        return sample_launch(a, stream);
+    }
+    const cudaError_t e = sample_launch(a, stream);
+    if (e != cudaSuccess) return e;
     return launch_pdl(sample_accept_kernel, dim3((unsigned)((a.B + kScanWarps - 1) / kScanWarps)),
                       dim3(kScanWarps * 32), 1, 0, stream, static_cast<const int32_t *>(a.tokens),
                       draft, a.B, a.W, accepted, next_token, committed);
