@@ -357,8 +357,8 @@ typedef struct {
  * With outputs apart from their inputs the call can be repeated and gives the
  * same result: it changes only stack entries from free_count on, and table
  * entries past the pages of old lengths.
- * Requires batch >= 0, 1 <= max_pages, max_pages * 64 < 2^31, and
- * pages * 64 < 2^31.
+ * Requires 0 <= batch <= 2^24, max_pages and pages in 1..2^25 - 1, and
+ * 0 <= max_slots <= 2^30.
  */
 das_status das_page_assign(const int32_t *seq_len, const int32_t *grow, int batch,
                            int32_t *block_table, int max_pages, int32_t *free_pages, int pages,
@@ -407,6 +407,13 @@ size_t das_workspace_size_paged(const das_kv_cache_paged *cache, int batch, int 
  * All other arguments, results and limits as das_mature_v_attention.  Bit 2
  * of the workspace's status word is set where a table entry is no page of the
  * cache; its 64 tokens are then taken as masked.
+ * The products run on the codes: a query row and the softmax weights are each
+ * split into two e4m3 parts, the queries exactly for elements down to about
+ * 2^-13 of the row's largest (queries must be finite), a weight to 2^-9 of
+ * itself or 2^-17 of the row's largest weight times value scale; scores, sums
+ * and outputs are accumulated in fp32.  The value scales that one sequence
+ * reads are to be within a factor of 2^100 of each other and of 1 (a scale of 0
+ * counts as 2^-60).
  */
 das_status das_mature_v_attention_paged(const das_kv_cache_paged *cache, int layer, int key_depth,
                                         int value_depth, const int32_t *block_table, int max_pages,

@@ -476,6 +476,7 @@ das_status das_page_assign(const int32_t *seq_len, const int32_t *grow, int batc
         max_pages >= (1 << 25) || pages < 1 || pages >= (1 << 25) || max_slots < 0 ||
         (max_slots > 0 && !slots))
         return DAS_ERR_INVALID_ARG;
+    if (batch > (1 << 24) || max_slots > (1 << 30)) return DAS_ERR_UNSUPPORTED;
     const das::PageAssignArgs a = {seq_len,    grow,           block_table, free_pages,
                                    free_count, slots,          slot_start,  new_len,
                                    new_free_count, error_flag, batch,       max_pages,

@@ -925,8 +925,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const float M = fmaxf(ml0.x, ml1.x), M0 = M == -INFINITY ? 0.f : M;
                 const float s0 = ex2(ml0.x - M0), s1 = ex2(ml1.x - M0);  // 0 for a group without tiles
                 const float l = s0 * ml0.y + s1 * ml1.y;
-                const float inv = l > 0.f ? 1.f / l : 0.f;
-                const float lse = l > 0.f ? (M - kHead + log2f(l)) * kLn2 : -INFINITY;
+                // 0: no visible key; NaN (a code that is none) stays NaN
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                const float lse = l == 0.f ? -INFINITY : (M - kHead + log2f(l)) * kLn2;
                 const bool whole = seg_t == 0 && has_blk;
                 const bool two = k_last > k_seg;  // both groups hold an O
                 const int gq = w.h * p.G + row % p.G;
@@ -1090,7 +1091,10 @@ __global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const Pag
             float m = M;
 #pragma unroll
             for (int u = 0; u < kMergeLoads; ++u) m = fmaxf(m, ls[u]);
-            if (m == -INFINITY) continue;
+            float any = 0.f;  // NaN where a partial is
+#pragma unroll
+            for (int u = 0; u < kMergeLoads; ++u) any += ls[u] == ls[u] ? 0.f : ls[u];
+            if (m == -INFINITY && any == 0.f) continue;
             const float a = __expf(M - m);
             L *= a;
 #pragma unroll
@@ -1105,11 +1109,11 @@ __global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const Pag
             M = m;
         }
     }
-    const float inv = L > 0.f ? 1.f / L : 0.f;
+    const float inv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
     for (int v = 0; v < V; v += 2)
         *reinterpret_cast<uint32_t *>(orow + v) = pack_bf16(acc[v] * inv, acc[v + 1] * inv);
-    if (lane == 0) *lrow = L > 0.f ? M + __logf(L) : -INFINITY;
+    if (lane == 0) *lrow = L == 0.f ? -INFINITY : M + __logf(L);
 }
 
 size_t round256(size_t n) { return (n + 255) & ~size_t(255); }

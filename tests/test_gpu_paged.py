@@ -309,6 +309,55 @@ def test_attention_entries_that_are_no_pages_are_masked_and_flagged():
     run_attention(*c, status=4, masked={(0, 2), (1, 0)}, where="bad pages")
 
 
+def test_attention_nan_stays_with_its_rows():
+    """A stored NaN makes the rows that see it NaN, lse too, and no others."""
+    rng = np.random.default_rng(15)
+    for prefix in (70, 1500):                               # one segment, and several joined
+        c = list(attention_case(rng, 64, 4, 2, 3, [prefix, 90], [3, 2]))
+        c[0] = c[0].copy()
+        c[0][c[4][0, 1], 1, 2, 7] = 0x7F                    # sequence 0, kv head 1
+        out, lse = run_attention_raw(*c)
+        bad = np.zeros(out.shape[:3], bool)
+        bad[0, :3, 2:] = True
+        assert np.isnan(out[bad]).all() and np.isfinite(out[~bad]).all()
+        assert np.isnan(lse.transpose(0, 2, 1)[bad]).all()
+        assert np.isfinite(lse[1, :, :2]).all() and np.isfinite(lse[0, :2]).all()
+
+
+def run_attention_raw(kc, ks, vc, vs, table, P, T, q, kb, vb):
+    dev = lambda a, dt: torch.from_numpy(np.ascontiguousarray(a)).to(dt).cuda()[None, None]
+    cache = das.PagedKVCache(dev(kc, torch.uint8), dev(vc, torch.uint8), dev(ks, torch.float32), dev(vs, torch.float32))
+    ws = das.new_workspace_paged(cache, q.shape[0], q.shape[2], q.shape[1])
+    out, lse = das.das_mature_v_attention_paged(cache, 0, 1, 1, dev_i32(table), dev_i32(P), dev_i32(T), bf16(q), bf16(kb),
+                                                bf16(vb), ws)
+    return out.float().cpu().numpy(), lse.cpu().numpy()
+
+
+def test_attention_lengths_that_change_between_calls():
+    """Calls in a row on one workspace, each with lengths that the one before it did not have."""
+    rng = np.random.default_rng(16)
+    c = list(attention_case(rng, 128, 4, 2, 4, [2000, 900, 64], [4, 4, 4], poison=False))
+    dev = lambda a, dt: torch.from_numpy(np.ascontiguousarray(a)).to(dt).cuda()[None, None]
+    cache = das.PagedKVCache(dev(c[0], torch.uint8), dev(c[2], torch.uint8), dev(c[1], torch.float32),
+                             dev(c[3], torch.float32))
+    ws = das.new_workspace_paged(cache, 3, 4, 4)
+    q, kb, vb = (bf16(x) for x in c[7:])
+    table, P, T = dev_i32(c[4]), dev_i32([0, 0, 0]), dev_i32([0, 0, 0])
+    steps = [([2000, 900, 64], [4, 4, 4]), ([0, 0, 0], [1, 0, 4]), ([1, 899, 0], [2, 2, 2]), ([1999, 65, 63], [0, 0, 0]),
+             ([640, 640, 64], [4, 1, 3])]
+    new = [(dev_i32(p), dev_i32(t)) for p, t in steps]
+    got = []
+    torch.cuda.synchronize()
+    for p, t in new:                                        # no host wait in between
+        P.copy_(p)
+        T.copy_(t)
+        got.append(das.das_mature_v_attention_paged(cache, 0, 1, 1, table, P, T, q, kb, vb, ws))
+    for (p, t), (out, lse) in zip(steps, got):
+        o, l = ref.attention(c[0], np.float32(c[1]), c[2], np.float32(c[3]), c[4], p, t, f64(q), f64(kb), f64(vb))
+        assert_close(f64(out), o, lse.cpu().numpy(), l, where=f"lengths {p}")
+    assert das.workspace_status(ws) == 0
+
+
 def test_attention_clamps_and_flags_lengths():
     rng = np.random.default_rng(11)
     c = list(attention_case(rng, 64, 2, 1, 4, [128, 64], [4, 4], rows=2, poison=False))

@@ -34,6 +34,11 @@ def test_cache_refusals(change, code):
     assert L.das_mature_v_attention_paged(c, 0, 1, 1, A, 4, A, A, 1, 1, A, A, A, 2, 0.0, A, A, A, 1 << 30, NULL) == code
 
 
+def test_page_assign_limits():
+    assert L.das_page_assign(A, A, (1 << 24) + 1, A, 4, A, 8, A, A, 16, A, A, A, A, NULL) == UNSUPPORTED
+    assert L.das_page_assign(A, A, 2, A, 4, A, 8, A, A, (1 << 30) + 1, A, A, A, A, NULL) == UNSUPPORTED
+
+
 def test_append_refusals():
     call = lambda c=cache(), k=A, batch=1, W=4, slots=A, n=4, start=A, flag=A: L.das_kv_append_paged(
         c, k, A, batch, W, slots, n, start, flag, NULL)
