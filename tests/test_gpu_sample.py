@@ -238,3 +238,31 @@ def test_temperatures_whose_quotients_round_awkwardly(T):
     u = np.random.default_rng(10).random((1, 8))
     check(x, u, [T], [0], [0.95], [0.0])
     check(x, u, [T], [300], [1.0], [0.0])
+
+
+@pytest.mark.parametrize("V", [9001, 140003])
+@pytest.mark.parametrize("kind", ["normal", "huge", "large", "small", "sliver", "around zero", "negative", "infinite"])
+@pytest.mark.parametrize("filters", [(0, 0.6, 0.0), (2500, 1.0, 0.0), (1500, 0.9, 0.0), (0, 1e-9, 0.0), (7001, 0.9999, 0.1)])
+def test_rows_of_16_bit_logits(V, kind, filters):
+    """Few distinct values, below, in and above the range of 2^-8 to 2^8 in size."""
+    g = torch.Generator(device="cuda").manual_seed(12)
+    x = torch.randn((2, 1, V), generator=g, device="cuda")
+    T = [1.0, 0.4]
+    if kind == "huge":                   # past the range, of both signs
+        x, T = x * 1e4, [3e3, 50.0]
+    elif kind == "large":                # the largest is below 2^8, many are below -2^8
+        x, T = (x * 100).clamp(max=255.0), [30.0, 5.0]
+    elif kind == "small":                # all below 2^-8
+        x, T = x * 1e-4, [1.0, 1e-5]
+    elif kind == "sliver":               # a few values in the range, the others below it
+        x = x * 2.0 ** -10
+        x[..., 11::1000] += 0.5
+    elif kind == "around zero":          # the threshold lies among logits below 2^-8
+        x = torch.where(torch.rand(x.shape, generator=g, device="cuda") < 0.7, x * 1e-3, x)
+    elif kind == "negative":
+        x, T = x - 40, [2.0, 0.1]
+    elif kind == "infinite":
+        x[..., 5::200] = torch.inf
+        x[1, :, ::3] = -torch.inf
+    k, p, m = filters
+    check(x.to(torch.bfloat16), np.random.default_rng(13).random((2, 1)), T, [k, k], [p, p], [m, m])
