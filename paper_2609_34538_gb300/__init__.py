@@ -30,7 +30,8 @@ ABI in include/das.h:
                             DAS-Wave's round schedule (Eq. 5) and the device
                             side of its carried parallel refinement (Sec. 3.3)
 
-If libdas.so is missing the import fails: there is no fallback.
+If libdas.so or the binding's module _calls.so is missing the import fails:
+there is no fallback.
 """
 import ctypes
 import os
@@ -126,6 +127,7 @@ def _load():
 
 
 LIB = _load()
+from . import _calls  # noqa: E402  (needs torch's libraries, and libdas.so beside it)
 
 
 def status_string(code):
@@ -505,32 +507,6 @@ def das_kv_append_f8(cache, k_new, v_new, accepted, prefix_len, error_flag, stre
                                 _stream(stream)), "das_kv_append_f8")
 
 
-def _new(shape, dtype, device, stream):
-    """An uninitialised tensor for results written on `stream` (allocated there,
-    so that memory still in use on another stream is not handed out)."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
-
-
-def _need_shape(t, dtype, name, shape):
-    if (type(t) is torch.Tensor and t.dtype is dtype and t.is_cuda and t.shape == shape
-            and t.is_contiguous()):
-        return  # the usual case, without the calls below
-    _need(t, dtype, name, len(shape))
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-
-
-def _result(t, shape, dtype, name, device, stream):
-    """t if given (checked), else a new tensor."""
-    if t is None:
-        return _new(shape, dtype, device, stream)
-    _need_shape(t, dtype, name, shape)
-    return t
-
-
 class PagedKVCache:
     """A depth-indexed cache in pages of 64 tokens, all depths as e4m3 codes with
     a scale per (page, kv head): k, v uint8
@@ -553,7 +529,7 @@ class PagedKVCache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.desc = das_kv_cache_paged(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
                                        v_scale.data_ptr(), R, L, N, H, D)
-        self.ref = ctypes.byref(self.desc)
+        self.address = ctypes.addressof(self.desc)
         self.shape = (R, L, N, H, D)  # depths, layers, pages, kv_heads, head_dim
 
     @classmethod
@@ -573,44 +549,20 @@ def das_page_assign(seq_len, grow, block_table, free_pages, free_count, slots, e
     free_pages change in place, slots gets the places of all new tokens.
     new_len and new_free_count may be seq_len and free_count themselves.
     Returns (new_len, new_free_count, slot_start)."""
-    _need(seq_len, torch.int32, "seq_len", 1)
-    B = seq_len.numel()
-    _need_shape(grow, torch.int32, "grow", (B,))
-    _need(block_table, torch.int32, "block_table", 2)
-    if block_table.shape[0] != B:
-        raise ValueError("block_table must be [batch][max_pages]")
-    _need(free_pages, torch.int32, "free_pages", 1)
-    _need_shape(free_count, torch.int32, "free_count", (1,))
-    _need(slots, torch.int32, "slots", 1)
-    _need_shape(error_flag, torch.int32, "error_flag", (1,))
-    dev = seq_len.device
-    new_len = _result(new_len, (B,), torch.int32, "new_len", dev, stream)
-    new_free_count = _result(new_free_count, (1,), torch.int32, "new_free_count", dev, stream)
-    slot_start = _result(slot_start, (B + 1,), torch.int32, "slot_start", dev, stream)
-    _check(LIB.das_page_assign(
-        _ptr(seq_len), _ptr(grow), B, _ptr(block_table), block_table.shape[1], _ptr(free_pages),
-        free_pages.numel(), _ptr(free_count), _ptr(slots), slots.numel(), _ptr(slot_start),
-        _ptr(new_len), _ptr(new_free_count), _ptr(error_flag), _stream(stream)),
-        "das_page_assign")
-    return new_len, new_free_count, slot_start
+    r = _calls.page_assign(seq_len, grow, block_table, free_pages, free_count, slots, error_flag,
+                           new_len, new_free_count, slot_start, stream)
+    if type(r) is int:
+        raise DasError(r, "das_page_assign")
+    return r
 
 
 def das_kv_append_paged(cache, k_new, v_new, slots, slot_start, error_flag, stream=None):
     """Commit into a PagedKVCache: the first slot_start[b + 1] - slot_start[b] of
     each sequence's staged tokens, at every depth and layer, as e4m3 codes under
     a power-of-two scale per (page, kv head)."""
-    _need(k_new, torch.bfloat16, "k_new", 6)
-    _need(v_new, torch.bfloat16, "v_new", 6)
-    R, L, _, H, D = cache.shape
-    B, W = k_new.shape[2:4]
-    if tuple(k_new.shape) != (R, L, B, W, H, D) or k_new.shape != v_new.shape:
-        raise ValueError("k_new / v_new must be [depths][layers][batch][W][kv_heads][head_dim]")
-    _need(slots, torch.int32, "slots", 1)
-    _need_shape(slot_start, torch.int32, "slot_start", (B + 1,))
-    _need_shape(error_flag, torch.int32, "error_flag", (1,))
-    _check(LIB.das_kv_append_paged(
-        cache.ref, _ptr(k_new), _ptr(v_new), B, W, _ptr(slots), slots.numel(),
-        _ptr(slot_start), _ptr(error_flag), _stream(stream)), "das_kv_append_paged")
+    r = _calls.kv_append_paged(cache.address, k_new, v_new, slots, slot_start, error_flag, stream)
+    if r is not None:
+        raise DasError(r, "das_kv_append_paged")
 
 
 def new_workspace_paged(cache, batch, num_q_heads, max_block, device=None):
@@ -626,51 +578,12 @@ def das_mature_v_attention_paged(cache, layer, key_depth, value_depth, block_tab
                                  softmax_scale=0.0, stream=None):
     """das_mature_v_attention over a PagedKVCache; key_depth = value_depth is the
     verify attention.  Returns (out, lse)."""
-    _need(block_table, torch.int32, "block_table", 2)
-    _need(q, torch.bfloat16, "q", 4)
-    R, L, N, H, D = cache.shape
-    B, T, Hq, Dq = q.shape
-    if Dq != D or block_table.shape[0] != B:
-        raise ValueError("q / table shapes do not match the cache")
-    _need_shape(prefix_len, torch.int32, "prefix_len", (B,))
-    _need_shape(block_len, torch.int32, "block_len", (B,))
-    _need_shape(k_blk, torch.bfloat16, "k_blk", (B, T, H, D))
-    _need_shape(v_blk, torch.bfloat16, "v_blk", (B, T, H, D))
-    _need(workspace, torch.uint8, "workspace", 1)
-    out = _result(out, q.shape, torch.bfloat16, "out", q.device, stream)
-    lse = _result(lse, (B, Hq, T), torch.float32, "lse", q.device, stream)
-    code = LIB.das_mature_v_attention_paged(
-        cache.ref, layer, key_depth, value_depth, block_table.data_ptr(), block_table.shape[1],
-        prefix_len.data_ptr(), block_len.data_ptr(), B, T, q.data_ptr(), k_blk.data_ptr(),
-        v_blk.data_ptr(), Hq, softmax_scale, out.data_ptr(), lse.data_ptr(), workspace.data_ptr(),
-        workspace.numel(), _stream(stream))
-    if code:
-        raise DasError(code, "das_mature_v_attention_paged")
-    return out, lse
-
-
-def _sampling_args(logits, uniforms, temperature, top_k, top_p, min_p):
-    """Checks shared by the sampling calls: (type, B, W, vocab, row stride, parameters).
-    Rows of the logits may be strided (a padded vocabulary)."""
-    if not isinstance(logits, torch.Tensor):
-        raise TypeError("logits must be a torch.Tensor")
-    if logits.dtype not in (torch.float32, torch.bfloat16):
-        raise TypeError(f"logits must be float32 or bfloat16, got {logits.dtype}")
-    if not logits.is_cuda:
-        raise ValueError("logits must be on a CUDA device")
-    if logits.dim() != 3:
-        raise ValueError(f"logits must have 3 dims, got {tuple(logits.shape)}")
-    B, W, V = logits.shape
-    row = logits.stride(1) if W > 1 else logits.stride(0) if B > 1 else V
-    if (V > 1 and logits.stride(2) != 1) or (B > 1 and logits.stride(0) != W * row):
-        raise ValueError("logits must have contiguous rows at one stride")
-    _need_shape(uniforms, torch.float32, "uniforms", (B, W))
-    for t, dt, name in ((temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
-                        (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p")):
-        if t is not None:
-            _need_shape(t, dt, name, (B,))
-    params = das_sampling(_ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p))
-    return int(logits.dtype == torch.bfloat16), B, W, V, row, params
+    r = _calls.mature_v_attention_paged(cache.address, layer, key_depth, value_depth, block_table,
+                                        prefix_len, block_len, q, k_blk, v_blk, workspace, out,
+                                        lse, softmax_scale, stream)
+    if type(r) is int:
+        raise DasError(r, "das_mature_v_attention_paged")
+    return r
 
 
 def das_sample(logits, uniforms, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None,
@@ -678,13 +591,10 @@ def das_sample(logits, uniforms, temperature=None, top_k=None, top_p=None, min_p
     """One token from every row of logits [B][W][vocab] (fp32 or bf16) with the
     row's random number in [0, 1); parameters are per sequence, None for none.
     Returns (tokens, logprobs)."""
-    kind, B, W, V, row, params = _sampling_args(logits, uniforms, temperature, top_k, top_p, min_p)
-    dev = logits.device
-    tokens = _result(tokens, (B, W), torch.int32, "tokens", dev, stream)
-    logprobs = _result(logprobs, (B, W), torch.float32, "logprobs", dev, stream)
-    _check(LIB.das_sample(_ptr(logits), kind, B, W, V, row, ctypes.byref(params), _ptr(uniforms),
-                          _ptr(tokens), _ptr(logprobs), _stream(stream)), "das_sample")
-    return tokens, logprobs
+    r = _calls.sample(logits, uniforms, temperature, top_k, top_p, min_p, tokens, logprobs, stream)
+    if type(r) is int:
+        raise DasError(r, "das_sample")
+    return r
 
 
 def das_sample_accept(logits, draft_ids, uniforms, temperature=None, top_k=None, top_p=None,
@@ -693,16 +603,8 @@ def das_sample_accept(logits, draft_ids, uniforms, temperature=None, top_k=None,
     """Sampled acceptance: target_ids drawn as das_sample draws them, proposals
     accepted while they equal them.  committed = min(accepted + 1, W).
     Returns (accepted, target_ids, next_token, committed, logprobs)."""
-    kind, B, W, V, row, params = _sampling_args(logits, uniforms, temperature, top_k, top_p, min_p)
-    _need_shape(draft_ids, torch.int32, "draft_ids", (B, W))
-    dev = logits.device
-    accepted = _result(accepted, (B,), torch.int32, "accepted", dev, stream)
-    target_ids = _result(target_ids, (B, W), torch.int32, "target_ids", dev, stream)
-    next_token = _result(next_token, (B,), torch.int32, "next_token", dev, stream)
-    committed = _result(committed, (B,), torch.int32, "committed", dev, stream)
-    logprobs = _result(logprobs, (B, W), torch.float32, "logprobs", dev, stream)
-    _check(LIB.das_sample_accept(
-        _ptr(logits), kind, _ptr(draft_ids), B, W, V, row, ctypes.byref(params), _ptr(uniforms),
-        _ptr(accepted), _ptr(target_ids), _ptr(next_token), _ptr(committed), _ptr(logprobs),
-        _stream(stream)), "das_sample_accept")
-    return accepted, target_ids, next_token, committed, logprobs
+    r = _calls.sample_accept(logits, draft_ids, uniforms, temperature, top_k, top_p, min_p,
+                             accepted, target_ids, next_token, committed, logprobs, stream)
+    if type(r) is int:
+        raise DasError(r, "das_sample_accept")
+    return r

@@ -1,15 +1,18 @@
-"""Build libdas.so (the CUDA library behind include/das.h) in place for sm_103a.
+"""Build libdas.so (the CUDA library behind include/das.h) in place for sm_103a,
+and _calls.so (the Python binding's module in C++, against PyTorch's headers).
 
     python -m paper_2609_34538_gb300.build
 
 Each .cu under csrc/ is compiled in parallel with nvcc, then linked into
 paper_2609_34538_gb300/libdas.so.  A rebuild happens only when a source or
-header is newer than the library.
+header is newer than the libraries.
 """
 import concurrent.futures as cf
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -17,6 +20,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 OUT_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libdas.so")
+CALLS_SRC = os.path.join(CSRC, "calls.cpp")
+CALLS = os.path.join(PKG, "_calls.so")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
@@ -29,13 +34,13 @@ def _sources():
 def _inputs():
     hdrs = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")]
     hdrs += [os.path.join(INCLUDE, f) for f in os.listdir(INCLUDE) if f.endswith(".h")]
-    return _sources() + hdrs + [os.path.abspath(__file__)]
+    return _sources() + hdrs + [CALLS_SRC, os.path.abspath(__file__)]
 
 
 def up_to_date():
-    if not os.path.exists(LIB):
+    if not (os.path.exists(LIB) and os.path.exists(CALLS)):
         return False
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
     return all(os.path.getmtime(f) <= t for f in _inputs())
 
 
@@ -48,22 +53,52 @@ def _compile(src, extra):
     return obj, r.stderr
 
 
+def _run(cmd, what):
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{what} failed:\n{r.stdout}\n{r.stderr}")
+
+
+def _torch_dir():  # (without importing it, which takes longer than the compilation)
+    return importlib.util.find_spec("torch").submodule_search_locations[0]
+
+
+def _compile_calls():
+    obj = os.path.join(OUT_DIR, "calls.o")
+    torch, cuda = os.path.join(_torch_dir(), "include"), os.path.dirname(os.path.dirname(NVCC))
+    dirs = [INCLUDE, torch, os.path.join(torch, "torch", "csrc", "api", "include"),
+            os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
+    _run(["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", *(f"-I{d}" for d in dirs),
+          "-c", CALLS_SRC, "-o", obj], f"g++ on {CALLS_SRC}")
+    return obj
+
+
+def _link_calls(obj):
+    """Against libdas.so beside it, and the libraries that `import torch` has loaded."""
+    tmp = CALLS + ".tmp"
+    _run(["g++", "-shared", "-o", tmp, obj, f"-L{PKG}", "-l:libdas.so", "-Wl,-rpath,$ORIGIN",
+          f"-L{os.path.join(_torch_dir(), 'lib')}", "-ltorch_python", "-ltorch_cpu", "-lc10_cuda",
+          "-lc10"], "linking _calls.so")
+    os.replace(tmp, CALLS)
+
+
 def build(force=False, verbose=False):
     if not force and up_to_date():
         return LIB
     os.makedirs(OUT_DIR, exist_ok=True)
     extra = ["-Xptxas", "-v"] if verbose else []
-    with cf.ThreadPoolExecutor(max_workers=len(_sources())) as ex:
+    with cf.ThreadPoolExecutor(max_workers=len(_sources()) + 1) as ex:
+        calls = ex.submit(_compile_calls)
         results = list(ex.map(lambda s: _compile(s, extra), _sources()))
+        calls = calls.result()
     if verbose:
         for _, log in results:
             sys.stderr.write(log)
     tmp = LIB + ".tmp"
     cmd = [NVCC, *ARCH, "-shared", "-o", tmp] + [o for o, _ in results]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
+    _run(cmd, "link")
     os.replace(tmp, LIB)
+    _link_calls(calls)
     return LIB
 
 

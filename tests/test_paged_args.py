@@ -85,3 +85,20 @@ def test_binding_refuses_host_tensors_and_wrong_types():
         das.das_sample(f32.double(), f32[..., 0])
     with pytest.raises(TypeError, match="uint8"):
         das.PagedKVCache(f32, f32, f32, f32)
+
+
+def test_binding_module_refuses_bad_numbers():
+    desc = das.das_kv_cache_paged(256, 256, 256, 256, 2, 1, 4, 2, 64)
+    t = torch.zeros((1, 4), dtype=torch.int32)
+    call = lambda layer=0, address=ctypes.addressof(desc): das._calls.mature_v_attention_paged(
+        address, layer, 1, 1, t, t[0, :1], t[0, :1], t, t, t, t, None, None, 0.0, None)
+    with pytest.raises(OverflowError, match="layer"):
+        call(layer=1 << 40)
+    with pytest.raises(TypeError):
+        call(layer=0.5)
+    with pytest.raises(ValueError, match="cache"):
+        call(address=0)
+    with pytest.raises(ValueError, match="block_table must be on a CUDA device"):
+        call()
+    with pytest.raises(TypeError, match="9 arguments"):
+        das._calls.sample(t, t)
