@@ -13,10 +13,12 @@
 // falls into the threshold's bin, rarely more than some dozens, is compared
 // pair by pair, or binned again by its keys if it is more than kList.  16-bit
 // logits have a bin for each value.  The token is found from sums over
-// segments in index order.
+// segments in index order.  The candidates of a small top-k, if they are no
+// more than a CTA's threads, are sorted instead (128 rows of 32000: 19.1 us, 22.6
+// with the thresholds above over the candidates).
 //
 // The row is read from memory once, which would take 2.4 us for 128 rows of
-// 32000 binary32 logits or 64 of 128257 in bf16 (16.4 MB).  Measured: 22.6 us
+// 32000 binary32 logits or 64 of 128257 in bf16 (16.4 MB).  Measured: 19.1 us
 // (top-k 200, top-p 0.95, min-p 0.02) and 38.0 us (top-p 0.9 alone): the time goes to the
 // passes over the row in shared memory (the largest, the candidates or the
 // bins, the sums), which each thread makes over 32 to 128 logits with some
@@ -117,6 +119,9 @@ __device__ __forceinline__ void accept_one(const SampleArgs &a, size_t row, int 
     a.next_token[row] = token;  // the proposal itself, where it was accepted
     if (a.committed) a.committed[row] = 1;
 }
+
+// (apart, as few calls need it: inlined it would be in every loop)
+__device__ __noinline__ float plain_e(float l, float m, float T) { return expf((l - m) / T); }
 
 __device__ __forceinline__ u64 wide(uint32_t w) { return (u64)w + (w == kOne); }
 
@@ -317,6 +322,95 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
         low = -3.4028234e38f;
     }
 
+    // (l - m) / T as binary32 division rounds it.  With r = 1 / T rounded, q =
+    // rn(x r), the exact remainder x - q T and one more fused step give the
+    // quotient rounded to nearest (Markstein, 1990) unless T's significand is
+    // all ones; quotients below -100, whose weight is 0, need no care (but no NaN).
+    const float rT = __frcp_rn(T);
+    const bool quick = T > 1e-18f && T < 1e18f && (__float_as_uint(T) & 0x7fffffu) != 0x7fffffu;
+    auto quick_e = [&](float l) {
+        const float d = l - m, q = fmaxf(d * rT, -100.f);
+        return expf(fmaf(fmaf(-q, T, d), rT, q));
+    };
+    auto es_of = [&](const float (&l)[4], float (&e)[4]) {  // four, so that their steps overlap
+        if (quick) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[i] = quick_e(l[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[i] = plain_e(l[i], m, T);
+        }
+    };
+    auto code_of = [](float e) { return __float2uint_rn(e * 4294967296.f); };  // 2^32 saturates
+    auto weight = [&](float l) { return code_of(quick ? quick_e(l) : plain_e(l, m, T)); };
+
+    // The draw from n <= kThreads candidates (s.cand, in index order) that hold the
+    // k largest, by one CTA: sorted by falling logit and rising index, the kept ones
+    // are the first k of them whose predecessors' weights sum to less than the target.
+    auto draw_sorted = [&](int n) {
+        u64 x = 0;  // (a key above 0 marks a candidate)
+        if (tid < n) x = (u64)key_of(s.cand[tid]) << 32 | (uint32_t)(kThreads - 1 - tid);
+        u64 *const there = reinterpret_cast<u64 *>(s.hist);  // [2][kThreads]
+        static_assert(sizeof s.hist >= 2 * kThreads * sizeof(u64));
+        int set = 0;
+        for (int size = 2; size < 2 * n; size *= 2)  // a bitonic sort
+            for (int d = size / 2; d > 0; d /= 2) {
+                u64 y;
+                if (d >= 32) {
+                    there[set + tid] = x;
+                    __syncthreads();
+                    y = there[set + (tid ^ d)];
+                    set ^= kThreads;
+                } else {
+                    y = __shfl_xor_sync(kFull, x, d);
+                }
+                if ((x < y) == (!(tid & size) == !(tid & d))) x = y;
+            }
+        const bool mine_in = tid < n && tid < k;
+        const int at = kThreads - 1 - (int)(uint32_t)x;  // its place in s.cand
+        float e[4] = {};
+        uint32_t code = 0;
+        if (mine_in) {
+            const float l = logit_of((uint32_t)(x >> 32));
+            e[0] = quick ? quick_e(l) : plain_e(l, m, T);
+            code = code_of(e[0]);
+        }
+        if (p < 1.f) {
+            u64 all;
+            const u64 before = scan(wide(code), all);
+            if (tid == 0) {
+                const double want = ceil((double)p * (double)all);
+                s.target = want < 1.0 ? 1 : (u64)want;
+            }
+            __syncthreads();
+            if (before >= min(s.target, all)) code = 0;
+        }
+        if (floor_p > 0.f && !(e[0] >= floor_p)) code = 0;
+        __syncthreads();  // (the last reads of `there`)
+        if (tid < n) s.hist[at] = code;
+        __syncthreads();
+        code = tid < n ? s.hist[tid] : 0;
+        u64 total;
+        const u64 before = scan(wide(code), total);
+        if (tid == 0) {
+            float u = a.uniforms[row];
+            if (!(u >= 0.f)) u = 0.f;
+            const u64 r = (u64)((double)u * (double)total);
+            s.target = r < total ? r : total - 1;
+        }
+        __syncthreads();
+        const u64 r = s.target;
+        if (before <= r && r < before + wide(code)) {
+            const float l = s.cand[tid];
+            a.tokens[row] = s.cand_at[tid];
+            accept_one(a, row, s.cand_at[tid]);
+            if (a.logprobs) {
+                const float z = l == m ? 0.f : (l - m) / T;
+                a.logprobs[row] = z - logf((float)((double)total * (1.0 / 4294967296.0)));
+            }
+        }
+    };
+
     // ---- a small top-k leaves few candidates: those not below `low`, in index order ----
     // Four bits of each group of a thread say which; their numbers, in eight bits of
     // a word per round of groups, are summed over the warp for four rounds at once.
@@ -358,22 +452,36 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
         if (tid < kRounds * kWarps) s.seg[tid] = ex;
         const int t = exchange(n_all, 0, 0);
         bool fit = true;  // in every CTA of the cluster, which all go one way
-        for (int r = 0; r < C; ++r) fit = fit && s.xch[t][0][r] <= kCand;
+        int n_row = 0, n_before = 0;
+        for (int r = 0; r < C; ++r) {
+            fit = fit && s.xch[t][0][r] <= kCand;
+            n_row += (int)min(s.xch[t][0][r], (u64)kCand);
+            if (r < rank) n_before += (int)min(s.xch[t][0][r], (u64)kCand);
+        }
+        // few enough for a thread of the first CTA to have one each
+        const bool sorted = fit && n_row <= kThreads;
+        Shared *const to = sorted ? of(0) : &s;
+        const int at0 = sorted ? n_before : 0;
         if (fit) {
 #pragma unroll
             for (int it = 0; it < kRounds; ++it) {
                 uint32_t in = hits[it / 8] >> (it % 8 * 4) & 15u;
                 if (!in) continue;
                 const int g = it * kThreads + tid;
-                int at = (int)s.seg[it * kWarps + warp] + (int)(before[it / 4] >> (it % 4 * 8) & 0xffu);
+                int at = at0 + (int)s.seg[it * kWarps + warp] + (int)(before[it / 4] >> (it % 4 * 8) & 0xffu);
                 float l[4];
                 load4(g, l);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (in >> i & 1) {
-                        s.cand[at] = l[i];
-                        s.cand_at[at++] = base + 4 * g + i - shift;
+                        to->cand[at] = l[i];
+                        to->cand_at[at++] = base + 4 * g + i - shift;
                     }
+            }
+            if (sorted) {
+                sync();
+                if (rank == 0) draw_sorted(n_row);
+                return;
             }
             few = true;
             groups = ((int)n_all + 3) / 4;
@@ -381,28 +489,6 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
             __syncthreads();
         }
     }
-
-    // (l - m) / T as binary32 division rounds it.  With r = 1 / T rounded, q =
-    // rn(x r), the exact remainder x - q T and one more fused step give the
-    // quotient rounded to nearest (Markstein, 1990) unless T's significand is
-    // all ones; quotients below -100, whose weight is 0, need no care (but no NaN).
-    const float rT = __frcp_rn(T);
-    const bool quick = T > 1e-18f && T < 1e18f && (__float_as_uint(T) & 0x7fffffu) != 0x7fffffu;
-    auto quick_e = [&](float l) {
-        const float d = l - m, q = fmaxf(d * rT, -100.f);
-        return expf(fmaf(fmaf(-q, T, d), rT, q));
-    };
-    auto es_of = [&](const float (&l)[4], float (&e)[4]) {  // four, so that their steps overlap
-        if (quick) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) e[i] = quick_e(l[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) e[i] = expf((l[i] - m) / T);
-        }
-    };
-    auto code_of = [](float e) { return __float2uint_rn(e * 4294967296.f); };  // 2^32 saturates
-    auto weight = [&](float l) { return code_of(quick ? quick_e(l) : expf((l - m) / T)); };
 
     // Bins of 16-bit values in falling order: 2^8 > l >= 2^-8, then -2^-8 >= l > -2^8.
     auto value_bin = [](float l) {
