@@ -31,8 +31,9 @@ cudaError_t launch_pdl(void (*kernel)(Params...), dim3 grid, dim3 block, cudaStr
 }
 
 // ---- page assignment ----------------------------------------------------------
-constexpr int kAssignThreads = 1024;
+constexpr int kAssignThreads = 1024, kAssignFew = 256;
 constexpr int kFillAlone = 8192;  // slots that one CTA writes along the way
+constexpr int kFillFew = 1024;    // and that kAssignFew threads do
 
 // What one request asks for.
 struct Ask {
@@ -56,60 +57,86 @@ __device__ __forceinline__ Ask ask_of(const PageAssignArgs &a, int b) {
     return r;
 }
 
-// Exclusive sum over the CTA's threads; total is the sum of all.
-__device__ __forceinline__ long long scan(long long v, long long &total, long long *sums) {
+// Exclusive sums of two values over the CTA's NT threads, and their totals.
+struct Pair {
+    long long x, y;
+};
+template <int NT>
+__device__ __forceinline__ Pair scan(Pair v, Pair &total, Pair (*sums)[NT / 32], int &turn) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    long long x = v;
+    Pair s = v;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const long long y = __shfl_up_sync(kFull, x, d);
-        if (lane >= d) x += y;
+        const long long x = __shfl_up_sync(kFull, s.x, d), y = __shfl_up_sync(kFull, s.y, d);
+        if (lane >= d) {
+            s.x += x;
+            s.y += y;
+        }
     }
-    if (lane == 31) sums[warp] = x;
+    turn ^= 1;  // two sets in turn, so that one barrier does
+    if (lane == 31) sums[turn][warp] = s;
     __syncthreads();
-    if (warp == 0) {
-        long long s = sums[lane];
+    // the warps' sums: by each thread for itself if they are few, else by a scan again
+    Pair before = {0, 0};
+    total = {0, 0};
+    if constexpr (NT <= 256) {
+#pragma unroll
+        for (int w = 0; w < NT / 32; ++w) {
+            const Pair p = sums[turn][w];
+            if (w < warp) {
+                before.x += p.x;
+                before.y += p.y;
+            }
+            total.x += p.x;
+            total.y += p.y;
+        }
+    } else {
+        Pair all = lane < NT / 32 ? sums[turn][lane] : Pair{0, 0};
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const long long y = __shfl_up_sync(kFull, s, d);
-            if (lane >= d) s += y;
+            const long long x = __shfl_up_sync(kFull, all.x, d), y = __shfl_up_sync(kFull, all.y, d);
+            if (lane >= d) {
+                all.x += x;
+                all.y += y;
+            }
         }
-        sums[lane] = s;
+        total = {__shfl_sync(kFull, all.x, 31), __shfl_sync(kFull, all.y, 31)};
+        before = {__shfl_sync(kFull, all.x, max(warp - 1, 0)), __shfl_sync(kFull, all.y, max(warp - 1, 0))};
+        if (warp == 0) before = {0, 0};
     }
-    __syncthreads();
-    total = sums[31];
-    const long long r = x - v + (warp > 0 ? sums[warp - 1] : 0);
-    __syncthreads();  // sums may be written again
-    return r;
+    return {before.x + s.x - v.x, before.y + s.y - v.y};
 }
 
-// One CTA.  FILL: it writes the table entries and the slots too; otherwise
-// slot_fill_kernel does, from new_len and slot_start.
-template <bool FILL>
-__global__ void __launch_bounds__(kAssignThreads) page_assign_kernel(const PageAssignArgs a) {
+// One CTA, a thread to a request.  FILL: it writes the table entries and the slots
+// too; otherwise slot_fill_kernel does, from new_len and slot_start.  Bound by
+// latency: 16 requests that grow by up to 17 tokens take 2.7 us, with the lengths,
+// the stack's pages and the stores behind one another and a barrier for each sum.
+template <int NT, bool FILL>
+__global__ void __launch_bounds__(NT) page_assign_kernel(const PageAssignArgs a) {
+    __shared__ Pair sums[2][NT / 32];
+    __shared__ int s_first[NT], s_have[NT], s_num[NT], s_at[NT], s_top[NT];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    __shared__ long long sums[32];
-    __shared__ int s_first[kAssignThreads], s_have[kAssignThreads], s_num[kAssignThreads],
-        s_at[kAssignThreads];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int listed = *a.free_count;
+    Ask r = ask_of(a, tid);
     const int count = listed < 0 ? 0 : (listed > a.pages ? a.pages : listed);
-    int flag = listed != count ? kFlagInvalid : 0;
+    int flag = listed != count ? kFlagInvalid : 0, turn = 0;
+    Pair total;
 
     // pages given back, in request order
     long long gave = 0;
-    for (int c0 = 0; c0 < a.batch; c0 += kAssignThreads) {
-        const Ask r = ask_of(a, c0 + tid);
+    for (int c0 = 0; c0 < a.batch; c0 += NT) {
+        if (c0 > 0) r = ask_of(a, c0 + tid);
         if (r.bad) flag |= kFlagInvalid;
         const int give = r.grows ? 0 : r.have - r.want;
-        long long total;
-        const long long ex = scan(give, total, sums);
+        const Pair ex = scan<NT>({give, 0}, total, sums, turn);
+        if (total.x == 0) continue;  // the same in every thread
         s_first[tid] = r.want;
         s_num[tid] = give;
-        s_at[tid] = (int)min(count + gave + ex, (long long)a.pages);
+        s_at[tid] = (int)min(count + gave + ex.x, (long long)a.pages);
         __syncthreads();
-        for (int i = warp; i < min(kAssignThreads, a.batch - c0); i += kAssignThreads / 32)
+        for (int i = warp; i < min(NT, a.batch - c0); i += NT / 32)
             for (int j = lane; j < s_num[i]; j += 32) {
                 const long long at = (long long)s_at[i] + j;
                 if (at < a.pages)
@@ -117,65 +144,59 @@ __global__ void __launch_bounds__(kAssignThreads) page_assign_kernel(const PageA
                 else
                     flag |= kFlagInvalid;  // more pages than the pool has
             }
-        gave += total;
+        gave += total.x;
         __syncthreads();
     }
     const long long avail = min(count + gave, (long long)a.pages);
 
-    long long asked_pages = 0, asked_slots = 0, took = 0, placed = 0;
-    for (int c0 = 0; c0 < a.batch; c0 += kAssignThreads) {
+    Pair asked = {0, 0}, took = {0, 0};  // pages, slots
+    for (int c0 = 0; c0 < a.batch; c0 += NT) {
         const int b = c0 + tid;
-        const Ask r = ask_of(a, b);
+        if (a.batch > NT) r = ask_of(a, b);
         const int need = r.fits ? r.want - r.have : 0;
         const long long more = r.fits ? r.new_len - r.old_len : 0;
-        long long total;
-        const long long p_in = asked_pages + scan(need, total, sums) + need;
-        asked_pages += total;
-        const long long s_in = asked_slots + scan(more, total, sums) + more;
-        asked_slots += total;
-        const bool served = r.fits && (need == 0 || p_in <= avail) && s_in <= a.max_slots;
-        if (r.grows && !served) flag |= kFlagRefused;
+        Pair ex = scan<NT>({need, more}, total, sums, turn);
+        const bool served = r.fits && (need == 0 || asked.x + ex.x + need <= avail) &&
+                            asked.y + ex.y + more <= a.max_slots;
+        const bool refused = r.grows && !served;
+        if (refused) flag |= kFlagRefused;
+        asked.x += total.x;
+        asked.y += total.y;
         const int take = served ? need : 0;
         const long long num = served ? more : 0;
-        const long long t_ex = took + scan(take, total, sums);
-        took += total;
-        const long long n_ex = placed + scan(num, total, sums);
-        placed += total;
+        if (__syncthreads_or(refused)) ex = scan<NT>({take, num}, total, sums, turn);
+        const long long t_ex = took.x + ex.x, n_ex = took.y + ex.y;
+        took.x += total.x;
+        took.y += total.y;
         if (b < a.batch) {
-            a.new_len[b] = (int)(r.grows && !served ? r.old_len : r.new_len);
+            a.new_len[b] = (int)(refused ? r.old_len : r.new_len);
             a.slot_start[b] = (int)n_ex;
         }
         if (!FILL) continue;
-        // pages from the stack's top into the rows' next entries
-        s_have[tid] = r.have;
-        s_num[tid] = take;
-        s_at[tid] = (int)(avail - 1 - t_ex);
-        __syncthreads();
-        const int nreq = min(kAssignThreads, a.batch - c0);
-        for (int i = warp; i < nreq; i += kAssignThreads / 32)
-            for (int j = lane; j < s_num[i]; j += 32)
-                a.table[(size_t)(c0 + i) * a.max_pages + s_have[i] + j] =
-                    a.free_pages[s_at[i] - j];
-        __syncthreads();
+        // slots, and pages from the stack's top into the rows' next entries
         s_first[tid] = (int)r.old_len;
+        s_have[tid] = r.have;
         s_num[tid] = (int)num;
         s_at[tid] = (int)n_ex;
+        s_top[tid] = (int)(avail - 1 - t_ex);
         __syncthreads();
-        for (int i = warp; i < nreq; i += kAssignThreads / 32)
+        for (int i = warp; i < min(NT, a.batch - c0); i += NT / 32)
             for (int j = lane; j < s_num[i]; j += 32) {
-                const int pos = s_first[i] + j;
-                const int page = a.table[(size_t)(c0 + i) * a.max_pages + pos / kPage];
+                const int pos = s_first[i] + j, at = pos / kPage, fresh = at - s_have[i];
+                int32_t *const entry = a.table + (size_t)(c0 + i) * a.max_pages + at;
+                const int page = fresh < 0 ? *entry : a.free_pages[s_top[i] - fresh];
+                if (fresh >= 0 && pos % kPage == 0) *entry = page;
                 const bool ok = page >= 0 && page < a.pages;
                 if (!ok) flag |= kFlagInvalid;
                 a.slots[s_at[i] + j] = ok ? page * kPage + pos % kPage : -1;
             }
-        __syncthreads();
+        if (a.batch > NT) __syncthreads();
     }
     if (FILL)
-        for (long long i = placed + tid; i < a.max_slots; i += kAssignThreads) a.slots[i] = -1;
+        for (long long i = took.y + tid; i < a.max_slots; i += NT) a.slots[i] = -1;
     if (tid == 0) {
-        a.slot_start[a.batch] = (int)placed;
-        *a.new_free_count = (int)(avail - took);
+        a.slot_start[a.batch] = (int)took.y;
+        *a.new_free_count = (int)(avail - took.x);
     }
     if (flag) atomicOr(a.error_flag, flag);
 }
@@ -533,14 +554,20 @@ __global__ void __launch_bounds__(kAppendThreads) append_paged_kernel(const Appe
 }  // namespace
 
 cudaError_t page_assign_launch(const PageAssignArgs &a, cudaStream_t stream) {
-    // One CTA alone takes 5.2 us for 16 requests and their 144 slots, but 182 us
-    // for 256 requests and 1.2 million slots; a second kernel, which costs the
-    // small call about 2 us, brings that to 14.5 us.
-    if (a.max_slots <= kFillAlone)
-        return launch_pdl(page_assign_kernel<true>, dim3(1), dim3(kAssignThreads), stream, a);
-    const cudaError_t e =
-        launch_pdl(page_assign_kernel<false>, dim3(1), dim3(kAssignThreads), stream, a);
-    if (e != cudaSuccess) return e;
+    // One CTA writes a few thousand slots along the way, but took 182 us for 256
+    // requests and 1.2 million of them; a second kernel, which costs 2 us or more where
+    // there is little to write, brings that to 10.8 us.
+    // The fewer warps, the shorter the barriers and sums: 16 requests and 272 slots take
+    // 2.6 us with 256 threads, 3.6 with 1024.  But the slots of a request are a
+    // warp's: 200 requests and 3400 slots take 8.8 and 5.9 us, and 1000 requests
+    // whose slots the second kernel writes 18.9 and 16.7.
+    const bool fill = a.max_slots <= kFillAlone;
+    const bool few = a.batch <= kAssignFew && (!fill || a.max_slots <= kFillFew);
+    const auto kernel = few ? (fill ? page_assign_kernel<kAssignFew, true> : page_assign_kernel<kAssignFew, false>)
+                            : (fill ? page_assign_kernel<kAssignThreads, true>
+                                    : page_assign_kernel<kAssignThreads, false>);
+    const cudaError_t e = launch_pdl(kernel, dim3(1), dim3(few ? kAssignFew : kAssignThreads), stream, a);
+    if (fill || e != cudaSuccess) return e;
     return launch_pdl(slot_fill_kernel, dim3((unsigned)((a.max_slots + kFillSlots - 1) / kFillSlots)),
                       dim3(kFillThreads), stream, a);
 }
