@@ -17,10 +17,11 @@ constexpr uint32_t kFull = 0xffffffffu;
 
 template <typename... Params, typename... Args>
 cudaError_t launch_pdl(void (*kernel)(Params...), dim3 grid, dim3 block, cudaStream_t stream,
-                       Args... args) {
+                       size_t smem, Args... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -328,7 +329,7 @@ __global__ void __launch_bounds__(kFillThreads) slot_fill_kernel(const PageAssig
 }
 
 // ---- commit -------------------------------------------------------------------
-constexpr int kAppendThreads = 128;
+constexpr int kAppendThreads = 128, kAppendWarps = kAppendThreads / 32;
 
 __device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi) {
     uint32_t r;
@@ -374,181 +375,172 @@ struct AppendArgs {
     const uint16_t *fresh[2];
     const int32_t *slots, *slot_start;
     int32_t *error_flag;
-    int batch, W, pages, kv_heads, max_slots, pieces;
+    int batch, W, pages, kv_heads, max_slots, pieces, rows;
+    unsigned jobs;  // CTAs to the same kAppendWarps heads
 };
 
-// One CTA: one page piece of one sequence, one slab (depth, layer), keys or
-// values, the kv heads one batch after the other.  A thread holds 8 elements of
-// every kStep-th of the piece's tokens; a piece of few tokens leaves places for
-// HB heads at once.  The next batch is on its way while one is converted.
-// Bound by memory: 1001 tokens of 4 sequences at 8 depths and 4 layers 103 us,
-// 6.15 TB/s read and written (134 us with the conversions' first form, which
-// the integer pipe bound); 83 tokens at 32 depths 23 us, 3.2 TB/s, where a CTA's
-// dependent look-ups of its place count.  Runs of slabs to a CTA, which share
-// those, were slower (46 and 182 us: fewer CTAs to an SM).
-template <int D, int HB>
-__device__ __forceinline__ void append_piece(const AppendArgs &a, const uint16_t *src, uint8_t *codes,
-                                             float *scales, int first, int last,
-                                             uint32_t (*s_max)[8][kAppendThreads / 32]) {
-    constexpr int kLanes = D / 8, kStep = kAppendThreads / kLanes, kEach = kPage / kStep / HB;
-    const int lane = threadIdx.x % kLanes, row0 = first + threadIdx.x / kLanes;
-    const int warp = threadIdx.x >> 5;
-    struct Batch {
-        uint4 x[HB][kEach];
-        float held[HB];
-    };
-    auto load = [&](int h0, Batch &v) {
+// The largest finite magnitude among eight elements, as bf16 bits.
+__device__ __forceinline__ uint32_t finite_amax(uint4 x) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    uint32_t amax = 0;
 #pragma unroll
-        for (int g = 0; g < HB; ++g) {
-            v.held[g] = first > 0 && h0 + g < a.kv_heads ? scales[h0 + g] : 0.f;
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t lo = w[j] & 0x7fffu, hi = (w[j] >> 16) & 0x7fffu;
+        if (lo < 0x7f80u) amax = max(amax, lo);
+        if (hi < 0x7f80u) amax = max(amax, hi);
+    }
+    return amax;
+}
+
+// Eight elements as codes under a scale.  A product with the reciprocal of a power
+// of two (a normal number itself) is the exact quotient; other scales, which only
+// pages that a caller has filled can have, take a division.
+struct Divisor {
+    __device__ __forceinline__ explicit Divisor(float scale) : scale(scale) {
+        const uint32_t bits = __float_as_uint(scale);
+        exact = (bits & 0x807fffffu) == 0 && bits >= 0x00800000u && bits < 0x7f000000u;
+        inverse = __uint_as_float(0x7f000000u - bits);
+    }
+    template <typename F>
+    __device__ __forceinline__ uint2 each(uint4 x, F f) const {
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        float v[8];
 #pragma unroll
-            for (int u = 0; u < kEach; ++u) {
-                const int i = row0 + u * kStep;
-                v.x[g][u] = make_uint4(0, 0, 0, 0);
-                if (i < last && h0 + g < a.kv_heads)
-                    v.x[g][u] = __ldcs(reinterpret_cast<const uint4 *>(
-                        src + ((ptrdiff_t)i * a.kv_heads + h0 + g) * D + lane * 8));
-            }
+        for (int j = 0; j < 4; ++j) {
+            v[2 * j] = f(__uint_as_float(w[j] << 16));
+            v[2 * j + 1] = f(__uint_as_float(w[j] & 0xffff0000u));
         }
-    };
-    Batch v, next;
-    load(0, v);
-    for (int h0 = 0, turn = 0; h0 < a.kv_heads; h0 += HB, turn ^= 1) {
-        if (h0 + HB < a.kv_heads) load(h0 + HB, next);
+        return make_uint2(pack4_e4m3(v[0], v[1], v[2], v[3]), pack4_e4m3(v[4], v[5], v[6], v[7]));
+    }
+    __device__ __forceinline__ uint2 codes(uint4 x) const {
+        return each(x, [&](float v) { return v * inverse; });
+    }
+    __device__ __forceinline__ uint2 divided(uint4 x) const {
+        return each(x, [&](float v) { return v / scale; });
+    }
+    float scale, inverse;
+    bool exact;
+};
+
+// The codes of rows i0, i0 + step, ... < end under a larger scale: times ratio.
+__device__ __forceinline__ void rescale(uint8_t *dst, int D, int i0, int step, int end, float ratio) {
+    for (int i = i0; i < end; i += step) {
+        uint2 *at = reinterpret_cast<uint2 *>(dst + i * D);
+        const uint2 was = *at;
+        const uint32_t w[4] = {was.x & 0xffffu, was.x >> 16, was.y & 0xffffu, was.y >> 16};
+        uint32_t c[4];
 #pragma unroll
-        for (int g = 0; g < HB; ++g) {
-            uint32_t amax = 0;
-#pragma unroll
-            for (int u = 0; u < kEach; ++u) {
-                const uint32_t w[4] = {v.x[g][u].x, v.x[g][u].y, v.x[g][u].z, v.x[g][u].w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) amax = max_bf16x2(amax, w[j] & 0x7fff7fffu);
-            }
-            amax = max(amax & 0xffffu, amax >> 16);
-            if (amax >= 0x7f80u) {  // an infinity (NaN loses): the largest finite one
-                amax = 0;
-#pragma unroll
-                for (int u = 0; u < kEach; ++u) {
-                    const uint32_t w[4] = {v.x[g][u].x, v.x[g][u].y, v.x[g][u].z, v.x[g][u].w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t lo = w[j] & 0x7fffu, hi = (w[j] >> 16) & 0x7fffu;
-                        if (lo < 0x7f80u) amax = max(amax, lo);
-                        if (hi < 0x7f80u) amax = max(amax, hi);
-                    }
-                }
-            }
-            amax = __reduce_max_sync(kFull, amax);
-            if ((threadIdx.x & 31) == 0) s_max[turn][g][warp] = amax;
+        for (int j = 0; j < 4; ++j) {
+            float lo, hi;
+            unpack_e4m3(w[j], lo, hi);
+            c[j] = pack_e4m3(lo * ratio, hi * ratio);
         }
-        __syncthreads();
-#pragma unroll
-        for (int g = 0; g < HB; ++g) {
-            if (h0 + g >= a.kv_heads) continue;
-            uint32_t amax = 0;
-#pragma unroll
-            for (int w = 0; w < kAppendThreads / 32; ++w) amax = max(amax, s_max[turn][g][w]);
-            const float held = v.held[g];
-            const float scale = first > 0 ? fmaxf(scale_of(amax), held) : scale_of(amax);
-            // a product with the reciprocal of a power of two is the exact quotient
-            const float inv = 1.f / scale;
-            const bool exact = (__float_as_uint(scale) & 0x7fffffu) == 0;
-            uint8_t *dst = codes + (size_t)(h0 + g) * (kPage * D) + lane * 8;
-#pragma unroll
-            for (int u = 0; u < kEach; ++u) {
-                const int i = row0 + u * kStep;
-                if (i >= last) continue;
-                const uint32_t w[4] = {v.x[g][u].x, v.x[g][u].y, v.x[g][u].z, v.x[g][u].w};
-                float f[8];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    f[2 * j] = __uint_as_float(w[j] << 16);
-                    f[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-                }
-                if (exact) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) f[j] *= inv;
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) f[j] /= scale;
-                }
-                *reinterpret_cast<uint2 *>(dst + i * D) =
-                    make_uint2(pack4_e4m3(f[0], f[1], f[2], f[3]), pack4_e4m3(f[4], f[5], f[6], f[7]));
-            }
-            if (first > 0 && scale != held) {  // the older tokens' codes under the larger scale
-                const float ratio = held / scale;
-                for (int i = threadIdx.x / kLanes; i < first; i += kStep) {
-                    uint2 *at = reinterpret_cast<uint2 *>(dst + i * D);
-                    const uint2 was = *at;
-                    const uint32_t w[4] = {was.x & 0xffffu, was.x >> 16, was.y & 0xffffu, was.y >> 16};
-                    uint32_t c[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        float lo, hi;
-                        unpack_e4m3(w[j], lo, hi);
-                        c[j] = pack_e4m3(lo * ratio, hi * ratio);
-                    }
-                    *at = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
-                }
-            }
-            if (threadIdx.x == 0) scales[h0 + g] = scale;
-        }
-        v = next;
+        *at = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
     }
 }
 
+// A warp to a (sequence, page piece, slab, keys or values, kv head); up to kPage tokens
+// are one piece, on whichever two pages they lie.  The tokens go into shared memory
+// while their places are looked up (of several pieces: the sequence's first place
+// before), and are read there twice, for the scale and for the codes: no head
+// waits for another, and short loops leave registers and instruction cache for
+// many warps.  Bound by memory: 1001 tokens of 4 sequences at 8 depths and 4
+// layers 92.3 us, 6.86 TB/s read and written; 83 tokens at 32 depths 17.9 us, 4.2 TB/s,
+// where the chain of a warp's look-ups counts.  A CTA to a piece of all heads with
+// the tokens in registers, which needs no shared memory, took 100 and 23 us: three
+// times the instructions, and warps that wait for each other's maxima.
 template <int D>
 __global__ void __launch_bounds__(kAppendThreads) append_paged_kernel(const AppendArgs a) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    __shared__ uint32_t s_max[2][8][kAppendThreads / 32];
+    extern __shared__ uint4 s_rows[];  // [warp][rows][D / 8]
+    constexpr int kLanes = D / 8, kStep = 32 / kLanes;
+    const int lane = threadIdx.x & 31, row = lane / kLanes, warp = threadIdx.x >> 5;
     unsigned x = blockIdx.x;
-    const int which = x & 1;
-    x >>= 1;
+    const int job = (int)(x / a.jobs) * kAppendWarps + warp;
+    const int which = job >= a.kv_heads, h = job - (which ? a.kv_heads : 0);
+    x %= a.jobs;
     const int piece = x % a.pieces;
     x /= a.pieces;
     const int b = x % a.batch;
     const size_t slab = x / a.batch;
+    uint4 *const mine = s_rows + warp * a.rows * kLanes + lane % kLanes;  // a lane reads what it copied
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (job >= 2 * a.kv_heads) return;
 
     const int s0 = a.slot_start[b];
-    const long long n = (long long)a.slot_start[b + 1] - s0;
-    if (n < 0 || n > a.W || s0 < 0 || s0 + n > a.max_slots) {
-        if (threadIdx.x == 0) atomicOr(a.error_flag, kFlagInvalid);
+    const long long n_all = (long long)a.slot_start[b + 1] - s0;
+    if (n_all < 0 || n_all > a.W || s0 < 0 || s0 + n_all > a.max_slots) {
+        if (lane == 0) atomicOr(a.error_flag, kFlagInvalid);
         return;
     }
-    if (n == 0) return;
-    const int slot0 = a.slots[s0];
-    if (slot0 < 0) {
-        if (threadIdx.x == 0) atomicOr(a.error_flag, kFlagInvalid);
-        return;
+    if (n_all == 0) return;
+    int slot = a.slots[s0], begin = 0, end = (int)n_all;
+    if (a.pieces > 1) {
+        if (slot < 0) {
+            if (lane == 0) atomicOr(a.error_flag, kFlagInvalid);
+            return;
+        }
+        const int t = piece * kPage - slot % kPage;  // the token at the page's first place
+        if (t >= end) return;
+        begin = max(t, 0);
+        end = min(t + kPage, end);
+        if (piece) slot = a.slots[s0 + begin];
     }
-    const int o = slot0 % kPage;
-    const int t0 = piece * kPage - o;  // the token at the page's first place (negative: an older one)
-    if (t0 >= n) return;
-    const int slot = piece ? a.slots[s0 + t0] : slot0;
-    const int page = slot / kPage;
-    if (slot < 0 || page >= a.pages || (piece && slot % kPage)) {
-        if (threadIdx.x == 0) atomicOr(a.error_flag, kFlagInvalid);
-        return;
+    {
+        const size_t stride = (size_t)a.kv_heads * D;
+        const uint16_t *src = a.fresh[which] + ((slab * a.batch + b) * a.W + begin + row) * stride +
+                              h * D + lane % kLanes * 8;
+        for (int t = begin + row; t < end; t += kStep, src += kStep * stride)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
+                             (uint32_t)__cvta_generic_to_shared(mine + (t - begin) * kLanes)),
+                         "l"(src)
+                         : "memory");
     }
-    const int first = piece ? 0 : o;                       // places [first, last) are new
-    const int last = (int)min((long long)kPage, n - t0);
-    const uint16_t *src =
-        a.fresh[which] + ((ptrdiff_t)(slab * a.batch + b) * a.W + t0) * a.kv_heads * D;
-    const size_t tile = (slab * a.pages + page) * a.kv_heads;
-    uint8_t *codes = a.codes[which] + tile * (kPage * D);
-    float *scales = a.scales[which] + tile;
-    // as many heads at once as leave every token a place
-    constexpr int kStep = kAppendThreads / (D / 8), kPlaces = kPage / kStep;
-    const int steps = (last - first + kStep - 1) / kStep;
-    if (kPlaces >= 8 && steps <= kPlaces / 8)
-        append_piece<D, kPlaces >= 8 ? 8 : 1>(a, src, codes, scales, first, last, s_max);
-    else if (steps <= kPlaces / 4)
-        append_piece<D, 4>(a, src, codes, scales, first, last, s_max);
-    else if (steps <= kPlaces / 2)
-        append_piece<D, 2>(a, src, codes, scales, first, last, s_max);
-    else
-        append_piece<D, 1>(a, src, codes, scales, first, last, s_max);
+    for (int t0 = begin; t0 < end;) {  // the tokens up to the page's end, then the others
+        const int first = slot < 0 ? 0 : slot % kPage, page = slot / kPage;
+        if (slot < 0 || page >= a.pages || ((t0 > 0 || piece) && first)) {
+            if (lane == 0) atomicOr(a.error_flag, kFlagInvalid);
+            break;
+        }
+        const int t1 = min(end, t0 + kPage - first);
+        if (t1 < end) slot = a.slots[s0 + t1];
+        const size_t tile = (slab * a.pages + page) * a.kv_heads + h;
+        float *const at_scale = a.scales[which] + tile;
+        const float held = first > 0 ? *at_scale : 0.f;
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        // this lane's rows of the page: [i, i_end) in steps of kStep
+        const int r0 = t0 - begin, i0 = r0 + (row + kStep - r0 % kStep) % kStep, i_end = t1 - begin;
+        uint32_t amax = 0;
+#pragma unroll 4
+        for (int i = i0; i < i_end; i += kStep) {
+            const uint4 x = mine[i * kLanes];
+            amax = max_bf16x2(max_bf16x2(amax, max_bf16x2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu)),
+                              max_bf16x2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
+        }
+        amax = max(amax & 0xffffu, amax >> 16);
+        if (amax >= 0x7f80u) {  // an infinity (NaN loses): the largest finite one
+            amax = 0;
+#pragma unroll 1
+            for (int i = i0; i < i_end; i += kStep) amax = max(amax, finite_amax(mine[i * kLanes]));
+        }
+        const float scale = fmaxf(scale_of(__reduce_max_sync(kFull, amax)), held);
+        uint8_t *const codes = a.codes[which] + tile * (kPage * D) + lane % kLanes * 8;
+        uint8_t *dst = codes + (first + i0 - r0) * D;
+        const Divisor by(scale);
+        if (by.exact) {
+#pragma unroll 4
+            for (int i = i0; i < i_end; i += kStep, dst += kStep * D)
+                *reinterpret_cast<uint2 *>(dst) = by.codes(mine[i * kLanes]);
+        } else {
+#pragma unroll 1
+            for (int i = i0; i < i_end; i += kStep, dst += kStep * D)
+                *reinterpret_cast<uint2 *>(dst) = by.divided(mine[i * kLanes]);
+        }
+        if (first > 0 && scale != held) rescale(codes, D, row, kStep, first, held / scale);
+        if (lane == 0) *at_scale = scale;
+        t0 = t1;
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 }  // namespace
@@ -566,10 +558,10 @@ cudaError_t page_assign_launch(const PageAssignArgs &a, cudaStream_t stream) {
     const auto kernel = few ? (fill ? page_assign_kernel<kAssignFew, true> : page_assign_kernel<kAssignFew, false>)
                             : (fill ? page_assign_kernel<kAssignThreads, true>
                                     : page_assign_kernel<kAssignThreads, false>);
-    const cudaError_t e = launch_pdl(kernel, dim3(1), dim3(few ? kAssignFew : kAssignThreads), stream, a);
+    const cudaError_t e = launch_pdl(kernel, dim3(1), dim3(few ? kAssignFew : kAssignThreads), stream, 0, a);
     if (fill || e != cudaSuccess) return e;
     return launch_pdl(slot_fill_kernel, dim3((unsigned)((a.max_slots + kFillSlots - 1) / kFillSlots)),
-                      dim3(kFillThreads), stream, a);
+                      dim3(kFillThreads), stream, 0, a);
 }
 
 cudaError_t append_paged_launch(const das_kv_cache_paged &c, const void *k_new, const void *v_new,
@@ -591,14 +583,21 @@ cudaError_t append_paged_launch(const das_kv_cache_paged &c, const void *k_new, 
     a.pages = c.pages;
     a.kv_heads = c.kv_heads;
     a.max_slots = max_slots;
-    a.pieces = (W + 2 * kPage - 2) / kPage;
-    const long long ctas = (long long)c.depths * c.layers * batch * a.pieces * 2;
+    a.pieces = W <= kPage ? 1 : (W + 2 * kPage - 2) / kPage;
+    a.rows = std::min(W, kPage);
+    const long long jobs = (long long)c.depths * c.layers * batch * a.pieces;
+    const long long ctas = jobs * ((2LL * c.kv_heads + kAppendWarps - 1) / kAppendWarps);
     if (ctas > 0x7fffffffLL) return cudaErrorInvalidValue;
+    a.jobs = (unsigned)jobs;
     if (ctas == 0) return cudaSuccess;
-    return c.head_dim == 128 ? launch_pdl(append_paged_kernel<128>, dim3((unsigned)ctas),
-                                          dim3(kAppendThreads), stream, a)
-                             : launch_pdl(append_paged_kernel<64>, dim3((unsigned)ctas),
-                                          dim3(kAppendThreads), stream, a);
+    const auto kernel = c.head_dim == 128 ? append_paged_kernel<128> : append_paged_kernel<64>;
+    const size_t smem = (size_t)kAppendWarps * a.rows * c.head_dim * 2;
+    if (smem > 49152) {
+        const cudaError_t e =
+            cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_pdl(kernel, dim3((unsigned)ctas), dim3(kAppendThreads), stream, smem, a);
 }
 
 }  // namespace das

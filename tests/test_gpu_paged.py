@@ -442,3 +442,22 @@ def test_assign_append_attend():
         fin = np.isfinite(l)
         assert np.abs(lse.cpu().numpy()[fin] - l[fin]).max() <= 1e-5 * max(10.0, np.abs(l[fin]).max())
     assert das.workspace_status(ws) == 0
+
+
+@pytest.mark.parametrize("H,D,first,n,W", [(3, 128, [10, 62], [3, 60], 64), (5, 64, [33, 1], [80, 63], 100),
+                                           (1, 64, [63, 9], [1, 15], 15), (2, 128, [40, 7], [64, 64], 64)])
+@pytest.mark.parametrize("held", [1.5 * 2.0 ** 5, 1.5 * 2.0 ** -20])
+def test_append_into_pages_with_other_scales(H, D, first, n, W, held):
+    """Scales that are no powers of two, kept (large) and replaced (small); infinities among the
+    new tokens, whose scale comes from the finite ones.  x / (1.5 2^j) is exact or lies a third
+    of a bfloat16's last place off every tie, so the rounding through binary32 changes no code."""
+    rng = np.random.default_rng(W + D)
+    codes, scales, x, slots, start = append_case(rng, 1, 1, H, D, first, n, W, 6)
+    scales[:] = held
+    x[..., 0, 3] = np.inf
+    cache, k, v, flag = run_append(codes, scales, x, slots, start)
+    wk, wks = ref.append(codes, scales, k, slots, start)
+    wv, wvs = ref.append(codes[..., ::-1], 2 * scales, v, slots, start)
+    assert same_codes(cache.k, wk) and same_codes(cache.v, wv)
+    assert np.array_equal(cache.k_scale.cpu().numpy(), wks) and np.array_equal(cache.v_scale.cpu().numpy(), wvs)
+    assert flag.item() == 0
