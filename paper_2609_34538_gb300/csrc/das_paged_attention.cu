@@ -205,6 +205,25 @@ __device__ int plan(const PagedAttnParams &p, const int *lens, Walk &w) {
     return (int)max(0ll, at[1] - at[0]);  // the host admits no more than 2^30 a CTA
 }
 
+// In clusters: the tiles of a pair that CTA `rank` of 1 << log_c takes, [lo, hi).  The block
+// tile, the last one, weighs kLastWeight pages where there are several to a CTA.
+constexpr int kLastWeight = 2;
+struct Share {
+    int lo, hi;
+};
+__device__ __forceinline__ Share share_of(int nt, int log_c, int rank) {  // (nt < 2^26)
+    const int W = nt + (nt >= 4 << log_c ? kLastWeight : 0);
+    return {min(nt, rank * W >> log_c), min(nt, (rank + 1) * W >> log_c)};
+}
+__device__ int plan_pair(const PagedAttnParams &p, const int *lens, Walk &w) {
+    const int pair = blockIdx.x >> p.log_cluster;
+    w = {pair / p.Hkv, pair % p.Hkv, 0, 1, 0, 0, lens};
+    walk_load(p, w);
+    const Share s = share_of(w.nt, p.log_cluster, blockIdx.x & ((1 << p.log_cluster) - 1));
+    w.t = s.lo;
+    return s.hi - s.lo;
+}
+
 // A place in a ring of N and the parity of its present phase, kept by counting
 // (a 64-bit remainder is a long dependent sequence).
 template <int N>
@@ -253,7 +272,9 @@ struct Layout {
     static constexpr uint32_t kSwizzle = D == 128 ? 2 : 4;  // 128- or 64-byte rows
     static_assert(kTile % 1024 == 0 && kQ8Off % 1024 == 0 && kPbOff % 1024 == 0, "alignment");
     static_assert(kInfos >= 32 + kStages + 1, "tile numbers in use are not written over");
+    static constexpr int kPartRow = D + 4;  // floats of a partial's row (and bank padding)
     static_assert(kBytes <= 232448, "shared memory per CTA");
+    static_assert(kRows * (kPartRow + 1) * 4 <= kStages * kStage, "a partial fits the stages");
 };
 
 // byte offset of 16-byte chunk c of row m: rows of D bytes, swizzled
@@ -356,7 +377,29 @@ __device__ __forceinline__ void load_block(const PagedAttnParams &p, const Walk 
     }
 }
 
-template <int D>
+__device__ __forceinline__ uint32_t at_rank(uint32_t addr, int rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float ld_cluster(uint32_t addr, int rank) {
+    float x;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(at_rank(addr, rank)) : "memory");
+    return x;
+}
+__device__ __forceinline__ void ld_cluster2(uint32_t addr, int rank, float &x, float &y) {
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];"
+                 : "=f"(x), "=f"(y)
+                 : "r"(at_rank(addr, rank))
+                 : "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// CLUSTER: a cluster of 1 << p.log_cluster CTAs to a pair, which join their partials through
+// their shared memory; else the list of all pairs' tiles, and paged_merge_kernel.
+template <int D, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads, 1)
     paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k,
                       const __grid_constant__ CUtensorMap tm_v, const PagedAttnParams p) {
@@ -373,6 +416,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                    b_pvdone = b_pready + 16, b_drain = b_pvdone + 16;
     TileInfo *info = reinterpret_cast<TileInfo *>(sm + Lt::kInfoOff);
     int *qexp = reinterpret_cast<int *>(sm + Lt::kExpOff);  // [2][kRows]
+    float *const part_sm = reinterpret_cast<float *>(sm);  // [kRows][kPartRow] O, [kRows] lse
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(sm + Lt::kMiscOff);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(sm + Lt::kMiscOff + 4);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -424,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     Walk w0 = {0, 0, 0, 1, 0, 0, nullptr};
     int ntiles = 0;
     if (early) {
-        ntiles = plan(p, len_sm, w0);
+        ntiles = CLUSTER ? plan_pair(p, len_sm, w0) : plan(p, len_sm, w0);
         // Into L2 while the kernels before this one finish: the range's first pages
         // (if the table still says other pages after the wait, these were for
         // nothing), their scales, and the first queries.
@@ -467,7 +511,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             __syncthreads();
         }
     }
-    if (!kept) ntiles = plan(p, early ? len_sm : nullptr, w0);
+    if (!kept) {
+        const int *const lens = early ? len_sm : nullptr;
+        ntiles = CLUSTER ? plan_pair(p, lens, w0) : plan(p, lens, w0);
+    }
     if (blockIdx.x == 0 && warp == 0)
         for (int b = lane; b < p.B; b += 32)
             if (p.prefix_len[b] != prefix_of(p, b) || p.block_len[b] != block_of(p, b))
@@ -934,7 +981,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const size_t slot =
                     ((size_t)(w.b * p.Hkv + w.h) + blockIdx.x) * p.rows_max + row;
                 uint16_t *orow = p.out + (((size_t)w.b * p.max_block + irow) * p.Hq + gq) * D;
-                float *prow = p.part_o + slot * D;
+                // (a cluster's partials take the place of the tiles, which are done with)
+                float *prow = CLUSTER ? part_sm + row * Lt::kPartRow : p.part_o + slot * D;
                 // group g writes columns [g D / 2, (g + 1) D / 2), 32 at a time
                 float x[D / 64][16];
                 const uint32_t o0 = lanes + kOCol + (uint32_t)((k_seg & 1) * kOStep);
@@ -986,6 +1034,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (half == 0 && group == 0) {
                         if (whole)
                             p.lse[((size_t)w.b * p.Hq + gq) * p.max_block + irow] = lse;
+                        else if (CLUSTER)
+                            part_sm[kRows * Lt::kPartRow + row] = lse;
                         else
                             p.part_lse[slot] = lse;
                     }
@@ -1024,6 +1074,65 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp == 0)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem),
                      "n"(kTmemCols));
+    if constexpr (CLUSTER) {
+        // ---- the cluster's partials joined: every C-th row by one of its CTAs ----
+        // (formulas as in paged_merge_kernel)
+        constexpr int V = D / 32, kMaxC = 8;
+        const int C = 1 << p.log_cluster, rank = blockIdx.x & (C - 1);
+        bool held[kMaxC];  // whether CTA r has a partial
+        int n = 0;
+#pragma unroll
+        for (int r = 0; r < kMaxC; ++r) {
+            const Share s = share_of(w0.nt, p.log_cluster, min(r, C - 1));
+            held[r] = r < C && s.hi > s.lo;
+            n += held[r];
+        }
+        if (n <= 1) return;  // one CTA had the pair (the same in all of them)
+        __syncwarp();
+        cluster_sync();
+        for (int row = rank + C * warp; row < p.rows_max; row += C * (kThreads / 32)) {
+            const int i = row / p.G, g = w0.h * p.G + row % p.G;
+            float ls[kMaxC], o[kMaxC][V], M = -INFINITY, L = 0.f, acc[V];
+            const uint32_t at_o = smem_u32(part_sm + row * Lt::kPartRow + V * lane);
+            const uint32_t at_l = smem_u32(part_sm + kRows * Lt::kPartRow + row);
+#pragma unroll
+            for (int r = 0; r < kMaxC; ++r) {
+                ls[r] = -INFINITY;
+#pragma unroll
+                for (int v = 0; v < V; ++v) o[r][v] = 0.f;
+                if (held[r] && row < p.G * w0.T) {
+                    ls[r] = ld_cluster(at_l, r);
+#pragma unroll
+                    for (int v = 0; v < V; v += 2) ld_cluster2(at_o + 4 * v, r, o[r][v], o[r][v + 1]);
+                }
+            }
+            bool nan = false;
+#pragma unroll
+            for (int r = 0; r < kMaxC; ++r) {
+                M = fmaxf(M, ls[r]);
+                nan = nan || ls[r] != ls[r];
+            }
+            const float m = M == -INFINITY && !nan ? 0.f : M;
+#pragma unroll
+            for (int v = 0; v < V; ++v) acc[v] = 0.f;
+#pragma unroll
+            for (int r = 0; r < kMaxC; ++r) {
+                const float x = __expf(ls[r] - m);
+                L += x;
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[v] += x * o[r][v];
+            }
+            const float inv = L == 0.f ? 0.f : 1.f / L;
+            uint16_t *orow = p.out + (((size_t)w0.b * p.max_block + i) * p.Hq + g) * D + V * lane;
+#pragma unroll
+            for (int v = 0; v < V; v += 2)
+                *reinterpret_cast<uint32_t *>(orow + v) = pack_bf16(acc[v] * inv, acc[v + 1] * inv);
+            if (lane == 0)
+                p.lse[((size_t)w0.b * p.Hq + g) * p.max_block + i] =
+                    L == 0.f ? -INFINITY : m + __logf(L);
+        }
+        cluster_sync();  // no CTA ends while another reads its partial
+    }
 }
 
 // ---- merge ------------------------------------------------------------------------
@@ -1118,8 +1227,49 @@ __global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const Pag
 
 size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 
+// The logarithm of the CTAs to a pair where clusters are used, else 0.
+// Joined in shared memory a call takes 2.7 us less than with the merge kernel (4 pairs
+// of 5 tiles: 6.8 and 9.6 us), as much as six tiles of a CTA; but pairs cannot share a CTA, so the longest sequence's tiles are
+// a cluster's alone and some SMs stay idle.  Lengths are not known here: clusters
+// are used where they cost no more than that for any, a CTA's tiles for the
+// longest length that the table allows against an equal share of the tiles of the
+// shortest (one sequence: of the same) length.
 template <int D>
-cudaError_t launch_d(const PagedAttnParams &p, const CUtensorMap &tm_k, const CUtensorMap &tm_v,
+int log_cluster_of(const PagedAttnParams &p, int dev) {
+    constexpr int kSaved = 6;
+    static std::atomic<int> most[64][4];  // 1 + the clusters of 1 << i CTAs that fit the device
+    if (dev >= 64) return 0;
+    const long long pairs = (long long)p.B * p.Hkv, nt = (long long)p.max_pages + 1;
+    for (int i = 3; i > 0; --i) {
+        const int C = 1 << i;
+        if (pairs * C > p.num_ctas) continue;
+        const long long own = (nt + C - 1) / C, shared = p.B == 1 ? pairs * nt / p.num_ctas : 0;
+        if (own - shared > kSaved) return 0;  // (smaller clusters cost more)
+        int fit = most[dev][i].load(std::memory_order_relaxed);
+        if (fit == 0) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3((unsigned)(p.num_ctas / C * C));
+            cfg.blockDim = dim3(kThreads);
+            cfg.dynamicSmemBytes = Layout<D>::kBytes;
+            cudaLaunchAttribute attr[1];
+            attr[0].id = cudaLaunchAttributeClusterDimension;
+            attr[0].val.clusterDim.x = C;
+            attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+            cfg.attrs = attr;
+            cfg.numAttrs = 1;
+            int n = 0;
+            if (cudaOccupancyMaxActiveClusters(&n, paged_attn_kernel<D, true>, &cfg) != cudaSuccess)
+                n = 0;
+            fit = 1 + n;
+            most[dev][i].store(fit, std::memory_order_relaxed);
+        }
+        if (pairs <= fit - 1) return i;
+    }
+    return 0;
+}
+
+template <int D>
+cudaError_t launch_d(PagedAttnParams &p, const CUtensorMap &tm_k, const CUtensorMap &tm_v,
                      cudaStream_t stream) {
     constexpr int smem = Layout<D>::kBytes;
     static std::atomic<bool> configured[64];  // the shared-memory opt-in, once per device
@@ -1127,22 +1277,32 @@ cudaError_t launch_d(const PagedAttnParams &p, const CUtensorMap &tm_k, const CU
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev >= 64 || !configured[dev].load(std::memory_order_acquire)) {
-        e = cudaFuncSetAttribute(paged_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 smem);
-        if (e != cudaSuccess) return e;
+        for (const auto kernel : {paged_attn_kernel<D, false>, paged_attn_kernel<D, true>}) {
+            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+            if (e != cudaSuccess) return e;
+        }
         if (dev < 64) configured[dev].store(true, std::memory_order_release);
     }
+    p.log_cluster = log_cluster_of<D>(p, dev);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)p.num_ctas);
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, paged_attn_kernel<D>, tm_k, tm_v, p);
+    if (p.log_cluster) {
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = 1 << p.log_cluster;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
+        cfg.gridDim = dim3((unsigned)(p.B * p.Hkv << p.log_cluster));
+        return cudaLaunchKernelEx(&cfg, paged_attn_kernel<D, true>, tm_k, tm_v, p);
+    }
+    e = cudaLaunchKernelEx(&cfg, paged_attn_kernel<D, false>, tm_k, tm_v, p);
     if (e != cudaSuccess) return e;
     const long long rblocks = (p.rows_max + kMergeWarps - 1) / kMergeWarps;
     cfg.gridDim = dim3((unsigned)((long long)p.B * p.Hkv * rblocks));
