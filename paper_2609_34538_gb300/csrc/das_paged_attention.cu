@@ -245,15 +245,17 @@ struct TileInfo {
 };
 constexpr int kInfos = 64;  // ring of the pages' numbers: 32 looked up, and those in the stages
 
-template <int D>
+template <int D, bool CLUSTER>
 struct Layout {
-    static constexpr int kStages = 8;
+    // in clusters the last stage and the second buffer of queries, side by side, take
+    // the cluster's partials: a CTA has one segment there
+    static constexpr int kAllStages = 8, kStages = CLUSTER ? 7 : 8;
     static constexpr int kTile = kTileKeys * D;         // an e4m3 tile
     static constexpr int kStage = 2 * kTile;            // keys, values
     static constexpr int kQ8 = 2 * kRows * D;           // split queries [128 rows][D]
     static constexpr int kBf = kTileKeys * D * 2;       // a bf16 tile or the bf16 queries
     static constexpr int kPb = 2 * kRows * kTileKeys * 2;  // P of the block tile
-    static constexpr int kQ8Off = kStages * kStage;
+    static constexpr int kQ8Off = kAllStages * kStage;
     static constexpr int kQbOff = kQ8Off + 2 * kQ8;
     // the block tile's P takes the place of its queries, which S is done with
     static constexpr int kPbOff = kQbOff;
@@ -262,7 +264,7 @@ struct Layout {
     static constexpr int kBarOff = kVbOff + kBf;
     // full, empty [kStages], qready, qfree [2], bready, bfree, sready, sfree
     // [kSBufs], pready, pvdone [2], drain [2]
-    static constexpr int kBars = 2 * kStages + 4 + 2 + 2 * kSBufs + 4 + 2;
+    static constexpr int kBars = 2 * kAllStages + 4 + 2 + 2 * kSBufs + 4 + 2;
     static constexpr int kInfoOff = (kBarOff + kBars * 8 + 15) / 16 * 16;
     static constexpr int kExpOff = kInfoOff + kInfos * 16;
     static constexpr int kMlOff = kExpOff + 2 * kRows * 4;  // (m, l) of each group's rows
@@ -272,9 +274,10 @@ struct Layout {
     static constexpr uint32_t kSwizzle = D == 128 ? 2 : 4;  // 128- or 64-byte rows
     static_assert(kTile % 1024 == 0 && kQ8Off % 1024 == 0 && kPbOff % 1024 == 0, "alignment");
     static_assert(kInfos >= 32 + kStages + 1, "tile numbers in use are not written over");
-    static constexpr int kPartRow = D + 4;  // floats of a partial's row (and bank padding)
+    static constexpr int kPartOff = kQ8Off - kStage;  // [kRows][D] floats, and [kRows] of lse:
+    static constexpr int kPartLseOff = kExpOff;       // the exponents' first half
     static_assert(kBytes <= 232448, "shared memory per CTA");
-    static_assert(kRows * (kPartRow + 1) * 4 <= kStages * kStage, "a partial fits the stages");
+    static_assert(kStage + kQ8 == kRows * D * 4, "partials take a stage and a buffer of queries");
 };
 
 // byte offset of 16-byte chunk c of row m: rows of D bytes, swizzled
@@ -382,19 +385,13 @@ __device__ __forceinline__ uint32_t at_rank(uint32_t addr, int rank) {
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
-__device__ __forceinline__ float ld_cluster(uint32_t addr, int rank) {
-    float x;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(at_rank(addr, rank)) : "memory");
-    return x;
+__device__ __forceinline__ void st_cluster(uint32_t addr, float x) {
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(x) : "memory");
 }
-__device__ __forceinline__ void ld_cluster2(uint32_t addr, int rank, float &x, float &y) {
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];"
-                 : "=f"(x), "=f"(y)
-                 : "r"(at_rank(addr, rank))
+__device__ __forceinline__ void st_cluster4(uint32_t addr, float x, float y, float z, float w) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(x), "f"(y),
+                 "f"(z), "f"(w)
                  : "memory");
-}
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // CLUSTER: a cluster of 1 << p.log_cluster CTAs to a pair, which join their partials through
@@ -403,7 +400,7 @@ template <int D, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads, 1)
     paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k,
                       const __grid_constant__ CUtensorMap tm_v, const PagedAttnParams p) {
-    using Lt = Layout<D>;
+    using Lt = Layout<D, CLUSTER>;
     constexpr int kStages = Lt::kStages;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -416,7 +413,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                    b_pvdone = b_pready + 16, b_drain = b_pvdone + 16;
     TileInfo *info = reinterpret_cast<TileInfo *>(sm + Lt::kInfoOff);
     int *qexp = reinterpret_cast<int *>(sm + Lt::kExpOff);  // [2][kRows]
-    float *const part_sm = reinterpret_cast<float *>(sm);  // [kRows][kPartRow] O, [kRows] lse
+    constexpr int kFirstQ = CLUSTER;  // the buffer of the first segment's queries
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(sm + Lt::kMiscOff);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(sm + Lt::kMiscOff + 4);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -450,6 +447,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             "n"(kTmemCols));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
+    if constexpr (CLUSTER)  // waited for before the first store to another CTA: it has begun
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    bool begun = false;
     int *len_sm = reinterpret_cast<int *>(sm + Lt::kLenOff);
     const bool early = p.B <= kLens;
     if (early && warp == kProducerWarp) {
@@ -638,7 +638,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int k_end = min(ntiles, k + w.nt - w.t);
             const bool has_blk = w.t + (k_end - k) == w.nt;
             const uint64_t dq8 =
-                sdesc(sbase + Lt::kQ8Off + (seg & 1) * Lt::kQ8, 16, 8 * D, Lt::kSwizzle);
+                sdesc(sbase + Lt::kQ8Off + ((seg + kFirstQ) & 1) * Lt::kQ8, 16, 8 * D, Lt::kSwizzle);
             ok = waits(b_qready + 8 * (seg & 1), (uint32_t)((seg >> 1) & 1));
             for (const int k_blk = has_blk ? k_end - 1 : k_end; k < k_blk && ok; ++k) {
                 ok = waits(b_full + 8 * st.i, st.phase);
@@ -736,7 +736,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int seg = 0; left > 0; ++seg) {
             const int q = seg & 1;
             if (seg >= 2 && !waits(b_qfree + 8 * q, (uint32_t)(((seg >> 1) - 1) & 1))) break;
-            split_queries<D>(p, w, sbase + Lt::kQ8Off + q * Lt::kQ8, qexp + q * kRows, ct);
+            const int buf = (seg + kFirstQ) & 1;
+            split_queries<D>(p, w, sbase + Lt::kQ8Off + buf * Lt::kQ8, qexp + buf * kRows, ct);
             fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(b_qready + 8 * q);
@@ -776,7 +777,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int q = seg & 1;
                 waits(b_qready + 8 * q, (uint32_t)((seg >> 1) & 1));
                 row_scale = p.scale_log2 *
-                            __uint_as_float((uint32_t)(127 - qexp[q * kRows + row]) << 23);
+                            __uint_as_float((uint32_t)(127 - qexp[((q + kFirstQ) & 1) * kRows + row]) << 23);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(b_qfree + 8 * q);
             }
@@ -981,8 +982,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const size_t slot =
                     ((size_t)(w.b * p.Hkv + w.h) + blockIdx.x) * p.rows_max + row;
                 uint16_t *orow = p.out + (((size_t)w.b * p.max_block + irow) * p.Hq + gq) * D;
-                // (a cluster's partials take the place of the tiles, which are done with)
-                float *prow = CLUSTER ? part_sm + row * Lt::kPartRow : p.part_o + slot * D;
+                float *prow = p.part_o + slot * D;
+                // in a cluster row r is joined by CTA r % C, where the partial of CTA c has
+                // place c * kRows / C + r / C, its 16-byte chunks xored with the row
+                const int log_c = p.log_cluster, C = 1 << log_c, to = row & (C - 1);
+                const int place = ((blockIdx.x & (C - 1)) << 6 >> log_c) + (row >> log_c);
+                const uint32_t far = CLUSTER ? at_rank(sbase + Lt::kPartOff + place * (D * 4), to) : 0;
                 // group g writes columns [g D / 2, (g + 1) D / 2), 32 at a time
                 float x[D / 64][16];
                 const uint32_t o0 = lanes + kOCol + (uint32_t)((k_seg & 1) * kOStep);
@@ -1011,6 +1016,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 // both groups have read both O and ml: the next segment may write them
                 fence_before();
+                if constexpr (CLUSTER) {
+                    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+                    begun = true;
+                }
                 asm volatile("bar.sync 1, 256;" ::: "memory");
                 if (live) {
 #pragma unroll
@@ -1024,6 +1033,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                                     pack_bf16(x[c][j + 2], x[c][j + 3]),
                                     pack_bf16(x[c][j + 4], x[c][j + 5]),
                                     pack_bf16(x[c][j + 6], x[c][j + 7]));
+                        } else if (CLUSTER) {
+#pragma unroll
+                            for (int j = 0; j < 16; j += 4)
+                                st_cluster4(far + (((d0 + j) / 4 ^ (place & (D / 4 - 1))) << 4), x[c][j],
+                                            x[c][j + 1], x[c][j + 2], x[c][j + 3]);
                         } else {
 #pragma unroll
                             for (int j = 0; j < 16; j += 4)
@@ -1035,7 +1049,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (whole)
                             p.lse[((size_t)w.b * p.Hq + gq) * p.max_block + irow] = lse;
                         else if (CLUSTER)
-                            part_sm[kRows * Lt::kPartRow + row] = lse;
+                            st_cluster(at_rank(sbase + Lt::kPartLseOff + place * 4, to), lse);
                         else
                             p.part_lse[slot] = lse;
                     }
@@ -1054,6 +1068,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             kp += k_blk - k_seg;
             k = k_end;
         }
+    }
+    if constexpr (CLUSTER) {  // this CTA's partials are where they belong
+        __syncwarp();
+        if (!begun) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     }
     if (warp == kSWarp || warp == kPvWarp) {
         // every MMA that this warp issued is complete before tensor memory is
@@ -1087,23 +1106,30 @@ __global__ void __launch_bounds__(kThreads, 1)
             held[r] = r < C && s.hi > s.lo;
             n += held[r];
         }
-        if (n <= 1) return;  // one CTA had the pair (the same in all of them)
         __syncwarp();
-        cluster_sync();
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (n <= 1) return;  // one CTA had the pair
+        const float *const part_o = reinterpret_cast<const float *>(sm + Lt::kPartOff);
+        const float *const part_lse = reinterpret_cast<const float *>(sm + Lt::kPartLseOff);
         for (int row = rank + C * warp; row < p.rows_max; row += C * (kThreads / 32)) {
             const int i = row / p.G, g = w0.h * p.G + row % p.G;
             float ls[kMaxC], o[kMaxC][V], M = -INFINITY, L = 0.f, acc[V];
-            const uint32_t at_o = smem_u32(part_sm + row * Lt::kPartRow + V * lane);
-            const uint32_t at_l = smem_u32(part_sm + kRows * Lt::kPartRow + row);
 #pragma unroll
             for (int r = 0; r < kMaxC; ++r) {
                 ls[r] = -INFINITY;
 #pragma unroll
                 for (int v = 0; v < V; ++v) o[r][v] = 0.f;
                 if (held[r] && row < p.G * w0.T) {
-                    ls[r] = ld_cluster(at_l, r);
+                    const int place = (r << 6 >> p.log_cluster) + (row >> p.log_cluster);
+                    const int chunk = (V * lane / 4) ^ (place & (D / 4 - 1));
+                    ls[r] = part_lse[place];
 #pragma unroll
-                    for (int v = 0; v < V; v += 2) ld_cluster2(at_o + 4 * v, r, o[r][v], o[r][v + 1]);
+                    for (int v = 0; v < V; v += 2) {
+                        const float2 x = *reinterpret_cast<const float2 *>(
+                            part_o + place * D + chunk * 4 + (V * lane & 3) + v);
+                        o[r][v] = x.x;
+                        o[r][v + 1] = x.y;
+                    }
                 }
             }
             bool nan = false;
@@ -1131,7 +1157,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                 p.lse[((size_t)w0.b * p.Hq + g) * p.max_block + i] =
                     L == 0.f ? -INFINITY : m + __logf(L);
         }
-        cluster_sync();  // no CTA ends while another reads its partial
     }
 }
 
@@ -1250,7 +1275,7 @@ int log_cluster_of(const PagedAttnParams &p, int dev) {
             cudaLaunchConfig_t cfg = {};
             cfg.gridDim = dim3((unsigned)(p.num_ctas / C * C));
             cfg.blockDim = dim3(kThreads);
-            cfg.dynamicSmemBytes = Layout<D>::kBytes;
+            cfg.dynamicSmemBytes = Layout<D, true>::kBytes;
             cudaLaunchAttribute attr[1];
             attr[0].id = cudaLaunchAttributeClusterDimension;
             attr[0].val.clusterDim.x = C;
@@ -1271,7 +1296,8 @@ int log_cluster_of(const PagedAttnParams &p, int dev) {
 template <int D>
 cudaError_t launch_d(PagedAttnParams &p, const CUtensorMap &tm_k, const CUtensorMap &tm_v,
                      cudaStream_t stream) {
-    constexpr int smem = Layout<D>::kBytes;
+    constexpr int smem = Layout<D, false>::kBytes;
+    static_assert(smem == Layout<D, true>::kBytes, "one size for both");
     static std::atomic<bool> configured[64];  // the shared-memory opt-in, once per device
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);

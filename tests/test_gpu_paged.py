@@ -461,3 +461,31 @@ def test_append_into_pages_with_other_scales(H, D, first, n, W, held):
     assert same_codes(cache.k, wk) and same_codes(cache.v, wv)
     assert np.array_equal(cache.k_scale.cpu().numpy(), wks) and np.array_equal(cache.v_scale.cpu().numpy(), wvs)
     assert flag.item() == 0
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=[str(s)[:60] for s in SHAPES])
+def test_attention_with_a_wide_table(shape):
+    """Tables far wider than the prefixes, whose unused entries name no page: the pairs' tiles are
+    then split as one list, where a narrow table has a pair's tiles shared by a cluster."""
+    D, Hq, Hkv, Tm, P, T = shape
+    rng = np.random.default_rng(D + Hq + Tm + len(P))
+    case = list(attention_case(rng, D, Hq, Hkv, Tm, P, T))
+    wide = np.full((len(P), 600), 10 ** 6, dtype=case[4].dtype)
+    for b, n in enumerate(P):
+        wide[b, :-(-n // PAGE)] = case[4][b, :-(-n // PAGE)]
+    case[4] = wide
+    run_attention(*case, where=str(shape)[:60])
+
+
+@pytest.mark.parametrize("D,Hq,Hkv,Tm,P,T", [
+    (128, 32, 32, 8, [1500], [8]), (128, 64, 16, 3, [1100], [2]), (64, 8, 8, 16, [2900], [16]),
+    (128, 8, 4, 32, [2047], [31]), (64, 76, 76, 1, [640], [1]), (128, 2, 2, 64, [450, 3], [64, 1]),
+    (128, 9, 3, 5, [0, 511, 64], [5, 0, 4])])
+def test_attention_of_pairs_shared_by_clusters(D, Hq, Hkv, Tm, P, T):
+    """One to several tiles a CTA, CTAs without any, rows of every number, and a row count that no
+    cluster divides; the same result every time."""
+    rng = np.random.default_rng(D + Hq + Tm)
+    case = attention_case(rng, D, Hq, Hkv, Tm, P, T)
+    out, lse = run_attention(*case, where="cluster")
+    again, lse2 = run_attention(*case, where="cluster")
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
