@@ -1014,13 +1014,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                             x[c][j] += (__uint_as_float(a[j]) + kPLoInv * __uint_as_float(e[j])) * f1;
                     }
                 }
-                // both groups have read both O and ml: the next segment may write them
-                fence_before();
                 if constexpr (CLUSTER) {
                     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
                     begun = true;
+                } else {  // both groups have read both O and ml: the next segment may write them
+                    fence_before();
+                    asm volatile("bar.sync 1, 256;" ::: "memory");
                 }
-                asm volatile("bar.sync 1, 256;" ::: "memory");
                 if (live) {
 #pragma unroll
                     for (int c = 0; c < D / 64; ++c) {
@@ -1074,23 +1074,28 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!begun) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     }
-    if (warp == kSWarp || warp == kPvWarp) {
-        // every MMA that this warp issued is complete before tensor memory is
-        // freed (only a timed-out run can leave any in flight)
-        const uint32_t drain = b_drain + (warp == kSWarp ? 8 : 0);
-        if (elect_one()) mma_commit(drain);
-        __syncwarp();
-        const unsigned long long t0 = globaltimer();
-        while (!mbar_try_wait(drain, 0) && globaltimer() - t0 < kWaitNs) {
-        }
-    }
     fence_before();
     __syncthreads();
     fence_after();
-    if (*abort_flag && warp == kProducerWarp && elect_one())  // copies in flight land before exit
-        for (int j = issued - 1; j >= 0 && j >= issued - kStages; --j)
-            drain_wait(b_full + 8 * (j % kStages), (uint32_t)(j / kStages) & 1);
-    if (warp == 0)
+    if (*abort_flag) {  // a timed-out run: MMAs and copies may be in flight yet
+        if (warp == kSWarp || warp == kPvWarp) {
+            const uint32_t drain = b_drain + (warp == kSWarp ? 8 : 0);
+            if (elect_one()) mma_commit(drain);
+            __syncwarp();
+            const unsigned long long t0 = globaltimer();
+            while (!mbar_try_wait(drain, 0) && globaltimer() - t0 < kWaitNs) {
+            }
+        }
+        if (warp == kProducerWarp && elect_one())
+            for (int j = issued - 1; j >= 0 && j >= issued - kStages; --j)
+                drain_wait(b_full + 8 * (j % kStages), (uint32_t)(j / kStages) & 1);
+        __syncwarp();
+        fence_before();
+        __syncthreads();
+        fence_after();
+    }
+    // (else the softmax warps have seen every product's completion)
+    if (warp == kThreads / 32 - 1)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem),
                      "n"(kTmemCols));
     if constexpr (CLUSTER) {
