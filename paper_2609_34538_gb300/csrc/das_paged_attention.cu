@@ -46,6 +46,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 
 #include "das_internal.h"
 #include "das_tcgen05.h"
@@ -1257,24 +1258,29 @@ __global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const Pag
 
 size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 
-// The logarithm of the CTAs to a pair where clusters are used, else 0.
-// Joined in shared memory a call takes 2.7 us less than with the merge kernel (4 pairs
-// of 5 tiles: 6.8 and 9.6 us), as much as six tiles of a CTA; but pairs cannot share a CTA, so the longest sequence's tiles are
-// a cluster's alone and some SMs stay idle.  Lengths are not known here: clusters
-// are used where they cost no more than that for any, a CTA's tiles for the
-// longest length that the table allows against an equal share of the tiles of the
-// shortest (one sequence: of the same) length.
+// The logarithm of the CTAs to a pair where clusters are used, else -1.
+// Measured (16 shapes, 2 to 32 pairs, 4096 to 32768 tokens, in tiles of 0.34 us): a cluster's
+// CTA takes its tiles and 23; in the list a CTA takes an equal share of all and
+// 29 + 1.3 for each of a pair's segments, which are joined one after the other.
+// One sequence of 4096 tokens with 32, 8 and 2 kv heads takes 13.6, 10.1 and 10.9 us
+// in clusters, 16.3, 18.5 and 30.7 in the list; of 32768 tokens 51.9, 29.2 and
+// 29.6, and 50.5, 26.0 and 43.4.
+// Lengths are not known here.  Taken is what the list could gain at most where x
+// pairs are as long as the table allows and the others empty, x from a sequence's kv heads to all
+// pairs: own - 6 - x nt / CTAs - 1.3 CTAs / x, largest at x = CTAs sqrt(1.3 / nt).
 template <int D>
 int log_cluster_of(const PagedAttnParams &p, int dev) {
-    constexpr int kSaved = 6;
     static std::atomic<int> most[64][4];  // 1 + the clusters of 1 << i CTAs that fit the device
-    if (dev >= 64) return 0;
+    if (dev >= 64) return -1;
     const long long pairs = (long long)p.B * p.Hkv, nt = (long long)p.max_pages + 1;
-    for (int i = 3; i > 0; --i) {
+    const double ctas = p.num_ctas,
+                 x = std::min(std::max(ctas * std::sqrt(1.3 / (double)nt), (double)p.Hkv), (double)pairs);
+    const double list = 6.0 + x * (double)nt / ctas + 1.3 * ctas / x;
+    for (int i = 3; i >= 0; --i) {
         const int C = 1 << i;
         if (pairs * C > p.num_ctas) continue;
-        const long long own = (nt + C - 1) / C, shared = p.B == 1 ? pairs * nt / p.num_ctas : 0;
-        if (own - shared > kSaved) return 0;  // (smaller clusters cost more)
+        if ((double)((nt + C - 1) / C) > list) return -1;  // (smaller clusters cost more)
+        if (i == 0) return 0;
         int fit = most[dev][i].load(std::memory_order_relaxed);
         if (fit == 0) {
             cudaLaunchConfig_t cfg = {};
@@ -1295,7 +1301,7 @@ int log_cluster_of(const PagedAttnParams &p, int dev) {
         }
         if (pairs <= fit - 1) return i;
     }
-    return 0;
+    return -1;
 }
 
 template <int D>
@@ -1325,7 +1331,7 @@ cudaError_t launch_d(PagedAttnParams &p, const CUtensorMap &tm_k, const CUtensor
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (p.log_cluster) {
+    if (p.log_cluster >= 0) {
         attr[1].id = cudaLaunchAttributeClusterDimension;
         attr[1].val.clusterDim.x = 1 << p.log_cluster;
         attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
