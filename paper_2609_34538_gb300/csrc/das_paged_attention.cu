@@ -1175,6 +1175,36 @@ __global__ void __launch_bounds__(kThreads, 1)
 constexpr int kMergeWarps = 2;
 constexpr int kMergeLoads = 4;
 
+struct Cut {  // a pair's segments: of CTAs c0, c0 + 1, ... if dense
+    Split sp;
+    long long q0;
+    int c0, n;
+    bool dense;
+};
+__device__ __forceinline__ Cut cut_of(const PagedAttnParams &p, int b, int h) {
+    const int lane = threadIdx.x & 31;
+    long long total = 0, before = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 32) {
+        const int nt = seq_tiles(p, b0 + lane);
+        total += (long long)__reduce_add_sync(kFull, (unsigned)nt) * p.Hkv;
+        before += (long long)__reduce_add_sync(kFull, b0 + lane < b ? (unsigned)nt : 0u) * p.Hkv;
+    }
+    Cut c;
+    c.sp = split_of(p, total);
+    const int nt = tiles_of(prefix_of(p, b));
+    c.q0 = before + (long long)h * nt + (long long)c.sp.beta * (b * p.Hkv + h);
+    c.c0 = cta_of(c.q0, c.sp, p.num_ctas);
+    // with fewer tiles than CTAs a tile is a CTA's own and the CTAs between are empty
+    c.dense = c.sp.beta > 0 || c.sp.N >= p.num_ctas;
+    c.n = c.dense ? cta_of(c.q0 + nt - 1, c.sp, p.num_ctas) - c.c0 + 1 : nt;
+    return c;
+}
+// where a row's partial of segment s is
+__device__ __forceinline__ size_t slot_of(const PagedAttnParams &p, const Cut &c, int pair, int s, int row) {
+    const int cta = c.dense ? c.c0 + s : cta_of(c.q0 + s, c.sp, p.num_ctas);
+    return ((size_t)pair + cta) * p.rows_max + row;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const PagedAttnParams p) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -1185,20 +1215,8 @@ __global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const Pag
     const int pair = blockIdx.x / rblocks, lane = threadIdx.x & 31;
     const int row = (blockIdx.x % rblocks) * kMergeWarps + (threadIdx.x >> 5);
     const int b = pair / p.Hkv, h = pair % p.Hkv;
-    long long total = 0, before = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 32) {
-        const int nt = seq_tiles(p, b0 + lane);
-        total += (long long)__reduce_add_sync(kFull, (unsigned)nt) * p.Hkv;
-        before += (long long)__reduce_add_sync(kFull, b0 + lane < b ? (unsigned)nt : 0u) * p.Hkv;
-    }
-    const Split sp = split_of(p, total);
-    const int nt = tiles_of(prefix_of(p, b));
-    const long long q0 = before + (long long)h * nt + (long long)sp.beta * pair;
-    const int c0 = cta_of(q0, sp, p.num_ctas);
-    // with fewer tiles than CTAs a tile is a CTA's own and the CTAs between are empty
-    const bool dense = sp.beta > 0 || sp.N >= p.num_ctas;
-    const int nseg = dense ? cta_of(q0 + nt - 1, sp, p.num_ctas) - c0 + 1 : nt;
-    const int rows_active = p.G * block_of(p, b);
+    const Cut cut = cut_of(p, b, h);
+    const int nseg = cut.n, rows_active = p.G * block_of(p, b);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (nseg <= 1 || row >= p.rows_max) return;
     const int i = row / p.G, g = h * p.G + row % p.G;
@@ -1216,8 +1234,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const Pag
 #pragma unroll
                 for (int v = 0; v < V; ++v) o[u][v] = 0.f;
                 if (s0 + u < nseg) {
-                    const int c = dense ? c0 + s0 + u : cta_of(q0 + s0 + u, sp, p.num_ctas);
-                    const size_t slot = ((size_t)pair + c) * p.rows_max + row;
+                    const size_t slot = slot_of(p, cut, pair, s0 + u, row);
                     ls[u] = __ldcg(p.part_lse + slot);
                     const float *src = p.part_o + slot * D + V * lane;
 #pragma unroll
@@ -1256,26 +1273,127 @@ __global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const Pag
     if (lane == 0) *lrow = L == 0.f ? -INFINITY : M + __logf(L);
 }
 
+// The same where pairs have many segments: a row by both warps of a CTA.  A warp's
+// four groups of eight lanes take every fourth segment, two at a time, with a
+// reference and sums of their own, so that sixteen segments of a row are on their
+// way at once.  2 kv heads, 32768 tokens in a table that no cluster is used for: 22 us, 43 with a warp
+// to a row and four at once.
+struct Part {  // sums under the reference M
+    float M, L;
+};
+// the factors of two parts under their common reference, for which a becomes their sum
+__device__ __forceinline__ float2 join(Part &a, Part b) {
+    const float m = fmaxf(a.M, b.M);
+    const float2 f = {a.M == m ? 1.f : __expf(a.M - m), b.M == m ? 1.f : __expf(b.M - m)};
+    a = {m, a.L * f.x + b.L * f.y};
+    return f;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_many_kernel(const PagedAttnParams p) {
+    __shared__ float4 s_acc[32];
+    __shared__ Part s_part;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    constexpr int kChunks = D / 32;  // of 8 lanes x 4 floats
+    constexpr int kGroups = 4, kLoads = 2, kStep = 2 * kGroups;
+    const int pair = blockIdx.x / p.rows_max, row = blockIdx.x % p.rows_max;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = lane >> 3, col = 4 * (lane & 7);
+    const int b = pair / p.Hkv, h = pair % p.Hkv;
+    const Cut cut = cut_of(p, b, h);
+    const int rows_active = p.G * block_of(p, b);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (cut.n <= 1) return;  // (the same in both warps)
+    Part part = {-INFINITY, 0.f};
+    float acc[4 * kChunks];
+#pragma unroll
+    for (int v = 0; v < 4 * kChunks; ++v) acc[v] = 0.f;
+    if (row < rows_active) {
+        for (int s0 = warp * kGroups + group; s0 < cut.n; s0 += kLoads * kStep) {
+            float ls[kLoads];
+            float4 o[kLoads][kChunks];
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) {
+                ls[u] = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) o[u][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (s0 + u * kStep < cut.n) {
+                    const size_t slot = slot_of(p, cut, pair, s0 + u * kStep, row);
+                    ls[u] = __ldcg(p.part_lse + slot);
+#pragma unroll
+                    for (int c = 0; c < kChunks; ++c)
+                        o[u][c] = __ldcg(reinterpret_cast<const float4 *>(p.part_o + slot * D + 32 * c + col));
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) {
+                if (ls[u] == -INFINITY) continue;
+                // (a NaN goes into the sums, not into the reference)
+                const float2 f = join(part, {ls[u] == ls[u] ? ls[u] : part.M, ls[u] == ls[u] ? 1.f : ls[u]});
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) {
+                    acc[4 * c] = acc[4 * c] * f.x + o[u][c].x * f.y;
+                    acc[4 * c + 1] = acc[4 * c + 1] * f.x + o[u][c].y * f.y;
+                    acc[4 * c + 2] = acc[4 * c + 2] * f.x + o[u][c].z * f.y;
+                    acc[4 * c + 3] = acc[4 * c + 3] * f.x + o[u][c].w * f.y;
+                }
+            }
+        }
+    }
+    // the groups' sums, the lower lane's first in both lanes; then group c has chunk c
+#pragma unroll
+    for (int d = 8; d < 32; d *= 2) {
+        const Part other = {__shfl_xor_sync(kFull, part.M, d), __shfl_xor_sync(kFull, part.L, d)};
+        Part low = lane & d ? other : part;
+        const float2 f = join(low, lane & d ? part : other);
+        part = low;
+#pragma unroll
+        for (int v = 0; v < 4 * kChunks; ++v) {
+            const float y = __shfl_xor_sync(kFull, acc[v], d);
+            acc[v] = lane & d ? y * f.x + acc[v] * f.y : acc[v] * f.x + y * f.y;
+        }
+    }
+    float4 x = make_float4(acc[0], acc[1], acc[2], acc[3]);
+#pragma unroll
+    for (int c = 1; c < kChunks; ++c)
+        if (group == c) x = make_float4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
+    if (warp == 1) {
+        s_acc[lane] = x;
+        if (lane == 0) s_part = part;
+    }
+    __syncthreads();
+    if (warp == 1) return;
+    const float4 y = s_acc[lane];
+    const float2 f = join(part, s_part);
+    const int i = row / p.G, g = h * p.G + row % p.G;
+    const float inv = part.L == 0.f ? 0.f : 1.f / part.L, fx = f.x * inv, fy = f.y * inv;
+    if (group < kChunks)
+        *reinterpret_cast<uint2 *>(p.out + (((size_t)b * p.max_block + i) * p.Hq + g) * D + 32 * group + col) =
+            make_uint2(pack_bf16(x.x * fx + y.x * fy, x.y * fx + y.y * fy),
+                       pack_bf16(x.z * fx + y.z * fy, x.w * fx + y.w * fy));
+    if (lane == 0)
+        p.lse[((size_t)b * p.Hq + g) * p.max_block + i] =
+            part.L == 0.f ? -INFINITY : part.M + __logf(part.L);
+}
+
 size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 
 // The logarithm of the CTAs to a pair where clusters are used, else -1.
-// Measured (16 shapes, 2 to 32 pairs, 4096 to 32768 tokens, in tiles of 0.34 us): a cluster's
-// CTA takes its tiles and 23; in the list a CTA takes an equal share of all and
-// 29 + 1.3 for each of a pair's segments, which are joined one after the other.
-// One sequence of 4096 tokens with 32, 8 and 2 kv heads takes 13.6, 10.1 and 10.9 us
-// in clusters, 16.3, 18.5 and 30.7 in the list; of 32768 tokens 51.9, 29.2 and
-// 29.6, and 50.5, 26.0 and 43.4.
-// Lengths are not known here.  Taken is what the list could gain at most where x
-// pairs are as long as the table allows and the others empty, x from a sequence's kv heads to all
-// pairs: own - 6 - x nt / CTAs - 1.3 CTAs / x, largest at x = CTAs sqrt(1.3 / nt).
+// Measured at 38 shapes, in tiles of 0.34 us: a cluster's CTA takes its own tiles and 23; in the
+// list a CTA takes an equal share of all tiles and 32 + 0.25 for each of a pair's
+// segments + 9 for the share of pairs that end in it.  One sequence of 4096 tokens with
+// 32, 8 and 2 kv heads takes 13.5, 10.1 and 10.9 us in clusters, 16.3, 13.9 and
+// 17.9 in the list; of 32768 tokens 51.9, 29.2 and 29.6, and 50.0, 21.6 and 19.6.
+// Lengths are not known here: the list's time is taken as the least it can be with x
+// pairs as long as the table allows and the others empty, x from a sequence's kv
+// heads to all pairs, which is at x = CTAs sqrt(0.25 / nt).
 template <int D>
 int log_cluster_of(const PagedAttnParams &p, int dev) {
     static std::atomic<int> most[64][4];  // 1 + the clusters of 1 << i CTAs that fit the device
     if (dev >= 64) return -1;
     const long long pairs = (long long)p.B * p.Hkv, nt = (long long)p.max_pages + 1;
     const double ctas = p.num_ctas,
-                 x = std::min(std::max(ctas * std::sqrt(1.3 / (double)nt), (double)p.Hkv), (double)pairs);
-    const double list = 6.0 + x * (double)nt / ctas + 1.3 * ctas / x;
+                 x = std::min(std::max(ctas * std::sqrt(0.25 / (double)nt), (double)p.Hkv), (double)pairs);
+    const double list = 9.0 + x * (double)nt / ctas + 0.25 * ctas / x + 9.0 * (double)pairs / ctas;
     for (int i = 3; i >= 0; --i) {
         const int C = 1 << i;
         if (pairs * C > p.num_ctas) continue;
@@ -1341,11 +1459,15 @@ cudaError_t launch_d(PagedAttnParams &p, const CUtensorMap &tm_k, const CUtensor
     }
     e = cudaLaunchKernelEx(&cfg, paged_attn_kernel<D, false>, tm_k, tm_v, p);
     if (e != cudaSuccess) return e;
-    const long long rblocks = (p.rows_max + kMergeWarps - 1) / kMergeWarps;
-    cfg.gridDim = dim3((unsigned)((long long)p.B * p.Hkv * rblocks));
+    // With more than two rounds of segments to a pair (16 pairs: 17.0 us, 17.6 with a
+    // warp to a row; 32: 17.1 and 17.2; 128: 43.5 and 41.0)
+    const long long pairs = (long long)p.B * p.Hkv;
+    const bool many = pairs * 2 * kMergeLoads < p.num_ctas;
+    const long long rblocks = many ? p.rows_max : (p.rows_max + kMergeWarps - 1) / kMergeWarps;
+    cfg.gridDim = dim3((unsigned)(pairs * rblocks));
     cfg.blockDim = dim3(kMergeWarps * 32);
     cfg.dynamicSmemBytes = 0;
-    return cudaLaunchKernelEx(&cfg, paged_merge_kernel<D>, p);
+    return cudaLaunchKernelEx(&cfg, many ? paged_merge_many_kernel<D> : paged_merge_kernel<D>, p);
 }
 
 }  // namespace
