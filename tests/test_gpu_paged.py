@@ -489,3 +489,58 @@ def test_attention_of_pairs_shared_by_clusters(D, Hq, Hkv, Tm, P, T):
     out, lse = run_attention(*case, where="cluster")
     again, lse2 = run_attention(*case, where="cluster")
     assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+def widen(case, columns=600):
+    case = list(case)
+    wide = np.full((case[4].shape[0], columns), 10 ** 6, dtype=case[4].dtype)
+    wide[:, :case[4].shape[1]] = case[4]
+    case[4] = wide
+    return case
+
+
+@pytest.mark.parametrize("Hkv", [2, 40])                    # joined by two warps a row, by one
+def test_attention_nan_in_joined_segments(Hkv):
+    rng = np.random.default_rng(17)
+    c = list(attention_case(rng, 64, 2 * Hkv, Hkv, 3, [1500, 90], [3, 2]))
+    c[0] = c[0].copy()
+    c[0][c[4][0, 1], 1, 2, 7] = 0x7F                        # sequence 0, kv head 1
+    out, lse = run_attention_raw(*widen(c))
+    bad = np.zeros(out.shape[:3], bool)
+    bad[0, :3, 2:4] = True
+    assert np.isnan(out[bad]).all() and np.isfinite(out[~bad]).all()
+    bad_lse = bad.transpose(0, 2, 1)
+    assert np.isnan(lse[bad_lse]).all() and np.isfinite(lse[0][~bad_lse[0]]).all()
+    assert np.isfinite(lse[1, :, :2]).all() and np.isneginf(lse[1, :, 2]).all()
+
+
+def test_attention_bad_pages_in_a_wide_table():
+    rng = np.random.default_rng(10)
+    c = widen(attention_case(rng, 128, 4, 2, 4, [300, 200], [4, 4]))
+    c[4][0, 2], c[4][1, 0] = -1, 10 ** 9
+    run_attention(*c, status=4, masked={(0, 2), (1, 0)}, where="bad pages")
+
+
+@pytest.mark.parametrize("columns", [32, 600])
+def test_attention_lengths_of_equal_sums_between_calls(columns):
+    """Lengths that change while their sum stays, from call to call on one workspace."""
+    rng = np.random.default_rng(18)
+    c = widen(attention_case(rng, 128, 8, 4, 4, [1000, 1000], [4, 4], poison=False), columns)
+    c[4][c[4] == 10 ** 6] = -1
+    dev = lambda a, dt: torch.from_numpy(np.ascontiguousarray(a)).to(dt).cuda()[None, None]
+    cache = das.PagedKVCache(dev(c[0], torch.uint8), dev(c[2], torch.uint8), dev(c[1], torch.float32),
+                             dev(c[3], torch.float32))
+    ws = das.new_workspace_paged(cache, 2, 8, 4)
+    q, kb, vb = (bf16(x) for x in c[7:])
+    table, P, T = dev_i32(c[4]), dev_i32([500, 500]), dev_i32([4, 4])
+    steps = [[900, 100], [100, 900], [1000, 0], [0, 1000], [500, 500]]
+    new = [dev_i32(p) for p in steps]
+    torch.cuda.synchronize()
+    got = []
+    for p in new:                                           # no host wait in between
+        P.copy_(p)
+        got.append(das.das_mature_v_attention_paged(cache, 0, 1, 1, table, P, T, q, kb, vb, ws))
+    for p, (out, lse) in zip(steps, got):
+        o, l = ref.attention(c[0], np.float32(c[1]), c[2], np.float32(c[3]), c[4], p, [4, 4], f64(q), f64(kb), f64(vb))
+        assert_close(f64(out), o, lse.cpu().numpy(), l, where=f"lengths {p}")
+    assert das.workspace_status(ws) == 0
