@@ -19,7 +19,7 @@
 //
 // The row is read from memory once, which would take 2.4 us for 128 rows of
 // 32000 binary32 logits or 64 of 128257 in bf16 (16.4 MB).  Measured: 19.1 us
-// (top-k 200, top-p 0.95, min-p 0.02) and 36.5 us (top-p 0.9 alone): the time goes to the
+// (top-k 200, top-p 0.95, min-p 0.02) and 35.1 us (top-p 0.9 alone): the time goes to the
 // passes over the row in shared memory (the largest, the candidates or the
 // bins, the sums), which each thread makes over 32 to 128 logits with some
 // dozens of instructions each, and to eight or so barriers of the cluster.  The
@@ -175,7 +175,11 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
     if (tid == 0) {
         s.key_max = 0;
         s.key_min = kOne;
+        s.list_n = 0;
     }
+    if (BF16)
+        for (int i = tid; i < kValues / 4; i += kThreads)
+            reinterpret_cast<uint4 *>(s.hist)[i] = make_uint4(0, 0, 0, 0);
     sync();  // every CTA of the cluster has started
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -192,7 +196,21 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
     T = fminf(T, 3.4028234e38f);
     if (k <= 0 || k > a.vocab) k = a.vocab;
 
+    // Bins of 16-bit values in falling order: 2^8 > l >= 2^-8, then -2^-8 >= l > -2^8.
+    auto value_bin = [](float l) {
+        const uint32_t bits = __float_as_uint(l), size = ((bits & 0x7fffffffu) >> 16) - kValueBase;
+        return size < kValues / 2 ? kValues / 2 + (bits >> 31 ? size : ~size) : 0xffffffffu;
+    };
+    auto value_of = [](int bin) {
+        const uint32_t size = bin < kValues / 2 ? kValues / 2 - 1 - bin : bin - kValues / 2;
+        return __uint_as_float((size + kValueBase) << 16 | (bin < kValues / 2 ? 0u : 0x80000000u));
+    };
+
     // ---- the row: NaN as -inf, -0 as 0 ----
+    // With top-p alone the values' bins (of search, below) are counted as the row comes
+    // (64 rows of 128257: 35.1 us, 36.5 with a pass of its own); the logits between
+    // the two signs' bins are listed in s.cand.
+    bool counted = BF16 && k >= a.vocab && p < 1.f;
     // Groups of four lie as the vector loads do: the CTA's first token is number
     // `shift` of group 0, and index `base` + 4 g + i - shift is token i of group g.
     using Elem = std::conditional_t<BF16, uint16_t, float>;
@@ -235,6 +253,17 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
             f[i] = f[i] == f[i] ? f[i] + 0.f : -INFINITY;
             mine = fmaxf(mine, f[i]);
         }
+        if (counted)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t at = value_bin(f[i]);
+                if (at < kValues) {
+                    atomicAdd(s.hist + at, 1u);
+                } else if (fabsf(f[i]) < 1.f) {
+                    const uint32_t n = atomicAdd(&s.list_n, 1u);
+                    if (n < kCand) s.cand[n] = f[i];
+                }
+            }
         if (BF16)
             reinterpret_cast<uint2 *>(held)[g] =
                 make_uint2(__float_as_uint(f[0]) >> 16 | (__float_as_uint(f[1]) & 0xffff0000u),
@@ -320,6 +349,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
         }
         m = 0.f;
         low = -3.4028234e38f;
+        counted = false;
     }
 
     // (l - m) / T as binary32 division rounds it.  With r = 1 / T rounded, q =
@@ -493,16 +523,6 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
         }
     }
 
-    // Bins of 16-bit values in falling order: 2^8 > l >= 2^-8, then -2^-8 >= l > -2^8.
-    auto value_bin = [](float l) {
-        const uint32_t bits = __float_as_uint(l), size = ((bits & 0x7fffffffu) >> 16) - kValueBase;
-        return size < kValues / 2 ? kValues / 2 + (bits >> 31 ? size : ~size) : 0xffffffffu;
-    };
-    auto value_of = [](int bin) {
-        const uint32_t size = bin < kValues / 2 ? kValues / 2 - 1 - bin : bin - kValues / 2;
-        return __uint_as_float((size + kValueBase) << 16 | (bin < kValues / 2 ? 0u : 0x80000000u));
-    };
-
     // ---- the threshold of a sum over the logits from `from` up ----
     // Finds the largest t with the sum of f over logits > t below the target
     // (then s.above), leaves its key in s.cut and how many have it in s.equal;
@@ -518,23 +538,28 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
             // of how often they come, and the product with the value's weight is the bin's
             // sum.  The smaller ones, between the two signs' bins, are summed one by one.
             // One atomic a logit and no exponential, where the bins below take two and one,
-            // and no second pass for what is in the bin: 64 rows of 128257 take 38 us, 62 us
+            // and no second pass for what is in the bin: 64 rows of 128257 took 38 us, 62 us
             // with the bins below, which remain for rows with logits out of this range.
             const float lim = kWeights ? fmaxf(lo, m - (kNats + 0.5f) * T) : lo;
             if (!few && fabsf(m) < 256.f && (!kWeights || m - (kNats + 0.5f) * T > -256.f)) {
-                for (int i = tid; i < kValues / 4; i += kThreads)
-                    reinterpret_cast<uint4 *>(s.hist)[i] = make_uint4(0, 0, 0, 0);
-                __syncthreads();
                 u64 small = 0;
-                for (int g = tid; g < groups; g += kThreads) {
-                    float l[4];
-                    load4(g, l);
+                if (kWeights && counted && s.list_n <= kCand) {
+                    // (the bins below lim hold what has no weight)
+                    for (int i = tid; i < (int)s.list_n; i += kThreads) small += wide(weight(s.cand[i]));
+                } else {
+                    for (int i = tid; i < kValues / 4; i += kThreads)
+                        reinterpret_cast<uint4 *>(s.hist)[i] = make_uint4(0, 0, 0, 0);
+                    __syncthreads();
+                    for (int g = tid; g < groups; g += kThreads) {
+                        float l[4];
+                        load4(g, l);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t at = value_bin(l[i]);
-                        if (l[i] >= lim) {
-                            if (at < kValues) atomicAdd(s.hist + at, 1u);
-                            else if (fabsf(l[i]) < 1.f) small += kWeights ? wide(weight(l[i])) : 1;
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t at = value_bin(l[i]);
+                            if (l[i] >= lim) {
+                                if (at < kValues) atomicAdd(s.hist + at, 1u);
+                                else if (fabsf(l[i]) < 1.f) small += kWeights ? wide(weight(l[i])) : 1;
+                            }
                         }
                     }
                 }
