@@ -110,7 +110,7 @@ __device__ __forceinline__ Pair scan(Pair v, Pair &total, Pair (*sums)[NT / 32],
 
 // One CTA, a thread to a request.  FILL: it writes the table entries and the slots
 // too; otherwise slot_fill_kernel does, from new_len and slot_start.  Bound by
-// latency: 16 requests that grow by up to 17 tokens take 2.7 us, with the lengths,
+// latency: 16 requests that grow by up to 17 tokens take 3.0 us, with the lengths,
 // the stack's pages and the stores behind one another and a barrier for each sum.
 template <int NT, bool FILL>
 __global__ void __launch_bounds__(NT) page_assign_kernel(const PageAssignArgs a) {
@@ -207,7 +207,9 @@ __global__ void __launch_bounds__(NT) page_assign_kernel(const PageAssignArgs a)
 // of every new page whose first token is among them.  Request b grew by n =
 // slot_start[b + 1] - slot_start[b] to new_len[b] and took the pages past
 // those of new_len[b] - n; the pages taken before its own, and by all, are
-// summed up again by every CTA.
+// summed up again by every CTA.  Four slots a thread share their search and mostly
+// their page.  Bound by latency: 256 requests and 1.2 million slots take 10.8 us with
+// the kernel before, of which the slots' 4.9 MB would take 0.7.
 constexpr int kFillThreads = 256, kFillSlots = 4096, kFillBatch = 256;
 
 __global__ void __launch_bounds__(kFillThreads) slot_fill_kernel(const PageAssignArgs a) {
@@ -550,7 +552,7 @@ cudaError_t page_assign_launch(const PageAssignArgs &a, cudaStream_t stream) {
     // requests and 1.2 million of them; a second kernel, which costs 2 us or more where
     // there is little to write, brings that to 10.8 us.
     // The fewer warps, the shorter the barriers and sums: 16 requests and 272 slots take
-    // 2.6 us with 256 threads, 3.6 with 1024.  But the slots of a request are a
+    // 2.5 us with 256 threads, 3.6 with 1024.  But the slots of a request are a
     // warp's: 200 requests and 3400 slots take 8.8 and 5.9 us, and 1000 requests
     // whose slots the second kernel writes 18.9 and 16.7.
     const bool fill = a.max_slots <= kFillAlone;

@@ -25,17 +25,27 @@
 // 32 (r / 16) + r % 16 and its lo part 16 lanes on, in the same warp's reach.
 //
 // Work split: every (sequence, kv head) pair owns one tile for each of its
-// ceil(P / 64) pages plus one for the block's own keys; all pairs' tiles are
-// one list, and CTA c of a persistent grid (one per SM) takes the c-th of C
-// equal ranges, cut into segments at pair boundaries.  A segment that is a
-// whole pair writes the output, others a partial (O / l, lse), which
-// paged_merge_kernel joins.
+// ceil(P / 64) pages plus one for the block's own keys.  There are two ways:
+//   clusters  a cluster of 1 to 8 CTAs to a pair, a CTA to a share of its tiles;
+//             the partials (O / l, lse) go into the shared memory of the CTA that
+//             joins their row;
+//   the list  of all pairs' tiles, of which CTA c of a persistent grid (one per
+//             SM) takes the c-th of C equal ranges, cut into segments at pair
+//             boundaries; a segment that is a whole pair writes the output, others a
+//             partial, which paged_merge_kernel (or paged_merge_many_kernel) joins.
+// log_cluster_of says which, with both measured.
+//
+// What bounds it: 4 sequences of 32768 tokens, 32 / 8 heads of 128 and blocks of 16
+// take 52.5 us, 5.1 TB/s of codes (bare TMA reads of the same tiles: 48.8 us); a tile
+// of 16 KB takes a CTA 0.37 us, the pace of the softmax groups below.  One
+// sequence of 4096 tokens with 32 heads takes 13.5 us (blocks of 1) and 14.4 us (8),
+// of which the tiles take 6; the smallest calls 5.8 us.
 //
 // One CTA = two groups of four softmax warps, which take turns at the tiles
 // (one warp per sub-partition left its latencies bare), + one TMA warp + two
-// MMA warps + four warps that prepare each segment's queries (split) and block keys and values (bf16,
-// with rows past the block zero).  The block tile runs bf16 products: S with
-// M = 64 (the hi lanes), P V with P split into two bf16 parts.
+// MMA warps + four warps that prepare each segment's queries (split) and block
+// keys and values (bf16, with rows past the block zero).  The block tile runs
+// bf16 products: S with M = 64 (the hi lanes), P V with P split into two bf16 parts.
 // The kernel is launched as a programmatic dependent: barrier set-up, the
 // tensor-memory allocation, the plan (from lengths read before the dependency
 // wait, read again after it) and L2 prefetches of the first tiles and queries
@@ -1276,7 +1286,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const Pag
 // The same where pairs have many segments: a row by both warps of a CTA.  A warp's
 // four groups of eight lanes take every fourth segment, two at a time, with a
 // reference and sums of their own, so that sixteen segments of a row are on their
-// way at once.  2 kv heads, 32768 tokens in a table that no cluster is used for: 22 us, 43 with a warp
+// way at once.  2 kv heads of 32768 tokens, the whole call: 19.4 us, 43 with a warp
 // to a row and four at once.
 struct Part {  // sums under the reference M
     float M, L;
@@ -1378,11 +1388,12 @@ __global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_many_kernel(cons
 size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 
 // The logarithm of the CTAs to a pair where clusters are used, else -1.
-// Measured at 38 shapes, in tiles of 0.34 us: a cluster's CTA takes its own tiles and 23; in the
-// list a CTA takes an equal share of all tiles and 32 + 0.25 for each of a pair's
-// segments + 9 for the share of pairs that end in it.  One sequence of 4096 tokens with
-// 32, 8 and 2 kv heads takes 13.5, 10.1 and 10.9 us in clusters, 16.3, 13.9 and
-// 17.9 in the list; of 32768 tokens 51.9, 29.2 and 29.6, and 50.0, 21.6 and 19.6.
+// Measured at 38 shapes, in tiles of 0.34 us: a cluster's CTA takes its own tiles and
+// 23; in the list a CTA takes an equal share of all tiles and 32, 0.25 for each of a
+// pair's segments, and 9 for each pair that ends in its range.  One sequence of
+// 4096 tokens with 32, 8 and 2 kv heads takes 13.5, 10.1 and 10.9 us in clusters,
+// 16.3, 13.9 and 17.9 in the list; of 32768 tokens 51.9, 29.2 and 29.6, and 50.0,
+// 21.6 and 19.6.
 // Lengths are not known here: the list's time is taken as the least it can be with x
 // pairs as long as the table allows and the others empty, x from a sequence's kv
 // heads to all pairs, which is at x = CTAs sqrt(0.25 / nt).

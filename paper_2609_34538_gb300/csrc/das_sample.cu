@@ -84,8 +84,12 @@ __device__ __forceinline__ T block_reduce(T v, T *sums, F f) {
 constexpr int kThreads = 1024, kWarps = kThreads / 32;
 static_assert(kWarps == 32, "a warp scans the warps' sums");
 constexpr int kMaxRowCtas = 8;                 // a portable cluster
-constexpr int kSliceBytes = 131072;            // logits per CTA, as they come
-constexpr int kMaxSegs = kSliceBytes / 2 / 128;  // of one warp's 32 groups of four
+// Logits per CTA, as they come: what shared memory holds, and fewer than 2^16, so that
+// a bin's sums of 16-bit pieces stay below 2^32.
+template <bool BF16>
+constexpr int kSliceBytes = BF16 ? 131072 : 180224;
+constexpr int kMaxSegs = 512;  // of one warp's 32 groups of four
+static_assert(kSliceBytes<true> / 2 <= kMaxSegs * 128 && kSliceBytes<false> / 4 <= kMaxSegs * 128, "segments");
 constexpr int kBins = 2048;
 constexpr int kList = 256;
 constexpr int kValues = 4096;               // bins of 16-bit values, sixteen octaves of each sign
@@ -448,13 +452,14 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
     // Four bits of each group of a thread say which; their numbers, in eight bits of
     // a word per round of groups, are summed over the warp for four rounds at once.
     if (k < a.vocab && k <= kCand / 4) {
-        constexpr int kRounds = kSliceBytes / (BF16 ? 2 : 4) / 4 / kThreads;
-        static_assert(kRounds * 4 * kThreads * (BF16 ? 2 : 4) == kSliceBytes && kRounds % 8 == 0);
-        uint32_t hits[kRounds / 8], count[kRounds / 4];
+        constexpr int kRounds = kSliceBytes<BF16> / (BF16 ? 2 : 4) / 4 / kThreads;
+        static_assert(kRounds * 4 * kThreads * (BF16 ? 2 : 4) == kSliceBytes<BF16> && kRounds * kWarps <= kMaxSegs);
+        constexpr int kHits = (kRounds + 7) / 8, kCounts = (kRounds + 3) / 4;
+        uint32_t hits[kHits], count[kCounts];
 #pragma unroll
-        for (int i = 0; i < kRounds / 8; ++i) hits[i] = 0;
+        for (int i = 0; i < kHits; ++i) hits[i] = 0;
 #pragma unroll
-        for (int i = 0; i < kRounds / 4; ++i) count[i] = 0;
+        for (int i = 0; i < kCounts; ++i) count[i] = 0;
 #pragma unroll
         for (int it = 0; it < kRounds; ++it) {
             if (it * kThreads >= groups) continue;
@@ -465,9 +470,9 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
             hits[it / 8] |= in << (it % 8 * 4);
             count[it / 4] |= __popc(in) << (it % 4 * 8);
         }
-        uint32_t before[kRounds / 4];  // exclusive, over the warp
+        uint32_t before[kCounts];  // exclusive, over the warp
 #pragma unroll
-        for (int i = 0; i < kRounds / 4; ++i) {
+        for (int i = 0; i < kCounts; ++i) {
             uint32_t x = count[i];
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -477,7 +482,8 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
             before[i] = x - count[i];
             if (lane == 31)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s.seg[(4 * i + j) * kWarps + warp] = x >> (8 * j) & 0xffu;
+                for (int j = 0; j < 4; ++j)
+                    if (4 * i + j < kRounds) s.seg[(4 * i + j) * kWarps + warp] = x >> (8 * j) & 0xffu;
         }
         __syncthreads();
         u64 n_all;
@@ -1007,8 +1013,10 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
 }
 
 // ---- longer rows --------------------------------------------------------------------
-// Rows of more than kMaxRowCtas * kMaxSlice logits: one CTA per row, which reads
-// the row (from L2 at best) for every step.
+// Rows of more than kMaxRowCtas * kMaxSlice logits (360,416 in binary32, 524,256 in
+// bf16): one CTA per row, which reads the row (from L2 at best) for every step.
+// Kept simple, and slow: 5.1 ms for one row of 400,009 where a cluster takes 44 us
+// for 360,000.
 template <bool BF16>
 __global__ void __launch_bounds__(kLongThreads) long_row_kernel(const SampleArgs a) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -1246,7 +1254,7 @@ cudaError_t sample_launch_t(const SampleArgs &a, cudaStream_t stream) {
     const int sms = attn_grid_size(dev);
     if (sms <= 0) return cudaErrorInvalidDevice;
     // CTAs per row: enough to hold the row, and as many as fill the SMs
-    constexpr int kMaxSlice = kSliceBytes / (BF16 ? 2 : 4) - 4;  // (with the shift of a first group)
+    constexpr int kMaxSlice = kSliceBytes<BF16> / (BF16 ? 2 : 4) - 4;  // (with the shift of a first group)
     const int hold = (int)(((long long)a.vocab + kMaxSlice - 1) / kMaxSlice);
     if (hold > kMaxRowCtas)
         return launch_pdl(long_row_kernel<BF16>, dim3((unsigned)rows), dim3(kLongThreads), 1, 0,
@@ -1260,7 +1268,7 @@ cudaError_t sample_launch_t(const SampleArgs &a, cudaStream_t stream) {
     static std::atomic<bool> configured[64];  // the shared-memory opt-in, once per device
     if (dev >= 64 || !configured[dev].load(std::memory_order_acquire)) {
         e = cudaFuncSetAttribute(sample_kernel<BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 kSliceBytes);
+                                 kSliceBytes<BF16>);
         if (e != cudaSuccess) return e;
         if (dev < 64) configured[dev].store(true, std::memory_order_release);
     }

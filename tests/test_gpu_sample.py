@@ -266,3 +266,23 @@ def test_rows_of_16_bit_logits(V, kind, filters):
         x[1, :, ::3] = -torch.inf
     k, p, m = filters
     check(x.to(torch.bfloat16), np.random.default_rng(13).random((2, 1)), T, [k, k], [p, p], [m, m])
+
+
+@pytest.mark.parametrize("V,dtype", [(360416, torch.float32), (360417, torch.float32), (524256, torch.bfloat16),
+                                     (524257, torch.bfloat16), (400009, torch.float32)])
+def test_rows_at_the_end_of_what_a_cluster_holds(V, dtype):
+    g = torch.Generator(device="cuda").manual_seed(V)
+    logits = (3 * torch.randn((1, 1, V), generator=g, device="cuda")).to(dtype)
+    for k, p, m in ((0, 0.9, 0.0), (60, 0.95, 0.001), (0, 1.0, 0.0)):
+        check(logits, np.array([[0.37]]), [0.8], [k], [p], [m])
+
+
+def test_more_equal_logits_than_a_half_word_counts():
+    """Every weight 2^32, and weights whose low halves are all ones, in one bin of a CTA."""
+    V = 524256
+    for x in (torch.zeros((1, 1, V), device="cuda"), torch.full((1, 1, V), -2.0, device="cuda")):
+        x[0, 0, 7] = 0.0
+        for dtype in (torch.bfloat16, torch.float32):
+            y = x.to(dtype)[..., : V if dtype == torch.bfloat16 else 360416].contiguous()
+            for T, k, p in ((1.0, 0, 0.6), (1.0, 400000 if dtype == torch.bfloat16 else 300000, 0.99), (3e8, 0, 0.5)):
+                check(y, np.array([[0.77]]), [T], [k], [p], [0.0])
