@@ -33,7 +33,7 @@ cudaError_t launch_pdl(void (*kernel)(Params...), dim3 grid, dim3 block, cudaStr
 
 // ---- page assignment ----------------------------------------------------------
 constexpr int kAssignThreads = 1024, kAssignFew = 256;
-constexpr int kFillAlone = 8192;  // slots that one CTA writes along the way
+constexpr int kFillAlone = 4096;  // slots that one CTA writes along the way
 constexpr int kFillFew = 1024;    // and that kAssignFew threads do
 
 // What one request asks for.
@@ -203,23 +203,23 @@ __global__ void __launch_bounds__(NT) page_assign_kernel(const PageAssignArgs a)
 }
 
 // Table entries and slots of the requests that page_assign_kernel served:
-// CTA x writes slots [x kFillSlots, (x + 1) kFillSlots), and the table entry
+// CTA x writes slots [x per_cta, (x + 1) per_cta), and the table entry
 // of every new page whose first token is among them.  Request b grew by n =
 // slot_start[b + 1] - slot_start[b] to new_len[b] and took the pages past
 // those of new_len[b] - n; the pages taken before its own, and by all, are
 // summed up again by every CTA.  Four slots a thread share their search and mostly
-// their page.  Bound by latency: 256 requests and 1.2 million slots take 10.8 us with
+// their page.  Bound by latency: 256 requests and 1.2 million slots take 9.1 us with
 // the kernel before, of which the slots' 4.9 MB would take 0.7.
-constexpr int kFillThreads = 256, kFillSlots = 4096, kFillBatch = 256;
+constexpr int kFillThreads = 256, kFillBatch = 256;
 
-__global__ void __launch_bounds__(kFillThreads) slot_fill_kernel(const PageAssignArgs a) {
+__global__ void __launch_bounds__(kFillThreads) slot_fill_kernel(const PageAssignArgs a, int per_cta) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    __shared__ long long sums[32];
+    __shared__ long long sums[3 * kFillThreads / 32];
     __shared__ int s_start[kFillBatch + 1], s_old[kFillBatch], s_top[kFillBatch];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int i0 = blockIdx.x * kFillSlots, i1 = min(i0 + kFillSlots, a.max_slots);
-    const int end = a.slot_start[a.batch];
+    const int i0 = blockIdx.x * per_cta, i1 = min(i0 + per_cta, a.max_slots);  // (below 2^30 + 2048)
+    const int end = a.slot_start[a.batch], left = *a.new_free_count;
     const bool wide = (reinterpret_cast<uintptr_t>(a.slots) & 15) == 0;
     int flag = 0;
     auto pages = [](int n) { return (n + kPage - 1) / kPage; };
@@ -229,19 +229,19 @@ __global__ void __launch_bounds__(kFillThreads) slot_fill_kernel(const PageAssig
         return n > 0 ? pages(len) - pages(old) : 0;
     };
     if (i0 < end) {
-        int b0 = 0;  // the first request with a slot past i0
-        for (int hi = a.batch; b0 < hi;) {
-            const int mid = (b0 + hi) / 2;
-            if (a.slot_start[mid + 1] > i0) hi = mid;
-            else b0 = mid + 1;
-        }
+        // b0: the first request with a slot past i0, the number of those that end before
         long long before = 0, all = 0;
-        int old;
+        int b0 = 0, old;
         for (int b = tid; b < a.batch; b += kFillThreads) {
             const int n = taken(b, old);
+            const bool done = a.slot_start[b + 1] <= i0;
             all += n;
-            if (b < b0) before += n;
+            if (done) {
+                before += n;
+                ++b0;
+            }
         }
+        b0 = __reduce_add_sync(kFull, b0);
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) {
             before += __shfl_xor_sync(kFull, before, d);
@@ -249,18 +249,21 @@ __global__ void __launch_bounds__(kFillThreads) slot_fill_kernel(const PageAssig
         }
         if (lane == 0) {
             sums[warp] = before;
-            sums[warp + 16] = all;
+            sums[warp + 8] = all;
+            sums[warp + 16] = b0;
         }
         __syncthreads();
         before = all = 0;
+        b0 = 0;
 #pragma unroll
         for (int w = 0; w < kFillThreads / 32; ++w) {
             before += sums[w];
-            all += sums[w + 16];
+            all += sums[w + 8];
+            b0 += (int)sums[w + 16];
         }
         __syncthreads();
         // the stack's place of the next page taken
-        long long top = (long long)*a.new_free_count + all - 1 - before;
+        long long top = (long long)left + all - 1 - before;
         for (; b0 < a.batch; b0 += kFillBatch) {
             const int nb = min(kFillBatch, a.batch - b0);
             const int start = a.slot_start[b0], stop = a.slot_start[b0 + nb];
@@ -549,8 +552,9 @@ __global__ void __launch_bounds__(kAppendThreads) append_paged_kernel(const Appe
 
 cudaError_t page_assign_launch(const PageAssignArgs &a, cudaStream_t stream) {
     // One CTA writes a few thousand slots along the way, but took 182 us for 256
-    // requests and 1.2 million of them; a second kernel, which costs 2 us or more where
-    // there is little to write, brings that to 10.8 us.
+    // requests and 1.2 million of them; a second kernel brings that to 9.1 us, with
+    // little to write to 7 (one CTA: 6.3 us for 256 requests and 4352 slots, 8.1 for
+    // 400 and 6800, 10.3 for 600 and 7800).
     // The fewer warps, the shorter the barriers and sums: 16 requests and 272 slots take
     // 2.5 us with 256 threads, 3.6 with 1024.  But the slots of a request are a
     // warp's: 200 requests and 3400 slots take 8.8 and 5.9 us, and 1000 requests
@@ -562,8 +566,11 @@ cudaError_t page_assign_launch(const PageAssignArgs &a, cudaStream_t stream) {
                                     : page_assign_kernel<kAssignThreads, false>);
     const cudaError_t e = launch_pdl(kernel, dim3(1), dim3(few ? kAssignFew : kAssignThreads), stream, 0, a);
     if (fill || e != cudaSuccess) return e;
-    return launch_pdl(slot_fill_kernel, dim3((unsigned)((a.max_slots + kFillSlots - 1) / kFillSlots)),
-                      dim3(kFillThreads), stream, 0, a);
+    // More CTAs while they are few to an SM: 40,000 slots 7.9 us by 1024, 9.2 by 2048;
+    // 1.2 million 10.2 and 9.1.
+    const int per_cta = a.max_slots <= 500000 ? 1024 : 2048;
+    return launch_pdl(slot_fill_kernel, dim3((unsigned)((a.max_slots + per_cta - 1) / per_cta)),
+                      dim3(kFillThreads), stream, 0, a, per_cta);
 }
 
 cudaError_t append_paged_launch(const das_kv_cache_paged &c, const void *k_new, const void *v_new,
