@@ -19,11 +19,11 @@
 //
 // The row is read from memory once, which would take 2.4 us for 128 rows of
 // 32000 binary32 logits or 64 of 128257 in bf16 (16.4 MB).  Measured: 19.1 us
-// (top-k 200, top-p 0.95, min-p 0.02) and 35.1 us (top-p 0.9 alone): the time goes to the
+// (top-k 200, top-p 0.95, min-p 0.02) and 34.5 us (top-p 0.9 alone): the time goes to the
 // passes over the row in shared memory (the largest, the candidates or the
 // bins, the sums), which each thread makes over 32 to 128 logits with some
 // dozens of instructions each, and to eight or so barriers of the cluster.  The
-// smallest call, one row of 32000 in a cluster of eight, takes 15.6 us, all
+// smallest call, one row of 32000 in a cluster of eight, takes 15.1 us, all
 // latency: the launch, the row from memory, and those barriers in turn.
 // Sorting the row would take a pass over it for every few bits of the key.
 //
@@ -32,6 +32,7 @@
 // every CTA executes that wait.
 #include <algorithm>
 #include <atomic>
+#include <cstddef>
 #include <type_traits>
 
 #include <cooperative_groups.h>
@@ -95,6 +96,7 @@ constexpr int kList = 256;
 constexpr int kValues = 4096;               // bins of 16-bit values, sixteen octaves of each sign
 constexpr uint32_t kValueBase = 0x3b80u;    // bf16 bits of 2^-8
 constexpr int kCand = 2048;
+constexpr int kSmall = 2 * kMaxSegs;
 // exponents past the last bin have weights that round to 0: e^-23 < 2^-33
 constexpr float kNats = 23.f;
 constexpr uint32_t kOne = 0xffffffffu;  // stands for the weight 2^32
@@ -213,7 +215,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
     // ---- the row: NaN as -inf, -0 as 0 ----
     // With top-p alone the values' bins (of search, below) are counted as the row comes
     // (64 rows of 128257: 35.1 us, 36.5 with a pass of its own); the logits between
-    // the two signs' bins are listed in s.cand.
+    // the two signs' bins are listed in s.seg.
     bool counted = BF16 && k >= a.vocab && p < 1.f;
     // Groups of four lie as the vector loads do: the CTA's first token is number
     // `shift` of group 0, and index `base` + 4 g + i - shift is token i of group g.
@@ -265,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
                     atomicAdd(s.hist + at, 1u);
                 } else if (fabsf(f[i]) < 1.f) {
                     const uint32_t n = atomicAdd(&s.list_n, 1u);
-                    if (n < kCand) s.cand[n] = f[i];
+                    if (n < kSmall) reinterpret_cast<float *>(s.seg)[n] = f[i];
                 }
             }
         if (BF16)
@@ -529,6 +531,27 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
         }
     }
 
+    // Of the first `words` words of s.hist (one row, or two of kBins), the parts
+    // [r per_cta, (r + 1) per_cta) go to CTA r, to [rank][row][per_cta] with `stride`
+    // words a rank, and are there after the next barrier.  Stores are not waited
+    // for as reads of the other CTAs' bins would be: one row of 32000 takes 15.1 us,
+    // 15.8 with those.  Returns the place: the candidates', or the row's if the
+    // candidates are in use.
+    auto send_bins = [&](int words, int per_cta, int stride) -> const uint32_t * {
+        uint32_t *const place = few ? reinterpret_cast<uint32_t *>(held) : reinterpret_cast<uint32_t *>(s.cand);
+        if (C == 1) return s.hist;
+        if (4 * tid < words) {
+            const int row = stride > per_cta ? 4 * tid / kBins : 0, bin = 4 * tid - row * kBins;
+            const int r = bin / per_cta, off = bin - r * per_cta;
+            uint32_t *const there = cluster.map_shared_rank(place, r);
+            *reinterpret_cast<uint4 *>(there + rank * stride + row * per_cta + off) =
+                reinterpret_cast<const uint4 *>(s.hist)[tid];
+        }
+        return place;
+    };
+    static_assert(sizeof s.cand + sizeof s.cand_at >= sizeof s.hist && kValues == 2 * kBins &&
+                  2 * kBins == 4 * kThreads && offsetof(Shared, cand_at) == sizeof s.cand, "bins sent");
+
     // ---- the threshold of a sum over the logits from `from` up ----
     // Finds the largest t with the sum of f over logits > t below the target
     // (then s.above), leaves its key in s.cut and how many have it in s.equal;
@@ -549,9 +572,10 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
             const float lim = kWeights ? fmaxf(lo, m - (kNats + 0.5f) * T) : lo;
             if (!few && fabsf(m) < 256.f && (!kWeights || m - (kNats + 0.5f) * T > -256.f)) {
                 u64 small = 0;
-                if (kWeights && counted && s.list_n <= kCand) {
+                if (kWeights && counted && s.list_n <= kSmall) {
                     // (the bins below lim hold what has no weight)
-                    for (int i = tid; i < (int)s.list_n; i += kThreads) small += wide(weight(s.cand[i]));
+                    for (int i = tid; i < (int)s.list_n; i += kThreads)
+                        small += wide(weight(reinterpret_cast<const float *>(s.seg)[i]));
                 } else {
                     for (int i = tid; i < kValues / 4; i += kThreads)
                         reinterpret_cast<uint4 *>(s.hist)[i] = make_uint4(0, 0, 0, 0);
@@ -574,25 +598,20 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
                     scan(small, sum);
                     return sum;
                 }();
+                const int per_cta = kValues / C, per_thread = max(1, per_cta / kThreads);
+                const uint32_t *bins = send_bins(kValues, per_cta, per_cta);
                 const int ts = exchange(small_all, 0, 0);  // (and the bins are there)
                 small = 0;
                 for (int r = 0; r < C; ++r) small += s.xch[ts][0][r];
                 // as the linear bins below: 1 / C of the bins to a CTA, up to four a thread
-                const int per_cta = kValues / C, per_thread = max(1, per_cta / kThreads);
                 u64 v[4] = {0, 0, 0, 0}, own = 0;
                 uint32_t n[4] = {0, 0, 0, 0};
                 const int i0 = rank * per_cta + tid * per_thread;
                 if (tid * per_thread < per_cta) {
-                    uint32_t x[4][kMaxRowCtas];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int r = 0; r < kMaxRowCtas; ++r)
-                            x[i][r] = i < per_thread && r < C && i * C < 4 ? of(r)->hist[i0 + i] : 0u;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-#pragma unroll
-                        for (int r = 0; r < kMaxRowCtas; ++r) n[i] += x[i][r];
+                        if (i >= per_thread) break;
+                        for (int r = 0; r < C; ++r) n[i] += bins[r * per_cta + tid * per_thread + i];
                         if (n[i]) v[i] = kWeights ? n[i] * wide(weight(value_of(i0 + i))) : n[i];
                         own += v[i];
                     }
@@ -703,10 +722,12 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
                             add(s.hist + bin_of(l[i]), kWeights ? weight(l[i]) : 0u);
                 }
             }
-            sync();
             // The bins' sums over the cluster: each CTA takes 1 / C of the bins,
             // one or two a thread in order, and tells the others its total.
             const int per_cta = kBins / C, per_thread = max(1, per_cta / kThreads);
+            if (C > 1) __syncthreads();
+            const uint32_t *bins = send_bins(kWeights ? 2 * kBins : kBins, per_cta, 2 * per_cta);
+            sync();
             u64 v[2] = {0, 0};
             if (tid * per_thread < per_cta) {
                 const int i0 = rank * per_cta + tid * per_thread;
@@ -715,15 +736,11 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
                     const uint2 high = *reinterpret_cast<const uint2 *>(s.hist + kBins + i0);
                     v[0] = low.x + ((u64)high.x << 16);
                     v[1] = low.y + ((u64)high.y << 16);
-                } else {  // (C >= 2: one bin a thread) all CTAs' on their way at once
-                    uint32_t low[kMaxRowCtas], high[kMaxRowCtas];
-#pragma unroll
-                    for (int r = 0; r < kMaxRowCtas; ++r) {
-                        low[r] = r < C ? of(r)->hist[i0] : 0u;
-                        high[r] = r < C && kWeights ? of(r)->hist[kBins + i0] : 0u;
+                } else {  // (C >= 2: one bin a thread)
+                    for (int r = 0; r < C; ++r) {
+                        v[0] += bins[2 * r * per_cta + tid];
+                        if (kWeights) v[0] += (u64)bins[(2 * r + 1) * per_cta + tid] << 16;
                     }
-#pragma unroll
-                    for (int r = 0; r < kMaxRowCtas; ++r) v[0] += low[r] + ((u64)high[r] << 16);
                 }
             }
             u64 total;
@@ -1264,7 +1281,8 @@ cudaError_t sample_launch_t(const SampleArgs &a, cudaStream_t stream) {
         C *= 2;
     const int slice = ((a.vocab + C - 1) / C + 3) / 4 * 4;
     const dim3 grid((unsigned)(rows * C)), block(kThreads);
-    const size_t smem = (size_t)(slice + 4) * (BF16 ? 2 : 4);  // (a group more where rows begin within one)
+    size_t smem = (size_t)(slice + 4) * (BF16 ? 2 : 4);  // (a group more where rows begin within one)
+    if (C > 1) smem = std::max(smem, 2 * kBins * sizeof(uint32_t));  // (bins may be sent there)
     static std::atomic<bool> configured[64];  // the shared-memory opt-in, once per device
     if (dev >= 64 || !configured[dev].load(std::memory_order_acquire)) {
         e = cudaFuncSetAttribute(sample_kernel<BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
