@@ -116,6 +116,7 @@ struct PagedAttnParams {
     float scale_log2;
     int num_ctas;
     int log_cluster;                      // of the CTAs to a pair; -1: the list of all tiles
+    bool whole;                           // the list in ranges of whole pairs
 };
 size_t paged_workspace_bytes(int device, int batch, int kv_heads, int rows_max, int head_dim);
 // tm_k / tm_v map the slabs read, e4m3 [pages * Hkv][64][D], with a {D, 64, 1}

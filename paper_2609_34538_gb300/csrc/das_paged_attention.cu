@@ -33,7 +33,8 @@
 //             SM) takes the c-th of C equal ranges, cut into segments at pair
 //             boundaries; a segment that is a whole pair writes the output, others a
 //             partial, which paged_merge_kernel (or paged_merge_many_kernel) joins.
-// log_cluster_of says which, with both measured.
+//             Many short pairs are split into ranges of whole pairs instead.
+// log_cluster_of and launch_d say which, with both measured.
 //
 // What bounds it: 4 sequences of 32768 tokens, 32 / 8 heads of 128 and blocks of 16
 // take 52.5 us, 5.1 TB/s of codes (bare TMA reads of the same tiles: 48.8 us); a tile
@@ -214,6 +215,19 @@ __device__ int plan(const PagedAttnParams &p, const int *lens, Walk &w) {
         run_t += (long long)chunk * p.Hkv;
     }
     return (int)max(0ll, at[1] - at[0]);  // the host admits no more than 2^30 a CTA
+}
+
+// The same where every range is to be whole pairs, as many as another CTA's.
+__device__ int plan_whole(const PagedAttnParams &p, const int *lens, Walk &w) {
+    const long long pairs = (long long)p.B * p.Hkv;
+    const int first = (int)(blockIdx.x * pairs / p.num_ctas),
+              last = (int)((blockIdx.x + 1) * pairs / p.num_ctas);
+    w = {first / p.Hkv, first % p.Hkv, 0, 1, 0, 0, lens};
+    walk_load(p, w);
+    Walk v = w;
+    int n = 0;
+    for (int i = first; i < last; ++i, walk_pair(p, v)) n += v.nt;
+    return n;
 }
 
 // In clusters: the tiles of a pair that CTA `rank` of 1 << log_c takes, [lo, hi).  The block
@@ -479,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     Walk w0 = {0, 0, 0, 1, 0, 0, nullptr};
     int ntiles = 0;
     if (early) {
-        ntiles = CLUSTER ? plan_pair(p, len_sm, w0) : plan(p, len_sm, w0);
+        ntiles = CLUSTER ? plan_pair(p, len_sm, w0) : p.whole ? plan_whole(p, len_sm, w0) : plan(p, len_sm, w0);
         // Into L2 while the kernels before this one finish: the range's first pages
         // (if the table still says other pages after the wait, these were for
         // nothing), their scales, and the first queries.
@@ -524,7 +538,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     if (!kept) {
         const int *const lens = early ? len_sm : nullptr;
-        ntiles = CLUSTER ? plan_pair(p, lens, w0) : plan(p, lens, w0);
+        ntiles = CLUSTER ? plan_pair(p, lens, w0) : p.whole ? plan_whole(p, lens, w0) : plan(p, lens, w0);
     }
     if (blockIdx.x == 0 && warp == 0)
         for (int b = lane; b < p.B; b += 32)
@@ -1468,11 +1482,20 @@ cudaError_t launch_d(PagedAttnParams &p, const CUtensorMap &tm_k, const CUtensor
         cfg.gridDim = dim3((unsigned)(p.B * p.Hkv << p.log_cluster));
         return cudaLaunchKernelEx(&cfg, paged_attn_kernel<D, true>, tm_k, tm_v, p);
     }
+    // Many short pairs: ranges of whole pairs need no merge kernel, whose time grows with
+    // the pairs, and no segments of cut ones.  12 sequences of 91 tokens with 32 heads
+    // take 18.8 us, 24.4 in equal ranges, of 832 27.7 and 33.1; 200 sequences of 190
+    // tokens with 8 heads 61.4 and 89.5.  They cost what some CTAs' share of pairs is
+    // above the mean, and with one long sequence among empty ones nearly that CTA's whole
+    // share (11 of 10 tokens and one of 832: 30.6 and 29.9).
+    const long long pairs = (long long)p.B * p.Hkv, nt = p.max_pages + 1LL;
+    const long long each = (pairs + p.num_ctas - 1) / p.num_ctas;
+    p.whole = pairs > p.num_ctas && each * nt <= 26 + pairs / 24 &&
+              (each * p.num_ctas - pairs) * nt <= (8 + pairs / 40) * p.num_ctas;
     e = cudaLaunchKernelEx(&cfg, paged_attn_kernel<D, false>, tm_k, tm_v, p);
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || p.whole) return e;
     // With more than two rounds of segments to a pair (16 pairs: 17.0 us, 17.6 with a
     // warp to a row; 32: 17.1 and 17.2; 128: 43.5 and 41.0)
-    const long long pairs = (long long)p.B * p.Hkv;
     const bool many = pairs * 2 * kMergeLoads < p.num_ctas;
     const long long rblocks = many ? p.rows_max : (p.rows_max + kMergeWarps - 1) / kMergeWarps;
     cfg.gridDim = dim3((unsigned)(pairs * rblocks));

@@ -544,3 +544,41 @@ def test_attention_lengths_of_equal_sums_between_calls(columns):
         o, l = ref.attention(c[0], np.float32(c[1]), c[2], np.float32(c[3]), c[4], p, [4, 4], f64(q), f64(kb), f64(vb))
         assert_close(f64(out), o, lse.cpu().numpy(), l, where=f"lengths {p}")
     assert das.workspace_status(ws) == 0
+
+
+@pytest.mark.parametrize("D,Hq,Hkv,Tm,P,T", [
+    (128, 16, 8, 3, [(37 * b) % 449 for b in range(20)], [b % 4 for b in range(20)]),
+    (64, 8, 8, 2, [(29 * b) % 193 for b in range(40)], [1 + b % 2 for b in range(40)]),
+    (128, 40, 40, 1, [0, 64, 65, 1, 0, 200], [1, 0, 1, 1, 1, 1])])
+def test_attention_of_many_short_pairs(D, Hq, Hkv, Tm, P, T):
+    """More pairs than SMs, few tiles to each: ranges of whole pairs, the same result every time and,
+    to the rounding of a joined row, as with the equal ranges of a wide table."""
+    rng = np.random.default_rng(D + Hq)
+    case = attention_case(rng, D, Hq, Hkv, Tm, P, T)
+    out, lse = run_attention(*case, where="short pairs")
+    again, lse2 = run_attention(*case, where="short pairs")
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+    run_attention(*widen(case), where="short pairs, wide table")
+
+
+def test_attention_of_many_short_pairs_with_changing_lengths():
+    rng = np.random.default_rng(19)
+    B = 24
+    c = list(attention_case(rng, 64, 8, 8, 2, [256] * B, [2] * B, poison=False))
+    dev = lambda a, dt: torch.from_numpy(np.ascontiguousarray(a)).to(dt).cuda()[None, None]
+    cache = das.PagedKVCache(dev(c[0], torch.uint8), dev(c[2], torch.uint8), dev(c[1], torch.float32),
+                             dev(c[3], torch.float32))
+    ws = das.new_workspace_paged(cache, B, 8, 2)
+    q, kb, vb = (bf16(x) for x in c[7:])
+    table, P, T = dev_i32(c[4]), dev_i32([256] * B), dev_i32([2] * B)
+    steps = [[256] * B, [0] * B, [(b * 31) % 257 for b in range(B)], [256 - (b * 31) % 257 for b in range(B)]]
+    new = [dev_i32(p) for p in steps]
+    torch.cuda.synchronize()
+    got = []
+    for p in new:                                           # no host wait in between
+        P.copy_(p)
+        got.append(das.das_mature_v_attention_paged(cache, 0, 1, 1, table, P, T, q, kb, vb, ws))
+    for p, (out, lse) in zip(steps, got):
+        o, l = ref.attention(c[0], np.float32(c[1]), c[2], np.float32(c[3]), c[4], p, [2] * B, f64(q), f64(kb), f64(vb))
+        assert_close(f64(out), o, lse.cpu().numpy(), l, where="lengths")
+    assert das.workspace_status(ws) == 0
