@@ -77,9 +77,10 @@ class das_sampling(ctypes.Structure):
 
 
 def _load():
-    if not os.path.exists(LIB_PATH):
-        raise ImportError(f"{LIB_PATH} is not built: run `python -m paper_2609_34538_gb300.build` "
-                          "(needs nvcc with sm_103a support)")
+    for path in (LIB_PATH, os.path.join(_HERE, "_calls.so")):
+        if not os.path.exists(path):
+            raise ImportError(f"{path} is not built: run `python paper_2609_34538_gb300/build.py` "
+                              "(needs nvcc with sm_103a support, and g++)")
     lib = ctypes.CDLL(LIB_PATH)
     i, p, f, sz = ctypes.c_int, ctypes.c_void_p, ctypes.c_float, ctypes.c_size_t
     cp = ctypes.POINTER(das_kv_cache)

@@ -1,7 +1,7 @@
 """Build libdas.so (the CUDA library behind include/das.h) in place for sm_103a,
 and _calls.so (the Python binding's module in C++, against PyTorch's headers).
 
-    python -m paper_2609_34538_gb300.build
+    python paper_2609_34538_gb300/build.py
 
 Each .cu under csrc/ is compiled in parallel with nvcc, then linked into
 paper_2609_34538_gb300/libdas.so.  A rebuild happens only when a source or
@@ -34,7 +34,8 @@ def _sources():
 def _inputs():
     hdrs = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")]
     hdrs += [os.path.join(INCLUDE, f) for f in os.listdir(INCLUDE) if f.endswith(".h")]
-    return _sources() + hdrs + [CALLS_SRC, os.path.abspath(__file__)]
+    torch = os.path.join(_torch_dir(), "version.py")  # _calls.so is for the PyTorch it was built with
+    return _sources() + hdrs + [CALLS_SRC, torch, os.path.abspath(__file__)]
 
 
 def up_to_date():
