@@ -14,11 +14,11 @@
 // pair by pair, or binned again by its keys if it is more than kList.  16-bit
 // logits have a bin for each value.  The token is found from sums over
 // segments in index order.  The candidates of a small top-k, if they are no
-// more than a CTA's threads, are sorted instead (128 rows of 32000: 19.1 us, 22.6
-// with the thresholds above over the candidates).
+// more than a CTA's threads, are sorted instead (128 rows of 32000: 3.5 us less
+// than with the thresholds above over the candidates).
 //
 // The row is read from memory once, which would take 2.4 us for 128 rows of
-// 32000 binary32 logits or 64 of 128257 in bf16 (16.4 MB).  Measured: 19.1 us
+// 32000 binary32 logits or 64 of 128257 in bf16 (16.4 MB).  Measured: 17.1 us
 // (top-k 200, top-p 0.95, min-p 0.02) and 34.5 us (top-p 0.9 alone): the time goes to the
 // passes over the row in shared memory (the largest, the candidates or the
 // bins, the sums), which each thread makes over 32 to 128 logits with some
@@ -180,7 +180,6 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
 
     if (tid == 0) {
         s.key_max = 0;
-        s.key_min = kOne;
         s.list_n = 0;
     }
     if (BF16)
@@ -307,28 +306,36 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
     };
 
     // ---- the largest logit m, and a logit that at least k are not below ----
-    // (the least over the cluster's warps of the ceil(k / warps)-th largest of
-    // the threads' largest)
+    // Of k' = ceil(k / C) logits, in each CTA: where j n >= k', the j-th largest of the
+    // warps' n-th largest of the threads' largest (the least such over the cluster).
+    // n = ceil(k' / warps) + 1 leaves some 350 candidates of 32000 for k = 200, which
+    // are sorted as 512; with n one less and the least of all warps they were 450 on
+    // average and more than 512 in every third row (128 rows of 32000: 19.2 us, 17.1 now).
     float m, low = -INFINITY;
     {
-        const uint32_t key = key_of(mine), top = __reduce_max_sync(kFull, key);
-        uint32_t nth = kKeyNone;
-        if (k < a.vocab) {
-            const long long n = (k + C * kWarps - 1) / (C * kWarps);
-            int above = 0;
+        auto sorted32 = [&](uint32_t x) {  // a warp's keys, the largest in lane 0
 #pragma unroll
-            for (int d = 1; d < 32; ++d) {
-                const uint32_t o = __shfl_xor_sync(kFull, key, d);
-                above += o > key || (o == key && (lane ^ d) < lane);
-            }
-            nth = n <= 32 ? __reduce_max_sync(kFull, above == n - 1 ? key : 0u) : kKeyNone;
+            for (int size = 2; size <= 32; size *= 2)
+#pragma unroll
+                for (int d = size / 2; d > 0; d /= 2) {
+                    const uint32_t o = __shfl_xor_sync(kFull, x, d);
+                    x = !(lane & size) == !(lane & d) ? max(x, o) : min(x, o);
+                }
+            return x;
+        };
+        const uint32_t key = key_of(mine), top = __reduce_max_sync(kFull, key);
+        const long long kc = (k + C - 1) / C, n = min((kc + kWarps - 1) / kWarps + 1, 32ll);
+        const bool bound = k < a.vocab && kc <= n * kWarps;
+        if (bound) {
+            const uint32_t nth = __shfl_sync(kFull, sorted32(key), (int)n - 1);
+            if (lane == 0) s.list[warp] = nth;
         }
-        if (lane == 0) {
-            atomicMax(&s.key_max, top);
-            atomicMin(&s.key_min, nth);
-        }
+        if (lane == 0) atomicMax(&s.key_max, top);
         __syncthreads();
-        const int t = exchange(s.key_max, s.key_min, 0);
+        uint32_t here = kKeyNone;
+        if (bound && warp == 0)
+            here = __shfl_sync(kFull, sorted32(s.list[lane]), (int)((kc + n - 1) / n) - 1);
+        const int t = exchange(s.key_max, here, 0);  // (by warp 0)
         uint32_t most = 0, least = kOne;
         for (int r = 0; r < C; ++r) {
             most = max(most, (uint32_t)s.xch[t][0][r]);
@@ -391,20 +398,22 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
         if (tid < n) x = (u64)key_of(s.cand[tid]) << 32 | (uint32_t)(kThreads - 1 - tid);
         u64 *const there = reinterpret_cast<u64 *>(s.hist);  // [2][kThreads]
         static_assert(sizeof s.hist >= 2 * kThreads * sizeof(u64));
-        int set = 0;
-        for (int size = 2; size < 2 * n; size *= 2)  // a bitonic sort
-            for (int d = size / 2; d > 0; d /= 2) {
-                u64 y;
-                if (d >= 32) {
-                    there[set + tid] = x;
-                    __syncthreads();
-                    y = there[set + (tid ^ d)];
-                    set ^= kThreads;
-                } else {
-                    y = __shfl_xor_sync(kFull, x, d);
+        int set = 0, span = 32;  // a bitonic sort, by the warps that it takes
+        while (span < n) span *= 2;
+        if (tid < span)
+            for (int size = 2; size <= span; size *= 2)
+                for (int d = size / 2; d > 0; d /= 2) {
+                    u64 y;
+                    if (d >= 32) {
+                        there[set + tid] = x;
+                        asm volatile("bar.sync 1, %0;" ::"r"(span) : "memory");
+                        y = there[set + (tid ^ d)];
+                        set ^= kThreads;
+                    } else {
+                        y = __shfl_xor_sync(kFull, x, d);
+                    }
+                    if ((x < y) == (!(tid & size) == !(tid & d))) x = y;
                 }
-                if ((x < y) == (!(tid & size) == !(tid & d))) x = y;
-            }
         const bool mine_in = tid < n && tid < k;
         const int at = kThreads - 1 - (int)(uint32_t)x;  // its place in s.cand
         float e[4] = {};
