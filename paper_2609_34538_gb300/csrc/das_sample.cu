@@ -536,7 +536,9 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
             few = true;
             groups = ((int)n_all + 3) / 4;
             if (tid < 4 * groups - (int)n_all) s.cand[n_all + tid] = -INFINITY;
-            __syncthreads();
+            // of the cluster: from here on other CTAs store their bins over the row, which
+            // every CTA has to have taken its candidates out of
+            sync();
         }
     }
 

@@ -286,3 +286,33 @@ def test_more_equal_logits_than_a_half_word_counts():
             y = x.to(dtype)[..., : V if dtype == torch.bfloat16 else 360416].contiguous()
             for T, k, p in ((1.0, 0, 0.6), (1.0, 400000 if dtype == torch.bfloat16 else 300000, 0.99), (3e8, 0, 0.5)):
                 check(y, np.array([[0.77]]), [T], [k], [p], [0.0])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,C", [(1, 8), (19, 8), (25, 4), (40, 2)])
+@pytest.mark.parametrize("k,p,values", [(512, 0.9, "distinct"), (450, 1.0, "ties"), (500, 0.7, "ties"), (512, 1.0, "distinct")])
+def test_many_candidates_of_a_small_top_k(B, C, dtype, k, p, values):
+    """Rows of C CTAs whose candidates are too many to be sorted: all tokens but 1025 to 2048 C are
+    masked, most of the rest stand at the start of the slices, unevenly.  The same result every time."""
+    g = torch.Generator(device="cuda").manual_seed(k + C)
+    V = 40003 if dtype == torch.bfloat16 else 33001
+    slice_ = (-(-V // C) + 3) // 4 * 4
+    logits = torch.full((B, 1, V), -torch.inf, device="cuda")
+    for r in range(C):
+        n = min(1500 if r % 4 == 0 else 90 + 400 * (r % 3), slice_ // 2, V - r * slice_)
+        x = 2 * torch.randn((B, n), generator=g, device="cuda")
+        if values == "ties":             # the k-th largest is one of many equal ones
+            x = x.round().clamp(max=1.0)
+            x[:, ::17] += 3
+        logits[:, 0, r * slice_: r * slice_ + n] = x
+    logits[:, 0, V - 3:] = 0.5
+    logits = logits.to(dtype)
+    u = np.random.default_rng(k).random((B, 1))
+    par = dict(temperature=f32([0.8] * B), top_k=dev_i32([k] * B), top_p=f32([p] * B))
+    runs = [das.das_sample(logits, f32(u), **par) for _ in range(40)]
+    for ids, logp in runs[1:]:
+        assert torch.equal(ids, runs[0][0]) and torch.equal(logp, runs[0][1])
+    some = sorted({0, B // 2, B - 1})
+    n = len(some)
+    ids, logp = check(logits[some].contiguous(), u[some], [0.8] * n, [k] * n, [p] * n, [0.0] * n)
+    assert torch.equal(ids, runs[0][0][some]) and torch.equal(logp, runs[0][1][some])
