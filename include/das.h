@@ -409,11 +409,11 @@ size_t das_workspace_size_paged(const das_kv_cache_paged *cache, int batch, int 
  * All other arguments, results and limits as das_mature_v_attention.  Bit 2
  * of the workspace's status word is set where a table entry is no page of the
  * cache; its 64 tokens are then taken as masked.
- * The products run on the codes: a query row and the softmax weights are each
- * split into two e4m3 parts, the queries exactly for elements down to about
- * 2^-13 of the row's largest (queries must be finite), a weight to 2^-9 of
- * itself or 2^-17 of the row's largest weight times value scale; scores, sums
- * and outputs are accumulated in fp32.  The value scales that one sequence
+ * The products run on the codes: a query row is split into two e4m3 parts,
+ * exactly for elements down to about 2^-13 of the row's largest (queries must
+ * be finite), a softmax weight into three e5m2 parts, to 2^-9 of itself (as a
+ * bf16 weight is) or 2^-30 of the row's largest weight times value scale;
+ * scores, sums and outputs are accumulated in fp32.  The value scales that one sequence
  * reads are to be within a factor of 2^100 of each other and of 1 (a scale of 0
  * counts as 2^-60).
  */

@@ -9,18 +9,23 @@
 // lse = ln 2 (m - kHead + log2 l): a page's value scale is part of the weight
 // that its codes are multiplied with, so the products run on the codes alone.
 // m moves (O and l are rescaled) only when a thread's weights of a tile sum to
-// more than kMost = 256 and the tile's largest x exceeds m by more than kWindow,
-// so that no weight is above 256 and all fit e4m3.
+// more than kMost = 2^13 and the tile's largest x exceeds m by more than kWindow,
+// so that no weight is above 2^13 and all parts of one fit their types.
 //
-// Both operands of an e4m3 product have 4 significant bits, which is too few
-// for queries and weights, so each is split into two rows of one M = 128
-// product (no second pass over the keys):
-//   queries  2^e q = hi + lo / 16, exact for elements down to about 2^-13 of
-//            the row's largest (a bf16 value has 8 significant bits); S = S_hi
-//            + S_lo / 16, added where the scores are read;
-//   weights  p = hi + lo / 32, off by at most 2^-9 of p (bf16 weights: 2^-8)
-//            or 2^-15, where the reference's weight is 2^kHead; O = O_hi +
-//            O_lo / 32, added at the end of a segment.
+// The operands of an 8-bit product have 3 or 4 significant bits, which is too few
+// for queries and weights, so each is split into parts:
+//   queries  2^e q = hi + lo / 16, both e4m3, two rows of one M = 128 product,
+//            exact for elements down to about 2^-13 of the row's largest (a
+//            bf16 value has 8 significant bits); S = S_hi + S_lo / 16, added
+//            where the scores are read;
+//   weights  p = a + b + c / 256, all e5m2 (which A may be beside an e4m3 B): a
+//            and c two rows of one product, b a second product into a's rows;
+//            O = O_hi + O_lo / 256, added at the end of a segment.  Off by 2^-9
+//            of p, as bf16 weights are, or by 2^-24, where the reference's
+//            weight is 2^kHead = 2^7: what one dominant key leaves to thousands of
+//            others is kept.  Two e4m3 parts, whose range ends 2^-17 below the reference,
+//            lost most of that; they took 53.0 us where three take 56.2 (4 x 32768
+//            tokens), and values widened to f16 in shared memory 60.7.
 // Row r of the pair (r = i * G + g) has its hi part in TMEM lane
 // 32 (r / 16) + r % 16 and its lo part 16 lanes on, in the same warp's reach.
 //
@@ -37,10 +42,10 @@
 // log_cluster_of and launch_d say which, with both measured.
 //
 // What bounds it: 4 sequences of 32768 tokens, 32 / 8 heads of 128 and blocks of 16
-// take 52.5 us, 5.1 TB/s of codes (bare TMA reads of the same tiles: 48.8 us); a tile
-// of 16 KB takes a CTA 0.37 us, the pace of the softmax groups below.  One
-// sequence of 4096 tokens with 32 heads takes 13.5 us (blocks of 1) and 14.4 us (8),
-// of which the tiles take 6; the smallest calls 5.8 us.
+// take 56.2 us, 4.8 TB/s of codes (bare TMA reads of the same tiles: 48.8 us); a tile
+// of 16 KB takes a CTA 0.39 us, the pace of the softmax groups below.  One
+// sequence of 4096 tokens with 32 heads takes 14.1 us (blocks of 1) and 14.6 us (8),
+// of which the tiles take 6 to 7; the smallest calls 5.9 us.
 //
 // One CTA = two groups of four softmax warps, which take turns at the tiles
 // (one warp per sub-partition left its latencies bare), + one TMA warp + two
@@ -79,15 +84,37 @@ constexpr int kQueryWarps = 4;
 constexpr int kThreads = (kQueryWarp0 + kQueryWarps) * 32;
 constexpr int kRows = 64;          // query rows per pair
 constexpr int kSBufs = 3;          // S buffers in tensor memory
-constexpr int kTmemCols = 512;     // S [0, 192), each group's O, each group's P (16 columns)
+constexpr int kTmemCols = 512;     // S [0, 192), each group's O, each group's P (2 x 16 columns)
 constexpr int kOCol = kSBufs * kTileKeys;
 constexpr int kOStep = 128;
 constexpr int kPCol = kOCol + kGroups * kOStep;
-constexpr float kHead = 2.f, kWindow = 3.f, kMost = 256.f;  // 2^(kHead + kWindow) <= kMost
-constexpr float kQLoInv = 1.f / 16.f, kPLoInv = 1.f / 32.f;
-constexpr uint32_t kPlusLo = 0x50005000u, kMinusLo = 0xd000d000u;  // f16x2 of 32, -32
+constexpr int kPStep = 32;
+static_assert(kPCol + kGroups * kPStep == kTmemCols, "tensor memory");
+constexpr float kHead = 7.f, kWindow = 6.f, kMost = 8192.f;  // 2^(kHead + kWindow) <= kMost
+constexpr float kQLoInv = 1.f / 16.f, kPLo = 256.f, kPLoInv = 1.f / kPLo;
+constexpr uint32_t kPLo2 = 0x5c005c00u;   // f16x2 of kPLo
 constexpr uint32_t kLoLanes = 16u << 16;
 constexpr int kPrefetch = 4;       // pages pulled into L2 before the dependency wait
+
+// Four weights, f16 pairs x and y (0 to kMost), as three e5m2 parts each: p = a + b +
+// c / kPLo, off by at most 2^-9 of p (each part leaves 2^-3 of what it rounds) or
+// 2^-25: e5m2 reaches as far down as f16 nearly, and c, kPLo times what remains
+// (2^7 at most), down to all of it.  The differences are exact.
+struct Parts {
+    uint32_t a, b, c;
+};
+__device__ __forceinline__ Parts parts_of(uint32_t x, uint32_t y) {
+    Parts r;
+    uint32_t u, v;
+    r.a = e5m2x4_f16(x, y);
+    f16_e5m2x4(r.a, u, v);
+    x = hsub2(x, u);
+    y = hsub2(y, v);
+    r.b = e5m2x4_f16(x, y);
+    f16_e5m2x4(r.b, u, v);
+    r.c = e5m2x4_f16(hmul2(hsub2(x, u), kPLo2), hmul2(hsub2(y, v), kPLo2));
+    return r;
+}
 
 // ---- tile list --------------------------------------------------------------------
 __device__ __forceinline__ int clamp_to(int v, int hi) { return v < 0 ? 0 : (v > hi ? hi : v); }
@@ -125,8 +152,8 @@ __device__ __forceinline__ void walk_pair(const PagedAttnParams &p, Walk &w) {
 // Tile x of pair n has weighted position x + beta n; CTA c takes the tiles at
 // [c W / C, (c + 1) W / C).  The end of a pair (its block tile, the joining of
 // the groups, the next pair's start) costs a CTA about as much as nine pages, so
-// a range that holds one takes beta tiles fewer (weights 3, 5, 7, 9, 12: 54.6,
-// 53.7, 53.5, 52.8, 52.9 us for 4 x 32768 tokens, 44.0, 43.2, 43.4, 41.2, 41.1
+// a range that holds one takes beta tiles fewer (weights 3, 5, 7, 9, 12: 57.7,
+// 57.0, 56.5, 56.2, 56.5 us for 4 x 32768 tokens, 49.6, 45.7, 46.3, 45.5, 45.1
 // for 16 ragged sequences); beta = 0 with more pairs than CTAs (nearly every
 // range then holds one) or where a CTA could stay empty.
 constexpr int kBlockWeight = 9;
@@ -706,7 +733,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
     } else if (warp == kPvWarp) {
         // ================================ O += P V ===============================
-        const uint32_t id8 = idesc_e4m3(2 * kRows, D, 0, 1);
+        const uint32_t id8 = idesc_e5m2_e4m3(2 * kRows, D, 0, 1);
         const uint32_t idb = idesc_bf16(2 * kRows, D, 0, 1);
         const uint64_t dv8 = sdesc(sbase + Lt::kTile, 8 * D, 8 * D, Lt::kSwizzle);
         Walk w = w0;
@@ -723,11 +750,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                 fence_after();
                 if (elect_one()) {
                     const uint32_t dO = tmem + kOCol + (uint32_t)((k & 1) * kOStep);
-                    const uint32_t a0 = tmem + kPCol + (uint32_t)((k & 1) * 16);
+                    const uint32_t a0 = tmem + kPCol + (uint32_t)((k & 1) * kPStep);
                     const uint64_t b0 = dv8 + (uint64_t)((st.i * Lt::kStage) >> 4);
                     // (the group's first tile of the segment begins its O)
-                    mma_e4m3_ta(dO, a0, b0, id8, k - k_seg >= kGroups);
-                    mma_e4m3_ta(dO, a0 + 8, b0 + (uint64_t)((32 * D) >> 4), id8, 1);
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk)  // parts a and c, then b, each of 2 x 32 keys
+                        mma_f8_ta(dO, a0 + 8 * kk, b0 + (uint64_t)(((kk & 1) * 32 * D) >> 4), id8,
+                                  k - k_seg >= kGroups || kk > 0);
                     mma_commit(b_empty + 8 * st.i);
                     mma_commit(b_pvdone + 8 * (k & 1));
                 }
@@ -788,6 +817,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
         const uint32_t o_col = lanes + kOCol + (uint32_t)(group * kOStep);
         float2 *ml = reinterpret_cast<float2 *>(sm + Lt::kMlOff);
+        const uint32_t p_col = lanes + kPCol + (uint32_t)(group * kPStep);
+        {  // beside b there is no fourth part
+            const uint32_t zero[8] = {};
+            st_half(p_col + kPStep / 2 + kLoLanes, zero);
+        }
         Walk w = w0;
         float m_ref = -INFINITY, l_sum = 0.f, row_scale = 1.f;
         int k = 0, kp = 0;  // the next tile, and the pages before it
@@ -917,22 +951,19 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (key0 + j >= lim) v[j] = -INFINITY;
                 }
                 const float sum = weights_of(v, e, scale, ti.lv, n < kTileKeys || !ok_s);
-                uint32_t hi[8], lo[8];
+                uint32_t pa[8], pb[8], pc[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    // 32 (x - hi), exact
-                    const uint32_t x = pack_f16(e[4 * j], e[4 * j + 1]);
-                    const uint32_t y = pack_f16(e[4 * j + 2], e[4 * j + 3]);
-                    hi[j] = e4m3x4_f16(x, y);
-                    uint32_t hx, hy;
-                    f16_e4m3x4(hi[j], hx, hy);
-                    lo[j] = e4m3x4_f16(hfma2(hx, kMinusLo, hmul2(x, kPlusLo)),
-                                       hfma2(hy, kMinusLo, hmul2(y, kPlusLo)));
+                    const Parts r = parts_of(pack_f16(e[4 * j], e[4 * j + 1]),
+                                             pack_f16(e[4 * j + 2], e[4 * j + 3]));
+                    pa[j] = r.a;
+                    pb[j] = r.b;
+                    pc[j] = r.c;
                 }
                 if (!pv_early) wait_pv();
-                const uint32_t pa = lanes + kPCol + (uint32_t)(group * 16);
-                st_half(pa, hi);
-                st_half(pa + kLoLanes, lo);
+                st_half(p_col, pa);
+                st_half(p_col + kLoLanes, pc);
+                st_half(p_col + kPStep / 2, pb);
                 // keys past the page's last token may hold anything: zero their value rows
                 if (n < kTileKeys) {
                     const uint32_t vt = sbase + s * Lt::kStage + Lt::kTile + n * D;
@@ -971,8 +1002,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int i = 0; i < 4; ++i) {
                         const float x = e[8 * c + 2 * i], y = e[8 * c + 2 * i + 1];
                         h[i] = pack_bf16(x, y);
-                        l[i] = pack_bf16((x - __uint_as_float(h[i] << 16)) * 32.f,
-                                         (y - __uint_as_float(h[i] & 0xffff0000u)) * 32.f);
+                        l[i] = pack_bf16((x - __uint_as_float(h[i] << 16)) * kPLo,
+                                         (y - __uint_as_float(h[i] & 0xffff0000u)) * kPLo);
                     }
                     st_shared(pb + chunk16(m, key0 / 8 + c), h[0], h[1], h[2], h[3]);
                     st_shared(pb + chunk16(m + 16, key0 / 8 + c), l[0], l[1], l[2], l[3]);
@@ -1300,7 +1331,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const Pag
 // The same where pairs have many segments: a row by both warps of a CTA.  A warp's
 // four groups of eight lanes take every fourth segment, two at a time, with a
 // reference and sums of their own, so that sixteen segments of a row are on their
-// way at once.  2 kv heads of 32768 tokens, the whole call: 19.4 us, 43 with a warp
+// way at once.  2 kv heads of 32768 tokens, the whole call: 16.1 us, 24.1 with a warp
 // to a row and four at once.
 struct Part {  // sums under the reference M
     float M, L;
@@ -1405,9 +1436,9 @@ size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 // Measured at 38 shapes, in tiles of 0.34 us: a cluster's CTA takes its own tiles and
 // 23; in the list a CTA takes an equal share of all tiles and 32, 0.25 for each of a
 // pair's segments, and 9 for each pair that ends in its range.  One sequence of
-// 4096 tokens with 32, 8 and 2 kv heads takes 13.5, 10.1 and 10.9 us in clusters,
-// 16.3, 13.9 and 17.9 in the list; of 32768 tokens 51.9, 29.2 and 29.6, and 50.0,
-// 21.6 and 19.6.
+// 4096 tokens with 32, 8 and 2 kv heads takes 14.1, 10.1 and 9.5 us in clusters,
+// 17.5, 12.4 and 15.0 in the list; of 32768 tokens 58.5, 32.3 and 31.5, and 54.3,
+// 22.7 and 16.3.
 // Lengths are not known here: the list's time is taken as the least it can be with x
 // pairs as long as the table allows and the others empty, x from a sequence's kv
 // heads to all pairs, which is at x = CTAs sqrt(0.25 / nt).
@@ -1484,18 +1515,18 @@ cudaError_t launch_d(PagedAttnParams &p, const CUtensorMap &tm_k, const CUtensor
     }
     // Many short pairs: ranges of whole pairs need no merge kernel, whose time grows with
     // the pairs, and no segments of cut ones.  12 sequences of 91 tokens with 32 heads
-    // take 18.8 us, 24.4 in equal ranges, of 832 27.7 and 33.1; 200 sequences of 190
-    // tokens with 8 heads 61.4 and 89.5.  They cost what some CTAs' share of pairs is
+    // take 19.0 us, 24.5 in equal ranges, of 832 30.2 and 35.2; 200 sequences of 190
+    // tokens with 8 heads 64.5 and 91.8.  They cost what some CTAs' share of pairs is
     // above the mean, and with one long sequence among empty ones nearly that CTA's whole
-    // share (11 of 10 tokens and one of 832: 30.6 and 29.9).
+    // share (11 of 10 tokens and one of 832: 31.9 and 30.5).
     const long long pairs = (long long)p.B * p.Hkv, nt = p.max_pages + 1LL;
     const long long each = (pairs + p.num_ctas - 1) / p.num_ctas;
     p.whole = pairs > p.num_ctas && each * nt <= 26 + pairs / 24 &&
               (each * p.num_ctas - pairs) * nt <= (8 + pairs / 40) * p.num_ctas;
     e = cudaLaunchKernelEx(&cfg, paged_attn_kernel<D, false>, tm_k, tm_v, p);
     if (e != cudaSuccess || p.whole) return e;
-    // With more than two rounds of segments to a pair (16 pairs: 17.0 us, 17.6 with a
-    // warp to a row; 32: 17.1 and 17.2; 128: 43.5 and 41.0)
+    // With more than two rounds of segments to a pair (16 pairs: 19.3 us, 20.7 with a
+    // warp to a row; 32: 17.4 and 17.4; 128: 54.8 and 42.8)
     const bool many = pairs * 2 * kMergeLoads < p.num_ctas;
     const long long rblocks = many ? p.rows_max : (p.rows_max + kMergeWarps - 1) / kMergeWarps;
     cfg.gridDim = dim3((unsigned)(pairs * rblocks));

@@ -102,7 +102,7 @@ __device__ __forceinline__ uint64_t sdesc(uint32_t addr, uint32_t lbo, uint32_t 
            (uint64_t)((sbo >> 4) & 0x3FFF) << 32 | (uint64_t)1 << 46 | (uint64_t)layout << 61;
 }
 // Instruction descriptors, fp32 D: kind::f16 with bf16 A and B, kind::f8f6f4
-// with e4m3 A and B.
+// with e4m3 B and e4m3 or e5m2 A.
 __host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, int a_mn_major, int b_mn_major) {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn_major << 15) |
            ((uint32_t)b_mn_major << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
@@ -110,6 +110,9 @@ __host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, int a_mn_major, 
 __host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N, int a_mn_major, int b_mn_major) {
     return (1u << 4) | ((uint32_t)a_mn_major << 15) | ((uint32_t)b_mn_major << 16) |
            ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+__host__ __device__ constexpr uint32_t idesc_e5m2_e4m3(int M, int N, int a_mn_major, int b_mn_major) {
+    return idesc_e4m3(M, N, a_mn_major, b_mn_major) | (1u << 7);
 }
 __device__ __forceinline__ void mma_bf16(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t id,
                                          uint32_t accumulate) {
@@ -127,9 +130,9 @@ __device__ __forceinline__ void mma_e4m3(uint32_t d_tmem, uint64_t a, uint64_t b
         "l"(a), "l"(b), "r"(id), "r"(accumulate)
         : "memory");
 }
-// A from tensor memory (lane m = row m, four e4m3 elements to a column)
-__device__ __forceinline__ void mma_e4m3_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b,
-                                            uint32_t id, uint32_t accumulate) {
+// A from tensor memory (lane m = row m, four 8-bit elements to a column)
+__device__ __forceinline__ void mma_f8_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b,
+                                          uint32_t id, uint32_t accumulate) {
     asm volatile(
         "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
         " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem),
@@ -295,18 +298,18 @@ __device__ __forceinline__ uint32_t e4m3_f32(float lo, float hi) {
         : "f"(hi), "f"(lo));
     return r;
 }
-// four f16 (two pairs) -> four e4m3 codes, and back
-__device__ __forceinline__ uint32_t e4m3x4_f16(uint32_t a, uint32_t b) {
+// four f16 (two pairs) -> four e5m2 codes (nearest even, saturating), and back
+__device__ __forceinline__ uint32_t e5m2x4_f16(uint32_t a, uint32_t b) {
     uint32_t r;
-    asm("{\n .reg .b16 l, u;\n cvt.rn.satfinite.e4m3x2.f16x2 l, %1;\n"
-        " cvt.rn.satfinite.e4m3x2.f16x2 u, %2;\n mov.b32 %0, {l, u};\n}"
+    asm("{\n .reg .b16 l, u;\n cvt.rn.satfinite.e5m2x2.f16x2 l, %1;\n"
+        " cvt.rn.satfinite.e5m2x2.f16x2 u, %2;\n mov.b32 %0, {l, u};\n}"
         : "=r"(r)
         : "r"(a), "r"(b));
     return r;
 }
-__device__ __forceinline__ void f16_e4m3x4(uint32_t c, uint32_t &a, uint32_t &b) {
-    asm("{\n .reg .b16 l, u;\n mov.b32 {l, u}, %2;\n cvt.rn.f16x2.e4m3x2 %0, l;\n"
-        " cvt.rn.f16x2.e4m3x2 %1, u;\n}"
+__device__ __forceinline__ void f16_e5m2x4(uint32_t c, uint32_t &a, uint32_t &b) {
+    asm("{\n .reg .b16 l, u;\n mov.b32 {l, u}, %2;\n cvt.rn.f16x2.e5m2x2 %0, l;\n"
+        " cvt.rn.f16x2.e5m2x2 %1, u;\n}"
         : "=r"(a), "=r"(b)
         : "r"(c));
 }
@@ -322,9 +325,9 @@ __device__ __forceinline__ void unpack_f16(uint32_t h2, float &lo, float &hi) {
         : "=f"(lo), "=f"(hi)
         : "r"(h2));
 }
-__device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
+__device__ __forceinline__ uint32_t hsub2(uint32_t a, uint32_t b) {
     uint32_t d;
-    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
 }
 __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {

@@ -582,3 +582,38 @@ def test_attention_of_many_short_pairs_with_changing_lengths():
         o, l = ref.attention(c[0], np.float32(c[1]), c[2], np.float32(c[3]), c[4], p, [2] * B, f64(q), f64(kb), f64(vb))
         assert_close(f64(out), o, lse.cpu().numpy(), l, where="lengths")
     assert das.workspace_status(ws) == 0
+
+
+def sink_case(rng, D, Hq, Hkv, Tm, P, T, gap, sinks):
+    """One key, or one of each page, whose score lies about `gap` above those of all others (deviation
+    0.3), with values of 0; the others' values have mean 0.5.  The output is then the others' share."""
+    kc, ks, vc, vs, table, P, T, q, kb, vb = attention_case(rng, D, Hq, Hkv, Tm, P, T)
+    used, pages = kc != 0x7F, np.unique(table[table >= 0])
+    sigma = 0.3 * 2.0 ** 4
+    k, v = rng.normal(0, sigma, kc.shape), rng.normal(0.5, 0.2, vc.shape) * 2.0 ** 6
+    k[..., 0] = 0                                           # a dimension of the sinks alone
+    ks[pages], vs[pages] = 2.0 ** -4, 2.0 ** -6
+    first = table[:, 0] if sinks == "first" else pages
+    k[first, :, 0, :], v[first, :, 0, :] = 0, 0
+    k[first, :, 0, 0] = 256.0
+    q[..., 0] = np.where(np.isnan(q[..., 0]), np.nan, gap * np.sqrt(D) / 16.0)
+    kb[..., 0], vb = np.where(np.isnan(kb[..., 0]), np.nan, -4.0), vb * 0.0
+    return (np.where(used, ref.to_e4m3(k), kc), ks, np.where(vc != 0x7F, ref.to_e4m3(v), vc), vs, table, P, T, q, kb, vb)
+
+
+@pytest.mark.parametrize("gap", [12.0, 16.0])
+@pytest.mark.parametrize("D,Hq,Hkv,Tm,P,sinks,columns", [
+    (128, 4, 2, 4, [32768], "first", 513), (128, 4, 2, 16, [8000, 3000], "pages", 600),
+    (64, 16, 1, 4, [5000], "pages", 600),                   # equal ranges and a merge
+    (128, 8, 8, 8, [4096], "pages", 64), (128, 8, 2, 8, [2500], "pages", 40),
+    (64, 4, 4, 1, [3000], "pages", 47), (128, 2, 2, 64, [1500], "pages", 24),  # clusters
+    (128, 8, 8, 2, [190] * 25, "pages", 3), (64, 32, 8, 16, [250, 128, 100, 64] * 6, "pages", 4)])  # whole pairs
+def test_attention_keeps_small_weights(D, Hq, Hkv, Tm, P, sinks, columns, gap):
+    """Thousands of keys of weight e^-gap beside one of weight 1: their share is kept as bfloat16
+    weights would keep it, each to 2^-9 of itself (the output's rounding is another 2^-9)."""
+    rng = np.random.default_rng(D + Hq + int(gap))
+    case = list(sink_case(rng, D, Hq, Hkv, Tm, P, [Tm] * len(P), gap, sinks))
+    if columns > case[4].shape[1]:
+        case = widen(case, columns)
+    out, lse = run_attention(*case, where=f"sinks, gap {gap}")
+    assert float(out[0, 0].float().abs().max()) > 0
