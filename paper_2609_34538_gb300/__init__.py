@@ -527,7 +527,11 @@ class PagedKVCache:
             raise ValueError(f"pages must have {PAGE_TOKENS} tokens, got {page}")
         if tuple(k_scale.shape) != (R, L, N, H) or tuple(v_scale.shape) != (R, L, N, H):
             raise ValueError("k_scale / v_scale must be [depths][layers][pages][kv_heads]")
+        for t, name in ((v, "v"), (k_scale, "k_scale"), (v_scale, "v_scale")):
+            if t.device != k.device:
+                raise ValueError(f"{name} is on {t.device}, k on {k.device}")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.gpu = k.device.index
         self.desc = das_kv_cache_paged(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
                                        v_scale.data_ptr(), R, L, N, H, D)
         self.address = ctypes.addressof(self.desc)
@@ -540,6 +544,11 @@ class PagedKVCache:
                                     device=device)
         scales = lambda: torch.ones(tiles, dtype=torch.float32, device=device)
         return cls(codes(), codes(), scales(), scales())
+
+
+def _on_gpu_of(cache, t, name):
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != cache.gpu:
+        raise ValueError(f"{name} is on {t.device}, the cache on cuda:{cache.gpu}")
 
 
 def das_page_assign(seq_len, grow, block_table, free_pages, free_count, slots, error_flag,
@@ -561,6 +570,7 @@ def das_kv_append_paged(cache, k_new, v_new, slots, slot_start, error_flag, stre
     """Commit into a PagedKVCache: the first slot_start[b + 1] - slot_start[b] of
     each sequence's staged tokens, at every depth and layer, as e4m3 codes under
     a power-of-two scale per (page, kv head)."""
+    _on_gpu_of(cache, k_new, "k_new")  # (the binding compares the others with it)
     r = _calls.kv_append_paged(cache.address, k_new, v_new, slots, slot_start, error_flag, stream)
     if r is not None:
         raise DasError(r, "das_kv_append_paged")
@@ -579,6 +589,7 @@ def das_mature_v_attention_paged(cache, layer, key_depth, value_depth, block_tab
                                  softmax_scale=0.0, stream=None):
     """das_mature_v_attention over a PagedKVCache; key_depth = value_depth is the
     verify attention.  Returns (out, lse)."""
+    _on_gpu_of(cache, q, "q")  # (the binding compares the others with it)
     r = _calls.mature_v_attention_paged(cache.address, layer, key_depth, value_depth, block_table,
                                         prefix_len, block_len, q, k_blk, v_blk, workspace, out,
                                         lse, softmax_scale, stream)

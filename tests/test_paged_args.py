@@ -102,3 +102,87 @@ def test_binding_module_refuses_bad_numbers():
         call()
     with pytest.raises(TypeError, match="9 arguments"):
         das._calls.sample(t, t)
+
+
+@pytest.fixture
+def fake():
+    """Tensors that say which GPU they are on and have no memory: nothing can be launched on them."""
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    with FakeTensorMode():
+        yield lambda dtype, *shape, gpu=0: torch.empty(shape, dtype=dtype, device=f"cuda:{gpu}")
+
+
+OTHER_GPU = "on cuda:1, other arguments on cuda:0"
+
+
+def test_page_assign_refuses_tensors_of_two_gpus(fake):
+    shapes = dict(seq_len=(3,), grow=(3,), block_table=(3, 4), free_pages=(8,), free_count=(1,), slots=(16,),
+                  error_flag=(1,), new_len=(3,), new_free_count=(1,), slot_start=(4,))
+    for other in list(shapes)[1:]:
+        args = {n: fake(torch.int32, *s, gpu=int(n == other)) for n, s in shapes.items()}
+        with pytest.raises(ValueError, match=f"{other} is {OTHER_GPU}"):
+            das.das_page_assign(**args)
+
+
+def test_sampling_refuses_tensors_of_two_gpus(fake):
+    i32, f32 = torch.int32, torch.float32
+    shapes = dict(logits=(f32, 2, 3, 50), draft_ids=(i32, 2, 3), uniforms=(f32, 2, 3), temperature=(f32, 2), top_k=(i32, 2),
+                  top_p=(f32, 2), min_p=(f32, 2), accepted=(i32, 2), target_ids=(i32, 2, 3), next_token=(i32, 2),
+                  committed=(i32, 2), logprobs=(f32, 2, 3))
+    for other in list(shapes)[1:]:
+        args = {n: fake(*s, gpu=int(n == other)) for n, s in shapes.items()}
+        with pytest.raises(ValueError, match=f"{other} is {OTHER_GPU}"):
+            das.das_sample_accept(**args)
+    shapes = {n: s for n, s in shapes.items() if n in ("logits", "uniforms", "temperature", "top_k", "top_p", "min_p")}
+    shapes |= dict(tokens=(i32, 2, 3), logprobs=(f32, 2, 3))
+    for other in list(shapes)[1:]:
+        args = {n: fake(*s, gpu=int(n == other)) for n, s in shapes.items()}
+        with pytest.raises(ValueError, match=f"{other} is {OTHER_GPU}"):
+            das.das_sample(**args)
+
+
+class CacheOnGpu0:
+    """What the calls read of a PagedKVCache before they launch."""
+    def __init__(self):
+        self.desc = das.das_kv_cache_paged(256, 256, 256, 256, 2, 1, 4, 2, 64)
+        self.address, self.gpu, self.shape = ctypes.addressof(self.desc), 0, (2, 1, 4, 2, 64)
+
+
+def test_cache_calls_refuse_tensors_of_two_gpus(fake):
+    i32, bf16 = torch.int32, torch.bfloat16
+    c = CacheOnGpu0()
+    shapes = dict(k_new=(bf16, 2, 1, 1, 4, 2, 64), v_new=(bf16, 2, 1, 1, 4, 2, 64), slots=(i32, 8), slot_start=(i32, 2),
+                  error_flag=(i32, 1))
+    for other in shapes:
+        args = {n: fake(*s, gpu=int(n == other)) for n, s in shapes.items()}
+        with pytest.raises(ValueError, match="on cuda:1" if other == "k_new" else f"{other} is {OTHER_GPU}"):
+            das.das_kv_append_paged(c, **args)
+    shapes = dict(block_table=(i32, 1, 4), prefix_len=(i32, 1), block_len=(i32, 1), q=(bf16, 1, 2, 4, 64),
+                  k_blk=(bf16, 1, 2, 2, 64), v_blk=(bf16, 1, 2, 2, 64), workspace=(torch.uint8, 1 << 20),
+                  out=(bf16, 1, 2, 4, 64), lse=(torch.float32, 1, 4, 2))
+    for other in shapes:
+        args = {n: fake(*s, gpu=int(n == other)) for n, s in shapes.items()}
+        with pytest.raises(ValueError, match="on cuda:1"):
+            das.das_mature_v_attention_paged(c, 0, 1, 1, **args)
+    # all of them on one GPU, the cache on another
+    for shapes, call in ((dict(k_new=(bf16, 2, 1, 1, 4, 2, 64), v_new=(bf16, 2, 1, 1, 4, 2, 64), slots=(i32, 8),
+                               slot_start=(i32, 2), error_flag=(i32, 1)), lambda **a: das.das_kv_append_paged(c, **a)),
+                         (shapes, lambda **a: das.das_mature_v_attention_paged(c, 0, 1, 1, **a))):
+        with pytest.raises(ValueError, match="on cuda:1, the cache on cuda:0"):
+            call(**{n: fake(*s, gpu=1) for n, s in shapes.items()})
+
+
+def test_a_cache_is_on_one_gpu(fake):
+    shapes = dict(k=(torch.uint8, 1, 1, 2, 1, 64, 64), v=(torch.uint8, 1, 1, 2, 1, 64, 64),
+                  k_scale=(torch.float32, 1, 1, 2, 1), v_scale=(torch.float32, 1, 1, 2, 1))
+    for other in list(shapes)[1:]:
+        with pytest.raises(ValueError, match=f"{other} is on cuda:1, k on cuda:0"):
+            das.PagedKVCache(**{n: fake(*s, gpu=int(n == other)) for n, s in shapes.items()})
+
+
+def test_a_stream_of_another_gpu_is_refused(fake):
+    class Stream:                        # what the binding reads of a torch.cuda.Stream
+        stream_id, device_index, device_type = 0, 1, 1
+    logits, u = fake(torch.float32, 1, 2, 9), fake(torch.float32, 1, 2)
+    with pytest.raises(ValueError, match="stream is of cuda:1, the arguments on cuda:0"):
+        das.das_sample(logits, u, stream=Stream())
