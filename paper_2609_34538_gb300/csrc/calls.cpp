@@ -171,10 +171,11 @@ PyObject *pack(R &...results) {
 
 template <typename F>
 das_status without_gil(F f) {
-    PyThreadState *const state = PyEval_SaveThread();
-    const das_status s = f();
-    PyEval_RestoreThread(state);
-    return s;
+    struct Released {  // taken again on an exception too (a tensor without memory has no address)
+        PyThreadState *const state = PyEval_SaveThread();
+        ~Released() { PyEval_RestoreThread(state); }
+    } released;
+    return f();
 }
 
 template <typename T>

@@ -316,3 +316,12 @@ def test_many_candidates_of_a_small_top_k(B, C, dtype, k, p, values):
     n = len(some)
     ids, logp = check(logits[some].contiguous(), u[some], [0.8] * n, [k] * n, [p] * n, [0.0] * n)
     assert torch.equal(ids, runs[0][0][some]) and torch.equal(logp, runs[0][1][some])
+
+
+def test_tensors_without_memory_are_refused():
+    """Inside vmap a tensor has no address: an exception, with the interpreter as it was."""
+    u = torch.rand((1, 2), device="cuda")
+    with pytest.raises(RuntimeError, match="storage"):
+        torch.vmap(lambda x: das.das_sample(x, u)[0])(torch.randn((3, 1, 2, 9), device="cuda"))
+    ids, _ = das.das_sample(torch.randn((1, 2, 9), device="cuda"), u)
+    assert ids.shape == (1, 2)
