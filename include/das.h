@@ -384,7 +384,8 @@ das_status das_page_assign(const int32_t *seq_len, const int32_t *grow, int batc
  *   error_flag    device int32 [1]: bit 1 is set (never cleared) and the page
  *                 left alone where a slot lies outside the cache, a page does
  *                 not start at its first place, or n_b is not in 0..W
- * Sequences do not share the pages that they write.  Requires W >= 1.
+ * Sequences do not share the pages that they write.  Requires W >= 1 and
+ * batch >= 0 (with 0, k_new and v_new may be NULL; with max_slots 0, slots).
  */
 das_status das_kv_append_paged(const das_kv_cache_paged *cache, const void *k_new,
                                const void *v_new, int batch, int W, const int32_t *slots,
@@ -457,7 +458,8 @@ typedef struct {
  *   uniforms  device fp32 [B][W], in [0, 1)
  *   tokens    device int32 [B][W]
  *   logprobs  device fp32 [B][W], or NULL
- * Requires 1 <= W <= 1024, 1 <= vocab < 2^31.
+ * Requires B >= 0 (with 0 the tensors may be NULL), 1 <= W <= 1024,
+ * 1 <= vocab < 2^31.
  */
 das_status das_sample(const void *logits, das_logits_type type, int B, int W, int vocab,
                       long long row_stride, const das_sampling *sampling, const float *uniforms,

@@ -491,9 +491,9 @@ das_status das_kv_append_paged(const das_kv_cache_paged *cache, const void *k_ne
                                int max_slots, const int32_t *slot_start, int32_t *error_flag,
                                void *stream) {
     if (cache && cache->head_dim != 64 && cache->head_dim != 128) return DAS_ERR_UNSUPPORTED;
-    if (!das::cache_paged_ok(cache) || !k_new || !v_new || batch < 0 || W < 1 || !slots ||
-        max_slots < 0 || !slot_start || !error_flag || !das::aligned16(k_new) ||
-        !das::aligned16(v_new))
+    if (!das::cache_paged_ok(cache) || (batch > 0 && (!k_new || !v_new)) || batch < 0 || W < 1 ||
+        (max_slots > 0 && !slots) || max_slots < 0 || !slot_start || !error_flag ||
+        !das::aligned16(k_new) || !das::aligned16(v_new))
         return DAS_ERR_INVALID_ARG;
     const long long pieces = ((long long)W + 2 * DAS_PAGE_TOKENS - 2) / DAS_PAGE_TOKENS;
     if (W > (1 << 24) || pieces * cache->depths * cache->layers > 0x7fffffffLL / 2 ||
@@ -533,9 +533,10 @@ das_status das_mature_v_attention_paged(const das_kv_cache_paged *cache, int lay
 
 static bool sample_args_ok(const das::SampleArgs &a, das_logits_type type) {
     const uintptr_t elem = type == DAS_LOGITS_BF16 ? 2 : 4;
-    return (type == DAS_LOGITS_F32 || type == DAS_LOGITS_BF16) && a.logits && a.uniforms &&
-           a.tokens && a.B >= 0 && a.W >= 1 && a.W <= 1024 && a.vocab >= 1 &&
-           a.row_stride >= a.vocab && (long long)a.B * a.W <= 0x7fffffffLL / 8 &&
+    return (type == DAS_LOGITS_F32 || type == DAS_LOGITS_BF16) &&
+           (a.B == 0 || (a.logits && a.uniforms && a.tokens)) && a.B >= 0 && a.W >= 1 &&
+           a.W <= 1024 && a.vocab >= 1 && a.row_stride >= a.vocab &&
+           (long long)a.B * a.W <= 0x7fffffffLL / 8 &&
            reinterpret_cast<uintptr_t>(a.logits) % elem == 0;
 }
 
@@ -558,7 +559,7 @@ das_status das_sample_accept(const void *logits, das_logits_type type, const int
     const das_sampling s = sampling ? *sampling : das_sampling{};
     const das::SampleArgs a = {logits,     type == DAS_LOGITS_BF16, B, W, vocab, row_stride, s,
                                uniforms, target_ids, logprobs, nullptr, nullptr, nullptr, nullptr};
-    if (!sample_args_ok(a, type) || !draft_ids || !accepted || !next_token)
+    if (!sample_args_ok(a, type) || (B > 0 && (!draft_ids || !accepted || !next_token)))
         return DAS_ERR_INVALID_ARG;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     return das::sample_accept_launch(a, draft_ids, accepted, next_token, committed, st) ==

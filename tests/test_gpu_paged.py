@@ -617,3 +617,27 @@ def test_attention_keeps_small_weights(D, Hq, Hkv, Tm, P, sinks, columns, gap):
         case = widen(case, columns)
     out, lse = run_attention(*case, where=f"sinks, gap {gap}")
     assert float(out[0, 0].float().abs().max()) > 0
+
+
+def test_a_step_without_requests():
+    """Empty tensors through every call of a step that takes them, and requests without new tokens."""
+    H, D, N = 2, 64, 3
+    cache = das.PagedKVCache.empty(2, 1, N, H, D)
+    cache.k.fill_(7)
+    free, count, flag = dev_i32(range(N)), dev_i32([N]), dev_i32([0])
+    f32, none = torch.float32, lambda dtype, *s: torch.empty(s, dtype=dtype, device="cuda")
+    out = das.das_sample_accept(none(f32, 0, 3, 50), none(torch.int32, 0, 3), none(f32, 0, 3), temperature=none(f32, 0))
+    assert [x.shape[0] for x in out] == [0] * 5
+    ids, logp = das.das_sample(none(torch.bfloat16, 0, 3, 50), none(f32, 0, 3))
+    assert ids.shape == logp.shape == (0, 3)
+    empty = none(torch.int32, 0)
+    n, c, start = das.das_page_assign(empty, out[3], none(torch.int32, 0, 4), free, count, empty, flag)
+    assert n.shape == (0,) and c.item() == N and start.tolist() == [0]
+    das.das_kv_append_paged(cache, none(torch.bfloat16, 2, 1, 0, 3, H, D), none(torch.bfloat16, 2, 1, 0, 3, H, D), empty,
+                            start, flag)
+    # two requests, none of which has committed a token: there are no slots
+    new = bf16(np.ones((2, 1, 2, 3, H, D)))
+    das.das_kv_append_paged(cache, new, new, empty, dev_i32([0, 0, 0]), flag)
+    assert flag.item() == 0 and bool((cache.k == 7).all())
+    das.das_kv_append_paged(cache, new, new, empty, dev_i32([0, 1, 1]), flag)   # a token without a slot is flagged
+    assert flag.item() == 2 and bool((cache.k == 7).all())

@@ -186,3 +186,19 @@ def test_a_stream_of_another_gpu_is_refused(fake):
     logits, u = fake(torch.float32, 1, 2, 9), fake(torch.float32, 1, 2)
     with pytest.raises(ValueError, match="stream is of cuda:1, the arguments on cuda:0"):
         das.das_sample(logits, u, stream=Stream())
+
+
+def test_empty_calls_do_nothing():
+    """No sequences: whatever has no elements has no address either."""
+    ok = das.DAS_OK
+    assert L.das_kv_append_paged(cache(), NULL, NULL, 0, 4, NULL, 0, A, A, NULL) == ok
+    assert L.das_kv_append_paged(cache(), NULL, NULL, 0, 4, A, 4, A, A, NULL) == ok
+    for kind in (0, 1):
+        assert L.das_sample(NULL, kind, 0, 3, 10, 10, None, NULL, NULL, NULL, NULL) == ok
+        assert L.das_sample_accept(NULL, kind, NULL, 0, 3, 10, 10, None, NULL, NULL, NULL, NULL, NULL, NULL, NULL) == ok
+    # what is out of range without any sequence is refused as with one
+    assert L.das_kv_append_paged(cache(), NULL, NULL, 0, 0, NULL, 0, A, A, NULL) == BAD
+    assert L.das_kv_append_paged(cache(), NULL, NULL, 0, 4, NULL, 4, A, A, NULL) == BAD
+    assert L.das_kv_append_paged(cache(dim=96), NULL, NULL, 0, 4, NULL, 0, A, A, NULL) == UNSUPPORTED
+    assert L.das_sample(NULL, 2, 0, 3, 10, 10, None, NULL, NULL, NULL, NULL) == BAD
+    assert L.das_sample(NULL, 0, 0, 3, 10, 9, None, NULL, NULL, NULL, NULL) == BAD
