@@ -30,8 +30,10 @@ ABI in include/das.h:
                             DAS-Wave's round schedule (Eq. 5) and the device
                             side of its carried parallel refinement (Sec. 3.3)
 
-If libdas.so or the binding's module _calls.so is missing the import fails:
-there is no fallback.
+If libdas.so is missing the import fails: there is no fallback.  The paged-cache
+and sampling calls need the binding's module _calls.so too, which is built
+against PyTorch's headers: without it they raise ImportError, the others do not
+need it.
 """
 import ctypes
 import os
@@ -77,10 +79,9 @@ class das_sampling(ctypes.Structure):
 
 
 def _load():
-    for path in (LIB_PATH, os.path.join(_HERE, "_calls.so")):
-        if not os.path.exists(path):
-            raise ImportError(f"{path} is not built: run `python paper_2609_34538_gb300/build.py` "
-                              "(needs nvcc with sm_103a support, and g++)")
+    if not os.path.exists(LIB_PATH):
+        raise ImportError(f"{LIB_PATH} is not built: run `python paper_2609_34538_gb300/build.py` "
+                          "(needs nvcc with sm_103a support)")
     lib = ctypes.CDLL(LIB_PATH)
     i, p, f, sz = ctypes.c_int, ctypes.c_void_p, ctypes.c_float, ctypes.c_size_t
     cp = ctypes.POINTER(das_kv_cache)
@@ -128,7 +129,23 @@ def _load():
 
 
 LIB = _load()
-from . import _calls  # noqa: E402  (needs torch's libraries, and libdas.so beside it)
+
+
+class _NoCalls:
+    """In the place of the binding's module where it could not be imported."""
+
+    def __init__(self, reason):
+        self._reason = reason
+
+    def __getattr__(self, name):
+        raise ImportError(f"{os.path.join(_HERE, '_calls.so')} is not there or does not fit this "
+                          f"PyTorch ({self._reason}): run `python paper_2609_34538_gb300/build.py`")
+
+
+try:
+    from . import _calls  # needs torch's libraries, and libdas.so beside it
+except ImportError as _e:
+    _calls = _NoCalls(_e)
 
 
 def status_string(code):

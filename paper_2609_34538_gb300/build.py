@@ -91,7 +91,6 @@ def build(force=False, verbose=False):
     with cf.ThreadPoolExecutor(max_workers=len(_sources()) + 1) as ex:
         calls = ex.submit(_compile_calls)
         results = list(ex.map(lambda s: _compile(s, extra), _sources()))
-        calls = calls.result()
     if verbose:
         for _, log in results:
             sys.stderr.write(log)
@@ -99,7 +98,7 @@ def build(force=False, verbose=False):
     cmd = [NVCC, *ARCH, "-shared", "-o", tmp] + [o for o, _ in results]
     _run(cmd, "link")
     os.replace(tmp, LIB)
-    _link_calls(calls)
+    _link_calls(calls.result())  # (last: libdas.so does not need it)
     return LIB
 
 
