@@ -325,3 +325,24 @@ def test_tensors_without_memory_are_refused():
         torch.vmap(lambda x: das.das_sample(x, u)[0])(torch.randn((3, 1, 2, 9), device="cuda"))
     ids, _ = das.das_sample(torch.randn((1, 2, 9), device="cuda"), u)
     assert ids.shape == (1, 2)
+
+
+@pytest.mark.parametrize("B,W,V,dtype", [(9, 1, 33001, torch.float32), (19, 1, 70001, torch.bfloat16),
+                                         (12, 2, 33001, torch.float32), (25, 3, 20003, torch.bfloat16),
+                                         (100, 2, 9001, torch.float32), (2, 1, 363001, torch.float32),
+                                         (3, 1, 530003, torch.bfloat16)])
+def test_parameters_of_each_sequence(B, W, V, dtype):
+    """Greedy, filtered and plain rows in one call, from eight CTAs a row to one, and past a cluster:
+    tokens and log-probabilities of every eighth row, and of the first and last ones."""
+    g = torch.Generator(device="cuda").manual_seed(V + B)
+    logits = (3 * torch.randn((B, W, V), generator=g, device="cuda")).to(dtype)
+    u = torch.rand((B, W), generator=g, device="cuda")
+    kinds = [(1.0, 40, 0.95, 0.0), (0.0, 0, 1.0, 0.0), (0.8, 0, 0.9, 0.0), (1.3, 700, 1.0, 0.02), (0.7, 5, 0.5, 0.1),
+             (1.0, 0, 1.0, 0.0), (-1.0, 9, 0.3, 0.5), (2.0, 0, 1.0, 0.3), (0.9, V, 0.999, 0.0)]
+    T, k, p, m = zip(*(kinds[b % len(kinds)] for b in range(B)))
+    ids, logp = das.das_sample(logits, u, temperature=f32(T), top_k=dev_i32(k), top_p=f32(p), min_p=f32(m))
+    some = sorted({0, B - 1, *range(0, B, 8), *range(min(B, 3))})
+    pick = lambda x: [x[b] for b in some]
+    part, part_u = logits[some].contiguous(), u[some].cpu().numpy()
+    want = check(part, part_u, pick(T), pick(k), pick(p), pick(m))      # (a call of its own, of other CTAs a row)
+    assert torch.equal(ids[some], want[0]) and torch.equal(logp[some], want[1])
