@@ -412,11 +412,12 @@ size_t das_workspace_size_paged(const das_kv_cache_paged *cache, int batch, int 
  * cache; its 64 tokens are then taken as masked.
  * The products run on the codes: a query row is split into two e4m3 parts,
  * exactly for elements down to about 2^-13 of the row's largest (queries must
- * be finite), a softmax weight into three e5m2 parts, to 2^-9 of itself (as a
- * bf16 weight is) or 2^-30 of the row's largest weight times value scale;
- * scores, sums and outputs are accumulated in fp32.  The value scales that one sequence
- * reads are to be within a factor of 2^100 of each other and of 1 (a scale of 0
- * counts as 2^-60).
+ * be finite), a softmax weight into three e5m2 parts: to 2^-9 of itself, as a
+ * bf16 weight is, where weight times value scale is above 2^-21 of the row's
+ * largest sum of these over a page, below to 2^-6 of itself or 2^-30 of that sum.
+ * Scores, sums and outputs are accumulated in fp32.  The value scales that one
+ * sequence reads are to be within a factor of 2^100 of each other and of 1 (a
+ * scale of 0 counts as 2^-60).
  */
 das_status das_mature_v_attention_paged(const das_kv_cache_paged *cache, int layer, int key_depth,
                                         int value_depth, const int32_t *block_table, int max_pages,

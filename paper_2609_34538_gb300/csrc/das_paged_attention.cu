@@ -9,8 +9,8 @@
 // lse = ln 2 (m - kHead + log2 l): a page's value scale is part of the weight
 // that its codes are multiplied with, so the products run on the codes alone.
 // m moves (O and l are rescaled) only when a thread's weights of a tile sum to
-// more than kMost = 2^13 and the tile's largest x exceeds m by more than kWindow,
-// so that no weight is above 2^13 and all parts of one fit their types.
+// more than kMost = 2^13, so that no weight is above 2^13 and all parts of one fit
+// their types; it is then set to where the row's weights of the tile sum to 2^7 to 2^8.
 //
 // The operands of an 8-bit product have 3 or 4 significant bits, which is too few
 // for queries and weights, so each is split into parts:
@@ -18,16 +18,17 @@
 //            exact for elements down to about 2^-13 of the row's largest (a
 //            bf16 value has 8 significant bits); S = S_hi + S_lo / 16, added
 //            where the scores are read;
-//   weights  p = a + b + c / 256, all e5m2 (which A may be beside an e4m3 B): a
-//            and c two rows of one product, b a second product into a's rows;
-//            O = O_hi + O_lo / 256, added at the end of a segment.  Off by 2^-9
-//            of p, as bf16 weights are, or by 2^-24, where the reference's
-//            weight is 2^kHead = 2^7: what one dominant key leaves to thousands of
-//            others is kept.  Two e4m3 parts, whose range ends 2^-17 below the reference,
-//            lost most of that; they took 53.0 us where three take 56.2 (4 x 32768
-//            tokens), and values widened to f16 in shared memory 60.7.
-// Row r of the pair (r = i * G + g) has its hi part in TMEM lane
-// 32 (r / 16) + r % 16 and its lo part 16 lanes on, in the same warp's reach.
+//   weights  p = a + (b + c) / 64, all e5m2 (which A may be beside an e4m3 B): a
+//            and b two rows of one product, c a second product into b's rows;
+//            O = O_hi + O_lo / 64, added at the end of a segment.  Off by 2^-9 of
+//            p, as bf16 weights are, down to p = 2^-14, which is 2^-21 of the tile's
+//            sum, and below by 2^-6 of p or 2^-30 of that sum: what one dominant key
+//            leaves to thousands of others is kept.  Two e4m3 parts, whose range ended
+//            2^-17 below the reference, lost most of that; they took 53.3 us where
+//            three take 55.4 (4 x 32768 tokens).  Values widened to f16 in shared
+//            memory, 16 KB more written and 8 more read a tile, took 60.7.
+// Row r of the pair (r = i * G + g) has its hi (a) part in TMEM lane
+// 32 (r / 16) + r % 16 and its lo (b, c) parts 16 lanes on, in the same warp's reach.
 //
 // Work split: every (sequence, kv head) pair owns one tile for each of its
 // ceil(P / 64) pages plus one for the block's own keys.  There are two ways:
@@ -42,9 +43,9 @@
 // log_cluster_of and launch_d say which, with both measured.
 //
 // What bounds it: 4 sequences of 32768 tokens, 32 / 8 heads of 128 and blocks of 16
-// take 56.2 us, 4.8 TB/s of codes (bare TMA reads of the same tiles: 48.8 us); a tile
+// take 55.4 us, 4.8 TB/s of codes (bare TMA reads of the same tiles: 48.8 us); a tile
 // of 16 KB takes a CTA 0.39 us, the pace of the softmax groups below.  One
-// sequence of 4096 tokens with 32 heads takes 14.1 us (blocks of 1) and 14.6 us (8),
+// sequence of 4096 tokens with 32 heads takes 14.2 us (blocks of 1) and 14.6 us (8),
 // of which the tiles take 6 to 7; the smallest calls 5.9 us.
 //
 // One CTA = two groups of four softmax warps, which take turns at the tiles
@@ -90,16 +91,22 @@ constexpr int kOStep = 128;
 constexpr int kPCol = kOCol + kGroups * kOStep;
 constexpr int kPStep = 32;
 static_assert(kPCol + kGroups * kPStep == kTmemCols, "tensor memory");
-constexpr float kHead = 7.f, kWindow = 6.f, kMost = 8192.f;  // 2^(kHead + kWindow) <= kMost
-constexpr float kQLoInv = 1.f / 16.f, kPLo = 256.f, kPLoInv = 1.f / kPLo;
-constexpr uint32_t kPLo2 = 0x5c005c00u;   // f16x2 of kPLo
+// A new reference leaves the row of the tile a sum of 2^kSumLog to twice that, which 64
+// equal weights of 2^kHead have.  The lower, the more the sums may grow before the
+// next one; the higher, the more of small weights is kept (kSumLog 6, 7, 8, 9, kHead
+// below: 54.3, 55.4, 57.7, about 60 us for 4 x 32768 tokens whose pages' scores and
+// values differ in size by a factor of 4).
+constexpr int kSumLog = 7;
+constexpr float kHead = 1.f, kMost = 8192.f;
+constexpr float kQLoInv = 1.f / 16.f, kPLo = 64.f, kPLoInv = 1.f / kPLo;
+constexpr uint32_t kPLo2 = 0x54005400u;   // f16x2 of kPLo
 constexpr uint32_t kLoLanes = 16u << 16;
 constexpr int kPrefetch = 4;       // pages pulled into L2 before the dependency wait
 
-// Four weights, f16 pairs x and y (0 to kMost), as three e5m2 parts each: p = a + b +
-// c / kPLo, off by at most 2^-9 of p (each part leaves 2^-3 of what it rounds) or
-// 2^-25: e5m2 reaches as far down as f16 nearly, and c, kPLo times what remains
-// (2^7 at most), down to all of it.  The differences are exact.
+// Four weights, f16 pairs x and y (0 to kMost), as three e5m2 parts each: p = a +
+// (b + c) / kPLo.  Each part leaves 2^-3 at most of what it rounds, so p is off by 2^-9 of
+// itself down to 2^-14, where a ends, and below by 2^-6 of itself or 2^-23 (a multiple of
+// b's least number).  kPLo times what a leaves is 2^15 at most.  The differences are exact.
 struct Parts {
     uint32_t a, b, c;
 };
@@ -108,11 +115,11 @@ __device__ __forceinline__ Parts parts_of(uint32_t x, uint32_t y) {
     uint32_t u, v;
     r.a = e5m2x4_f16(x, y);
     f16_e5m2x4(r.a, u, v);
-    x = hsub2(x, u);
-    y = hsub2(y, v);
+    x = hmul2(hsub2(x, u), kPLo2);
+    y = hmul2(hsub2(y, v), kPLo2);
     r.b = e5m2x4_f16(x, y);
     f16_e5m2x4(r.b, u, v);
-    r.c = e5m2x4_f16(hmul2(hsub2(x, u), kPLo2), hmul2(hsub2(y, v), kPLo2));
+    r.c = e5m2x4_f16(hsub2(x, u), hsub2(y, v));
     return r;
 }
 
@@ -152,8 +159,8 @@ __device__ __forceinline__ void walk_pair(const PagedAttnParams &p, Walk &w) {
 // Tile x of pair n has weighted position x + beta n; CTA c takes the tiles at
 // [c W / C, (c + 1) W / C).  The end of a pair (its block tile, the joining of
 // the groups, the next pair's start) costs a CTA about as much as nine pages, so
-// a range that holds one takes beta tiles fewer (weights 3, 5, 7, 9, 12: 57.7,
-// 57.0, 56.5, 56.2, 56.5 us for 4 x 32768 tokens, 49.6, 45.7, 46.3, 45.5, 45.1
+// a range that holds one takes beta tiles fewer (weights 3, 5, 7, 9, 12: 57.6,
+// 56.9, 56.4, 55.7, 56.2 us for 4 x 32768 tokens, 49.9, 45.7, 46.1, 45.4, 44.9
 // for 16 ragged sequences); beta = 0 with more pairs than CTAs (nearly every
 // range then holds one) or where a CTA could stay empty.
 constexpr int kBlockWeight = 9;
@@ -754,7 +761,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const uint64_t b0 = dv8 + (uint64_t)((st.i * Lt::kStage) >> 4);
                     // (the group's first tile of the segment begins its O)
 #pragma unroll
-                    for (int kk = 0; kk < 4; ++kk)  // parts a and c, then b, each of 2 x 32 keys
+                    for (int kk = 0; kk < 4; ++kk)  // parts a and b, then c, each of 2 x 32 keys
                         mma_f8_ta(dO, a0 + 8 * kk, b0 + (uint64_t)(((kk & 1) * 32 * D) >> 4), id8,
                                   k - k_seg >= kGroups || kk > 0);
                     mma_commit(b_empty + 8 * st.i);
@@ -818,9 +825,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t o_col = lanes + kOCol + (uint32_t)(group * kOStep);
         float2 *ml = reinterpret_cast<float2 *>(sm + Lt::kMlOff);
         const uint32_t p_col = lanes + kPCol + (uint32_t)(group * kPStep);
-        {  // beside b there is no fourth part
+        {  // beside c there is no fourth part
             const uint32_t zero[8] = {};
-            st_half(p_col + kPStep / 2 + kLoLanes, zero);
+            st_half(p_col + kPStep / 2, zero);
         }
         Walk w = w0;
         float m_ref = -INFINITY, l_sum = 0.f, row_scale = 1.f;
@@ -844,8 +851,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             // Weights of a tile from its scores v (hidden ones -inf), in e, and their
             // sum.  They are taken under the present reference; a thread whose 32
             // weights sum to no more than kMost has none above it, and only where
-            // that fails is the row's maximum found, the reference moved if it asks
-            // for it (O and l rescaled) and the weights taken again.
+            // that fails, or there is no reference yet, is the row's maximum found and the
+            // reference set by it (O and l rescaled) and the weights taken again.
             auto weights_of = [&](float (&v)[32], float (&e)[32], float scale, float lv, bool hidden) {
                 auto exps = [&] {
                     const float off = lv + kHead - (m_ref == -INFINITY ? 0.f : m_ref);
@@ -871,6 +878,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             add2(x[j], x[j + 1], x[j], x[j + 1], x[j + d], x[j + d + 1]);
                     return x[0] + x[1];
                 };
+                const bool fresh = k - k_seg < kGroups;  // the segment's first tile of the group
                 float sum = exps();
                 if (__any_sync(kFull, live && (m_ref == -INFINITY || !(sum <= kMost)))) {
                     float x[11];
@@ -882,14 +890,27 @@ __global__ void __launch_bounds__(kThreads, 1)
                                      fmaxf(x[9], x[10]));
                     mt = fmaxf(mt, __shfl_xor_sync(kFull, mt, 16));
                     mt = mt == -INFINITY ? -INFINITY : mt * scale + lv;
-                    const bool jump = live && mt > m_ref + kWindow;
+                    const bool over = !(sum <= kMost);
+                    const bool over_row = __shfl_xor_sync(kFull, over, 16) || over;
+                    const bool jump = live && mt > -INFINITY && (m_ref == -INFINITY || over_row);
                     if (__any_sync(kFull, jump)) {
-                        const float alpha = jump ? ex2(m_ref - mt) : 1.f;  // from -inf: 0
-                        if (jump) {
-                            m_ref = mt;
+                        const float old = m_ref;
+                        if (jump) m_ref = mt;
+                        sum = exps();
+                        const float row_sum = sum + __shfl_xor_sync(kFull, sum, 16);
+                        float alpha = 1.f;
+                        if (jump) {  // by the row's sum: what is far below one large weight is kept
+                            const int log_sum = (int)(__float_as_uint(row_sum) >> 23 & 0xffu) - 127;
+                            const int up = max(0, min(kSumLog - log_sum, kSumLog - (int)kHead));
+                            const float f = __uint_as_float((uint32_t)(127 + up) << 23);
+                            m_ref -= (float)up;
+                            sum *= f;
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) e[j] *= f;
+                            alpha = ex2(old - m_ref);  // from -inf: 0
                             l_sum *= alpha;
                         }
-                        if (k - k_seg >= kGroups) {  // the group has an O here
+                        if (!fresh) {  // the group has an O here
                             waits(b_pvdone + 8 * group, (uint32_t)((k / kGroups - 1) & 1));
                             fence_after();
                             // thread t holds lane t: row t % 16's hi or lo part, the same alpha
@@ -904,7 +925,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                             }
                             st_wait();
                         }
-                        sum = exps();
                     }
                 }
                 return sum;
@@ -962,8 +982,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 if (!pv_early) wait_pv();
                 st_half(p_col, pa);
-                st_half(p_col + kLoLanes, pc);
-                st_half(p_col + kPStep / 2, pb);
+                st_half(p_col + kLoLanes, pb);
+                st_half(p_col + kPStep / 2 + kLoLanes, pc);
                 // keys past the page's last token may hold anything: zero their value rows
                 if (n < kTileKeys) {
                     const uint32_t vt = sbase + s * Lt::kStage + Lt::kTile + n * D;
@@ -1331,7 +1351,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const Pag
 // The same where pairs have many segments: a row by both warps of a CTA.  A warp's
 // four groups of eight lanes take every fourth segment, two at a time, with a
 // reference and sums of their own, so that sixteen segments of a row are on their
-// way at once.  2 kv heads of 32768 tokens, the whole call: 16.1 us, 24.1 with a warp
+// way at once.  2 kv heads of 32768 tokens, the whole call: 16.2 us, 25.3 with a warp
 // to a row and four at once.
 struct Part {  // sums under the reference M
     float M, L;
@@ -1436,9 +1456,9 @@ size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 // Measured at 38 shapes, in tiles of 0.34 us: a cluster's CTA takes its own tiles and
 // 23; in the list a CTA takes an equal share of all tiles and 32, 0.25 for each of a
 // pair's segments, and 9 for each pair that ends in its range.  One sequence of
-// 4096 tokens with 32, 8 and 2 kv heads takes 14.1, 10.1 and 9.5 us in clusters,
-// 17.5, 12.4 and 15.0 in the list; of 32768 tokens 58.5, 32.3 and 31.5, and 54.3,
-// 22.7 and 16.3.
+// 4096 tokens with 32, 8 and 2 kv heads takes 14.2, 10.1 and 9.5 us in clusters,
+// 17.4, 12.7 and 15.3 in the list; of 32768 tokens 58.3, 32.3 and 31.4, and 53.8,
+// 22.8 and 16.2.
 // Lengths are not known here: the list's time is taken as the least it can be with x
 // pairs as long as the table allows and the others empty, x from a sequence's kv
 // heads to all pairs, which is at x = CTAs sqrt(0.25 / nt).
@@ -1515,18 +1535,18 @@ cudaError_t launch_d(PagedAttnParams &p, const CUtensorMap &tm_k, const CUtensor
     }
     // Many short pairs: ranges of whole pairs need no merge kernel, whose time grows with
     // the pairs, and no segments of cut ones.  12 sequences of 91 tokens with 32 heads
-    // take 19.0 us, 24.5 in equal ranges, of 832 30.2 and 35.2; 200 sequences of 190
-    // tokens with 8 heads 64.5 and 91.8.  They cost what some CTAs' share of pairs is
+    // take 19.5 us, 26.1 in equal ranges, of 832 31.4 and 36.6; 200 sequences of 190
+    // tokens with 8 heads 67.5 and 96.9.  They cost what some CTAs' share of pairs is
     // above the mean, and with one long sequence among empty ones nearly that CTA's whole
-    // share (11 of 10 tokens and one of 832: 31.9 and 30.5).
+    // share (11 of 10 tokens and one of 832: 33.3 and 31.6).
     const long long pairs = (long long)p.B * p.Hkv, nt = p.max_pages + 1LL;
     const long long each = (pairs + p.num_ctas - 1) / p.num_ctas;
     p.whole = pairs > p.num_ctas && each * nt <= 26 + pairs / 24 &&
               (each * p.num_ctas - pairs) * nt <= (8 + pairs / 40) * p.num_ctas;
     e = cudaLaunchKernelEx(&cfg, paged_attn_kernel<D, false>, tm_k, tm_v, p);
     if (e != cudaSuccess || p.whole) return e;
-    // With more than two rounds of segments to a pair (16 pairs: 19.3 us, 20.7 with a
-    // warp to a row; 32: 17.4 and 17.4; 128: 54.8 and 42.8)
+    // With more than two rounds of segments to a pair (16 pairs: 19.5 us, 20.6 with a
+    // warp to a row; 32: 17.4 and 17.4; 128: 55.1 and 42.8)
     const bool many = pairs * 2 * kMergeLoads < p.num_ctas;
     const long long rblocks = many ? p.rows_max : (p.rows_max + kMergeWarps - 1) / kMergeWarps;
     cfg.gridDim = dim3((unsigned)(pairs * rblocks));

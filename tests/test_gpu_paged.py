@@ -609,8 +609,7 @@ def sink_case(rng, D, Hq, Hkv, Tm, P, T, gap, sinks):
     (64, 4, 4, 1, [3000], "pages", 47), (128, 2, 2, 64, [1500], "pages", 24),  # clusters
     (128, 8, 8, 2, [190] * 25, "pages", 3), (64, 32, 8, 16, [250, 128, 100, 64] * 6, "pages", 4)])  # whole pairs
 def test_attention_keeps_small_weights(D, Hq, Hkv, Tm, P, sinks, columns, gap):
-    """Thousands of keys of weight e^-gap beside one of weight 1: their share is kept as bfloat16
-    weights would keep it, each to 2^-9 of itself (the output's rounding is another 2^-9)."""
+    """Thousands of keys of weight e^-gap beside one of weight 1: their share is kept."""
     rng = np.random.default_rng(D + Hq + int(gap))
     case = list(sink_case(rng, D, Hq, Hkv, Tm, P, [Tm] * len(P), gap, sinks))
     if columns > case[4].shape[1]:
@@ -641,3 +640,15 @@ def test_a_step_without_requests():
     assert flag.item() == 0 and bool((cache.k == 7).all())
     das.das_kv_append_paged(cache, new, new, empty, dev_i32([0, 1, 1]), flag)   # a token without a slot is flagged
     assert flag.item() == 2 and bool((cache.k == 7).all())
+
+
+@pytest.mark.parametrize("gap", [10.3, 12.9, 14.1, 15.2, 15.556, 15.645])
+def test_attention_rounds_equal_small_weights(gap):
+    """As above with equal scores beside the sinks', whose weights are rounded alike: off by up to 0.6 %
+    (2^-30 of a page's sum, beside e^-15.7 of it), and the output by up to 0.4 % more."""
+    rng = np.random.default_rng(int(10 * gap))
+    case = list(sink_case(rng, 128, 8, 2, 8, [1500, 700], [8, 3], gap, "pages"))
+    used = (case[0] != 0x7F) & (ref.TABLE[case[0]][..., :1] == 0)       # all keys but the sinks
+    case[0] = np.where(used, 0, case[0])
+    run_attention(*case, where=f"equal, gap {gap}")
+    run_attention(*widen(case), where=f"equal, gap {gap}, wide table")
