@@ -404,7 +404,8 @@ size_t das_workspace_size_paged(const das_kv_cache_paged *cache, int batch, int 
  *   block_table  device int32 [batch][max_pages]; entries past a sequence's
  *                ceil(prefix_len / 64) pages are not read.  The host, which does
  *                not know the lengths, chooses how to split the work by max_pages:
- *                a table much wider than the prefixes can cost some microseconds
+ *                a table much wider than the prefixes can cost some
+ *                microseconds, with hundreds of short sequences half as much again
  *   prefix_len   device int32 [batch], 0..64 max_pages
  *   k_blk, v_blk device bf16 [batch][max_block][kv_heads][head_dim]
  * All other arguments, results and limits as das_mature_v_attention.  Bit 2

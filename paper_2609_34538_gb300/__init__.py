@@ -33,7 +33,9 @@ ABI in include/das.h:
 If libdas.so is missing the import fails: there is no fallback.  The paged-cache
 and sampling calls need the binding's module _calls.so too, which is built
 against PyTorch's headers: without it they raise ImportError, the others do not
-need it.
+need it.  Their tensors, cache and stream are to be on one GPU.  Results that a
+call allocates belong to its stream (`stream`, or the current one): a user of
+them on another stream says so with record_stream.
 """
 import ctypes
 import os

@@ -110,8 +110,9 @@ __device__ __forceinline__ Pair scan(Pair v, Pair &total, Pair (*sums)[NT / 32],
 
 // One CTA, a thread to a request.  FILL: it writes the table entries and the slots
 // too; otherwise slot_fill_kernel does, from new_len and slot_start.  Bound by
-// latency: 16 requests that grow by up to 17 tokens take 3.0 us, with the lengths,
-// the stack's pages and the stores behind one another and a barrier for each sum.
+// latency: 16 requests that grow by up to 17 tokens take 2.5 us (3.0 a call in a
+// loop), with the lengths, the stack's pages and the stores behind one another and
+// a barrier for each sum.
 template <int NT, bool FILL>
 __global__ void __launch_bounds__(NT) page_assign_kernel(const PageAssignArgs a) {
     __shared__ Pair sums[2][NT / 32];
@@ -209,7 +210,8 @@ __global__ void __launch_bounds__(NT) page_assign_kernel(const PageAssignArgs a)
 // those of new_len[b] - n; the pages taken before its own, and by all, are
 // summed up again by every CTA.  Four slots a thread share their search and mostly
 // their page.  Bound by latency: 256 requests and 1.2 million slots take 9.1 us with
-// the kernel before, of which the slots' 4.9 MB would take 0.7.
+// the kernel before (9.2 to 9.5 a call in a loop), of which the slots' 4.9 MB would
+// take 0.7.
 constexpr int kFillThreads = 256, kFillBatch = 256;
 
 __global__ void __launch_bounds__(kFillThreads) slot_fill_kernel(const PageAssignArgs a, int per_cta) {

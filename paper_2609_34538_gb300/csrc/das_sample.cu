@@ -5,7 +5,8 @@
 // equal ones by index), so each is one threshold: a key (the logit's bits made
 // monotone) and how many of the tokens equal to it, lowest index first, stay.
 // The threshold is where a sum over keys >= t first reaches a target: a sum of
-// ones for top-k, of the whole-number weights for top-p.  Nothing is sorted.
+// ones for top-k, of the whole-number weights for top-p.  The row is not sorted for
+// it; the few candidates of a small top-k are.
 //
 // sample_kernel: a cluster of CTAs holds a row in shared memory, read once.  A
 // threshold is found from a histogram of kBins bins in shared memory, over
