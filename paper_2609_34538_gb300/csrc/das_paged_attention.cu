@@ -93,8 +93,8 @@ constexpr int kPStep = 32;
 static_assert(kPCol + kGroups * kPStep == kTmemCols, "tensor memory");
 // A new reference leaves the row of the tile a sum of 2^kSumLog to twice that, which 64
 // equal weights of 2^kHead have.  The lower, the more the sums may grow before the
-// next one; the higher, the more of small weights is kept (kSumLog 6, 7, 8, 9, kHead
-// below: 54.3, 55.4, 57.7, about 60 us for 4 x 32768 tokens whose pages' scores and
+// next one; the higher, the more of small weights is kept (kSumLog 6, 7, 8, 10, kHead
+// 6 less: 54.3, 55.4, 57.7, 63.9 us for 4 x 32768 tokens whose pages' scores and
 // values differ in size by a factor of 4).
 constexpr int kSumLog = 7;
 constexpr float kHead = 1.f, kMost = 8192.f;
