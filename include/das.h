@@ -298,6 +298,51 @@ das_status das_kv_append_f8(const das_kv_cache_f8 *cache, const void *k_new, con
                             int32_t *error_flag, void *stream);
 
 /*
+ * ---- Before attention: norms and rotation -----------------------------------
+ * The paper has no counterpart (its models' layers do this in their own code).
+ */
+
+typedef enum { DAS_WEIGHTS_F32 = 0, DAS_WEIGHTS_BF16 = 1 } das_weight_type;
+
+/* bf16 rows of head_dim elements: that of head h of place i of sequence b begins at element
+ * b * batch_stride + i * token_stride + h * head_stride. */
+typedef struct {
+    const void *data;
+    long long batch_stride, token_stride, head_stride;
+} das_head_rows;
+
+/*
+ * The queries, keys and values of a block as the attention calls take them, out of a
+ * projection's rows.  With x a head's row of D elements and n = prefix_len[b] + i its
+ * position,
+ *   y = x / sqrt(mean of x^2 + eps) * weight     (queries and keys; eps < 0: y = x),
+ *   (y_a, y_c) -> (y_a cos t - y_c sin t, y_c cos t + y_a sin t),  t = n inv_freq[j],
+ * for j < rotary_dim / 2, where (a, c) is (j, j + rotary_dim / 2), or (2 j, 2 j + 1) with
+ * `interleaved`; the elements from rotary_dim on, and values, are not rotated.
+ * Computed in binary32 and rounded once, to bf16; t is reduced exactly (the product n
+ * inv_freq is not rounded to 32 bits), so far positions lose nothing.
+ *   q, k, v      any strides that are multiples of 4 elements, 8-byte aligned; v (and
+ *                v_out) may be NULL
+ *   q_weight, k_weight  device [head_dim], fp32 or bf16, or NULL for ones (with eps < 0
+ *                they are not read)
+ *   inv_freq     device fp32 [rotary_dim / 2] (NULL with rotary_dim 0); rotary_dim a
+ *                multiple of 8 from 0 to head_dim
+ *   prefix_len   device int32 [batch], or NULL for zeros; negative counts as 0
+ *   block_len    device int32 [batch], or NULL: max_block; rows i >= block_len[b] of the
+ *                outputs are left as they were
+ *   q_out        device bf16 [batch][max_block][num_q_heads][head_dim]
+ *   k_out, v_out device bf16 [batch][max_block][kv_heads][head_dim]
+ * An output may be its own input (the same address and strides), else they do not
+ * overlap.  head_dim is 64 or 128.
+ */
+das_status das_qk_norm_rope(const das_head_rows *q, const das_head_rows *k, const das_head_rows *v,
+                            int batch, int max_block, int num_q_heads, int kv_heads, int head_dim,
+                            const void *q_weight, const void *k_weight, das_weight_type weight_type,
+                            float eps, const float *inv_freq, int rotary_dim, int interleaved,
+                            const int32_t *prefix_len, const int32_t *block_len, void *q_out,
+                            void *k_out, void *v_out, void *stream);
+
+/*
  * ---- Paged cache with block scales, and sampling ----------------------------
  * The paper has no counterpart for what follows: its experiments decode one
  * sequence greedily out of one contiguous cache.
@@ -428,6 +473,75 @@ das_status das_mature_v_attention_paged(const das_kv_cache_paged *cache, int lay
                                         void *out, float *lse, void *workspace,
                                         size_t workspace_bytes, void *stream);
 
+/* Elements of a token's head that share one scale of the 4-bit cache. */
+#define DAS_SCALE_GROUP 32
+
+/*
+ * A depth-indexed cache in pages of 64 tokens, every depth held in 4 bits with a scale
+ * for every 32 elements of a token's head: 4.25 bits an element.
+ *   k        device [depths][layers][pages][kv_heads][64][head_dim / 2]: element d of a
+ *            token is in byte d / 2, the even one in its low four bits
+ *   v        device [depths][layers][pages][kv_heads][8][head_dim][4]: element d of the
+ *            page's token t is in byte (t % 8) / 2 of [t / 8][d], the even token in its
+ *            low four bits
+ *   k_scale  device bytes [depths][layers][pages][kv_heads][64][head_dim / 32]
+ *   v_scale  device bytes [depths][layers][pages][kv_heads][head_dim / 32][64]
+ *   k_unit, v_unit  device fp32 [depths][layers][kv_heads], powers of two from 2^-40 to
+ *            2^40 (of another value the power of two below counts), or NULL: 1
+ * A code c of 1 to 15 under the scale byte s stands for (c - 8) * f16(s) * unit, f16(s) the
+ * binary16 number of the bits s << 7: 4 significant bits from 2^-14 to 60 (s = 0xa7), multiples of
+ * 2^-17 below, 0 for s = 0, NaN for s = 0xff.  Other scale bytes above 0xa7 and code 0 are not
+ * written (code 0 would stand for -8).  All pointers to codes and scales are 16-byte aligned.
+ * Places of a page past its sequence's length may hold anything.
+ */
+typedef struct {
+    void *k;
+    void *v;
+    void *k_scale;
+    void *v_scale;
+    const float *k_unit;
+    const float *v_unit;
+    int depths, layers, pages, kv_heads, head_dim; /* head_dim: 64 or 128 */
+} das_kv_cache_paged4;
+
+/*
+ * Commit into a 4-bit cache: tokens, slots and errors as das_kv_append_paged.
+ * For each 32 elements x of a token's head that share a scale, with m the largest size of the
+ * finite ones / unit, the scale is m times 1 / 7 (both binary32) rounded to what a scale byte can
+ * hold (nearest, ties to even; 60 at most), and a code is 8 + x / (scale * unit) rounded to the
+ * nearest whole number, ties to even, 1 to 15 (8 under a scale of 0).  Infinities count
+ * as the largest code of their sign; a NaN among the 32 makes them all NaN (scale 0xff).
+ * Nothing but the new tokens' codes and scales is changed: a page's older tokens stay as
+ * they are, and so do its later places.
+ */
+das_status das_kv_append_paged4(const das_kv_cache_paged4 *cache, const void *k_new,
+                                const void *v_new, int batch, int W, const int32_t *slots,
+                                int max_slots, const int32_t *slot_start, int32_t *error_flag,
+                                void *stream);
+
+/* Workspace bytes for das_mature_v_attention_paged4; a workspace is zeroed before its first
+ * use. */
+size_t das_workspace_size_paged4(const das_kv_cache_paged4 *cache, int batch, int num_q_heads,
+                                 int max_block);
+
+/*
+ * das_mature_v_attention over a 4-bit cache (Eqs. 2-3 on the values that its codes and scales
+ * stand for): keys of key_depth, values of value_depth; key_depth = value_depth is the
+ * verify attention.  Arguments, results, limits and status bits as
+ * das_mature_v_attention_paged, but for the width of the table, which does not matter
+ * here, and the value scales, which need no limits.  Queries are to be finite; keys, values and weights
+ * are binary16 in the products over the cache (exact for keys and values; a weight
+ * is off by 2^-12 of itself or 2^-30 of the row's largest; a query's elements are exact down to 2^-31 of
+ * its row's largest), bf16 in those over the block's own.  Sums are in fp32.
+ */
+das_status das_mature_v_attention_paged4(const das_kv_cache_paged4 *cache, int layer, int key_depth,
+                                         int value_depth, const int32_t *block_table, int max_pages,
+                                         const int32_t *prefix_len, const int32_t *block_len,
+                                         int batch, int max_block, const void *q, const void *k_blk,
+                                         const void *v_blk, int num_q_heads, float softmax_scale,
+                                         void *out, float *lse, void *workspace,
+                                         size_t workspace_bytes, void *stream);
+
 typedef enum { DAS_LOGITS_F32 = 0, DAS_LOGITS_BF16 = 1 } das_logits_type;
 
 /* Sampling parameters, each device memory of one value per sequence, or NULL. */
@@ -483,6 +597,39 @@ das_status das_sample_accept(const void *logits, das_logits_type type, const int
                              const das_sampling *sampling, const float *uniforms,
                              int32_t *accepted, int32_t *target_ids, int32_t *next_token,
                              int32_t *committed, float *logprobs, void *stream);
+
+/*
+ * Acceptance of proposals that a drafter drew by chance: draft_ids[b][i] from
+ * draft_logits[b][i] as das_sample draws it with draft_sampling.  With e_v and R as das_sample
+ * defines them for a row and its parameters (e_v = 0 for tokens that its filters leave out),
+ * probabilities are binary32 numbers e_v * (1 / Z), Z = R / 2^32 and 1 / Z rounded to
+ * binary32; p_v are the target's and q_v the drafter's.  Proposal y at place i is accepted if
+ *   uniforms[b][i] * q_y < p_y     (in binary64; no y outside the vocabulary is),
+ * and accepted[b] counts the proposals before the first that is not.  In that one's place
+ * stands a draw from what the target has more: weights r_v = max(p_v - q_v, 0) * 2^40
+ * rounded to whole numbers, their sum S, and the least v for which those up to and
+ * including v sum to more than floor(u S), u = resample[b] (binary64, clamped to
+ * [0, 1)).  So every emitted token is a draw from the target's own (truncated)
+ * distribution.  If S = 0, which only rounding can cause, the draw is das_sample's from the
+ * target's row; a target row with no logit above -inf gives token -1.
+ *   target_logits, draft_logits  device, of one type and as das_sample's logits, each with a
+ *              row stride of its own
+ *   uniforms   device fp32 [B][W];  resample  device fp32 [B]
+ *   accepted   device int32 [B]
+ *   next_token device int32 [B]: the draw, or the last proposal if all W were accepted
+ *   committed  device int32 [B], or NULL: min(accepted + 1, W)
+ *   records    device memory of DAS_RECORD_BYTES * 2 * B * W bytes, 16-byte aligned: what the
+ *              first kernel leaves of each row for the second
+ * draft_sampling may be NULL: the target's parameters.  Limits as das_sample.
+ */
+#define DAS_RECORD_BYTES 32
+das_status das_speculative_accept(const void *target_logits, long long target_stride,
+                                  const void *draft_logits, long long draft_stride,
+                                  das_logits_type type, const int32_t *draft_ids, int B, int W,
+                                  int vocab, const das_sampling *sampling,
+                                  const das_sampling *draft_sampling, const float *uniforms,
+                                  const float *resample, int32_t *accepted, int32_t *next_token,
+                                  int32_t *committed, void *records, void *stream);
 
 /* Static text for a status code. */
 const char *das_status_string(das_status s);

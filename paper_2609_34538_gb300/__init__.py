@@ -24,6 +24,14 @@ ABI in include/das.h:
                             sampling (temperature, top-k, top-p, min-p) from
                             given random numbers, and acceptance against the
                             draws (not in the paper)
+    das_speculative_accept  acceptance of proposals that were drawn from a
+                            drafter's distribution (not in the paper)
+    PagedKVCache4, das_kv_append_paged4, das_mature_v_attention_paged4
+                            the paged cache held in 4 bits, with a scale for every
+                            32 elements of a token's head (not in the paper)
+    das_qk_norm_rope        the attention calls' q, k_blk and v_blk out of a
+                            projection's rows: norms per head, rotation by
+                            position (not in the paper)
     AttentionCall           the attention calls with arguments checked once, for
                             loops that call with the same tensors every step
     wave_widths, WaveRefinement
@@ -73,6 +81,18 @@ class das_kv_cache_paged(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
                 ("v_scale", ctypes.c_void_p), ("depths", ctypes.c_int), ("layers", ctypes.c_int),
                 ("pages", ctypes.c_int), ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int)]
+
+
+class das_kv_cache_paged4(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("k_unit", ctypes.c_void_p),
+                ("v_unit", ctypes.c_void_p), ("depths", ctypes.c_int), ("layers", ctypes.c_int),
+                ("pages", ctypes.c_int), ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int)]
+
+
+class das_head_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_longlong),
+                ("token_stride", ctypes.c_longlong), ("head_stride", ctypes.c_longlong)]
 
 
 class das_sampling(ctypes.Structure):
@@ -125,6 +145,19 @@ def _load():
     lib.das_sample.restype = i
     lib.das_sample_accept.argtypes = [p, i, p, i, i, i, ll, sp, p, p, p, p, p, p, p]
     lib.das_sample_accept.restype = i
+    cp4, hr = ctypes.POINTER(das_kv_cache_paged4), ctypes.POINTER(das_head_rows)
+    lib.das_qk_norm_rope.argtypes = [hr, hr, hr, i, i, i, i, i, p, p, i, f, p, i, i, p, p, p, p, p,
+                                     p]
+    lib.das_qk_norm_rope.restype = i
+    lib.das_kv_append_paged4.argtypes = [cp4, p, p, i, i, p, i, p, p, p]
+    lib.das_kv_append_paged4.restype = i
+    lib.das_workspace_size_paged4.argtypes = [cp4, i, i, i]
+    lib.das_workspace_size_paged4.restype = sz
+    lib.das_mature_v_attention_paged4.argtypes = [cp4, i, i, i, p, i, p, p, i, i, p, p, p, i, f, p,
+                                                  p, p, sz, p]
+    lib.das_mature_v_attention_paged4.restype = i
+    lib.das_speculative_accept.argtypes = [p, ll, p, ll, i, p, i, i, i, sp, sp, p, p, p, p, p, p, p]
+    lib.das_speculative_accept.restype = i
     lib.das_status_string.argtypes = [i]
     lib.das_status_string.restype = ctypes.c_char_p
     return lib
@@ -614,6 +647,119 @@ def das_mature_v_attention_paged(cache, layer, key_depth, value_depth, block_tab
                                         lse, softmax_scale, stream)
     if type(r) is int:
         raise DasError(r, "das_mature_v_attention_paged")
+    return r
+
+
+class PagedKVCache4:
+    """A depth-indexed cache in pages of 64 tokens, all depths in 4 bits with a scale byte for every
+    32 elements of a token's head: uint8
+        k [depths][layers][pages][kv_heads][64][head_dim / 2], k_scale [...][64][head_dim / 32],
+        v [depths][layers][pages][kv_heads][8][head_dim][4],   v_scale [...][head_dim / 32][64]
+    and, if given, k_unit and v_unit, fp32 powers of two [depths][layers][kv_heads] that the scales
+    are multiples of (None: 1).  include/das.h says what the bits stand for.  Which pages a sequence
+    has is its row of a block table (das_page_assign)."""
+
+    def __init__(self, k, v, k_scale, v_scale, k_unit=None, v_unit=None):
+        for t, name in ((k, "k"), (v, "v"), (k_scale, "k_scale"), (v_scale, "v_scale")):
+            _need(t, torch.uint8, name, 7 if name == "v" else 6)
+        R, L, N, H, page, half = k.shape
+        D = 2 * half
+        if page != PAGE_TOKENS:
+            raise ValueError(f"pages must have {PAGE_TOKENS} tokens, got {page}")
+        for t, name, shape in ((v, "v", (8, D, 4)), (k_scale, "k_scale", (PAGE_TOKENS, D // 32)),
+                               (v_scale, "v_scale", (D // 32, PAGE_TOKENS))):
+            if tuple(t.shape) != (R, L, N, H) + shape:
+                raise ValueError(f"{name} must be {(R, L, N, H) + shape}, got {tuple(t.shape)}")
+        for t, name in ((k_unit, "k_unit"), (v_unit, "v_unit")):
+            if t is not None:
+                _need(t, torch.float32, name, 3)
+                if tuple(t.shape) != (R, L, H):
+                    raise ValueError(f"{name} must be [depths][layers][kv_heads]")
+        for t, name in ((v, "v"), (k_scale, "k_scale"), (v_scale, "v_scale"), (k_unit, "k_unit"),
+                        (v_unit, "v_unit")):
+            if t is not None and t.device != k.device:
+                raise ValueError(f"{name} is on {t.device}, k on {k.device}")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.k_unit, self.v_unit = k_unit, v_unit
+        self.gpu = k.device.index
+        self.desc = das_kv_cache_paged4(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
+                                        v_scale.data_ptr(), _ptr(k_unit), _ptr(v_unit), R, L, N, H,
+                                        D)
+        self.address = ctypes.addressof(self.desc)
+        self.shape = (R, L, N, H, D)  # depths, layers, pages, kv_heads, head_dim
+
+    @classmethod
+    def empty(cls, depths, layers, pages, kv_heads, head_dim, k_unit=None, v_unit=None,
+              device="cuda"):
+        tiles = (depths, layers, pages, kv_heads)
+        make = lambda *shape: torch.empty(tiles + shape, dtype=torch.uint8, device=device)
+        return cls(make(PAGE_TOKENS, head_dim // 2), make(8, head_dim, 4),
+                   make(PAGE_TOKENS, head_dim // 32), make(head_dim // 32, PAGE_TOKENS), k_unit,
+                   v_unit)
+
+
+def das_kv_append_paged4(cache, k_new, v_new, slots, slot_start, error_flag, stream=None):
+    """Commit into a PagedKVCache4: the first slot_start[b + 1] - slot_start[b] of each
+    sequence's staged tokens, at every depth and layer, as 4-bit codes with a scale to 32 elements.
+    A page's other tokens stay as they are."""
+    _on_gpu_of(cache, k_new, "k_new")  # (the binding compares the others with it)
+    r = _calls.kv_append_paged4(cache.address, k_new, v_new, slots, slot_start, error_flag, stream)
+    if r is not None:
+        raise DasError(r, "das_kv_append_paged4")
+
+
+def new_workspace_paged4(cache, batch, num_q_heads, max_block, device=None):
+    """Zeroed workspace for das_mature_v_attention_paged4."""
+    n = int(LIB.das_workspace_size_paged4(ctypes.byref(cache.desc), batch, num_q_heads, max_block))
+    if n == 0:
+        raise DasError(DAS_ERR_UNSUPPORTED, "das_workspace_size_paged4")
+    return torch.zeros(n, dtype=torch.uint8, device=device or cache.k.device)
+
+
+def das_mature_v_attention_paged4(cache, layer, key_depth, value_depth, block_table, prefix_len,
+                                  block_len, q, k_blk, v_blk, workspace, out=None, lse=None,
+                                  softmax_scale=0.0, stream=None):
+    """das_mature_v_attention over a PagedKVCache4; key_depth = value_depth is the
+    verify attention.  Returns (out, lse)."""
+    _on_gpu_of(cache, q, "q")  # (the binding compares the others with it)
+    r = _calls.mature_v_attention_paged4(cache.address, layer, key_depth, value_depth, block_table,
+                                         prefix_len, block_len, q, k_blk, v_blk, workspace, out,
+                                         lse, softmax_scale, stream)
+    if type(r) is int:
+        raise DasError(r, "das_mature_v_attention_paged4")
+    return r
+
+
+def das_qk_norm_rope(q, k, v, inv_freq, prefix_len=None, block_len=None, q_weight=None,
+                     k_weight=None, eps=1e-6, interleaved=False, q_out=None, k_out=None, v_out=None,
+                     stream=None):
+    """The attention calls' q, k_blk and v_blk from a projection's rows, bf16 [batch][max_block]
+    [heads][head_dim] at any strides (multiples of 4; views of one projection's output): queries and
+    keys divided by their root mean square (eps None: not) and multiplied by weights [head_dim], then
+    their first 2 * len(inv_freq) elements rotated by the position prefix_len[b] + i; v (may be None)
+    copied.  Rows i >= block_len[b] of the outputs are left as they were; an output may be its
+    own input.  Returns (q_out, k_out, v_out)."""
+    r = _calls.qk_norm_rope(q, k, v, inv_freq, prefix_len, block_len, q_weight, k_weight, eps,
+                            interleaved, q_out, k_out, v_out, stream)
+    if type(r) is int:
+        raise DasError(r, "das_qk_norm_rope")
+    return r
+
+
+def das_speculative_accept(target_logits, draft_logits, draft_ids, uniforms, resample,
+                           temperature=None, top_k=None, top_p=None, min_p=None,
+                           draft_temperature=None, draft_top_k=None, draft_top_p=None,
+                           draft_min_p=None, accepted=None, next_token=None, committed=None,
+                           stream=None):
+    """Acceptance of proposals that das_sample drew from draft_logits (with the draft_ parameters; each
+    None: the target's): one is accepted with probability min(1, p / q), uniforms [B][W] deciding,
+    and the first that is not is replaced by a draw from max(p - q, 0) with resample [B].
+    committed = min(accepted + 1, W).  Returns (accepted, next_token, committed)."""
+    r = _calls.speculative_accept(target_logits, draft_logits, draft_ids, uniforms, resample,
+                                  temperature, top_k, top_p, min_p, draft_temperature, draft_top_k,
+                                  draft_top_p, draft_min_p, accepted, next_token, committed, stream)
+    if type(r) is int:
+        raise DasError(r, "das_speculative_accept")
     return r
 
 

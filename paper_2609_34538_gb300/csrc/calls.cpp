@@ -182,13 +182,14 @@ das_status without_gil(F f) {
 template <typename T>
 T *at_of(const at::Tensor &t) { return static_cast<T *>(t.data_ptr()); }
 
-const das_kv_cache_paged *cache_of(PyObject *o) {  // PagedKVCache.address
+template <typename Cache>
+const Cache *cache_of(PyObject *o) {  // PagedKVCache.address, PagedKVCache4.address
     const void *p = PyLong_AsVoidPtr(o);
     if (!p) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "no cache");
         fail();
     }
-    return static_cast<const das_kv_cache_paged *>(p);
+    return static_cast<const Cache *>(p);
 }
 
 void count_args(Py_ssize_t n, Py_ssize_t want) {
@@ -227,10 +228,11 @@ PyObject *page_assign(PyObject *, PyObject *const *a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-PyObject *kv_append_paged(PyObject *, PyObject *const *a, Py_ssize_t n) {
+template <typename Cache, auto CALL>
+PyObject *kv_append(PyObject *const *a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     count_args(n, 7);
-    const das_kv_cache_paged *cache = cache_of(a[0]);
+    const Cache *cache = cache_of<Cache>(a[0]);
     Gpu gpu;
     const at::Tensor &k = need(gpu, a[1], at::kBFloat16, "k_new", 6);
     const at::Tensor &v = need(gpu, a[2], at::kBFloat16, "v_new", 6);
@@ -244,18 +246,27 @@ PyObject *kv_append_paged(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const Stream stream(a[6], gpu);
     const int batch = to_int(B, "batch"), width = to_int(W, "W"), n_slots = to_int(slots.numel(), "slots");
     const das_status s = without_gil([&] {
-        return das_kv_append_paged(cache, k.data_ptr(), v.data_ptr(), batch, width, at_of<int32_t>(slots), n_slots,
-                                   at_of<int32_t>(start), at_of<int32_t>(flag), stream.handle);
+        return CALL(cache, k.data_ptr(), v.data_ptr(), batch, width, at_of<int32_t>(slots), n_slots,
+                    at_of<int32_t>(start), at_of<int32_t>(flag), stream.handle);
     });
     if (s != DAS_OK) return PyLong_FromLong(s);
     Py_RETURN_NONE;
     END_HANDLE_TH_ERRORS
 }
 
-PyObject *mature_v_attention_paged(PyObject *, PyObject *const *a, Py_ssize_t n) {
+PyObject *kv_append_paged(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return kv_append<das_kv_cache_paged, das_kv_append_paged>(a, n);
+}
+
+PyObject *kv_append_paged4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return kv_append<das_kv_cache_paged4, das_kv_append_paged4>(a, n);
+}
+
+template <typename Cache, auto CALL>
+PyObject *attention(PyObject *const *a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     count_args(n, 15);
-    const das_kv_cache_paged *cache = cache_of(a[0]);
+    const Cache *cache = cache_of<Cache>(a[0]);
     const int layer = int_of(a[1], "layer"), key_depth = int_of(a[2], "key_depth");
     const int value_depth = int_of(a[3], "value_depth");
     Gpu gpu;
@@ -278,51 +289,147 @@ PyObject *mature_v_attention_paged(PyObject *, PyObject *const *a, Py_ssize_t n)
     const int batch = to_int(B, "batch"), width = to_int(T, "max_block"), heads = to_int(Hq, "num_q_heads");
     const int rows = to_int(table.size(1), "max_pages");
     const das_status s = without_gil([&] {
-        return das_mature_v_attention_paged(cache, layer, key_depth, value_depth, at_of<int32_t>(table), rows,
-                                            at_of<int32_t>(prefix), at_of<int32_t>(block), batch, width, q.data_ptr(),
-                                            kb.data_ptr(), vb.data_ptr(), heads, (float)scale, out.as<>(),
-                                            lse.as<float>(), ws.data_ptr(), (size_t)ws.numel(), stream.handle);
+        return CALL(cache, layer, key_depth, value_depth, at_of<int32_t>(table), rows, at_of<int32_t>(prefix),
+                    at_of<int32_t>(block), batch, width, q.data_ptr(), kb.data_ptr(), vb.data_ptr(), heads,
+                    (float)scale, out.as<>(), lse.as<float>(), ws.data_ptr(), (size_t)ws.numel(), stream.handle);
     });
     if (s != DAS_OK) return PyLong_FromLong(s);
     return pack(out, lse);
     END_HANDLE_TH_ERRORS
 }
 
-// What the sampling calls share: logits, uniforms, temperature, top_k, top_p, min_p.
+PyObject *mature_v_attention_paged(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return attention<das_kv_cache_paged, das_mature_v_attention_paged>(a, n);
+}
+
+PyObject *mature_v_attention_paged4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return attention<das_kv_cache_paged4, das_mature_v_attention_paged4>(a, n);
+}
+
+// Rows of heads [batch][max_block][heads][head_dim] at any strides that the call takes.
+const at::Tensor &need_rows(Gpu &gpu, PyObject *o, const char *name, das_head_rows &rows) {
+    const at::Tensor &t = tensor(o, name);
+    if (t.scalar_type() != at::kBFloat16) wrong_type(o, name, type_name(at::kBFloat16));
+    gpu.check(t, name);
+    if (t.dim() != 4) {
+        THPObjectPtr got(tuple_of(t.sizes()));
+        refuse(PyExc_ValueError, "%s must have 4 dims, got %R", name, got.get());
+    }
+    if (t.stride(3) != 1) refuse(PyExc_ValueError, "%s must have contiguous rows of head_dim", name);
+    int64_t stride[3];
+    for (int i = 0; i < 3; ++i) {  // (the stride of a single one does not matter)
+        stride[i] = t.size(i) > 1 ? t.stride(i) : 0;
+        if (stride[i] % 4 != 0) refuse(PyExc_ValueError, "strides of %s must be multiples of 4", name);
+    }
+    rows = {nullptr, stride[0], stride[1], stride[2]};
+    return t;
+}
+
+PyObject *qk_norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    count_args(n, 14);
+    Gpu gpu;
+    das_head_rows rows[3] = {};
+    const char *names[3] = {"q", "k", "v"}, *outs[3] = {"q_out", "k_out", "v_out"};
+    const int parts = a[2] == Py_None ? 2 : 3;
+    const at::Tensor *in[3] = {};
+    for (int i = 0; i < parts; ++i) in[i] = &need_rows(gpu, a[i], names[i], rows[i]);
+    const int64_t B = in[0]->size(0), T = in[0]->size(1), Hq = in[0]->size(2), D = in[0]->size(3), H = in[1]->size(2);
+    for (int i = 1; i < parts; ++i)
+        if (in[i]->sizes() != at::IntArrayRef({B, T, H, D}))
+            refuse(PyExc_ValueError, "%s must be [batch][max_block][kv_heads][head_dim]", names[i]);
+    const at::Tensor &freq = need(gpu, a[3], at::kFloat, "inv_freq", 1);
+    const at::Tensor *lens[2] = {};
+    const char *len_names[2] = {"prefix_len", "block_len"};
+    for (int i = 0; i < 2; ++i)
+        if (a[4 + i] != Py_None) lens[i] = &need(gpu, a[4 + i], at::kInt, len_names[i], {B});
+    const at::Tensor *weight[2] = {};
+    const char *weight_names[2] = {"q_weight", "k_weight"};
+    ScalarType type = at::kFloat;
+    for (int i = 0; i < 2; ++i) {
+        if (a[6 + i] == Py_None) continue;
+        const ScalarType got = tensor(a[6 + i], weight_names[i]).scalar_type();
+        if (got != at::kFloat && got != at::kBFloat16) wrong_type(a[6 + i], weight_names[i], "float32 or bfloat16");
+        if (i == 1 && weight[0] && got != type) wrong_type(a[7], "k_weight", "of q_weight's type");
+        type = got;
+        weight[i] = &need(gpu, a[6 + i], type, weight_names[i], {D});
+    }
+    double eps = -1.0;
+    if (a[8] != Py_None) {
+        eps = PyFloat_AsDouble(a[8]);
+        if (eps == -1.0 && PyErr_Occurred()) fail();
+        if (!(eps >= 0.0)) refuse(PyExc_ValueError, "eps must be at least 0 (None: no norm)");
+    }
+    const int interleaved = PyObject_IsTrue(a[9]);
+    if (interleaved < 0) fail();
+    if (parts == 2 && a[12] != Py_None) refuse(PyExc_ValueError, "v_out without v");
+    Result q_out(gpu, a[10], at::kBFloat16, outs[0], {B, T, Hq, D});
+    Result k_out(gpu, a[11], at::kBFloat16, outs[1], {B, T, H, D});
+    Result v_out(gpu, a[12], at::kBFloat16, outs[2], {B, T, H, D});
+    const Stream stream(a[13], gpu);
+    q_out.ready(stream, *in[0]);
+    k_out.ready(stream, *in[0]);
+    if (parts == 3) v_out.ready(stream, *in[0]);
+    const int batch = to_int(B, "batch"), width = to_int(T, "max_block"), heads = to_int(Hq, "num_q_heads");
+    const int kv_heads = to_int(H, "kv_heads"), dim = to_int(D, "head_dim"), turned = to_int(2 * freq.numel(), "inv_freq");
+    const das_status s = without_gil([&] {
+        for (int i = 0; i < parts; ++i) rows[i].data = in[i]->data_ptr();
+        return das_qk_norm_rope(&rows[0], &rows[1], parts == 3 ? &rows[2] : nullptr, batch, width, heads, kv_heads, dim,
+                                weight[0] ? weight[0]->data_ptr() : nullptr, weight[1] ? weight[1]->data_ptr() : nullptr,
+                                type == at::kFloat ? DAS_WEIGHTS_F32 : DAS_WEIGHTS_BF16, (float)eps,
+                                turned ? at_of<float>(freq) : nullptr, turned, interleaved,
+                                lens[0] ? at_of<int32_t>(*lens[0]) : nullptr, lens[1] ? at_of<int32_t>(*lens[1]) : nullptr,
+                                q_out.as<>(), k_out.as<>(), parts == 3 ? v_out.as<>() : nullptr, stream.handle);
+    });
+    if (s != DAS_OK) return PyLong_FromLong(s);
+    if (parts == 2) v_out.object = Py_NewRef(Py_None);
+    return pack(q_out, k_out, v_out);
+    END_HANDLE_TH_ERRORS
+}
+
+// Sampling parameters of one value per sequence: temperature, top_k, top_p, min_p.
+struct Filters {
+    Filters(Gpu &gpu, PyObject *const *params, int64_t B, bool draft = false) {
+        const struct {
+            const char *name, *draft_name;
+            ScalarType type;
+        } kinds[4] = {{"temperature", "draft_temperature", at::kFloat}, {"top_k", "draft_top_k", at::kInt},
+                      {"top_p", "draft_top_p", at::kFloat}, {"min_p", "draft_min_p", at::kFloat}};
+        for (int i = 0; i < 4; ++i)
+            if (params[i] != Py_None)
+                at[i] = &need(gpu, params[i], kinds[i].type, draft ? kinds[i].draft_name : kinds[i].name, {B});
+    }
+    template <typename T>
+    const T *of(int i) const { return at[i] ? at_of<T>(*at[i]) : nullptr; }
+    das_sampling sampling() const { return {of<float>(0), of<int32_t>(1), of<float>(2), of<float>(3)}; }
+    const at::Tensor *at[4] = {};
+};
+
+// What the sampling calls share: logits, and uniforms of one value per row.
 struct Rows {
-    Rows(Gpu &gpu, PyObject *logits_o, PyObject *uniforms_o, PyObject *const *params)
-        : logits(tensor(logits_o, "logits")) {
+    Rows(Gpu &gpu, PyObject *logits_o, PyObject *uniforms_o, const char *name = "logits")
+        : logits(tensor(logits_o, name)) {
         const ScalarType type = logits.scalar_type();
-        if (type != at::kFloat && type != at::kBFloat16) wrong_type(logits_o, "logits", "float32 or bfloat16");
+        if (type != at::kFloat && type != at::kBFloat16) wrong_type(logits_o, name, "float32 or bfloat16");
         kind = type == at::kFloat ? DAS_LOGITS_F32 : DAS_LOGITS_BF16;
-        gpu.check(logits, "logits");
+        gpu.check(logits, name);
         if (logits.dim() != 3) {
             THPObjectPtr got(tuple_of(logits.sizes()));
-            refuse(PyExc_ValueError, "logits must have 3 dims, got %R", got.get());
+            refuse(PyExc_ValueError, "%s must have 3 dims, got %R", name, got.get());
         }
         B = logits.size(0);
         W = logits.size(1);
         const int64_t V = logits.size(2);
         stride = W > 1 ? logits.stride(1) : B > 1 ? logits.stride(0) : V;  // of a row: a vocabulary may be padded
         if ((V > 1 && logits.stride(2) != 1) || (B > 1 && logits.stride(0) != W * stride))
-            refuse(PyExc_ValueError, "logits must have contiguous rows at one stride");
+            refuse(PyExc_ValueError, "%s must have contiguous rows at one stride", name);
         u = &need(gpu, uniforms_o, at::kFloat, "uniforms", {B, W});
-        const struct {
-            const char *name;
-            ScalarType type;
-        } kinds[4] = {{"temperature", at::kFloat}, {"top_k", at::kInt}, {"top_p", at::kFloat}, {"min_p", at::kFloat}};
-        for (int i = 0; i < 4; ++i)
-            if (params[i] != Py_None) filters[i] = &need(gpu, params[i], kinds[i].type, kinds[i].name, {B});
         batch = to_int(B, "batch");
         width = to_int(W, "W");
         vocab = to_int(V, "vocab");
     }
-    template <typename T>
-    const T *filter(int i) const { return filters[i] ? at_of<T>(*filters[i]) : nullptr; }
     const float *uniforms() const { return at_of<float>(*u); }
-    das_sampling sampling() const { return {filter<float>(0), filter<int32_t>(1), filter<float>(2), filter<float>(3)}; }
     const at::Tensor &logits, *u;
-    const at::Tensor *filters[4] = {};
     das_logits_type kind;
     int64_t B, W, stride;
     int batch, width, vocab;
@@ -332,12 +439,13 @@ PyObject *sample(PyObject *, PyObject *const *a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     count_args(n, 9);
     Gpu gpu;
-    const Rows r(gpu, a[0], a[1], a + 2);
+    const Rows r(gpu, a[0], a[1]);
+    const Filters filters(gpu, a + 2, r.B);
     Result tokens(gpu, a[6], at::kInt, "tokens", {r.B, r.W});
     Result logprobs(gpu, a[7], at::kFloat, "logprobs", {r.B, r.W});
     const Stream stream(a[8], gpu);
     for (Result *x : {&tokens, &logprobs}) x->ready(stream, r.logits);
-    const das_sampling sampling = r.sampling();
+    const das_sampling sampling = filters.sampling();
     const das_status s = without_gil([&] {
         return das_sample(r.logits.data_ptr(), r.kind, r.batch, r.width, r.vocab, r.stride, &sampling, r.uniforms(),
                           tokens.as<int32_t>(), logprobs.as<float>(), stream.handle);
@@ -351,7 +459,8 @@ PyObject *sample_accept(PyObject *, PyObject *const *a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     count_args(n, 13);
     Gpu gpu;
-    const Rows r(gpu, a[0], a[2], a + 3);
+    const Rows r(gpu, a[0], a[2]);
+    const Filters filters(gpu, a + 3, r.B);
     const at::Tensor &draft = need(gpu, a[1], at::kInt, "draft_ids", {r.B, r.W});
     Result accepted(gpu, a[7], at::kInt, "accepted", {r.B});
     Result target(gpu, a[8], at::kInt, "target_ids", {r.B, r.W});
@@ -360,7 +469,7 @@ PyObject *sample_accept(PyObject *, PyObject *const *a, Py_ssize_t n) {
     Result logprobs(gpu, a[11], at::kFloat, "logprobs", {r.B, r.W});
     const Stream stream(a[12], gpu);
     for (Result *x : {&accepted, &target, &next, &committed, &logprobs}) x->ready(stream, r.logits);
-    const das_sampling sampling = r.sampling();
+    const das_sampling sampling = filters.sampling();
     const das_status s = without_gil([&] {
         return das_sample_accept(r.logits.data_ptr(), r.kind, at_of<int32_t>(draft), r.batch, r.width, r.vocab,
                                  r.stride, &sampling, r.uniforms(), accepted.as<int32_t>(), target.as<int32_t>(),
@@ -371,9 +480,44 @@ PyObject *sample_accept(PyObject *, PyObject *const *a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+PyObject *speculative_accept(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    count_args(n, 17);
+    Gpu gpu;
+    const Rows r(gpu, a[0], a[3], "target_logits"), d(gpu, a[1], a[3], "draft_logits");
+    if (d.kind != r.kind) wrong_type(a[1], "draft_logits", "of target_logits' type");
+    if (d.logits.sizes() != r.logits.sizes())
+        refuse(PyExc_ValueError, "draft_logits must have target_logits' shape");
+    const at::Tensor &draft = need(gpu, a[2], at::kInt, "draft_ids", {r.B, r.W});
+    const at::Tensor &again = need(gpu, a[4], at::kFloat, "resample", {r.B});
+    const Filters filters(gpu, a + 5, r.B), draft_filters(gpu, a + 9, r.B, true);
+    Result accepted(gpu, a[13], at::kInt, "accepted", {r.B});
+    Result next(gpu, a[14], at::kInt, "next_token", {r.B});
+    Result committed(gpu, a[15], at::kInt, "committed", {r.B});
+    Result records(gpu, Py_None, at::kByte, "records", {2 * DAS_RECORD_BYTES * r.B * r.W});
+    const Stream stream(a[16], gpu);
+    for (Result *x : {&accepted, &next, &committed, &records}) x->ready(stream, r.logits);
+    const das_sampling sampling = filters.sampling();
+    das_sampling draft_sampling = draft_filters.sampling();
+    if (!draft_sampling.temperature) draft_sampling.temperature = sampling.temperature;
+    if (!draft_sampling.top_k) draft_sampling.top_k = sampling.top_k;
+    if (!draft_sampling.top_p) draft_sampling.top_p = sampling.top_p;
+    if (!draft_sampling.min_p) draft_sampling.min_p = sampling.min_p;
+    const das_status s = without_gil([&] {
+        return das_speculative_accept(r.logits.data_ptr(), r.stride, d.logits.data_ptr(), d.stride, r.kind,
+                                      at_of<int32_t>(draft), r.batch, r.width, r.vocab, &sampling, &draft_sampling,
+                                      r.uniforms(), at_of<float>(again), accepted.as<int32_t>(), next.as<int32_t>(),
+                                      committed.as<int32_t>(), records.as<>(), stream.handle);
+    });
+    if (s != DAS_OK) return PyLong_FromLong(s);
+    return pack(accepted, next, committed);
+    END_HANDLE_TH_ERRORS
+}
+
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(page_assign), METHOD(kv_append_paged), METHOD(mature_v_attention_paged),
-                         METHOD(sample), METHOD(sample_accept), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(kv_append_paged4), METHOD(mature_v_attention_paged4), METHOD(qk_norm_rope),
+                         METHOD(sample), METHOD(sample_accept), METHOD(speculative_accept), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -362,6 +362,84 @@ das_status attention_paged(const das_kv_cache_paged *c, int layer, int key_depth
                : DAS_ERR_CUDA;
 }
 
+bool cache_paged4_ok(const das_kv_cache_paged4 *c) {
+    return c && c->k && c->v && c->k_scale && c->v_scale && c->depths >= 1 && c->depths <= 63 &&
+           c->layers >= 1 && c->layers <= (1 << 20) && c->pages >= 1 && c->pages < (1 << 25) &&
+           c->kv_heads >= 1 && c->kv_heads <= (1 << 20) &&
+           (c->head_dim == 64 || c->head_dim == 128) && aligned16(c->k) && aligned16(c->v) &&
+           aligned16(c->k_scale) && aligned16(c->v_scale);
+}
+
+das_status attention_paged4(const das_kv_cache_paged4 *c, int layer, int key_depth, int value_depth,
+                            const int32_t *block_table, int max_pages, const int32_t *prefix_len,
+                            const int32_t *block_len, int batch, int max_block, const void *q,
+                            const void *k_blk, const void *v_blk, int num_q_heads,
+                            float softmax_scale, void *out, float *lse, void *workspace,
+                            size_t workspace_bytes, void *stream) {
+    if (c && c->head_dim != 64 && c->head_dim != 128) return DAS_ERR_UNSUPPORTED;
+    if (!cache_paged4_ok(c) || layer < 0 || layer >= c->layers || key_depth < 1 ||
+        key_depth > c->depths || value_depth < 1 || value_depth > c->depths || !block_table ||
+        max_pages < 1 || max_pages >= (1 << 25) || !prefix_len || !block_len || batch < 1 || !q ||
+        !k_blk || !v_blk || !out || !lse || num_q_heads < 1 || max_block < 1 ||
+        num_q_heads % c->kv_heads != 0 || !aligned16(q) || !aligned16(k_blk) ||
+        !aligned16(v_blk) || !aligned16(out) || !isfinite(softmax_scale))
+        return DAS_ERR_INVALID_ARG;
+    const int G = num_q_heads / c->kv_heads;
+    if (max_block > kTileKeys || (long long)G * max_block > kMaxRows || batch > (1 << 20) ||
+        (long long)batch * c->kv_heads * G * max_block > 0x7fffffffLL ||
+        (long long)c->pages * c->kv_heads > 0x7fffffffLL ||
+        // tiles of one CTA, if every table is full, are counted in 32 bits
+        (double)batch * c->kv_heads * (max_pages + 1.0) > 64.0 * (1 << 30))
+        return DAS_ERR_UNSUPPORTED;
+    const size_t need = das_workspace_size_paged4(c, batch, num_q_heads, max_block);
+    if (need == 0) return DAS_ERR_CUDA;
+    if (!workspace || workspace_bytes < need ||
+        (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
+        return DAS_ERR_WORKSPACE;
+    const size_t slab_tiles = (size_t)c->pages * c->kv_heads;
+    const size_t tile_codes = (size_t)DAS_PAGE_TOKENS * c->head_dim / 2;
+    const size_t tile_scales = (size_t)DAS_PAGE_TOKENS * c->head_dim / DAS_SCALE_GROUP;
+    const size_t ks = (size_t)(key_depth - 1) * c->layers + layer;
+    const size_t vs = (size_t)(value_depth - 1) * c->layers + layer;
+    Paged4AttnParams p = {};
+    p.k = static_cast<const uint8_t *>(c->k) + ks * slab_tiles * tile_codes;
+    p.v = static_cast<const uint8_t *>(c->v) + vs * slab_tiles * tile_codes;
+    p.k_scale = static_cast<const uint8_t *>(c->k_scale) + ks * slab_tiles * tile_scales;
+    p.v_scale = static_cast<const uint8_t *>(c->v_scale) + vs * slab_tiles * tile_scales;
+    p.k_unit = c->k_unit ? c->k_unit + ks * c->kv_heads : nullptr;
+    p.v_unit = c->v_unit ? c->v_unit + vs * c->kv_heads : nullptr;
+    p.table = block_table;
+    p.prefix_len = prefix_len;
+    p.block_len = block_len;
+    p.q = static_cast<const uint16_t *>(q);
+    p.k_blk = static_cast<const uint16_t *>(k_blk);
+    p.v_blk = static_cast<const uint16_t *>(v_blk);
+    p.out = static_cast<uint16_t *>(out);
+    p.lse = lse;
+    p.B = batch;
+    p.Hq = num_q_heads;
+    p.Hkv = c->kv_heads;
+    p.G = G;
+    p.max_block = max_block;
+    p.rows_max = G * max_block;
+    p.max_pages = max_pages;
+    p.pages = c->pages;
+    const double scale =
+        softmax_scale > 0.f ? (double)softmax_scale : 1.0 / sqrt((double)c->head_dim);
+    p.scale_log2 = (float)(scale * 1.4426950408889634);
+    return paged4_attn_launch(p, c->head_dim, workspace, static_cast<cudaStream_t>(stream)) ==
+                   cudaSuccess
+               ? DAS_OK
+               : DAS_ERR_CUDA;
+}
+
+// 8-byte aligned rows at strides of whole groups of four elements
+bool rows_ok(const das_head_rows *r) {
+    return r->data && reinterpret_cast<uintptr_t>(r->data) % 8 == 0 && r->batch_stride % 4 == 0 &&
+           r->token_stride % 4 == 0 && r->head_stride % 4 == 0;
+}
+bool aligned8(const void *p) { return reinterpret_cast<uintptr_t>(p) % 8 == 0; }
+
 }  // namespace
 }  // namespace das
 
@@ -564,6 +642,129 @@ das_status das_sample_accept(const void *logits, das_logits_type type, const int
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     return das::sample_accept_launch(a, draft_ids, accepted, next_token, committed, st) ==
                    cudaSuccess
+               ? DAS_OK
+               : DAS_ERR_CUDA;
+}
+
+das_status das_qk_norm_rope(const das_head_rows *q, const das_head_rows *k, const das_head_rows *v,
+                            int batch, int max_block, int num_q_heads, int kv_heads, int head_dim,
+                            const void *q_weight, const void *k_weight, das_weight_type weight_type,
+                            float eps, const float *inv_freq, int rotary_dim, int interleaved,
+                            const int32_t *prefix_len, const int32_t *block_len, void *q_out,
+                            void *k_out, void *v_out, void *stream) {
+    if (batch < 0 || max_block < 1 || num_q_heads < 1 || kv_heads < 1 || !q || !k ||
+        (batch > 0 && (v != nullptr) != (v_out != nullptr)) || eps != eps || rotary_dim < 0 || rotary_dim % 8 != 0 ||
+        rotary_dim > head_dim || (rotary_dim > 0 && !inv_freq) ||
+        (weight_type != DAS_WEIGHTS_F32 && weight_type != DAS_WEIGHTS_BF16))
+        return DAS_ERR_INVALID_ARG;
+    if (head_dim != 64 && head_dim != 128) return DAS_ERR_UNSUPPORTED;
+    const uintptr_t wide = weight_type == DAS_WEIGHTS_BF16 ? 8 : 16;
+    if (reinterpret_cast<uintptr_t>(q_weight) % wide || reinterpret_cast<uintptr_t>(k_weight) % wide)
+        return DAS_ERR_INVALID_ARG;
+    if (batch > 0 && (!das::rows_ok(q) || !das::rows_ok(k) || (v && !das::rows_ok(v)) || !q_out ||
+                      !k_out || !das::aligned8(q_out) || !das::aligned8(k_out) || !das::aligned8(v_out)))
+        return DAS_ERR_INVALID_ARG;
+    const long long heads = (long long)num_q_heads + 2LL * kv_heads;
+    if (heads > (1 << 20) || (double)batch * max_block * heads > 2147483647.0) return DAS_ERR_UNSUPPORTED;
+    const das::RopeArgs a = {{*q, *k, v ? *v : das_head_rows{}},
+                             {q_out, k_out, v_out},
+                             {q_weight, k_weight},
+                             weight_type == DAS_WEIGHTS_BF16,
+                             interleaved != 0,
+                             eps,
+                             inv_freq,
+                             rotary_dim,
+                             prefix_len,
+                             block_len,
+                             batch,
+                             max_block,
+                             num_q_heads,
+                             kv_heads};
+    return das::rope_launch(a, head_dim, static_cast<cudaStream_t>(stream)) == cudaSuccess
+               ? DAS_OK
+               : DAS_ERR_CUDA;
+}
+
+das_status das_kv_append_paged4(const das_kv_cache_paged4 *cache, const void *k_new,
+                                const void *v_new, int batch, int W, const int32_t *slots,
+                                int max_slots, const int32_t *slot_start, int32_t *error_flag,
+                                void *stream) {
+    if (cache && cache->head_dim != 64 && cache->head_dim != 128) return DAS_ERR_UNSUPPORTED;
+    if (!das::cache_paged4_ok(cache) || (batch > 0 && (!k_new || !v_new)) || batch < 0 || W < 1 ||
+        (max_slots > 0 && !slots) || max_slots < 0 || !slot_start || !error_flag ||
+        !das::aligned16(k_new) || !das::aligned16(v_new))
+        return DAS_ERR_INVALID_ARG;
+    const long long pieces = ((long long)W + 2 * DAS_PAGE_TOKENS - 2) / DAS_PAGE_TOKENS;
+    if (W > (1 << 24) || pieces * cache->depths * cache->layers > 0x7fffffffLL / 2 ||
+        (double)pieces * cache->depths * cache->layers * batch * cache->kv_heads * 2 > 2147483647.0)
+        return DAS_ERR_UNSUPPORTED;
+    return das::append_paged4_launch(*cache, k_new, v_new, batch, W, slots, max_slots, slot_start,
+                                     error_flag, static_cast<cudaStream_t>(stream)) == cudaSuccess
+               ? DAS_OK
+               : DAS_ERR_CUDA;
+}
+
+size_t das_workspace_size_paged4(const das_kv_cache_paged4 *cache, int batch, int num_q_heads,
+                                 int max_block) {
+    if (!cache || cache->kv_heads < 1 || batch < 1 || batch > (1 << 20) || num_q_heads < 1 ||
+        num_q_heads % cache->kv_heads != 0 || max_block < 1 ||
+        (cache->head_dim != 64 && cache->head_dim != 128))
+        return 0;
+    const int G = num_q_heads / cache->kv_heads;
+    if (max_block > das::kTileKeys || (long long)G * max_block > das::kMaxRows) return 0;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    return das::paged4_workspace_bytes(dev, batch, cache->kv_heads, G * max_block, cache->head_dim);
+}
+
+das_status das_mature_v_attention_paged4(const das_kv_cache_paged4 *cache, int layer, int key_depth,
+                                         int value_depth, const int32_t *block_table, int max_pages,
+                                         const int32_t *prefix_len, const int32_t *block_len,
+                                         int batch, int max_block, const void *q, const void *k_blk,
+                                         const void *v_blk, int num_q_heads, float softmax_scale,
+                                         void *out, float *lse, void *workspace,
+                                         size_t workspace_bytes, void *stream) {
+    return das::attention_paged4(cache, layer, key_depth, value_depth, block_table, max_pages,
+                                 prefix_len, block_len, batch, max_block, q, k_blk, v_blk,
+                                 num_q_heads, softmax_scale, out, lse, workspace, workspace_bytes,
+                                 stream);
+}
+
+das_status das_speculative_accept(const void *target_logits, long long target_stride,
+                                  const void *draft_logits, long long draft_stride,
+                                  das_logits_type type, const int32_t *draft_ids, int B, int W,
+                                  int vocab, const das_sampling *sampling,
+                                  const das_sampling *draft_sampling, const float *uniforms,
+                                  const float *resample, int32_t *accepted, int32_t *next_token,
+                                  int32_t *committed, void *records, void *stream) {
+    das::SpeculateArgs a = {};
+    a.rows.logits = target_logits;
+    a.rows.bf16 = type == DAS_LOGITS_BF16;
+    a.rows.B = B;
+    a.rows.W = W;
+    a.rows.vocab = vocab;
+    a.rows.row_stride = target_stride;
+    a.rows.sampling = sampling ? *sampling : das_sampling{};
+    a.rows.second = draft_logits;
+    a.rows.second_stride = draft_stride;
+    a.rows.second_sampling = draft_sampling ? *draft_sampling : a.rows.sampling;
+    a.rows.records = static_cast<das::RowRecord *>(records);
+    a.draft = draft_ids;
+    a.uniforms = uniforms;
+    a.resample = resample;
+    a.accepted = accepted;
+    a.next_token = next_token;
+    a.committed = committed;
+    const uintptr_t elem = type == DAS_LOGITS_BF16 ? 2 : 4;
+    if ((type != DAS_LOGITS_F32 && type != DAS_LOGITS_BF16) || B < 0 || W < 1 || W > 1024 ||
+        vocab < 1 || target_stride < vocab || draft_stride < vocab ||
+        (long long)B * W > 0x7fffffffLL / 16 ||
+        reinterpret_cast<uintptr_t>(target_logits) % elem != 0 ||
+        reinterpret_cast<uintptr_t>(draft_logits) % elem != 0 || !das::aligned16(records) ||
+        (B > 0 && (!target_logits || !draft_logits || !draft_ids || !uniforms || !resample ||
+                   !accepted || !next_token || !records)))
+        return DAS_ERR_INVALID_ARG;
+    return das::speculative_accept_launch(a, static_cast<cudaStream_t>(stream)) == cudaSuccess
                ? DAS_OK
                : DAS_ERR_CUDA;
 }

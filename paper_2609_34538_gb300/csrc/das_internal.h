@@ -124,6 +124,41 @@ size_t paged_workspace_bytes(int device, int batch, int kv_heads, int rows_max, 
 cudaError_t paged_attn_launch(PagedAttnParams &p, int head_dim, const CUtensorMap &tm_k,
                               const CUtensorMap &tm_v, void *workspace, cudaStream_t stream);
 
+cudaError_t append_paged4_launch(const das_kv_cache_paged4 &c, const void *k_new, const void *v_new,
+                                 int batch, int W, const int32_t *slots, int max_slots,
+                                 const int32_t *slot_start, int32_t *error_flag,
+                                 cudaStream_t stream);
+
+struct Paged4AttnParams {
+    const uint8_t *k, *v;                 // the slabs read, as in das_kv_cache_paged4
+    const uint8_t *k_scale, *v_scale;
+    const float *k_unit, *v_unit;         // [Hkv], or null
+    const int32_t *table;                 // [B][max_pages]
+    const int32_t *prefix_len, *block_len;
+    const uint16_t *q, *k_blk, *v_blk;    // bf16
+    uint16_t *out;
+    float *lse;
+    int32_t *status;
+    int B, Hq, Hkv, G, max_block, rows_max, max_pages, pages;
+    float scale_log2;
+};
+size_t paged4_workspace_bytes(int device, int batch, int kv_heads, int rows_max, int head_dim);
+cudaError_t paged4_attn_launch(Paged4AttnParams &p, int head_dim, void *workspace,
+                               cudaStream_t stream);
+
+struct RopeArgs {
+    das_head_rows in[3];                  // queries, keys, values (no data: none)
+    void *out[3];
+    const void *weight[2];
+    bool weights_bf16, interleaved;
+    float eps;
+    const float *inv_freq;
+    int rotary_dim;
+    const int32_t *prefix_len, *block_len;
+    int batch, max_block, num_q_heads, kv_heads;
+};
+cudaError_t rope_launch(const RopeArgs &a, int head_dim, cudaStream_t stream);
+
 struct SampleArgs {
     const void *logits;
     bool bf16;
@@ -136,7 +171,31 @@ struct SampleArgs {
     // with draft set (W = 1 only) the sampling kernel accepts too
     const int32_t *draft;
     int32_t *accepted, *next_token, *committed;
+    // of rows past B * W, with `second` set: another B * W rows of its own parameters
+    const void *second;
+    long long second_stride;
+    das_sampling second_sampling;
+    struct RowRecord *records;  // with it set rows are recorded and nothing is drawn
 };
+// What a row's filters leave: the tokens of a larger key than `key` and those of the key up to
+// index `last`, of e >= `floor`; top is the largest logit's key (0: no logit above -inf), total the
+// sum of the kept weights.
+struct alignas(16) RowRecord {
+    uint32_t top, key;
+    int32_t last;
+    float T;
+    float floor;
+    uint32_t unused;
+    unsigned long long total;
+};
+static_assert(sizeof(RowRecord) == DAS_RECORD_BYTES, "records");
+struct SpeculateArgs {
+    SampleArgs rows;            // the target's, second: the drafter's
+    const int32_t *draft;
+    const float *uniforms, *resample;
+    int32_t *accepted, *next_token, *committed;
+};
+cudaError_t speculative_accept_launch(const SpeculateArgs &a, cudaStream_t stream);
 cudaError_t sample_launch(const SampleArgs &a, cudaStream_t stream);
 // sampling, and acceptance of draft ids against the tokens (= target_ids)
 cudaError_t sample_accept_launch(SampleArgs a, const int32_t *draft, int32_t *accepted,

@@ -1,0 +1,170 @@
+// das_rope.cu -- norms of queries and keys per head, their rotation by position, and the
+// copy of values, from a projection's rows into the attention calls' tensors.
+//
+// A warp takes one token's heads, or a part of them.  D / 8 lanes have a head's row, a
+// lane 8 of its elements: the two elements of every rotated pair are the same lane's, so
+// rows need no exchange but the sum of squares, and any output may overwrite its
+// input.  The angle n f_j is taken in turns as a 64-bit fraction: n times f_j / (2 pi)
+// modulo 1 is an integer product whose overflow is what is not wanted.  The lane's
+// four angles serve all of the token's heads; lanes of two heads share their work.
+//
+// Bound by memory, reads and writes of 2 bytes an element each.
+#include <algorithm>
+
+#include "das_internal.h"
+
+namespace das {
+namespace {
+
+constexpr uint32_t kFull = 0xffffffffu;
+constexpr int kWarps = 4;
+
+struct RopeParams {
+    RopeArgs a;
+    int heads, part, parts;  // all heads of a token, of one warp, warps to a token
+};
+
+__device__ __forceinline__ void unpack(uint2 u, float *x) {
+    x[0] = __uint_as_float(u.x << 16);
+    x[1] = __uint_as_float(u.x & 0xffff0000u);
+    x[2] = __uint_as_float(u.y << 16);
+    x[3] = __uint_as_float(u.y & 0xffff0000u);
+}
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ void weights(const void *w, bool bf16, int unit, float *x) {
+    if (!w) {
+        x[0] = x[1] = x[2] = x[3] = 1.f;
+    } else if (bf16) {
+        unpack(__ldg(static_cast<const uint2 *>(w) + unit), x);
+    } else {
+        const float4 f = __ldg(static_cast<const float4 *>(w) + unit);
+        x[0] = f.x;
+        x[1] = f.y;
+        x[2] = f.z;
+        x[3] = f.w;
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kWarps * 32) rope_kernel(const RopeParams p) {
+    constexpr int kLanes = D / 8, kRows = 32 / kLanes;  // lanes to a head, heads at once
+    const RopeArgs &a = p.a;
+    const int lane = threadIdx.x & 31, l = lane % kLanes, r = lane / kLanes;
+    const long long item = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const int part = (int)(item % p.parts);
+    const long long token = item / p.parts;
+    const int i = (int)(token % a.max_block);
+    const long long b = token / a.max_block;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (b >= a.batch || (a.block_len && i >= a.block_len[b])) return;
+
+    // the lane's two units of four elements
+    const int rd8 = a.rotary_dim / 8;
+    const bool turned = l < rd8;
+    const int u0 = a.interleaved ? 2 * l : turned ? l : 2 * l, u1 = a.interleaved || !turned ? 2 * l + 1 : l + rd8;
+    float cs[4], sn[4];
+    {
+        const unsigned long long n = (a.prefix_len ? max(a.prefix_len[b], 0) : 0) + (long long)i;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            cs[j] = 1.f;
+            sn[j] = 0.f;
+            if (!turned) continue;
+            double t = (double)a.inv_freq[4 * l + j] * 0.15915494309189535;  // 1 / (2 pi)
+            t -= floor(t);
+            const unsigned long long f = t < 1.0 ? (unsigned long long)(t * 18446744073709551616.0) : 0;
+            const float x = (float)(int)(n * f >> 32) * 4.656612873077393e-10f;  // half turns, 2^-31
+            sincospif(x, &sn[j], &cs[j]);
+        }
+    }
+    const int end = min(p.heads, (part + 1) * p.part);
+    for (int h0 = part * p.part; h0 < end; h0 += kRows) {
+        const int h = h0 + r;
+        const bool live = h < end;
+        const int kind = h < a.num_q_heads ? 0 : h < a.num_q_heads + a.kv_heads ? 1 : 2;
+        const int at = kind == 0 ? h : h - a.num_q_heads - (kind == 2 ? a.kv_heads : 0);
+        const das_head_rows &src = a.in[kind];
+        uint2 x0 = make_uint2(0, 0), x1 = x0;
+        if (live) {
+            const uint16_t *row = static_cast<const uint16_t *>(src.data) + b * src.batch_stride +
+                                  i * src.token_stride + at * src.head_stride;
+            x0 = *reinterpret_cast<const uint2 *>(row + 4 * u0);
+            x1 = *reinterpret_cast<const uint2 *>(row + 4 * u1);
+        }
+        float y[8];
+        unpack(x0, y);
+        unpack(x1, y + 4);
+        if (a.eps >= 0.f) {
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum += y[j] * y[j];
+#pragma unroll
+            for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor_sync(kFull, sum, d);
+            const float f = rsqrtf(sum * (1.f / D) + a.eps);
+            if (kind < 2) {
+                float w[8];
+                weights(a.weight[kind], a.weights_bf16, u0, w);
+                weights(a.weight[kind], a.weights_bf16, u1, w + 4);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = y[j] * f * w[j];
+            }
+        }
+        if (!live) continue;
+        if (kind < 2) {
+            float z[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                // pair j: elements j of both units, or 2 j and 2 j + 1 of the eight
+                const float s = a.interleaved ? y[2 * j] : y[j], t = a.interleaved ? y[2 * j + 1] : y[j + 4];
+                const float zs = s * cs[j] - t * sn[j], zt = t * cs[j] + s * sn[j];
+                z[j] = zs;
+                z[j + 4] = zt;
+            }
+            if (a.interleaved) {
+                x0 = make_uint2(pack(z[0], z[4]), pack(z[1], z[5]));
+                x1 = make_uint2(pack(z[2], z[6]), pack(z[3], z[7]));
+            } else {
+                x0 = make_uint2(pack(z[0], z[1]), pack(z[2], z[3]));
+                x1 = make_uint2(pack(z[4], z[5]), pack(z[6], z[7]));
+            }
+        }
+        uint16_t *row = static_cast<uint16_t *>(a.out[kind]) +
+                        ((b * a.max_block + i) * (kind ? a.kv_heads : a.num_q_heads) + at) * D;
+        *reinterpret_cast<uint2 *>(row + 4 * u0) = x0;
+        *reinterpret_cast<uint2 *>(row + 4 * u1) = x1;
+    }
+}
+
+}  // namespace
+
+cudaError_t rope_launch(const RopeArgs &a, int head_dim, cudaStream_t stream) {
+    RopeParams p = {};
+    p.a = a;
+    p.heads = a.num_q_heads + a.kv_heads * (a.in[2].data ? 2 : 1);
+    const long long tokens = (long long)a.batch * a.max_block;
+    if (tokens == 0) return cudaSuccess;
+    const int rows = 256 / head_dim;  // heads that a warp takes at once
+    // as many warps to a token as fill the GPU, each with whole steps
+    p.part = p.heads;
+    while (p.part > rows && tokens * ((p.heads + p.part - 1) / p.part) < 152 * 32) p.part = (p.part / 2 + rows - 1) / rows * rows;
+    p.parts = (p.heads + p.part - 1) / p.part;
+    const long long ctas = (tokens * p.parts + kWarps - 1) / kWarps;
+    if (ctas > 0x7fffffffLL) return cudaErrorInvalidValue;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(kWarps * 32);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, head_dim == 128 ? rope_kernel<128> : rope_kernel<64>, p);
+}
+
+}  // namespace das

@@ -118,6 +118,24 @@ struct alignas(16) Shared {
     u64 above, target, sum, equal;
 };
 
+// Where a row comes from: of two sets of rows, if rows are recorded.
+struct Source {
+    const void *logits;
+    size_t row;
+    long long stride;
+    const das_sampling *sampling;
+    int b;
+};
+template <bool RECORD>
+__device__ __forceinline__ Source source_of(const SampleArgs &a, size_t row) {
+    if constexpr (RECORD) {
+        const size_t rows = (size_t)a.B * a.W;
+        if (row >= rows)
+            return {a.second, row - rows, a.second_stride, &a.second_sampling, (int)((row - rows) / a.W)};
+    }
+    return {a.logits, row, a.row_stride, &a.sampling, (int)(row / a.W)};
+}
+
 // With one proposal a sequence its acceptance needs no other row.
 __device__ __forceinline__ void accept_one(const SampleArgs &a, size_t row, int token) {
     if (!a.draft) return;
@@ -132,7 +150,9 @@ __device__ __noinline__ float plain_e(float l, float m, float T) { return expf((
 
 __device__ __forceinline__ u64 wide(uint32_t w) { return (u64)w + (w == kOne); }
 
-template <bool BF16>
+// With RECORD rows are not drawn from: what their filters leave is recorded, of the rows of
+// a.logits and then of a.second.
+template <bool BF16, bool RECORD>
 __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a, int slice) {
     __shared__ Shared s;
     extern __shared__ uint4 held[];  // the CTA's logits in groups of four, padded with -inf
@@ -140,7 +160,9 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
     const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const size_t row = blockIdx.x / C;
-    const int b = (int)(row / a.W);
+    const Source from_row = source_of<RECORD>(a, row);
+    const int b = from_row.b;
+    const das_sampling &sampling = *from_row.sampling;
     auto of = [&](int r) { return C > 1 ? cluster.map_shared_rank(&s, r) : &s; };
     auto sync = [&] {  // the cluster's threads, or the CTA's
         if (C > 1) cluster.sync();
@@ -190,10 +212,10 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    float T = a.sampling.temperature ? a.sampling.temperature[b] : 1.f;
-    long long k = a.sampling.top_k ? a.sampling.top_k[b] : 0;
-    const float p = a.sampling.top_p ? a.sampling.top_p[b] : 1.f;
-    float floor_p = a.sampling.min_p ? a.sampling.min_p[b] : 0.f;
+    float T = sampling.temperature ? sampling.temperature[b] : 1.f;
+    long long k = sampling.top_k ? sampling.top_k[b] : 0;
+    const float p = sampling.top_p ? sampling.top_p[b] : 1.f;
+    float floor_p = sampling.min_p ? sampling.min_p[b] : 0.f;
     floor_p = floor_p > 0.f ? fminf(floor_p, 1.f) : 0.f;  // NaN: none
     if (!(T > 0.f)) {
         T = 1.f;
@@ -221,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
     // `shift` of group 0, and index `base` + 4 g + i - shift is token i of group g.
     using Elem = std::conditional_t<BF16, uint16_t, float>;
     const int base = rank * slice, len = max(0, min(slice, a.vocab - base));
-    const Elem *src = static_cast<const Elem *>(a.logits) + row * (size_t)a.row_stride + base;
+    const Elem *src = static_cast<const Elem *>(from_row.logits) + from_row.row * (size_t)from_row.stride + base;
     const int shift = (int)(reinterpret_cast<uintptr_t>(src) / sizeof(Elem) & 3);
     int groups = len ? (len + shift + 3) / 4 : 0;
     bool few = false;  // whether the candidates alone are left
@@ -344,16 +366,27 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
         }
         if (most <= kKeyNone) {  // the same in every CTA
             if (rank == 0 && tid == 0) {
-                accept_one(a, row, -1);
-                a.tokens[row] = -1;
-                if (a.logprobs) a.logprobs[row] = -INFINITY;
+                if constexpr (RECORD) {
+                    a.records[row] = RowRecord{};
+                } else {
+                    accept_one(a, row, -1);
+                    a.tokens[row] = -1;
+                    if (a.logprobs) a.logprobs[row] = -INFINITY;
+                }
             }
             return;
         }
         m = logit_of(most);
         low = logit_of(max(least, kKeyNone + 1));
     }
-    if (m == INFINITY) {  // the infinite ones alone have weight, and the same
+    const bool infinite = m == INFINITY;
+    const uint32_t top = key_of(m);
+    // (a key of the row that stands in shared memory is one of the row, but for the infinite logits')
+    auto record = [&](uint32_t cut, int last, u64 total) {
+        if (infinite && cut == key_of(0.f)) cut = top;
+        a.records[row] = RowRecord{top, cut, last, T, floor_p, 0u, total};
+    };
+    if (infinite) {  // the infinite ones alone have weight, and the same
         for (int g = tid; g < groups; g += kThreads) {
             float l[4];
             load4(g, l);
@@ -416,6 +449,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
                     if ((x < y) == (!(tid & size) == !(tid & d))) x = y;
                 }
         const bool mine_in = tid < n && tid < k;
+        bool in = mine_in;
         const int at = kThreads - 1 - (int)(uint32_t)x;  // its place in s.cand
         float e[4] = {};
         uint32_t code = 0;
@@ -432,9 +466,21 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
                 s.target = want < 1.0 ? 1 : (u64)want;
             }
             __syncthreads();
-            if (before >= min(s.target, all)) code = 0;
+            if (before >= min(s.target, all)) {
+                code = 0;
+                in = false;
+            }
         }
+        in = in && (floor_p <= 0.f || e[0] >= floor_p);
         if (floor_p > 0.f && !(e[0] >= floor_p)) code = 0;
+        if constexpr (RECORD) {
+            // what is kept is the first of the sorted ones, though the last may have no weight
+            u64 total;
+            scan(wide(code), total);
+            const int n_kept = __syncthreads_count(in);
+            if (tid == n_kept - 1) record((uint32_t)(x >> 32), s.cand_at[at], total);
+            return;
+        }
         __syncthreads();  // (the last reads of `there`)
         if (tid < n) s.hist[at] = code;
         __syncthreads();
@@ -990,6 +1036,34 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
             total += s.xch[t][0][r];
         }
     }
+    if constexpr (RECORD) {
+        // the last kept one of those equal to the cut
+        if (!part) {
+            if (rank == 0 && tid == 0) record(cut, ties ? 0x7fffffff : -1, total);
+            return;
+        }
+        if (tid == 0) s.where = -1;
+        __syncthreads();
+        const u64 n = tid < segs ? s.n_seg[tid] : 0;
+        if (ties_before < ties && ties <= ties_before + n) {
+            s.where = tid;
+            s.equal = ties_before;
+        }
+        __syncthreads();
+        if (s.where < 0 || warp != 0) return;  // (in another CTA of the cluster)
+        const int g = s.where * 32 + lane;
+        float l[4];
+        load4(g, l);
+        uint32_t n_here = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n_here += l[i] == at_cut;
+        u64 place = s.equal + warp_scan(n_here) - n_here;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (l[i] == at_cut && ++place == ties)
+                record(cut, few ? s.cand_at[4 * g + i] : base + 4 * g + i - shift, total);
+        return;
+    }
     if (tid == 0) {
         float u = a.uniforms[row];
         if (!(u >= 0.f)) u = 0.f;
@@ -1046,7 +1120,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
 // bf16): one CTA per row, which reads the row (from L2 at best) for every step.
 // Kept simple, and slow: 5.1 ms for one row of 400,009 where a cluster takes 44 us
 // for 360,000.
-template <bool BF16>
+template <bool BF16, bool RECORD>
 __global__ void __launch_bounds__(kLongThreads) long_row_kernel(const SampleArgs a) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -1056,16 +1130,18 @@ __global__ void __launch_bounds__(kLongThreads) long_row_kernel(const SampleArgs
     __shared__ int s_bin;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const size_t row = blockIdx.x;
-    const int b = (int)(row / a.W), V = a.vocab;
+    const Source src = source_of<RECORD>(a, row);
+    const das_sampling &sampling = *src.sampling;
+    const int b = src.b, V = a.vocab;
     auto key = [&](int i) {
-        const size_t at = row * a.row_stride + i;
-        return key_of(BF16 ? __uint_as_float((uint32_t)static_cast<const uint16_t *>(a.logits)[at] << 16)
-                           : static_cast<const float *>(a.logits)[at]);
+        const size_t at = src.row * src.stride + i;
+        return key_of(BF16 ? __uint_as_float((uint32_t)static_cast<const uint16_t *>(src.logits)[at] << 16)
+                           : static_cast<const float *>(src.logits)[at]);
     };
-    float T = a.sampling.temperature ? a.sampling.temperature[b] : 1.f;
-    long long k = a.sampling.top_k ? a.sampling.top_k[b] : 0;
-    const float p = a.sampling.top_p ? a.sampling.top_p[b] : 1.f;
-    float floor_p = a.sampling.min_p ? a.sampling.min_p[b] : 0.f;
+    float T = sampling.temperature ? sampling.temperature[b] : 1.f;
+    long long k = sampling.top_k ? sampling.top_k[b] : 0;
+    const float p = sampling.top_p ? sampling.top_p[b] : 1.f;
+    float floor_p = sampling.min_p ? sampling.min_p[b] : 0.f;
     floor_p = floor_p > 0.f ? fminf(floor_p, 1.f) : 0.f;  // NaN: none
     if (!(T > 0.f)) {
         T = 1.f;
@@ -1081,9 +1157,13 @@ __global__ void __launch_bounds__(kLongThreads) long_row_kernel(const SampleArgs
         (uint32_t)block_reduce<u64>(mine, sums, [](u64 x, u64 y) { return x > y ? x : y; });
     if (top <= kKeyNone) {
         if (tid == 0) {
-            accept_one(a, row, -1);
-            a.tokens[row] = -1;
-            if (a.logprobs) a.logprobs[row] = -INFINITY;
+            if constexpr (RECORD) {
+                a.records[row] = RowRecord{};
+            } else {
+                accept_one(a, row, -1);
+                a.tokens[row] = -1;
+                if (a.logprobs) a.logprobs[row] = -INFINITY;
+            }
         }
         return;
     }
@@ -1186,6 +1266,10 @@ __global__ void __launch_bounds__(kLongThreads) long_row_kernel(const SampleArgs
     u64 total = 0;
     for (int i = tid; i < V; i += kLongThreads) total += kept(i);
     total = block_reduce<u64>(total, sums, add);
+    if constexpr (RECORD) {
+        if (tid == 0) a.records[row] = RowRecord{top, cut, last, T, floor_p, 0u, total};
+        return;
+    }
     float u = a.uniforms[row];
     if (!(u >= 0.f)) u = 0.f;
     u64 r = (u64)((double)u * (double)total);
@@ -1254,6 +1338,134 @@ __global__ void __launch_bounds__(kScanWarps * 32)
     }
 }
 
+// ---- proposals that were drawn by chance -------------------------------------------
+// From the rows' records: the first proposal that is refused, and the draw in its place from
+// what the target's row has more.  A cluster to a sequence; each of its warps has a run of
+// the row, whose sum says whether the draw is in it, and goes over its run again if so.
+struct RowProbs {
+    RowRecord r;
+    const void *logits;
+    size_t at;
+    float m, inv;
+    bool bf16;
+    __device__ __forceinline__ RowProbs(const SampleArgs &a, size_t row, bool second) {
+        const size_t rows = (size_t)a.B * a.W;
+        r = a.records[second ? rows + row : row];
+        logits = second ? a.second : a.logits;
+        at = row * (size_t)(second ? a.second_stride : a.row_stride);
+        bf16 = a.bf16;
+        m = logit_of(r.top);
+        inv = 1.f / (float)((double)r.total * (1.0 / 4294967296.0));
+    }
+    __device__ __forceinline__ float e(int v) const {  // 0: left out
+        if (r.top == 0) return 0.f;
+        const uint32_t x = key_of(bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t *>(logits)[at + v] << 16)
+                                       : static_cast<const float *>(logits)[at + v]);
+        if (x < r.key || (x == r.key && v > r.last)) return 0.f;
+        const float y = e_of(x, r.top, m, r.T);
+        return r.floor > 0.f && !(y >= r.floor) ? 0.f : y;
+    }
+    __device__ __forceinline__ float p(int v) const {
+        const float y = e(v);
+        return y > 0.f ? y * inv : 0.f;
+    }
+};
+
+__global__ void __launch_bounds__(kThreads, 1) speculative_accept_kernel(const SpeculateArgs a) {
+    __shared__ u64 s_sum[kWarps], s_cta[2][kMaxRowCtas];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int W = a.rows.W, V = a.rows.vocab;
+    const size_t b = blockIdx.x / C;
+    auto sync = [&] {
+        if (C > 1) cluster.sync();
+        else __syncthreads();
+    };
+    sync();  // every CTA of the cluster has started
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    bool refused = false;
+    if (tid < W) {  // (W <= 1024 = kThreads)
+        const int y = a.draft[b * W + tid];
+        refused = true;
+        if (y >= 0 && y < V) {
+            const float p = RowProbs(a.rows, b * W + tid, false).p(y), q = RowProbs(a.rows, b * W + tid, true).p(y);
+            refused = !((double)a.uniforms[b * W + tid] * (double)q < (double)p);
+        }
+    }
+    const unsigned some = __ballot_sync(kFull, refused);
+    if (lane == 0) s_sum[warp] = some ? warp * 32 + __ffs(some) - 1 : 0x7fffffff;
+    __syncthreads();
+    const int first = (int)min(__reduce_min_sync(kFull, (uint32_t)s_sum[lane]), (uint32_t)W);
+    __syncthreads();
+    if (rank == 0 && tid == 0) {
+        a.accepted[b] = first;
+        if (a.committed) a.committed[b] = min(first + 1, W);
+        if (first == W) a.next_token[b] = a.draft[b * W + W - 1];
+    }
+    if (first == W) return;  // the same in the whole cluster
+
+    const RowProbs p(a.rows, b * W + first, false), q(a.rows, b * W + first, true);
+    const long long run = ((long long)V + C * kWarps * 128 - 1) / (C * kWarps * 128) * 128;
+    const long long lo = min((long long)V, (rank * kWarps + warp) * run), hi = min((long long)V, lo + run);
+    auto own = [&](int v) { return w_of(p.e(v)); };
+    auto rest = [&](int v) { return __float2ull_rn(fmaxf(p.p(v) - q.p(v), 0.f) * 1099511627776.f); };
+    u64 total = 0, mine = 0, before = 0;
+    bool plain = false;  // rounding has left nothing: the target's own weights
+    for (int turn = 0; turn < 2; ++turn) {
+        mine = 0;
+#pragma unroll 4
+        for (long long v = lo + lane; v < hi; v += 32) mine += plain ? own((int)v) : rest((int)v);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(kFull, mine, d);
+        if (lane == 0) s_sum[warp] = mine;
+        __syncthreads();
+        u64 cta = s_sum[lane], up = lane < warp ? cta : 0;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+            cta += __shfl_xor_sync(kFull, cta, d);
+            up += __shfl_xor_sync(kFull, up, d);
+        }
+        if (tid < C) {
+            u64(*to)[kMaxRowCtas] = C > 1 ? cluster.map_shared_rank(s_cta, tid) : s_cta;
+            to[turn][rank] = cta;
+        }
+        sync();
+        total = 0;
+        before = up;
+        for (int r = 0; r < C; ++r) {
+            if (r < rank) before += s_cta[turn][r];
+            total += s_cta[turn][r];
+        }
+        if (total > 0) break;
+        plain = true;
+    }
+    if (total == 0) {
+        if (rank == 0 && tid == 0) a.next_token[b] = -1;
+        return;
+    }
+    float u = a.resample[b];
+    if (!(u >= 0.f)) u = 0.f;
+    u64 r = (u64)((double)u * (double)total);
+    r = r < total ? r : total - 1;
+    if (r < before || r >= before + mine) return;
+    for (long long v0 = lo; v0 < hi; v0 += 32) {
+        const long long v = v0 + lane;
+        const u64 w = v < hi ? (plain ? own((int)v) : rest((int)v)) : 0;
+        u64 x = w;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const u64 o = __shfl_up_sync(kFull, x, d);
+            if (lane >= d) x += o;
+        }
+        x += before;
+        if (r >= x - w && r < x) a.next_token[b] = (int)v;
+        before = __shfl_sync(kFull, x, 31);
+        if (before > r) break;
+    }
+}
+
 template <typename... Params, typename... Args>
 cudaError_t launch_pdl(void (*kernel)(Params...), dim3 grid, dim3 block, unsigned cluster,
                        size_t smem, cudaStream_t stream, Args... args) {
@@ -1274,9 +1486,9 @@ cudaError_t launch_pdl(void (*kernel)(Params...), dim3 grid, dim3 block, unsigne
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
 }
 
-template <bool BF16>
+template <bool BF16, bool RECORD>
 cudaError_t sample_launch_t(const SampleArgs &a, cudaStream_t stream) {
-    const long long rows = (long long)a.B * a.W;
+    const long long rows = (long long)a.B * a.W * (RECORD ? 2 : 1);
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
@@ -1286,7 +1498,7 @@ cudaError_t sample_launch_t(const SampleArgs &a, cudaStream_t stream) {
     constexpr int kMaxSlice = kSliceBytes<BF16> / (BF16 ? 2 : 4) - 4;  // (with the shift of a first group)
     const int hold = (int)(((long long)a.vocab + kMaxSlice - 1) / kMaxSlice);
     if (hold > kMaxRowCtas)
-        return launch_pdl(long_row_kernel<BF16>, dim3((unsigned)rows), dim3(kLongThreads), 1, 0,
+        return launch_pdl(long_row_kernel<BF16, RECORD>, dim3((unsigned)rows), dim3(kLongThreads), 1, 0,
                           stream, a);
     int C = 1;  // a power of two: the bins divide by it
     while (C < kMaxRowCtas && (C < hold || (rows * C * 2 <= sms && a.vocab > C * 4 * kThreads)))
@@ -1297,19 +1509,29 @@ cudaError_t sample_launch_t(const SampleArgs &a, cudaStream_t stream) {
     if (C > 1) smem = std::max(smem, 2 * kBins * sizeof(uint32_t));  // (bins may be sent there)
     static std::atomic<bool> configured[64];  // the shared-memory opt-in, once per device
     if (dev >= 64 || !configured[dev].load(std::memory_order_acquire)) {
-        e = cudaFuncSetAttribute(sample_kernel<BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        e = cudaFuncSetAttribute(sample_kernel<BF16, RECORD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                  kSliceBytes<BF16>);
         if (e != cudaSuccess) return e;
         if (dev < 64) configured[dev].store(true, std::memory_order_release);
     }
-    return launch_pdl(sample_kernel<BF16>, grid, block, C, smem, stream, a, slice);
+    return launch_pdl(sample_kernel<BF16, RECORD>, grid, block, C, smem, stream, a, slice);
 }
 
 }  // namespace
 
 cudaError_t sample_launch(const SampleArgs &a, cudaStream_t stream) {
     if ((long long)a.B * a.W == 0) return cudaSuccess;
-    return a.bf16 ? sample_launch_t<true>(a, stream) : sample_launch_t<false>(a, stream);
+    return a.bf16 ? sample_launch_t<true, false>(a, stream) : sample_launch_t<false, false>(a, stream);
+}
+
+cudaError_t speculative_accept_launch(const SpeculateArgs &a, cudaStream_t stream) {
+    if (a.rows.B == 0) return cudaSuccess;
+    const cudaError_t e = a.rows.bf16 ? sample_launch_t<true, true>(a.rows, stream)
+                                      : sample_launch_t<false, true>(a.rows, stream);
+    if (e != cudaSuccess) return e;
+    int C = 1;
+    while (C < kMaxRowCtas && a.rows.vocab > C * 4 * kThreads) C *= 2;
+    return launch_pdl(speculative_accept_kernel, dim3((unsigned)(a.rows.B * C)), dim3(kThreads), C, 0, stream, a);
 }
 
 cudaError_t sample_accept_launch(SampleArgs a, const int32_t *draft, int32_t *accepted,

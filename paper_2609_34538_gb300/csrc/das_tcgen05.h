@@ -49,7 +49,7 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
 // Bounded wait; false after 2 s or once another thread of the CTA gave up.
 // The first try, which mostly succeeds or is woken, is all that is inlined:
 // the single-warp roles run at the pace of their instruction fetches.
-__device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int *abort_flag,
+static __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int *abort_flag,
                                        int32_t *status) {
     const unsigned long long t0 = globaltimer();
     for (uint32_t it = 1;; ++it) {
@@ -69,7 +69,7 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int
     return mbar_try_wait(bar, parity) || wait_slow(bar, parity, abort_flag, status);
 }
 // On the abort path only: at most 20 ms for copies in flight to land.
-__device__ __noinline__ void drain_wait(uint32_t bar, uint32_t parity) {
+static __device__ __noinline__ void drain_wait(uint32_t bar, uint32_t parity) {
     const unsigned long long t0 = globaltimer();
     while (!mbar_try_wait(bar, parity) && globaltimer() - t0 < 20000000ull) {
     }

@@ -1,0 +1,413 @@
+"""The commit into the 4-bit cache and attention over it, against plain references in 64 bits
+(tests/paged4_ref.py)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_34538_gb300 as das
+from tests import paged4_ref as ref
+from tests.gpu_util import assert_close, dev_i32
+
+pytestmark = pytest.mark.gpu
+PAGE, GROUP = 64, 32
+
+
+def bf16(x):
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).to(torch.bfloat16).cuda()
+
+
+def f64(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+def u8(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(torch.uint8).cuda()
+
+
+def f32(a):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).cuda()
+
+
+def host(cache):
+    return [t.cpu().numpy() for t in (cache.k, cache.k_scale, cache.v, cache.v_scale)]
+
+
+# ---- commit -----------------------------------------------------------------------
+
+def append_case(rng, R, L, H, D, first, n, W, N):
+    z = lambda *s: rng.integers(0, 256, (R, L, N, H) + s).astype(np.uint8)
+    old = [z(PAGE, D // 2), z(PAGE, D // GROUP), z(8, D, 4), z(D // GROUP, PAGE)]
+    units = [2.0 ** rng.integers(-3, 4, (R, L, H)) for _ in range(2)]
+    B = len(n)
+    x = rng.normal(0, 1, (2, R, L, B, W, H, D)) * 2.0 ** rng.integers(-4, 5, (2, R, L, B, W, H, 1))
+    ids, slots, start = list(rng.permutation(N)), [], [0]
+    for b in range(B):
+        pg = [ids.pop() for _ in range(-(-(first[b] + n[b]) // PAGE))]
+        slots += [pg[(first[b] + j) // PAGE] * PAGE + (first[b] + j) % PAGE for j in range(n[b])]
+        start.append(len(slots))
+    return old, units, x, slots, start
+
+
+def run_append(old, units, x, slots, start, repeat=1):
+    cache = das.PagedKVCache4(u8(old[0]), u8(old[2]), u8(old[1]), u8(old[3]), *(u if u is None else f32(u) for u in units))
+    flag = dev_i32([0])
+    k, v = bf16(x[0]), bf16(x[1])
+    for _ in range(repeat):
+        das.das_kv_append_paged4(cache, k, v, dev_i32(slots if len(slots) else [0]), dev_i32(start), flag)
+    return cache, f64(k), f64(v), flag.item()
+
+
+def same(cache, want):
+    k, ks, v, vs = want
+    return all(np.array_equal(a, b) for a, b in zip(host(cache), (k, ks, v, vs)))
+
+
+@pytest.mark.parametrize("repeat", [1, 2])
+@pytest.mark.parametrize("R,L,H,D,first,n,W", [
+    (1, 1, 1, 64, [0], [1], 1), (1, 1, 1, 128, [63], [1], 1), (2, 2, 3, 64, [5], [16], 16),
+    (3, 1, 2, 128, [63, 0, 32], [1, 64, 33], 64), (1, 2, 8, 128, [10, 62], [200, 3], 201),
+    (2, 1, 1, 128, [1, 0, 7], [0, 5, 0], 9), (1, 1, 5, 64, [33], [95], 95), (1, 1, 2, 64, [7, 8, 9], [2, 7, 8], 12)])
+def test_append_codes_and_scales(R, L, H, D, first, n, W, repeat):
+    rng = np.random.default_rng(D + W + H)
+    old, units, x, slots, start = append_case(rng, R, L, H, D, first, n, W, 12)
+    cache, k, v, flag = run_append(old, units, x, slots, start, repeat)
+    assert same(cache, ref.append(*old, *units, k, v, slots, start)) and flag == 0
+
+
+def test_append_extreme_values():
+    rng = np.random.default_rng(3)
+    old, units, x, slots, start = append_case(rng, 1, 1, 9, 64, [9], [20], 20, 2)
+    for y in x:
+        y[..., 0, :] *= 0.0
+        y[..., 1, :] *= 2.0 ** 100
+        y[..., 2, :] *= 2.0 ** -60
+        y[..., 3, 5] = np.inf
+        y[..., 4, 6] = np.nan
+        y[..., 5, :] = 7.0
+        y[..., 6, :] = np.sign(y[..., 6, :]) * np.inf
+        y[..., 7, :32] = np.nan
+        y[..., 8, :] = 2.0 ** -17 * 3.5 * rng.integers(-2, 3, y[..., 8, :].shape)   # at the least scales, and at ties
+    for u in (units, [None, None], [np.full((1, 1, 9), 2.0 ** 40), np.full((1, 1, 9), 2.0 ** -40)]):
+        cache, k, v, flag = run_append(old, u, x, slots, start)
+        one = np.ones((1, 1, 9))
+        want = ref.append(*old, *(one if t is None else t for t in u), k, v, slots, start)
+        assert same(cache, want) and flag == 0
+
+
+def test_append_ties_of_scales_and_codes():
+    """Every bf16 significand as a group's largest, and multiples of half a step."""
+    rng = np.random.default_rng(4)
+    old, _, x, slots, start = append_case(rng, 1, 1, 4, 128, [0], [64], 64, 1)
+    largest = (128 + np.arange(512) % 128) / 128.0 * 2.0 ** ((np.arange(512) // 128) - 2)
+    x[0] = rng.uniform(-1, 1, x[0].shape)
+    x[0].reshape(-1, 32)[:, 0] = 1.0
+    x[0].reshape(-1, 32)[:] *= np.resize(largest, x[0].size // 32)[:, None]
+    x[1] = rng.integers(-14, 15, x[1].shape) / 2.0        # ties, with the largest 7 or less
+    cache, k, v, _ = run_append(old, [None, None], x, slots, start)
+    one = np.ones((1, 1, 4))
+    assert same(cache, ref.append(*old, one, one, k, v, slots, start))
+
+
+def test_append_leaves_what_it_refuses():
+    rng = np.random.default_rng(5)
+    old, units, x, slots, start = append_case(rng, 1, 1, 2, 64, [60, 0, 0, 0], [8, 4, 4, 4], 8, 8)
+    slots = list(slots)
+    slots[start[0] + 4] += 1                               # a second page that does not start at its first place
+    slots[start[1]:start[2]] = [-1] * 4                    # no place
+    slots[start[2]:start[3]] = [8 * PAGE + i for i in range(4)]  # a page past the pool
+    cache, k, v, flag = run_append(old, units, x, slots, start)
+    want = ref.append(*old, *units, k[:, :, :1], v[:, :, :1], slots[:4], [0, 4])
+    want = ref.append(*want, *units, k[:, :, 3:], v[:, :, 3:], slots[start[3]:], [0, 4])
+    assert flag == 2 and same(cache, want)
+    for bad in ([0, 9, 9, 9, 9], [0, 0, 0, 0, 999], [4, 2, 2, 2, 2], [-3, -1, 0, 0, 0]):
+        cache, k, v, flag = run_append(old, units, x, slots, bad)
+        assert flag == 2 and same(cache, old)
+
+
+# ---- attention --------------------------------------------------------------------
+
+def attention_case(rng, D, Hq, Hkv, Tm, P, T, rows=None, poison=True):
+    """Two depths: keys read at depth 1, values at depth 2; what no call may use reads as NaN."""
+    B = len(P)
+    need = [-(-p // PAGE) for p in P]
+    rows = max(1, max(need)) if rows is None else rows
+    N = sum(need) + 2
+    ids = rng.permutation(N)
+    table = np.full((B, rows), -1)
+    at, used = 0, np.zeros((N, PAGE), bool)
+    for b in range(B):
+        table[b, :need[b]] = ids[at:at + need[b]]
+        for t in range(need[b]):
+            used[table[b, t], :min(PAGE, P[b] - t * PAGE)] = True
+        at += need[b]
+    c = lambda *s: np.clip(np.rint(rng.normal(0, 2.6, (N, Hkv) + s)), -7, 7) + 8
+    pack = lambda *s: (c(*s).astype(np.uint8) | c(*s).astype(np.uint8) << 4).astype(np.uint8)
+    k, v = pack(PAGE, D // 2), pack(8, D, 4)
+    ks, vs = (rng.integers(100, 117, (N, Hkv) + s).astype(np.uint8) for s in ((PAGE, D // GROUP), (D // GROUP, PAGE)))
+    if poison:
+        ks[np.broadcast_to(~used[:, None, :, None], ks.shape)] = 0xff
+        vs[np.broadcast_to(~used[:, None, None, :], vs.shape)] = 0xff
+    ku, vu = (2.0 ** rng.integers(-2, 2, Hkv) for _ in range(2))
+    f = lambda *s: rng.normal(0, 1, s)
+    q, kb, vb = f(B, Tm, Hq, D), f(B, Tm, Hkv, D), f(B, Tm, Hkv, D)
+    if poison:
+        for b in range(B):
+            q[b, T[b]:], kb[b, T[b]:], vb[b, T[b]:] = np.nan, np.nan, np.nan
+    return dict(k=k, ks=ks, v=v, vs=vs, ku=ku, vu=vu, table=table, P=np.array(P), T=np.array(T), q=q, kb=kb, vb=vb)
+
+
+def cache_of(c):
+    two = lambda a, first, other: u8(np.stack([a, np.full_like(a, other)] if first else [np.full_like(a, other), a])[:, None])
+    unit = lambda a, first: f32(np.stack([a, a * 8] if first else [a * 8, a])[:, None])
+    return das.PagedKVCache4(two(c["k"], True, 0), two(c["v"], False, 0), two(c["ks"], True, 0xff),
+                             two(c["vs"], False, 0xff), unit(c["ku"], True), unit(c["vu"], False))
+
+
+def reference(c, q, kb, vb, P, T, scale=None, masked=()):
+    with np.errstate(invalid="ignore"):
+        K, V = ref.keys(c["k"], c["ks"], c["ku"]), ref.values(c["v"], c["vs"], c["vu"])
+    return ref.attention(K, V, c["table"], P, T, q, kb, vb, scale=scale, masked=masked)
+
+
+def run_attention(c, scale=0.0, stream=None, status=0, masked=(), where="", repeat=1):
+    cache = cache_of(c)
+    B, Tm, Hq, D = c["q"].shape
+    ws = das.new_workspace_paged4(cache, B, Hq, Tm)
+    qd, kbd, vbd = (bf16(c[n]) for n in ("q", "kb", "vb"))
+    torch.cuda.synchronize()
+    for _ in range(repeat):
+        out, lse = das.das_mature_v_attention_paged4(cache, 0, 1, 2, dev_i32(c["table"]), dev_i32(c["P"]),
+                                                     dev_i32(c["T"]), qd, kbd, vbd, ws, softmax_scale=scale,
+                                                     stream=stream)
+    torch.cuda.synchronize()
+    assert das.workspace_status(ws) == status
+    Pc, Tc = np.clip(c["P"], 0, c["table"].shape[1] * PAGE), np.clip(c["T"], 0, Tm)
+    o, l = reference(c, f64(qd), f64(kbd), f64(vbd), Pc, Tc, scale=scale or None, masked=masked)
+    assert_close(f64(out), o, lse.cpu().numpy(), l, where=where)
+    for b in range(B):
+        assert not out[b, Tc[b]:].any() and torch.isneginf(lse[b, :, Tc[b]:]).all()
+    return out, lse
+
+
+SHAPES = [  # D, Hq, Hkv, max_block, prefix lengths, block lengths
+    (64, 4, 4, 4, [256], [4]), (64, 1, 1, 1, [0], [1]), (64, 1, 1, 1, [1], [1]), (128, 1, 1, 1, [63], [1]),
+    (128, 2, 2, 1, [64, 65], [1, 1]), (128, 8, 2, 16, [127, 0, 128], [16, 3, 0]), (128, 5, 1, 12, [1000], [11]),
+    (64, 10, 2, 12, [129, 700], [12, 1]), (128, 32, 8, 8, [300, 64, 1, 449], [8, 7, 1, 0]),
+    (128, 1, 1, 64, [190], [64]), (64, 8, 1, 8, [4097], [8]), (128, 32, 32, 1, [513], [1]),
+    (128, 4, 4, 16, [2000, 5], [16, 16]), (128, 6, 2, 9, [320] * 5, [9, 8, 7, 6, 5]),
+    (128, 4, 2, 16, [0] * 40, list(range(16)) * 2 + [16] * 8), (64, 2, 1, 32, list(range(0, 99, 3)), [32] * 33),
+    (128, 16, 4, 4, [640, 64, 1], [4, 4, 4]), (128, 3, 1, 21, [777], [20]), (64, 64, 1, 1, [130, 3], [1, 0]),
+    (128, 4, 1, 4, [12000], [4]), (64, 8, 1, 5, [9000, 130], [5, 2]), (128, 32, 8, 2, [190] * 60, [2] * 60)]
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=[str(s)[:60] for s in SHAPES])
+def test_attention_matches_64_bits(shape):
+    D, Hq, Hkv, Tm, P, T = shape
+    rng = np.random.default_rng(D + Hq + Tm + len(P))
+    run_attention(attention_case(rng, D, Hq, Hkv, Tm, P, T), where=str(shape)[:60], repeat=2)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Tm", [1, 7, 16])
+def test_attention_sharp_and_rising_scores(D, Tm):
+    """Maxima that keep moving along the prefix, weights of one key near 1."""
+    rng = np.random.default_rng(D + Tm)
+    c = attention_case(rng, D, 4, 2, Tm, [1500, 700], [Tm, max(1, Tm - 1)])
+    keep = c["ks"].copy()
+    for b in range(2):                                      # scores grow page by page
+        for t in range(-(-int(c["P"][b]) // PAGE)):
+            pg = c["table"][b, t]
+            c["ks"][pg] = np.where(keep[pg] == 0xff, 0xff, 8 * (9 + min(t, 6)))
+    run_attention(c, scale=0.5, where="rising")
+    c["ks"] = np.where(keep == 0xff, 0xff, 8 * 14).astype(np.uint8)
+    run_attention(c, scale=1.0, where="sharp")
+
+
+def test_attention_one_dominant_key_among_thousands():
+    """What thousands of keys add beside one of 16 nats more is kept: the dominant key has no values, so that
+    the output is the others' alone.  With weights w_j = 2^x_j, the largest 2^9 or more, off by 2^-25 at most where
+    they are below 2^-14: 4000 others of e^-16 2^9 = 2^-14.1 each are off by 2^-11 of themselves."""
+    rng = np.random.default_rng(18)
+    for gap in (12.0, 16.0):
+        D = 64
+        c = attention_case(rng, D, 2, 1, 2, [4000], [2], poison=False)
+        q = np.zeros((1, 2, 2, D))
+        q[..., 0] = 1.0
+        c["q"], c["kb"], c["vb"] = q, np.zeros_like(c["kb"]), np.zeros_like(c["vb"])
+        c["kb"][..., 0] = -1000.0                             # the block's own keys have no weight
+        c["ku"], c["vu"] = np.ones(1), np.ones(1)
+        c["k"][:], c["ks"][:] = 0x88, 8 * 15                   # scores 0 but for one key, scale 1
+        pg = c["table"][0, 7]
+        c["k"][pg, 0, 5, 0] = 8 + 4 | 8 << 4                   # 4 in element 0
+        c["v"][pg, 0, 0, :, 2] = c["v"][pg, 0, 0, :, 2] & 0x0f | 8 << 4   # token 5's values are 0
+        cache = cache_of(c)
+        ws = das.new_workspace_paged4(cache, 1, 2, 2)
+        out, lse = das.das_mature_v_attention_paged4(cache, 0, 1, 2, dev_i32(c["table"]), dev_i32([4000]), dev_i32([2]),
+                                                     bf16(c["q"]), bf16(c["kb"]), bf16(c["vb"]), ws,
+                                                     softmax_scale=gap / 4)
+        o, l = reference(c, c["q"], c["kb"], c["vb"], [4000], [2], scale=gap / 4)
+        # a bf16 output's half step, and 2^-10 for the weights
+        assert np.abs(f64(out) - o).max() <= np.abs(o).max() * (2.0 ** -8 + 2.0 ** -10)
+        assert np.abs(lse.cpu().numpy() - l).max() <= 1e-5 * np.abs(l).max()
+
+
+def test_attention_scales_far_apart():
+    """Scales from 2^-14 to 60 in one sequence, groups of zeros, queries whose rows differ by 2^40 in size."""
+    rng = np.random.default_rng(8)
+    c = attention_case(rng, 128, 4, 1, 8, [64 * 12 + 5], [8])
+    pages = c["table"][0]
+    for a, lo in (("ks", 30), ("vs", 0)):
+        for i, pg in enumerate(pages[:12]):
+            c[a][pg] = lo + 7 * (i % 12)
+    c["vs"][pages[3]] = 0
+    c["ks"][pages[5]] = 0
+    run_attention(c, where="scales")
+    c["q"][0, 3] *= 2.0 ** -40
+    c["q"][0, 5] *= 2.0 ** 3
+    run_attention(c, where="queries")
+
+
+def test_attention_units():
+    rng = np.random.default_rng(9)
+    c = attention_case(rng, 64, 2, 2, 2, [100, 64], [0, 2])
+    c["vu"] = np.array([2.0 ** -40, 2.0 ** -38])
+    c["vb"] = c["vb"] * 2.0 ** -40
+    run_attention(c, where="small values")
+    c = attention_case(rng, 64, 2, 2, 2, [100, 164], [1, 2])
+    c["ku"] = np.array([2.0 ** 3, 2.0 ** -30])
+    c["vb"][:] = 0
+    c["vu"] = np.array([2.0 ** -1, 2.0 ** -2])
+    run_attention(c, scale=0.05, where="key units")
+
+
+def test_attention_entries_that_are_no_pages_are_masked_and_flagged():
+    rng = np.random.default_rng(10)
+    for P in ([300, 200], [3000, 64]):
+        c = attention_case(rng, 128, 4, 2, 4, P, [4, 4])
+        c["table"][0, 2], c["table"][1, 0] = -1, 10 ** 9
+        run_attention(c, status=4, masked={(0, 2), (1, 0)}, where="bad pages")
+    c = attention_case(rng, 64, 2, 2, 1, [64, 100], [1, 1])
+    c["table"][:] = -7                                      # the block alone is left
+    run_attention(c, status=4, masked={(0, 0), (1, 0), (1, 1)}, where="no pages")
+
+
+def test_attention_rows_without_keys():
+    """No prefix and no block: nothing is seen."""
+    rng = np.random.default_rng(11)
+    c = attention_case(rng, 64, 4, 2, 3, [0, 70, 0], [0, 0, 2])
+    run_attention(c, where="no keys")
+
+
+def test_attention_nan_stays_with_its_rows():
+    """A group that reads as NaN makes the rows that see it NaN, keys lse too, and no others."""
+    rng = np.random.default_rng(15)
+    for prefix in (70, 1500, 20000):
+        for which in ("ks", "vs"):
+            c = attention_case(rng, 64, 4, 2, 3, [prefix, 90], [3, 2], poison=False)
+            at = (c["table"][0, 1], 1, 2, 1) if which == "ks" else (c["table"][0, 1], 1, 1, 2)
+            c[which][at] = 0xff                               # sequence 0, kv head 1
+            cache = cache_of(c)
+            ws = das.new_workspace_paged4(cache, 2, 4, 3)
+            out, lse = das.das_mature_v_attention_paged4(cache, 0, 1, 2, dev_i32(c["table"]), dev_i32(c["P"]),
+                                                         dev_i32(c["T"]), bf16(c["q"]), bf16(c["kb"]), bf16(c["vb"]), ws)
+            out, lse = f64(out), lse.cpu().numpy()
+            bad = np.zeros(out.shape, bool)
+            bad[0, :3, 2:, slice(None) if which == "ks" else slice(32, 64)] = True
+            assert np.isnan(out[bad]).all() and np.isfinite(out[~bad]).all()
+            assert np.isfinite(lse[1, :, :2]).all() and np.isfinite(lse[0, :2]).all()
+            assert np.isnan(lse[0, 2:]).all() if which == "ks" else np.isfinite(lse[0, 2:]).all()
+            assert das.workspace_status(ws) == 0
+
+
+def test_attention_lengths_that_change_between_calls():
+    """Calls in a row on one workspace, each with lengths that the one before it did not have."""
+    rng = np.random.default_rng(16)
+    c = attention_case(rng, 128, 4, 2, 4, [2000, 900, 64], [4, 4, 4], poison=False)
+    cache = cache_of(c)
+    ws = das.new_workspace_paged4(cache, 3, 4, 4)
+    q, kb, vb = (bf16(c[n]) for n in ("q", "kb", "vb"))
+    table, P, T = dev_i32(c["table"]), dev_i32([0, 0, 0]), dev_i32([0, 0, 0])
+    steps = [([2000, 900, 64], [4, 4, 4]), ([0, 0, 0], [1, 0, 4]), ([1, 899, 0], [2, 2, 2]), ([1999, 65, 63], [0, 0, 0]),
+             ([640, 640, 64], [4, 1, 3])]
+    new = [(dev_i32(p), dev_i32(t)) for p, t in steps]
+    got = []
+    torch.cuda.synchronize()
+    for p, t in new:                                        # no host wait in between
+        P.copy_(p)
+        T.copy_(t)
+        got.append(das.das_mature_v_attention_paged4(cache, 0, 1, 2, table, P, T, q, kb, vb, ws))
+    for (p, t), (out, lse) in zip(steps, got):
+        o, l = reference(c, f64(q), f64(kb), f64(vb), p, t)
+        assert_close(f64(out), o, lse.cpu().numpy(), l, where=f"lengths {p}")
+    assert das.workspace_status(ws) == 0
+
+
+def test_attention_clamps_and_flags_lengths():
+    rng = np.random.default_rng(11)
+    c = attention_case(rng, 64, 2, 1, 4, [128, 64], [4, 4], rows=2, poison=False)
+    c["P"], c["T"] = np.array([10 ** 9, -3]), np.array([9, -1])
+    c["table"][1, 1] = 0
+    run_attention(c, status=2, where="lengths")
+
+
+def test_attention_on_another_stream_twice_and_in_wide_tables():
+    rng = np.random.default_rng(12)
+    c = attention_case(rng, 128, 8, 2, 8, [500, 70], [8, 5])
+    a = run_attention(c, stream=torch.cuda.Stream())
+    b = run_attention(c)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    c["table"] = np.pad(c["table"], ((0, 0), (0, 1000)), constant_values=-9)
+    b = run_attention(c)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_attention_two_graphs_that_share_a_workspace():
+    rng = np.random.default_rng(19)
+    cases = [attention_case(rng, 128, 8, 2, 4, P, [4, 3]) for P in ([3000, 700], [64, 5000])]
+    caches = [cache_of(c) for c in cases]
+    ws = das.new_workspace_paged4(caches[0], 2, 8, 4)
+    graphs, outs, args = [], [], []
+    for c, cache in zip(cases, caches):
+        a = [dev_i32(c[n]) for n in ("table", "P", "T")] + [bf16(c[n]) for n in ("q", "kb", "vb")]
+        das.das_mature_v_attention_paged4(cache, 0, 1, 2, *a, ws)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(das.das_mature_v_attention_paged4(cache, 0, 1, 2, *a, ws))
+        graphs.append(g)
+        args.append(a)
+    for i in (0, 1, 1, 0, 1, 0):
+        for o in outs[i]:
+            o.fill_(float("nan"))
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        c, a = cases[i], args[i]
+        o, l = reference(c, *(f64(x) for x in a[3:]), c["P"], c["T"])
+        assert_close(f64(outs[i][0]), o, outs[i][1].cpu().numpy(), l, where=f"graph {i}")
+    assert das.workspace_status(ws) == 0
+
+
+def test_attention_offsets_past_32_bits():
+    """Pages whose codes lie more than 4 GiB into the cache, and commits to them."""
+    rng = np.random.default_rng(13)
+    D, H, P = 128, 8, 200
+    pages = (5 << 30) // (H * PAGE * D // 2)
+    cache = das.PagedKVCache4.empty(1, 1, pages, H, D)
+    ids = [pages - 1, 3, pages - 7, pages // 2 + 1]
+    new = bf16(rng.normal(0, 1, (2, 1, 1, 1, P, H, D)))
+    flag = dev_i32([0])
+    slots = [ids[t // PAGE] * PAGE + t % PAGE for t in range(P)]
+    das.das_kv_append_paged4(cache, new[0], new[1], dev_i32(slots), dev_i32([0, P]), flag)
+    part = [t[0, 0, ids].cpu().numpy() for t in (cache.k, cache.k_scale, cache.v, cache.v_scale)]
+    zero = [np.zeros((1, 1) + a.shape, np.uint8) for a in part]
+    one = np.ones((1, 1, H))
+    want = ref.append(*zero, one, one, f64(new[0]), f64(new[1]), np.arange(P), [0, P])
+    K, V = ref.keys(want[0][0, 0], want[1][0, 0], one[0, 0]), ref.values(want[2][0, 0], want[3][0, 0], one[0, 0])
+    got_k, got_v = ref.keys(part[0], part[1], one[0, 0]), ref.values(part[2], part[3], one[0, 0])
+    flat = lambda a: np.swapaxes(a, 1, 2).reshape(-1, H, D)[:P]
+    assert flag.item() == 0 and np.array_equal(flat(got_k), flat(K)) and np.array_equal(flat(got_v), flat(V))
+    ws = das.new_workspace_paged4(cache, 1, H, 4)
+    q, kb, vb = (bf16(rng.normal(0, 1, (1, 4, H, D))) for _ in range(3))
+    out, lse = das.das_mature_v_attention_paged4(cache, 0, 1, 1, dev_i32([ids]), dev_i32([P]), dev_i32([4]), q, kb, vb, ws)
+    o, l = ref.attention(K, V, np.array([[0, 1, 2, 3]]), [P], [4], f64(q), f64(kb), f64(vb))
+    assert_close(f64(out), o, lse.cpu().numpy(), l, where="far pages")

@@ -1,0 +1,128 @@
+"""Norm and rotation of queries and keys against the formula in 64 bits (tests/paged4_ref.py)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_34538_gb300 as das
+from tests import paged4_ref as ref
+from tests.gpu_util import dev_i32, half_ulp_bf16
+
+pytestmark = pytest.mark.gpu
+
+
+def f64(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+def make(seed, B, T, Hq, H, D, rd, base=10000.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rows = (torch.randn((B, T, Hq + 2 * H, D), generator=g, device="cuda") * 3).to(torch.bfloat16)
+    w = [1 + 0.3 * torch.randn(D, generator=g, device="cuda") for _ in range(2)]
+    freq = (base ** (-torch.arange(0, rd, 2, device="cuda", dtype=torch.float64) / max(rd, 1))).float()
+    return rows[:, :, :Hq], rows[:, :, Hq:Hq + H], rows[:, :, Hq + H:], w, freq
+
+
+def check(got, x, weight, eps, place, freq, interleaved, live):
+    """Half a bf16 step, and the binary32 arithmetic: a norm is off by 8e-7 of itself (a sum of 12 steps, its
+    root, two products), an angle by 1e-6, the rotation by 2 roundings: 2.5e-6 of the pair's sizes."""
+    w = None if weight is None else f64(weight)
+    want, size = ref.norm_rope(f64(x), w, eps, ref.angles(place, freq.cpu().numpy()), interleaved)
+    err = np.abs(f64(got) - want)
+    bound = half_ulp_bf16(np.abs(want) + 2.5e-6 * size) + 2.5e-6 * size + 1e-38
+    assert np.all((err <= bound)[live]), float((err / bound)[live].max())
+
+
+@pytest.mark.parametrize("B,T,Hq,H,D,rd,interleaved,eps,wtype", [
+    (1, 1, 1, 1, 64, 64, False, 1e-6, None), (1, 1, 32, 32, 128, 128, False, 1e-6, torch.bfloat16),
+    (2, 3, 4, 1, 64, 32, True, 1e-5, torch.float32), (3, 17, 5, 5, 128, 64, True, 1e-6, torch.bfloat16),
+    (2, 9, 8, 2, 128, 48, False, 0.0, torch.float32), (2, 5, 7, 3, 64, 8, False, None, None),
+    (1, 70, 6, 2, 128, 0, False, 1e-6, torch.bfloat16), (5, 40, 3, 1, 128, 128, True, None, None),
+    (2, 333, 16, 4, 64, 64, False, 1e-6, torch.float32), (33, 2, 1, 1, 128, 8, True, 1e-6, torch.bfloat16)])
+def test_matches_the_formula(B, T, Hq, H, D, rd, interleaved, eps, wtype):
+    q, k, v, w, freq = make(B + T + D + rd, B, T, Hq, H, D, rd)
+    w = [None, None] if wtype is None else [x.to(wtype) for x in w]
+    rng = np.random.default_rng(T)
+    P, n = rng.integers(0, 40000, B), rng.integers(0, T + 1, B)
+    n[0] = T
+    outs = [torch.full((B, T, h, D), 7.0, dtype=torch.bfloat16, device="cuda") for h in (Hq, H, H)]
+    r = das.das_qk_norm_rope(q, k, v, freq, dev_i32(P), dev_i32(n), q_weight=w[0], k_weight=w[1], eps=eps,
+                             interleaved=interleaved, q_out=outs[0], k_out=outs[1], v_out=outs[2])
+    assert all(a is b for a, b in zip(r, outs))
+    live = np.arange(T)[None] < n[:, None]
+    place = P[:, None] + np.arange(T)[None]
+    check(outs[0], q, w[0], eps, place, freq, interleaved, live)
+    check(outs[1], k, w[1], eps, place, freq, interleaved, live)
+    assert torch.equal(outs[2][torch.from_numpy(live)], v[torch.from_numpy(live)])
+    for o in outs:                                        # rows past a block are left as they were
+        assert (o[torch.from_numpy(~live)] == 7).all()
+
+
+def test_far_positions():
+    """Positions near 2^31: a binary32 product of position and frequency would be off by whole turns."""
+    q, k, v, _, freq = make(1, 3, 4, 2, 2, 64, 64, base=500000.0)
+    P = np.array([2 ** 31 - 8, 12345678, 2 ** 24 + 1])
+    qo, ko, _ = das.das_qk_norm_rope(q, k, None, freq, dev_i32(P), eps=None)
+    place = P[:, None] + np.arange(4)[None]
+    live = np.ones((3, 4), bool)
+    # (n f / 2 pi is held to 2^-52 of itself: 2^-23 turns at 2^31, 7e-7 more)
+    check(qo, q, None, None, place, freq, False, live)
+    check(ko, k, None, None, place, freq, False, live)
+
+
+def test_defaults_and_lengths_left_out():
+    q, k, v, _, freq = make(2, 2, 6, 4, 2, 128, 128)
+    qo, ko, vo = das.das_qk_norm_rope(q, k, v, freq)
+    place = np.broadcast_to(np.arange(6), (2, 6))
+    check(qo, q, None, 1e-6, place, freq, False, np.ones((2, 6), bool))
+    assert torch.equal(vo, v)
+    neg, _, none = das.das_qk_norm_rope(q, k, None, freq, dev_i32([-5, 0]))
+    assert none is None and torch.equal(neg, qo)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_in_place_and_strided(interleaved):
+    q, k, v, w, freq = make(3, 2, 21, 8, 2, 128, 96)
+    args = dict(q_weight=w[0], k_weight=w[1], interleaved=interleaved)
+    want = das.das_qk_norm_rope(q, k, v, freq, dev_i32([5, 900]), **args)
+    # heads before tokens, and a batch whose rows lie backwards in memory order
+    t = lambda x: x.transpose(1, 2).contiguous().transpose(1, 2)
+    got = das.das_qk_norm_rope(t(q), t(k), t(v), freq, dev_i32([5, 900]), **args)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    own = [x.contiguous() for x in (q, k, v)]
+    das.das_qk_norm_rope(*own, freq, dev_i32([5, 900]), q_out=own[0], k_out=own[1], v_out=own[2], **args)
+    assert all(torch.equal(a, b) for a, b in zip(own, want))
+
+
+def test_zero_rows_infinities_and_nan_stay_with_their_heads():
+    q, k, v, _, freq = (x.clone() if torch.is_tensor(x) else x for x in make(4, 1, 4, 4, 1, 64, 64))
+    clean, _, _ = das.das_qk_norm_rope(q, k, v, freq)
+    q[0, 1, 2] = 0
+    q[0, 2, 0, 5] = float("nan")
+    q[0, 3, 1, 7] = float("inf")
+    out, _, _ = das.das_qk_norm_rope(q, k, v, freq)
+    assert (out[0, 1, 2] == 0).all() and out[0, 2, 0].isnan().all() and out[0, 3, 1].isnan().any()
+    same = torch.ones((1, 4, 4), dtype=torch.bool)
+    same[0, 1, 2] = same[0, 2, 0] = same[0, 3, 1] = False
+    assert torch.equal(out[same], clean[same])
+
+
+def test_empty_batch_other_stream_and_graph():
+    q, k, v, _, freq = make(5, 0, 4, 4, 1, 64, 64)
+    out = das.das_qk_norm_rope(q, k, v, freq, dev_i32([]))
+    assert out[0].shape == (0, 4, 4, 64)
+    q, k, v, _, freq = make(6, 3, 5, 4, 2, 64, 64)
+    P = dev_i32([1, 2, 3])
+    want = das.das_qk_norm_rope(q, k, v, freq, P)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    got = das.das_qk_norm_rope(q, k, v, freq, P, stream=s)
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    outs = [torch.zeros_like(x) for x in want]
+    with torch.cuda.graph(graph):
+        das.das_qk_norm_rope(q, k, v, freq, P, q_out=outs[0], k_out=outs[1], v_out=outs[2])
+    P.fill_(77)                                           # the captured call reads lengths when it is replayed
+    graph.replay()
+    again = das.das_qk_norm_rope(q, k, v, freq, P)
+    assert all(torch.equal(a, b) for a, b in zip(outs, again)) and not torch.equal(outs[0], want[0])
