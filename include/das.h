@@ -529,10 +529,10 @@ size_t das_workspace_size_paged4(const das_kv_cache_paged4 *cache, int batch, in
  * stand for): keys of key_depth, values of value_depth; key_depth = value_depth is the
  * verify attention.  Arguments, results, limits and status bits as
  * das_mature_v_attention_paged, but for the width of the table, which does not matter
- * here, and the value scales, which need no limits.  Queries are to be finite; keys, values and weights
- * are binary16 in the products over the cache (exact for keys and values; a weight
- * is off by 2^-12 of itself or 2^-30 of the row's largest; a query's elements are exact down to 2^-31 of
- * its row's largest), bf16 in those over the block's own.  Sums are in fp32.
+ * here, and the value scales, which need no limits.  All products run in bf16, which
+ * queries and stored keys and values are; a weight is rounded to it, off by 2^-8 of itself at most, or
+ * by 2^-65 of the row's sum.  Sums and outputs before their rounding are in fp32.  A
+ * value of the block's own that is not finite makes that element of the rows that see it NaN.
  */
 das_status das_mature_v_attention_paged4(const das_kv_cache_paged4 *cache, int layer, int key_depth,
                                          int value_depth, const int32_t *block_table, int max_pages,

@@ -427,7 +427,12 @@ das_status attention_paged4(const das_kv_cache_paged4 *c, int layer, int key_dep
     const double scale =
         softmax_scale > 0.f ? (double)softmax_scale : 1.0 / sqrt((double)c->head_dim);
     p.scale_log2 = (float)(scale * 1.4426950408889634);
-    return paged4_attn_launch(p, c->head_dim, workspace, static_cast<cudaStream_t>(stream)) ==
+    // a page's keys are one box of rows of 128 bytes
+    const cuuint64_t dims[3] = {128, tile_codes / 128, (cuuint64_t)slab_tiles};
+    const cuuint32_t box[3] = {128, (cuuint32_t)(tile_codes / 128), 1};
+    CUtensorMap tm_k;
+    if (!encode(&tm_k, const_cast<uint8_t *>(p.k), 3, dims, box, true, true)) return DAS_ERR_CUDA;
+    return paged4_attn_launch(p, c->head_dim, tm_k, workspace, static_cast<cudaStream_t>(stream)) ==
                    cudaSuccess
                ? DAS_OK
                : DAS_ERR_CUDA;

@@ -139,12 +139,17 @@ struct Paged4AttnParams {
     uint16_t *out;
     float *lse;
     int32_t *status;
+    float *part_o, *part_lse;             // [slots][rows_max][D], [slots][rows_max]
+    int32_t *count_run, *count_pair;      // [slots], [B * Hkv]: 0 between calls
     int B, Hq, Hkv, G, max_block, rows_max, max_pages, pages;
     float scale_log2;
+    int num_ctas;
 };
 size_t paged4_workspace_bytes(int device, int batch, int kv_heads, int rows_max, int head_dim);
-cudaError_t paged4_attn_launch(Paged4AttnParams &p, int head_dim, void *workspace,
-                               cudaStream_t stream);
+// tm_k maps the slab of keys read, bytes [pages * Hkv][head_dim / 4][128], with a {128, head_dim / 4, 1}
+// box and 128-byte swizzle; carves the workspace.
+cudaError_t paged4_attn_launch(Paged4AttnParams &p, int head_dim, const CUtensorMap &tm_k,
+                               void *workspace, cudaStream_t stream);
 
 struct RopeArgs {
     das_head_rows in[3];                  // queries, keys, values (no data: none)

@@ -1,9 +1,38 @@
 // das_paged4_attention.cu -- depth-asynchronous attention (Eqs. 2-3) over the paged 4-bit
-// cache.
+// cache, on the 5th-generation tensor cores of sm_103a with keys and values in
+// tensor memory.
 //
-// One CTA to a query row: its warps take every fourth key, a running maximum and sum
-// each, and join at the end.
+// The mathematics.  A stored value (c - 8) s has at most 8 significant bits, so it is a bf16
+// number, and all products run in bf16: S^T = K Q^T and O^T = V^T P^T, with keys (or the
+// elements of a value) as the 128 rows of the product and the query rows as its columns.
+// The stored codes become A operands in tensor memory, which is where their widening
+// ends, and a tile costs in proportion to the query rows there are (16, 32 or 64 columns).
+// With x_j = s_j + off, off = -m - kBelow, m the score of one key of the segment,
+//     p_j = 2^(x_j),  O = sum p_j v_j,  l = sum p_j,
+// out = O / l and lse = ln 2 (m + kBelow + log2 l).  bf16 has fp32's exponents: p_j keeps its
+// 8 bits from 2^-126 to 2, so m need not be the largest score: any key's will do that is within
+// kBelow binary orders below it.  Only where a weight of a tile comes to 2 or more is the
+// row's reference set again, to the tile's largest, and O and l are rescaled.  The output
+// is divided by the sum of the rounded weights, taken by the tensor core with a row of
+// ones, and is so a mean of the values with the very weights in use; the lse is from the
+// unrounded ones.
+//
+// A word of eight codes gives four pairs (elements i and i + 4): or-ing four bits into bf16 128
+// makes 128 + c, and (128 + c) s - 136 s is exact.  The order of elements (keys) that comes of it
+// is undone in the other operand: in the queries, and in the places of P's rows.
+//
+// Work split: every (sequence, kv head) pair owns a tile for each 128 of its prefix (two
+// pages) and one for the block's own keys.  All pairs' tiles are one list, of which CTA
+// c takes the c-th of C ranges, cut into segments at pair boundaries.  A segment that is
+// a whole pair writes the output, others a partial (O / l, lse); who comes last at the pair's counter
+// joins them.  Lengths are read on the device, so the table's width does not matter.
+//
+// One CTA = two groups of four softmax warps (each has half of the query rows, a thread
+// one key of a tile) + four warps that widen keys, four that widen values, and one
+// each for loads, S and P V.  Every wait is bounded (2 s); a time-out sets the status
+// word and ends the CTA's waits.  Tensor memory is freed before the CTA exits.
 #include <algorithm>
+#include <atomic>
 
 #include "das_internal.h"
 #include "das_tcgen05.h"
@@ -11,123 +40,990 @@
 namespace das {
 namespace {
 
-using t5::kFull;
-constexpr int kWarps = 4;
-constexpr float kLn2 = 0.6931471805599453f;
+using namespace t5;
 
-__device__ __forceinline__ float scale_of(uint8_t byte) {
-    float lo, hi;
-    t5::unpack_f16((uint32_t)byte << 7, lo, hi);
-    return lo;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kKeys = 128;  // of a tile: the rows of a product
+constexpr int kPage = DAS_PAGE_TOKENS;
+constexpr int kGroupWarps = 4, kSoftWarps = 8;
+constexpr int kKeyWarp0 = 8, kValueWarp0 = 12, kProducerWarp = 16, kSWarp = 17, kPvWarp = 18;
+constexpr int kThreads = 19 * 32;
+constexpr float kBelow = 60.f;
+// Tensor memory: keys [2], values [2], S [2], O, the sums of P.
+constexpr int kKCol = 0, kVCol = 128, kSCol = 256, kOCol = 384, kSumCol = 448, kCols = 512;
+constexpr int kInfos = 64;  // ring of the tiles' visible keys
+// The end of a pair (its block tile, the read-out and what joins it) weighs kEnd tiles more.
+constexpr int kEnd = 4;
+constexpr int kLeast = 7;   // weight of a CTA's range, where there is more than one
+constexpr int kFan = 8;     // partials that are joined at once
+
+template <int D, int N>
+struct Layout {
+    static constexpr int kCodes = kPage * D / 2;               // of a page's keys, or values
+    static constexpr int kScales = kPage * D / DAS_SCALE_GROUP;
+    static constexpr int kVOff = 2 * kCodes, kKsOff = 4 * kCodes, kVsOff = kKsOff + 2 * kScales;
+    static constexpr int kStage = (4 * kCodes + 4 * kScales + 1023) / 1024 * 1024;
+    static constexpr int kStages = 8;
+    static constexpr int kQ = N * D * 2, kP = kKeys * 128;
+    static constexpr int kQOff = kStages * kStage;
+    static constexpr int kPOff = kQOff + 2 * kQ;
+    static constexpr int kOnesOff = kPOff + 2 * kP;            // a 64 x 16 operand of ones
+    static constexpr int kBarOff = kOnesOff + 2048;
+    // full, empty [kStages], qready, qfree [2], kready, vready, sdone, sfree, pready, pvdone [2],
+    // drain [2]
+    static constexpr int kBars = 2 * kStages + 4 + 12 + 2;
+    static constexpr int kInfoOff = (kBarOff + 8 * kBars + 15) / 16 * 16;
+    static constexpr int kRowOff = kInfoOff + kInfos * 8;      // floats: off, alpha, 1 / l, lse [64]
+    static constexpr int kSumOff = kRowOff + 4 * 64 * 4;       // [8 warps][32]: sums or largest
+    static constexpr int kVsxOff = kSumOff + 8 * 32 * 4;       // [4 warps][64]: the values' scales
+    static constexpr int kNfOff = kVsxOff + 4 * 64 * 4;        // [128]: first key that is not finite
+    static constexpr int kMiscOff = kNfOff + 128 * 4;
+    static constexpr int kBytes = kMiscOff + 128 + 1024;       // + alignment slack
+    static_assert(kBytes <= 232448, "shared memory per CTA");
+};
+
+// ---- the list of tiles ------------------------------------------------------------
+__device__ __forceinline__ int clamp_to(int v, int hi) { return v < 0 ? 0 : (v > hi ? hi : v); }
+__device__ __forceinline__ int prefix_of(const Paged4AttnParams &p, int b) {
+    return clamp_to(__ldcg(p.prefix_len + b), p.max_pages * kPage);
 }
+__device__ __forceinline__ int block_of(const Paged4AttnParams &p, int b) {
+    return clamp_to(__ldcg(p.block_len + b), p.max_block);
+}
+// a sequence without rows has nothing but its outputs to clear
+__device__ __forceinline__ int tiles_of(int P, int T) { return T > 0 ? (P + kKeys - 1) / kKeys + 1 : 1; }
+
+struct Walk {
+    int b, h, t, nt, P, T;
+};
+__device__ __forceinline__ void walk_load(const Paged4AttnParams &p, Walk &w) {
+    if (w.b < p.B) {
+        w.P = prefix_of(p, w.b);
+        w.T = block_of(p, w.b);
+        w.nt = tiles_of(w.P, w.T);
+    }
+}
+__device__ __forceinline__ void walk_pair(const Paged4AttnParams &p, Walk &w) {
+    w.t = 0;
+    if (++w.h == p.Hkv) {
+        w.h = 0;
+        ++w.b;
+        walk_load(p, w);
+    }
+}
+
+// What a CTA has of the list: tile t of the pair that begins at weighted position q has
+// position q + t, and the range [c W / C, (c + 1) W / C) the tiles of positions in it.
+struct Plan {
+    Walk w;
+    int ntiles, ctas;
+    long long W, q;  // all weight; position of the first pair
+};
+__device__ __forceinline__ int cta_of(const Plan &pl, long long q) {
+    return (int)(((unsigned long long)(q + 1) * (unsigned)pl.ctas - 1) / (unsigned long long)pl.W);
+}
+// (by one whole warp)
+__device__ void make_plan(const Paged4AttnParams &p, Plan &pl) {
+    const int lane = threadIdx.x & 31;
+    auto weight = [&](int b) {
+        return b < p.B ? tiles_of(prefix_of(p, b), block_of(p, b)) + kEnd : 0;
+    };
+    long long W = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 32)
+        W += (long long)__reduce_add_sync(kFull, (unsigned)weight(b0 + lane)) * p.Hkv;
+    const int ctas = (int)max(1ll, min((long long)p.num_ctas, W / kLeast));
+    pl.W = W;
+    pl.ctas = ctas;
+    pl.ntiles = 0;
+    pl.w = {p.B, 0, 0, 1, 0, 0};
+    pl.q = W;
+    if ((int)blockIdx.x >= ctas) return;
+    const long long at[2] = {(long long)((unsigned long long)blockIdx.x * (unsigned long long)W / (unsigned)ctas),
+                             (long long)((unsigned long long)(blockIdx.x + 1) * (unsigned long long)W / (unsigned)ctas)};
+    long long index[2] = {-1, -1};  // tiles before at[i]
+    long long run = 0, tiles = 0;   // weight, tiles before the chunk
+    for (int b0 = 0, found = 0; b0 < p.B && found < 2; b0 += 32) {
+        const int wt = weight(b0 + lane);
+        int inc = wt;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int u = __shfl_up_sync(kFull, inc, d);
+            if (lane >= d) inc += u;
+        }
+        const int n = min(32, p.B - b0);
+        while (found < 2) {
+            const unsigned m = __ballot_sync(kFull, run + (long long)inc * p.Hkv > at[found]);
+            if (!m) break;
+            const int f = __ffs(m) - 1;
+            const int wf = __shfl_sync(kFull, wt, f), before = __shfl_sync(kFull, inc, f) - wf;
+            const long long q0 = run + (long long)before * p.Hkv, off = at[found] - q0;
+            int h = (int)((unsigned long long)off / (unsigned)wf), t = (int)(off - (long long)h * wf);
+            const int nt = wf - kEnd;
+            index[found] = tiles + ((long long)before - (long long)kEnd * f) * p.Hkv + (long long)h * nt + min(t, nt);
+            if (found == 0) {
+                pl.w.b = b0 + f;
+                pl.w.h = h;
+                pl.w.t = t;
+                pl.q = q0 + (long long)h * wf;
+                if (t >= nt) {  // past its last tile: the next pair
+                    pl.q += wf;
+                    pl.w.t = 0;
+                    if (++pl.w.h == p.Hkv) {
+                        pl.w.h = 0;
+                        ++pl.w.b;
+                    }
+                }
+            }
+            ++found;
+        }
+        const int all = __shfl_sync(kFull, inc, 31);
+        run += (long long)all * p.Hkv;
+        tiles += ((long long)all - (long long)kEnd * n) * p.Hkv;
+    }
+    if (index[0] < 0) index[0] = tiles;
+    if (index[1] < 0) index[1] = tiles;
+    walk_load(p, pl.w);
+    pl.ntiles = (int)(index[1] - index[0]);
+}
+
+// A segment: tiles [w.t, end) of a pair.
+struct Segment {
+    int n, pre;  // tiles, those of them before the block's
+};
+__device__ __forceinline__ Segment segment_of(const Walk &w, int left) {
+    const int n = min(left, w.nt - w.t);
+    return {n, min(n, w.nt - 1 - w.t)};
+}
+
 __device__ __forceinline__ float unit_of(const float *unit, int h) {
     if (!unit) return 1.f;
     const uint32_t bits = __float_as_uint(unit[h]);
     const int e = bits >> 31 ? 0 : min(max((int)(bits >> 23) - 127, -40), 40);
     return __uint_as_float((uint32_t)(127 + e) << 23);
 }
-__device__ __forceinline__ float bf(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+// A scale byte's number, which is a bf16 number: its bits are those of the fp32 number 2^-112 times it.
+__device__ __forceinline__ float scale_of(uint32_t byte) {
+    return byte == 0xffu ? __uint_as_float(0x7fffffffu) : __uint_as_float(byte << 20) * 5.192296858534828e33f;
+}
 
+// byte offset of 16-byte chunk c of row m, rows of 128 bytes, swizzled
+__device__ __forceinline__ uint32_t chunk16(int m, int c) { return m * 128 + ((c ^ (m & 7)) << 4); }
+// 16-byte chunk c of a token's keys: a page's are rows of 128 bytes
 template <int D>
-__global__ void __launch_bounds__(kWarps * 32) paged4_row_kernel(const Paged4AttnParams p) {
-    constexpr int V = D / 32;
-    __shared__ float s_m[kWarps], s_l[kWarps], s_o[kWarps][D];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int row = blockIdx.x % p.rows_max, pair = blockIdx.x / p.rows_max;
-    const int b = pair / p.Hkv, h = pair % p.Hkv, i = row / p.G, hq = h * p.G + row % p.G;
+__device__ __forceinline__ uint32_t key_chunk(int t, int c) {
+    constexpr int kTokens = 256 / D;  // tokens to a row
+    return chunk16(t / kTokens, (t % kTokens) * (8 / kTokens) + c);
+}
+__device__ __forceinline__ void st_shared(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w)
+                 : "memory");
+}
+// Eight bf16 elements in the order that a word of eight codes is widened in.
+__device__ __forceinline__ uint4 paired(uint4 x) {
+    return make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632),
+                      __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
+}
+// Four pairs 128 + c of a word's codes.
+__device__ __forceinline__ void widen(uint32_t w, uint32_t (&h)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = (w >> (4 * i) & 0x000f000fu) | 0x43004300u;
+}
+__device__ __forceinline__ uint32_t ordered(float x) {
+    const uint32_t u = __float_as_uint(x);
+    return u >> 31 ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float unordered(uint32_t u) {
+    return __uint_as_float(u >> 31 ? u & 0x7fffffffu : ~u);
+}
+
+template <int D, int N>
+__global__ void __launch_bounds__(kThreads, 1)
+    paged4_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const Paged4AttnParams p) {
+    using Lt = Layout<D, N>;
+    constexpr int kStages = Lt::kStages, R = N / 2;  // rows of a group
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                              ~uintptr_t(1023));
+    const uint32_t sbase = smem_u32(sm);
+    const uint32_t b_full = sbase + Lt::kBarOff, b_empty = b_full + 8 * kStages,
+                   b_qready = b_empty + 8 * kStages, b_qfree = b_qready + 16, b_kready = b_qfree + 16,
+                   b_vready = b_kready + 16, b_sdone = b_vready + 16, b_sfree = b_sdone + 16,
+                   b_pready = b_sfree + 16, b_pvdone = b_pready + 16, b_drain = b_pvdone + 16;
+    int2 *info = reinterpret_cast<int2 *>(sm + Lt::kInfoOff);
+    float *s_off = reinterpret_cast<float *>(sm + Lt::kRowOff), *s_alpha = s_off + 64,
+          *s_inv = s_off + 128, *s_lse = s_off + 192;
+    float *s_sum = reinterpret_cast<float *>(sm + Lt::kSumOff);
+    uint32_t *s_vsx = reinterpret_cast<uint32_t *>(sm + Lt::kVsxOff);
+    int *s_nf = reinterpret_cast<int *>(sm + Lt::kNfOff);
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(sm + Lt::kMiscOff);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(sm + Lt::kMiscOff + 4);
+    volatile int *s_ticket = reinterpret_cast<volatile int *>(sm + Lt::kMiscOff + 8);
+    Plan *s_plan = reinterpret_cast<Plan *>(sm + Lt::kMiscOff + 16);
+    static_assert(sizeof(Plan) <= 112, "plan");
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(b_full + 8 * s, 1);
+            mbar_init(b_empty + 8 * s, 8);  // the warps that widen
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(b_qready + 8 * i, 4);
+            mbar_init(b_qfree + 8 * i, 1);
+            mbar_init(b_kready + 8 * i, 4);
+            mbar_init(b_vready + 8 * i, 4);
+            mbar_init(b_sdone + 8 * i, 1);
+            mbar_init(b_sfree + 8 * i, kSoftWarps);
+            mbar_init(b_pready + 8 * i, kSoftWarps);
+            mbar_init(b_pvdone + 8 * i, 1);
+            mbar_init(b_drain + 8 * i, 1);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        *abort_flag = 0;
+    }
+    if (warp == kSWarp) {
+        asm volatile(
+            "tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                smem_u32(const_cast<uint32_t *>(tmem_slot))),
+            "n"(kCols));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (warp == kProducerWarp && elect_one())
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tm_k)) : "memory");
+    for (int i = threadIdx.x; i < 2048 / 16; i += kThreads)
+        st_shared(sbase + Lt::kOnesOff + 16 * i, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+    fence_async_smem();
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int P0 = p.prefix_len[b], T0 = p.block_len[b];
-    const int P = min(max(P0, 0), p.max_pages * kTileKeys), T = min(max(T0, 0), p.max_block);
-    if ((P != P0 || T != T0) && threadIdx.x == 0) atomicOr(p.status, kStatusClamped);
-    uint16_t *out = p.out + (((size_t)b * p.max_block + i) * p.Hq + hq) * D;
-    float *lse = p.lse + ((size_t)b * p.Hq + hq) * p.max_block + i;
-    if (i >= T) {
-        for (int d = threadIdx.x; d < D; d += kWarps * 32) out[d] = 0;
-        if (threadIdx.x == 0) *lse = -INFINITY;
-        return;
+    if (warp == 0) {
+        Plan pl;
+        make_plan(p, pl);
+        if (lane == 0) *s_plan = pl;
     }
-    const float ku = unit_of(p.k_unit, h), vu = unit_of(p.v_unit, h);
-    float q[V], o[V], m = -INFINITY, l = 0.f;
+    if (blockIdx.x == 0 && warp == 1)
+        for (int b = lane; b < p.B; b += 32)
+            if (__ldcg(p.prefix_len + b) != prefix_of(p, b) || __ldcg(p.block_len + b) != block_of(p, b))
+                atomicOr(p.status, kStatusClamped);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *tmem_slot;
+    Walk w = s_plan->w;
+    const int ntiles = s_plan->ntiles;
+
+    auto waits = [&](uint32_t bar, uint32_t parity) {
+        return wait(bar, parity, abort_flag, p.status);
+    };
+    // Tile k of the range has buffers k % 2; of its prefix tiles, the kp-th has stage kp % kStages.
+    auto half_of = [](int k) { return (uint32_t)(k >> 1) & 1; };
+    int loaded = 0;  // (the producer's)
+    if (warp == kProducerWarp) {
+        // ================================ loads ==================================
+        uint64_t policy;
+        asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+        bool ok = true;
+        for (int left = ntiles; left > 0 && ok; walk_pair(p, w)) {
+            const Segment s = segment_of(w, left);
+            const int pages = (w.P + kPage - 1) / kPage;
+            for (int i0 = 0; i0 < s.pre && ok; i0 += 16) {  // 32 pages at a time, one a lane
+                const int at = 2 * (w.t + i0) + lane, n_here = min(16, s.pre - i0);
+                int page = -1, n = 0;
+                if (at < pages && lane < 2 * n_here) {
+                    page = __ldcg(p.table + (size_t)w.b * p.max_pages + at);
+                    if (page < 0 || page >= p.pages) {
+                        atomicOr(p.status, kStatusBadPage);
+                        page = -1;
+                    } else {
+                        n = min(kPage, w.P - at * kPage);
+                    }
+                }
+                for (int i = 0; i < n_here; ++i) {
+                    const int p0 = __shfl_sync(kFull, page, 2 * i), p1 = __shfl_sync(kFull, page, 2 * i + 1);
+                    const int n0 = __shfl_sync(kFull, n, 2 * i), n1 = __shfl_sync(kFull, n, 2 * i + 1);
+                    const int st = loaded % kStages;
+                    if (loaded >= kStages)
+                        ok = waits(b_empty + 8 * st, (uint32_t)(loaded / kStages - 1) & 1);
+                    if (!ok) break;
+                    if (elect_one()) {
+                        info[loaded % kInfos] = make_int2(n0, n1);
+                        const uint32_t full = b_full + 8 * st, dst = sbase + st * Lt::kStage;
+                        mbar_arrive_expect_tx(full, ((p0 >= 0) + (p1 >= 0)) * 2 * (Lt::kCodes + Lt::kScales));
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        q[j] = bf(p.q[(((size_t)b * p.max_block + i) * p.Hq + hq) * D + 32 * j + lane]);
-        o[j] = 0.f;
-    }
-    for (int key = warp; key < P + i + 1; key += kWarps) {
-        float k[V], v[V];
-        if (key < P) {
-            const int page = p.table[(size_t)b * p.max_pages + key / kTileKeys], t = key % kTileKeys;
-            if (page < 0 || page >= p.pages) {
-                atomicOr(p.status, kStatusBadPage);
-                continue;
+                        for (int j = 0; j < 2; ++j) {
+                            const int pg = j ? p1 : p0;
+                            if (pg < 0) continue;
+                            const int tile = pg * p.Hkv + w.h;
+                            tma_3d(dst + j * Lt::kCodes, &tm_k, full, 0, 0, tile, policy);
+                            bulk_load(dst + Lt::kVOff + j * Lt::kCodes, p.v + (size_t)tile * Lt::kCodes, Lt::kCodes,
+                                      full, policy);
+                            bulk_load(dst + Lt::kKsOff + j * Lt::kScales, p.k_scale + (size_t)tile * Lt::kScales,
+                                      Lt::kScales, full, policy);
+                            bulk_load(dst + Lt::kVsOff + j * Lt::kScales, p.v_scale + (size_t)tile * Lt::kScales,
+                                      Lt::kScales, full, policy);
+                        }
+                    }
+                    __syncwarp();
+                    ++loaded;
+                }
             }
-            const size_t tile = (size_t)page * p.Hkv + h;
+            left -= s.n;
+        }
+    } else if (warp == kSWarp) {
+        // ============================= S^T = K Q^T ===============================
+        constexpr uint32_t id = idesc_bf16(kKeys, N, 0, 0);
+        bool ok = true;
+        int k = 0;
+        for (int seg = 0; k < ntiles && ok; ++seg, walk_pair(p, w)) {
+            const int end = k + segment_of(w, ntiles - k).n;
+            const uint64_t dq = sdesc(sbase + Lt::kQOff + (seg & 1) * Lt::kQ, 16, 1024, 2);
+            ok = waits(b_qready + 8 * (seg & 1), half_of(seg));
+            for (; k < end && ok; ++k) {
+                const int s = k & 1;
+                ok = waits(b_kready + 8 * s, half_of(k)) && (k < 2 || waits(b_sfree + 8 * s, half_of(k) ^ 1));
+                if (!ok) break;
+                fence_after();
+                if (elect_one()) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const int d = 32 * j + lane;
-                const int ck = p.k[(tile * kTileKeys + t) * (D / 2) + d / 2] >> (4 * (d & 1)) & 15;
-                const int cv = p.v[((tile * 8 + t / 8) * D + d) * 4 + t % 8 / 2] >> (4 * (t & 1)) & 15;
-                k[j] = (float)(ck - 8) * scale_of(p.k_scale[(tile * kTileKeys + t) * V + j]) * ku;
-                v[j] = (float)(cv - 8) * scale_of(p.v_scale[(tile * V + j) * kTileKeys + t]) * vu;
-            }
-        } else {
-            const size_t at = (((size_t)b * p.max_block + (key - P)) * p.Hkv + h) * D + lane;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                k[j] = bf(p.k_blk[at + 32 * j]);
-                v[j] = bf(p.v_blk[at + 32 * j]);
+                    for (int kk = 0; kk < D / 16; ++kk)
+                        mma_bf16_ta(tmem + kSCol + 64 * s, tmem + kKCol + 64 * s + 8 * kk,
+                                    dq + (((kk >> 2) * (N * 128) + (kk & 3) * 32) >> 4), id, kk > 0);
+                    mma_commit(b_sdone + 8 * s);
+                    if (k + 1 == end) mma_commit(b_qfree + 8 * (seg & 1));
+                }
+                __syncwarp();
             }
         }
-        float s = 0.f;
+    } else if (warp == kPvWarp) {
+        // ============================ O^T += V^T P^T =============================
+        constexpr uint32_t id = idesc_bf16(kKeys, N, 0, 1), id_sum = idesc_bf16(64, N, 0, 1);
+        const uint64_t ones = sdesc(sbase + Lt::kOnesOff, 128, 256, 0);
+        bool ok = true;
+        int k = 0;
+        for (; k < ntiles && ok; walk_pair(p, w)) {
+            const Segment sg = segment_of(w, ntiles - k);
+            for (int i = 0; i < sg.n && ok; ++i, ++k) {
+                const int s = k & 1;
+                ok = waits(b_vready + 8 * s, half_of(k)) && waits(b_pready + 8 * s, half_of(k));
+                if (!ok) break;
+                fence_after();
+                if (elect_one()) {
+                    const uint64_t dp = sdesc(sbase + Lt::kPOff + s * Lt::kP, Lt::kP, 1024, 2);
+                    const int steps = i < sg.pre ? 8 : 4;  // (the block has 64 keys at most)
+                    for (int kk = 0; kk < steps; ++kk)
+                        mma_bf16_ta(tmem + kOCol, tmem + kVCol + 64 * s + 8 * kk, dp + ((kk * 2048) >> 4), id,
+                                    i > 0 || kk > 0);
+                    if (D == 128)  // (with 64 elements, ones are beside them)
+                        for (int kk = 0; kk < steps; ++kk)
+                            mma_bf16(tmem + kSumCol, ones, dp + ((kk * 2048) >> 4), id_sum, i > 0 || kk > 0);
+                    mma_commit(b_pvdone + 8 * s);
+                }
+                __syncwarp();
+            }
+        }
+    } else if (warp >= kValueWarp0) {
+        // ============================ values, widened ============================
+        // Thread (warp, lane): element d of a value; 32 elements share a scale.
+        const int quad = warp - kValueWarp0, d = quad * 32 + lane;
+        const uint32_t dst = tmem + kVCol + ((uint32_t)(quad * 32) << 16);
+        const bool mine = d < D;  // (a whole warp's)
+        uint32_t *const scales = s_vsx + quad * 64;
+        if (!mine) {
+            uint32_t one[32];
 #pragma unroll
-        for (int j = 0; j < V; ++j) s += q[j] * k[j];
+            for (int j = 0; j < 32; ++j) one[j] = 0x3f803f80u;
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(kFull, s, d);
-        s *= p.scale_log2;
-        const float n = fmaxf(m, s), c = m == -INFINITY ? 0.f : exp2f(m - n), w = s == -INFINITY ? 0.f : exp2f(s - n);
-        m = n;
-        l = l * c + w;
+            for (int j = 0; j < 4; ++j) st_lanes(dst + 32 * j, one);
+        }
+        int k = 0, kp = 0;
+        bool ok = true;
+        for (; k < ntiles && ok; walk_pair(p, w)) {
+            const Segment sg = segment_of(w, ntiles - k);
+            for (int i = 0; i < sg.n && ok; ++i, ++k) {
+                const int s = k & 1;
+                if (i < sg.pre) {
+                    const int st = kp % kStages;
+                    const uint8_t *stage = sm + st * Lt::kStage;
+                    ok = waits(b_full + 8 * st, (uint32_t)(kp / kStages) & 1);
+                    if (!ok) break;
+                    if (mine) {
+                        // the scales of this warp's elements, in pairs of keys: columns 2 lane and 2 lane + 1
+                        // are keys 8 o + q and 8 o + q + 4, q = 2 (lane % 2) and one more
+                        const int2 n = info[kp % kInfos];
+                        const int o = lane >> 1, pg = o >> 3, left = (pg ? n.y : n.x) - (o & 7) * 8;
+                        uint2 by = *reinterpret_cast<const uint2 *>(stage + Lt::kVsOff + pg * Lt::kScales + quad * kPage +
+                                                                    (o & 7) * 8);
+                        if (left < 8) {  // places past the last token may hold anything
+                            const unsigned long long keep = left <= 0 ? 0 : (1ull << 8 * left) - 1;
+                            by.x &= (uint32_t)keep;
+                            by.y &= (uint32_t)(keep >> 32);
+                        }
+                        const int q = 16 * (lane & 1);
+                        uint2 x;
+                        x.x = pack_bf16(scale_of(by.x >> q & 0xffu), scale_of(by.y >> q & 0xffu));
+                        x.y = pack_bf16(scale_of(by.x >> (q + 8) & 0xffu), scale_of(by.y >> (q + 8) & 0xffu));
+                        __syncwarp();
+                        *reinterpret_cast<uint2 *>(scales + 2 * lane) = x;
+                        __syncwarp();
+                    }
+                    if (k >= 2) ok = waits(b_pvdone + 8 * s, half_of(k) ^ 1);
+                    if (!ok) break;
+                    fence_after();
+                    if (mine) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) o[j] = o[j] * c + w * v[j];
+                        for (int c = 0; c < 2; ++c) {  // a page's 64 keys: 32 columns
+                            uint32_t r[32];
+#pragma unroll
+                            for (int o = 0; o < 8; ++o) {
+                                const uint32_t word = *reinterpret_cast<const uint32_t *>(
+                                    stage + Lt::kVOff + c * Lt::kCodes + (o * D + d) * 4);
+                                const uint4 x = *reinterpret_cast<const uint4 *>(scales + 32 * c + 4 * o);
+                                uint32_t h[4];
+                                widen(word, h);
+                                const uint32_t m8 = 0xc308c308u;  // -136
+                                r[4 * o] = bf16_mul2(bf16_add2(h[0], m8), x.x);
+                                r[4 * o + 1] = bf16_mul2(bf16_add2(h[1], m8), x.y);
+                                r[4 * o + 2] = bf16_mul2(bf16_add2(h[2], m8), x.z);
+                                r[4 * o + 3] = bf16_mul2(bf16_add2(h[3], m8), x.w);
+                            }
+                            st_lanes(dst + 64 * s + 32 * c, r);
+                        }
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(b_empty + 8 * st);
+                    ++kp;
+                } else {  // the block's own, in units of the stored ones'
+                    if (k >= 2) ok = waits(b_pvdone + 8 * s, half_of(k) ^ 1);
+                    if (!ok) break;
+                    fence_after();
+                    if (mine) {
+                        const float unit = 1.f / unit_of(p.v_unit, w.h);
+                        const uint16_t *src = p.v_blk + ((size_t)w.b * p.max_block * p.Hkv + w.h) * D + d;
+                        uint32_t r[32];
+                        int nf = kKeys;
+#pragma unroll
+                        for (int o = 0; o < 8; ++o) {
+                            float x[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                x[j] = 8 * o + j < w.T
+                                           ? __uint_as_float((uint32_t)src[(size_t)(8 * o + j) * p.Hkv * D] << 16)
+                                           : 0.f;
+#pragma unroll
+                            for (int j = 7; j >= 0; --j)
+                                if (!(fabsf(x[j]) < INFINITY)) {
+                                    nf = min(nf, 8 * o + j);
+                                    x[j] = 0.f;
+                                }
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) r[4 * o + j] = pack_bf16(x[j] * unit, x[j + 4] * unit);
+                        }
+                        s_nf[d] = nf;
+                        st_lanes(dst + 64 * s, r);
+                    }
+                }
+                st_wait();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_vready + 8 * s);
+            }
+        }
+    } else if (warp >= kKeyWarp0) {
+        // ======================== queries; keys, widened =========================
+        // Thread (warp, lane): a key of the tile.
+        const int quad = warp - kKeyWarp0, key = quad * 32 + lane;
+        const uint32_t dst = tmem + kKCol + ((uint32_t)(quad * 32) << 16);
+        int k = 0, kp = 0;
+        bool ok = true;
+        for (int seg = 0; k < ntiles && ok; ++seg, walk_pair(p, w)) {
+            const Segment sg = segment_of(w, ntiles - k);
+            if (seg >= 2) ok = waits(b_qfree + 8 * (seg & 1), half_of(seg) ^ 1);
+            if (!ok) break;
+            {
+                const uint32_t q = sbase + Lt::kQOff + (seg & 1) * Lt::kQ;
+                constexpr int kPerRow = D / 8;
+                const int rows = p.G * w.T;
+#pragma unroll 4
+                for (int i = key; i < N * kPerRow; i += kKeys) {
+                    const int r = i / kPerRow, c = i % kPerRow;
+                    uint4 x = make_uint4(0, 0, 0, 0);
+                    if (r < rows)
+                        x = *reinterpret_cast<const uint4 *>(
+                            p.q + (((size_t)w.b * p.max_block + r / p.G) * p.Hq + w.h * p.G + r % p.G) * D + c * 8);
+                    x = paired(x);
+                    st_shared(q + (c >> 3) * (N * 128) + chunk16(r, c & 7), x.x, x.y, x.z, x.w);
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_qready + 8 * (seg & 1));
+            }
+            for (int i = 0; i < sg.n && ok; ++i, ++k) {
+                const int s = k & 1;
+                if (k >= 2) ok = waits(b_sdone + 8 * s, half_of(k) ^ 1);
+                if (!ok) break;
+                if (i < sg.pre) {
+                    const int st = kp % kStages;
+                    const uint32_t stage = sbase + st * Lt::kStage;
+                    ok = waits(b_full + 8 * st, (uint32_t)(kp / kStages) & 1);
+                    if (!ok) break;
+                    fence_after();
+                    const int pg = key / kPage, t = key % kPage;
+                    uint32_t by;
+                    if (D == 128)
+                        by = *reinterpret_cast<const uint32_t *>(sm + st * Lt::kStage + Lt::kKsOff + pg * Lt::kScales + t * 4);
+                    else
+                        by = *reinterpret_cast<const uint16_t *>(sm + st * Lt::kStage + Lt::kKsOff + pg * Lt::kScales + t * 2);
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c) {  // 32 elements under a scale
+                        uint4 x;
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                     : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
+                                     : "r"(stage + pg * Lt::kCodes + key_chunk<D>(t, c)));
+                        const float f = scale_of(by >> (8 * c) & 0xffu);
+                        const uint32_t sc = pack_bf16(f, f), m8 = bf16_mul2(sc, 0xc308c308u);
+                        const uint32_t word[4] = {x.x, x.y, x.z, x.w};
+                        uint32_t r[16];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            uint32_t h[4];
+                            widen(word[j], h);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) r[4 * j + e] = bf16_fma2(h[e], sc, m8);
+                        }
+                        st_lanes(dst + 64 * s + 16 * c, r);
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(b_empty + 8 * st);
+                    ++kp;
+                } else {  // the block's own (S of keys past it is not looked at)
+                    fence_after();
+                    if (quad < 2) {
+                        const uint4 *src = reinterpret_cast<const uint4 *>(
+                            p.k_blk + (((size_t)w.b * p.max_block + key) * p.Hkv + w.h) * D);
+#pragma unroll
+                        for (int c = 0; c < D / 32; ++c) {
+                            uint32_t r[16];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                uint4 x = make_uint4(0, 0, 0, 0);
+                                if (key < w.T) x = src[4 * c + j];
+                                x = paired(x);
+                                r[4 * j] = x.x;
+                                r[4 * j + 1] = x.y;
+                                r[4 * j + 2] = x.z;
+                                r[4 * j + 3] = x.w;
+                            }
+                            st_lanes(dst + 64 * s + 16 * c, r);
+                        }
+                    }
+                }
+                st_wait();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_kready + 8 * s);
+            }
+        }
+    } else {
+        // ================================ softmax ================================
+        const int group = warp / kGroupWarps, quad = warp % kGroupWarps, key = quad * 32 + lane;
+        const int bar = 1 + group, row0 = group * R;
+        const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
+        const int place = (key & ~7) | (key & 3) << 1 | (key >> 2 & 1);  // of the key among P's rows
+        float *const off = s_off + row0, *const alpha = s_alpha + row0;
+        float *const sums = s_sum + warp * 32, *const group_sums = s_sum + group * kGroupWarps * 32;
+        auto group_sync = [&] { asm volatile("bar.sync %0, 128;" ::"r"(bar) : "memory"); };
+        auto all_sync = [&] { asm volatile("bar.sync 3, 256;" ::: "memory"); };
+        long long q_pair = s_plan->q;
+        int k = 0, kp = 0;
+        for (; k < ntiles; q_pair += w.nt + kEnd, walk_pair(p, w)) {
+            const Segment sg = segment_of(w, ntiles - k);
+            const int rows = p.G * w.T, seg_t = w.t;
+            const float sc_page = fmaxf(p.scale_log2 * unit_of(p.k_unit, w.h), 1.2e-38f);
+            float l[R];
+#pragma unroll
+            for (int j = 0; j < R; ++j) l[j] = 0.f;
+            bool has_ref = false;  // the same in the whole group
+            for (int i = 0; i < sg.n; ++i, ++k) {
+                const int s = k & 1;
+                const bool blk = i >= sg.pre;
+                int2 n = make_int2(0, 0);
+                const bool ok = waits(b_sdone + 8 * s, half_of(k));
+                fence_after();
+                uint32_t a[R];
+                ld_lanes(lanes + kSCol + 64 * s + row0, a);
+                if (!blk) {
+                    n = info[kp % kInfos];
+                    ++kp;
+                }
+                ld_wait(a);
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_sfree + 8 * s);
+                const float sc = blk ? p.scale_log2 : sc_page;
+                if (blk) {  // the causal mask: key i is seen by the rows from i G on
+                    const int from = ok && key < w.T ? key * p.G : N;
+#pragma unroll
+                    for (int j = 0; j < R; ++j)
+                        if (row0 + j < from || row0 + j >= rows) a[j] = 0xff800000u;
+                } else if (n.x < kPage || n.y < kPage) {
+                    if (!ok || key % kPage >= (key < kPage ? n.x : n.y))
+#pragma unroll
+                        for (int j = 0; j < R; ++j) a[j] = 0xff800000u;
+                }
+                if (!has_ref) {
+                    // the segment's first key that is seen, if this tile has one
+                    const int first = blk ? 0 : n.x > 0 ? 0 : n.y > 0 ? kPage : -1;
+                    if (first >= 0) {
+                        if (key == first)
+#pragma unroll
+                            for (int j = 0; j < R; ++j) {
+                                const float m = __uint_as_float(a[j]) * sc;
+                                off[j] = (fabsf(m) < INFINITY ? -m : 0.f) - kBelow;
+                            }
+                        group_sync();
+                        has_ref = true;
+                    }
+                }
+                float e[R];
+                uint32_t pk[R / 2], big = 0;
+                auto weights = [&] {
+#pragma unroll
+                    for (int j = 0; j < R; j += 4) {
+                        const float4 o = *reinterpret_cast<const float4 *>(off + j);
+                        axpy2(e[j], e[j + 1], sc, __uint_as_float(a[j]), __uint_as_float(a[j + 1]), o.x, o.y);
+                        axpy2(e[j + 2], e[j + 3], sc, __uint_as_float(a[j + 2]), __uint_as_float(a[j + 3]), o.z, o.w);
+                    }
+                    big = 0;
+#pragma unroll
+                    for (int j = 0; j < R; ++j) e[j] = ex2(e[j]);
+#pragma unroll
+                    for (int j = 0; j < R / 2; ++j) {
+                        pk[j] = pack_bf16(e[2 * j], e[2 * j + 1]);
+                        big |= pk[j];
+                    }
+                };
+                if (has_ref) {
+                    weights();
+                } else {  // nothing is seen yet
+#pragma unroll
+                    for (int j = 0; j < R; ++j) e[j] = 0.f;
+#pragma unroll
+                    for (int j = 0; j < R / 2; ++j) pk[j] = 0;
+                }
+                uint32_t over;
+                asm volatile(
+                    "{\n .reg .pred p, q;\n setp.ne.b32 p, %1, 0;\n"
+                    " barrier.cta.red.or.pred q, %2, 128, p;\n selp.u32 %0, 1, 0, q;\n}"
+                    : "=r"(over)
+                    : "r"(big & 0x40004000u), "r"(bar)
+                    : "memory");
+                if (over) {  // a weight of 2 or more: the references are set to the tile's largest
+#pragma unroll
+                    for (int j = 0; j < R; ++j) {
+                        const float x = __uint_as_float(a[j]) * sc;
+                        const uint32_t m = __reduce_max_sync(kFull, ordered(x == x ? x : -INFINITY));
+                        if (lane == 0) sums[j] = unordered(m);
+                    }
+                    group_sync();
+                    if (quad == 0 && lane < R) {
+                        float m = -INFINITY;
+                        for (int v = 0; v < kGroupWarps; ++v) m = fmaxf(m, group_sums[v * 32 + lane]);
+                        const float was = off[lane], now = fminf(was, (m < INFINITY ? -m : 0.f) - kBelow);
+                        off[lane] = now;
+                        alpha[lane] = ex2(now - was);
+                    }
+                    group_sync();
+                    if (i > 0) {
+                        waits(b_pvdone + 8 * (s ^ 1), half_of(k - 1));
+                        fence_after();
+                        uint32_t o[R];
+                        auto rescale = [&](uint32_t col) {
+                            ld_lanes(lanes + col + row0, o);
+                            ld_wait(o);
+#pragma unroll
+                            for (int j = 0; j < R; ++j)
+                                o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha[j]);
+                            st_lanes(lanes + col + row0, o);
+                        };
+                        rescale(kOCol);
+                        if (D == 128) rescale(kSumCol);
+                        st_wait();
+                    }
+#pragma unroll
+                    for (int j = 0; j < R; ++j) l[j] *= alpha[j];
+                    weights();
+                }
+#pragma unroll
+                for (int j = 0; j < R; j += 2) add2(l[j], l[j + 1], l[j], l[j + 1], e[j], e[j + 1]);
+                if (k >= 2) waits(b_pvdone + 8 * s, half_of(k) ^ 1);
+                const uint32_t dst = sbase + Lt::kPOff + s * Lt::kP;
+#pragma unroll
+                for (int j = 0; j < R / 8; ++j)
+                    st_shared(dst + chunk16(place, row0 / 8 + j), pk[4 * j], pk[4 * j + 1], pk[4 * j + 2], pk[4 * j + 3]);
+                fence_async_smem();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_pready + 8 * s);
+            }
+
+            // ---- the end of a segment: O / l and lse, as output or as a partial ----
+            // l of row j over the warp's keys, in lane j (R lanes)
+            {
+                int n = R;
+#pragma unroll
+                for (int d = 16; d > 0; d >>= 1) {
+                    if (2 * d > R) {
+#pragma unroll
+                        for (int j = 0; j < R; ++j) l[j] += __shfl_xor_sync(kFull, l[j], d);
+                    } else {
+                        n = d;
+#pragma unroll
+                        for (int j = 0; j < R / 2; ++j)
+                            if (j < d) {
+                                const bool up = lane & d;
+                                const float give = up ? l[j] : l[j + d], keep = up ? l[j + d] : l[j];
+                                l[j] = keep + __shfl_xor_sync(kFull, give, d);
+                            }
+                    }
+                }
+                if (lane < R) sums[lane] = l[0];
+            }
+            const int last = (k - 1) & 1;
+            waits(b_pvdone + 8 * last, half_of(k - 1));
+            fence_after();
+            if (quad == (D == 128 ? 0 : 2)) {  // the sums of the rounded weights, in any lane that has them
+                uint32_t o[R];
+                ld_lanes(lanes + (D == 128 ? kSumCol : kOCol) + row0, o);
+                ld_wait(o);
+                if (lane == 0)
+#pragma unroll
+                    for (int j = 0; j < R; ++j) alpha[j] = __uint_as_float(o[j]);
+            }
+            group_sync();
+            const bool has_blk = sg.n > sg.pre, whole = seg_t == 0 && has_blk;
+            const float vu = unit_of(p.v_unit, w.h);
+            if (quad == 0 && lane < R) {
+                float sum = 0.f;
+                for (int v = 0; v < kGroupWarps; ++v) sum += group_sums[v * 32 + lane];
+                // no visible key: 0 and -inf; NaN stays NaN
+                s_inv[row0 + lane] = sum == 0.f ? 0.f : vu / alpha[lane];
+                s_lse[row0 + lane] = sum == 0.f || !has_ref ? -INFINITY : log2f(sum) - off[lane];
+            }
+            group_sync();
+            const size_t pair = (size_t)w.b * p.Hkv + w.h;
+            const size_t slot = pair + blockIdx.x;
+            if (quad * 32 < D) {
+                uint32_t o[R];
+                ld_lanes(lanes + kOCol + row0, o);
+                ld_wait(o);
+                const int nf = has_blk ? s_nf[key] : kKeys;  // (key: the element d here)
+                if (nf < kKeys)
+#pragma unroll
+                    for (int j = 0; j < R; ++j)
+                        if (row0 + j >= nf * p.G) o[j] = 0x7fffffffu;
+                if (whole) {
+#pragma unroll
+                    for (int j = 0; j < R; j += 2) {
+                        // lane d has rows j and j + 1 of element d: an even lane stores row j's two elements, an odd
+                        // one row j + 1's
+                        const float x = __uint_as_float(o[j]) * s_inv[row0 + j], y = __uint_as_float(o[j + 1]) * s_inv[row0 + j + 1];
+                        const bool odd = lane & 1;
+                        const float got = __shfl_xor_sync(kFull, odd ? x : y, 1);
+                        const int r = row0 + j + odd, i = r / p.G;
+                        if (r < p.rows_max)
+                            *reinterpret_cast<uint32_t *>(
+                                p.out + (((size_t)w.b * p.max_block + i) * p.Hq + w.h * p.G + r % p.G) * D + (key & ~1)) =
+                                r < rows ? (odd ? pack_bf16(got, y) : pack_bf16(x, got)) : 0u;
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < R; ++j)
+                        if (row0 + j < rows)
+                            p.part_o[(slot * p.rows_max + row0 + j) * D + key] = __uint_as_float(o[j]) * s_inv[row0 + j];
+                }
+            }
+            fence_before();
+            if (quad == 3 && lane < R && row0 + lane < p.rows_max) {
+                const int r = row0 + lane;
+                if (whole)
+                    p.lse[((size_t)w.b * p.Hq + w.h * p.G + r % p.G) * p.max_block + r / p.G] =
+                        r < rows ? s_lse[r] * kLn2 : -INFINITY;
+                else
+                    p.part_lse[slot * p.rows_max + r] = r < rows ? s_lse[r] : -INFINITY;
+            }
+            if (!whole) {
+                // ---- whoever comes last joins the pair's partials ----
+                // With more than kFan of them, runs of about as many as there are runs are joined first,
+                // each into its first place.
+                const Plan &pl = *s_plan;
+                const int c0 = cta_of(pl, q_pair), n = cta_of(pl, q_pair + w.nt - 1) - c0 + 1;
+                int run = n;
+                if (n > kFan) {
+                    run = 2;
+                    while (run * run < n) ++run;
+                }
+                auto last_of = [&](int32_t *counter, int count) {
+                    __threadfence();
+                    all_sync();
+                    if (threadIdx.x == 0) {
+                        const int t = atomicAdd(counter, 1);
+                        if (t == count - 1) *counter = 0;
+                        *s_ticket = t == count - 1;
+                    }
+                    all_sync();
+                    const bool yes = *s_ticket;
+                    if (yes) __threadfence();
+                    return yes;
+                };
+                // partials at places first, first + step, ...: to the output, or into the first
+                auto join = [&](size_t first, int step, int count, bool final) {
+                    constexpr int kPer = D / 4;  // threads to a row
+                    for (int r0 = 0; r0 < p.rows_max; r0 += 256 / kPer) {
+                        const int r = r0 + threadIdx.x / kPer, c = threadIdx.x % kPer * 4;
+                        float M = -INFINITY, L = 0.f;
+                        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                        if (r < rows) {
+                            for (int j0 = 0; j0 < count; j0 += 4) {
+                                float ls[4];
+                                float4 x[4];
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    ls[j] = -INFINITY;
+                                    x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                                    if (j0 + j < count) {
+                                        const size_t at = (first + (size_t)(j0 + j) * step) * p.rows_max + r;
+                                        ls[j] = __ldcg(p.part_lse + at);
+                                        x[j] = __ldcg(reinterpret_cast<const float4 *>(p.part_o + at * D + c));
+                                    }
+                                }
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    if (ls[j] == -INFINITY) continue;
+                                    // (NaN goes into the sums, not into the reference)
+                                    const float m = fmaxf(M, ls[j]);
+                                    const float f = M == m ? 1.f : ex2(M - m), g = m == ls[j] ? 1.f : ex2(ls[j] - m);
+                                    M = m;
+                                    L = L * f + g;
+                                    acc.x = acc.x * f + x[j].x * g;
+                                    acc.y = acc.y * f + x[j].y * g;
+                                    acc.z = acc.z * f + x[j].z * g;
+                                    acc.w = acc.w * f + x[j].w * g;
+                                }
+                            }
+                        }
+                        const float inv = L == 0.f ? 0.f : 1.f / L, lse = L == 0.f ? -INFINITY : M + log2f(L);
+                        if (final) {
+                            if (r < p.rows_max) {
+                                const int hq = w.h * p.G + r % p.G, i = r / p.G;
+                                *reinterpret_cast<uint2 *>(p.out + (((size_t)w.b * p.max_block + i) * p.Hq + hq) * D + c) =
+                                    make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+                                if (c == 0) p.lse[((size_t)w.b * p.Hq + hq) * p.max_block + i] = lse * kLn2;
+                            }
+                        } else {
+                            all_sync();  // the row's threads have read its lse
+                            if (r < rows) {
+                                const size_t at = first * p.rows_max + r;
+                                *reinterpret_cast<float4 *>(p.part_o + at * D + c) =
+                                    make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+                                if (c == 0) p.part_lse[at] = lse;
+                            }
+                        }
+                    }
+                };
+                const int mine = (int)blockIdx.x - c0, r0 = mine / run * run, runs = (n + run - 1) / run;
+                if (last_of(p.count_run + pair + c0 + r0, min(run, n - r0))) {
+                    join(pair + c0 + r0, 1, min(run, n - r0), runs == 1);
+                    if (runs > 1 && last_of(p.count_pair + pair, runs)) join(pair + c0, run, runs, true);
+                }
+            }
+            group_sync();  // the rows' arrays may be written again
+        }
     }
-    if (lane == 0) {
-        s_m[warp] = m;
-        s_l[warp] = l;
-    }
-#pragma unroll
-    for (int j = 0; j < V; ++j) s_o[warp][32 * j + lane] = o[j];
+    fence_before();
     __syncthreads();
-    float M = -INFINITY, L = 0.f;
-    for (int w = 0; w < kWarps; ++w) M = fmaxf(M, s_m[w]);
-    const float M0 = M == -INFINITY ? 0.f : M;
-    for (int w = 0; w < kWarps; ++w) L += s_l[w] * exp2f(s_m[w] - M0);
-    for (int d = threadIdx.x; d < D; d += kWarps * 32) {
-        float x = 0.f;
-        for (int w = 0; w < kWarps; ++w) x += s_o[w][d] * exp2f(s_m[w] - M0);
-        out[d] = (uint16_t)t5::pack_bf16(L == 0.f ? 0.f : x / L, 0.f);
+    fence_after();
+    if (*abort_flag) {  // a timed-out run: products and copies may be in flight yet
+        if (warp == kSWarp || warp == kPvWarp) {
+            const uint32_t drain = b_drain + (warp == kSWarp ? 8 : 0);
+            if (elect_one()) mma_commit(drain);
+            __syncwarp();
+            drain_wait(drain, 0);
+        }
+        if (warp == kProducerWarp && elect_one())
+            for (int j = loaded - 1; j >= 0 && j >= loaded - kStages; --j)
+                drain_wait(b_full + 8 * (j % kStages), (uint32_t)(j / kStages) & 1);
+        __syncwarp();
+        fence_before();
+        __syncthreads();
+        fence_after();
     }
-    if (threadIdx.x == 0) *lse = L == 0.f ? -INFINITY : (M0 + log2f(L)) * kLn2;
+    // (else the softmax warps have seen every product's completion)
+    if (warp == kSWarp)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kCols));
 }
 
-}  // namespace
+size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 
-size_t paged4_workspace_bytes(int device, int batch, int kv_heads, int rows_max, int head_dim) {
-    return kWorkspaceHeader;
-}
-
-cudaError_t paged4_attn_launch(Paged4AttnParams &p, int head_dim, void *workspace, cudaStream_t stream) {
-    p.status = static_cast<int32_t *>(workspace);
+template <int D, int N>
+cudaError_t launch(const Paged4AttnParams &p, const CUtensorMap &tm_k, cudaStream_t stream) {
+    constexpr int smem = Layout<D, N>::kBytes;
+    static std::atomic<bool> configured[64];  // the shared-memory opt-in, once per device
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !configured[dev].load(std::memory_order_acquire)) {
+        e = cudaFuncSetAttribute(paged4_attn_kernel<D, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) configured[dev].store(true, std::memory_order_release);
+    }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(p.B * p.Hkv * p.rows_max));
-    cfg.blockDim = dim3(kWarps * 32);
+    cfg.gridDim = dim3((unsigned)p.num_ctas);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, head_dim == 128 ? paged4_row_kernel<128> : paged4_row_kernel<64>, p);
+    return cudaLaunchKernelEx(&cfg, paged4_attn_kernel<D, N>, tm_k, p);
+}
+
+template <int D>
+cudaError_t launch_d(const Paged4AttnParams &p, const CUtensorMap &tm_k, cudaStream_t stream) {
+    return p.rows_max <= 16   ? launch<D, 16>(p, tm_k, stream)
+           : p.rows_max <= 32 ? launch<D, 32>(p, tm_k, stream)
+                              : launch<D, 64>(p, tm_k, stream);
+}
+
+}  // namespace
+
+// header | counters of runs [slots], of pairs [pairs] | part_lse [slots][rows_max] | part_o
+// [slots][rows_max][D], slots = pairs + C (a segment's slot is its pair + its CTA).
+size_t paged4_workspace_bytes(int device, int batch, int kv_heads, int rows_max, int head_dim) {
+    const int C = attn_grid_size(device);
+    if (C <= 0) return 0;
+    const size_t pairs = (size_t)batch * kv_heads, slots = pairs + (size_t)C;
+    return kWorkspaceHeader + round256((slots + pairs) * sizeof(int32_t)) +
+           round256(slots * rows_max * sizeof(float)) + round256(slots * rows_max * head_dim * sizeof(float));
+}
+
+cudaError_t paged4_attn_launch(Paged4AttnParams &p, int head_dim, const CUtensorMap &tm_k, void *workspace,
+                               cudaStream_t stream) {
+    int dev = 0;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    p.num_ctas = attn_grid_size(dev);
+    if (p.num_ctas <= 0) return cudaErrorInvalidDevice;
+    const size_t pairs = (size_t)p.B * p.Hkv, slots = pairs + (size_t)p.num_ctas;
+    uint8_t *ws = static_cast<uint8_t *>(workspace);
+    p.status = reinterpret_cast<int32_t *>(ws);
+    ws += kWorkspaceHeader;
+    p.count_run = reinterpret_cast<int32_t *>(ws);
+    p.count_pair = p.count_run + slots;
+    ws += round256((slots + pairs) * sizeof(int32_t));
+    p.part_lse = reinterpret_cast<float *>(ws);
+    p.part_o = reinterpret_cast<float *>(ws + round256(slots * p.rows_max * sizeof(float)));
+    return head_dim == 128 ? launch_d<128>(p, tm_k, stream) : launch_d<64>(p, tm_k, stream);
 }
 
 }  // namespace das

@@ -1,4 +1,4 @@
-// das_tcgen05.h -- device primitives of the paged attention kernel: bounded
+// das_tcgen05.h -- device primitives of the paged attention kernels: bounded
 // mbarrier waits, TMA tile loads, tcgen05 descriptors, MMAs and tensor-memory
 // accesses for sm_103a.  (das_attention.cu keeps its own: its counters are
 // recorded against a digest of that file.)
@@ -85,6 +85,16 @@ __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap *map, uin
         : "memory");
 }
 
+// 16-byte aligned bytes, a multiple of 16
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes,
+                                          uint32_t bar, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+        " [%0], [%1], %2, [%3], %4;" ::"r"(dst),
+        "l"(src), "r"(bytes), "r"(bar), "l"(policy)
+        : "memory");
+}
+
 // L2 prefetches (no shared memory, no barrier): 16-byte aligned bytes, a line.
 __device__ __forceinline__ void prefetch_bulk(const void *src, uint32_t bytes) {
     asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
@@ -136,6 +146,15 @@ __device__ __forceinline__ void mma_f8_ta(uint32_t d_tmem, uint32_t a_tmem, uint
     asm volatile(
         "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
         " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem),
+        "r"(a_tmem), "l"(b), "r"(id), "r"(accumulate)
+        : "memory");
+}
+// (two 16-bit elements to a column)
+__device__ __forceinline__ void mma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b,
+                                            uint32_t id, uint32_t accumulate) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem),
         "r"(a_tmem), "l"(b), "r"(id), "r"(accumulate)
         : "memory");
 }
@@ -246,6 +265,42 @@ __device__ __forceinline__ void st_lanes32(uint32_t a, const uint32_t (&r)[32]) 
         DAS_I8(r, 0), DAS_I8(r, 8), DAS_I8(r, 16), DAS_I8(r, 24)
         : "memory");
 }
+// The same for fewer columns, loads without a wait (as ld_half).
+__device__ __forceinline__ void ld_lanes(uint32_t a, uint32_t (&r)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : DAS_R8(r, 0)
+                 : "r"(a)
+                 : "memory");
+}
+__device__ __forceinline__ void ld_lanes(uint32_t a, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
+        "%15}, [%16];"
+        : DAS_R8(r, 0), DAS_R8(r, 8)
+        : "r"(a)
+        : "memory");
+}
+__device__ __forceinline__ void ld_lanes(uint32_t a, uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
+        "%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : DAS_R8(r, 0), DAS_R8(r, 8), DAS_R8(r, 16), DAS_R8(r, 24)
+        : "r"(a)
+        : "memory");
+}
+__device__ __forceinline__ void st_lanes(uint32_t a, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(a),
+                 DAS_I8(r, 0)
+                 : "memory");
+}
+__device__ __forceinline__ void st_lanes(uint32_t a, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,"
+        "%14,%15,%16};" ::"r"(a),
+        DAS_I8(r, 0), DAS_I8(r, 8)
+        : "memory");
+}
+__device__ __forceinline__ void st_lanes(uint32_t a, const uint32_t (&r)[32]) { st_lanes32(a, r); }
 #undef DAS_I8
 #undef DAS_R8
 
@@ -328,6 +383,21 @@ __device__ __forceinline__ void unpack_f16(uint32_t h2, float &lo, float &hi) {
 __device__ __forceinline__ uint32_t hsub2(uint32_t a, uint32_t b) {
     uint32_t d;
     asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t bf16_fma2(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t d;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+__device__ __forceinline__ uint32_t bf16_add2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t bf16_mul2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
 }
 __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {

@@ -72,12 +72,13 @@ def values(v, vs, unit):
 
 
 def attention(K, V, table, P, T, q, kb, vb, scale=None, masked=()):
-    """K, V float64 [N][H][64][D]; the rest as paged_ref.attention.  (out, lse)."""
+    """K, V float64 [N][H][64][D]; the rest as paged_ref.attention.  (out, lse, and the weighted mean distance of
+    the values from the output, by which an error of the weights moves it)."""
     B, Tm, Hq, D = q.shape
     H = kb.shape[2]
     G = Hq // H
     scale = 1 / math.sqrt(D) if scale is None else scale
-    out, lse = np.zeros((B, Tm, Hq, D)), np.full((B, Hq, Tm), -np.inf)
+    out, lse, dev = np.zeros((B, Tm, Hq, D)), np.full((B, Hq, Tm), -np.inf), np.zeros((B, Tm, Hq, D))
     for b in range(B):
         tiles = [(table[b, t], min(PAGE, int(P[b]) - t * PAGE)) for t in range(-(-int(P[b]) // PAGE))
                  if (b, t) not in masked]
@@ -90,9 +91,12 @@ def attention(K, V, table, P, T, q, kb, vb, scale=None, masked=()):
                 m = s.max(1, keepdims=True)
                 w = np.exp(s - m)
                 l = w.sum(1, keepdims=True)
-                out[b, i, h * G:(h + 1) * G] = w @ v / l
+                o = w @ v / l
+                out[b, i, h * G:(h + 1) * G] = o
                 lse[b, h * G:(h + 1) * G, i] = (m + np.log(l))[:, 0]
-    return out, lse
+                for g in range(G):
+                    dev[b, i, h * G + g] = w[g] @ np.abs(v - o[g]) / l[g]
+    return out, lse, dev
 
 
 TWO_PI = 2 * Fraction(314159265358979323846264338327950288419716939937510, 10 ** 50)
