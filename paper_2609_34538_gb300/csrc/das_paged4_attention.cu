@@ -214,20 +214,25 @@ __device__ __forceinline__ uint32_t key_chunk(int t, int c) {
     constexpr int kTokens = 256 / D;  // tokens to a row
     return chunk16(t / kTokens, (t % kTokens) * (8 / kTokens) + c);
 }
-__device__ __forceinline__ void st_shared(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w)
-                 : "memory");
-}
 // Eight bf16 elements in the order that a word of eight codes is widened in.
 __device__ __forceinline__ uint4 paired(uint4 x) {
     return make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632),
                       __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
 }
-// Four pairs 128 + c of a word's codes.
-__device__ __forceinline__ void widen(uint32_t w, uint32_t (&h)[4]) {
+// Four pairs 128 + c of a word's codes.  (The masks are registers, so that both take one
+// instruction.)
+struct Widen {
+    uint32_t mask, base;
+    __device__ __forceinline__ Widen() {
+        asm volatile("mov.u32 %0, 0x000f000f;" : "=r"(mask));
+        asm volatile("mov.u32 %0, 0x43004300;" : "=r"(base));
+    }
+    __device__ __forceinline__ void operator()(uint32_t w, uint32_t (&h)[4]) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = (w >> (4 * i) & 0x000f000fu) | 0x43004300u;
-}
+        for (int i = 0; i < 4; ++i)
+            asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(h[i]) : "r"(w >> (4 * i)), "r"(mask), "r"(base));
+    }
+};
 __device__ __forceinline__ uint32_t ordered(float x) {
     const uint32_t u = __float_as_uint(x);
     return u >> 31 ? ~u : u | 0x80000000u;
@@ -249,15 +254,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                    b_qready = b_empty + 8 * kStages, b_qfree = b_qready + 16, b_kready = b_qfree + 16,
                    b_vready = b_kready + 16, b_sdone = b_vready + 16, b_sfree = b_sdone + 16,
                    b_pready = b_sfree + 16, b_pvdone = b_pready + 16, b_drain = b_pvdone + 16;
-    int2 *info = reinterpret_cast<int2 *>(sm + Lt::kInfoOff);
-    float *s_off = reinterpret_cast<float *>(sm + Lt::kRowOff), *s_alpha = s_off + 64,
-          *s_inv = s_off + 128, *s_lse = s_off + 192;
-    float *s_sum = reinterpret_cast<float *>(sm + Lt::kSumOff);
-    uint32_t *s_vsx = reinterpret_cast<uint32_t *>(sm + Lt::kVsxOff);
-    int *s_nf = reinterpret_cast<int *>(sm + Lt::kNfOff);
-    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(sm + Lt::kMiscOff);
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(sm + Lt::kMiscOff + 4);
-    volatile int *s_ticket = reinterpret_cast<volatile int *>(sm + Lt::kMiscOff + 8);
+    const uint32_t infos = sbase + Lt::kInfoOff, tmem_slot = sbase + Lt::kMiscOff,
+                   abort_flag = tmem_slot + 4, s_ticket = tmem_slot + 8, s_nf = sbase + Lt::kNfOff;
+    // of the rows: minus the reference, a factor or the rounded weights' sum, 1 / l, lse
+    const uint32_t s_off = sbase + Lt::kRowOff, s_alpha = s_off + 256, s_inv = s_off + 512, s_lse = s_off + 768;
     Plan *s_plan = reinterpret_cast<Plan *>(sm + Lt::kMiscOff + 16);
     static_assert(sizeof(Plan) <= 112, "plan");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -279,19 +279,19 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(b_drain + 8 * i, 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        *abort_flag = 0;
+        sts(abort_flag, 0);
     }
     if (warp == kSWarp) {
         asm volatile(
             "tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
-                smem_u32(const_cast<uint32_t *>(tmem_slot))),
+                tmem_slot),
             "n"(kCols));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     if (warp == kProducerWarp && elect_one())
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tm_k)) : "memory");
     for (int i = threadIdx.x; i < 2048 / 16; i += kThreads)
-        st_shared(sbase + Lt::kOnesOff + 16 * i, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+        sts4(sbase + Lt::kOnesOff + 16 * i, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
     fence_async_smem();
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -307,12 +307,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_before();
     __syncthreads();
     fence_after();
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = lds(tmem_slot);
     Walk w = s_plan->w;
     const int ntiles = s_plan->ntiles;
 
     auto waits = [&](uint32_t bar, uint32_t parity) {
-        return wait(bar, parity, abort_flag, p.status);
+        return suspend(bar, parity, abort_flag, p.status);
     };
     // Tile k of the range has buffers k % 2; of its prefix tiles, the kp-th has stage kp % kStages.
     auto half_of = [](int k) { return (uint32_t)(k >> 1) & 1; };
@@ -345,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         ok = waits(b_empty + 8 * st, (uint32_t)(loaded / kStages - 1) & 1);
                     if (!ok) break;
                     if (elect_one()) {
-                        info[loaded % kInfos] = make_int2(n0, n1);
+                        sts2(infos + loaded % kInfos * 8, n0, n1);
                         const uint32_t full = b_full + 8 * st, dst = sbase + st * Lt::kStage;
                         mbar_arrive_expect_tx(full, ((p0 >= 0) + (p1 >= 0)) * 2 * (Lt::kCodes + Lt::kScales));
 #pragma unroll
@@ -426,7 +426,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int quad = warp - kValueWarp0, d = quad * 32 + lane;
         const uint32_t dst = tmem + kVCol + ((uint32_t)(quad * 32) << 16);
         const bool mine = d < D;  // (a whole warp's)
-        uint32_t *const scales = s_vsx + quad * 64;
+        const uint32_t scales = sbase + Lt::kVsxOff + quad * 256;
+        const Widen widen;
         if (!mine) {
             uint32_t one[32];
 #pragma unroll
@@ -442,50 +443,47 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int s = k & 1;
                 if (i < sg.pre) {
                     const int st = kp % kStages;
-                    const uint8_t *stage = sm + st * Lt::kStage;
+                    const uint32_t stage = sbase + st * Lt::kStage;
                     ok = waits(b_full + 8 * st, (uint32_t)(kp / kStages) & 1);
                     if (!ok) break;
                     if (mine) {
                         // the scales of this warp's elements, in pairs of keys: columns 2 lane and 2 lane + 1
                         // are keys 8 o + q and 8 o + q + 4, q = 2 (lane % 2) and one more
-                        const int2 n = info[kp % kInfos];
-                        const int o = lane >> 1, pg = o >> 3, left = (pg ? n.y : n.x) - (o & 7) * 8;
-                        uint2 by = *reinterpret_cast<const uint2 *>(stage + Lt::kVsOff + pg * Lt::kScales + quad * kPage +
-                                                                    (o & 7) * 8);
+                        const uint2 n = lds2(infos + kp % kInfos * 8);
+                        const int o = lane >> 1, pg = o >> 3, left = (int)(pg ? n.y : n.x) - (o & 7) * 8;
+                        uint2 by = lds2(stage + Lt::kVsOff + pg * Lt::kScales + quad * kPage + (o & 7) * 8);
                         if (left < 8) {  // places past the last token may hold anything
                             const unsigned long long keep = left <= 0 ? 0 : (1ull << 8 * left) - 1;
                             by.x &= (uint32_t)keep;
                             by.y &= (uint32_t)(keep >> 32);
                         }
                         const int q = 16 * (lane & 1);
-                        uint2 x;
-                        x.x = pack_bf16(scale_of(by.x >> q & 0xffu), scale_of(by.y >> q & 0xffu));
-                        x.y = pack_bf16(scale_of(by.x >> (q + 8) & 0xffu), scale_of(by.y >> (q + 8) & 0xffu));
                         __syncwarp();
-                        *reinterpret_cast<uint2 *>(scales + 2 * lane) = x;
+                        sts2(scales + 8 * lane, pack_bf16(scale_of(by.x >> q & 0xffu), scale_of(by.y >> q & 0xffu)),
+                             pack_bf16(scale_of(by.x >> (q + 8) & 0xffu), scale_of(by.y >> (q + 8) & 0xffu)));
                         __syncwarp();
                     }
                     if (k >= 2) ok = waits(b_pvdone + 8 * s, half_of(k) ^ 1);
                     if (!ok) break;
                     fence_after();
                     if (mine) {
+                        const uint32_t m8 = 0xc308c308u;  // -136
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {  // half a page's keys: 16 columns
+                            uint32_t r[16];
+                            const uint32_t words = stage + Lt::kVOff + c * (Lt::kCodes / 2) + d * 4;
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) {  // a page's 64 keys: 32 columns
-                            uint32_t r[32];
-#pragma unroll
-                            for (int o = 0; o < 8; ++o) {
-                                const uint32_t word = *reinterpret_cast<const uint32_t *>(
-                                    stage + Lt::kVOff + c * Lt::kCodes + (o * D + d) * 4);
-                                const uint4 x = *reinterpret_cast<const uint4 *>(scales + 32 * c + 4 * o);
+                            for (int o = 0; o < 4; ++o) {
+                                const uint32_t word = lds(words + o * D * 4);
+                                const uint4 x = lds4(scales + 64 * c + 16 * o);
                                 uint32_t h[4];
                                 widen(word, h);
-                                const uint32_t m8 = 0xc308c308u;  // -136
                                 r[4 * o] = bf16_mul2(bf16_add2(h[0], m8), x.x);
                                 r[4 * o + 1] = bf16_mul2(bf16_add2(h[1], m8), x.y);
                                 r[4 * o + 2] = bf16_mul2(bf16_add2(h[2], m8), x.z);
                                 r[4 * o + 3] = bf16_mul2(bf16_add2(h[3], m8), x.w);
                             }
-                            st_lanes(dst + 64 * s + 32 * c, r);
+                            st_lanes(dst + 64 * s + 16 * c, r);
                         }
                     }
                     __syncwarp();
@@ -517,7 +515,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                             for (int j = 0; j < 4; ++j) r[4 * o + j] = pack_bf16(x[j] * unit, x[j + 4] * unit);
                         }
-                        s_nf[d] = nf;
+                        sts(s_nf + 4 * d, nf);
                         st_lanes(dst + 64 * s, r);
                     }
                 }
@@ -531,6 +529,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // ======================== queries; keys, widened =========================
         // Thread (warp, lane): a key of the tile.
         const int quad = warp - kKeyWarp0, key = quad * 32 + lane;
+        const Widen widen;
         const uint32_t dst = tmem + kKCol + ((uint32_t)(quad * 32) << 16);
         int k = 0, kp = 0;
         bool ok = true;
@@ -550,7 +549,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         x = *reinterpret_cast<const uint4 *>(
                             p.q + (((size_t)w.b * p.max_block + r / p.G) * p.Hq + w.h * p.G + r % p.G) * D + c * 8);
                     x = paired(x);
-                    st_shared(q + (c >> 3) * (N * 128) + chunk16(r, c & 7), x.x, x.y, x.z, x.w);
+                    sts4(q + (c >> 3) * (N * 128) + chunk16(r, c & 7), x.x, x.y, x.z, x.w);
                 }
                 fence_async_smem();
                 __syncwarp();
@@ -567,18 +566,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (!ok) break;
                     fence_after();
                     const int pg = key / kPage, t = key % kPage;
-                    uint32_t by;
-                    if (D == 128)
-                        by = *reinterpret_cast<const uint32_t *>(sm + st * Lt::kStage + Lt::kKsOff + pg * Lt::kScales + t * 4);
-                    else
-                        by = *reinterpret_cast<const uint16_t *>(sm + st * Lt::kStage + Lt::kKsOff + pg * Lt::kScales + t * 2);
-#pragma unroll
-                    for (int c = 0; c < D / 32; ++c) {  // 32 elements under a scale
-                        uint4 x;
-                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                     : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
-                                     : "r"(stage + pg * Lt::kCodes + key_chunk<D>(t, c)));
-                        const float f = scale_of(by >> (8 * c) & 0xffu);
+                    const uint32_t at_scale = stage + Lt::kKsOff + pg * Lt::kScales + t * (D / 32);
+                    uint32_t by = D == 128 ? lds(at_scale) : lds(at_scale & ~3u) >> (8 * (at_scale & 2));
+#pragma unroll 1
+                    for (int c = 0; c < D / 32; ++c, by >>= 8) {  // 32 elements under a scale
+                        const uint4 x = lds4(stage + pg * Lt::kCodes + key_chunk<D>(t, c));
+                        const float f = scale_of(by & 0xffu);
                         const uint32_t sc = pack_bf16(f, f), m8 = bf16_mul2(sc, 0xc308c308u);
                         const uint32_t word[4] = {x.x, x.y, x.z, x.w};
                         uint32_t r[16];
@@ -628,8 +621,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int bar = 1 + group, row0 = group * R;
         const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
         const int place = (key & ~7) | (key & 3) << 1 | (key >> 2 & 1);  // of the key among P's rows
-        float *const off = s_off + row0, *const alpha = s_alpha + row0;
-        float *const sums = s_sum + warp * 32, *const group_sums = s_sum + group * kGroupWarps * 32;
+        const uint32_t off = s_off + 4 * row0, alpha = s_alpha + 4 * row0;
+        const uint32_t group_sums = sbase + Lt::kSumOff + group * (kGroupWarps * 128), sums = group_sums + quad * 128;
         auto group_sync = [&] { asm volatile("bar.sync %0, 128;" ::"r"(bar) : "memory"); };
         auto all_sync = [&] { asm volatile("bar.sync 3, 256;" ::: "memory"); };
         long long q_pair = s_plan->q;
@@ -645,70 +638,69 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int i = 0; i < sg.n; ++i, ++k) {
                 const int s = k & 1;
                 const bool blk = i >= sg.pre;
-                int2 n = make_int2(0, 0);
+                uint2 n = make_uint2(0, 0);
                 const bool ok = waits(b_sdone + 8 * s, half_of(k));
                 fence_after();
-                uint32_t a[R];
-                ld_lanes(lanes + kSCol + 64 * s + row0, a);
+                const float sc = blk ? p.scale_log2 : sc_page;
                 if (!blk) {
-                    n = info[kp % kInfos];
+                    n = lds2(infos + kp % kInfos * 8);
                     ++kp;
                 }
-                ld_wait(a);
-                fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(b_sfree + 8 * s);
-                const float sc = blk ? p.scale_log2 : sc_page;
-                if (blk) {  // the causal mask: key i is seen by the rows from i G on
-                    const int from = ok && key < w.T ? key * p.G : N;
+                uint32_t a[R];  // scores, then weights
+                auto scores = [&] {
+                    ld_lanes(lanes + kSCol + 64 * s + row0, a);
+                    ld_wait(a);
+                    if (blk) {  // the causal mask: key i is seen by the rows from i G on
+                        const int from = ok && key < w.T ? key * p.G : N;
 #pragma unroll
-                    for (int j = 0; j < R; ++j)
-                        if (row0 + j < from || row0 + j >= rows) a[j] = 0xff800000u;
-                } else if (n.x < kPage || n.y < kPage) {
-                    if (!ok || key % kPage >= (key < kPage ? n.x : n.y))
+                        for (int j = 0; j < R; ++j)
+                            if (row0 + j < from || row0 + j >= rows) a[j] = 0xff800000u;
+                    } else if (n.x < kPage || n.y < kPage || !ok) {
+                        if (!ok || key % kPage >= (int)(key < kPage ? n.x : n.y))
 #pragma unroll
-                        for (int j = 0; j < R; ++j) a[j] = 0xff800000u;
-                }
-                if (!has_ref) {
-                    // the segment's first key that is seen, if this tile has one
-                    const int first = blk ? 0 : n.x > 0 ? 0 : n.y > 0 ? kPage : -1;
-                    if (first >= 0) {
-                        if (key == first)
-#pragma unroll
-                            for (int j = 0; j < R; ++j) {
-                                const float m = __uint_as_float(a[j]) * sc;
-                                off[j] = (fabsf(m) < INFINITY ? -m : 0.f) - kBelow;
-                            }
-                        group_sync();
-                        has_ref = true;
-                    }
-                }
-                float e[R];
-                uint32_t pk[R / 2], big = 0;
-                auto weights = [&] {
-#pragma unroll
-                    for (int j = 0; j < R; j += 4) {
-                        const float4 o = *reinterpret_cast<const float4 *>(off + j);
-                        axpy2(e[j], e[j + 1], sc, __uint_as_float(a[j]), __uint_as_float(a[j + 1]), o.x, o.y);
-                        axpy2(e[j + 2], e[j + 3], sc, __uint_as_float(a[j + 2]), __uint_as_float(a[j + 3]), o.z, o.w);
-                    }
-                    big = 0;
-#pragma unroll
-                    for (int j = 0; j < R; ++j) e[j] = ex2(e[j]);
-#pragma unroll
-                    for (int j = 0; j < R / 2; ++j) {
-                        pk[j] = pack_bf16(e[2 * j], e[2 * j + 1]);
-                        big |= pk[j];
+                            for (int j = 0; j < R; ++j) a[j] = 0xff800000u;
                     }
                 };
-                if (has_ref) {
-                    weights();
-                } else {  // nothing is seen yet
+                scores();
+                if (!has_ref) {
+                    // the segment's first key that is seen, if this tile has one
+                    const int first = blk || n.x > 0 ? 0 : n.y > 0 ? kPage : -1;
+                    if (key == max(first, 0))
 #pragma unroll
-                    for (int j = 0; j < R; ++j) e[j] = 0.f;
-#pragma unroll
-                    for (int j = 0; j < R / 2; ++j) pk[j] = 0;
+                        for (int j = 0; j < R; ++j) {
+                            const float m = __uint_as_float(a[j]) * sc;
+                            stsf(off + 4 * j, (fabsf(m) < INFINITY ? -m : 0.f) - kBelow);
+                        }
+                    group_sync();
+                    has_ref = first >= 0;
                 }
+                if (k >= 2) waits(b_pvdone + 8 * s, half_of(k) ^ 1);  // P's buffer is free
+                const uint32_t dst = sbase + Lt::kPOff + s * Lt::kP;
+                uint32_t big;
+                auto weights = [&] {
+                    big = 0;
+#pragma unroll
+                    for (int j = 0; j < R; j += 8) {
+                        const uint4 o = lds4(off + 4 * j), o2 = lds4(off + 4 * j + 16);
+                        const uint32_t os[8] = {o.x, o.y, o.z, o.w, o2.x, o2.y, o2.z, o2.w};
+                        float e[8];
+#pragma unroll
+                        for (int t = 0; t < 8; t += 2)
+                            axpy2(e[t], e[t + 1], sc, __uint_as_float(a[j + t]), __uint_as_float(a[j + t + 1]),
+                                  __uint_as_float(os[t]), __uint_as_float(os[t + 1]));
+                        uint32_t pk[4];
+#pragma unroll
+                        for (int t = 0; t < 8; ++t) {
+                            e[t] = ex2(e[t]);
+                            a[j + t] = __float_as_uint(e[t]);
+                        }
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) pk[t] = pack_bf16(e[2 * t], e[2 * t + 1]);
+                        big |= pk[0] | pk[1] | pk[2] | pk[3];
+                        sts4(dst + chunk16(place, (row0 + j) / 8), pk[0], pk[1], pk[2], pk[3]);
+                    }
+                };
+                weights();
                 uint32_t over;
                 asm volatile(
                     "{\n .reg .pred p, q;\n setp.ne.b32 p, %1, 0;\n"
@@ -717,52 +709,55 @@ __global__ void __launch_bounds__(kThreads, 1)
                     : "r"(big & 0x40004000u), "r"(bar)
                     : "memory");
                 if (over) {  // a weight of 2 or more: the references are set to the tile's largest
-#pragma unroll
+                    scores();
+#pragma unroll 1
                     for (int j = 0; j < R; ++j) {
-                        const float x = __uint_as_float(a[j]) * sc;
+                        float x = 0.f;
+#pragma unroll
+                        for (int t = 0; t < R; ++t)
+                            if (t == j) x = __uint_as_float(a[t]) * sc;
                         const uint32_t m = __reduce_max_sync(kFull, ordered(x == x ? x : -INFINITY));
-                        if (lane == 0) sums[j] = unordered(m);
+                        if (lane == 0) stsf(sums + 4 * j, unordered(m));
                     }
                     group_sync();
                     if (quad == 0 && lane < R) {
                         float m = -INFINITY;
-                        for (int v = 0; v < kGroupWarps; ++v) m = fmaxf(m, group_sums[v * 32 + lane]);
-                        const float was = off[lane], now = fminf(was, (m < INFINITY ? -m : 0.f) - kBelow);
-                        off[lane] = now;
-                        alpha[lane] = ex2(now - was);
+                        for (int v = 0; v < kGroupWarps; ++v) m = fmaxf(m, ldsf(group_sums + v * 128 + 4 * lane));
+                        const float was = ldsf(off + 4 * lane), now = fminf(was, (m < INFINITY ? -m : 0.f) - kBelow);
+                        stsf(off + 4 * lane, now);
+                        stsf(alpha + 4 * lane, ex2(now - was));
                     }
                     group_sync();
                     if (i > 0) {
                         waits(b_pvdone + 8 * (s ^ 1), half_of(k - 1));
                         fence_after();
-                        uint32_t o[R];
-                        auto rescale = [&](uint32_t col) {
-                            ld_lanes(lanes + col + row0, o);
+#pragma unroll 1
+                        for (int c = 0; c < (D == 128 ? 2 : 1) * R; c += 8) {
+                            const uint32_t col = lanes + (c < R ? kOCol + c : kSumCol + c - R) + row0;
+                            uint32_t o[8];
+                            ld_lanes(col, o);
                             ld_wait(o);
 #pragma unroll
-                            for (int j = 0; j < R; ++j)
-                                o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha[j]);
-                            st_lanes(lanes + col + row0, o);
-                        };
-                        rescale(kOCol);
-                        if (D == 128) rescale(kSumCol);
+                            for (int j = 0; j < 8; ++j)
+                                o[j] = __float_as_uint(__uint_as_float(o[j]) * ldsf(alpha + 4 * (c % R + j)));
+                            st_lanes(col, o);
+                        }
                         st_wait();
                     }
 #pragma unroll
-                    for (int j = 0; j < R; ++j) l[j] *= alpha[j];
+                    for (int j = 0; j < R; ++j) l[j] *= ldsf(alpha + 4 * j);
                     weights();
                 }
 #pragma unroll
-                for (int j = 0; j < R; j += 2) add2(l[j], l[j + 1], l[j], l[j + 1], e[j], e[j + 1]);
-                if (k >= 2) waits(b_pvdone + 8 * s, half_of(k) ^ 1);
-                const uint32_t dst = sbase + Lt::kPOff + s * Lt::kP;
-#pragma unroll
-                for (int j = 0; j < R / 8; ++j)
-                    st_shared(dst + chunk16(place, row0 / 8 + j), pk[4 * j], pk[4 * j + 1], pk[4 * j + 2], pk[4 * j + 3]);
+                for (int j = 0; j < R; j += 2)
+                    add2(l[j], l[j + 1], l[j], l[j + 1], __uint_as_float(a[j]), __uint_as_float(a[j + 1]));
                 fence_async_smem();
                 fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(b_pready + 8 * s);
+                if (lane == 0) {
+                    mbar_arrive(b_sfree + 8 * s);
+                    mbar_arrive(b_pready + 8 * s);
+                }
             }
 
             // ---- the end of a segment: O / l and lse, as output or as a partial ----
@@ -785,60 +780,68 @@ __global__ void __launch_bounds__(kThreads, 1)
                             }
                     }
                 }
-                if (lane < R) sums[lane] = l[0];
+                if (lane < R) stsf(sums + 4 * lane, l[0]);
             }
             const int last = (k - 1) & 1;
             waits(b_pvdone + 8 * last, half_of(k - 1));
             fence_after();
             if (quad == (D == 128 ? 0 : 2)) {  // the sums of the rounded weights, in any lane that has them
-                uint32_t o[R];
-                ld_lanes(lanes + (D == 128 ? kSumCol : kOCol) + row0, o);
-                ld_wait(o);
-                if (lane == 0)
+#pragma unroll 1
+                for (int c = 0; c < R; c += 8) {
+                    uint32_t o[8];
+                    ld_lanes(lanes + (D == 128 ? kSumCol : kOCol) + row0 + c, o);
+                    ld_wait(o);
+                    if (lane == 0)
 #pragma unroll
-                    for (int j = 0; j < R; ++j) alpha[j] = __uint_as_float(o[j]);
+                        for (int j = 0; j < 8; ++j) sts(alpha + 4 * (c + j), o[j]);
+                }
             }
             group_sync();
             const bool has_blk = sg.n > sg.pre, whole = seg_t == 0 && has_blk;
             const float vu = unit_of(p.v_unit, w.h);
             if (quad == 0 && lane < R) {
                 float sum = 0.f;
-                for (int v = 0; v < kGroupWarps; ++v) sum += group_sums[v * 32 + lane];
+                for (int v = 0; v < kGroupWarps; ++v) sum += ldsf(group_sums + v * 128 + 4 * lane);
                 // no visible key: 0 and -inf; NaN stays NaN
-                s_inv[row0 + lane] = sum == 0.f ? 0.f : vu / alpha[lane];
-                s_lse[row0 + lane] = sum == 0.f || !has_ref ? -INFINITY : log2f(sum) - off[lane];
+                stsf(s_inv + 4 * (row0 + lane), sum == 0.f ? 0.f : vu / ldsf(alpha + 4 * lane));
+                stsf(s_lse + 4 * (row0 + lane), sum == 0.f || !has_ref ? -INFINITY : log2f(sum) - ldsf(off + 4 * lane));
             }
             group_sync();
             const size_t pair = (size_t)w.b * p.Hkv + w.h;
             const size_t slot = pair + blockIdx.x;
             if (quad * 32 < D) {
-                uint32_t o[R];
-                ld_lanes(lanes + kOCol + row0, o);
-                ld_wait(o);
-                const int nf = has_blk ? s_nf[key] : kKeys;  // (key: the element d here)
-                if (nf < kKeys)
+                const int nf = has_blk ? (int)lds(s_nf + 4 * key) : kKeys;  // (key: the element d here)
+#pragma unroll 1
+                for (int c = 0; c < R && row0 + c < p.rows_max; c += 8) {
+                    uint32_t o[8];
+                    ld_lanes(lanes + kOCol + row0 + c, o);
+                    ld_wait(o);
+                    float x[8];
 #pragma unroll
-                    for (int j = 0; j < R; ++j)
-                        if (row0 + j >= nf * p.G) o[j] = 0x7fffffffu;
-                if (whole) {
-#pragma unroll
-                    for (int j = 0; j < R; j += 2) {
-                        // lane d has rows j and j + 1 of element d: an even lane stores row j's two elements, an odd
-                        // one row j + 1's
-                        const float x = __uint_as_float(o[j]) * s_inv[row0 + j], y = __uint_as_float(o[j + 1]) * s_inv[row0 + j + 1];
-                        const bool odd = lane & 1;
-                        const float got = __shfl_xor_sync(kFull, odd ? x : y, 1);
-                        const int r = row0 + j + odd, i = r / p.G;
-                        if (r < p.rows_max)
-                            *reinterpret_cast<uint32_t *>(
-                                p.out + (((size_t)w.b * p.max_block + i) * p.Hq + w.h * p.G + r % p.G) * D + (key & ~1)) =
-                                r < rows ? (odd ? pack_bf16(got, y) : pack_bf16(x, got)) : 0u;
+                    for (int j = 0; j < 8; ++j) {
+                        const int r = row0 + c + j;
+                        x[j] = r >= nf * p.G ? __uint_as_float(0x7fffffffu) : __uint_as_float(o[j]) * ldsf(s_inv + 4 * r);
                     }
-                } else {
+                    if (whole) {
+                        // lane d has rows r and r + 1 of element d: an even lane stores row r's two elements, an
+                        // odd one row r + 1's
 #pragma unroll
-                    for (int j = 0; j < R; ++j)
-                        if (row0 + j < rows)
-                            p.part_o[(slot * p.rows_max + row0 + j) * D + key] = __uint_as_float(o[j]) * s_inv[row0 + j];
+                        for (int j = 0; j < 8; j += 2) {
+                            const bool odd = lane & 1;
+                            const float got = __shfl_xor_sync(kFull, odd ? x[j] : x[j + 1], 1);
+                            const int r = row0 + c + j + odd, i = r / p.G;
+                            if (r < p.rows_max)
+                                *reinterpret_cast<uint32_t *>(
+                                    p.out + (((size_t)w.b * p.max_block + i) * p.Hq + w.h * p.G + r % p.G) * D + (key & ~1)) =
+                                    r < rows ? (odd ? pack_bf16(got, x[j + 1]) : pack_bf16(x[j], got)) : 0u;
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const int r = row0 + c + j;
+                            if (r < rows) p.part_o[(slot * p.rows_max + r) * D + key] = x[j];
+                        }
+                    }
                 }
             }
             fence_before();
@@ -846,9 +849,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int r = row0 + lane;
                 if (whole)
                     p.lse[((size_t)w.b * p.Hq + w.h * p.G + r % p.G) * p.max_block + r / p.G] =
-                        r < rows ? s_lse[r] * kLn2 : -INFINITY;
+                        r < rows ? ldsf(s_lse + 4 * r) * kLn2 : -INFINITY;
                 else
-                    p.part_lse[slot * p.rows_max + r] = r < rows ? s_lse[r] : -INFINITY;
+                    p.part_lse[slot * p.rows_max + r] = r < rows ? ldsf(s_lse + 4 * r) : -INFINITY;
             }
             if (!whole) {
                 // ---- whoever comes last joins the pair's partials ----
@@ -867,10 +870,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (threadIdx.x == 0) {
                         const int t = atomicAdd(counter, 1);
                         if (t == count - 1) *counter = 0;
-                        *s_ticket = t == count - 1;
+                        sts(s_ticket, t == count - 1);
                     }
                     all_sync();
-                    const bool yes = *s_ticket;
+                    const bool yes = lds(s_ticket);
                     if (yes) __threadfence();
                     return yes;
                 };
@@ -941,7 +944,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_before();
     __syncthreads();
     fence_after();
-    if (*abort_flag) {  // a timed-out run: products and copies may be in flight yet
+    if (lds(abort_flag)) {  // a timed-out run: products and copies may be in flight yet
         if (warp == kSWarp || warp == kPvWarp) {
             const uint32_t drain = b_drain + (warp == kSWarp ? 8 : 0);
             if (elect_one()) mma_commit(drain);
