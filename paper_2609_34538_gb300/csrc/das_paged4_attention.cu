@@ -247,17 +247,19 @@ __global__ void __launch_bounds__(kThreads, 1)
     using Lt = Layout<D, N>;
     constexpr int kStages = Lt::kStages, R = N / 2;  // rows of a group
     extern __shared__ uint8_t smem_raw[];
-    uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
-                                              ~uintptr_t(1023));
+    uint8_t *const sm = smem_raw + (-smem_u32(smem_raw) & 1023u);
     const uint32_t sbase = smem_u32(sm);
     const uint32_t b_full = sbase + Lt::kBarOff, b_empty = b_full + 8 * kStages,
                    b_qready = b_empty + 8 * kStages, b_qfree = b_qready + 16, b_kready = b_qfree + 16,
                    b_vready = b_kready + 16, b_sdone = b_vready + 16, b_sfree = b_sdone + 16,
                    b_pready = b_sfree + 16, b_pvdone = b_pready + 16, b_drain = b_pvdone + 16;
-    const uint32_t infos = sbase + Lt::kInfoOff, tmem_slot = sbase + Lt::kMiscOff,
-                   abort_flag = tmem_slot + 4, s_ticket = tmem_slot + 8, s_nf = sbase + Lt::kNfOff;
+    int2 *const infos = reinterpret_cast<int2 *>(sm + Lt::kInfoOff);
+    volatile uint32_t *const misc = reinterpret_cast<volatile uint32_t *>(sm + Lt::kMiscOff);
+    volatile int *const abort_flag = reinterpret_cast<volatile int *>(sm + Lt::kMiscOff + 4);
+    int *const s_nf = reinterpret_cast<int *>(sm + Lt::kNfOff);
     // of the rows: minus the reference, a factor or the rounded weights' sum, 1 / l, lse
-    const uint32_t s_off = sbase + Lt::kRowOff, s_alpha = s_off + 256, s_inv = s_off + 512, s_lse = s_off + 768;
+    float *const s_off = reinterpret_cast<float *>(sm + Lt::kRowOff), *const s_alpha = s_off + 64,
+                 *const s_inv = s_off + 128, *const s_lse = s_off + 192;
     Plan *s_plan = reinterpret_cast<Plan *>(sm + Lt::kMiscOff + 16);
     static_assert(sizeof(Plan) <= 112, "plan");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -279,12 +281,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(b_drain + 8 * i, 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        sts(abort_flag, 0);
+        *abort_flag = 0;
     }
     if (warp == kSWarp) {
         asm volatile(
             "tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
-                tmem_slot),
+                sbase + Lt::kMiscOff),
             "n"(kCols));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
@@ -307,12 +309,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_before();
     __syncthreads();
     fence_after();
-    const uint32_t tmem = lds(tmem_slot);
+    const uint32_t tmem = misc[0];
     Walk w = s_plan->w;
     const int ntiles = s_plan->ntiles;
 
     auto waits = [&](uint32_t bar, uint32_t parity) {
-        return suspend(bar, parity, abort_flag, p.status);
+        return wait(bar, parity, abort_flag, p.status);
     };
     // Tile k of the range has buffers k % 2; of its prefix tiles, the kp-th has stage kp % kStages.
     auto half_of = [](int k) { return (uint32_t)(k >> 1) & 1; };
@@ -345,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         ok = waits(b_empty + 8 * st, (uint32_t)(loaded / kStages - 1) & 1);
                     if (!ok) break;
                     if (elect_one()) {
-                        sts2(infos + loaded % kInfos * 8, n0, n1);
+                        infos[loaded % kInfos] = make_int2(n0, n1);
                         const uint32_t full = b_full + 8 * st, dst = sbase + st * Lt::kStage;
                         mbar_arrive_expect_tx(full, ((p0 >= 0) + (p1 >= 0)) * 2 * (Lt::kCodes + Lt::kScales));
 #pragma unroll
@@ -426,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int quad = warp - kValueWarp0, d = quad * 32 + lane;
         const uint32_t dst = tmem + kVCol + ((uint32_t)(quad * 32) << 16);
         const bool mine = d < D;  // (a whole warp's)
-        const uint32_t scales = sbase + Lt::kVsxOff + quad * 256;
+        uint32_t *const scales = reinterpret_cast<uint32_t *>(sm + Lt::kVsxOff) + quad * 64;
         const Widen widen;
         if (!mine) {
             uint32_t one[32];
@@ -443,15 +445,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int s = k & 1;
                 if (i < sg.pre) {
                     const int st = kp % kStages;
-                    const uint32_t stage = sbase + st * Lt::kStage;
+                    const uint8_t *const stage = sm + st * Lt::kStage;
                     ok = waits(b_full + 8 * st, (uint32_t)(kp / kStages) & 1);
                     if (!ok) break;
                     if (mine) {
                         // the scales of this warp's elements, in pairs of keys: columns 2 lane and 2 lane + 1
                         // are keys 8 o + q and 8 o + q + 4, q = 2 (lane % 2) and one more
-                        const uint2 n = lds2(infos + kp % kInfos * 8);
-                        const int o = lane >> 1, pg = o >> 3, left = (int)(pg ? n.y : n.x) - (o & 7) * 8;
-                        uint2 by = lds2(stage + Lt::kVsOff + pg * Lt::kScales + quad * kPage + (o & 7) * 8);
+                        const int2 n = infos[kp % kInfos];
+                        const int o = lane >> 1, pg = o >> 3, left = (pg ? n.y : n.x) - (o & 7) * 8;
+                        uint2 by = *reinterpret_cast<const uint2 *>(stage + Lt::kVsOff + pg * Lt::kScales + quad * kPage +
+                                                                    (o & 7) * 8);
                         if (left < 8) {  // places past the last token may hold anything
                             const unsigned long long keep = left <= 0 ? 0 : (1ull << 8 * left) - 1;
                             by.x &= (uint32_t)keep;
@@ -459,8 +462,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                         const int q = 16 * (lane & 1);
                         __syncwarp();
-                        sts2(scales + 8 * lane, pack_bf16(scale_of(by.x >> q & 0xffu), scale_of(by.y >> q & 0xffu)),
-                             pack_bf16(scale_of(by.x >> (q + 8) & 0xffu), scale_of(by.y >> (q + 8) & 0xffu)));
+                        reinterpret_cast<uint2 *>(scales)[lane] =
+                            make_uint2(pack_bf16(scale_of(by.x >> q & 0xffu), scale_of(by.y >> q & 0xffu)),
+                                       pack_bf16(scale_of(by.x >> (q + 8) & 0xffu), scale_of(by.y >> (q + 8) & 0xffu)));
                         __syncwarp();
                     }
                     if (k >= 2) ok = waits(b_pvdone + 8 * s, half_of(k) ^ 1);
@@ -471,11 +475,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
                         for (int c = 0; c < 4; ++c) {  // half a page's keys: 16 columns
                             uint32_t r[16];
-                            const uint32_t words = stage + Lt::kVOff + c * (Lt::kCodes / 2) + d * 4;
+                            const uint32_t *const words =
+                                reinterpret_cast<const uint32_t *>(stage + Lt::kVOff + c * (Lt::kCodes / 2)) + d;
 #pragma unroll
                             for (int o = 0; o < 4; ++o) {
-                                const uint32_t word = lds(words + o * D * 4);
-                                const uint4 x = lds4(scales + 64 * c + 16 * o);
+                                const uint32_t word = words[o * D];
+                                const uint4 x = reinterpret_cast<const uint4 *>(scales)[4 * c + o];
                                 uint32_t h[4];
                                 widen(word, h);
                                 r[4 * o] = bf16_mul2(bf16_add2(h[0], m8), x.x);
@@ -515,7 +520,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                             for (int j = 0; j < 4; ++j) r[4 * o + j] = pack_bf16(x[j] * unit, x[j + 4] * unit);
                         }
-                        sts(s_nf + 4 * d, nf);
+                        s_nf[d] = nf;
                         st_lanes(dst + 64 * s, r);
                     }
                 }
@@ -561,16 +566,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!ok) break;
                 if (i < sg.pre) {
                     const int st = kp % kStages;
-                    const uint32_t stage = sbase + st * Lt::kStage;
+                    const uint8_t *const stage = sm + st * Lt::kStage;
                     ok = waits(b_full + 8 * st, (uint32_t)(kp / kStages) & 1);
                     if (!ok) break;
                     fence_after();
                     const int pg = key / kPage, t = key % kPage;
-                    const uint32_t at_scale = stage + Lt::kKsOff + pg * Lt::kScales + t * (D / 32);
-                    uint32_t by = D == 128 ? lds(at_scale) : lds(at_scale & ~3u) >> (8 * (at_scale & 2));
+                    const uint8_t *const at_scale = stage + Lt::kKsOff + pg * Lt::kScales + t * (D / 32);
+                    uint32_t by = D == 128 ? *reinterpret_cast<const uint32_t *>(at_scale)
+                                           : *reinterpret_cast<const uint16_t *>(at_scale);
 #pragma unroll 1
                     for (int c = 0; c < D / 32; ++c, by >>= 8) {  // 32 elements under a scale
-                        const uint4 x = lds4(stage + pg * Lt::kCodes + key_chunk<D>(t, c));
+                        const uint4 x = *reinterpret_cast<const uint4 *>(stage + pg * Lt::kCodes + key_chunk<D>(t, c));
                         const float f = scale_of(by & 0xffu);
                         const uint32_t sc = pack_bf16(f, f), m8 = bf16_mul2(sc, 0xc308c308u);
                         const uint32_t word[4] = {x.x, x.y, x.z, x.w};
@@ -621,8 +627,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int bar = 1 + group, row0 = group * R;
         const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
         const int place = (key & ~7) | (key & 3) << 1 | (key >> 2 & 1);  // of the key among P's rows
-        const uint32_t off = s_off + 4 * row0, alpha = s_alpha + 4 * row0;
-        const uint32_t group_sums = sbase + Lt::kSumOff + group * (kGroupWarps * 128), sums = group_sums + quad * 128;
+        float *const off = s_off + row0, *const alpha = s_alpha + row0;
+        float *const group_sums = reinterpret_cast<float *>(sm + Lt::kSumOff) + group * (kGroupWarps * 32),
+                     *const sums = group_sums + quad * 32;
         auto group_sync = [&] { asm volatile("bar.sync %0, 128;" ::"r"(bar) : "memory"); };
         auto all_sync = [&] { asm volatile("bar.sync 3, 256;" ::: "memory"); };
         long long q_pair = s_plan->q;
@@ -638,12 +645,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int i = 0; i < sg.n; ++i, ++k) {
                 const int s = k & 1;
                 const bool blk = i >= sg.pre;
-                uint2 n = make_uint2(0, 0);
+                int2 n = make_int2(0, 0);
                 const bool ok = waits(b_sdone + 8 * s, half_of(k));
                 fence_after();
                 const float sc = blk ? p.scale_log2 : sc_page;
                 if (!blk) {
-                    n = lds2(infos + kp % kInfos * 8);
+                    n = infos[kp % kInfos];
                     ++kp;
                 }
                 uint32_t a[R];  // scores, then weights
@@ -656,7 +663,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         for (int j = 0; j < R; ++j)
                             if (row0 + j < from || row0 + j >= rows) a[j] = 0xff800000u;
                     } else if (n.x < kPage || n.y < kPage || !ok) {
-                        if (!ok || key % kPage >= (int)(key < kPage ? n.x : n.y))
+                        if (!ok || key % kPage >= (key < kPage ? n.x : n.y))
 #pragma unroll
                             for (int j = 0; j < R; ++j) a[j] = 0xff800000u;
                     }
@@ -669,7 +676,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                         for (int j = 0; j < R; ++j) {
                             const float m = __uint_as_float(a[j]) * sc;
-                            stsf(off + 4 * j, (fabsf(m) < INFINITY ? -m : 0.f) - kBelow);
+                            off[j] = (fabsf(m) < INFINITY ? -m : 0.f) - kBelow;
                         }
                     group_sync();
                     has_ref = first >= 0;
@@ -678,24 +685,23 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const uint32_t dst = sbase + Lt::kPOff + s * Lt::kP;
                 uint32_t big;
                 auto weights = [&] {
+                    // (all exponentials first, so that their chains overlap)
+#pragma unroll
+                    for (int j = 0; j < R; j += 4) {
+                        const float4 o = *reinterpret_cast<const float4 *>(off + j);
+                        float e[4];
+                        axpy2(e[0], e[1], sc, __uint_as_float(a[j]), __uint_as_float(a[j + 1]), o.x, o.y);
+                        axpy2(e[2], e[3], sc, __uint_as_float(a[j + 2]), __uint_as_float(a[j + 3]), o.z, o.w);
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) a[j + t] = __float_as_uint(ex2(e[t]));
+                    }
                     big = 0;
 #pragma unroll
                     for (int j = 0; j < R; j += 8) {
-                        const uint4 o = lds4(off + 4 * j), o2 = lds4(off + 4 * j + 16);
-                        const uint32_t os[8] = {o.x, o.y, o.z, o.w, o2.x, o2.y, o2.z, o2.w};
-                        float e[8];
-#pragma unroll
-                        for (int t = 0; t < 8; t += 2)
-                            axpy2(e[t], e[t + 1], sc, __uint_as_float(a[j + t]), __uint_as_float(a[j + t + 1]),
-                                  __uint_as_float(os[t]), __uint_as_float(os[t + 1]));
                         uint32_t pk[4];
 #pragma unroll
-                        for (int t = 0; t < 8; ++t) {
-                            e[t] = ex2(e[t]);
-                            a[j + t] = __float_as_uint(e[t]);
-                        }
-#pragma unroll
-                        for (int t = 0; t < 4; ++t) pk[t] = pack_bf16(e[2 * t], e[2 * t + 1]);
+                        for (int t = 0; t < 4; ++t)
+                            pk[t] = pack_bf16(__uint_as_float(a[j + 2 * t]), __uint_as_float(a[j + 2 * t + 1]));
                         big |= pk[0] | pk[1] | pk[2] | pk[3];
                         sts4(dst + chunk16(place, (row0 + j) / 8), pk[0], pk[1], pk[2], pk[3]);
                     }
@@ -717,15 +723,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                         for (int t = 0; t < R; ++t)
                             if (t == j) x = __uint_as_float(a[t]) * sc;
                         const uint32_t m = __reduce_max_sync(kFull, ordered(x == x ? x : -INFINITY));
-                        if (lane == 0) stsf(sums + 4 * j, unordered(m));
+                        if (lane == 0) sums[j] = unordered(m);
                     }
                     group_sync();
                     if (quad == 0 && lane < R) {
                         float m = -INFINITY;
-                        for (int v = 0; v < kGroupWarps; ++v) m = fmaxf(m, ldsf(group_sums + v * 128 + 4 * lane));
-                        const float was = ldsf(off + 4 * lane), now = fminf(was, (m < INFINITY ? -m : 0.f) - kBelow);
-                        stsf(off + 4 * lane, now);
-                        stsf(alpha + 4 * lane, ex2(now - was));
+                        for (int v = 0; v < kGroupWarps; ++v) m = fmaxf(m, group_sums[v * 32 + lane]);
+                        const float was = off[lane], now = fminf(was, (m < INFINITY ? -m : 0.f) - kBelow);
+                        off[lane] = now;
+                        alpha[lane] = ex2(now - was);
                     }
                     group_sync();
                     if (i > 0) {
@@ -739,13 +745,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                             ld_wait(o);
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
-                                o[j] = __float_as_uint(__uint_as_float(o[j]) * ldsf(alpha + 4 * (c % R + j)));
+                                o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha[c % R + j]);
                             st_lanes(col, o);
                         }
                         st_wait();
                     }
 #pragma unroll
-                    for (int j = 0; j < R; ++j) l[j] *= ldsf(alpha + 4 * j);
+                    for (int j = 0; j < R; ++j) l[j] *= alpha[j];
                     weights();
                 }
 #pragma unroll
@@ -780,7 +786,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             }
                     }
                 }
-                if (lane < R) stsf(sums + 4 * lane, l[0]);
+                if (lane < R) sums[lane] = l[0];
             }
             const int last = (k - 1) & 1;
             waits(b_pvdone + 8 * last, half_of(k - 1));
@@ -793,7 +799,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     ld_wait(o);
                     if (lane == 0)
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) sts(alpha + 4 * (c + j), o[j]);
+                        for (int j = 0; j < 8; ++j) alpha[c + j] = __uint_as_float(o[j]);
                 }
             }
             group_sync();
@@ -801,16 +807,16 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float vu = unit_of(p.v_unit, w.h);
             if (quad == 0 && lane < R) {
                 float sum = 0.f;
-                for (int v = 0; v < kGroupWarps; ++v) sum += ldsf(group_sums + v * 128 + 4 * lane);
+                for (int v = 0; v < kGroupWarps; ++v) sum += group_sums[v * 32 + lane];
                 // no visible key: 0 and -inf; NaN stays NaN
-                stsf(s_inv + 4 * (row0 + lane), sum == 0.f ? 0.f : vu / ldsf(alpha + 4 * lane));
-                stsf(s_lse + 4 * (row0 + lane), sum == 0.f || !has_ref ? -INFINITY : log2f(sum) - ldsf(off + 4 * lane));
+                s_inv[row0 + lane] = sum == 0.f ? 0.f : vu / alpha[lane];
+                s_lse[row0 + lane] = sum == 0.f || !has_ref ? -INFINITY : log2f(sum) - off[lane];
             }
             group_sync();
             const size_t pair = (size_t)w.b * p.Hkv + w.h;
             const size_t slot = pair + blockIdx.x;
             if (quad * 32 < D) {
-                const int nf = has_blk ? (int)lds(s_nf + 4 * key) : kKeys;  // (key: the element d here)
+                const int nf = has_blk ? s_nf[key] : kKeys;  // (key: the element d here)
 #pragma unroll 1
                 for (int c = 0; c < R && row0 + c < p.rows_max; c += 8) {
                     uint32_t o[8];
@@ -820,7 +826,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         const int r = row0 + c + j;
-                        x[j] = r >= nf * p.G ? __uint_as_float(0x7fffffffu) : __uint_as_float(o[j]) * ldsf(s_inv + 4 * r);
+                        x[j] = r >= nf * p.G ? __uint_as_float(0x7fffffffu) : __uint_as_float(o[j]) * s_inv[r];
                     }
                     if (whole) {
                         // lane d has rows r and r + 1 of element d: an even lane stores row r's two elements, an
@@ -849,9 +855,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int r = row0 + lane;
                 if (whole)
                     p.lse[((size_t)w.b * p.Hq + w.h * p.G + r % p.G) * p.max_block + r / p.G] =
-                        r < rows ? ldsf(s_lse + 4 * r) * kLn2 : -INFINITY;
+                        r < rows ? s_lse[r] * kLn2 : -INFINITY;
                 else
-                    p.part_lse[slot * p.rows_max + r] = r < rows ? ldsf(s_lse + 4 * r) : -INFINITY;
+                    p.part_lse[slot * p.rows_max + r] = r < rows ? s_lse[r] : -INFINITY;
             }
             if (!whole) {
                 // ---- whoever comes last joins the pair's partials ----
@@ -870,10 +876,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (threadIdx.x == 0) {
                         const int t = atomicAdd(counter, 1);
                         if (t == count - 1) *counter = 0;
-                        sts(s_ticket, t == count - 1);
+                        misc[2] = t == count - 1;
                     }
                     all_sync();
-                    const bool yes = lds(s_ticket);
+                    const bool yes = misc[2];
                     if (yes) __threadfence();
                     return yes;
                 };
@@ -944,7 +950,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_before();
     __syncthreads();
     fence_after();
-    if (lds(abort_flag)) {  // a timed-out run: products and copies may be in flight yet
+    if (*abort_flag) {  // a timed-out run: products and copies may be in flight yet
         if (warp == kSWarp || warp == kPvWarp) {
             const uint32_t drain = b_drain + (warp == kSWarp ? 8 : 0);
             if (elect_one()) mma_commit(drain);

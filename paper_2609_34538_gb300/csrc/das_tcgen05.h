@@ -68,37 +68,6 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int
                                      int32_t *status) {
     return mbar_try_wait(bar, parity) || wait_slow(bar, parity, abort_flag, status);
 }
-// The same with a thread suspended for up to 20 us at a time: polls of many waiting warps
-// take issue slots from those at work.
-__device__ __forceinline__ bool mbar_wait_try(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 20000;\n"
-        " selp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-static __device__ __noinline__ bool suspend_slow(uint32_t bar, uint32_t parity, uint32_t abort_flag,
-                                                 int32_t *status) {
-    const unsigned long long t0 = globaltimer();
-    for (;;) {
-        if (mbar_wait_try(bar, parity)) return true;
-        uint32_t aborted;
-        asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(aborted) : "r"(abort_flag) : "memory");
-        if (aborted) return false;
-        if (globaltimer() - t0 > kWaitNs) {
-            asm volatile("st.volatile.shared.u32 [%0], %1;" ::"r"(abort_flag), "r"(1) : "memory");
-            atomicOr(status, kStatusWaitTimeout);
-            return false;
-        }
-    }
-}
-__device__ __forceinline__ bool suspend(uint32_t bar, uint32_t parity, uint32_t abort_flag,
-                                        int32_t *status) {
-    return mbar_wait_try(bar, parity) || suspend_slow(bar, parity, abort_flag, status);
-}
 // On the abort path only: at most 20 ms for copies in flight to land.
 static __device__ __noinline__ void drain_wait(uint32_t bar, uint32_t parity) {
     const unsigned long long t0 = globaltimer();
@@ -336,32 +305,6 @@ __device__ __forceinline__ void st_lanes(uint32_t a, const uint32_t (&r)[32]) { 
 #undef DAS_R8
 
 // ---- shared memory by its address ---------------------------------------------------
-__device__ __forceinline__ uint32_t lds(uint32_t a) {
-    uint32_t v;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint2 lds2(uint32_t a) {
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint4 lds4(uint32_t a) {
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                 : "r"(a)
-                 : "memory");
-    return v;
-}
-__device__ __forceinline__ float ldsf(uint32_t a) { return __uint_as_float(lds(a)); }
-__device__ __forceinline__ void sts(uint32_t a, uint32_t v) {
-    asm volatile("st.shared.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
-}
-__device__ __forceinline__ void stsf(uint32_t a, float v) { sts(a, __float_as_uint(v)); }
-__device__ __forceinline__ void sts2(uint32_t a, uint32_t x, uint32_t y) {
-    asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(a), "r"(x), "r"(y) : "memory");
-}
 __device__ __forceinline__ void sts4(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w)
                  : "memory");
