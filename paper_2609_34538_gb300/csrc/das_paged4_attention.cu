@@ -67,17 +67,18 @@ struct Layout {
     static constexpr int kQ = N * D * 2, kP = kKeys * 128;
     static constexpr int kQOff = kStages * kStage;
     static constexpr int kPOff = kQOff + 2 * kQ;
-    static constexpr int kOnesOff = kPOff + 2 * kP;            // a 64 x 16 operand of ones
-    static constexpr int kBarOff = kOnesOff + 2048;
+    static constexpr int kOnesOff = kPOff + 2 * kP;            // an 8 x 16 operand of ones
+    static constexpr int kBarOff = kOnesOff + 256;
     // full, empty [kStages], qready, qfree [2], kready, vready, sdone, sfree, pready, pvdone [2],
     // drain [2]
     static constexpr int kBars = 2 * kStages + 4 + 12 + 2;
     static constexpr int kInfoOff = (kBarOff + 8 * kBars + 15) / 16 * 16;
     static constexpr int kRowOff = kInfoOff + kInfos * 8;      // floats: off, alpha, 1 / l, lse [64]
     static constexpr int kSumOff = kRowOff + 4 * 64 * 4;       // [8 warps][32]: sums or largest
-    static constexpr int kVsxOff = kSumOff + 8 * 32 * 4;       // [4 warps][64]: the values' scales
-    static constexpr int kNfOff = kVsxOff + 4 * 64 * 4;        // [128]: first key that is not finite
-    static constexpr int kMiscOff = kNfOff + 128 * 4;
+    static constexpr int kVsxOff = kSumOff + 8 * 32 * 4;       // [4 warps][64] pairs: the values' scales
+    static constexpr int kNfOff = kVsxOff + 4 * 64 * 8;        // [128]: first key that is not finite
+    static constexpr int kJoinOff = kNfOff + 128 * 4;
+    static constexpr int kMiscOff = kJoinOff + 64;
     static constexpr int kBytes = kMiscOff + 128 + 1024;       // + alignment slack
     static_assert(kBytes <= 232448, "shared memory per CTA");
 };
@@ -241,6 +242,85 @@ __device__ __forceinline__ float unordered(uint32_t u) {
     return __uint_as_float(u >> 31 ? u & 0x7fffffffu : ~u);
 }
 
+// A bounded wait (as t5::wait) that sleeps between its tries: what the many warps that wait would
+// poll away are issue slots of those that work.
+static __device__ __noinline__ bool sleep_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag,
+                                               int32_t *status) {
+    const unsigned long long t0 = globaltimer();
+    for (uint32_t it = 1;; ++it) {
+        if (mbar_try_wait(bar, parity)) return true;
+        __nanosleep(20);
+        if ((it & 15u) == 0) {
+            if (*abort_flag) return false;
+            if (globaltimer() - t0 > kWaitNs) {
+                *abort_flag = 1;
+                atomicOr(status, kStatusWaitTimeout);
+                return false;
+            }
+        }
+    }
+}
+
+// A run of a pair's partials to be joined: run r0 / run of n segments, CTA c0's first.
+struct Join {
+    int pair, rows, c0, n, run, r0;
+};
+// Partials at places first, first + step, ... of rows to the output, or into the first one.
+// out = sum_s 2^(lse_s - M) O_s / sum_s 2^(lse_s - M), lse = M + log2 of that sum.  (The whole CTA.)
+template <int D>
+__device__ void join(const Paged4AttnParams &p, const Join &jn, size_t first, int step, int count, bool final,
+                     float *lses) {
+    constexpr int kPer = D / 4;  // threads to a row
+    const int b = jn.pair / p.Hkv, h = jn.pair % p.Hkv;
+    const int all = final ? p.rows_max : jn.rows;
+    for (int u = threadIdx.x; u < all * kPer; u += kThreads) {
+        const int r = u / kPer, c = u % kPer * 4;
+        float M = -INFINITY, L = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s0 = 0; s0 < (r < jn.rows ? count : 0); s0 += kFan) {
+            float ls[kFan];
+            float4 x[kFan];
+#pragma unroll
+            for (int s = 0; s < kFan; ++s) {
+                ls[s] = -INFINITY;
+                x[s] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (s0 + s < count) {
+                    const size_t at = (first + (size_t)(s0 + s) * step) * p.rows_max + r;
+                    ls[s] = __ldcg(p.part_lse + at);
+                    x[s] = __ldcg(reinterpret_cast<const float4 *>(p.part_o + at * D + c));
+                }
+            }
+            float m = M;
+#pragma unroll
+            for (int s = 0; s < kFan; ++s) m = fmaxf(m, ls[s]);  // (NaN goes into the sums alone)
+            const float f = M == m ? 1.f : ex2(M - m);
+            M = m;
+            L *= f;
+            acc = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
+#pragma unroll
+            for (int s = 0; s < kFan; ++s) {
+                const float g = ls[s] == -INFINITY ? 0.f : ex2(ls[s] - m);
+                L += g;
+                acc = make_float4(acc.x + x[s].x * g, acc.y + x[s].y * g, acc.z + x[s].z * g, acc.w + x[s].w * g);
+            }
+        }
+        const float inv = L == 0.f ? 0.f : 1.f / L, lse = L == 0.f ? -INFINITY : M + log2f(L);
+        if (final) {
+            const int hq = h * p.G + r % p.G, i = r / p.G;
+            *reinterpret_cast<uint2 *>(p.out + (((size_t)b * p.max_block + i) * p.Hq + hq) * D + c) =
+                make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+            if (c == 0) p.lse[((size_t)b * p.Hq + hq) * p.max_block + i] = lse * kLn2;
+        } else {
+            *reinterpret_cast<float4 *>(p.part_o + (first * p.rows_max + r) * D + c) =
+                make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+            if (c == 0) lses[r] = lse;
+        }
+    }
+    if (final) return;
+    __syncthreads();  // all have read the first one's lse
+    for (int r = threadIdx.x; r < jn.rows; r += kThreads) p.part_lse[first * p.rows_max + r] = lses[r];
+}
+
 template <int D, int N>
 __global__ void __launch_bounds__(kThreads, 1)
     paged4_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const Paged4AttnParams p) {
@@ -260,6 +340,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // of the rows: minus the reference, a factor or the rounded weights' sum, 1 / l, lse
     float *const s_off = reinterpret_cast<float *>(sm + Lt::kRowOff), *const s_alpha = s_off + 64,
                  *const s_inv = s_off + 128, *const s_lse = s_off + 192;
+    Join *const s_joins = reinterpret_cast<Join *>(sm + Lt::kJoinOff);  // [2]: cut pairs of a CTA
     Plan *s_plan = reinterpret_cast<Plan *>(sm + Lt::kMiscOff + 16);
     static_assert(sizeof(Plan) <= 112, "plan");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -292,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     if (warp == kProducerWarp && elect_one())
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tm_k)) : "memory");
-    for (int i = threadIdx.x; i < 2048 / 16; i += kThreads)
+    for (int i = threadIdx.x; i < 256 / 16; i += kThreads)
         sts4(sbase + Lt::kOnesOff + 16 * i, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
     fence_async_smem();
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -314,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int ntiles = s_plan->ntiles;
 
     auto waits = [&](uint32_t bar, uint32_t parity) {
-        return wait(bar, parity, abort_flag, p.status);
+        return mbar_try_wait(bar, parity) || sleep_wait(bar, parity, abort_flag, p.status);
     };
     // Tile k of the range has buffers k % 2; of its prefix tiles, the kp-th has stage kp % kStages.
     auto half_of = [](int k) { return (uint32_t)(k >> 1) & 1; };
@@ -397,7 +478,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
     } else if (warp == kPvWarp) {
         // ============================ O^T += V^T P^T =============================
-        constexpr uint32_t id = idesc_bf16(kKeys, N, 0, 1), id_sum = idesc_bf16(64, N, 0, 1);
+        constexpr uint32_t id = idesc_bf16(kKeys, N, 0, 1), id_sum = idesc_bf16(64, 8, 1, 0);
         const uint64_t ones = sdesc(sbase + Lt::kOnesOff, 128, 256, 0);
         bool ok = true;
         int k = 0;
@@ -414,9 +495,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int kk = 0; kk < steps; ++kk)
                         mma_bf16_ta(tmem + kOCol, tmem + kVCol + 64 * s + 8 * kk, dp + ((kk * 2048) >> 4), id,
                                     i > 0 || kk > 0);
-                    if (D == 128)  // (with 64 elements, ones are beside them)
-                        for (int kk = 0; kk < steps; ++kk)
-                            mma_bf16(tmem + kSumCol, ones, dp + ((kk * 2048) >> 4), id_sum, i > 0 || kk > 0);
+                    for (int kk = 0; kk < steps; ++kk)
+                        mma_bf16(tmem + kSumCol, dp + ((kk * 2048) >> 4), ones, id_sum, i > 0 || kk > 0);
                     mma_commit(b_pvdone + 8 * s);
                 }
                 __syncwarp();
@@ -428,15 +508,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int quad = warp - kValueWarp0, d = quad * 32 + lane;
         const uint32_t dst = tmem + kVCol + ((uint32_t)(quad * 32) << 16);
         const bool mine = d < D;  // (a whole warp's)
-        uint32_t *const scales = reinterpret_cast<uint32_t *>(sm + Lt::kVsxOff) + quad * 64;
+        uint4 *const scales = reinterpret_cast<uint4 *>(sm + Lt::kVsxOff) + quad * 32;  // two columns each
         const Widen widen;
-        if (!mine) {
-            uint32_t one[32];
-#pragma unroll
-            for (int j = 0; j < 32; ++j) one[j] = 0x3f803f80u;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) st_lanes(dst + 32 * j, one);
-        }
         int k = 0, kp = 0;
         bool ok = true;
         for (; k < ntiles && ok; walk_pair(p, w)) {
@@ -462,16 +535,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                         const int q = 16 * (lane & 1);
                         __syncwarp();
-                        reinterpret_cast<uint2 *>(scales)[lane] =
-                            make_uint2(pack_bf16(scale_of(by.x >> q & 0xffu), scale_of(by.y >> q & 0xffu)),
-                                       pack_bf16(scale_of(by.x >> (q + 8) & 0xffu), scale_of(by.y >> (q + 8) & 0xffu)));
+                        const uint32_t x0 = pack_bf16(scale_of(by.x >> q & 0xffu), scale_of(by.y >> q & 0xffu));
+                        const uint32_t x1 = pack_bf16(scale_of(by.x >> (q + 8) & 0xffu), scale_of(by.y >> (q + 8) & 0xffu));
+                        scales[lane] = make_uint4(x0, bf16_mul2(x0, 0xc308c308u), x1, bf16_mul2(x1, 0xc308c308u));  // -136
                         __syncwarp();
                     }
                     if (k >= 2) ok = waits(b_pvdone + 8 * s, half_of(k) ^ 1);
                     if (!ok) break;
                     fence_after();
                     if (mine) {
-                        const uint32_t m8 = 0xc308c308u;  // -136
 #pragma unroll 1
                         for (int c = 0; c < 4; ++c) {  // half a page's keys: 16 columns
                             uint32_t r[16];
@@ -480,13 +552,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                             for (int o = 0; o < 4; ++o) {
                                 const uint32_t word = words[o * D];
-                                const uint4 x = reinterpret_cast<const uint4 *>(scales)[4 * c + o];
+                                const uint4 x = scales[8 * c + 2 * o], y = scales[8 * c + 2 * o + 1];
                                 uint32_t h[4];
                                 widen(word, h);
-                                r[4 * o] = bf16_mul2(bf16_add2(h[0], m8), x.x);
-                                r[4 * o + 1] = bf16_mul2(bf16_add2(h[1], m8), x.y);
-                                r[4 * o + 2] = bf16_mul2(bf16_add2(h[2], m8), x.z);
-                                r[4 * o + 3] = bf16_mul2(bf16_add2(h[3], m8), x.w);
+                                r[4 * o] = bf16_fma2(h[0], x.x, x.y);
+                                r[4 * o + 1] = bf16_fma2(h[1], x.z, x.w);
+                                r[4 * o + 2] = bf16_fma2(h[2], y.x, y.y);
+                                r[4 * o + 3] = bf16_fma2(h[3], y.z, y.w);
                             }
                             st_lanes(dst + 64 * s + 16 * c, r);
                         }
@@ -628,11 +700,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
         const int place = (key & ~7) | (key & 3) << 1 | (key >> 2 & 1);  // of the key among P's rows
         float *const off = s_off + row0, *const alpha = s_alpha + row0;
+        // the row whose sum this lane has, in the group's column of the eight equal ones
+        const int sum_row = 16 * quad + lane;
+        const bool mine = lane < 16 && sum_row >= row0 && sum_row < row0 + R;
         float *const group_sums = reinterpret_cast<float *>(sm + Lt::kSumOff) + group * (kGroupWarps * 32),
                      *const sums = group_sums + quad * 32;
         auto group_sync = [&] { asm volatile("bar.sync %0, 128;" ::"r"(bar) : "memory"); };
         auto all_sync = [&] { asm volatile("bar.sync 3, 256;" ::: "memory"); };
         long long q_pair = s_plan->q;
+        int joins = 0;  // (thread 0's)
         int k = 0, kp = 0;
         for (; k < ntiles; q_pair += w.nt + kEnd, walk_pair(p, w)) {
             const Segment sg = segment_of(w, ntiles - k);
@@ -705,6 +781,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         big |= pk[0] | pk[1] | pk[2] | pk[3];
                         sts4(dst + chunk16(place, (row0 + j) / 8), pk[0], pk[1], pk[2], pk[3]);
                     }
+                    fence_async_smem();
                 };
                 weights();
                 uint32_t over;
@@ -738,32 +815,36 @@ __global__ void __launch_bounds__(kThreads, 1)
                         waits(b_pvdone + 8 * (s ^ 1), half_of(k - 1));
                         fence_after();
 #pragma unroll 1
-                        for (int c = 0; c < (D == 128 ? 2 : 1) * R; c += 8) {
-                            const uint32_t col = lanes + (c < R ? kOCol + c : kSumCol + c - R) + row0;
+                        for (int c = 0; c < R; c += 8) {
+                            const uint32_t col = lanes + kOCol + c + row0;
                             uint32_t o[8];
                             ld_lanes(col, o);
                             ld_wait(o);
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
-                                o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha[c % R + j]);
+                                o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha[c + j]);
                             st_lanes(col, o);
                         }
+                        uint32_t o[1];
+                        ld_lanes(lanes + kSumCol + group, o);
+                        ld_wait(o);
+                        if (mine) o[0] = __float_as_uint(__uint_as_float(o[0]) * s_alpha[sum_row]);
+                        st_lanes(lanes + kSumCol + group, o);
                         st_wait();
                     }
 #pragma unroll
                     for (int j = 0; j < R; ++j) l[j] *= alpha[j];
                     weights();
+                    __syncwarp();
                 }
-#pragma unroll
-                for (int j = 0; j < R; j += 2)
-                    add2(l[j], l[j + 1], l[j], l[j + 1], __uint_as_float(a[j]), __uint_as_float(a[j + 1]));
-                fence_async_smem();
                 fence_before();
-                __syncwarp();
                 if (lane == 0) {
                     mbar_arrive(b_sfree + 8 * s);
                     mbar_arrive(b_pready + 8 * s);
                 }
+#pragma unroll
+                for (int j = 0; j < R; j += 2)
+                    add2(l[j], l[j + 1], l[j], l[j + 1], __uint_as_float(a[j]), __uint_as_float(a[j + 1]));
             }
 
             // ---- the end of a segment: O / l and lse, as output or as a partial ----
@@ -791,16 +872,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int last = (k - 1) & 1;
             waits(b_pvdone + 8 * last, half_of(k - 1));
             fence_after();
-            if (quad == (D == 128 ? 0 : 2)) {  // the sums of the rounded weights, in any lane that has them
-#pragma unroll 1
-                for (int c = 0; c < R; c += 8) {
-                    uint32_t o[8];
-                    ld_lanes(lanes + (D == 128 ? kSumCol : kOCol) + row0 + c, o);
-                    ld_wait(o);
-                    if (lane == 0)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) alpha[c + j] = __uint_as_float(o[j]);
-                }
+            {  // the sums of the rounded weights
+                uint32_t o[1];
+                ld_lanes(lanes + kSumCol + group, o);
+                ld_wait(o);
+                if (mine) s_alpha[sum_row] = __uint_as_float(o[0]);
             }
             group_sync();
             const bool has_blk = sg.n > sg.pre, whole = seg_t == 0 && has_blk;
@@ -860,9 +936,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     p.part_lse[slot * p.rows_max + r] = r < rows ? s_lse[r] : -INFINITY;
             }
             if (!whole) {
-                // ---- whoever comes last joins the pair's partials ----
-                // With more than kFan of them, runs of about as many as there are runs are joined first,
-                // each into its first place.
+                // Whoever comes last at its run's counter joins the run when its tiles are done.
+                // With more than kFan partials a pair's are cut into runs of about as many as there are runs.
                 const Plan &pl = *s_plan;
                 const int c0 = cta_of(pl, q_pair), n = cta_of(pl, q_pair + w.nt - 1) - c0 + 1;
                 int run = n;
@@ -870,82 +945,21 @@ __global__ void __launch_bounds__(kThreads, 1)
                     run = 2;
                     while (run * run < n) ++run;
                 }
-                auto last_of = [&](int32_t *counter, int count) {
-                    __threadfence();
-                    all_sync();
-                    if (threadIdx.x == 0) {
-                        const int t = atomicAdd(counter, 1);
-                        if (t == count - 1) *counter = 0;
-                        misc[2] = t == count - 1;
+                const int r0 = ((int)blockIdx.x - c0) / run * run, count = min(run, n - r0);
+                __threadfence();
+                all_sync();
+                if (threadIdx.x == 0) {
+                    int32_t *const counter = p.count_run + pair + c0 + r0;
+                    if (atomicAdd(counter, 1) == count - 1) {
+                        *counter = 0;
+                        __threadfence();
+                        s_joins[joins++] = {(int)pair, rows, c0, n, run, r0};
                     }
-                    all_sync();
-                    const bool yes = misc[2];
-                    if (yes) __threadfence();
-                    return yes;
-                };
-                // partials at places first, first + step, ...: to the output, or into the first
-                auto join = [&](size_t first, int step, int count, bool final) {
-                    constexpr int kPer = D / 4;  // threads to a row
-                    for (int r0 = 0; r0 < p.rows_max; r0 += 256 / kPer) {
-                        const int r = r0 + threadIdx.x / kPer, c = threadIdx.x % kPer * 4;
-                        float M = -INFINITY, L = 0.f;
-                        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-                        if (r < rows) {
-                            for (int j0 = 0; j0 < count; j0 += 4) {
-                                float ls[4];
-                                float4 x[4];
-#pragma unroll
-                                for (int j = 0; j < 4; ++j) {
-                                    ls[j] = -INFINITY;
-                                    x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-                                    if (j0 + j < count) {
-                                        const size_t at = (first + (size_t)(j0 + j) * step) * p.rows_max + r;
-                                        ls[j] = __ldcg(p.part_lse + at);
-                                        x[j] = __ldcg(reinterpret_cast<const float4 *>(p.part_o + at * D + c));
-                                    }
-                                }
-#pragma unroll
-                                for (int j = 0; j < 4; ++j) {
-                                    if (ls[j] == -INFINITY) continue;
-                                    // (NaN goes into the sums, not into the reference)
-                                    const float m = fmaxf(M, ls[j]);
-                                    const float f = M == m ? 1.f : ex2(M - m), g = m == ls[j] ? 1.f : ex2(ls[j] - m);
-                                    M = m;
-                                    L = L * f + g;
-                                    acc.x = acc.x * f + x[j].x * g;
-                                    acc.y = acc.y * f + x[j].y * g;
-                                    acc.z = acc.z * f + x[j].z * g;
-                                    acc.w = acc.w * f + x[j].w * g;
-                                }
-                            }
-                        }
-                        const float inv = L == 0.f ? 0.f : 1.f / L, lse = L == 0.f ? -INFINITY : M + log2f(L);
-                        if (final) {
-                            if (r < p.rows_max) {
-                                const int hq = w.h * p.G + r % p.G, i = r / p.G;
-                                *reinterpret_cast<uint2 *>(p.out + (((size_t)w.b * p.max_block + i) * p.Hq + hq) * D + c) =
-                                    make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-                                if (c == 0) p.lse[((size_t)w.b * p.Hq + hq) * p.max_block + i] = lse * kLn2;
-                            }
-                        } else {
-                            all_sync();  // the row's threads have read its lse
-                            if (r < rows) {
-                                const size_t at = first * p.rows_max + r;
-                                *reinterpret_cast<float4 *>(p.part_o + at * D + c) =
-                                    make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-                                if (c == 0) p.part_lse[at] = lse;
-                            }
-                        }
-                    }
-                };
-                const int mine = (int)blockIdx.x - c0, r0 = mine / run * run, runs = (n + run - 1) / run;
-                if (last_of(p.count_run + pair + c0 + r0, min(run, n - r0))) {
-                    join(pair + c0 + r0, 1, min(run, n - r0), runs == 1);
-                    if (runs > 1 && last_of(p.count_pair + pair, runs)) join(pair + c0, run, runs, true);
                 }
             }
             group_sync();  // the rows' arrays may be written again
         }
+        if (threadIdx.x == 0) misc[2] = joins;
     }
     fence_before();
     __syncthreads();
@@ -968,6 +982,25 @@ __global__ void __launch_bounds__(kThreads, 1)
     // (else the softmax warps have seen every product's completion)
     if (warp == kSWarp)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kCols));
+    // ---- partials joined, by all of the CTA ----
+    for (int j = 0, n = misc[2]; j < n; ++j) {
+        const Join jn = s_joins[j];
+        const size_t first = (size_t)jn.pair + jn.c0;
+        const int runs = (jn.n + jn.run - 1) / jn.run;
+        join<D>(p, jn, first + jn.r0, 1, min(jn.run, jn.n - jn.r0), runs == 1, s_off);
+        if (runs == 1) continue;
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            int32_t *const counter = p.count_pair + jn.pair;
+            const bool last = atomicAdd(counter, 1) == runs - 1;
+            if (last) *counter = 0;
+            __threadfence();
+            misc[3] = last;
+        }
+        __syncthreads();
+        if (misc[3]) join<D>(p, jn, first, jn.run, runs, true, s_off);
+    }
 }
 
 size_t round256(size_t n) { return (n + 255) & ~size_t(255); }

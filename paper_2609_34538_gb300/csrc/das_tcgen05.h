@@ -266,6 +266,12 @@ __device__ __forceinline__ void st_lanes32(uint32_t a, const uint32_t (&r)[32]) 
         : "memory");
 }
 // The same for fewer columns, loads without a wait (as ld_half).
+__device__ __forceinline__ void ld_lanes(uint32_t a, uint32_t (&r)[1]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r[0]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void st_lanes(uint32_t a, const uint32_t (&r)[1]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(a), "r"(r[0]) : "memory");
+}
 __device__ __forceinline__ void ld_lanes(uint32_t a, uint32_t (&r)[8]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                  : DAS_R8(r, 0)
