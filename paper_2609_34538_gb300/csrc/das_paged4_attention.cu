@@ -46,8 +46,18 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kKeys = 128;  // of a tile: the rows of a product
 constexpr int kPage = DAS_PAGE_TOKENS;
 constexpr int kGroupWarps = 4, kSoftWarps = 8;
-constexpr int kKeyWarp0 = 8, kValueWarp0 = 12, kProducerWarp = 16, kSWarp = 17, kPvWarp = 18;
-constexpr int kThreads = 19 * 32;
+// The roles of a CTA's warps, for N columns.
+template <int N>
+struct Roles {
+    // With few rows the two softmax groups take turns at the tiles, each with a reference, sums and an O
+    // of its own; with 64 each has half of every tile's rows.
+    static constexpr bool kTurns = N <= 32;
+    // Sets of four warps that widen keys, and of those that widen values: tile k is set k % kSets's.
+    static constexpr int kSets = N == 16 ? 2 : 1;
+    static constexpr int kKeyWarp0 = kSoftWarps, kValueWarp0 = kKeyWarp0 + 4 * kSets;
+    static constexpr int kProducerWarp = kValueWarp0 + 4 * kSets, kSWarp = kProducerWarp + 1;
+    static constexpr int kPvWarp = kSWarp + 1, kThreads = (kPvWarp + 1) * 32;
+};
 constexpr float kBelow = 60.f;
 // Tensor memory: keys [2], values [2], S [2], O, the sums of P.
 constexpr int kKCol = 0, kVCol = 128, kSCol = 256, kOCol = 384, kSumCol = 448, kCols = 512;
@@ -73,11 +83,11 @@ struct Layout {
     // drain [2]
     static constexpr int kBars = 2 * kStages + 4 + 12 + 2;
     static constexpr int kInfoOff = (kBarOff + 8 * kBars + 15) / 16 * 16;
-    static constexpr int kRowOff = kInfoOff + kInfos * 8;      // floats: off, alpha, 1 / l, lse [64]
-    static constexpr int kSumOff = kRowOff + 4 * 64 * 4;       // [8 warps][32]: sums or largest
-    static constexpr int kVsxOff = kSumOff + 8 * 32 * 4;       // [4 warps][64] pairs: the values' scales
-    static constexpr int kNfOff = kVsxOff + 4 * 64 * 8;        // [128]: first key that is not finite
-    static constexpr int kJoinOff = kNfOff + 128 * 4;
+    static constexpr int kRowOff = kInfoOff + kInfos * 8;      // floats of the rows: 4 x [2][64], [64]
+    static constexpr int kSumOff = kRowOff + 9 * 64 * 4;       // [8 warps][32]: sums or largest
+    static constexpr int kVsxOff = kSumOff + 8 * 32 * 4;       // [8 warps][64]: the values' scales
+    static constexpr int kNfOff = kVsxOff + 2 * 4 * 64 * 4;    // [4][128]: first key that is not finite
+    static constexpr int kJoinOff = kNfOff + 4 * 128 * 4;
     static constexpr int kMiscOff = kJoinOff + 64;
     static constexpr int kBytes = kMiscOff + 128 + 1024;       // + alignment slack
     static_assert(kBytes <= 232448, "shared memory per CTA");
@@ -273,15 +283,16 @@ __device__ void join(const Paged4AttnParams &p, const Join &jn, size_t first, in
     constexpr int kPer = D / 4;  // threads to a row
     const int b = jn.pair / p.Hkv, h = jn.pair % p.Hkv;
     const int all = final ? p.rows_max : jn.rows;
-    for (int u = threadIdx.x; u < all * kPer; u += kThreads) {
+    for (int u = threadIdx.x; u < all * kPer; u += blockDim.x) {
         const int r = u / kPer, c = u % kPer * 4;
         float M = -INFINITY, L = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int s0 = 0; s0 < (r < jn.rows ? count : 0); s0 += kFan) {
-            float ls[kFan];
-            float4 x[kFan];
+        constexpr int kLoads = 4;
+        for (int s0 = 0; s0 < (r < jn.rows ? count : 0); s0 += kLoads) {
+            float ls[kLoads];
+            float4 x[kLoads];
 #pragma unroll
-            for (int s = 0; s < kFan; ++s) {
+            for (int s = 0; s < kLoads; ++s) {
                 ls[s] = -INFINITY;
                 x[s] = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (s0 + s < count) {
@@ -292,13 +303,13 @@ __device__ void join(const Paged4AttnParams &p, const Join &jn, size_t first, in
             }
             float m = M;
 #pragma unroll
-            for (int s = 0; s < kFan; ++s) m = fmaxf(m, ls[s]);  // (NaN goes into the sums alone)
+            for (int s = 0; s < kLoads; ++s) m = fmaxf(m, ls[s]);  // (NaN goes into the sums alone)
             const float f = M == m ? 1.f : ex2(M - m);
             M = m;
             L *= f;
             acc = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
 #pragma unroll
-            for (int s = 0; s < kFan; ++s) {
+            for (int s = 0; s < kLoads; ++s) {
                 const float g = ls[s] == -INFINITY ? 0.f : ex2(ls[s] - m);
                 L += g;
                 acc = make_float4(acc.x + x[s].x * g, acc.y + x[s].y * g, acc.z + x[s].z * g, acc.w + x[s].w * g);
@@ -318,14 +329,20 @@ __device__ void join(const Paged4AttnParams &p, const Join &jn, size_t first, in
     }
     if (final) return;
     __syncthreads();  // all have read the first one's lse
-    for (int r = threadIdx.x; r < jn.rows; r += kThreads) p.part_lse[first * p.rows_max + r] = lses[r];
+    for (int r = threadIdx.x; r < jn.rows; r += blockDim.x) p.part_lse[first * p.rows_max + r] = lses[r];
 }
 
 template <int D, int N>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Roles<N>::kThreads, 1)
     paged4_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const Paged4AttnParams p) {
     using Lt = Layout<D, N>;
-    constexpr int kStages = Lt::kStages, R = N / 2;  // rows of a group
+    using Ro = Roles<N>;
+    constexpr bool kTurns = Ro::kTurns;
+    constexpr int kSets = Ro::kSets, kKeyWarp0 = Ro::kKeyWarp0, kValueWarp0 = Ro::kValueWarp0,
+                  kProducerWarp = Ro::kProducerWarp, kSWarp = Ro::kSWarp, kPvWarp = Ro::kPvWarp,
+                  kThreads = Ro::kThreads;
+    constexpr int kStages = Lt::kStages, R = kTurns ? N : N / 2;  // rows of a group
+    constexpr int kStep = kTurns ? 2 : 1;                         // from one tile of a group to its next
     extern __shared__ uint8_t smem_raw[];
     uint8_t *const sm = smem_raw + (-smem_u32(smem_raw) & 1023u);
     const uint32_t sbase = smem_u32(sm);
@@ -337,9 +354,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     volatile uint32_t *const misc = reinterpret_cast<volatile uint32_t *>(sm + Lt::kMiscOff);
     volatile int *const abort_flag = reinterpret_cast<volatile int *>(sm + Lt::kMiscOff + 4);
     int *const s_nf = reinterpret_cast<int *>(sm + Lt::kNfOff);
-    // of the rows: minus the reference, a factor or the rounded weights' sum, 1 / l, lse
-    float *const s_off = reinterpret_cast<float *>(sm + Lt::kRowOff), *const s_alpha = s_off + 64,
-                 *const s_inv = s_off + 128, *const s_lse = s_off + 192;
+    // of each group's rows: minus the reference, a factor or the rounded weights' sum, the weights' sum,
+    // the factor of the group's O; lse
+    float *const s_off = reinterpret_cast<float *>(sm + Lt::kRowOff), *const s_alpha = s_off + 128,
+                 *const s_total = s_off + 256, *const s_factor = s_off + 384, *const s_lse = s_off + 512;
     Join *const s_joins = reinterpret_cast<Join *>(sm + Lt::kJoinOff);  // [2]: cut pairs of a CTA
     Plan *s_plan = reinterpret_cast<Plan *>(sm + Lt::kMiscOff + 16);
     static_assert(sizeof(Plan) <= 112, "plan");
@@ -356,8 +374,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(b_kready + 8 * i, 4);
             mbar_init(b_vready + 8 * i, 4);
             mbar_init(b_sdone + 8 * i, 1);
-            mbar_init(b_sfree + 8 * i, kSoftWarps);
-            mbar_init(b_pready + 8 * i, kSoftWarps);
+            mbar_init(b_sfree + 8 * i, kTurns ? kGroupWarps : kSoftWarps);
+            mbar_init(b_pready + 8 * i, kTurns ? kGroupWarps : kSoftWarps);
             mbar_init(b_pvdone + 8 * i, 1);
             mbar_init(b_drain + 8 * i, 1);
         }
@@ -492,11 +510,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (elect_one()) {
                     const uint64_t dp = sdesc(sbase + Lt::kPOff + s * Lt::kP, Lt::kP, 1024, 2);
                     const int steps = i < sg.pre ? 8 : 4;  // (the block has 64 keys at most)
+                    const uint32_t dO = tmem + kOCol + (kTurns ? 32 * s : 0), d_sum = tmem + kSumCol + (kTurns ? 8 * s : 0);
                     for (int kk = 0; kk < steps; ++kk)
-                        mma_bf16_ta(tmem + kOCol, tmem + kVCol + 64 * s + 8 * kk, dp + ((kk * 2048) >> 4), id,
-                                    i > 0 || kk > 0);
+                        mma_bf16_ta(dO, tmem + kVCol + 64 * s + 8 * kk, dp + ((kk * 2048) >> 4), id,
+                                    i >= kStep || kk > 0);
                     for (int kk = 0; kk < steps; ++kk)
-                        mma_bf16(tmem + kSumCol, dp + ((kk * 2048) >> 4), ones, id_sum, i > 0 || kk > 0);
+                        mma_bf16(d_sum, dp + ((kk * 2048) >> 4), ones, id_sum, i >= kStep || kk > 0);
                     mma_commit(b_pvdone + 8 * s);
                 }
                 __syncwarp();
@@ -505,61 +524,77 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else if (warp >= kValueWarp0) {
         // ============================ values, widened ============================
         // Thread (warp, lane): element d of a value; 32 elements share a scale.
-        const int quad = warp - kValueWarp0, d = quad * 32 + lane;
+        const int quad = warp % 4, set = (warp - kValueWarp0) / 4, d = quad * 32 + lane;
         const uint32_t dst = tmem + kVCol + ((uint32_t)(quad * 32) << 16);
         const bool mine = d < D;  // (a whole warp's)
-        uint4 *const scales = reinterpret_cast<uint4 *>(sm + Lt::kVsxOff) + quad * 32;  // two columns each
+        // the warp's scales of a tile, in pairs of keys: columns 2 lane and 2 lane + 1 are keys 8 o + q and
+        // 8 o + q + 4, q = 2 (lane % 2) and one more
+        uint2 *const scales = reinterpret_cast<uint2 *>(sm + Lt::kVsxOff) + (warp - kValueWarp0) * 32;
+        const int at_o = lane >> 1, at_pg = at_o >> 3, at_q = 16 * (lane & 1);
         const Widen widen;
+        const uint32_t m8 = 0xc308c308u;  // -136
         int k = 0, kp = 0;
         bool ok = true;
         for (; k < ntiles && ok; walk_pair(p, w)) {
             const Segment sg = segment_of(w, ntiles - k);
             for (int i = 0; i < sg.n && ok; ++i, ++k) {
                 const int s = k & 1;
+                if (kSets == 2 && s != set) {
+                    kp += i < sg.pre;
+                    continue;
+                }
                 if (i < sg.pre) {
                     const int st = kp % kStages;
                     const uint8_t *const stage = sm + st * Lt::kStage;
                     ok = waits(b_full + 8 * st, (uint32_t)(kp / kStages) & 1);
                     if (!ok) break;
                     if (mine) {
-                        // the scales of this warp's elements, in pairs of keys: columns 2 lane and 2 lane + 1
-                        // are keys 8 o + q and 8 o + q + 4, q = 2 (lane % 2) and one more
                         const int2 n = infos[kp % kInfos];
-                        const int o = lane >> 1, pg = o >> 3, left = (pg ? n.y : n.x) - (o & 7) * 8;
-                        uint2 by = *reinterpret_cast<const uint2 *>(stage + Lt::kVsOff + pg * Lt::kScales + quad * kPage +
-                                                                    (o & 7) * 8);
+                        const int left = (at_pg ? n.y : n.x) - (at_o & 7) * 8;
+                        uint2 by = *reinterpret_cast<const uint2 *>(stage + Lt::kVsOff + at_pg * Lt::kScales +
+                                                                    quad * kPage + (at_o & 7) * 8);
                         if (left < 8) {  // places past the last token may hold anything
                             const unsigned long long keep = left <= 0 ? 0 : (1ull << 8 * left) - 1;
                             by.x &= (uint32_t)keep;
                             by.y &= (uint32_t)(keep >> 32);
                         }
-                        const int q = 16 * (lane & 1);
                         __syncwarp();
-                        const uint32_t x0 = pack_bf16(scale_of(by.x >> q & 0xffu), scale_of(by.y >> q & 0xffu));
-                        const uint32_t x1 = pack_bf16(scale_of(by.x >> (q + 8) & 0xffu), scale_of(by.y >> (q + 8) & 0xffu));
-                        scales[lane] = make_uint4(x0, bf16_mul2(x0, 0xc308c308u), x1, bf16_mul2(x1, 0xc308c308u));  // -136
+                        scales[lane] = make_uint2(
+                            pack_bf16(scale_of(by.x >> at_q & 0xffu), scale_of(by.y >> at_q & 0xffu)),
+                            pack_bf16(scale_of(by.x >> (at_q + 8) & 0xffu), scale_of(by.y >> (at_q + 8) & 0xffu)));
                         __syncwarp();
                     }
                     if (k >= 2) ok = waits(b_pvdone + 8 * s, half_of(k) ^ 1);
                     if (!ok) break;
                     fence_after();
                     if (mine) {
-#pragma unroll 1
-                        for (int c = 0; c < 4; ++c) {  // half a page's keys: 16 columns
-                            uint32_t r[16];
-                            const uint32_t *const words =
-                                reinterpret_cast<const uint32_t *>(stage + Lt::kVOff + c * (Lt::kCodes / 2)) + d;
+                        const uint32_t *words = reinterpret_cast<const uint32_t *>(stage + Lt::kVOff) + d;
+                        const uint4 *f = reinterpret_cast<const uint4 *>(scales);
+                        uint32_t word[4];
+                        uint4 sc[4];
+                        auto load = [&] {
 #pragma unroll
                             for (int o = 0; o < 4; ++o) {
-                                const uint32_t word = words[o * D];
-                                const uint4 x = scales[8 * c + 2 * o], y = scales[8 * c + 2 * o + 1];
-                                uint32_t h[4];
-                                widen(word, h);
-                                r[4 * o] = bf16_fma2(h[0], x.x, x.y);
-                                r[4 * o + 1] = bf16_fma2(h[1], x.z, x.w);
-                                r[4 * o + 2] = bf16_fma2(h[2], y.x, y.y);
-                                r[4 * o + 3] = bf16_fma2(h[3], y.z, y.w);
+                                word[o] = words[o * D];
+                                sc[o] = f[o];
                             }
+                            words += 4 * D;
+                            f += 4;
+                        };
+                        load();
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {  // half a page's keys: 16 columns
+                            uint32_t r[16];
+#pragma unroll
+                            for (int o = 0; o < 4; ++o) {
+                                uint32_t h[4];
+                                widen(word[o], h);
+                                r[4 * o] = bf16_mul2(bf16_add2(h[0], m8), sc[o].x);
+                                r[4 * o + 1] = bf16_mul2(bf16_add2(h[1], m8), sc[o].y);
+                                r[4 * o + 2] = bf16_mul2(bf16_add2(h[2], m8), sc[o].z);
+                                r[4 * o + 3] = bf16_mul2(bf16_add2(h[3], m8), sc[o].w);
+                            }
+                            if (c < 3) load();  // (no load is moved over a store)
                             st_lanes(dst + 64 * s + 16 * c, r);
                         }
                     }
@@ -573,27 +608,30 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (mine) {
                         const float unit = 1.f / unit_of(p.v_unit, w.h);
                         const uint16_t *src = p.v_blk + ((size_t)w.b * p.max_block * p.Hkv + w.h) * D + d;
-                        uint32_t r[32];
                         int nf = kKeys;
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {  // 16 keys: 8 columns
+                            uint32_t r[8];
 #pragma unroll
-                        for (int o = 0; o < 8; ++o) {
-                            float x[8];
+                            for (int o = 0; o < 2; ++o) {
+                                const int key = 16 * c + 8 * o;
+                                float x[8];
 #pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                x[j] = 8 * o + j < w.T
-                                           ? __uint_as_float((uint32_t)src[(size_t)(8 * o + j) * p.Hkv * D] << 16)
-                                           : 0.f;
+                                for (int j = 0; j < 8; ++j)
+                                    x[j] = key + j < w.T ? __uint_as_float((uint32_t)src[(size_t)(key + j) * p.Hkv * D] << 16)
+                                                         : 0.f;
 #pragma unroll
-                            for (int j = 7; j >= 0; --j)
-                                if (!(fabsf(x[j]) < INFINITY)) {
-                                    nf = min(nf, 8 * o + j);
-                                    x[j] = 0.f;
-                                }
+                                for (int j = 7; j >= 0; --j)
+                                    if (!(fabsf(x[j]) < INFINITY)) {
+                                        nf = min(nf, key + j);
+                                        x[j] = 0.f;
+                                    }
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) r[4 * o + j] = pack_bf16(x[j] * unit, x[j + 4] * unit);
+                                for (int j = 0; j < 4; ++j) r[4 * o + j] = pack_bf16(x[j] * unit, x[j + 4] * unit);
+                            }
+                            st_lanes(dst + 64 * s + 8 * c, r);
                         }
-                        s_nf[d] = nf;
-                        st_lanes(dst + 64 * s, r);
+                        s_nf[(k & 3) * kKeys + d] = nf;
                     }
                 }
                 st_wait();
@@ -605,16 +643,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else if (warp >= kKeyWarp0) {
         // ======================== queries; keys, widened =========================
         // Thread (warp, lane): a key of the tile.
-        const int quad = warp - kKeyWarp0, key = quad * 32 + lane;
+        const int quad = warp % 4, set = (warp - kKeyWarp0) / 4, key = quad * 32 + lane;
         const Widen widen;
         const uint32_t dst = tmem + kKCol + ((uint32_t)(quad * 32) << 16);
         int k = 0, kp = 0;
         bool ok = true;
         for (int seg = 0; k < ntiles && ok; ++seg, walk_pair(p, w)) {
             const Segment sg = segment_of(w, ntiles - k);
-            if (seg >= 2) ok = waits(b_qfree + 8 * (seg & 1), half_of(seg) ^ 1);
-            if (!ok) break;
-            {
+            if (kSets == 1 || (seg & 1) == set) {  // the queries
+                if (seg >= 2) ok = waits(b_qfree + 8 * (seg & 1), half_of(seg) ^ 1);
+                if (!ok) break;
                 const uint32_t q = sbase + Lt::kQOff + (seg & 1) * Lt::kQ;
                 constexpr int kPerRow = D / 8;
                 const int rows = p.G * w.T;
@@ -634,6 +672,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             for (int i = 0; i < sg.n && ok; ++i, ++k) {
                 const int s = k & 1;
+                if (kSets == 2 && s != set) {
+                    kp += i < sg.pre;
+                    continue;
+                }
                 if (k >= 2) ok = waits(b_sdone + 8 * s, half_of(k) ^ 1);
                 if (!ok) break;
                 if (i < sg.pre) {
@@ -646,9 +688,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const uint8_t *const at_scale = stage + Lt::kKsOff + pg * Lt::kScales + t * (D / 32);
                     uint32_t by = D == 128 ? *reinterpret_cast<const uint32_t *>(at_scale)
                                            : *reinterpret_cast<const uint16_t *>(at_scale);
-#pragma unroll 1
+                    uint4 codes[D / 32];
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c)
+                        codes[c] = *reinterpret_cast<const uint4 *>(stage + pg * Lt::kCodes + key_chunk<D>(t, c));
+#pragma unroll
                     for (int c = 0; c < D / 32; ++c, by >>= 8) {  // 32 elements under a scale
-                        const uint4 x = *reinterpret_cast<const uint4 *>(stage + pg * Lt::kCodes + key_chunk<D>(t, c));
+                        const uint4 x = codes[c];
                         const float f = scale_of(by & 0xffu);
                         const uint32_t sc = pack_bf16(f, f), m8 = bf16_mul2(sc, 0xc308c308u);
                         const uint32_t word[4] = {x.x, x.y, x.z, x.w};
@@ -695,41 +741,42 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
     } else {
         // ================================ softmax ================================
+        // Thread (warp, lane): a key of a tile; rows [row0, row0 + R).
         const int group = warp / kGroupWarps, quad = warp % kGroupWarps, key = quad * 32 + lane;
-        const int bar = 1 + group, row0 = group * R;
+        const int bar = 1 + group, row0 = kTurns ? 0 : group * R;
         const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
-        const int place = (key & ~7) | (key & 3) << 1 | (key >> 2 & 1);  // of the key among P's rows
-        float *const off = s_off + row0, *const alpha = s_alpha + row0;
-        // the row whose sum this lane has, in the group's column of the eight equal ones
+        const uint32_t o_col = lanes + kOCol + (kTurns ? 32 * group : row0);
+        // the row whose rounded weights' sum this lane has, in the group's one of the equal columns
+        const uint32_t sum_col = lanes + kSumCol + (kTurns ? 8 * group : group);
         const int sum_row = 16 * quad + lane;
-        const bool mine = lane < 16 && sum_row >= row0 && sum_row < row0 + R;
+        const bool sum_mine = lane < 16 && sum_row >= row0 && sum_row < row0 + R;
+        const int place = (key & ~7) | (key & 3) << 1 | (key >> 2 & 1);  // of the key among P's rows
+        float *const off = s_off + 64 * group, *const alpha = s_alpha + 64 * group;
         float *const group_sums = reinterpret_cast<float *>(sm + Lt::kSumOff) + group * (kGroupWarps * 32),
                      *const sums = group_sums + quad * 32;
         auto group_sync = [&] { asm volatile("bar.sync %0, 128;" ::"r"(bar) : "memory"); };
         auto all_sync = [&] { asm volatile("bar.sync 3, 256;" ::: "memory"); };
         long long q_pair = s_plan->q;
+        int k_seg = 0, kp_seg = 0;
         int joins = 0;  // (thread 0's)
-        int k = 0, kp = 0;
-        for (; k < ntiles; q_pair += w.nt + kEnd, walk_pair(p, w)) {
-            const Segment sg = segment_of(w, ntiles - k);
-            const int rows = p.G * w.T, seg_t = w.t;
+        for (; k_seg < ntiles; q_pair += w.nt + kEnd, walk_pair(p, w)) {
+            const Segment sg = segment_of(w, ntiles - k_seg);
+            const int rows = p.G * w.T;
             const float sc_page = fmaxf(p.scale_log2 * unit_of(p.k_unit, w.h), 1.2e-38f);
             float l[R];
 #pragma unroll
             for (int j = 0; j < R; ++j) l[j] = 0.f;
             bool has_ref = false;  // the same in the whole group
-            for (int i = 0; i < sg.n; ++i, ++k) {
-                const int s = k & 1;
+#pragma unroll 1
+            for (int i = kTurns ? (k_seg ^ group) & 1 : 0; i < sg.n; i += kStep) {
+                const int k = k_seg + i, s = k & 1;
                 const bool blk = i >= sg.pre;
-                int2 n = make_int2(0, 0);
                 const bool ok = waits(b_sdone + 8 * s, half_of(k));
                 fence_after();
-                const float sc = blk ? p.scale_log2 : sc_page;
-                if (!blk) {
-                    n = infos[kp % kInfos];
-                    ++kp;
-                }
                 uint32_t a[R];  // scores, then weights
+                const float sc = blk ? p.scale_log2 : sc_page;
+                int2 n = make_int2(0, 0);
+                if (!blk) n = infos[(kp_seg + i) % kInfos];
                 auto scores = [&] {
                     ld_lanes(lanes + kSCol + 64 * s + row0, a);
                     ld_wait(a);
@@ -752,7 +799,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                         for (int j = 0; j < R; ++j) {
                             const float m = __uint_as_float(a[j]) * sc;
-                            off[j] = (fabsf(m) < INFINITY ? -m : 0.f) - kBelow;
+                            off[row0 + j] = (fabsf(m) < INFINITY ? -m : 0.f) - kBelow;
                         }
                     group_sync();
                     has_ref = first >= 0;
@@ -764,7 +811,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     // (all exponentials first, so that their chains overlap)
 #pragma unroll
                     for (int j = 0; j < R; j += 4) {
-                        const float4 o = *reinterpret_cast<const float4 *>(off + j);
+                        const float4 o = *reinterpret_cast<const float4 *>(off + row0 + j);
                         float e[4];
                         axpy2(e[0], e[1], sc, __uint_as_float(a[j]), __uint_as_float(a[j + 1]), o.x, o.y);
                         axpy2(e[2], e[3], sc, __uint_as_float(a[j + 2]), __uint_as_float(a[j + 3]), o.z, o.w);
@@ -806,34 +853,33 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (quad == 0 && lane < R) {
                         float m = -INFINITY;
                         for (int v = 0; v < kGroupWarps; ++v) m = fmaxf(m, group_sums[v * 32 + lane]);
-                        const float was = off[lane], now = fminf(was, (m < INFINITY ? -m : 0.f) - kBelow);
-                        off[lane] = now;
-                        alpha[lane] = ex2(now - was);
+                        const float was = off[row0 + lane], now = fminf(was, (m < INFINITY ? -m : 0.f) - kBelow);
+                        off[row0 + lane] = now;
+                        alpha[row0 + lane] = ex2(now - was);
                     }
                     group_sync();
-                    if (i > 0) {
-                        waits(b_pvdone + 8 * (s ^ 1), half_of(k - 1));
+                    if (i >= kStep) {
+                        waits(b_pvdone + 8 * (k - kStep & 1), half_of(k - kStep));
                         fence_after();
 #pragma unroll 1
                         for (int c = 0; c < R; c += 8) {
-                            const uint32_t col = lanes + kOCol + c + row0;
                             uint32_t o[8];
-                            ld_lanes(col, o);
+                            ld_lanes(o_col + c, o);
                             ld_wait(o);
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
-                                o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha[c + j]);
-                            st_lanes(col, o);
+                                o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha[row0 + c + j]);
+                            st_lanes(o_col + c, o);
                         }
                         uint32_t o[1];
-                        ld_lanes(lanes + kSumCol + group, o);
+                        ld_lanes(sum_col, o);
                         ld_wait(o);
-                        if (mine) o[0] = __float_as_uint(__uint_as_float(o[0]) * s_alpha[sum_row]);
-                        st_lanes(lanes + kSumCol + group, o);
+                        if (sum_mine) o[0] = __float_as_uint(__uint_as_float(o[0]) * alpha[sum_row]);
+                        st_lanes(sum_col, o);
                         st_wait();
                     }
 #pragma unroll
-                    for (int j = 0; j < R; ++j) l[j] *= alpha[j];
+                    for (int j = 0; j < R; ++j) l[j] *= alpha[row0 + j];
                     weights();
                     __syncwarp();
                 }
@@ -849,61 +895,97 @@ __global__ void __launch_bounds__(kThreads, 1)
 
             // ---- the end of a segment: O / l and lse, as output or as a partial ----
             // l of row j over the warp's keys, in lane j (R lanes)
-            {
-                int n = R;
 #pragma unroll
-                for (int d = 16; d > 0; d >>= 1) {
-                    if (2 * d > R) {
+            for (int d = 16; d > 0; d >>= 1) {
+                if (2 * d > R) {
 #pragma unroll
-                        for (int j = 0; j < R; ++j) l[j] += __shfl_xor_sync(kFull, l[j], d);
-                    } else {
-                        n = d;
+                    for (int j = 0; j < R; ++j) l[j] += __shfl_xor_sync(kFull, l[j], d);
+                } else {
 #pragma unroll
-                        for (int j = 0; j < R / 2; ++j)
-                            if (j < d) {
-                                const bool up = lane & d;
-                                const float give = up ? l[j] : l[j + d], keep = up ? l[j + d] : l[j];
-                                l[j] = keep + __shfl_xor_sync(kFull, give, d);
-                            }
-                    }
+                    for (int j = 0; j < R / 2; ++j)
+                        if (j < d) {
+                            const bool up = lane & d;
+                            const float give = up ? l[j] : l[j + d], keep = up ? l[j + d] : l[j];
+                            l[j] = keep + __shfl_xor_sync(kFull, give, d);
+                        }
                 }
-                if (lane < R) sums[lane] = l[0];
             }
-            const int last = (k - 1) & 1;
-            waits(b_pvdone + 8 * last, half_of(k - 1));
-            fence_after();
-            {  // the sums of the rounded weights
+            if (lane < R) sums[lane] = l[0];
+            // with turns, a group may have none of the segment's tiles
+            const bool had = !kTurns || sg.n > 1 || (k_seg & 1) == group;
+            if (had) {
+                const int last = k_seg + sg.n - 1, mine = kTurns && (last & 1) != group ? last - 1 : last;
+                waits(b_pvdone + 8 * (mine & 1), half_of(mine));
+                fence_after();
                 uint32_t o[1];
-                ld_lanes(lanes + kSumCol + group, o);
+                ld_lanes(sum_col, o);
                 ld_wait(o);
-                if (mine) s_alpha[sum_row] = __uint_as_float(o[0]);
+                if (sum_mine) alpha[sum_row] = __uint_as_float(o[0]);
             }
             group_sync();
-            const bool has_blk = sg.n > sg.pre, whole = seg_t == 0 && has_blk;
-            const float vu = unit_of(p.v_unit, w.h);
             if (quad == 0 && lane < R) {
                 float sum = 0.f;
                 for (int v = 0; v < kGroupWarps; ++v) sum += group_sums[v * 32 + lane];
+                s_total[64 * group + row0 + lane] = had ? sum : 0.f;
+                if (!has_ref) off[row0 + lane] = INFINITY;
+                if (!had) alpha[row0 + lane] = 0.f;
+            }
+            // from here a group has the rows [orow0, orow0 + kOut) of the output
+            constexpr int kOut = N / 2;
+            const int orow0 = group * kOut;
+            if (kTurns) all_sync();
+            else group_sync();
+            const bool has_blk = sg.n > sg.pre, whole = w.t == 0 && has_blk;
+            if (quad == 0 && lane < kOut) {
+                const int r = orow0 + lane;
+                float f[2] = {0.f, 0.f}, total = 0.f, sum = 0.f, least;
+                if (kTurns) {  // both groups' under the larger reference
+                    least = fminf(s_off[r], s_off[64 + r]);
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        const float mine = s_off[64 * g + r];
+                        f[g] = mine == INFINITY ? 0.f : ex2(least - mine);
+                        total += f[g] * s_total[64 * g + r];
+                        sum += f[g] * s_alpha[64 * g + r];
+                    }
+                } else {
+                    least = off[r];
+                    f[0] = 1.f;
+                    total = s_total[64 * group + r];
+                    sum = alpha[r];
+                }
                 // no visible key: 0 and -inf; NaN stays NaN
-                s_inv[row0 + lane] = sum == 0.f ? 0.f : vu / alpha[lane];
-                s_lse[row0 + lane] = sum == 0.f || !has_ref ? -INFINITY : log2f(sum) - off[lane];
+                const float inv = total == 0.f ? 0.f : unit_of(p.v_unit, w.h) / sum;
+                s_factor[r] = f[0] * inv;
+                s_factor[64 + r] = f[1] * inv;
+                s_lse[r] = total == 0.f ? -INFINITY : log2f(total) - least;
             }
             group_sync();
             const size_t pair = (size_t)w.b * p.Hkv + w.h;
             const size_t slot = pair + blockIdx.x;
             if (quad * 32 < D) {
-                const int nf = has_blk ? s_nf[key] : kKeys;  // (key: the element d here)
+                const int k_last = k_seg + sg.n - 1;
+                const int nf = has_blk ? s_nf[(k_last & 3) * kKeys + key] : kKeys;  // (key: the element d here)
+                const bool two = kTurns && sg.n > 1, second = kTurns && (k_seg & 1);  // whose O the first tile's is
+                const float *const f0 = s_factor + (second ? 64 : 0), *const f1 = s_factor + (second ? 0 : 64);
+                const uint32_t o0 = lanes + kOCol + orow0 + (second ? 32 : 0), o1 = lanes + kOCol + orow0 + (second ? 0 : 32);
 #pragma unroll 1
-                for (int c = 0; c < R && row0 + c < p.rows_max; c += 8) {
+                for (int c = 0; c < kOut && orow0 + c < p.rows_max; c += 8) {
                     uint32_t o[8];
-                    ld_lanes(lanes + kOCol + row0 + c, o);
-                    ld_wait(o);
                     float x[8];
+                    ld_lanes(o0 + c, o);
+                    ld_wait(o);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int r = row0 + c + j;
-                        x[j] = r >= nf * p.G ? __uint_as_float(0x7fffffffu) : __uint_as_float(o[j]) * s_inv[r];
+                    for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(o[j]) * f0[orow0 + c + j];
+                    if (two) {
+                        ld_lanes(o1 + c, o);
+                        ld_wait(o);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) x[j] += __uint_as_float(o[j]) * f1[orow0 + c + j];
                     }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (orow0 + c + j >= nf * p.G) x[j] = __uint_as_float(0x7fffffffu);
                     if (whole) {
                         // lane d has rows r and r + 1 of element d: an even lane stores row r's two elements, an
                         // odd one row r + 1's
@@ -911,7 +993,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         for (int j = 0; j < 8; j += 2) {
                             const bool odd = lane & 1;
                             const float got = __shfl_xor_sync(kFull, odd ? x[j] : x[j + 1], 1);
-                            const int r = row0 + c + j + odd, i = r / p.G;
+                            const int r = orow0 + c + j + odd, i = r / p.G;
                             if (r < p.rows_max)
                                 *reinterpret_cast<uint32_t *>(
                                     p.out + (((size_t)w.b * p.max_block + i) * p.Hq + w.h * p.G + r % p.G) * D + (key & ~1)) =
@@ -920,22 +1002,23 @@ __global__ void __launch_bounds__(kThreads, 1)
                     } else {
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
-                            const int r = row0 + c + j;
+                            const int r = orow0 + c + j;
                             if (r < rows) p.part_o[(slot * p.rows_max + r) * D + key] = x[j];
                         }
                     }
                 }
             }
             fence_before();
-            if (quad == 3 && lane < R && row0 + lane < p.rows_max) {
-                const int r = row0 + lane;
+            if (quad == 3 && lane < kOut && orow0 + lane < p.rows_max) {
+                const int r = orow0 + lane;
                 if (whole)
                     p.lse[((size_t)w.b * p.Hq + w.h * p.G + r % p.G) * p.max_block + r / p.G] =
                         r < rows ? s_lse[r] * kLn2 : -INFINITY;
                 else
                     p.part_lse[slot * p.rows_max + r] = r < rows ? s_lse[r] : -INFINITY;
             }
-            if (!whole) {
+            all_sync();  // (the rows' arrays, and with turns the other group's O, may be written again)
+            if (!whole && threadIdx.x == 0) {
                 // Whoever comes last at its run's counter joins the run when its tiles are done.
                 // With more than kFan partials a pair's are cut into runs of about as many as there are runs.
                 const Plan &pl = *s_plan;
@@ -946,18 +1029,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                     while (run * run < n) ++run;
                 }
                 const int r0 = ((int)blockIdx.x - c0) / run * run, count = min(run, n - r0);
-                __threadfence();
-                all_sync();
-                if (threadIdx.x == 0) {
-                    int32_t *const counter = p.count_run + pair + c0 + r0;
-                    if (atomicAdd(counter, 1) == count - 1) {
-                        *counter = 0;
-                        __threadfence();
-                        s_joins[joins++] = {(int)pair, rows, c0, n, run, r0};
-                    }
+                __threadfence();  // (for the other threads' stores too, which the barrier puts before)
+                int32_t *const counter = p.count_run + pair + c0 + r0;
+                if (atomicAdd(counter, 1) == count - 1) {
+                    *counter = 0;
+                    __threadfence();
+                    s_joins[joins++] = {(int)pair, rows, c0, n, run, r0};
                 }
             }
-            group_sync();  // the rows' arrays may be written again
+            k_seg += sg.n;
+            kp_seg += sg.pre;
         }
         if (threadIdx.x == 0) misc[2] = joins;
     }
@@ -987,7 +1068,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const Join jn = s_joins[j];
         const size_t first = (size_t)jn.pair + jn.c0;
         const int runs = (jn.n + jn.run - 1) / jn.run;
-        join<D>(p, jn, first + jn.r0, 1, min(jn.run, jn.n - jn.r0), runs == 1, s_off);
+        join<D>(p, jn, first + jn.r0, 1, min(jn.run, jn.n - jn.r0), runs == 1, s_lse);
         if (runs == 1) continue;
         __threadfence();
         __syncthreads();
@@ -999,7 +1080,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             misc[3] = last;
         }
         __syncthreads();
-        if (misc[3]) join<D>(p, jn, first, jn.run, runs, true, s_off);
+        if (misc[3]) join<D>(p, jn, first, jn.run, runs, true, s_lse);
     }
 }
 
@@ -1019,7 +1100,7 @@ cudaError_t launch(const Paged4AttnParams &p, const CUtensorMap &tm_k, cudaStrea
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)p.num_ctas);
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(Roles<N>::kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
