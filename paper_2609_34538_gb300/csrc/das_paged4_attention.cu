@@ -52,10 +52,10 @@ struct Roles {
     // With few rows the two softmax groups take turns at the tiles, each with a reference, sums and an O
     // of its own; with 64 each has half of every tile's rows.
     static constexpr bool kTurns = N <= 32;
-    // Sets of four warps that widen keys, and of those that widen values: tile k is set k % kSets's.
-    static constexpr int kSets = N == 16 ? 2 : 1;
-    static constexpr int kKeyWarp0 = kSoftWarps, kValueWarp0 = kKeyWarp0 + 4 * kSets;
-    static constexpr int kProducerWarp = kValueWarp0 + 4 * kSets, kSWarp = kProducerWarp + 1;
+    // Sets of four warps that widen keys, and of those that widen values: tile k is set k % the sets' number's.
+    static constexpr int kKeySets = 1, kValueSets = N == 16 ? 2 : 1;
+    static constexpr int kKeyWarp0 = kSoftWarps, kValueWarp0 = kKeyWarp0 + 4 * kKeySets;
+    static constexpr int kProducerWarp = kValueWarp0 + 4 * kValueSets, kSWarp = kProducerWarp + 1;
     static constexpr int kPvWarp = kSWarp + 1, kThreads = (kPvWarp + 1) * 32;
 };
 constexpr float kBelow = 60.f;
@@ -66,6 +66,7 @@ constexpr int kInfos = 64;  // ring of the tiles' visible keys
 constexpr int kEnd = 4;
 constexpr int kLeast = 7;   // weight of a CTA's range, where there is more than one
 constexpr int kFan = 8;     // partials that are joined at once
+constexpr int kPrefetch = 8;  // pages pulled into L2 before the dependency wait
 
 template <int D, int N>
 struct Layout {
@@ -87,7 +88,8 @@ struct Layout {
     static constexpr int kSumOff = kRowOff + 9 * 64 * 4;       // [8 warps][32]: sums or largest
     static constexpr int kVsxOff = kSumOff + 8 * 32 * 4;       // [8 warps][64]: the values' scales
     static constexpr int kNfOff = kVsxOff + 2 * 4 * 64 * 4;    // [4][128]: first key that is not finite
-    static constexpr int kJoinOff = kNfOff + 4 * 128 * 4;
+    static constexpr int kTableOff = kNfOff + 4 * 128 * 4;     // [256]: scale bytes' numbers, bf16 twice
+    static constexpr int kJoinOff = kTableOff + 256 * 4;
     static constexpr int kMiscOff = kJoinOff + 64;
     static constexpr int kBytes = kMiscOff + 128 + 1024;       // + alignment slack
     static_assert(kBytes <= 232448, "shared memory per CTA");
@@ -130,14 +132,18 @@ struct Plan {
     int ntiles, ctas;
     long long W, q;  // all weight; position of the first pair
 };
-__device__ __forceinline__ int cta_of(const Plan &pl, long long q) {
-    return (int)(((unsigned long long)(q + 1) * (unsigned)pl.ctas - 1) / (unsigned long long)pl.W);
+__device__ __forceinline__ unsigned long long udiv(unsigned long long a, unsigned long long b) {
+    return ((a | b) >> 32) == 0 ? (uint32_t)a / (uint32_t)b : a / b;
 }
-// (by one whole warp)
-__device__ void make_plan(const Paged4AttnParams &p, Plan &pl) {
+__device__ __forceinline__ int cta_of(const Plan &pl, long long q) {
+    return (int)udiv((unsigned long long)(q + 1) * (unsigned)pl.ctas - 1, (unsigned long long)pl.W);
+}
+// (by one whole warp; P and T: the lane's sequence's lengths if there are no more than 32)
+__device__ void make_plan(const Paged4AttnParams &p, Plan &pl, int P, int T) {
     const int lane = threadIdx.x & 31;
     auto weight = [&](int b) {
-        return b < p.B ? tiles_of(prefix_of(p, b), block_of(p, b)) + kEnd : 0;
+        if (b >= p.B) return 0;
+        return (p.B <= 32 ? tiles_of(P, T) : tiles_of(prefix_of(p, b), block_of(p, b))) + kEnd;
     };
     long long W = 0;
     for (int b0 = 0; b0 < p.B; b0 += 32)
@@ -149,8 +155,8 @@ __device__ void make_plan(const Paged4AttnParams &p, Plan &pl) {
     pl.w = {p.B, 0, 0, 1, 0, 0};
     pl.q = W;
     if ((int)blockIdx.x >= ctas) return;
-    const long long at[2] = {(long long)((unsigned long long)blockIdx.x * (unsigned long long)W / (unsigned)ctas),
-                             (long long)((unsigned long long)(blockIdx.x + 1) * (unsigned long long)W / (unsigned)ctas)};
+    const long long at[2] = {(long long)udiv((unsigned long long)blockIdx.x * (unsigned long long)W, (unsigned)ctas),
+                             (long long)udiv((unsigned long long)(blockIdx.x + 1) * (unsigned long long)W, (unsigned)ctas)};
     long long index[2] = {-1, -1};  // tiles before at[i]
     long long run = 0, tiles = 0;   // weight, tiles before the chunk
     for (int b0 = 0, found = 0; b0 < p.B && found < 2; b0 += 32) {
@@ -168,7 +174,7 @@ __device__ void make_plan(const Paged4AttnParams &p, Plan &pl) {
             const int f = __ffs(m) - 1;
             const int wf = __shfl_sync(kFull, wt, f), before = __shfl_sync(kFull, inc, f) - wf;
             const long long q0 = run + (long long)before * p.Hkv, off = at[found] - q0;
-            int h = (int)((unsigned long long)off / (unsigned)wf), t = (int)(off - (long long)h * wf);
+            int h = (int)udiv((unsigned long long)off, (unsigned)wf), t = (int)(off - (long long)h * wf);
             const int nt = wf - kEnd;
             index[found] = tiles + ((long long)before - (long long)kEnd * f) * p.Hkv + (long long)h * nt + min(t, nt);
             if (found == 0) {
@@ -193,7 +199,13 @@ __device__ void make_plan(const Paged4AttnParams &p, Plan &pl) {
     }
     if (index[0] < 0) index[0] = tiles;
     if (index[1] < 0) index[1] = tiles;
-    walk_load(p, pl.w);
+    if (p.B <= 32) {
+        pl.w.P = __shfl_sync(kFull, P, pl.w.b & 31);
+        pl.w.T = __shfl_sync(kFull, T, pl.w.b & 31);
+        pl.w.nt = tiles_of(pl.w.P, pl.w.T);
+    } else {
+        walk_load(p, pl.w);
+    }
     pl.ntiles = (int)(index[1] - index[0]);
 }
 
@@ -338,7 +350,7 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
     using Lt = Layout<D, N>;
     using Ro = Roles<N>;
     constexpr bool kTurns = Ro::kTurns;
-    constexpr int kSets = Ro::kSets, kKeyWarp0 = Ro::kKeyWarp0, kValueWarp0 = Ro::kValueWarp0,
+    constexpr int kKeySets = Ro::kKeySets, kValueSets = Ro::kValueSets, kKeyWarp0 = Ro::kKeyWarp0, kValueWarp0 = Ro::kValueWarp0,
                   kProducerWarp = Ro::kProducerWarp, kSWarp = Ro::kSWarp, kPvWarp = Ro::kPvWarp,
                   kThreads = Ro::kThreads;
     constexpr int kStages = Lt::kStages, R = kTurns ? N : N / 2;  // rows of a group
@@ -393,13 +405,48 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tm_k)) : "memory");
     for (int i = threadIdx.x; i < 256 / 16; i += kThreads)
         sts4(sbase + Lt::kOnesOff + 16 * i, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+    uint32_t *const table = reinterpret_cast<uint32_t *>(sm + Lt::kTableOff);
+    for (int i = threadIdx.x; i < 256; i += kThreads) table[i] = pack_bf16(scale_of(i), scale_of(i));
     fence_async_smem();
+    // The plan, from lengths that the kernel before may yet write: they are compared below.  Into L2 in the
+    // meantime: the first pages (for nothing if the table then says others), the first queries.
+    int P0 = 0, T0 = 0;
+    if (warp == 0 && p.B <= 32) {
+        if (lane < p.B) {
+            P0 = prefix_of(p, lane);
+            T0 = block_of(p, lane);
+        }
+        Plan pl;
+        make_plan(p, pl, P0, T0);
+        if (lane == 0) *s_plan = pl;
+        const int page0 = 2 * pl.w.t + lane;
+        if (lane < kPrefetch && pl.ntiles > 0 && page0 < (pl.w.P + kPage - 1) / kPage && page0 < 2 * (pl.w.t + pl.ntiles)) {
+            const int pg = __ldcg(p.table + (size_t)pl.w.b * p.max_pages + page0);
+            if (pg >= 0 && pg < p.pages) {
+                const size_t tile = (size_t)pg * p.Hkv + pl.w.h;
+                prefetch_bulk(p.k + tile * Lt::kCodes, Lt::kCodes);
+                prefetch_bulk(p.v + tile * Lt::kCodes, Lt::kCodes);
+                prefetch_bulk(p.k_scale + tile * Lt::kScales, Lt::kScales);
+                prefetch_bulk(p.v_scale + tile * Lt::kScales, Lt::kScales);
+            }
+        }
+        for (int r = lane; r < (pl.ntiles > 0 ? p.G * pl.w.T : 0); r += 32)
+            for (int c = 0; c < D; c += 64)
+                prefetch_line(p.q + (((size_t)pl.w.b * p.max_block + r / p.G) * p.Hq + pl.w.h * p.G + r % p.G) * D + c);
+    }
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (warp == 0) {
-        Plan pl;
-        make_plan(p, pl);
-        if (lane == 0) *s_plan = pl;
+        int P1 = 0, T1 = 0;
+        if (p.B <= 32 && lane < p.B) {
+            P1 = prefix_of(p, lane);
+            T1 = block_of(p, lane);
+        }
+        if (p.B > 32 || !__all_sync(kFull, P0 == P1 && T0 == T1)) {
+            Plan pl;
+            make_plan(p, pl, P1, T1);
+            if (lane == 0) *s_plan = pl;
+        }
     }
     if (blockIdx.x == 0 && warp == 1)
         for (int b = lane; b < p.B; b += 32)
@@ -539,7 +586,7 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
             const Segment sg = segment_of(w, ntiles - k);
             for (int i = 0; i < sg.n && ok; ++i, ++k) {
                 const int s = k & 1;
-                if (kSets == 2 && s != set) {
+                if (kValueSets == 2 && s != set) {
                     kp += i < sg.pre;
                     continue;
                 }
@@ -559,9 +606,9 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
                             by.y &= (uint32_t)(keep >> 32);
                         }
                         __syncwarp();
-                        scales[lane] = make_uint2(
-                            pack_bf16(scale_of(by.x >> at_q & 0xffu), scale_of(by.y >> at_q & 0xffu)),
-                            pack_bf16(scale_of(by.x >> (at_q + 8) & 0xffu), scale_of(by.y >> (at_q + 8) & 0xffu)));
+                        const uint32_t b0 = by.x >> at_q, b1 = by.y >> at_q;
+                        scales[lane] = make_uint2(__byte_perm(table[b0 & 0xffu], table[b1 & 0xffu], 0x5410),
+                                                  __byte_perm(table[b0 >> 8 & 0xffu], table[b1 >> 8 & 0xffu], 0x5410));
                         __syncwarp();
                     }
                     if (k >= 2) ok = waits(b_pvdone + 8 * s, half_of(k) ^ 1);
@@ -650,7 +697,7 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
         bool ok = true;
         for (int seg = 0; k < ntiles && ok; ++seg, walk_pair(p, w)) {
             const Segment sg = segment_of(w, ntiles - k);
-            if (kSets == 1 || (seg & 1) == set) {  // the queries
+            if (kKeySets == 1 || (seg & 1) == set) {  // the queries
                 if (seg >= 2) ok = waits(b_qfree + 8 * (seg & 1), half_of(seg) ^ 1);
                 if (!ok) break;
                 const uint32_t q = sbase + Lt::kQOff + (seg & 1) * Lt::kQ;
@@ -672,7 +719,7 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
             }
             for (int i = 0; i < sg.n && ok; ++i, ++k) {
                 const int s = k & 1;
-                if (kSets == 2 && s != set) {
+                if (kKeySets == 2 && s != set) {
                     kp += i < sg.pre;
                     continue;
                 }
@@ -686,17 +733,19 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
                     fence_after();
                     const int pg = key / kPage, t = key % kPage;
                     const uint8_t *const at_scale = stage + Lt::kKsOff + pg * Lt::kScales + t * (D / 32);
-                    uint32_t by = D == 128 ? *reinterpret_cast<const uint32_t *>(at_scale)
+                    const uint32_t by = D == 128 ? *reinterpret_cast<const uint32_t *>(at_scale)
                                            : *reinterpret_cast<const uint16_t *>(at_scale);
                     uint4 codes[D / 32];
+                    uint32_t scs[D / 32];
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c) scs[c] = table[by >> 8 * c & 0xffu];
 #pragma unroll
                     for (int c = 0; c < D / 32; ++c)
                         codes[c] = *reinterpret_cast<const uint4 *>(stage + pg * Lt::kCodes + key_chunk<D>(t, c));
 #pragma unroll
-                    for (int c = 0; c < D / 32; ++c, by >>= 8) {  // 32 elements under a scale
+                    for (int c = 0; c < D / 32; ++c) {  // 32 elements under a scale
                         const uint4 x = codes[c];
-                        const float f = scale_of(by & 0xffu);
-                        const uint32_t sc = pack_bf16(f, f), m8 = bf16_mul2(sc, 0xc308c308u);
+                        const uint32_t sc = scs[c], m8 = bf16_mul2(sc, 0xc308c308u);  // -136
                         const uint32_t word[4] = {x.x, x.y, x.z, x.w};
                         uint32_t r[16];
 #pragma unroll
@@ -763,6 +812,7 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
             const Segment sg = segment_of(w, ntiles - k_seg);
             const int rows = p.G * w.T;
             const float sc_page = fmaxf(p.scale_log2 * unit_of(p.k_unit, w.h), 1.2e-38f);
+            const float v_unit = unit_of(p.v_unit, w.h);
             float l[R];
 #pragma unroll
             for (int j = 0; j < R; ++j) l[j] = 0.f;
@@ -955,7 +1005,7 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
                     sum = alpha[r];
                 }
                 // no visible key: 0 and -inf; NaN stays NaN
-                const float inv = total == 0.f ? 0.f : unit_of(p.v_unit, w.h) / sum;
+                const float inv = total == 0.f ? 0.f : v_unit / sum;
                 s_factor[r] = f[0] * inv;
                 s_factor[64 + r] = f[1] * inv;
                 s_lse[r] = total == 0.f ? -INFINITY : log2f(total) - least;
