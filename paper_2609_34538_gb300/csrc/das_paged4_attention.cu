@@ -355,6 +355,8 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
                   kThreads = Ro::kThreads;
     constexpr int kStages = Lt::kStages, R = kTurns ? N : N / 2;  // rows of a group
     constexpr int kStep = kTurns ? 2 : 1;                         // from one tile of a group to its next
+    constexpr int kChunk = 16;                                    // rows whose scores a softmax thread has at once
+    static_assert(R % kChunk == 0, "rows in chunks");
     extern __shared__ uint8_t smem_raw[];
     uint8_t *const sm = smem_raw + (-smem_u32(smem_raw) & 1023u);
     const uint32_t sbase = smem_u32(sm);
@@ -819,68 +821,80 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
             bool has_ref = false;  // the same in the whole group
 #pragma unroll 1
             for (int i = kTurns ? (k_seg ^ group) & 1 : 0; i < sg.n; i += kStep) {
-                const int k = k_seg + i, s = k & 1;
+                const int k = k_seg + i, s = kTurns ? group : k & 1;
                 const bool blk = i >= sg.pre;
                 const bool ok = waits(b_sdone + 8 * s, half_of(k));
                 fence_after();
-                uint32_t a[R];  // scores, then weights
                 const float sc = blk ? p.scale_log2 : sc_page;
-                int2 n = make_int2(0, 0);
+                int2 n = make_int2(kPage, kPage);
                 if (!blk) n = infos[(kp_seg + i) % kInfos];
-                auto scores = [&] {
-                    ld_lanes(lanes + kSCol + 64 * s + row0, a);
+                // hidden keys: of pages past the prefix, of the block past it or the row (key i is seen by the
+                // rows from i G on)
+                const bool some_hidden = blk || n.x + n.y < kKeys || !ok;
+                const int from = !ok ? N : blk ? (key < w.T ? key * p.G : N) : key % kPage < (key < kPage ? n.x : n.y) ? 0 : N;
+                const int until = blk ? rows : N;
+                const uint32_t s_col = lanes + kSCol + 64 * s + row0;
+                auto scores = [&](int c, uint32_t(&a)[kChunk]) {
+                    ld_lanes(s_col + c, a);
                     ld_wait(a);
-                    if (blk) {  // the causal mask: key i is seen by the rows from i G on
-                        const int from = ok && key < w.T ? key * p.G : N;
+                    if (some_hidden)
 #pragma unroll
-                        for (int j = 0; j < R; ++j)
-                            if (row0 + j < from || row0 + j >= rows) a[j] = 0xff800000u;
-                    } else if (n.x < kPage || n.y < kPage || !ok) {
-                        if (!ok || key % kPage >= (key < kPage ? n.x : n.y))
-#pragma unroll
-                            for (int j = 0; j < R; ++j) a[j] = 0xff800000u;
-                    }
+                        for (int j = 0; j < kChunk; ++j)
+                            if (row0 + c + j < from || row0 + c + j >= until) a[j] = 0xff800000u;
                 };
-                scores();
                 if (!has_ref) {
                     // the segment's first key that is seen, if this tile has one
-                    const int first = blk || n.x > 0 ? 0 : n.y > 0 ? kPage : -1;
-                    if (key == max(first, 0))
+                    const int first = n.x > 0 ? 0 : n.y > 0 ? kPage : -1;
+#pragma unroll 1
+                    for (int c = 0; c < R; c += kChunk) {
+                        uint32_t a[kChunk];
+                        scores(c, a);
+                        if (key == max(first, 0))
 #pragma unroll
-                        for (int j = 0; j < R; ++j) {
-                            const float m = __uint_as_float(a[j]) * sc;
-                            off[row0 + j] = (fabsf(m) < INFINITY ? -m : 0.f) - kBelow;
-                        }
+                            for (int j = 0; j < kChunk; ++j) {
+                                const float m = __uint_as_float(a[j]) * sc;
+                                off[row0 + c + j] = (fabsf(m) < INFINITY ? -m : 0.f) - kBelow;
+                            }
+                    }
                     group_sync();
                     has_ref = first >= 0;
                 }
                 if (k >= 2) waits(b_pvdone + 8 * s, half_of(k) ^ 1);  // P's buffer is free
-                const uint32_t dst = sbase + Lt::kPOff + s * Lt::kP;
-                uint32_t big;
-                auto weights = [&] {
-                    // (all exponentials first, so that their chains overlap)
+                const uint32_t dst = sbase + Lt::kPOff + s * Lt::kP + place * 128, turn = (place & 7) << 4;
+                // (all exponentials of a chunk first, so that their chains overlap)
+                auto weights = [&](int c, uint32_t(&a)[kChunk]) {
 #pragma unroll
-                    for (int j = 0; j < R; j += 4) {
-                        const float4 o = *reinterpret_cast<const float4 *>(off + row0 + j);
+                    for (int j = 0; j < kChunk; j += 4) {
+                        const float4 o = *reinterpret_cast<const float4 *>(off + row0 + c + j);
                         float e[4];
                         axpy2(e[0], e[1], sc, __uint_as_float(a[j]), __uint_as_float(a[j + 1]), o.x, o.y);
                         axpy2(e[2], e[3], sc, __uint_as_float(a[j + 2]), __uint_as_float(a[j + 3]), o.z, o.w);
 #pragma unroll
                         for (int t = 0; t < 4; ++t) a[j + t] = __float_as_uint(ex2(e[t]));
                     }
-                    big = 0;
+                    uint32_t big = 0;
 #pragma unroll
-                    for (int j = 0; j < R; j += 8) {
+                    for (int j = 0; j < kChunk; j += 8) {
                         uint32_t pk[4];
 #pragma unroll
                         for (int t = 0; t < 4; ++t)
                             pk[t] = pack_bf16(__uint_as_float(a[j + 2 * t]), __uint_as_float(a[j + 2 * t + 1]));
                         big |= pk[0] | pk[1] | pk[2] | pk[3];
-                        sts4(dst + chunk16(place, (row0 + j) / 8), pk[0], pk[1], pk[2], pk[3]);
+                        sts4(dst + ((uint32_t)((row0 + c + j) / 8 * 16) ^ turn), pk[0], pk[1], pk[2], pk[3]);
                     }
-                    fence_async_smem();
+                    return big;
                 };
-                weights();
+                uint32_t big = 0;
+#pragma unroll
+                for (int c = 0; c < R; c += kChunk) {
+                    uint32_t a[kChunk];
+                    scores(c, a);
+                    big |= weights(c, a);
+#pragma unroll
+                    for (int j = 0; j < kChunk; j += 2)
+                        add2(l[c + j], l[c + j + 1], l[c + j], l[c + j + 1], __uint_as_float(a[j]), __uint_as_float(a[j + 1]));
+                }
+                fence_async_smem();
                 uint32_t over;
                 asm volatile(
                     "{\n .reg .pred p, q;\n setp.ne.b32 p, %1, 0;\n"
@@ -888,24 +902,30 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
                     : "=r"(over)
                     : "r"(big & 0x40004000u), "r"(bar)
                     : "memory");
-                if (over) {  // a weight of 2 or more: the references are set to the tile's largest
-                    scores();
+                if (over) {
+                    // A weight of 2 or more: its row's reference is set to the tile's largest score, and O and the
+                    // sums are rescaled, by two factors as one could be 0 where the product is not.  (l has the
+                    // tile's weights under the old reference already; where one made it infinite, what it was
+                    // before counts nothing.)
 #pragma unroll 1
-                    for (int j = 0; j < R; ++j) {
-                        float x = 0.f;
+                    for (int c = 0; c < R; c += kChunk) {
+                        uint32_t a[kChunk];
+                        scores(c, a);
 #pragma unroll
-                        for (int t = 0; t < R; ++t)
-                            if (t == j) x = __uint_as_float(a[t]) * sc;
-                        const uint32_t m = __reduce_max_sync(kFull, ordered(x == x ? x : -INFINITY));
-                        if (lane == 0) sums[j] = unordered(m);
+                        for (int j = 0; j < kChunk; ++j) {
+                            const float x = __uint_as_float(a[j]) * sc;
+                            const uint32_t m = __reduce_max_sync(kFull, ordered(x == x ? x : -INFINITY));
+                            if (lane == 0) sums[c + j] = unordered(m);
+                        }
                     }
                     group_sync();
                     if (quad == 0 && lane < R) {
                         float m = -INFINITY;
                         for (int v = 0; v < kGroupWarps; ++v) m = fmaxf(m, group_sums[v * 32 + lane]);
-                        const float was = off[row0 + lane], now = fminf(was, (m < INFINITY ? -m : 0.f) - kBelow);
-                        off[row0 + lane] = now;
-                        alpha[row0 + lane] = ex2(now - was);
+                        const float was = off[row0 + lane];
+                        const bool jump = m + was >= 1.f && m < INFINITY;
+                        if (jump) off[row0 + lane] = -m - kBelow;
+                        alpha[row0 + lane] = jump ? ex2(0.5f * (-m - kBelow - was)) : 1.f;
                     }
                     group_sync();
                     if (i >= kStep) {
@@ -918,19 +938,29 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
                             ld_wait(o);
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
-                                o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha[row0 + c + j]);
+                                o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha[row0 + c + j] * alpha[row0 + c + j]);
                             st_lanes(o_col + c, o);
                         }
                         uint32_t o[1];
                         ld_lanes(sum_col, o);
                         ld_wait(o);
-                        if (sum_mine) o[0] = __float_as_uint(__uint_as_float(o[0]) * alpha[sum_row]);
+                        if (sum_mine) o[0] = __float_as_uint(__uint_as_float(o[0]) * alpha[sum_row] * alpha[sum_row]);
                         st_lanes(sum_col, o);
                         st_wait();
                     }
 #pragma unroll
-                    for (int j = 0; j < R; ++j) l[j] *= alpha[row0 + j];
-                    weights();
+                    for (int c = 0; c < R; c += kChunk) {
+                        uint32_t a[kChunk];
+                        scores(c, a);
+                        weights(c, a);
+#pragma unroll
+                        for (int j = 0; j < kChunk; ++j)
+                            {
+                            const float f = alpha[row0 + c + j];
+                            l[c + j] = l[c + j] == INFINITY ? __uint_as_float(a[j]) : l[c + j] * f * f;
+                        }
+                    }
+                    fence_async_smem();
                     __syncwarp();
                 }
                 fence_before();
@@ -938,9 +968,6 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
                     mbar_arrive(b_sfree + 8 * s);
                     mbar_arrive(b_pready + 8 * s);
                 }
-#pragma unroll
-                for (int j = 0; j < R; j += 2)
-                    add2(l[j], l[j + 1], l[j], l[j + 1], __uint_as_float(a[j]), __uint_as_float(a[j + 1]));
             }
 
             // ---- the end of a segment: O / l and lse, as output or as a partial ----
