@@ -83,8 +83,10 @@ __device__ __forceinline__ T block_reduce(T v, T *sums, F f) {
 }
 
 // ---- a row in the shared memory of a cluster ---------------------------------------
-constexpr int kThreads = 1024, kWarps = kThreads / 32;
-static_assert(kWarps == 32, "a warp scans the warps' sums");
+constexpr int kDrawThreads = 1024;
+// Rows that are recorded are not held but read again, from L2: two CTAs of half the threads
+// share an SM, and one's waits are the other's time.
+constexpr int kRecordThreads = 512;
 constexpr int kMaxRowCtas = 8;                 // a portable cluster
 // Logits per CTA, as they come: what shared memory holds, and fewer than 2^16, so that
 // a bin's sums of 16-bit pieces stay below 2^32.
@@ -97,6 +99,7 @@ constexpr int kList = 256;
 constexpr int kValues = 4096;               // bins of 16-bit values, sixteen octaves of each sign
 constexpr uint32_t kValueBase = 0x3b80u;    // bf16 bits of 2^-8
 constexpr int kCand = 2048;
+static_assert(kRecordThreads >= kMaxSegs, "a thread has a segment");
 constexpr int kSmall = 2 * kMaxSegs;
 // exponents past the last bin have weights that round to 0: e^-23 < 2^-33
 constexpr float kNats = 23.f;
@@ -106,7 +109,7 @@ struct alignas(16) Shared {
     float cand[kCand];              // the candidates left by a small top-k,
     int cand_at[kCand];             // in index order
     uint32_t hist[2 * kBins];       // bin i's sum: [i] + 2^16 [kBins + i]; or kValues counts
-    u64 scan[kWarps];
+    u64 scan[32];
     u64 seg[kMaxSegs];
     uint32_t n_seg[kMaxSegs];
     u64 xch[2][3][kMaxRowCtas];  // values of every CTA of the cluster
@@ -153,9 +156,13 @@ __device__ __forceinline__ u64 wide(uint32_t w) { return (u64)w + (w == kOne); }
 // With RECORD rows are not drawn from: what their filters leave is recorded, of the rows of
 // a.logits and then of a.second.
 template <bool BF16, bool RECORD>
-__global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a, int slice) {
+__global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD ? 2 : 1)
+    sample_kernel(const SampleArgs a, int slice) {
+    constexpr int kThreads = RECORD ? kRecordThreads : kDrawThreads, kWarps = kThreads / 32;
+    static_assert(kWarps <= 32, "a warp scans the warps' sums");
     __shared__ Shared s;
-    extern __shared__ uint4 held[];  // the CTA's logits in groups of four, padded with -inf
+    // the CTA's logits in groups of four, padded with -inf (RECORD: bins of other CTAs alone)
+    extern __shared__ uint4 held[];
     cg::cluster_group cluster = cg::this_cluster();
     const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -194,7 +201,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
         const u64 x = warp_scan(v);
         if (lane == 31) s.scan[warp] = x;
         __syncthreads();
-        const u64 sums = warp_scan(s.scan[lane]);  // by every warp for itself
+        const u64 sums = warp_scan(lane < kWarps ? s.scan[lane] : 0);  // by every warp for itself
         total = __shfl_sync(kFull, sums, 31);
         const u64 before = __shfl_sync(kFull, sums, warp > 0 ? warp - 1 : 0);
         __syncthreads();
@@ -249,18 +256,18 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
     bool few = false;  // whether the candidates alone are left
     float mine = -INFINITY;
     src -= shift;
-#pragma unroll 4
-    for (int g = tid; g < groups; g += kThreads) {
-        float f[4];
+    auto fetch4 = [&](int g, float (&f)[4]) {
         if (4 * g >= shift && 4 * g + 4 <= len + shift) {
             if constexpr (BF16) {
-                const uint2 u = __ldcs(reinterpret_cast<const uint2 *>(src) + g);
+                const uint2 *at = reinterpret_cast<const uint2 *>(src) + g;
+                const uint2 u = RECORD ? *at : __ldcs(at);
                 f[0] = __uint_as_float(u.x << 16);
                 f[1] = __uint_as_float(u.x & 0xffff0000u);
                 f[2] = __uint_as_float(u.y << 16);
                 f[3] = __uint_as_float(u.y & 0xffff0000u);
             } else {
-                const float4 u = __ldcs(reinterpret_cast<const float4 *>(src) + g);
+                const float4 *at = reinterpret_cast<const float4 *>(src) + g;
+                const float4 u = RECORD ? *at : __ldcs(at);
                 f[0] = u.x;
                 f[1] = u.y;
                 f[2] = u.z;
@@ -277,10 +284,13 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
             }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f[i] = f[i] == f[i] ? f[i] + 0.f : -INFINITY;
-            mine = fmaxf(mine, f[i]);
-        }
+        for (int i = 0; i < 4; ++i) f[i] = f[i] == f[i] ? f[i] + 0.f : -INFINITY;
+    };
+#pragma unroll 4
+    for (int g = tid; g < groups; g += kThreads) {
+        float f[4];
+        fetch4(g, f);
+        mine = fmaxf(fmaxf(mine, fmaxf(f[0], f[1])), fmaxf(f[2], f[3]));
         if (counted)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -292,6 +302,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
                     if (n < kSmall) reinterpret_cast<float *>(s.seg)[n] = f[i];
                 }
             }
+        if constexpr (RECORD) continue;
         if (BF16)
             reinterpret_cast<uint2 *>(held)[g] =
                 make_uint2(__float_as_uint(f[0]) >> 16 | (__float_as_uint(f[1]) & 0xffff0000u),
@@ -299,9 +310,15 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
         else
             reinterpret_cast<float4 *>(held)[g] = make_float4(f[0], f[1], f[2], f[3]);
     }
+    bool infinite = false;
     auto load4 = [&](int g, float (&l)[4]) {
         if (g >= groups) {
             l[0] = l[1] = l[2] = l[3] = -INFINITY;
+        } else if (RECORD && !few) {
+            fetch4(g, l);
+            if (infinite)  // (those have weight, and the same)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) l[i] = l[i] == INFINITY ? 0.f : -INFINITY;
         } else if (BF16 && !few) {
             const uint2 u = reinterpret_cast<const uint2 *>(held)[g];
             l[0] = __uint_as_float(u.x << 16);
@@ -357,7 +374,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
         __syncthreads();
         uint32_t here = kKeyNone;
         if (bound && warp == 0)
-            here = __shfl_sync(kFull, sorted32(s.list[lane]), (int)((kc + n - 1) / n) - 1);
+            here = __shfl_sync(kFull, sorted32(lane < kWarps ? s.list[lane] : 0u), (int)((kc + n - 1) / n) - 1);
         const int t = exchange(s.key_max, here, 0);  // (by warp 0)
         uint32_t most = 0, least = kOne;
         for (int r = 0; r < C; ++r) {
@@ -379,21 +396,22 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
         m = logit_of(most);
         low = logit_of(max(least, kKeyNone + 1));
     }
-    const bool infinite = m == INFINITY;
+    infinite = m == INFINITY;
     const uint32_t top = key_of(m);
-    // (a key of the row that stands in shared memory is one of the row, but for the infinite logits')
+    // (a key that load4 gives is one of the row, but for the infinite logits')
     auto record = [&](uint32_t cut, int last, u64 total) {
         if (infinite && cut == key_of(0.f)) cut = top;
         a.records[row] = RowRecord{top, cut, last, T, floor_p, 0u, total};
     };
     if (infinite) {  // the infinite ones alone have weight, and the same
-        for (int g = tid; g < groups; g += kThreads) {
-            float l[4];
-            load4(g, l);
+        if constexpr (!RECORD)
+            for (int g = tid; g < groups; g += kThreads) {
+                float l[4];
+                load4(g, l);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) l[i] = l[i] == INFINITY ? 0.f : -INFINITY;
-            store4(g, l);
-        }
+                for (int i = 0; i < 4; ++i) l[i] = l[i] == INFINITY ? 0.f : -INFINITY;
+                store4(g, l);
+            }
         m = 0.f;
         low = -3.4028234e38f;
         counted = false;
@@ -598,17 +616,17 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
     auto send_bins = [&](int words, int per_cta, int stride) -> const uint32_t * {
         uint32_t *const place = few ? reinterpret_cast<uint32_t *>(held) : reinterpret_cast<uint32_t *>(s.cand);
         if (C == 1) return s.hist;
-        if (4 * tid < words) {
-            const int row = stride > per_cta ? 4 * tid / kBins : 0, bin = 4 * tid - row * kBins;
+        for (int i = tid; 4 * i < words; i += kThreads) {
+            const int row = stride > per_cta ? 4 * i / kBins : 0, bin = 4 * i - row * kBins;
             const int r = bin / per_cta, off = bin - r * per_cta;
             uint32_t *const there = cluster.map_shared_rank(place, r);
             *reinterpret_cast<uint4 *>(there + rank * stride + row * per_cta + off) =
-                reinterpret_cast<const uint4 *>(s.hist)[tid];
+                reinterpret_cast<const uint4 *>(s.hist)[i];
         }
         return place;
     };
     static_assert(sizeof s.cand + sizeof s.cand_at >= sizeof s.hist && kValues == 2 * kBins &&
-                  2 * kBins == 4 * kThreads && offsetof(Shared, cand_at) == sizeof s.cand, "bins sent");
+                  offsetof(Shared, cand_at) == sizeof s.cand, "bins sent");
 
     // ---- the threshold of a sum over the logits from `from` up ----
     // Finds the largest t with the sum of f over logits > t below the target
@@ -661,13 +679,14 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
                 const int ts = exchange(small_all, 0, 0);  // (and the bins are there)
                 small = 0;
                 for (int r = 0; r < C; ++r) small += s.xch[ts][0][r];
-                // as the linear bins below: 1 / C of the bins to a CTA, up to four a thread
-                u64 v[4] = {0, 0, 0, 0}, own = 0;
-                uint32_t n[4] = {0, 0, 0, 0};
+                // as the linear bins below: 1 / C of the bins to a CTA, up to kMost a thread
+                constexpr int kMost = kValues / kThreads;
+                u64 v[kMost] = {}, own = 0;
+                uint32_t n[kMost] = {};
                 const int i0 = rank * per_cta + tid * per_thread;
                 if (tid * per_thread < per_cta) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < kMost; ++i) {
                         if (i >= per_thread) break;
                         for (int r = 0; r < C; ++r) n[i] += bins[r * per_cta + tid * per_thread + i];
                         if (n[i]) v[i] = kWeights ? n[i] * wide(weight(value_of(i0 + i))) : n[i];
@@ -695,7 +714,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
                 if (target <= total) {
                     sync();  // no CTA's s.bin is set from here on
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < kMost; ++i) {
                         if (n[i] && before < target && before + v[i] >= target)
                             for (int r = 0; r < C; ++r) {
                                 Shared *o = of(r);
@@ -781,28 +800,29 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
                 }
             }
             // The bins' sums over the cluster: each CTA takes 1 / C of the bins,
-            // one or two a thread in order, and tells the others its total.
+            // up to kMost a thread in order, and tells the others its total.
             const int per_cta = kBins / C, per_thread = max(1, per_cta / kThreads);
             if (C > 1) __syncthreads();
             const uint32_t *bins = send_bins(kWeights ? 2 * kBins : kBins, per_cta, 2 * per_cta);
             sync();
-            u64 v[2] = {0, 0};
-            if (tid * per_thread < per_cta) {
-                const int i0 = rank * per_cta + tid * per_thread;
+            constexpr int kMost = kBins / kThreads;
+            u64 v[kMost] = {}, own = 0;
+#pragma unroll
+            for (int i = 0; i < kMost; ++i) {
+                const int at = tid * per_thread + i;
+                if (i >= per_thread || at >= per_cta) break;
                 if (C == 1) {
-                    const uint2 low = *reinterpret_cast<const uint2 *>(s.hist + i0);
-                    const uint2 high = *reinterpret_cast<const uint2 *>(s.hist + kBins + i0);
-                    v[0] = low.x + ((u64)high.x << 16);
-                    v[1] = low.y + ((u64)high.y << 16);
-                } else {  // (C >= 2: one bin a thread)
+                    v[i] = s.hist[at] + ((u64)s.hist[kBins + at] << 16);
+                } else {
                     for (int r = 0; r < C; ++r) {
-                        v[0] += bins[2 * r * per_cta + tid];
-                        if (kWeights) v[0] += (u64)bins[(2 * r + 1) * per_cta + tid] << 16;
+                        v[i] += bins[2 * r * per_cta + at];
+                        if (kWeights) v[i] += (u64)bins[(2 * r + 1) * per_cta + at] << 16;
                     }
                 }
+                own += v[i];
             }
             u64 total;
-            u64 before = scan(v[0] + v[1], total);
+            u64 before = scan(own, total);
             if (C > 1) {
                 const int t = exchange(total, 0, 0);
                 total = 0;
@@ -819,7 +839,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
             }
             before += above;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int i = 0; i < kMost; ++i) {
                 if (before < target && before + v[i] >= target)
                     for (int r = 0; r < C; ++r) {
                         Shared *o = of(r);
@@ -896,11 +916,11 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
                     s.all[tid] = make_uint2(key, kWeights ? weight(logit_of(key)) : 1u);
                 }
                 __syncthreads();
-                if (tid - lane < 4 * (int)n) {  // four threads to an entry, each every fourth
-                    const uint32_t key = s.all[min(tid >> 2, (int)n - 1)].x;
+                for (int t0 = tid; t0 - lane < 4 * (int)n; t0 += kThreads) {  // four threads to an entry, each every fourth
+                    const uint32_t key = s.all[min(t0 >> 2, (int)n - 1)].x;
                     u64 more = 0, equal = 0, count = 0;
 #pragma unroll 4
-                    for (int i = tid & 3; i < (int)n; i += 4) {
+                    for (int i = t0 & 3; i < (int)n; i += 4) {
                         const uint2 o = s.all[i];
                         const u64 w = wide(o.y);
                         if (o.x > key) more += w;
@@ -935,6 +955,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
     // ---- kept: keys > cut, and the first `ties` of those equal to it ----
     uint32_t cut = kKeyNone;
     u64 ties = 0, equal = 0;  // of `equal` tokens equal to the cut `ties` stay
+    u64 kept_sum = 0;         // with top-p, the sum of what stays
     if (k < a.vocab) {
         const float span = m - low;
         const float per_logit = span > 0.f && span < 3e38f ? (kBins - 1) / span : 0.f;
@@ -958,8 +979,10 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
             const u64 w = wide(weight(logit_of(cut)));
             ties = (s.target - s.above + w - 1) / w;
             equal = s.equal;
+            kept_sum = s.above + ties * w;
         } else {  // it ends among the tokens equal to the top-k cut
             ties = (s.target - s.sum + w_cut - 1) / w_cut;
+            kept_sum = s.sum + ties * w_cut;
         }
     }
     // Of the tokens equal to the cut the first `ties` in index order stay.  Where
@@ -987,14 +1010,27 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
         code_cut = floor_p > 0.f && !(e[0] >= floor_p) ? 0u : code_of(e[0]);
     }
 
+    // (a record needs no sums where the search has left one that min-p takes nothing from: expf is
+    // off by two steps at most, so no larger logit's e is below the floor if the cut's is well above)
+    bool summed = false;
+    if constexpr (RECORD) {
+        const float l = at_cut;
+        summed = p < 1.f && (floor_p <= 0.f || (quick ? quick_e(l) : plain_e(l, m, T)) * (1.f - 0x1p-20f) >= floor_p);
+        if (summed && !part) {
+            if (rank == 0 && tid == 0) record(cut, ties ? 0x7fffffff : -1, kept_sum);
+            return;  // (after the barrier of search)
+        }
+    }
+
     // ---- the token at which the running sum in index order passes r ----
     const int segs = (groups + 31) / 32;
+#pragma unroll RECORD ? 4 : 1
     for (int g0 = warp * 32; g0 < groups; g0 += kThreads) {  // segments of 32 groups
         float l[4];
         load4(g0 + lane, l);
         const float most = fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3]));
         u64 sum = 0;
-        if (__any_sync(kFull, most >= from)) {
+        if (!summed && __any_sync(kFull, most >= from)) {
             uint32_t w[4];
             kept(l, w);
             sum = (u64)w[0] + w[1] + w[2] + w[3];
@@ -1037,6 +1073,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a,
         }
     }
     if constexpr (RECORD) {
+        if (summed) total = kept_sum;
         // the last kept one of those equal to the cut
         if (!part) {
             if (rank == 0 && tid == 0) record(cut, ties ? 0x7fffffff : -1, total);
@@ -1341,37 +1378,64 @@ __global__ void __launch_bounds__(kScanWarps * 32)
 // ---- proposals that were drawn by chance -------------------------------------------
 // From the rows' records: the first proposal that is refused, and the draw in its place from
 // what the target's row has more.  A cluster to a sequence; each of its warps has a run of
-// the row, whose sum says whether the draw is in it, and goes over its run again if so.
+// the row in 32 steps at most, whose sums stand in its lanes: the warp that the draw falls
+// to finds the step in them and computes that alone again.
+constexpr int kAcceptThreads = 1024;
+template <bool BF16>
 struct RowProbs {
+    using Elem = std::conditional_t<BF16, uint16_t, float>;
     RowRecord r;
-    const void *logits;
-    size_t at;
-    float m, inv;
-    bool bf16;
+    const Elem *logits;
+    float m, inv, cut, rT;
+    bool quick;
     __device__ __forceinline__ RowProbs(const SampleArgs &a, size_t row, bool second) {
         const size_t rows = (size_t)a.B * a.W;
         r = a.records[second ? rows + row : row];
-        logits = second ? a.second : a.logits;
-        at = row * (size_t)(second ? a.second_stride : a.row_stride);
-        bf16 = a.bf16;
-        m = logit_of(r.top);
+        logits = static_cast<const Elem *>(second ? a.second : a.logits) +
+                 row * (size_t)(second ? a.second_stride : a.row_stride);
+        const bool none = r.top == 0;  // (no logit above -inf)
+        m = none ? 0.f : logit_of(r.top);
+        cut = none ? INFINITY : logit_of(max(r.key, kKeyNone));
+        if (none) r.last = -1;
         inv = 1.f / (float)((double)r.total * (1.0 / 4294967296.0));
+        rT = none ? 1.f : __frcp_rn(r.T);
+        quick = r.T > 1e-18f && r.T < 1e18f && (__float_as_uint(r.T) & 0x7fffffu) != 0x7fffffu;
     }
-    __device__ __forceinline__ float e(int v) const {  // 0: left out
-        if (r.top == 0) return 0.f;
-        const uint32_t x = key_of(bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t *>(logits)[at + v] << 16)
-                                       : static_cast<const float *>(logits)[at + v]);
-        if (x < r.key || (x == r.key && v > r.last)) return 0.f;
-        const float y = e_of(x, r.top, m, r.T);
-        return r.floor > 0.f && !(y >= r.floor) ? 0.f : y;
+    __device__ __forceinline__ float logit(int v) const {
+        float l;
+        if constexpr (BF16) l = __uint_as_float((uint32_t)logits[v] << 16);
+        else l = logits[v];
+        return l == l ? l : -INFINITY;
     }
+    __device__ __forceinline__ bool kept(float l, int v) const { return l > cut || (l == cut && v <= r.last); }
+    __device__ __forceinline__ float floored(float e) const { return r.floor > 0.f && !(e >= r.floor) ? 0.f : e; }
+    // of a token alone
     __device__ __forceinline__ float p(int v) const {
-        const float y = e(v);
-        return y > 0.f ? y * inv : 0.f;
+        const float l = logit(v);
+        if (!kept(l, v)) return 0.f;
+        const float e = floored(e_of(key_of(l), r.top, m, r.T));
+        return e > 0.f ? e * inv : 0.f;
+    }
+    // e, the quotient by Markstein's steps as in sample_kernel: where it differs, below
+    // e^-100, no weight is left
+    __device__ __forceinline__ float e(float l) const {
+        const float d = l - m;
+        float y;
+        if (r.T == 1.f) {
+            y = expf(d);
+        } else if (quick) {
+            const float q = fmaxf(d * rT, -100.f);
+            y = expf(fmaf(fmaf(-q, r.T, d), rT, q));
+        } else {
+            y = plain_e(l, m, r.T);
+        }
+        return floored(l == m ? 1.f : y);
     }
 };
 
-__global__ void __launch_bounds__(kThreads, 1) speculative_accept_kernel(const SpeculateArgs a) {
+template <bool BF16>
+__global__ void __launch_bounds__(kAcceptThreads, 1) speculative_accept_kernel(const SpeculateArgs a) {
+    constexpr int kWarps = kAcceptThreads / 32;
     __shared__ u64 s_sum[kWarps], s_cta[2][kMaxRowCtas];
     cg::cluster_group cluster = cg::this_cluster();
     const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -1386,13 +1450,10 @@ __global__ void __launch_bounds__(kThreads, 1) speculative_accept_kernel(const S
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     bool refused = false;
-    if (tid < W) {  // (W <= 1024 = kThreads)
+    if (tid < W) {  // (W <= 1024 = kAcceptThreads)
         const int y = a.draft[b * W + tid];
-        refused = true;
-        if (y >= 0 && y < V) {
-            const float p = RowProbs(a.rows, b * W + tid, false).p(y), q = RowProbs(a.rows, b * W + tid, true).p(y);
-            refused = !((double)a.uniforms[b * W + tid] * (double)q < (double)p);
-        }
+        const RowProbs<BF16> p(a.rows, b * W + tid, false), q(a.rows, b * W + tid, true);
+        refused = y < 0 || y >= V || !((double)a.uniforms[b * W + tid] * (double)q.p(y) < (double)p.p(y));
     }
     const unsigned some = __ballot_sync(kFull, refused);
     if (lane == 0) s_sum[warp] = some ? warp * 32 + __ffs(some) - 1 : 0x7fffffff;
@@ -1406,19 +1467,34 @@ __global__ void __launch_bounds__(kThreads, 1) speculative_accept_kernel(const S
     }
     if (first == W) return;  // the same in the whole cluster
 
-    const RowProbs p(a.rows, b * W + first, false), q(a.rows, b * W + first, true);
-    const long long run = ((long long)V + C * kWarps * 128 - 1) / (C * kWarps * 128) * 128;
-    const long long lo = min((long long)V, (rank * kWarps + warp) * run), hi = min((long long)V, lo + run);
-    auto own = [&](int v) { return w_of(p.e(v)); };
-    auto rest = [&](int v) { return __float2ull_rn(fmaxf(p.p(v) - q.p(v), 0.f) * 1099511627776.f); };
-    u64 total = 0, mine = 0, before = 0;
+    const RowProbs<BF16> p(a.rows, b * W + first, false), q(a.rows, b * W + first, true);
+    // the warp's run of `parts` times 32 tokens, 1 << log_step of them to a step
+    const int parts = (int)(((long long)V + C * kWarps * 32 - 1) / (C * kWarps * 32));
+    int log_step = 0;
+    while (parts > 32 << log_step) ++log_step;
+    const long long lo = (long long)(rank * kWarps + warp) * parts * 32;
     bool plain = false;  // rounding has left nothing: the target's own weights
+    auto weights = [&](long long v0) -> u64 {
+        const long long v = v0 + lane;
+        if (v >= V) return 0;
+        const float lp = p.logit((int)v), lq = q.logit((int)v);
+        if (!p.kept(lp, (int)v)) return 0;
+        const float e = p.e(lp);
+        if (plain) return w_of(e);
+        const float x = e * p.inv - (q.kept(lq, (int)v) ? q.e(lq) * q.inv : 0.f);
+        return __float2ull_rn(fmaxf(x, 0.f) * 1099511627776.f);
+    };
+    u64 total = 0, mine = 0, before = 0, step_sum = 0;
     for (int turn = 0; turn < 2; ++turn) {
-        mine = 0;
+        mine = step_sum = 0;
 #pragma unroll 4
-        for (long long v = lo + lane; v < hi; v += 32) mine += plain ? own((int)v) : rest((int)v);
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(kFull, mine, d);
+        for (int i = 0; i < parts; ++i) {
+            const u64 w = weights(lo + i * 32);  // (2^40 at most)
+            const u64 sum = __reduce_add_sync(kFull, (uint32_t)w & 0x3ffffffu) +
+                            ((u64)__reduce_add_sync(kFull, (uint32_t)(w >> 26)) << 26);
+            if (lane == i >> log_step) step_sum += sum;
+            mine += sum;
+        }
         if (lane == 0) s_sum[warp] = mine;
         __syncthreads();
         u64 cta = s_sum[lane], up = lane < warp ? cta : 0;
@@ -1450,17 +1526,21 @@ __global__ void __launch_bounds__(kThreads, 1) speculative_accept_kernel(const S
     u64 r = (u64)((double)u * (double)total);
     r = r < total ? r : total - 1;
     if (r < before || r >= before + mine) return;
-    for (long long v0 = lo; v0 < hi; v0 += 32) {
-        const long long v = v0 + lane;
-        const u64 w = v < hi ? (plain ? own((int)v) : rest((int)v)) : 0;
-        u64 x = w;
+    auto scan = [&](u64 x) {  // inclusive, from `before` on
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const u64 o = __shfl_up_sync(kFull, x, d);
             if (lane >= d) x += o;
         }
-        x += before;
-        if (r >= x - w && r < x) a.next_token[b] = (int)v;
+        return x + before;
+    };
+    u64 x = scan(step_sum);
+    const int step = __ffs(__ballot_sync(kFull, r < x)) - 1;
+    before = __shfl_sync(kFull, x - step_sum, step);
+    for (int i = step << log_step; i < (step + 1) << log_step; ++i) {
+        const u64 w = weights(lo + i * 32);
+        x = scan(w);
+        if (r >= x - w && r < x) a.next_token[b] = (int)(lo + i * 32 + lane);
         before = __shfl_sync(kFull, x, 31);
         if (before > r) break;
     }
@@ -1501,11 +1581,11 @@ cudaError_t sample_launch_t(const SampleArgs &a, cudaStream_t stream) {
         return launch_pdl(long_row_kernel<BF16, RECORD>, dim3((unsigned)rows), dim3(kLongThreads), 1, 0,
                           stream, a);
     int C = 1;  // a power of two: the bins divide by it
-    while (C < kMaxRowCtas && (C < hold || (rows * C * 2 <= sms && a.vocab > C * 4 * kThreads)))
+    while (C < kMaxRowCtas && (C < hold || (rows * C * 2 <= sms && a.vocab > C * 4 * kDrawThreads)))
         C *= 2;
     const int slice = ((a.vocab + C - 1) / C + 3) / 4 * 4;
-    const dim3 grid((unsigned)(rows * C)), block(kThreads);
-    size_t smem = (size_t)(slice + 4) * (BF16 ? 2 : 4);  // (a group more where rows begin within one)
+    const dim3 grid((unsigned)(rows * C)), block(RECORD ? kRecordThreads : kDrawThreads);
+    size_t smem = RECORD ? 0 : (size_t)(slice + 4) * (BF16 ? 2 : 4);  // (a group more where rows begin within one)
     if (C > 1) smem = std::max(smem, 2 * kBins * sizeof(uint32_t));  // (bins may be sent there)
     static std::atomic<bool> configured[64];  // the shared-memory opt-in, once per device
     if (dev >= 64 || !configured[dev].load(std::memory_order_acquire)) {
@@ -1530,8 +1610,9 @@ cudaError_t speculative_accept_launch(const SpeculateArgs &a, cudaStream_t strea
                                       : sample_launch_t<false, true>(a.rows, stream);
     if (e != cudaSuccess) return e;
     int C = 1;
-    while (C < kMaxRowCtas && a.rows.vocab > C * 4 * kThreads) C *= 2;
-    return launch_pdl(speculative_accept_kernel, dim3((unsigned)(a.rows.B * C)), dim3(kThreads), C, 0, stream, a);
+    while (C < kMaxRowCtas && a.rows.vocab > C * 4 * kAcceptThreads) C *= 2;
+    return launch_pdl(a.rows.bf16 ? speculative_accept_kernel<true> : speculative_accept_kernel<false>,
+                      dim3((unsigned)(a.rows.B * C)), dim3(kAcceptThreads), C, 0, stream, a);
 }
 
 cudaError_t sample_accept_launch(SampleArgs a, const int32_t *draft, int32_t *accepted,
