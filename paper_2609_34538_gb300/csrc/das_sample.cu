@@ -116,6 +116,7 @@ struct alignas(16) Shared {
     uint32_t list[kList];  // the CTA's keys in a bin
     uint2 all[kList];      // the cluster's, with their weights
     uint32_t list_n, key_min, key_max;
+    int n_cand;
     int bin, where;
     uint32_t cut;
     u64 above, target, sum, equal;
@@ -256,18 +257,21 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
     bool few = false;  // whether the candidates alone are left
     float mine = -INFINITY;
     src -= shift;
-    auto fetch4 = [&](int g, float (&f)[4]) {
-        if (4 * g >= shift && 4 * g + 4 <= len + shift) {
+    bool infinite = false;
+    using Vec = std::conditional_t<BF16, uint2, float4>;
+    auto whole = [&](int g) { return 4 * g >= shift && 4 * g + 4 <= len + shift; };
+    auto vector_of = [&](int g) {
+        const Vec *at = reinterpret_cast<const Vec *>(src) + g;
+        return RECORD ? *at : __ldcs(at);
+    };
+    auto unpack = [&](int g, const Vec &u, float (&f)[4]) {  // u: of a whole group
+        if (whole(g)) {
             if constexpr (BF16) {
-                const uint2 *at = reinterpret_cast<const uint2 *>(src) + g;
-                const uint2 u = RECORD ? *at : __ldcs(at);
                 f[0] = __uint_as_float(u.x << 16);
                 f[1] = __uint_as_float(u.x & 0xffff0000u);
                 f[2] = __uint_as_float(u.y << 16);
                 f[3] = __uint_as_float(u.y & 0xffff0000u);
             } else {
-                const float4 *at = reinterpret_cast<const float4 *>(src) + g;
-                const float4 u = RECORD ? *at : __ldcs(at);
                 f[0] = u.x;
                 f[1] = u.y;
                 f[2] = u.z;
@@ -285,11 +289,32 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = f[i] == f[i] ? f[i] + 0.f : -INFINITY;
+        if (infinite)  // (those have weight, and the same)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i] = f[i] == INFINITY ? 0.f : -INFINITY;
     };
-#pragma unroll 4
-    for (int g = tid; g < groups; g += kThreads) {
-        float f[4];
-        fetch4(g, f);
+    // kBatch groups from g on, `step` apart: all loads before the first is used
+    constexpr int kBatch = 4;
+    auto batch = [&](int g, int step, int end, auto f) {
+        Vec u[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            u[j] = Vec{};
+            if (whole(g + j * step)) u[j] = vector_of(g + j * step);
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            if (g + j * step - lane >= end) return;  // the same in the warp
+            float l[4];
+            unpack(g + j * step, u[j], l);
+            f(g + j * step, l);
+        }
+    };
+    // f(g, logits) of each group, those of a warp together
+    auto sweep = [&](auto f) {
+        for (int g = tid; g - lane < groups; g += kBatch * kThreads) batch(g, kThreads, groups, f);
+    };
+    auto first_seen = [&](const float (&f)[4]) {
         mine = fmaxf(fmaxf(mine, fmaxf(f[0], f[1])), fmaxf(f[2], f[3]));
         if (counted)
 #pragma unroll
@@ -302,7 +327,15 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
                     if (n < kSmall) reinterpret_cast<float *>(s.seg)[n] = f[i];
                 }
             }
-        if constexpr (RECORD) continue;
+    };
+    if constexpr (RECORD) {
+        sweep([&](int, const float (&f)[4]) { first_seen(f); });
+    }
+#pragma unroll 4
+    for (int g = tid; !RECORD && g < groups; g += kThreads) {
+        float f[4];
+        unpack(g, whole(g) ? vector_of(g) : Vec{}, f);
+        first_seen(f);
         if (BF16)
             reinterpret_cast<uint2 *>(held)[g] =
                 make_uint2(__float_as_uint(f[0]) >> 16 | (__float_as_uint(f[1]) & 0xffff0000u),
@@ -310,15 +343,11 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
         else
             reinterpret_cast<float4 *>(held)[g] = make_float4(f[0], f[1], f[2], f[3]);
     }
-    bool infinite = false;
     auto load4 = [&](int g, float (&l)[4]) {
         if (g >= groups) {
             l[0] = l[1] = l[2] = l[3] = -INFINITY;
         } else if (RECORD && !few) {
-            fetch4(g, l);
-            if (infinite)  // (those have weight, and the same)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) l[i] = l[i] == INFINITY ? 0.f : -INFINITY;
+            unpack(g, whole(g) ? vector_of(g) : Vec{}, l);
         } else if (BF16 && !few) {
             const uint2 u = reinterpret_cast<const uint2 *>(held)[g];
             l[0] = __uint_as_float(u.x << 16);
@@ -447,7 +476,8 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
     // are the first k of them whose predecessors' weights sum to less than the target.
     auto draw_sorted = [&](int n) {
         u64 x = 0;  // (a key above 0 marks a candidate)
-        if (tid < n) x = (u64)key_of(s.cand[tid]) << 32 | (uint32_t)(kThreads - 1 - tid);
+        if (tid < n)  // (a record's candidates are in no order)
+            x = (u64)key_of(s.cand[tid]) << 32 | (RECORD ? ~(uint32_t)s.cand_at[tid] : (uint32_t)(kThreads - 1 - tid));
         u64 *const there = reinterpret_cast<u64 *>(s.hist);  // [2][kThreads]
         static_assert(sizeof s.hist >= 2 * kThreads * sizeof(u64));
         int set = 0, span = 32;  // a bitonic sort, by the warps that it takes
@@ -496,7 +526,7 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
             u64 total;
             scan(wide(code), total);
             const int n_kept = __syncthreads_count(in);
-            if (tid == n_kept - 1) record((uint32_t)(x >> 32), s.cand_at[at], total);
+            if (tid == n_kept - 1) record((uint32_t)(x >> 32), (int)~(uint32_t)x, total);
             return;
         }
         __syncthreads();  // (the last reads of `there`)
@@ -527,7 +557,52 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
     // ---- a small top-k leaves few candidates: those not below `low`, in index order ----
     // Four bits of each group of a thread say which; their numbers, in eight bits of
     // a word per round of groups, are summed over the warp for four rounds at once.
-    if (k < a.vocab && k <= kCand / 4) {
+    int n_cand = 0;
+    if constexpr (RECORD) {
+        // (as they come: they are sorted by their indexes too, or what is found needs no order)
+        if (k < a.vocab && k <= kCand / 4) {
+            sweep([&](int g, const float (&l)[4]) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (l[i] >= low) {
+                        const uint32_t n = atomicAdd(&s.list_n, 1u);
+                        if (n >= kCand) continue;
+                        s.cand[n] = l[i];
+                        s.cand_at[n] = base + 4 * g + i - shift;
+                    }
+            });
+            __syncthreads();
+            n_cand = (int)s.list_n;
+            const int t = exchange(n_cand, 0, 0);
+            bool fit = true;
+            int n_row = 0, n_before = 0;
+            for (int r = 0; r < C; ++r) {
+                const int n = (int)min(s.xch[t][0][r], (u64)kCand + 1);
+                fit = fit && n <= kCand;
+                n_row += n;
+                if (r < rank) n_before += n;
+            }
+            if (fit && n_row <= kThreads) {
+                if (C > 1) {
+                    Shared *const to = of(0);
+                    for (int i = tid; rank > 0 && i < n_cand; i += kThreads) {
+                        to->cand[n_before + i] = s.cand[i];
+                        to->cand_at[n_before + i] = s.cand_at[i];
+                    }
+                    sync();
+                }
+                if (rank == 0) draw_sorted(n_row);
+                return;
+            }
+            if (fit) {
+                few = true;
+                groups = (n_cand + 3) / 4;
+                if (tid < 4 * groups - n_cand) s.cand[n_cand + tid] = -INFINITY;
+                if (tid == 0) s.n_cand = n_cand;
+            }
+            sync();
+        }
+    } else if (k < a.vocab && k <= kCand / 4) {
         constexpr int kRounds = kSliceBytes<BF16> / (BF16 ? 2 : 4) / 4 / kThreads;
         static_assert(kRounds * 4 * kThreads * (BF16 ? 2 : 4) == kSliceBytes<BF16> && kRounds * kWarps <= kMaxSegs);
         constexpr int kHits = (kRounds + 7) / 8, kCounts = (kRounds + 3) / 4;
@@ -628,6 +703,19 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
     static_assert(sizeof s.cand + sizeof s.cand_at >= sizeof s.hist && kValues == 2 * kBins &&
                   offsetof(Shared, cand_at) == sizeof s.cand, "bins sent");
 
+    // f(g, logits) of each group of the row, or of the candidates if they are in use
+    auto each_group = [&](auto f) {
+        if (RECORD && !few) {
+            sweep(f);
+        } else {
+            for (int g = tid; g - lane < groups; g += kThreads) {
+                float l[4];
+                load4(g, l);
+                f(g, l);
+            }
+        }
+    };
+
     // ---- the threshold of a sum over the logits from `from` up ----
     // Finds the largest t with the sum of f over logits > t below the target
     // (then s.above), leaves its key in s.cut and how many have it in s.equal;
@@ -656,9 +744,7 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
                     for (int i = tid; i < kValues / 4; i += kThreads)
                         reinterpret_cast<uint4 *>(s.hist)[i] = make_uint4(0, 0, 0, 0);
                     __syncthreads();
-                    for (int g = tid; g < groups; g += kThreads) {
-                        float l[4];
-                        load4(g, l);
+                    each_group([&](int, const float (&l)[4]) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const uint32_t at = value_bin(l[i]);
@@ -667,7 +753,7 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
                                 else if (fabsf(l[i]) < 1.f) small += kWeights ? wide(weight(l[i])) : 1;
                             }
                         }
-                    }
+                    });
                 }
                 const u64 small_all = [&] {  // the CTA's
                     u64 sum;
@@ -777,10 +863,8 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
                 }
             };
             if (level == 0) {
-                for (int g = tid; g - lane < groups; g += kThreads) {
-                    float l[4];
-                    load4(g, l);
-                    if (!__any_sync(kFull, fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])) >= lo)) continue;
+                each_group([&](int, const float (&l)[4]) {
+                    if (!__any_sync(kFull, fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])) >= lo)) return;
                     float e[4] = {0.f, 0.f, 0.f, 0.f};
                     if (kWeights) es_of(l, e);
 #pragma unroll
@@ -788,16 +872,14 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
                         const uint32_t bin = __float_as_uint(linear(l[i])) - 0x4b000000u;
                         if (l[i] >= lo) add(s.hist + bin, code_of(e[i]));
                     }
-                }
+                });
             } else {
-                for (int g = tid; g < groups; g += kThreads) {
-                    float l[4];
-                    load4(g, l);
+                each_group([&](int, const float (&l)[4]) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         if (l[i] >= lo && l[i] <= hi)
                             add(s.hist + bin_of(l[i]), kWeights ? weight(l[i]) : 0u);
-                }
+                });
             }
             // The bins' sums over the cluster: each CTA takes 1 / C of the bins,
             // up to kMost a thread in order, and tells the others its total.
@@ -854,9 +936,7 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
             // what is in the bin
             uint32_t kmin = kOne, kmax = 0, in_bin_n = 0;
             const float in_bin = (float)bin + 8388608.f;
-            for (int g = tid; g < groups; g += kThreads) {
-                float l[4];
-                load4(g, l);
+            each_group([&](int, const float (&l)[4]) {
                 uint32_t in = 0;
                 if (level == 0) {
 #pragma unroll
@@ -867,7 +947,7 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
                     for (int i = 0; i < 4; ++i)
                         in |= (uint32_t)(l[i] >= lo && l[i] <= hi && bin_of(l[i]) == bin) << i;
                 }
-                if (!in) continue;
+                if (!in) return;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if (!(in >> i & 1)) continue;
@@ -881,7 +961,7 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
                         if (n < kList) s.list[n] = key;
                     }
                 }
-            }
+            });
             if (BF16 && !few) {
                 in_bin_n = __reduce_add_sync(kFull, in_bin_n);
                 if (lane == 0 && in_bin_n) atomicAdd(&s.list_n, in_bin_n);
@@ -1010,27 +1090,81 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
         code_cut = floor_p > 0.f && !(e[0] >= floor_p) ? 0u : code_of(e[0]);
     }
 
-    // (a record needs no sums where the search has left one that min-p takes nothing from: expf is
-    // off by two steps at most, so no larger logit's e is below the floor if the cut's is well above)
-    bool summed = false;
     if constexpr (RECORD) {
-        const float l = at_cut;
-        summed = p < 1.f && (floor_p <= 0.f || (quick ? quick_e(l) : plain_e(l, m, T)) * (1.f - 0x1p-20f) >= floor_p);
-        if (summed && !part) {
-            if (rank == 0 && tid == 0) record(cut, ties ? 0x7fffffff : -1, kept_sum);
-            return;  // (after the barrier of search)
+        // Top-p's search has left the sum, if min-p takes nothing from it: expf is off by two steps at
+        // most, so no larger logit's e is below the floor if the cut's is well above.
+        u64 total = kept_sum;
+        const float e_cut = quick ? quick_e(at_cut) : plain_e(at_cut, m, T);
+        if (!(p < 1.f && (floor_p <= 0.f || e_cut * (1.f - 0x1p-20f) >= floor_p))) {
+            u64 sum = 0;
+            each_group([&](int, const float (&l)[4]) {
+                if (!(fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])) >= from)) return;
+                uint32_t w[4];
+                kept(l, w);
+                sum += (wide(w[0]) + wide(w[1])) + (wide(w[2]) + wide(w[3]));
+            });
+            u64 here;
+            scan(sum, here);
+            const int t = exchange(here, 0, 0);
+            total = part ? ties * wide(code_cut) : 0;
+            for (int r = 0; r < C; ++r) total += s.xch[t][0][r];
         }
+        if (!part) {
+            if (rank == 0 && tid == 0) record(cut, ties ? 0x7fffffff : -1, total);
+            return;
+        }
+        // the last kept one of those equal to the cut: of the candidates the one with ties - 1 before it,
+        if (few) {
+            for (int i = tid; i < n_cand; i += kThreads) {
+                if (s.cand[i] != at_cut) continue;
+                u64 before = 0;
+                for (int r = 0; r < C; ++r) {
+                    const Shared *o = of(r);
+                    for (int j = 0; j < o->n_cand; ++j) before += o->cand[j] == at_cut && o->cand_at[j] < s.cand_at[i];
+                }
+                if (before + 1 == ties) record(cut, s.cand_at[i], total);
+            }
+            sync();  // no CTA leaves while another reads its candidates
+            return;
+        }
+        // of the row by counts of its segments of 32 groups, a run of them to a warp, one to a lane
+        static_assert(kMaxSegs <= 32 * kWarps);
+        const int per = ((groups + 31) / 32 + kWarps - 1) / kWarps, g0 = warp * per * 32 + lane;
+        uint32_t own = 0;
+        for (int j = 0; j < per; j += kBatch)
+            batch(g0 + j * 32, 32, min(groups, (warp + 1) * per * 32), [&](int g, const float (&l)[4]) {
+                uint32_t n = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) n += l[i] == at_cut;
+                n = __reduce_add_sync(kFull, n);
+                if (lane == (g - g0) / 32) own = n;
+            });
+        u64 here, before = scan(own, here);
+        const int t = exchange(here, 0, 0);
+        for (int r = 0; r < rank; ++r) before += s.xch[t][0][r];
+        const unsigned found = __ballot_sync(kFull, before < ties && ties <= before + own);
+        if (!found) return;
+        const int seg = __ffs(found) - 1, g = g0 + 32 * seg;
+        float l[4];
+        load4(g, l);
+        uint32_t n = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n += l[i] == at_cut;
+        u64 place = __shfl_sync(kFull, before, seg) + warp_scan(n) - n;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (l[i] == at_cut && ++place == ties) record(cut, base + 4 * g + i - shift, total);
+        return;
     }
 
     // ---- the token at which the running sum in index order passes r ----
     const int segs = (groups + 31) / 32;
-#pragma unroll RECORD ? 4 : 1
     for (int g0 = warp * 32; g0 < groups; g0 += kThreads) {  // segments of 32 groups
         float l[4];
         load4(g0 + lane, l);
         const float most = fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3]));
         u64 sum = 0;
-        if (!summed && __any_sync(kFull, most >= from)) {
+        if (__any_sync(kFull, most >= from)) {
             uint32_t w[4];
             kept(l, w);
             sum = (u64)w[0] + w[1] + w[2] + w[3];
@@ -1071,35 +1205,6 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
             if (r < rank) before += s.xch[t][0][r];
             total += s.xch[t][0][r];
         }
-    }
-    if constexpr (RECORD) {
-        if (summed) total = kept_sum;
-        // the last kept one of those equal to the cut
-        if (!part) {
-            if (rank == 0 && tid == 0) record(cut, ties ? 0x7fffffff : -1, total);
-            return;
-        }
-        if (tid == 0) s.where = -1;
-        __syncthreads();
-        const u64 n = tid < segs ? s.n_seg[tid] : 0;
-        if (ties_before < ties && ties <= ties_before + n) {
-            s.where = tid;
-            s.equal = ties_before;
-        }
-        __syncthreads();
-        if (s.where < 0 || warp != 0) return;  // (in another CTA of the cluster)
-        const int g = s.where * 32 + lane;
-        float l[4];
-        load4(g, l);
-        uint32_t n_here = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) n_here += l[i] == at_cut;
-        u64 place = s.equal + warp_scan(n_here) - n_here;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (l[i] == at_cut && ++place == ties)
-                record(cut, few ? s.cand_at[4 * g + i] : base + 4 * g + i - shift, total);
-        return;
     }
     if (tid == 0) {
         float u = a.uniforms[row];
@@ -1388,9 +1493,8 @@ struct RowProbs {
     const Elem *logits;
     float m, inv, cut, rT;
     bool quick;
-    __device__ __forceinline__ RowProbs(const SampleArgs &a, size_t row, bool second) {
-        const size_t rows = (size_t)a.B * a.W;
-        r = a.records[second ? rows + row : row];
+    __device__ __forceinline__ RowProbs(const SampleArgs &a, const RowRecord &record, size_t row, bool second) {
+        r = record;
         logits = static_cast<const Elem *>(second ? a.second : a.logits) +
                  row * (size_t)(second ? a.second_stride : a.row_stride);
         const bool none = r.top == 0;  // (no logit above -inf)
@@ -1435,8 +1539,9 @@ struct RowProbs {
 
 template <bool BF16>
 __global__ void __launch_bounds__(kAcceptThreads, 1) speculative_accept_kernel(const SpeculateArgs a) {
-    constexpr int kWarps = kAcceptThreads / 32;
+    constexpr int kWarps = kAcceptThreads / 32, kBatch = 8;
     __shared__ u64 s_sum[kWarps], s_cta[2][kMaxRowCtas];
+    __shared__ RowRecord s_record[2];
     cg::cluster_group cluster = cg::this_cluster();
     const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -1452,13 +1557,15 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) speculative_accept_kernel(c
     bool refused = false;
     if (tid < W) {  // (W <= 1024 = kAcceptThreads)
         const int y = a.draft[b * W + tid];
-        const RowProbs<BF16> p(a.rows, b * W + tid, false), q(a.rows, b * W + tid, true);
+        const RowRecord *const at = a.rows.records + b * W + tid;
+        const RowProbs<BF16> p(a.rows, at[0], b * W + tid, false), q(a.rows, at[(size_t)a.rows.B * W], b * W + tid, true);
         refused = y < 0 || y >= V || !((double)a.uniforms[b * W + tid] * (double)q.p(y) < (double)p.p(y));
     }
     const unsigned some = __ballot_sync(kFull, refused);
     if (lane == 0) s_sum[warp] = some ? warp * 32 + __ffs(some) - 1 : 0x7fffffff;
     __syncthreads();
     const int first = (int)min(__reduce_min_sync(kFull, (uint32_t)s_sum[lane]), (uint32_t)W);
+    if (tid < 2 && first < W) s_record[tid] = a.rows.records[((size_t)tid * a.rows.B + b) * W + first];
     __syncthreads();
     if (rank == 0 && tid == 0) {
         a.accepted[b] = first;
@@ -1467,17 +1574,14 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) speculative_accept_kernel(c
     }
     if (first == W) return;  // the same in the whole cluster
 
-    const RowProbs<BF16> p(a.rows, b * W + first, false), q(a.rows, b * W + first, true);
+    const RowProbs<BF16> p(a.rows, s_record[0], b * W + first, false), q(a.rows, s_record[1], b * W + first, true);
     // the warp's run of `parts` times 32 tokens, 1 << log_step of them to a step
     const int parts = (int)(((long long)V + C * kWarps * 32 - 1) / (C * kWarps * 32));
     int log_step = 0;
     while (parts > 32 << log_step) ++log_step;
     const long long lo = (long long)(rank * kWarps + warp) * parts * 32;
     bool plain = false;  // rounding has left nothing: the target's own weights
-    auto weights = [&](long long v0) -> u64 {
-        const long long v = v0 + lane;
-        if (v >= V) return 0;
-        const float lp = p.logit((int)v), lq = q.logit((int)v);
+    auto weight = [&](long long v, float lp, float lq) -> u64 {  // (past the row lp is -inf)
         if (!p.kept(lp, (int)v)) return 0;
         const float e = p.e(lp);
         if (plain) return w_of(e);
@@ -1487,13 +1591,25 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) speculative_accept_kernel(c
     u64 total = 0, mine = 0, before = 0, step_sum = 0;
     for (int turn = 0; turn < 2; ++turn) {
         mine = step_sum = 0;
-#pragma unroll 4
-        for (int i = 0; i < parts; ++i) {
-            const u64 w = weights(lo + i * 32);  // (2^40 at most)
-            const u64 sum = __reduce_add_sync(kFull, (uint32_t)w & 0x3ffffffu) +
-                            ((u64)__reduce_add_sync(kFull, (uint32_t)(w >> 26)) << 26);
-            if (lane == i >> log_step) step_sum += sum;
-            mine += sum;
+        for (int i0 = 0; i0 < parts; i0 += kBatch) {
+            float lp[kBatch], lq[kBatch];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                const long long v = lo + (i0 + j) * 32 + lane;
+                lp[j] = lq[j] = -INFINITY;
+                if (i0 + j < parts && v < V) {
+                    lp[j] = p.logit((int)v);
+                    lq[j] = q.logit((int)v);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                const u64 w = weight(lo + (i0 + j) * 32 + lane, lp[j], lq[j]);  // (2^40 at most)
+                const u64 sum = __reduce_add_sync(kFull, (uint32_t)w & 0x3ffffffu) +
+                                ((u64)__reduce_add_sync(kFull, (uint32_t)(w >> 26)) << 26);
+                if (lane == (i0 + j) >> log_step) step_sum += sum;
+                mine += sum;
+            }
         }
         if (lane == 0) s_sum[warp] = mine;
         __syncthreads();
@@ -1538,9 +1654,10 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) speculative_accept_kernel(c
     const int step = __ffs(__ballot_sync(kFull, r < x)) - 1;
     before = __shfl_sync(kFull, x - step_sum, step);
     for (int i = step << log_step; i < (step + 1) << log_step; ++i) {
-        const u64 w = weights(lo + i * 32);
+        const long long v = lo + i * 32 + lane;
+        const u64 w = v < V ? weight(v, p.logit((int)v), q.logit((int)v)) : 0;
         x = scan(w);
-        if (r >= x - w && r < x) a.next_token[b] = (int)(lo + i * 32 + lane);
+        if (r >= x - w && r < x) a.next_token[b] = (int)v;
         before = __shfl_sync(kFull, x, 31);
         if (before > r) break;
     }
