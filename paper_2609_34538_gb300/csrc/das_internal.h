@@ -184,13 +184,13 @@ struct SampleArgs {
 };
 // What a row's filters leave: the tokens of a larger key than `key` and those of the key up to
 // index `last`, of e >= `floor`; top is the largest logit's key (0: no logit above -inf), total the
-// sum of the kept weights.
+// sum of the kept weights and inv the inverse of the probabilities' sum of e.
 struct alignas(16) RowRecord {
     uint32_t top, key;
     int32_t last;
     float T;
     float floor;
-    uint32_t unused;
+    float inv;
     unsigned long long total;
 };
 static_assert(sizeof(RowRecord) == DAS_RECORD_BYTES, "records");

@@ -140,6 +140,10 @@ __device__ __forceinline__ Source source_of(const SampleArgs &a, size_t row) {
     return {a.logits, row, a.row_stride, &a.sampling, (int)(row / a.W)};
 }
 
+__device__ __forceinline__ RowRecord record_of(uint32_t top, uint32_t key, int last, float T, float floor, u64 total) {
+    return {top, key, last, T, floor, 1.f / (float)((double)total * (1.0 / 4294967296.0)), total};
+}
+
 // With one proposal a sequence its acceptance needs no other row.
 __device__ __forceinline__ void accept_one(const SampleArgs &a, size_t row, int token) {
     if (!a.draft) return;
@@ -264,38 +268,41 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
         const Vec *at = reinterpret_cast<const Vec *>(src) + g;
         return RECORD ? *at : __ldcs(at);
     };
-    auto unpack = [&](int g, const Vec &u, float (&f)[4]) {  // u: of a whole group
-        if (whole(g)) {
-            if constexpr (BF16) {
-                f[0] = __uint_as_float(u.x << 16);
-                f[1] = __uint_as_float(u.x & 0xffff0000u);
-                f[2] = __uint_as_float(u.y << 16);
-                f[3] = __uint_as_float(u.y & 0xffff0000u);
-            } else {
-                f[0] = u.x;
-                f[1] = u.y;
-                f[2] = u.z;
-                f[3] = u.w;
-            }
-        } else {
+    auto part_of = [&](int g) {  // a group that is not whole, padded
+        Elem e[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                f[i] = -INFINITY;
-                if (4 * g + i >= shift && 4 * g + i < len + shift) {
-                    if constexpr (BF16) f[i] = __uint_as_float((uint32_t)src[4 * g + i] << 16);
-                    else f[i] = src[4 * g + i];
-                }
-            }
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (BF16) e[i] = 0xff80;
+            else e[i] = -INFINITY;
+            if (4 * g + i >= shift && 4 * g + i < len + shift) e[i] = src[4 * g + i];
         }
+        if constexpr (BF16) return make_uint2(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16);
+        else return make_float4(e[0], e[1], e[2], e[3]);
+    };
+    auto split = [](const Vec &u, float (&f)[4]) {  // as they come
+        if constexpr (BF16) {
+            f[0] = __uint_as_float(u.x << 16);
+            f[1] = __uint_as_float(u.x & 0xffff0000u);
+            f[2] = __uint_as_float(u.y << 16);
+            f[3] = __uint_as_float(u.y & 0xffff0000u);
+        } else {
+            f[0] = u.x;
+            f[1] = u.y;
+            f[2] = u.z;
+            f[3] = u.w;
+        }
+    };
+    auto unpack = [&](const Vec &u, float (&f)[4]) {
+        split(u, f);
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = f[i] == f[i] ? f[i] + 0.f : -INFINITY;
         if (infinite)  // (those have weight, and the same)
 #pragma unroll
             for (int i = 0; i < 4; ++i) f[i] = f[i] == INFINITY ? 0.f : -INFINITY;
     };
-    // kBatch groups from g on, `step` apart: all loads before the first is used
-    constexpr int kBatch = 4;
-    auto batch = [&](int g, int step, int end, auto f) {
+    // f(g, vector) of kBatch groups from g on, `step` apart: all loads before the first is used
+    auto batch = [&](auto groups_at_once, int g, int step, int end, auto f) {
+        constexpr int kBatch = decltype(groups_at_once)::value;
         Vec u[kBatch];
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
@@ -305,17 +312,17 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
             if (g + j * step - lane >= end) return;  // the same in the warp
-            float l[4];
-            unpack(g + j * step, u[j], l);
-            f(g + j * step, l);
+            if (!whole(g + j * step)) u[j] = part_of(g + j * step);
+            f(g + j * step, u[j]);
         }
     };
-    // f(g, logits) of each group, those of a warp together
+    // f(g, vector) of each group, those of a warp together
     auto sweep = [&](auto f) {
-        for (int g = tid; g - lane < groups; g += kBatch * kThreads) batch(g, kThreads, groups, f);
+        for (int g = tid; g - lane < groups; g += 4 * kThreads)
+            batch(std::integral_constant<int, 4>(), g, kThreads, groups, f);
     };
     auto first_seen = [&](const float (&f)[4]) {
-        mine = fmaxf(fmaxf(mine, fmaxf(f[0], f[1])), fmaxf(f[2], f[3]));
+        if (!(RECORD && BF16)) mine = fmaxf(fmaxf(mine, fmaxf(f[0], f[1])), fmaxf(f[2], f[3]));
         if (counted)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -329,12 +336,21 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
             }
     };
     if constexpr (RECORD) {
-        sweep([&](int, const float (&f)[4]) { first_seen(f); });
+        // (fmaxf and the bins take no NaN; key_of takes -0 for 0)
+        uint32_t most = 0xff80ff80u;  // bf16 pairs
+        sweep([&](int, const Vec &u) {
+            if constexpr (BF16)
+                asm("{\n .reg .b32 t;\n max.bf16x2 t, %1, %2;\n max.bf16x2 %0, %0, t;\n}" : "+r"(most) : "r"(u.x), "r"(u.y));
+            float f[4];
+            split(u, f);
+            first_seen(f);
+        });
+        if (BF16) mine = fmaxf(__uint_as_float(most << 16), __uint_as_float(most & 0xffff0000u));
     }
 #pragma unroll 4
     for (int g = tid; !RECORD && g < groups; g += kThreads) {
         float f[4];
-        unpack(g, whole(g) ? vector_of(g) : Vec{}, f);
+        unpack(whole(g) ? vector_of(g) : part_of(g), f);
         first_seen(f);
         if (BF16)
             reinterpret_cast<uint2 *>(held)[g] =
@@ -347,7 +363,7 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
         if (g >= groups) {
             l[0] = l[1] = l[2] = l[3] = -INFINITY;
         } else if (RECORD && !few) {
-            unpack(g, whole(g) ? vector_of(g) : Vec{}, l);
+            unpack(whole(g) ? vector_of(g) : part_of(g), l);
         } else if (BF16 && !few) {
             const uint2 u = reinterpret_cast<const uint2 *>(held)[g];
             l[0] = __uint_as_float(u.x << 16);
@@ -380,6 +396,8 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
     // n = ceil(k' / warps) + 1 leaves some 350 candidates of 32000 for k = 200, which
     // are sorted as 512; with n one less and the least of all warps they were 450 on
     // average and more than 512 in every third row (128 rows of 32000: 19.2 us, 17.1 now).
+    // With the 16 warps of a recorded row n is one more: 395 candidates, and 512 or fewer of
+    // 200 rows in all, where one more row in 200 had more with n as above.
     float m, low = -INFINITY;
     {
         auto sorted32 = [&](uint32_t x) {  // a warp's keys, the largest in lane 0
@@ -393,7 +411,7 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
             return x;
         };
         const uint32_t key = key_of(mine), top = __reduce_max_sync(kFull, key);
-        const long long kc = (k + C - 1) / C, n = min((kc + kWarps - 1) / kWarps + 1, 32ll);
+        const long long kc = (k + C - 1) / C, n = min((kc + kWarps - 1) / kWarps + (RECORD ? 2 : 1), 32ll);
         const bool bound = k < a.vocab && kc <= n * kWarps;
         if (bound) {
             const uint32_t nth = __shfl_sync(kFull, sorted32(key), (int)n - 1);
@@ -430,7 +448,7 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
     // (a key that load4 gives is one of the row, but for the infinite logits')
     auto record = [&](uint32_t cut, int last, u64 total) {
         if (infinite && cut == key_of(0.f)) cut = top;
-        a.records[row] = RowRecord{top, cut, last, T, floor_p, 0u, total};
+        a.records[row] = record_of(top, cut, last, T, floor_p, total);
     };
     if (infinite) {  // the infinite ones alone have weight, and the same
         if constexpr (!RECORD)
@@ -561,13 +579,16 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
     if constexpr (RECORD) {
         // (as they come: they are sorted by their indexes too, or what is found needs no order)
         if (k < a.vocab && k <= kCand / 4) {
-            sweep([&](int g, const float (&l)[4]) {
+            const float least = infinite ? INFINITY : low;
+            sweep([&](int g, const Vec &u) {
+                float l[4];
+                split(u, l);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (l[i] >= low) {
+                    if (l[i] >= least) {
                         const uint32_t n = atomicAdd(&s.list_n, 1u);
                         if (n >= kCand) continue;
-                        s.cand[n] = l[i];
+                        s.cand[n] = infinite ? 0.f : l[i] + 0.f;
                         s.cand_at[n] = base + 4 * g + i - shift;
                     }
             });
@@ -706,7 +727,11 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
     // f(g, logits) of each group of the row, or of the candidates if they are in use
     auto each_group = [&](auto f) {
         if (RECORD && !few) {
-            sweep(f);
+            sweep([&](int g, const Vec &u) {
+                float l[4];
+                unpack(u, l);
+                f(g, l);
+            });
         } else {
             for (int g = tid; g - lane < groups; g += kThreads) {
                 float l[4];
@@ -782,7 +807,8 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
                 u64 total;
                 u64 before = scan(own, total);
                 {
-                    const int t = exchange(total, 0, 0);
+                    if (tid == 0) s.bin = -1;
+                    const int t = exchange(total, 0, 0);  // (no CTA's s.bin is set from here on)
                     total = small;
                     for (int r = 0; r < C; ++r) {
                         if (r < rank) before += s.xch[t][0][r];
@@ -790,15 +816,11 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
                     }
                 }
                 if (i0 >= kValues / 2) before += small;
-                if (tid == 0) {
-                    s.target = target_of(total);
-                    s.bin = -1;
-                }
+                if (tid == 0) s.target = target_of(total);
                 __syncthreads();
                 target = s.target;
                 if (kWeights && target > total) return false;  // (the same in every CTA)
                 if (target <= total) {
-                    sync();  // no CTA's s.bin is set from here on
 #pragma unroll
                     for (int i = 0; i < kMost; ++i) {
                         if (n[i] && before < target && before + v[i] >= target)
@@ -1131,11 +1153,15 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
         static_assert(kMaxSegs <= 32 * kWarps);
         const int per = ((groups + 31) / 32 + kWarps - 1) / kWarps, g0 = warp * per * 32 + lane;
         uint32_t own = 0;
+        const float which = infinite ? INFINITY : at_cut;
+        constexpr int kBatch = BF16 ? 8 : 4;
         for (int j = 0; j < per; j += kBatch)
-            batch(g0 + j * 32, 32, min(groups, (warp + 1) * per * 32), [&](int g, const float (&l)[4]) {
+            batch(std::integral_constant<int, kBatch>(), g0 + j * 32, 32, min(groups, (warp + 1) * per * 32), [&](int g, const Vec &u) {
+                float l[4];
+                split(u, l);
                 uint32_t n = 0;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) n += l[i] == at_cut;
+                for (int i = 0; i < 4; ++i) n += l[i] == which;
                 n = __reduce_add_sync(kFull, n);
                 if (lane == (g - g0) / 32) own = n;
             });
@@ -1409,7 +1435,7 @@ __global__ void __launch_bounds__(kLongThreads) long_row_kernel(const SampleArgs
     for (int i = tid; i < V; i += kLongThreads) total += kept(i);
     total = block_reduce<u64>(total, sums, add);
     if constexpr (RECORD) {
-        if (tid == 0) a.records[row] = RowRecord{top, cut, last, T, floor_p, 0u, total};
+        if (tid == 0) a.records[row] = record_of(top, cut, last, T, floor_p, total);
         return;
     }
     float u = a.uniforms[row];
@@ -1491,7 +1517,7 @@ struct RowProbs {
     using Elem = std::conditional_t<BF16, uint16_t, float>;
     RowRecord r;
     const Elem *logits;
-    float m, inv, cut, rT;
+    float m, cut, rT;
     bool quick;
     __device__ __forceinline__ RowProbs(const SampleArgs &a, const RowRecord &record, size_t row, bool second) {
         r = record;
@@ -1501,7 +1527,6 @@ struct RowProbs {
         m = none ? 0.f : logit_of(r.top);
         cut = none ? INFINITY : logit_of(max(r.key, kKeyNone));
         if (none) r.last = -1;
-        inv = 1.f / (float)((double)r.total * (1.0 / 4294967296.0));
         rT = none ? 1.f : __frcp_rn(r.T);
         quick = r.T > 1e-18f && r.T < 1e18f && (__float_as_uint(r.T) & 0x7fffffu) != 0x7fffffu;
     }
@@ -1512,22 +1537,21 @@ struct RowProbs {
         return l == l ? l : -INFINITY;
     }
     __device__ __forceinline__ bool kept(float l, int v) const { return l > cut || (l == cut && v <= r.last); }
-    __device__ __forceinline__ float floored(float e) const { return r.floor > 0.f && !(e >= r.floor) ? 0.f : e; }
+    __device__ __forceinline__ float floored(float e) const { return e >= r.floor ? e : 0.f; }
     // of a token alone
     __device__ __forceinline__ float p(int v) const {
         const float l = logit(v);
         if (!kept(l, v)) return 0.f;
         const float e = floored(e_of(key_of(l), r.top, m, r.T));
-        return e > 0.f ? e * inv : 0.f;
+        return e > 0.f ? e * r.inv : 0.f;
     }
-    // e, the quotient by Markstein's steps as in sample_kernel: where it differs, below
-    // e^-100, no weight is left
+    // e; where all T are `quick` the quotient by Markstein's steps as in sample_kernel, which differ
+    // from the division below e^-100 alone, where no weight is left
+    template <bool QUICK>
     __device__ __forceinline__ float e(float l) const {
         const float d = l - m;
         float y;
-        if (r.T == 1.f) {
-            y = expf(d);
-        } else if (quick) {
+        if (QUICK) {
             const float q = fmaxf(d * rT, -100.f);
             y = expf(fmaf(fmaf(-q, r.T, d), rT, q));
         } else {
@@ -1539,7 +1563,7 @@ struct RowProbs {
 
 template <bool BF16>
 __global__ void __launch_bounds__(kAcceptThreads, 1) speculative_accept_kernel(const SpeculateArgs a) {
-    constexpr int kWarps = kAcceptThreads / 32, kBatch = 8;
+    constexpr int kWarps = kAcceptThreads / 32, kBatch = 2;
     __shared__ u64 s_sum[kWarps], s_cta[2][kMaxRowCtas];
     __shared__ RowRecord s_record[2];
     cg::cluster_group cluster = cg::this_cluster();
@@ -1581,15 +1605,19 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) speculative_accept_kernel(c
     while (parts > 32 << log_step) ++log_step;
     const long long lo = (long long)(rank * kWarps + warp) * parts * 32;
     bool plain = false;  // rounding has left nothing: the target's own weights
-    auto weight = [&](long long v, float lp, float lq) -> u64 {  // (past the row lp is -inf)
-        if (!p.kept(lp, (int)v)) return 0;
-        const float e = p.e(lp);
-        if (plain) return w_of(e);
-        const float x = e * p.inv - (q.kept(lq, (int)v) ? q.e(lq) * q.inv : 0.f);
-        return __float2ull_rn(fmaxf(x, 0.f) * 1099511627776.f);
+    // x 2^40 rounded, x in [0, 1], as (the upper part of it) 2^20 + the lower: 64-bit conversions
+    // are slow
+    auto weight = [&](auto quick, long long v, float lp, float lq) -> uint2 {  // (past the row lp is -inf)
+        if (!p.kept(lp, (int)v)) return make_uint2(0, 0);
+        const float e = p.template e<quick.value>(lp);
+        float x = e * p.r.inv - (q.kept(lq, (int)v) ? q.template e<quick.value>(lq) * q.r.inv : 0.f);
+        x = (plain ? e * 0x1p-8f : fmaxf(x, 0.f)) * 0x1p20f;
+        const uint32_t up = __float2uint_rz(x);
+        return make_uint2(up, __float2uint_rn((x - (float)up) * 0x1p20f));
     };
+    auto sum_of = [](uint2 w) { return ((u64)w.x << 20) + w.y; };
     u64 total = 0, mine = 0, before = 0, step_sum = 0;
-    for (int turn = 0; turn < 2; ++turn) {
+    auto sweep = [&](auto quick) {
         mine = step_sum = 0;
         for (int i0 = 0; i0 < parts; i0 += kBatch) {
             float lp[kBatch], lq[kBatch];
@@ -1604,13 +1632,18 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) speculative_accept_kernel(c
             }
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
-                const u64 w = weight(lo + (i0 + j) * 32 + lane, lp[j], lq[j]);  // (2^40 at most)
-                const u64 sum = __reduce_add_sync(kFull, (uint32_t)w & 0x3ffffffu) +
-                                ((u64)__reduce_add_sync(kFull, (uint32_t)(w >> 26)) << 26);
+                uint2 w = weight(quick, lo + (i0 + j) * 32 + lane, lp[j], lq[j]);
+                w = make_uint2(__reduce_add_sync(kFull, w.x), __reduce_add_sync(kFull, w.y));
+                const u64 sum = sum_of(w);
                 if (lane == (i0 + j) >> log_step) step_sum += sum;
                 mine += sum;
             }
         }
+    };
+    const bool quick = p.quick && q.quick;
+    for (int turn = 0; turn < 2; ++turn) {
+        if (quick) sweep(std::true_type());
+        else sweep(std::false_type());
         if (lane == 0) s_sum[warp] = mine;
         __syncthreads();
         u64 cta = s_sum[lane], up = lane < warp ? cta : 0;
@@ -1637,10 +1670,14 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) speculative_accept_kernel(c
         if (rank == 0 && tid == 0) a.next_token[b] = -1;
         return;
     }
-    float u = a.resample[b];
-    if (!(u >= 0.f)) u = 0.f;
-    u64 r = (u64)((double)u * (double)total);
-    r = r < total ? r : total - 1;
+    if (tid == 0) {  // (one thread: doubles are slow)
+        float u = a.resample[b];
+        if (!(u >= 0.f)) u = 0.f;
+        const u64 r = (u64)((double)u * (double)total);
+        s_sum[0] = r < total ? r : total - 1;
+    }
+    __syncthreads();
+    const u64 r = s_sum[0];
     if (r < before || r >= before + mine) return;
     auto scan = [&](u64 x) {  // inclusive, from `before` on
 #pragma unroll
@@ -1655,7 +1692,7 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) speculative_accept_kernel(c
     before = __shfl_sync(kFull, x - step_sum, step);
     for (int i = step << log_step; i < (step + 1) << log_step; ++i) {
         const long long v = lo + i * 32 + lane;
-        const u64 w = v < V ? weight(v, p.logit((int)v), q.logit((int)v)) : 0;
+        const u64 w = v < V ? sum_of(weight(std::false_type(), v, p.logit((int)v), q.logit((int)v))) : 0;
         x = scan(w);
         if (r >= x - w && r < x) a.next_token[b] = (int)v;
         before = __shfl_sync(kFull, x, 31);
