@@ -2,19 +2,25 @@
 // a byte for every 32 elements of a token's head.
 //
 // The mathematics.  A scale has 4 significant bits and a bf16 element 8, so a quotient x / s
-// comes within 2^-9 of a half only if it is one: x times the rounded reciprocal, rounded once
-// more to multiples of 2^-11 (by adding 6144), decides a code as the quotient does.
+// is a half or no nearer to one than 1/255 of itself: x times a reciprocal that is off by 2^-22,
+// rounded once more to multiples of 2^-11 (by adding 6144), decides a code as the quotient does.
+// A scale is rounded down by 1/17 of itself at most, so the largest quotient is below 7.5 and needs
+// no bound but where a scale is below 2^-14 (multiples of 2^-17), is cut at 60, or a group has an
+// infinity or NaN: such a warp takes the general way (quantise), token by token.
 //
-// A warp to a (sequence, page of it, slab, keys or values, kv head).  D / 8 lanes have a
-// token's row, 8 elements each, so that a scale is a matter of four lanes.  Keys lie token by
+// A warp to the tokens on a page of (sequence, slab, keys or values, kv head), of some of
+// them in turn.  D / 8 lanes have a token's row, 8 elements each, so that a scale is a matter
+// of four lanes; each of them has four tokens at once and makes the scale of one.
+// A code is the low bits of a sum with 1.5 2^23, and codes are put together by
+// multiply-adds of such sums, whose high parts a constant takes away.  Keys lie token by
 // token and go straight out.  Of the values eight tokens share a word: a lane collects its
-// elements' bits over eight tokens, the lanes of the other rows add theirs, and
-// each stores a part.  Words and scales that older tokens share are read first and
-// keep their bits.
+// elements' bits over its tokens and changes half of the words for the same half of the lanes
+// that have the other tokens.  Words that older tokens share are read first and keep their bits.
 //
 // The kernel is launched as a programmatic dependent of the previous kernel in the
 // stream: it reads nothing before griddepcontrol.wait, and every CTA executes that wait.
 #include <algorithm>
+#include <type_traits>
 
 #include "das_internal.h"
 
@@ -23,7 +29,7 @@ namespace {
 
 constexpr int kPage = DAS_PAGE_TOKENS;
 constexpr uint32_t kFull = 0xffffffffu;
-constexpr int kWarps = 4;
+constexpr int kWarps = 4, kJobs = 2;
 
 struct Append4Args {
     const uint16_t *fresh[2];  // staged keys, values
@@ -32,7 +38,7 @@ struct Append4Args {
     const int32_t *slots, *slot_start;
     int32_t *error_flag;
     int batch, W, pages, kv_heads, max_slots, pieces;
-    unsigned jobs;
+    int jobs, splits;  // (slab, keys or values, head)s, and the CTAs to a page that share them
 };
 
 __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {  // of sizes: NaN loses
@@ -55,7 +61,7 @@ struct Codes {
     uint32_t c[8];
     uint32_t byte;
 };
-__device__ __forceinline__ Codes quantise(uint4 x, int unit) {
+__device__ __noinline__ Codes quantise(uint4 x, int unit) {
     uint32_t w[4] = {x.x, x.y, x.z, x.w};
     uint32_t m = 0;
 #pragma unroll
@@ -106,32 +112,34 @@ __device__ __forceinline__ Codes quantise(uint4 x, int unit) {
     return r;
 }
 
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kWarps * 32) append_paged4_kernel(const Append4Args a) {
     constexpr int kLanes = D / 8, kRows = 32 / kLanes, kGroups = D / DAS_SCALE_GROUP;
+    constexpr int kPass = 4 * kRows, kOcts = kPass / 8;  // tokens at once, and eights of them
+    constexpr uint32_t kMagic = 0x4b400000u;             // 1.5 2^23
     const int lane = threadIdx.x & 31, row = lane / kLanes, l = lane % kLanes, warp = threadIdx.x >> 5;
-    unsigned x = blockIdx.x;
-    const int job = (int)(x / a.jobs) * kWarps + warp;
-    const int which = job >= a.kv_heads, h = job - (which ? a.kv_heads : 0);
-    x %= a.jobs;
-    const int piece = x % a.pieces;
-    x /= a.pieces;
-    const int b = x % a.batch;
-    const size_t slab = x / a.batch;
+    const int quarter = lane & 3;
+    const int part = blockIdx.x % a.splits, piece = blockIdx.x / a.splits % a.pieces;
+    const int b = blockIdx.x / a.splits / a.pieces;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (job >= 2 * a.kv_heads) return;
 
     const int s0 = a.slot_start[b];
     const long long n_all = (long long)a.slot_start[b + 1] - s0;
     if (n_all < 0 || n_all > a.W || s0 < 0 || s0 + n_all > a.max_slots) {
-        if (lane == 0) atomicOr(a.error_flag, kFlagInvalid);
+        if (threadIdx.x == 0) atomicOr(a.error_flag, kFlagInvalid);
         return;
     }
     if (n_all == 0) return;
     int slot = a.slots[s0], begin = 0, end = (int)n_all;
     if (slot < 0) {
-        if (lane == 0) atomicOr(a.error_flag, kFlagInvalid);
+        if (threadIdx.x == 0) atomicOr(a.error_flag, kFlagInvalid);
         return;
     }
     {  // the piece-th page that the tokens lie on
@@ -141,75 +149,127 @@ __global__ void __launch_bounds__(kWarps * 32) append_paged4_kernel(const Append
         end = min(t + kPage, end);
         if (piece) slot = a.slots[s0 + begin];
     }
-    const int page = slot / kPage, first = slot % kPage;
+    const int page = slot / kPage, first = slot % kPage, last = first + end - begin;
     if (slot < 0 || page >= a.pages || (piece && first)) {
-        if (lane == 0) atomicOr(a.error_flag, kFlagInvalid);
+        if (threadIdx.x == 0) atomicOr(a.error_flag, kFlagInvalid);
         return;
     }
-    const size_t tile = (slab * a.pages + page) * a.kv_heads + h;
     const size_t stride = (size_t)a.kv_heads * D;
-    const int unit = unit_log(a.unit[which], slab * a.kv_heads + h);
-    const uint4 *src = reinterpret_cast<const uint4 *>(a.fresh[which] + ((slab * a.batch + b) * a.W) * stride + h * D) + l;
-    auto load = [&](int t) {  // token t's part, or zeros
-        return t >= begin && t < end ? __ldcs(src + t * (stride / 8)) : make_uint4(0, 0, 0, 0);
-    };
-    uint8_t *const scales = a.scales[which] + tile * (kPage * kGroups);
-    if (which == 0) {
-        uint32_t *const codes = reinterpret_cast<uint32_t *>(a.codes[0] + tile * (kPage * D / 2)) + l;
-#pragma unroll 4
-        for (int t0 = begin; t0 < end; t0 += kRows) {
-            const int t = t0 + row, place = first + t - begin;
-            const Codes q = quantise(load(t), unit);
-            uint32_t w = 0;
+    for (int job = part * kWarps + warp; job < a.jobs; job += a.splits * kWarps) {
+        const int h = job % a.kv_heads, which = job / a.kv_heads & 1;
+        const size_t slab = job / a.kv_heads / 2;
+        const size_t tile = (slab * a.pages + page) * a.kv_heads + h;
+        const int unit = unit_log(a.unit[which], slab * a.kv_heads + h);
+        const float per_unit = exp2i(-unit);
+        // of the token at place 0 of the page (not read before `first`)
+        const uint16_t *src = a.fresh[which] + ((long long)((slab * a.batch + b) * a.W) + begin - first) * (long long)stride +
+                              h * D + 8 * l;
+        uint8_t *const scales = a.scales[which] + tile * (kPage * kGroups);
+        uint32_t *const codes = reinterpret_cast<uint32_t *>(a.codes[which] + tile * (kPage * D / 2));
+        for (int p0 = first / kPass * kPass; p0 < last; p0 += kPass) {
+            auto place = [&](int i) { return p0 + i * kRows + row; };
+            auto fresh = [&](int p) { return p >= first && p < last; };
+            uint4 x[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w |= q.c[j] << (4 * j);
-            if (t < end) {
-                codes[place * (D / 8)] = w;
-                if (l % 4 == 0) scales[place * kGroups + l / 4] = (uint8_t)q.byte;
+            for (int i = 0; i < 4; ++i) {
+                x[i] = make_uint4(0, 0, 0, 0);
+                if (fresh(place(i))) x[i] = __ldcs(reinterpret_cast<const uint4 *>(src + place(i) * (long long)stride));
             }
-        }
-    } else {
-        uint32_t *const codes = reinterpret_cast<uint32_t *>(a.codes[1] + tile * (kPage * D / 2));
-        const int last = first + end - begin;  // the place past the last
-        for (int o = first / 8; o * 8 < last; ++o) {  // eight places that share words
-            const int t0 = begin + o * 8 - first;     // the token at the first of them
-            uint32_t w[8];
+            // the largest sizes of four tokens, two to a word, and of this lane's one of them
+            uint32_t m[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = 0;
-            unsigned long long bytes = 0;
-#pragma unroll
-            for (int i = 0; i < 8 / kRows; ++i) {
-                const int at = i * kRows + row;
-                const Codes q = quantise(load(t0 + at), unit);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] |= q.c[j] << (4 * at);
-                bytes |= (unsigned long long)q.byte << (8 * at);
+            for (int i = 0; i < 4; ++i) {
+                m[i] = max_u16x2(max_u16x2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu),
+                                 max_u16x2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu));
+                if (!fresh(place(i))) m[i] = 0x3f80u;  // (any that needs no care)
             }
-            // the other rows' bits: lane (row, l) is to store its elements [row 8 / kRows, ...)
 #pragma unroll
-            for (int d = kLanes; d < 32; d <<= 1) {
+            for (int i = 0; i < 2; ++i) {
+                m[i] = max_u16x2(__byte_perm(m[i], m[i + 2], 0x5410), __byte_perm(m[i], m[i + 2], 0x7632));
 #pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] |= __shfl_xor_sync(kFull, w[j], d);
-                bytes |= __shfl_xor_sync(kFull, bytes, d);
+                for (int d = 1; d < 4; d <<= 1) m[i] = max_u16x2(m[i], __shfl_xor_sync(kFull, m[i], d));
             }
-            const int lo = max(first - o * 8, 0), hi = min(last - o * 8, 8);  // the new ones of the eight
-            const uint32_t keep = ~(uint32_t)(((1ull << 4 * hi) - 1) & ~((1ull << 4 * lo) - 1));
-            constexpr int kMine = 8 / kRows;
-            uint32_t *const dst = codes + o * D + 8 * l + kMine * row;
+            const uint32_t both = quarter & 1 ? m[1] : m[0], most = quarter & 2 ? both >> 16 : both & 0xffffu;
+            const float t = __uint_as_float(most << 16) * per_unit * (1.f / 7.f);
+            uint32_t bits = __float_as_uint(t);
+            bits = (bits + 0x7ffffu + (bits >> 20 & 1u)) & 0xfff00000u;
+            uint32_t byte = (bits >> 20) - (112u << 3);
+            float inv;
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(__uint_as_float(bits)));
+            inv *= per_unit;
+            uint32_t w[4][8];  // 0x4b400000 + code
+            if (__any_sync(kFull, most >= 0x7f80u || t < 6.103515625e-05f || bits > 0x42700000u)) {
 #pragma unroll
-            for (int j = 0; j < kMine; ++j) {
-                uint32_t v = w[j];
+                for (int i = 0; i < 4; ++i) {
+                    const Codes q = quantise(x[i], unit);
 #pragma unroll
-                for (int r = 1; r < kRows; ++r)
-                    if (row == r) v = w[r * kMine + j];
-                if (keep) v = (v & ~keep) | (dst[j] & keep);
-                dst[j] = v;
+                    for (int j = 0; j < 8; ++j) w[i][j] = kMagic + q.c[j];
+                    if (quarter == i) byte = q.byte;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float f = __shfl_sync(kFull, inv, (lane & ~3) + i);
+                    const uint32_t v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        w[i][j] = __float_as_uint(fmaf(__uint_as_float(j & 1 ? v[j >> 1] & 0xffff0000u : v[j >> 1] << 16), f,
+                                                       6144.f) + (12582912.f + 8.f - 6144.f));
+                }
             }
-            if (row == 0 && l % 4 == 0) {
-                uint8_t *const at = scales + (l / 4) * kPage + o * 8;
-                if (!keep) *reinterpret_cast<unsigned long long *>(at) = bytes;
-                else
-                    for (int i = lo; i < hi; ++i) at[i] = (uint8_t)(bytes >> 8 * i);
+            {
+                const int p = p0 + quarter * kRows + row;
+                if (fresh(p)) scales[which ? l / 4 * kPage + p : p * kGroups + l / 4] = (uint8_t)byte;
+            }
+            if (which == 0) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t c = -(kMagic * 0x11111111u);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) c += w[i][j] << (4 * j);
+                    if (fresh(place(i))) codes[place(i) * (D / 8) + l] = c;
+                }
+                continue;
+            }
+            const uint32_t at_row = 1u << 4 * row;  // (the token's place in the word)
+#pragma unroll
+            for (int o = 0; o < kOcts; ++o) {
+                constexpr int kEach = 4 / kOcts;  // a lane's tokens of the eight
+                uint32_t c[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    uint32_t sum = -(kMagic * (kEach == 4 ? 0x01010101u : 0x00010001u));
+#pragma unroll
+                    for (int i = 0; i < kEach; ++i) sum += w[o * kEach + i][j] << (4 * kRows * i);
+                    c[j] = sum * at_row;
+                }
+                // half of the words for the other half of the lanes' tokens, until all eight are in
+#pragma unroll
+                for (int d = 16, n = 4; d >= kLanes; d >>= 1, n >>= 1) {
+                    const bool up = lane & d;
+#pragma unroll
+                    for (int j = 0; j < n; ++j) {
+                        const uint32_t give = up ? c[j] : c[j + n], mine = up ? c[j + n] : c[j];
+                        c[j] = mine | __shfl_xor_sync(kFull, give, d);
+                    }
+                }
+                constexpr int kMine = 8 / kRows;
+                const int p = p0 + o * 8;  // the place of the first of the eight
+                const int lo = max(first - p, 0), hi = min(last - p, 8);  // the new ones
+                if (lo >= hi) continue;
+                const uint32_t keep = ~(uint32_t)(((1ull << 4 * hi) - 1) & ~((1ull << 4 * lo) - 1));
+                using Out = std::conditional_t<kMine == 4, uint4, uint2>;
+                // the first of the words that are left here: those of half the lanes' elements, halved
+                const int j0 = kMine == 4 ? (lane & 16 ? 4 : 0) : (lane & 16 ? 4 : 0) + (lane & 8 ? 2 : 0);
+                Out *const dst = reinterpret_cast<Out *>(codes + p / 8 * D + 8 * l + j0);
+                if (keep) {
+                    const Out old = *dst;
+                    const uint32_t *const was = reinterpret_cast<const uint32_t *>(&old);
+#pragma unroll
+                    for (int j = 0; j < kMine; ++j) c[j] = (c[j] & ~keep) | (was[j] & keep);
+                }
+                if constexpr (kMine == 4) *dst = make_uint4(c[0], c[1], c[2], c[3]);
+                else *dst = make_uint2(c[0], c[1]);
             }
         }
     }
@@ -238,11 +298,13 @@ cudaError_t append_paged4_launch(const das_kv_cache_paged4 &c, const void *k_new
     a.kv_heads = c.kv_heads;
     a.max_slots = max_slots;
     a.pieces = (W + 2 * kPage - 2) / kPage;
-    const long long jobs = (long long)c.depths * c.layers * batch * a.pieces;
-    const long long ctas = jobs * ((2LL * c.kv_heads + kWarps - 1) / kWarps);
+    if (batch == 0 || W == 0) return cudaSuccess;
+    const long long jobs = 2LL * c.depths * c.layers * c.kv_heads;
+    if (jobs > 0x7fffffffLL / 2) return cudaErrorInvalidValue;
+    a.jobs = (int)jobs;
+    a.splits = (int)((jobs + kWarps * kJobs - 1) / (kWarps * kJobs));
+    const long long ctas = (long long)a.splits * a.pieces * batch;
     if (ctas > 0x7fffffffLL) return cudaErrorInvalidValue;
-    a.jobs = (unsigned)jobs;
-    if (ctas == 0) return cudaSuccess;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas);
     cfg.blockDim = dim3(kWarps * 32);
