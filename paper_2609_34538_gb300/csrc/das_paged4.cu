@@ -8,8 +8,7 @@
 // no bound but where a scale is below 2^-14 (multiples of 2^-17), is cut at 60, or a group has an
 // infinity or NaN: such a warp takes the general way (quantise), token by token.
 //
-// A warp to the tokens on a page of (sequence, slab, keys or values, kv head), of some of
-// them in turn.  D / 8 lanes have a token's row, 8 elements each, so that a scale is a matter
+// A warp to the tokens on a page of (sequence, slab, keys or values, kv head).  D / 8 lanes have a token's row, 8 elements each, so that a scale is a matter
 // of four lanes; each of them has four tokens at once and makes the scale of one.
 // A code is the low bits of a sum with 1.5 2^23, and codes are put together by
 // multiply-adds of such sums, whose high parts a constant takes away.  Keys lie token by
@@ -29,7 +28,7 @@ namespace {
 
 constexpr int kPage = DAS_PAGE_TOKENS;
 constexpr uint32_t kFull = 0xffffffffu;
-constexpr int kWarps = 4, kJobs = 2;
+constexpr int kWarps = 4;
 
 struct Append4Args {
     const uint16_t *fresh[2];  // staged keys, values
@@ -38,7 +37,7 @@ struct Append4Args {
     const int32_t *slots, *slot_start;
     int32_t *error_flag;
     int batch, W, pages, kv_heads, max_slots, pieces;
-    int jobs, splits;  // (slab, keys or values, head)s, and the CTAs to a page that share them
+    int jobs, splits;  // (slab, keys or values, head)s, and the CTAs that they take
 };
 
 __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {  // of sizes: NaN loses
@@ -119,7 +118,7 @@ __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
 }
 
 template <int D>
-__global__ void __launch_bounds__(kWarps * 32) append_paged4_kernel(const Append4Args a) {
+__global__ void __launch_bounds__(kWarps * 32, 8) append_paged4_kernel(const Append4Args a) {
     constexpr int kLanes = D / 8, kRows = 32 / kLanes, kGroups = D / DAS_SCALE_GROUP;
     constexpr int kPass = 4 * kRows, kOcts = kPass / 8;  // tokens at once, and eights of them
     constexpr uint32_t kMagic = 0x4b400000u;             // 1.5 2^23
@@ -155,122 +154,123 @@ __global__ void __launch_bounds__(kWarps * 32) append_paged4_kernel(const Append
         return;
     }
     const size_t stride = (size_t)a.kv_heads * D;
-    for (int job = part * kWarps + warp; job < a.jobs; job += a.splits * kWarps) {
-        const int h = job % a.kv_heads, which = job / a.kv_heads & 1;
-        const size_t slab = job / a.kv_heads / 2;
-        const size_t tile = (slab * a.pages + page) * a.kv_heads + h;
-        const int unit = unit_log(a.unit[which], slab * a.kv_heads + h);
-        const float per_unit = exp2i(-unit);
-        // of the token at place 0 of the page (not read before `first`)
-        const uint16_t *src = a.fresh[which] + ((long long)((slab * a.batch + b) * a.W) + begin - first) * (long long)stride +
-                              h * D + 8 * l;
-        uint8_t *const scales = a.scales[which] + tile * (kPage * kGroups);
-        uint32_t *const codes = reinterpret_cast<uint32_t *>(a.codes[which] + tile * (kPage * D / 2));
-        for (int p0 = first / kPass * kPass; p0 < last; p0 += kPass) {
-            auto place = [&](int i) { return p0 + i * kRows + row; };
-            auto fresh = [&](int p) { return p >= first && p < last; };
-            uint4 x[4];
+    const int job = part * kWarps + warp;
+    if (job >= a.jobs) return;
+    const int h = job % a.kv_heads, which = job / a.kv_heads & 1;
+    const size_t slab = job / a.kv_heads / 2;
+    const size_t tile = (slab * a.pages + page) * a.kv_heads + h;
+    const int unit = unit_log(a.unit[which], slab * a.kv_heads + h);
+    const float per_unit = exp2i(-unit);
+    // of the token at place 0 of the page (not read before `first`)
+    const uint16_t *src = a.fresh[which] + ((long long)((slab * a.batch + b) * a.W) + begin - first) * (long long)stride +
+                          h * D + 8 * l;
+    uint8_t *const scales = a.scales[which] + tile * (kPage * kGroups);
+    uint32_t *const codes = reinterpret_cast<uint32_t *>(a.codes[which] + tile * (kPage * D / 2));
+    // (values by whole words; keys have no need to)
+    for (int p0 = which ? first / 8 * 8 : first; p0 < last; p0 += kPass) {
+        auto place = [&](int i) { return p0 + i * kRows + row; };
+        auto fresh = [&](int p) { return p >= first && p < last; };
+        uint4 x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = make_uint4(0, 0, 0, 0);
+            if (fresh(place(i))) x[i] = __ldcs(reinterpret_cast<const uint4 *>(src + place(i) * (long long)stride));
+        }
+        // the largest sizes of four tokens, two to a word, and of this lane's one of them
+        uint32_t m[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            m[i] = max_u16x2(max_u16x2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu),
+                             max_u16x2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu));
+            if (!fresh(place(i))) m[i] = 0x3f80u;  // (any that needs no care)
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            m[i] = max_u16x2(__byte_perm(m[i], m[i + 2], 0x5410), __byte_perm(m[i], m[i + 2], 0x7632));
+#pragma unroll
+            for (int d = 1; d < 4; d <<= 1) m[i] = max_u16x2(m[i], __shfl_xor_sync(kFull, m[i], d));
+        }
+        const uint32_t both = quarter & 1 ? m[1] : m[0], most = quarter & 2 ? both >> 16 : both & 0xffffu;
+        const float t = __uint_as_float(most << 16) * per_unit * (1.f / 7.f);
+        uint32_t bits = __float_as_uint(t);
+        bits = (bits + 0x7ffffu + (bits >> 20 & 1u)) & 0xfff00000u;
+        uint32_t byte = (bits >> 20) - (112u << 3);
+        float inv;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(__uint_as_float(bits)));
+        inv *= per_unit;
+        uint32_t w[4][8];  // 0x4b400000 + code
+        if (__any_sync(kFull, most >= 0x7f80u || t < 6.103515625e-05f || bits > 0x42700000u)) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                x[i] = make_uint4(0, 0, 0, 0);
-                if (fresh(place(i))) x[i] = __ldcs(reinterpret_cast<const uint4 *>(src + place(i) * (long long)stride));
+                const Codes q = quantise(x[i], unit);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[i][j] = kMagic + q.c[j];
+                if (quarter == i) byte = q.byte;
             }
-            // the largest sizes of four tokens, two to a word, and of this lane's one of them
-            uint32_t m[4];
+        } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                m[i] = max_u16x2(max_u16x2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu),
-                                 max_u16x2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu));
-                if (!fresh(place(i))) m[i] = 0x3f80u;  // (any that needs no care)
+                const float f = __shfl_sync(kFull, inv, (lane & ~3) + i);
+                const uint32_t v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    w[i][j] = __float_as_uint(fmaf(__uint_as_float(j & 1 ? v[j >> 1] & 0xffff0000u : v[j >> 1] << 16), f,
+                                                   6144.f) + (12582912.f + 8.f - 6144.f));
             }
+        }
+        {
+            const int p = p0 + quarter * kRows + row;
+            if (fresh(p)) scales[which ? l / 4 * kPage + p : p * kGroups + l / 4] = (uint8_t)byte;
+        }
+        if (which == 0) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                m[i] = max_u16x2(__byte_perm(m[i], m[i + 2], 0x5410), __byte_perm(m[i], m[i + 2], 0x7632));
+            for (int i = 0; i < 4; ++i) {
+                uint32_t c = -(kMagic * 0x11111111u);
 #pragma unroll
-                for (int d = 1; d < 4; d <<= 1) m[i] = max_u16x2(m[i], __shfl_xor_sync(kFull, m[i], d));
+                for (int j = 0; j < 8; ++j) c += w[i][j] << (4 * j);
+                if (fresh(place(i))) codes[place(i) * (D / 8) + l] = c;
             }
-            const uint32_t both = quarter & 1 ? m[1] : m[0], most = quarter & 2 ? both >> 16 : both & 0xffffu;
-            const float t = __uint_as_float(most << 16) * per_unit * (1.f / 7.f);
-            uint32_t bits = __float_as_uint(t);
-            bits = (bits + 0x7ffffu + (bits >> 20 & 1u)) & 0xfff00000u;
-            uint32_t byte = (bits >> 20) - (112u << 3);
-            float inv;
-            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(__uint_as_float(bits)));
-            inv *= per_unit;
-            uint32_t w[4][8];  // 0x4b400000 + code
-            if (__any_sync(kFull, most >= 0x7f80u || t < 6.103515625e-05f || bits > 0x42700000u)) {
+            continue;
+        }
+        const uint32_t at_row = 1u << 4 * row;  // (the token's place in the word)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const Codes q = quantise(x[i], unit);
+        for (int o = 0; o < kOcts; ++o) {
+            constexpr int kEach = 4 / kOcts;  // a lane's tokens of the eight
+            uint32_t c[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) w[i][j] = kMagic + q.c[j];
-                    if (quarter == i) byte = q.byte;
-                }
-            } else {
+            for (int j = 0; j < 8; ++j) {
+                uint32_t sum = -(kMagic * (kEach == 4 ? 0x01010101u : 0x00010001u));
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float f = __shfl_sync(kFull, inv, (lane & ~3) + i);
-                    const uint32_t v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+                for (int i = 0; i < kEach; ++i) sum += w[o * kEach + i][j] << (4 * kRows * i);
+                c[j] = sum * at_row;
+            }
+            // half of the words for the other half of the lanes' tokens, until all eight are in
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        w[i][j] = __float_as_uint(fmaf(__uint_as_float(j & 1 ? v[j >> 1] & 0xffff0000u : v[j >> 1] << 16), f,
-                                                       6144.f) + (12582912.f + 8.f - 6144.f));
+            for (int d = 16, n = 4; d >= kLanes; d >>= 1, n >>= 1) {
+                const bool up = lane & d;
+#pragma unroll
+                for (int j = 0; j < n; ++j) {
+                    const uint32_t give = up ? c[j] : c[j + n], mine = up ? c[j + n] : c[j];
+                    c[j] = mine | __shfl_xor_sync(kFull, give, d);
                 }
             }
-            {
-                const int p = p0 + quarter * kRows + row;
-                if (fresh(p)) scales[which ? l / 4 * kPage + p : p * kGroups + l / 4] = (uint8_t)byte;
+            constexpr int kMine = 8 / kRows;
+            const int p = p0 + o * 8;  // the place of the first of the eight
+            const int lo = max(first - p, 0), hi = min(last - p, 8);  // the new ones
+            if (lo >= hi) continue;
+            const uint32_t keep = ~(uint32_t)(((1ull << 4 * hi) - 1) & ~((1ull << 4 * lo) - 1));
+            using Out = std::conditional_t<kMine == 4, uint4, uint2>;
+            // the first of the words that are left here: those of half the lanes' elements, halved
+            const int j0 = kMine == 4 ? (lane & 16 ? 4 : 0) : (lane & 16 ? 4 : 0) + (lane & 8 ? 2 : 0);
+            Out *const dst = reinterpret_cast<Out *>(codes + p / 8 * D + 8 * l + j0);
+            if (keep) {
+                const Out old = *dst;
+                const uint32_t *const was = reinterpret_cast<const uint32_t *>(&old);
+#pragma unroll
+                for (int j = 0; j < kMine; ++j) c[j] = (c[j] & ~keep) | (was[j] & keep);
             }
-            if (which == 0) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t c = -(kMagic * 0x11111111u);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) c += w[i][j] << (4 * j);
-                    if (fresh(place(i))) codes[place(i) * (D / 8) + l] = c;
-                }
-                continue;
-            }
-            const uint32_t at_row = 1u << 4 * row;  // (the token's place in the word)
-#pragma unroll
-            for (int o = 0; o < kOcts; ++o) {
-                constexpr int kEach = 4 / kOcts;  // a lane's tokens of the eight
-                uint32_t c[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    uint32_t sum = -(kMagic * (kEach == 4 ? 0x01010101u : 0x00010001u));
-#pragma unroll
-                    for (int i = 0; i < kEach; ++i) sum += w[o * kEach + i][j] << (4 * kRows * i);
-                    c[j] = sum * at_row;
-                }
-                // half of the words for the other half of the lanes' tokens, until all eight are in
-#pragma unroll
-                for (int d = 16, n = 4; d >= kLanes; d >>= 1, n >>= 1) {
-                    const bool up = lane & d;
-#pragma unroll
-                    for (int j = 0; j < n; ++j) {
-                        const uint32_t give = up ? c[j] : c[j + n], mine = up ? c[j + n] : c[j];
-                        c[j] = mine | __shfl_xor_sync(kFull, give, d);
-                    }
-                }
-                constexpr int kMine = 8 / kRows;
-                const int p = p0 + o * 8;  // the place of the first of the eight
-                const int lo = max(first - p, 0), hi = min(last - p, 8);  // the new ones
-                if (lo >= hi) continue;
-                const uint32_t keep = ~(uint32_t)(((1ull << 4 * hi) - 1) & ~((1ull << 4 * lo) - 1));
-                using Out = std::conditional_t<kMine == 4, uint4, uint2>;
-                // the first of the words that are left here: those of half the lanes' elements, halved
-                const int j0 = kMine == 4 ? (lane & 16 ? 4 : 0) : (lane & 16 ? 4 : 0) + (lane & 8 ? 2 : 0);
-                Out *const dst = reinterpret_cast<Out *>(codes + p / 8 * D + 8 * l + j0);
-                if (keep) {
-                    const Out old = *dst;
-                    const uint32_t *const was = reinterpret_cast<const uint32_t *>(&old);
-#pragma unroll
-                    for (int j = 0; j < kMine; ++j) c[j] = (c[j] & ~keep) | (was[j] & keep);
-                }
-                if constexpr (kMine == 4) *dst = make_uint4(c[0], c[1], c[2], c[3]);
-                else *dst = make_uint2(c[0], c[1]);
-            }
+            if constexpr (kMine == 4) *dst = make_uint4(c[0], c[1], c[2], c[3]);
+            else *dst = make_uint2(c[0], c[1]);
         }
     }
 }
@@ -302,7 +302,7 @@ cudaError_t append_paged4_launch(const das_kv_cache_paged4 &c, const void *k_new
     const long long jobs = 2LL * c.depths * c.layers * c.kv_heads;
     if (jobs > 0x7fffffffLL / 2) return cudaErrorInvalidValue;
     a.jobs = (int)jobs;
-    a.splits = (int)((jobs + kWarps * kJobs - 1) / (kWarps * kJobs));
+    a.splits = (int)((jobs + kWarps - 1) / kWarps);
     const long long ctas = (long long)a.splits * a.pieces * batch;
     if (ctas > 0x7fffffffLL) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
