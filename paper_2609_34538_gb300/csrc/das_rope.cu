@@ -6,7 +6,7 @@
 // rows need no exchange but the sum of squares, and any output may overwrite its
 // input.  The angle n f_j is taken in turns as a 64-bit fraction: n times f_j / (2 pi)
 // modulo 1 is an integer product whose overflow is what is not wanted.  The lane's
-// four angles serve all of the token's heads; lanes of two heads share their work.
+// four angles serve all of the token's heads.
 //
 // Bound by memory, reads and writes of 2 bytes an element each.
 #include <algorithm>
@@ -49,9 +49,27 @@ __device__ __forceinline__ void weights(const void *w, bool bf16, int unit, floa
     }
 }
 
+// f / (2 pi) modulo 1 in steps of 2^-64: the significand times the first 64 bits of 1 / (2 pi).
+__device__ __forceinline__ unsigned long long turns(float f) {
+    constexpr unsigned long long kInverse = 0xa2f9836e4e441529ull;  // 2^66 / (2 pi)
+    const uint32_t bits = __float_as_uint(f), e = bits >> 23 & 0xffu;
+    if (e == 0xffu) return 0;
+    const uint32_t m = (bits & 0x7fffffu) | (e ? 0x800000u : 0u);
+    const unsigned long long low = (unsigned long long)m * (uint32_t)kInverse,
+                             high = (unsigned long long)m * (uint32_t)(kInverse >> 32) + (low >> 32);
+    // the product, high 2^32 + (the lower half of low), times 2^-down
+    const int down = 152 - (int)max(e, 1u);
+    unsigned long long t;
+    if (down >= 32) t = down < 96 ? high >> (down - 32) : 0;
+    else if (down >= 0) t = (high << 32 | (uint32_t)low) >> down | (down ? high >> 32 << (64 - down) : 0);
+    else t = down > -64 ? (high << 32 | (uint32_t)low) << -down : 0;
+    return bits >> 31 ? 0 - t : t;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kWarps * 32) rope_kernel(const RopeParams p) {
     constexpr int kLanes = D / 8, kRows = 32 / kLanes;  // lanes to a head, heads at once
+    constexpr int kBatch = 4;                           // steps whose loads are made together
     const RopeArgs &a = p.a;
     const int lane = threadIdx.x & 31, l = lane % kLanes, r = lane / kLanes;
     const long long item = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
@@ -75,68 +93,80 @@ __global__ void __launch_bounds__(kWarps * 32) rope_kernel(const RopeParams p) {
             cs[j] = 1.f;
             sn[j] = 0.f;
             if (!turned) continue;
-            double t = (double)a.inv_freq[4 * l + j] * 0.15915494309189535;  // 1 / (2 pi)
-            t -= floor(t);
-            const unsigned long long f = t < 1.0 ? (unsigned long long)(t * 18446744073709551616.0) : 0;
-            const float x = (float)(int)(n * f >> 32) * 4.656612873077393e-10f;  // half turns, 2^-31
+            const float x = (float)(int)(n * turns(a.inv_freq[4 * l + j]) >> 32) * 4.656612873077393e-10f;  // half turns, 2^-31
             sincospif(x, &sn[j], &cs[j]);
         }
     }
-    const int end = min(p.heads, (part + 1) * p.part);
-    for (int h0 = part * p.part; h0 < end; h0 += kRows) {
-        const int h = h0 + r;
-        const bool live = h < end;
-        const int kind = h < a.num_q_heads ? 0 : h < a.num_q_heads + a.kv_heads ? 1 : 2;
-        const int at = kind == 0 ? h : h - a.num_q_heads - (kind == 2 ? a.kv_heads : 0);
+    // the heads of a kind that are this warp's
+    int kind_begin = 0;
+#pragma unroll 1
+    for (int kind = 0; kind < 3; ++kind) {
+        const int n = kind == 0 ? a.num_q_heads : a.kv_heads;
+        const int begin = max(part * p.part - kind_begin, 0), end = min((part + 1) * p.part - kind_begin, n);
+        kind_begin += n;
         const das_head_rows &src = a.in[kind];
-        uint2 x0 = make_uint2(0, 0), x1 = x0;
-        if (live) {
-            const uint16_t *row = static_cast<const uint16_t *>(src.data) + b * src.batch_stride +
-                                  i * src.token_stride + at * src.head_stride;
-            x0 = *reinterpret_cast<const uint2 *>(row + 4 * u0);
-            x1 = *reinterpret_cast<const uint2 *>(row + 4 * u1);
-        }
-        float y[8];
-        unpack(x0, y);
-        unpack(x1, y + 4);
-        if (a.eps >= 0.f) {
-            float sum = 0.f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum += y[j] * y[j];
-#pragma unroll
-            for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor_sync(kFull, sum, d);
-            const float f = rsqrtf(sum * (1.f / D) + a.eps);
-            if (kind < 2) {
-                float w[8];
-                weights(a.weight[kind], a.weights_bf16, u0, w);
-                weights(a.weight[kind], a.weights_bf16, u1, w + 4);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = y[j] * f * w[j];
-            }
-        }
-        if (!live) continue;
+        if (!src.data || begin >= end) continue;
+        const uint16_t *const in = static_cast<const uint16_t *>(src.data) + b * src.batch_stride + i * src.token_stride;
+        uint16_t *const out = static_cast<uint16_t *>(a.out[kind]) + (b * a.max_block + i) * n * D;
+        float w[8];
         if (kind < 2) {
-            float z[8];
+            weights(a.weight[kind], a.weights_bf16, u0, w);
+            weights(a.weight[kind], a.weights_bf16, u1, w + 4);
+        }
+        for (int h0 = begin + r; h0 - r < end; h0 += kBatch * kRows) {
+            uint2 x0[kBatch], x1[kBatch];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                // pair j: elements j of both units, or 2 j and 2 j + 1 of the eight
-                const float s = a.interleaved ? y[2 * j] : y[j], t = a.interleaved ? y[2 * j + 1] : y[j + 4];
-                const float zs = s * cs[j] - t * sn[j], zt = t * cs[j] + s * sn[j];
-                z[j] = zs;
-                z[j + 4] = zt;
+            for (int k = 0; k < kBatch; ++k) {
+                const int h = h0 + k * kRows;
+                x0[k] = x1[k] = make_uint2(0, 0);
+                if (h < end) {
+                    const uint16_t *const row = in + h * src.head_stride;
+                    x0[k] = *reinterpret_cast<const uint2 *>(row + 4 * u0);
+                    x1[k] = *reinterpret_cast<const uint2 *>(row + 4 * u1);
+                }
             }
-            if (a.interleaved) {
-                x0 = make_uint2(pack(z[0], z[4]), pack(z[1], z[5]));
-                x1 = make_uint2(pack(z[2], z[6]), pack(z[3], z[7]));
-            } else {
-                x0 = make_uint2(pack(z[0], z[1]), pack(z[2], z[3]));
-                x1 = make_uint2(pack(z[4], z[5]), pack(z[6], z[7]));
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int h = h0 + k * kRows;
+                if (h - r >= end) break;
+                if (kind < 2) {
+                    float y[8];
+                    unpack(x0[k], y);
+                    unpack(x1[k], y + 4);
+                    if (a.eps >= 0.f) {
+                        float sum = 0.f;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) sum += y[j] * y[j];
+#pragma unroll
+                        for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor_sync(kFull, sum, d);
+                        const float f = rsqrtf(sum * (1.f / D) + a.eps);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) y[j] = y[j] * f * w[j];
+                    }
+                    float z[8];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        // pair j: elements j of both units, or 2 j and 2 j + 1 of the eight
+                        const float s = a.interleaved ? y[2 * j] : y[j], t = a.interleaved ? y[2 * j + 1] : y[j + 4];
+                        const float zs = s * cs[j] - t * sn[j], zt = t * cs[j] + s * sn[j];
+                        z[j] = zs;
+                        z[j + 4] = zt;
+                    }
+                    if (a.interleaved) {
+                        x0[k] = make_uint2(pack(z[0], z[4]), pack(z[1], z[5]));
+                        x1[k] = make_uint2(pack(z[2], z[6]), pack(z[3], z[7]));
+                    } else {
+                        x0[k] = make_uint2(pack(z[0], z[1]), pack(z[2], z[3]));
+                        x1[k] = make_uint2(pack(z[4], z[5]), pack(z[6], z[7]));
+                    }
+                }
+                if (h < end) {
+                    uint16_t *const row = out + h * D;
+                    *reinterpret_cast<uint2 *>(row + 4 * u0) = x0[k];
+                    *reinterpret_cast<uint2 *>(row + 4 * u1) = x1[k];
+                }
             }
         }
-        uint16_t *row = static_cast<uint16_t *>(a.out[kind]) +
-                        ((b * a.max_block + i) * (kind ? a.kv_heads : a.num_q_heads) + at) * D;
-        *reinterpret_cast<uint2 *>(row + 4 * u0) = x0;
-        *reinterpret_cast<uint2 *>(row + 4 * u1) = x1;
     }
 }
 
