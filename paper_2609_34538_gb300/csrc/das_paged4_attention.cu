@@ -62,9 +62,12 @@ constexpr float kBelow = 60.f;
 // Tensor memory: keys [2], values [2], S [2], O, the sums of P.
 constexpr int kKCol = 0, kVCol = 128, kSCol = 256, kOCol = 384, kSumCol = 448, kCols = 512;
 constexpr int kInfos = 64;  // ring of the tiles' visible keys
-// The end of a pair (its block tile, the read-out and what joins it) weighs kEnd tiles more.
-constexpr int kEnd = 4;
-constexpr int kLeast = 7;   // weight of a CTA's range, where there is more than one
+// The end of a pair (its block tile, the read-out and what joins it) weighs kEnd tiles more.  (24 sequences of
+// 500 to 16384 tokens, 4 x 32768 with 64 rows: 51.4 and 69.8 us; with 4 52.3 and 70.3, with 6 50.8 and 70.2.)
+constexpr int kEnd = 5;
+// Weight of a CTA's range, unless it is a pair.  (A pair of 1500 and one of 4000 tokens take 12.6 and 12.1 us,
+// with 10 13.7 and 14.7; with 6 11.0 and 11.4, but 4 pairs of 256 tokens 8.1 us instead of 7.0, as they are split.)
+constexpr int kLeast = 7;
 constexpr int kFan = 8;     // partials that are joined at once
 constexpr int kPrefetch = 8;  // pages pulled into L2 before the dependency wait
 
@@ -148,7 +151,7 @@ __device__ void make_plan(const Paged4AttnParams &p, Plan &pl, int P, int T) {
     long long W = 0;
     for (int b0 = 0; b0 < p.B; b0 += 32)
         W += (long long)__reduce_add_sync(kFull, (unsigned)weight(b0 + lane)) * p.Hkv;
-    const int ctas = (int)max(1ll, min((long long)p.num_ctas, W / kLeast));
+    const int ctas = (int)max(1ll, min((long long)p.num_ctas, max((long long)p.B * p.Hkv, W / kLeast)));
     pl.W = W;
     pl.ctas = ctas;
     pl.ntiles = 0;
@@ -355,7 +358,7 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
                   kThreads = Ro::kThreads;
     constexpr int kStages = Lt::kStages, R = kTurns ? N : N / 2;  // rows of a group
     constexpr int kStep = kTurns ? 2 : 1;                         // from one tile of a group to its next
-    constexpr int kChunk = 16;                                    // rows whose scores a softmax thread has at once
+    constexpr int kChunk = N == 16 ? 16 : 8;                      // rows whose scores a softmax thread has at once
     static_assert(R % kChunk == 0, "rows in chunks");
     extern __shared__ uint8_t smem_raw[];
     uint8_t *const sm = smem_raw + (-smem_u32(smem_raw) & 1023u);
