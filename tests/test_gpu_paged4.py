@@ -108,6 +108,39 @@ def test_append_ties_of_scales_and_codes():
     assert same(cache, ref.append(*old, one, one, k, v, slots, start))
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_append_values_of_every_kind_side_by_side(D):
+    """Groups that need care among many that do not, in every place of the four tokens that a lane has."""
+    rng = np.random.default_rng(6)
+    old, units, x, slots, start = append_case(rng, 2, 1, 4, D, [3, 40, 0], [130, 60, 25], 130, 8)
+    groups = x.reshape(-1, 32)
+    for y in (0.0, 2.0 ** -30, 2.0 ** 20, np.inf, np.nan, 2.0 ** -13):
+        at = rng.choice(len(groups), len(groups) // 60, replace=False)
+        few = rng.random((len(at), 32)) < 0.3
+        groups[at] = np.where(few, y, groups[at] * (min(y, 1.0) if y == y else 1.0))
+    x = groups.reshape(x.shape)
+    cache, k, v, flag = run_append(old, units, x, slots, start, 2)
+    assert same(cache, ref.append(*old, *units, k, v, slots, start)) and flag == 0
+
+
+def test_append_two_streams_at_once():
+    """Two sequences' tokens by two calls beside each other, on pages of their own."""
+    rng = np.random.default_rng(7)
+    old, units, x, slots, start = append_case(rng, 4, 2, 4, 128, [70, 5], [100, 100], 100, 8)
+    want, k, v, _ = run_append(old, units, x, slots, start)
+    cache = das.PagedKVCache4(u8(old[0]), u8(old[2]), u8(old[1]), u8(old[3]), *(f32(u) for u in units))
+    flag, ks, vs = dev_i32([0]), bf16(x[0]), bf16(x[1])
+    a = [(ks[:, :, b:b + 1].contiguous(), vs[:, :, b:b + 1].contiguous(), dev_i32(slots[start[b]:start[b + 1]]),
+          dev_i32([0, 100])) for b in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        for args, s in zip(a, streams):
+            das.das_kv_append_paged4(cache, *args, flag, stream=s)
+    torch.cuda.synchronize()
+    assert same(cache, host(want)) and flag.item() == 0
+
+
 def test_append_leaves_what_it_refuses():
     rng = np.random.default_rng(5)
     old, units, x, slots, start = append_case(rng, 1, 1, 2, 64, [60, 0, 0, 0], [8, 4, 4, 4], 8, 8)
@@ -265,6 +298,33 @@ def test_attention_one_dominant_key_among_thousands():
         o, l, dev = reference(c, c["q"], c["kb"], c["vb"], [4000], [2], scale=gap / 4)
         assert np.abs(o).max() > 0
         assert_close(f64(out), o, lse.cpu().numpy(), l, dev, where=f"gap {gap}")
+
+
+@pytest.mark.parametrize("Hq,Tm", [(1, 2), (4, 7), (8, 8)])
+@pytest.mark.parametrize("gap", [8.0, 61.0, 63.0, 70.0, 140.0, 300.0])
+def test_attention_steps_of_the_largest_score(Hq, Tm, gap):
+    """Keys' scores are steps of `gap` binary orders: the first key's is 7 below 0, then come keys of 0, of 1 and of 2 steps
+    within a tile and tiles later, so that the reference moves early, late, by a little or by more than a float's range, and
+    what was summed before it still counts where the step is small.  Rows have scores of their own; values are as they come."""
+    rng = np.random.default_rng(int(gap) + Tm)
+    D = 64
+    c = attention_case(rng, D, Hq, 1, Tm, [900, 300], [Tm, Tm - 1], poison=False)
+    c["q"] = np.zeros_like(c["q"])
+    c["q"][..., 0] = 1.0
+    c["q"][:, :, -1, 0] = 0.25                                # (a row whose steps are a quarter)
+    c["kb"] = np.zeros_like(c["kb"])
+    c["kb"][..., 0] = -6.0
+    c["ku"], c["k"][:], c["ks"][:] = np.ones(1), 0x88, 8 * 15   # scores 0, scale 1
+    code = lambda x: 8 + x | 8 << 4
+    for b, at in ((0, {0: -7, 100: 1, 500: 1, 501: 2, 700: 1}), (1, {0: -7, 1: -6, 290: 1})):
+        for t, x in at.items():
+            c["k"][c["table"][b, t // PAGE], 0, t % PAGE, 0] = code(x)
+    if gap < 10:                                              # all keys within a few steps of one another
+        for b in range(2):
+            for t in range(int(c["P"][b])):
+                c["k"][c["table"][b, t // PAGE], 0, t % PAGE, 0] = code(int(rng.integers(-7, 8)))
+    run_attention(c, scale=gap * float(np.log(2)) / 7, where=f"gap {gap} first")
+    run_attention(c, scale=gap * float(np.log(2)), where=f"gap {gap}")
 
 
 def test_attention_scales_far_apart():

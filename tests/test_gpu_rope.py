@@ -126,3 +126,28 @@ def test_empty_batch_other_stream_and_graph():
     graph.replay()
     again = das.das_qk_norm_rope(q, k, v, freq, P)
     assert all(torch.equal(a, b) for a, b in zip(outs, again)) and not torch.equal(outs[0], want[0])
+
+
+def test_frequencies_of_any_size():
+    """Frequencies from 2^-149 to 2^40, of both signs; no others than finite ones turn anything.  A frequency up to 2^20 is
+    held to 2^-46 turns (2^66 / (2 pi) is cut to a whole number), times 100 below 2^-39: nothing beside 2.5e-6."""
+    q, k, _, _, _ = make(6, 2, 100, 2, 1, 128, 128)
+    rng = np.random.default_rng(6)
+    f = np.ldexp(rng.uniform(1, 2, 64), rng.integers(-40, 21, 64)) * rng.choice([-1, 1], 64)
+    f[:6] = [0.0, -0.0, 2.0 ** -149, 1.0, 1048575.9375, -3.0 * 2.0 ** -140]
+    freq = torch.from_numpy(f.astype(np.float32)).cuda()
+    place = np.broadcast_to(np.arange(100), (2, 100))
+    qo, ko, _ = das.das_qk_norm_rope(q, k, None, freq, eps=None)
+    check(qo, q, None, None, place, freq, False, np.ones((2, 100), bool))
+    freq[3], freq[9], freq[11] = torch.inf, -torch.inf, torch.nan
+    got, _, _ = das.das_qk_norm_rope(q, k, None, freq, eps=None)
+    still = [3, 9, 11, 67, 73, 75]
+    assert torch.equal(got[..., still], q[..., still])
+    rest = [i for i in range(128) if i not in still]
+    assert torch.equal(got[..., rest], qo[..., rest])
+    freq[5] = 2.0 ** 40                                      # held to 2^-26 turns at position 1
+    got, _, _ = das.das_qk_norm_rope(q, k, None, freq, eps=None)
+    turn = 2.0 ** 40 / (2 * np.pi) % 1.0                     # (binary64 has 2^-16 of it: 1e-4 of a turn)
+    want = f64(q)[:, 1, :, 5] * np.cos(2 * np.pi * turn) - f64(q)[:, 1, :, 69] * np.sin(2 * np.pi * turn)
+    size = np.abs(f64(q)[:, 1, :, 5]) + np.abs(f64(q)[:, 1, :, 69])
+    assert (np.abs(f64(got)[:, 1, :, 5] - want) <= half_ulp_bf16(size) + 1e-3 * size).all()

@@ -170,3 +170,69 @@ def test_empty_batch_other_stream_and_graph():
         torch.cuda.synchronize()
         want = das.das_speculative_accept(target, drafter, ids, u, again)
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [900, 33000, 70001])
+def test_ties_at_the_cut(V, dtype):
+    """Few different logits: top-k and top-p end among thousands of equal ones, and proposals are drawn of them."""
+    B, W = 6, 3
+    g = torch.Generator(device="cuda").manual_seed(V)
+    target, drafter = (torch.randint(-3, 3, (B, W, V), generator=g, device="cuda").float().div(2).to(dtype) for _ in range(2))
+    target[3:], drafter[3:] = target[3:] / 64 * 0, 0.0        # all equal, -0 among them
+    target[4, :, ::2] = -0.0
+    u, again, u0 = (torch.rand(s, generator=g, device="cuda") for s in ((B, W), (B,), (B, W)))
+    for params in ((1.0, 300, 1.0, 0.0), (0.7, 300, 0.6, 0.0), (1.0, 0, 0.35, 0.0), (1.0, 700, 0.9, 0.2), (1.3, 0, 0.99, 0.1),
+                   (1.0, 0, 1.0, 0.6)):
+        full = lambda i, dt: torch.full((B,), params[i], dtype=dt, device="cuda")
+        ids, _ = das.das_sample(drafter, u0, full(0, torch.float32), full(1, torch.int32), full(2, torch.float32),
+                                full(3, torch.float32))
+        check(target, drafter, ids, u, again, [params] * B)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_candidates_of_every_number(dtype):
+    """Numbers of the largest logits around what is sorted (512) and listed (2048 to a part of the row), with equal ones among
+    them and few others near; infinite ones among and beside them."""
+    V = 20000
+    for n, k in ((500, 400), (513, 500), (600, 512), (2040, 512), (2100, 512), (9000, 512), (30, 511)):
+        g = torch.Generator(device="cuda").manual_seed(n)
+        target = torch.randn((2, 2, V), generator=g, device="cuda") - 20
+        where = torch.randperm(V, generator=g, device="cuda")[:n]
+        target[:, :, where] = torch.randint(0, 8, (2, 2, n), generator=g, device="cuda").float() / 4
+        target[1, 1, where[::3]] = torch.inf
+        drafter = target.roll(1, -1)
+        u, again, u0 = (torch.rand(s, generator=g, device="cuda") for s in ((2, 2), (2,), (2, 2)))
+        for params in ((1.0, k, 1.0, 0.0), (0.9, k, 0.7, 0.3)):
+            full = lambda i, dt: torch.full((2,), params[i], dtype=dt, device="cuda")
+            ids, _ = das.das_sample(drafter.to(dtype), u0, full(0, torch.float32), full(1, torch.int32),
+                                    full(2, torch.float32), full(3, torch.float32))
+            check(target.to(dtype), drafter.to(dtype), ids, u, again, [params] * 2)
+
+
+def test_the_largest_logits_and_temperatures():
+    """Temperatures whose quotients go the plain way, logits past the counted bins, rows of one logit above -inf."""
+    target, drafter, u, again, u0 = make(12, 5, 2, 3000, torch.bfloat16, spread=300.0)
+    target[4, :, 1:], drafter[4, :, :-1] = -torch.inf, -torch.inf
+    params = [(1e-30, 0, 0.9, 0.0), (1e25, 0, 0.9, 0.0), (float(np.float32(1.9999999)), 0, 0.9, 0.0), (300.0, 50, 0.9, 0.01),
+              (1.0, 10, 0.9, 0.1)]
+    ids = torch.stack([drafter[b].float().argmax(-1) for b in range(5)]).int()
+    check(target, drafter, ids, u, again, params)
+
+
+def test_two_streams_at_once():
+    """Calls that run beside each other share nothing."""
+    cases = [make(13 + i, 4, 4, 32000, torch.float32) for i in range(2)]
+    ids = [das.das_sample(c[1], c[4])[0] for c in cases]
+    want = [das.das_speculative_accept(*c[:2], i, *c[2:4], top_k=torch.full((4,), 100, dtype=torch.int32, device="cuda"))
+            for c, i in zip(cases, ids)]
+    k = torch.full((4,), 100, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(10):
+        for i, (c, s) in enumerate(zip(cases, streams)):
+            got[i].append(das.das_speculative_accept(*c[:2], ids[i], *c[2:4], top_k=k, stream=s))
+    torch.cuda.synchronize()
+    for w, runs in zip(want, got):
+        assert all(torch.equal(a, b) for r in runs for a, b in zip(w, r))
