@@ -85,7 +85,8 @@ __device__ __forceinline__ T block_reduce(T v, T *sums, F f) {
 // ---- a row in the shared memory of a cluster ---------------------------------------
 constexpr int kDrawThreads = 1024;
 // Rows that are recorded are not held but read again, from L2: two CTAs of half the threads
-// share an SM, and one's waits are the other's time.
+// share an SM, and one's waits are the other's time (2 x 128 rows of 32000 and the acceptance: 28.7 us,
+// 40 with the rows held; 2 x 64 of 128257: 50 us).
 constexpr int kRecordThreads = 512;
 constexpr int kMaxRowCtas = 8;                 // a portable cluster
 // Logits per CTA, as they come: what shared memory holds, and fewer than 2^16, so that
@@ -117,6 +118,7 @@ struct alignas(16) Shared {
     uint2 all[kList];      // the cluster's, with their weights
     uint32_t list_n, key_min, key_max;
     int n_cand;
+    uint4 edge[3];  // a recorded part's first and last group, where they are not whole, and padding
     int bin, where;
     uint32_t cut;
     u64 above, target, sum, equal;
@@ -279,6 +281,10 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
         if constexpr (BF16) return make_uint2(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16);
         else return make_float4(e[0], e[1], e[2], e[3]);
     };
+    if constexpr (RECORD) {  // (out of the loops, whose code would be three times as long)
+        if (tid < 3) reinterpret_cast<Vec &>(s.edge[tid]) = part_of(tid == 0 ? 0 : groups - 2 + tid);
+        __syncthreads();
+    }
     auto split = [](const Vec &u, float (&f)[4]) {  // as they come
         if constexpr (BF16) {
             f[0] = __uint_as_float(u.x << 16);
@@ -306,13 +312,13 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
         Vec u[kBatch];
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
-            u[j] = Vec{};
-            if (whole(g + j * step)) u[j] = vector_of(g + j * step);
+            const int at = g + j * step;
+            if (whole(at)) u[j] = vector_of(at);
+            else u[j] = reinterpret_cast<const Vec &>(s.edge[at >= groups ? 2 : at > 0]);
         }
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
             if (g + j * step - lane >= end) return;  // the same in the warp
-            if (!whole(g + j * step)) u[j] = part_of(g + j * step);
             f(g + j * step, u[j]);
         }
     };
@@ -790,20 +796,20 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
                 const int ts = exchange(small_all, 0, 0);  // (and the bins are there)
                 small = 0;
                 for (int r = 0; r < C; ++r) small += s.xch[ts][0][r];
-                // as the linear bins below: 1 / C of the bins to a CTA, up to kMost a thread
-                constexpr int kMost = kValues / kThreads;
-                u64 v[kMost] = {}, own = 0;
-                uint32_t n[kMost] = {};
+                // as the linear bins below: 1 / C of the bins to a CTA, some a thread
+                // (not unrolled, and the bins of the thread that has the threshold added up again: code that is run
+                // once costs its fetching)
                 const int i0 = rank * per_cta + tid * per_thread;
-                if (tid * per_thread < per_cta) {
-#pragma unroll
-                    for (int i = 0; i < kMost; ++i) {
-                        if (i >= per_thread) break;
-                        for (int r = 0; r < C; ++r) n[i] += bins[r * per_cta + tid * per_thread + i];
-                        if (n[i]) v[i] = kWeights ? n[i] * wide(weight(value_of(i0 + i))) : n[i];
-                        own += v[i];
-                    }
-                }
+                const bool has = tid * per_thread < per_cta;
+                auto bin_sum = [&](int i, uint32_t &n) -> u64 {
+                    n = 0;
+                    for (int r = 0; r < C; ++r) n += bins[r * per_cta + tid * per_thread + i];
+                    return !n ? 0 : kWeights ? n * wide(weight(value_of(i0 + i))) : n;
+                };
+                u64 own = 0;
+                uint32_t n;
+#pragma unroll 1
+                for (int i = 0; has && i < per_thread; ++i) own += bin_sum(i, n);
                 u64 total;
                 u64 before = scan(own, total);
                 {
@@ -821,20 +827,24 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
                 target = s.target;
                 if (kWeights && target > total) return false;  // (the same in every CTA)
                 if (target <= total) {
-#pragma unroll
-                    for (int i = 0; i < kMost; ++i) {
-                        if (n[i] && before < target && before + v[i] >= target)
-                            for (int r = 0; r < C; ++r) {
-                                Shared *o = of(r);
-                                o->bin = i0 + i;
-                                o->above = before;
-                                o->equal = n[i];
+                    if (has && before < target && before + own >= target)
+#pragma unroll 1
+                        for (int i = 0; i < per_thread; ++i) {
+                            const u64 v = bin_sum(i, n);
+                            if (n && before + v >= target) {
+                                for (int r = 0; r < C; ++r) {
+                                    Shared *o = of(r);
+                                    o->bin = i0 + i;
+                                    o->above = before;
+                                    o->equal = n;
+                                }
+                                break;
                             }
-                        // the small ones lie before the first bin of the negative values
-                        if (i0 + i == kValues / 2 && i < per_thread && before - small < target && before >= target)
-                            for (int r = 0; r < C; ++r) of(r)->above = before - small;
-                        before += v[i];
-                    }
+                            before += v;
+                        }
+                    // the small ones lie before the first bin of the negative values
+                    else if (has && i0 == kValues / 2 && before - small < target && before >= target)
+                        for (int r = 0; r < C; ++r) of(r)->above = before - small;
                     sync();
                     if (s.bin >= 0) {
                         if (tid == 0) s.cut = key_of(value_of(s.bin));
@@ -904,27 +914,23 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
                 });
             }
             // The bins' sums over the cluster: each CTA takes 1 / C of the bins,
-            // up to kMost a thread in order, and tells the others its total.
+            // some a thread in order, and tells the others its total.
             const int per_cta = kBins / C, per_thread = max(1, per_cta / kThreads);
             if (C > 1) __syncthreads();
             const uint32_t *bins = send_bins(kWeights ? 2 * kBins : kBins, per_cta, 2 * per_cta);
             sync();
-            constexpr int kMost = kBins / kThreads;
-            u64 v[kMost] = {}, own = 0;
-#pragma unroll
-            for (int i = 0; i < kMost; ++i) {
-                const int at = tid * per_thread + i;
-                if (i >= per_thread || at >= per_cta) break;
-                if (C == 1) {
-                    v[i] = s.hist[at] + ((u64)s.hist[kBins + at] << 16);
-                } else {
-                    for (int r = 0; r < C; ++r) {
-                        v[i] += bins[2 * r * per_cta + at];
-                        if (kWeights) v[i] += (u64)bins[(2 * r + 1) * per_cta + at] << 16;
-                    }
+            auto bin_sum = [&](int at) -> u64 {
+                if (C == 1) return s.hist[at] + ((u64)s.hist[kBins + at] << 16);
+                u64 v = 0;
+                for (int r = 0; r < C; ++r) {
+                    v += bins[2 * r * per_cta + at];
+                    if (kWeights) v += (u64)bins[(2 * r + 1) * per_cta + at] << 16;
                 }
-                own += v[i];
-            }
+                return v;
+            };
+            u64 own = 0;
+#pragma unroll 1
+            for (int at = tid * per_thread, i = 0; i < per_thread && at < per_cta; ++i, ++at) own += bin_sum(at);
             u64 total;
             u64 before = scan(own, total);
             if (C > 1) {
@@ -942,16 +948,20 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
                 if (target > total) return false;  // (the same in every CTA)
             }
             before += above;
-#pragma unroll
-            for (int i = 0; i < kMost; ++i) {
-                if (before < target && before + v[i] >= target)
-                    for (int r = 0; r < C; ++r) {
-                        Shared *o = of(r);
-                        o->bin = rank * per_cta + tid * per_thread + i;
-                        o->above = before;
+            if (before < target && before + own >= target)
+#pragma unroll 1
+                for (int at = tid * per_thread;; ++at) {
+                    const u64 v = bin_sum(at);
+                    if (before + v >= target) {
+                        for (int r = 0; r < C; ++r) {
+                            Shared *o = of(r);
+                            o->bin = rank * per_cta + at;
+                            o->above = before;
+                        }
+                        break;
                     }
-                before += v[i];
-            }
+                    before += v;
+                }
             sync();
             const uint32_t bin = (uint32_t)s.bin;
             above = s.above;
@@ -1508,7 +1518,11 @@ __global__ void __launch_bounds__(kScanWarps * 32)
 
 // ---- proposals that were drawn by chance -------------------------------------------
 // From the rows' records: the first proposal that is refused, and the draw in its place from
-// what the target's row has more.  A cluster to a sequence; each of its warps has a run of
+// what the target's row has more.  What bounds a call: of the 50 us of 64 proposals of 128257 bf16
+// logits each, whose 33 MB take 4.8 us, the rows' first pass (largest logit and bins) takes 12, the
+// look for the cut 10, the count of the logits equal to it 6, and this kernel 13, of which 8 are the
+// sweep over one row of target and drafter by 64 of the SMs.  One sequence's 8 proposals of 32000 take
+// 22 us, all latency.  A cluster to a sequence; each of its warps has a run of
 // the row in 32 steps at most, whose sums stand in its lanes: the warp that the draw falls
 // to finds the step in them and computes that alone again.
 constexpr int kAcceptThreads = 1024;
