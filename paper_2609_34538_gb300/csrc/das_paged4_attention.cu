@@ -62,6 +62,8 @@ struct Roles {
     // of its own; with 64 each has half of every tile's rows.
     static constexpr bool kTurns = N <= 32;
     // Sets of four warps that widen keys, and of those that widen values: tile k is set k % the sets' number's.
+    // (A second one for values: 4 x 32768 tokens with one row 44.8 us, 46.8 without, a single token 15.2 and 14.7.
+    // With 32 rows or 64 a thread has fewer registers for it than the softmax needs: 56.3 and 75.8 us, 54.1 and 72.1 without.)
     static constexpr int kKeySets = 1, kValueSets = N == 16 ? 2 : 1;
     static constexpr int kKeyWarp0 = kSoftWarps, kValueWarp0 = kKeyWarp0 + 4 * kKeySets;
     static constexpr int kProducerWarp = kValueWarp0 + 4 * kValueSets, kSWarp = kProducerWarp + 1;
@@ -367,7 +369,9 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
                   kThreads = Ro::kThreads;
     constexpr int kStages = Lt::kStages, R = kTurns ? N : N / 2;  // rows of a group
     constexpr int kStep = kTurns ? 2 : 1;                         // from one tile of a group to its next
-    constexpr int kChunk = N == 16 ? 16 : 8;                      // rows whose scores a softmax thread has at once
+    // rows whose scores a softmax thread has at once (with 16 for all 16 ragged sequences take 56.9 us, 52.2 with
+    // 8, and 4 x 32768 with 64 rows 72.1 and 70.1; with 8 for all 4 x 32768 with one row 46.1, 45.1 with 16)
+    constexpr int kChunk = N == 16 ? 16 : 8;
     static_assert(R % kChunk == 0, "rows in chunks");
     extern __shared__ uint8_t smem_raw[];
     uint8_t *const sm = smem_raw + (-smem_u32(smem_raw) & 1023u);
