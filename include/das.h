@@ -320,7 +320,8 @@ typedef struct {
  * for j < rotary_dim / 2, where (a, c) is (j, j + rotary_dim / 2), or (2 j, 2 j + 1) with
  * `interleaved`; the elements from rotary_dim on, and values, are not rotated.
  * Computed in binary32 and rounded once, to bf16; t is reduced exactly (the product n
- * inv_freq is not rounded to 32 bits), so far positions lose nothing.
+ * inv_freq is not rounded to 32 bits), so far positions lose nothing.  A frequency that is not
+ * finite turns nothing.
  *   q, k, v      any strides that are multiples of 4 elements, 8-byte aligned; v (and
  *                v_out) may be NULL
  *   q_weight, k_weight  device [head_dim], fp32 or bf16, or NULL for ones (with eps < 0

@@ -8,7 +8,8 @@
 // ones for top-k, of the whole-number weights for top-p.  The row is not sorted for
 // it; the few candidates of a small top-k are.
 //
-// sample_kernel: a cluster of CTAs holds a row in shared memory, read once.  A
+// sample_kernel: a cluster of CTAs holds a row in shared memory, read once (rows that are
+// recorded for speculative acceptance are read again instead).  A
 // threshold is found from a histogram of kBins bins in shared memory, over
 // the logits (top-k) or the exponents (top-p), summed over the cluster; what
 // falls into the threshold's bin, rarely more than some dozens, is compared
@@ -578,9 +579,7 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
         }
     };
 
-    // ---- a small top-k leaves few candidates: those not below `low`, in index order ----
-    // Four bits of each group of a thread say which; their numbers, in eight bits of
-    // a word per round of groups, are summed over the warp for four rounds at once.
+    // ---- a small top-k leaves few candidates: those not below `low` ----
     int n_cand = 0;
     if constexpr (RECORD) {
         // (as they come: they are sorted by their indexes too, or what is found needs no order)
@@ -630,6 +629,8 @@ __global__ void __launch_bounds__(RECORD ? kRecordThreads : kDrawThreads, RECORD
             sync();
         }
     } else if (k < a.vocab && k <= kCand / 4) {
+        // In index order: four bits of each group of a thread say which; their numbers, in eight bits of
+        // a word per round of groups, are summed over the warp for four rounds at once.
         constexpr int kRounds = kSliceBytes<BF16> / (BF16 ? 2 : 4) / 4 / kThreads;
         static_assert(kRounds * 4 * kThreads * (BF16 ? 2 : 4) == kSliceBytes<BF16> && kRounds * kWarps <= kMaxSegs);
         constexpr int kHits = (kRounds + 7) / 8, kCounts = (kRounds + 3) / 4;
