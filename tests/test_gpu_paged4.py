@@ -141,6 +141,37 @@ def test_append_two_streams_at_once():
     assert same(cache, host(want)) and flag.item() == 0
 
 
+def test_append_captured_with_page_assignment():
+    """Steps of page assignment and commit, captured once and replayed: what they store is what eager steps store."""
+    rng = np.random.default_rng(8)
+    R, L, H, D, W = 2, 1, 3, 64, 10
+    k, v = bf16(rng.normal(0, 1, (R, L, 2, W, H, D))), bf16(rng.normal(0, 1, (R, L, 2, W, H, D)))
+
+    def books():
+        cache = das.PagedKVCache4(*(u8(np.zeros(s, np.uint8)) for s in (
+            (R, L, 8, H, PAGE, D // 2), (R, L, 8, H, 8, D, 4), (R, L, 8, H, PAGE, D // GROUP), (R, L, 8, H, D // GROUP, PAGE))))
+        return cache, dev_i32([0, 0]), dev_i32(list(range(8))), dev_i32([8]), dev_i32([[0] * 4] * 2), dev_i32([0] * 2 * W), dev_i32([0])
+
+    def step(b, grow):
+        cache, length, free, count, table, slots, flag = b
+        start = das.das_page_assign(length, grow, table, free, count, slots, flag, new_len=length, new_free_count=count)[2]
+        das.das_kv_append_paged4(cache, k, v, slots, start, flag)
+
+    a, b, grow = books(), books(), dev_i32([0, 0])
+    step(a, grow)                                           # nothing grows
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(a, grow)
+    for n in ([7, 3], [10, 0], [1, 9], [8, 8]) * 3:
+        grow.copy_(dev_i32(n))
+        graph.replay()
+        step(b, grow)
+    torch.cuda.synchronize()
+    assert same(a[0], host(b[0])) and a[0].k.any() and all(torch.equal(x, y) for x, y in zip(a[1:], b[1:]))
+    assert a[1].tolist() == [78, 60] and a[6].item() == 0
+
+
 def test_append_leaves_what_it_refuses():
     rng = np.random.default_rng(5)
     old, units, x, slots, start = append_case(rng, 1, 1, 2, 64, [60, 0, 0, 0], [8, 4, 4, 4], 8, 8)
