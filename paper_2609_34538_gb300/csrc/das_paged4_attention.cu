@@ -545,7 +545,11 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
             ok = waits(b_qready + 8 * (seg & 1), half_of(seg));
             for (; k < end && ok; ++k) {
                 const int s = k & 1;
-                ok = waits(b_kready + 8 * s, half_of(k)) && (k < 2 || waits(b_sfree + 8 * s, half_of(k) ^ 1));
+                // (where the groups share the tiles, P's buffer is waited for here, with time to spare, and S being
+                // done says that it is free)
+                ok = waits(b_kready + 8 * s, half_of(k)) &&
+                     (k < 2 || (waits(b_sfree + 8 * s, half_of(k) ^ 1) &&
+                                (Ro::kTurns || waits(b_pvdone + 8 * s, half_of(k) ^ 1))));
                 if (!ok) break;
                 fence_after();
                 if (elect_one()) {
@@ -875,7 +879,7 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
                     group_sync();
                     has_ref = first >= 0;
                 }
-                if (k >= 2) waits(b_pvdone + 8 * s, half_of(k) ^ 1);  // P's buffer is free
+                if (kTurns && k >= 2) waits(b_pvdone + 8 * s, half_of(k) ^ 1);  // P's buffer is free
                 const uint32_t dst = sbase + Lt::kPOff + s * Lt::kP + place * 128, turn = (place & 7) << 4;
                 // (all exponentials of a chunk first, so that their chains overlap)
                 auto weights = [&](int c, uint32_t(&a)[kChunk]) {
