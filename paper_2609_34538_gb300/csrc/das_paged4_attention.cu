@@ -94,9 +94,9 @@ struct Layout {
     static constexpr int kPOff = kQOff + 2 * kQ;
     static constexpr int kOnesOff = kPOff + 2 * kP;            // an 8 x 16 operand of ones
     static constexpr int kBarOff = kOnesOff + 256;
-    // full, empty [kStages], qready, qfree [2], kready, vready, sdone, sfree, pready, pvdone [2],
+    // full, empty [kStages], qready, qfree [2], kready, vready, sdone, pready, pvdone [2],
     // drain [2]
-    static constexpr int kBars = 2 * kStages + 4 + 12 + 2;
+    static constexpr int kBars = 2 * kStages + 4 + 10 + 2;
     static constexpr int kInfoOff = (kBarOff + 8 * kBars + 15) / 16 * 16;
     static constexpr int kRowOff = kInfoOff + kInfos * 8;      // floats of the rows: 4 x [2][64], [64]
     static constexpr int kSumOff = kRowOff + 9 * 64 * 4;       // [8 warps][32]: sums or largest
@@ -378,8 +378,8 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
     const uint32_t sbase = smem_u32(sm);
     const uint32_t b_full = sbase + Lt::kBarOff, b_empty = b_full + 8 * kStages,
                    b_qready = b_empty + 8 * kStages, b_qfree = b_qready + 16, b_kready = b_qfree + 16,
-                   b_vready = b_kready + 16, b_sdone = b_vready + 16, b_sfree = b_sdone + 16,
-                   b_pready = b_sfree + 16, b_pvdone = b_pready + 16, b_drain = b_pvdone + 16;
+                   b_vready = b_kready + 16, b_sdone = b_vready + 16,
+                   b_pready = b_sdone + 16, b_pvdone = b_pready + 16, b_drain = b_pvdone + 16;
     int2 *const infos = reinterpret_cast<int2 *>(sm + Lt::kInfoOff);
     volatile uint32_t *const misc = reinterpret_cast<volatile uint32_t *>(sm + Lt::kMiscOff);
     volatile int *const abort_flag = reinterpret_cast<volatile int *>(sm + Lt::kMiscOff + 4);
@@ -404,7 +404,6 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
             mbar_init(b_kready + 8 * i, 4);
             mbar_init(b_vready + 8 * i, 4);
             mbar_init(b_sdone + 8 * i, 1);
-            mbar_init(b_sfree + 8 * i, kTurns ? kGroupWarps : kSoftWarps);
             mbar_init(b_pready + 8 * i, kTurns ? kGroupWarps : kSoftWarps);
             mbar_init(b_pvdone + 8 * i, 1);
             mbar_init(b_drain + 8 * i, 1);
@@ -545,11 +544,10 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
             ok = waits(b_qready + 8 * (seg & 1), half_of(seg));
             for (; k < end && ok; ++k) {
                 const int s = k & 1;
-                // (where the groups share the tiles, P's buffer is waited for here, with time to spare, and S being
-                // done says that it is free)
+                // S is free when P has been made of it.  Where the groups share the tiles, its product is waited for
+                // instead, with time to spare: S being done then says that P's buffer is free.
                 ok = waits(b_kready + 8 * s, half_of(k)) &&
-                     (k < 2 || (waits(b_sfree + 8 * s, half_of(k) ^ 1) &&
-                                (Ro::kTurns || waits(b_pvdone + 8 * s, half_of(k) ^ 1))));
+                     (k < 2 || waits((kTurns ? b_pready : b_pvdone) + 8 * s, half_of(k) ^ 1));
                 if (!ok) break;
                 fence_after();
                 if (elect_one()) {
@@ -851,8 +849,11 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
                 // hidden keys: of pages past the prefix, of the block past it or the row (key i is seen by the
                 // rows from i G on)
                 const bool some_hidden = blk || n.x + n.y < kKeys || !ok;
-                const int from = !ok ? N : blk ? (key < w.T ? key * p.G : N) : key % kPage < (key < kPage ? n.x : n.y) ? 0 : N;
-                const int until = blk ? rows : N;
+                int from = 0, until = N;
+                if (some_hidden) {
+                    from = !ok ? N : blk ? (key < w.T ? key * p.G : N) : key % kPage < (key < kPage ? n.x : n.y) ? 0 : N;
+                    if (blk) until = rows;
+                }
                 const uint32_t s_col = lanes + kSCol + 64 * s + row0;
                 auto scores = [&](int c, uint32_t(&a)[kChunk]) {
                     ld_lanes(s_col + c, a);
@@ -984,10 +985,7 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
                     __syncwarp();
                 }
                 fence_before();
-                if (lane == 0) {
-                    mbar_arrive(b_sfree + 8 * s);
-                    mbar_arrive(b_pready + 8 * s);
-                }
+                if (lane == 0) mbar_arrive(b_pready + 8 * s);
             }
 
             // ---- the end of a segment: O / l and lse, as output or as a partial ----
