@@ -34,11 +34,11 @@
 // memory is freed before the CTA exits.
 //
 // What bounds it: the warps' instructions, not the bytes.  4 x 32768 tokens with 32 query and 8 kv
-// heads of 128 (143 MB, 21 us at the copy rate) take 44.8 us with one row a head, 3.2 TB/s, and 69.8 us
+// heads of 128 (143 MB, 21 us at the copy rate) take 44.3 us with one row a head, 3.2 TB/s, and 67.3 us
 // with 16.  Of the 0.8 us that a tile takes with one row, 0.6 are left without the widening's
-// arithmetic; with 16 the warps that widen values and the softmax groups are both busy throughout,
-// 2200 cycles a tile, of which a thousand are a tile's own waits, barrier and masks; the products
-// take 540.  Scheduled instructions are half of the issue slots' number.  A call of one token
+// arithmetic; with 16 the softmax groups are busy throughout, 2100 cycles a tile, of which almost a thousand
+// are a tile's own waits, barrier and masks; the products take 540.  (Scores loaded a chunk ahead made
+// it 70.7 us, as their registers spill.)  Scheduled instructions are half of the issue slots' number.  A call of one token
 // (15.1 us) spends half of its time before the first tile and after the last.
 #include <algorithm>
 #include <atomic>
@@ -73,8 +73,9 @@ constexpr float kBelow = 60.f;
 // Tensor memory: keys [2], values [2], S [2], O, the sums of P.
 constexpr int kKCol = 0, kVCol = 128, kSCol = 256, kOCol = 384, kSumCol = 448, kCols = 512;
 constexpr int kInfos = 64;  // ring of the tiles' visible keys
-// The end of a pair (its block tile, the read-out and what joins it) weighs kEnd tiles more.  (24 sequences of
-// 500 to 16384 tokens, 4 x 32768 with 64 rows: 51.4 and 69.8 us; with 4 52.3 and 70.3, with 6 50.8 and 70.2.)
+// The end of a pair (its block tile, the read-out and what joins it) weighs kEnd tiles more.  (16 sequences of
+// 1024 to 8192 tokens, 4 x 32768, both with 64 rows, as measured when it was chosen: 51.4 and 69.8 us; with 4
+// 52.3 and 70.3, with 6 50.8 and 70.2.)
 constexpr int kEnd = 5;
 // Weight of a CTA's range, unless it is a pair.  (A pair of 1500 and one of 4000 tokens take 12.6 and 12.1 us,
 // with 10 13.7 and 14.7; with 6 11.0 and 11.4, but 4 pairs of 256 tokens 8.1 us instead of 7.0, as they are split.)
