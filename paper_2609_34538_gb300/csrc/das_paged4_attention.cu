@@ -61,11 +61,11 @@ struct Roles {
     // With few rows the two softmax groups take turns at the tiles, each with a reference, sums and an O
     // of its own; with 64 each has half of every tile's rows.
     static constexpr bool kTurns = N <= 32;
-    // Sets of four warps that widen keys, and of those that widen values: tile k is set k % the sets' number's.
+    // Sets of four warps that widen values: tile k is set k % the sets' number's.  (Keys have one.)
     // (A second one for values: 4 x 32768 tokens with one row 44.8 us, 46.8 without, a single token 15.2 and 14.7.
     // With 32 rows or 64 a thread has fewer registers for it than the softmax needs: 56.3 and 75.8 us, 54.1 and 72.1 without.)
-    static constexpr int kKeySets = 1, kValueSets = N == 16 ? 2 : 1;
-    static constexpr int kKeyWarp0 = kSoftWarps, kValueWarp0 = kKeyWarp0 + 4 * kKeySets;
+    static constexpr int kValueSets = N == 16 ? 2 : 1;
+    static constexpr int kKeyWarp0 = kSoftWarps, kValueWarp0 = kKeyWarp0 + 4;
     static constexpr int kProducerWarp = kValueWarp0 + 4 * kValueSets, kSWarp = kProducerWarp + 1;
     static constexpr int kPvWarp = kSWarp + 1, kThreads = (kPvWarp + 1) * 32;
 };
@@ -365,7 +365,7 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
     using Lt = Layout<D, N>;
     using Ro = Roles<N>;
     constexpr bool kTurns = Ro::kTurns;
-    constexpr int kKeySets = Ro::kKeySets, kValueSets = Ro::kValueSets, kKeyWarp0 = Ro::kKeyWarp0, kValueWarp0 = Ro::kValueWarp0,
+    constexpr int kValueSets = Ro::kValueSets, kKeyWarp0 = Ro::kKeyWarp0, kValueWarp0 = Ro::kValueWarp0,
                   kProducerWarp = Ro::kProducerWarp, kSWarp = Ro::kSWarp, kPvWarp = Ro::kPvWarp,
                   kThreads = Ro::kThreads;
     constexpr int kStages = Lt::kStages, R = kTurns ? N : N / 2;  // rows of a group
@@ -711,39 +711,34 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
     } else if (warp >= kKeyWarp0) {
         // ======================== queries; keys, widened =========================
         // Thread (warp, lane): a key of the tile.
-        const int quad = warp % 4, set = (warp - kKeyWarp0) / 4, key = quad * 32 + lane;
+        const int quad = warp % 4, key = quad * 32 + lane;
         const Widen widen;
         const uint32_t dst = tmem + kKCol + ((uint32_t)(quad * 32) << 16);
         int k = 0, kp = 0;
         bool ok = true;
         for (int seg = 0; k < ntiles && ok; ++seg, walk_pair(p, w)) {
             const Segment sg = segment_of(w, ntiles - k);
-            if (kKeySets == 1 || (seg & 1) == set) {  // the queries
-                if (seg >= 2) ok = waits(b_qfree + 8 * (seg & 1), half_of(seg) ^ 1);
-                if (!ok) break;
-                const uint32_t q = sbase + Lt::kQOff + (seg & 1) * Lt::kQ;
-                constexpr int kPerRow = D / 8;
-                const int rows = p.G * w.T;
+            // the queries
+            if (seg >= 2) ok = waits(b_qfree + 8 * (seg & 1), half_of(seg) ^ 1);
+            if (!ok) break;
+            const uint32_t q = sbase + Lt::kQOff + (seg & 1) * Lt::kQ;
+            constexpr int kPerRow = D / 8;
+            const int rows = p.G * w.T;
 #pragma unroll 4
-                for (int i = key; i < N * kPerRow; i += kKeys) {
-                    const int r = i / kPerRow, c = i % kPerRow;
-                    uint4 x = make_uint4(0, 0, 0, 0);
-                    if (r < rows)
-                        x = *reinterpret_cast<const uint4 *>(
-                            p.q + (((size_t)w.b * p.max_block + r / p.G) * p.Hq + w.h * p.G + r % p.G) * D + c * 8);
-                    x = paired(x);
-                    sts4(q + (c >> 3) * (N * 128) + chunk16(r, c & 7), x.x, x.y, x.z, x.w);
-                }
-                fence_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(b_qready + 8 * (seg & 1));
+            for (int i = key; i < N * kPerRow; i += kKeys) {
+                const int r = i / kPerRow, c = i % kPerRow;
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (r < rows)
+                    x = *reinterpret_cast<const uint4 *>(
+                        p.q + (((size_t)w.b * p.max_block + r / p.G) * p.Hq + w.h * p.G + r % p.G) * D + c * 8);
+                x = paired(x);
+                sts4(q + (c >> 3) * (N * 128) + chunk16(r, c & 7), x.x, x.y, x.z, x.w);
             }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(b_qready + 8 * (seg & 1));
             for (int i = 0; i < sg.n && ok; ++i, ++k) {
                 const int s = k & 1;
-                if (kKeySets == 2 && s != set) {
-                    kp += i < sg.pre;
-                    continue;
-                }
                 if (k >= 2) ok = waits(b_sdone + 8 * s, half_of(k) ^ 1);
                 if (!ok) break;
                 if (i < sg.pre) {

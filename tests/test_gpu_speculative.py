@@ -236,3 +236,23 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for w, runs in zip(want, got):
         assert all(torch.equal(a, b) for r in runs for a, b in zip(w, r))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [50, 9001, 40003])
+def test_nan_and_infinities_among_the_logits(V, dtype):
+    """NaN counts as -inf wherever it stands, whole groups and ends of rows among them, and -0 as 0."""
+    target, drafter, u, again, u0 = make(14 + V, 4, 3, V, dtype)
+    g = torch.Generator(device="cuda").manual_seed(V)
+    for x in (target, drafter):
+        some = torch.rand(x.shape, generator=g, device="cuda")
+        x[some < 0.2], x[some > 0.9] = torch.nan, -torch.inf
+        x[(some > 0.5) & (some < 0.55)] = -0.0
+        x[..., :9], x[..., -7:] = torch.nan, torch.nan
+        x[2, :, 20:40] = torch.nan
+    target[3, :, 12:45:4] = torch.inf
+    for params in ((0.9, 0, 0.9, 0.0), (1.0, 0, 1.0, 0.0), (1.0, 40, 0.95, 0.01)):
+        full = lambda i, dt: torch.full((4,), params[i], dtype=dt, device="cuda")
+        ids, _ = das.das_sample(drafter, u0, full(0, torch.float32), full(1, torch.int32), full(2, torch.float32),
+                                full(3, torch.float32))
+        check(target, drafter, ids, u, again, [params] * 4)
