@@ -1004,8 +1004,9 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
             if (lane < R) sums[lane] = l[0];
             // with turns, a group may have none of the segment's tiles
             const bool had = !kTurns || sg.n > 1 || (k_seg & 1) == group;
+            const int last = k_seg + sg.n - 1;
             if (had) {
-                const int last = k_seg + sg.n - 1, mine = kTurns && (last & 1) != group ? last - 1 : last;
+                const int mine = kTurns && (last & 1) != group ? last - 1 : last;
                 waits(b_pvdone + 8 * (mine & 1), half_of(mine));
                 fence_after();
                 uint32_t o[1];
@@ -1024,8 +1025,16 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
             // from here a group has the rows [orow0, orow0 + kOut) of the output
             constexpr int kOut = N / 2;
             const int orow0 = group * kOut;
-            if (kTurns) all_sync();
-            else group_sync();
+            if (kTurns) {
+                all_sync();
+                // Both groups read both O below: each thread sees the last products of either complete itself, as the
+                // barrier does not order tensor memory.  (After it, as the phase before those has then ended.)
+                waits(b_pvdone + 8 * (last & 1), half_of(last));
+                if (sg.n > 1) waits(b_pvdone + 8 * (last - 1 & 1), half_of(last - 1));
+                fence_after();
+            } else {
+                group_sync();
+            }
             const bool has_blk = sg.n > sg.pre, whole = w.t == 0 && has_blk;
             if (quad == 0 && lane < kOut) {
                 const int r = orow0 + lane;

@@ -494,6 +494,19 @@ def test_attention_two_graphs_that_share_a_workspace():
     assert das.workspace_status(ws) == 0
 
 
+@pytest.mark.parametrize("D,Hq,Hkv,Tm", [(64, 4, 2, 3), (128, 32, 4, 4)])
+def test_attention_segments_of_every_number_of_tiles(D, Hq, Hkv, Tm):
+    """Pairs of one tile to many, which the softmax groups begin in either order and of which one group may have none: both
+    read both groups' sums in the end.  Runs repeat each other bit for bit."""
+    rng = np.random.default_rng(D + Hq)
+    P = [128 * n + int(rng.integers(0, 128)) for n in (0, 1, 2, 3, 4, 5, 0, 1, 0, 9, 2, 30, 0)] + [0, 0, 0]
+    c = attention_case(rng, D, Hq, Hkv, Tm, P, [max(1, Tm - b % 2) for b in range(len(P))])
+    first = run_attention(c)
+    for _ in range(5):
+        again = run_attention(c, repeat=20)
+        assert torch.equal(again[0], first[0]) and torch.equal(again[1], first[1])
+
+
 def test_attention_offsets_past_32_bits():
     """Pages whose codes lie more than 4 GiB into the cache, and commits to them."""
     rng = np.random.default_rng(13)
