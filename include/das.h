@@ -520,8 +520,9 @@ das_status das_kv_append_paged4(const das_kv_cache_paged4 *cache, const void *k_
                                 int max_slots, const int32_t *slot_start, int32_t *error_flag,
                                 void *stream);
 
-/* Workspace bytes for das_mature_v_attention_paged4; a workspace is zeroed before its first
- * use. */
+/* Workspace bytes for das_mature_v_attention_paged4.  A workspace is zeroed before its first
+ * use and keeps counters from call to call: it may serve calls of any shapes that it is large enough
+ * for, one after the other, but no other function's. */
 size_t das_workspace_size_paged4(const das_kv_cache_paged4 *cache, int batch, int num_q_heads,
                                  int max_block);
 

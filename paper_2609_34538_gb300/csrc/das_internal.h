@@ -140,7 +140,7 @@ struct Paged4AttnParams {
     float *lse;
     int32_t *status;
     float *part_o, *part_lse;             // [slots][rows_max][D], [slots][rows_max]
-    int32_t *count_run, *count_pair;      // [slots], [B * Hkv]: 0 between calls
+    int32_t *counts;                      // [3][num_ctas]: 0 between calls
     int B, Hq, Hkv, G, max_block, rows_max, max_pages, pages;
     float scale_log2;
     int num_ctas;

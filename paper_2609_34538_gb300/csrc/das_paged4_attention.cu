@@ -1130,7 +1130,7 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
                 }
                 const int r0 = ((int)blockIdx.x - c0) / run * run, count = min(run, n - r0);
                 __threadfence();  // (for the other threads' stores too, which the barrier puts before)
-                int32_t *const counter = p.count_run + pair + c0 + r0;
+                int32_t *const counter = p.counts + (r0 == 0 ? c0 : p.num_ctas + c0 + r0);
                 if (atomicAdd(counter, 1) == count - 1) {
                     *counter = 0;
                     __threadfence();
@@ -1173,7 +1173,7 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
         __threadfence();
         __syncthreads();
         if (threadIdx.x == 0) {
-            int32_t *const counter = p.count_pair + jn.pair;
+            int32_t *const counter = p.counts + 2 * p.num_ctas + jn.c0;
             const bool last = atomicAdd(counter, 1) == runs - 1;
             if (last) *counter = 0;
             __threadfence();
@@ -1220,14 +1220,20 @@ cudaError_t launch_d(const Paged4AttnParams &p, const CUtensorMap &tm_k, cudaStr
 
 }  // namespace
 
-// header | counters of runs [slots], of pairs [pairs] | part_lse [slots][rows_max] | part_o
-// [slots][rows_max][D], slots = pairs + C (a segment's slot is its pair + its CTA).
+// header | counters [3][C] | part_lse [slots][rows_max] | part_o [slots][rows_max][D], slots = pairs + C (a
+// segment's slot is its pair + its CTA).
+// Counters are 0 between calls, and lie in the same place for every shape, so that no call's partials lie over
+// another's.  They go by CTAs: a pair of several segments has tiles on both sides of the border after its first CTA c0
+// and of that before each other, and no two pairs lie across one border.  So [0][c0] is the run of segments
+// that begins with the pair's first, [1][c] a run that begins with a later CTA c, and [2][c0] the pair's runs.
+constexpr int kCounters = 3;
+
 size_t paged4_workspace_bytes(int device, int batch, int kv_heads, int rows_max, int head_dim) {
     const int C = attn_grid_size(device);
     if (C <= 0) return 0;
-    const size_t pairs = (size_t)batch * kv_heads, slots = pairs + (size_t)C;
-    return kWorkspaceHeader + round256((slots + pairs) * sizeof(int32_t)) +
-           round256(slots * rows_max * sizeof(float)) + round256(slots * rows_max * head_dim * sizeof(float));
+    const size_t slots = (size_t)batch * kv_heads + (size_t)C;
+    return kWorkspaceHeader + round256(kCounters * C * sizeof(int32_t)) + round256(slots * rows_max * sizeof(float)) +
+           round256(slots * rows_max * head_dim * sizeof(float));
 }
 
 cudaError_t paged4_attn_launch(Paged4AttnParams &p, int head_dim, const CUtensorMap &tm_k, void *workspace,
@@ -1237,13 +1243,12 @@ cudaError_t paged4_attn_launch(Paged4AttnParams &p, int head_dim, const CUtensor
     if (e != cudaSuccess) return e;
     p.num_ctas = attn_grid_size(dev);
     if (p.num_ctas <= 0) return cudaErrorInvalidDevice;
-    const size_t pairs = (size_t)p.B * p.Hkv, slots = pairs + (size_t)p.num_ctas;
+    const size_t slots = (size_t)p.B * p.Hkv + (size_t)p.num_ctas;
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     p.status = reinterpret_cast<int32_t *>(ws);
     ws += kWorkspaceHeader;
-    p.count_run = reinterpret_cast<int32_t *>(ws);
-    p.count_pair = p.count_run + slots;
-    ws += round256((slots + pairs) * sizeof(int32_t));
+    p.counts = reinterpret_cast<int32_t *>(ws);
+    ws += round256(kCounters * p.num_ctas * sizeof(int32_t));
     p.part_lse = reinterpret_cast<float *>(ws);
     p.part_o = reinterpret_cast<float *>(ws + round256(slots * p.rows_max * sizeof(float)));
     return head_dim == 128 ? launch_d<128>(p, tm_k, stream) : launch_d<64>(p, tm_k, stream);

@@ -507,6 +507,59 @@ def test_attention_segments_of_every_number_of_tiles(D, Hq, Hkv, Tm):
         assert torch.equal(again[0], first[0]) and torch.equal(again[1], first[1])
 
 
+def test_attention_shapes_that_share_a_workspace():
+    """One workspace of the largest size serves batches, heads, blocks and head sizes in turn: each call joins its segments,
+    whatever the ones before it have left there."""
+    rng = np.random.default_rng(20)
+    shapes = [(128, 32, 8, 16, [rng.integers(1, 3000) for _ in range(16)]), (128, 8, 8, 1, [9000]), (64, 4, 2, 7, [4000, 0, 777]),
+              (128, 64, 1, 1, [20000]), (64, 1, 1, 64, [64 * 150, 1])]
+    cases, calls, size = [], [], 0
+    for D, Hq, Hkv, Tm, P in shapes:
+        c = attention_case(rng, D, Hq, Hkv, Tm, P, [max(1, Tm - b % 3) for b in range(len(P))], poison=False)
+        cache = cache_of(c)
+        size = max(size, das.new_workspace_paged4(cache, len(P), Hq, Tm).numel())
+        cases.append((c, cache, [dev_i32(c[n]) for n in ("table", "P", "T")] + [bf16(c[n]) for n in ("q", "kb", "vb")]))
+    ws = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    for i in (0, 1, 0, 2, 0, 3, 1, 4, 2, 0, 4, 3, 0):
+        c, cache, args = cases[i]
+        B, Tm, Hq, D = c["q"].shape
+        out = torch.full((B, Tm, Hq, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+        lse = torch.full((B, Hq, Tm), float("nan"), device="cuda")
+        das.das_mature_v_attention_paged4(cache, 0, 1, 2, *args, ws, out=out, lse=lse)
+        calls.append((i, out, lse))
+    wants = [reference(c, *(f64(x) for x in args[3:]), c["P"], c["T"]) for c, _, args in cases]
+    for at, (i, out, lse) in enumerate(calls):
+        o, l, dev = wants[i]
+        assert_close(f64(out), o, lse.cpu().numpy(), l, dev, where=f"call {at}, shape {i}")
+    assert das.workspace_status(ws) == 0
+
+
+def test_attention_graphs_of_two_batches_that_share_a_workspace():
+    """A server's captured steps, one for each batch size, over one workspace."""
+    rng = np.random.default_rng(21)
+    c = attention_case(rng, 128, 8, 2, 4, [3000, 700, 1500, 64, 5000, 900], [4, 3, 4, 4, 1, 2], poison=False)
+    cache = cache_of(c)
+    ws = das.new_workspace_paged4(cache, 6, 8, 4)
+    host_args = [c[n] for n in ("table", "P", "T", "q", "kb", "vb")]
+    graphs, outs = {}, {}
+    for B in (6, 1, 4):
+        a = [dev_i32(x[:B]) for x in host_args[:3]] + [bf16(x[:B]) for x in host_args[3:]]
+        das.das_mature_v_attention_paged4(cache, 0, 1, 2, *a, ws)
+        torch.cuda.synchronize()
+        graphs[B] = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graphs[B]):
+            outs[B] = das.das_mature_v_attention_paged4(cache, 0, 1, 2, *a, ws) + (a,)
+    o, l, dev = reference(c, *(f64(x) for x in outs[6][2][3:]), c["P"], c["T"])
+    for B in (6, 1, 6, 4, 6, 6, 1, 4, 6):
+        out, lse, _ = outs[B]
+        out.fill_(float("nan"))
+        lse.fill_(float("nan"))
+        graphs[B].replay()
+        torch.cuda.synchronize()
+        assert_close(f64(out), o[:B], lse.cpu().numpy(), l[:B], dev[:B], where=f"batch of {B}")
+    assert das.workspace_status(ws) == 0
+
+
 def test_attention_offsets_past_32_bits():
     """Pages whose codes lie more than 4 GiB into the cache, and commits to them."""
     rng = np.random.default_rng(13)
