@@ -1558,7 +1558,7 @@ struct RowProbs {
         const float l = logit(v);
         if (!kept(l, v)) return 0.f;
         const float e = floored(e_of(key_of(l), r.top, m, r.T));
-        return e > 0.f ? e * r.inv : 0.f;
+        return e > 0.f ? __fmul_rn(e, r.inv) : 0.f;
     }
     // e; where all T are `quick` the quotient by Markstein's steps as in sample_kernel, which differ
     // from the division below e^-100 alone, where no weight is left
@@ -1624,8 +1624,10 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) speculative_accept_kernel(c
     // are slow
     auto weight = [&](auto quick, long long v, float lp, float lq) -> uint2 {  // (past the row lp is -inf)
         if (!p.kept(lp, (int)v)) return make_uint2(0, 0);
+        // (products and difference each rounded, never fused: equal probabilities leave 0)
         const float e = p.template e<quick.value>(lp);
-        float x = e * p.r.inv - (q.kept(lq, (int)v) ? q.template e<quick.value>(lq) * q.r.inv : 0.f);
+        const float taken = q.kept(lq, (int)v) ? __fmul_rn(q.template e<quick.value>(lq), q.r.inv) : 0.f;
+        float x = __fsub_rn(__fmul_rn(e, p.r.inv), taken);
         x = (plain ? e * 0x1p-8f : fmaxf(x, 0.f)) * 0x1p20f;
         const uint32_t up = __float2uint_rz(x);
         return make_uint2(up, __float2uint_rn((x - (float)up) * 0x1p20f));
@@ -1707,7 +1709,11 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) speculative_accept_kernel(c
     before = __shfl_sync(kFull, x - step_sum, step);
     for (int i = step << log_step; i < (step + 1) << log_step; ++i) {
         const long long v = lo + i * 32 + lane;
-        const u64 w = v < V ? sum_of(weight(std::false_type(), v, p.logit((int)v), q.logit((int)v))) : 0;
+        u64 w = 0;  // (as in the sweep, to the last bit)
+        if (v < V) {
+            const float lp = p.logit((int)v), lq = q.logit((int)v);
+            w = sum_of(quick ? weight(std::true_type(), v, lp, lq) : weight(std::false_type(), v, lp, lq));
+        }
         x = scan(w);
         if (r >= x - w && r < x) a.next_token[b] = (int)v;
         before = __shfl_sync(kFull, x, 31);

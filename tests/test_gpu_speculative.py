@@ -256,3 +256,50 @@ def test_nan_and_infinities_among_the_logits(V, dtype):
         ids, _ = das.das_sample(drafter, u0, full(0, torch.float32), full(1, torch.int32), full(2, torch.float32),
                                 full(3, torch.float32))
         check(target, drafter, ids, u, again, [params] * 4)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [40, 3001, 40003, 128257])
+def test_refused_between_equal_rows(V, dtype):
+    """A proposal that is no token, where drafter and target are the same: nothing is left of the target beside the drafter's,
+    to the last bit, and the draw is das_sample's from the target's row."""
+    B, W = 6, 2
+    target, _, u, again, _ = make(20 + V, B, W, V, dtype)
+    target[3] = target[3].round()                             # many equal logits
+    target[4, :, ::3], target[4, :, 5] = torch.nan, -torch.inf
+    target[5, :, 7:9] = torch.inf
+    ids = torch.full((B, W), -1, dtype=torch.int32, device="cuda")
+    for params in ((1.0, 0, 1.0, 0.0), (0.7, 0, 1.0, 0.0), (1.3, 0, 0.9, 0.0), (0.9, 30, 0.95, 0.01), (1.0, 1200, 1.0, 0.0),
+                   (0.0, 0, 1.0, 0.0)):
+        check(target, target.clone(), ids, u, again, [params] * B)
+        full = lambda i, dt: torch.full((B,), params[i], dtype=dt, device="cuda")
+        sampling = full(0, torch.float32), full(1, torch.int32), full(2, torch.float32), full(3, torch.float32)
+        drawn, _ = das.das_sample(target[:, :1], again[:, None], *sampling)
+        accepted, nxt, _ = das.das_speculative_accept(target, target, ids, u, again, *sampling)
+        assert not accepted.any() and torch.equal(nxt, drawn[:, 0])
+
+
+def test_refused_between_equal_longest_rows():
+    target, _, u, again, _ = make(21, 2, 1, 400009, torch.float32)
+    ids = torch.full((2, 1), -1, dtype=torch.int32, device="cuda")
+    check(target, target, ids, u, again, [(1.0, 0, 1.0, 0.0), (0.8, 500, 0.95, 0.0)])
+
+
+@pytest.mark.parametrize("V", [40, 40003])
+def test_refused_at_rows_without_logits_and_with_infinities(V):
+    """Refusals that are certain (no token's number is -1), of every kind of row, alone in a CTA and over a cluster."""
+    target, drafter, u, again, _ = make(22, 6, 2, V, torch.float32)
+    drafter[0, 0] = torch.nan                                 # the drafter had nothing
+    target[1, 0, 3] = target[1, 0, V - 1] = torch.inf         # both with half of the weight
+    drafter[2, 0, 5] = torch.inf
+    target[3, 0, :V // 2] = torch.nan
+    drafter[4, 0, V // 3:] = -torch.inf
+    target[5, 0, 1:] = -torch.inf                             # one token alone
+    ids = torch.full((6, 2), -1, dtype=torch.int32, device="cuda")
+    for params in ((1.0, 0, 1.0, 0.0), (0.8, 12, 0.9, 0.02)):
+        accepted, nxt, _ = check(target, drafter, ids, u, again, [params] * 6)
+        assert not accepted.any() and nxt[1].item() in (3, V - 1) and nxt[3] >= V // 2 and nxt[5] == 0
+    target[0, 0] = -torch.inf                                 # nothing to draw from, and from neither
+    target[1, 0], drafter[1, 0] = torch.nan, torch.nan
+    accepted, nxt, committed = das.das_speculative_accept(target, drafter, ids, u, again)
+    assert nxt[:2].tolist() == [-1, -1] and accepted[:2].tolist() == [0, 0] and committed[:2].tolist() == [1, 1]
