@@ -90,18 +90,22 @@ __global__ void __launch_bounds__(kWarps * 32, 8) rope_kernel(const RopeParams p
     const int rd8 = a.rotary_dim / 8;
     const bool turned = l < rd8;
     const int u0 = PAIRS ? 2 * l : turned ? l : 2 * l, u1 = PAIRS || !turned ? 2 * l + 1 : l + rd8;
+    // (cs 2: of a pair that nothing turns, which passes as it is, as 0 times an infinity beside it would be NaN)
     float cs[4], sn[4];
     {
         const unsigned long long n = (a.prefix_len ? max(a.prefix_len[b], 0) : 0) + (long long)i;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            cs[j] = 1.f;
+            cs[j] = 2.f;
             sn[j] = 0.f;
             if (!turned) continue;
-            const float x = (float)(int)(n * turns(a.inv_freq[4 * l + j]) >> 32) * 4.656612873077393e-10f;  // half turns, 2^-31
+            const float f = a.inv_freq[4 * l + j];
+            const float x = (float)(int)(n * turns(f) >> 32) * 4.656612873077393e-10f;  // half turns, 2^-31
             sincospif(x, &sn[j], &cs[j]);
+            if (!(fabsf(f) < INFINITY)) cs[j] = 2.f;
         }
     }
+    const bool some_still = __any_sync(kFull, cs[0] > 1.5f || cs[1] > 1.5f || cs[2] > 1.5f || cs[3] > 1.5f);
     // the heads of a kind that are this warp's
     int kind_begin = 0;
 #pragma unroll 1
@@ -157,6 +161,13 @@ __global__ void __launch_bounds__(kWarps * 32, 8) rope_kernel(const RopeParams p
                         z[j] = zs;
                         z[j + 4] = zt;
                     }
+                    if (some_still)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (cs[j] > 1.5f) {
+                                z[j] = PAIRS ? y[2 * j] : y[j];
+                                z[j + 4] = PAIRS ? y[2 * j + 1] : y[j + 4];
+                            }
                     if (PAIRS) {
                         x0[k] = make_uint2(pack(z[0], z[4]), pack(z[1], z[5]));
                         x1[k] = make_uint2(pack(z[2], z[6]), pack(z[3], z[7]));

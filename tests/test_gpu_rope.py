@@ -151,3 +151,42 @@ def test_frequencies_of_any_size():
     want = f64(q)[:, 1, :, 5] * np.cos(2 * np.pi * turn) - f64(q)[:, 1, :, 69] * np.sin(2 * np.pi * turn)
     size = np.abs(f64(q)[:, 1, :, 5]) + np.abs(f64(q)[:, 1, :, 69])
     assert (np.abs(f64(got)[:, 1, :, 5] - want) <= half_ulp_bf16(size) + 1e-3 * size).all()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("D,rd", [(64, 0), (64, 32), (128, 8), (128, 64), (128, 120)])
+def test_infinities_beside_what_is_not_rotated(D, rd, interleaved):
+    """Elements from rotary_dim on are not rotated: without a norm they pass as they are, whatever stands beside them; with one
+    an infinity makes its row's finite elements 0 and itself NaN."""
+    q, k, _, w, freq = make(30 + rd, 2, 3, 2, 1, D, rd)
+    q, k = q.clone(), k.clone()
+    tail = list(range(rd, D))
+    q[0, 1, 0, tail[1]], q[0, 2, 1, tail[2]], q[1, 0, 0, tail[4]] = torch.inf, torch.nan, -torch.inf
+    k[1, 1, 0, tail[-1]], k[1, 2, 0, tail[0]] = -torch.inf, torch.inf
+    P = dev_i32([3, 70])
+    qo, ko, _ = das.das_qk_norm_rope(q, k, None, freq, P, eps=None, interleaved=interleaved)
+    for got, x in ((qo, q), (ko, k)):
+        a, b = f64(got)[..., rd:], f64(x)[..., rd:]
+        assert np.array_equal(a, b, equal_nan=True) and np.isfinite(f64(got)[..., :rd]).all()
+    place = np.array([3, 70])[:, None] + np.arange(3)
+    qo, ko, _ = das.das_qk_norm_rope(q, k, None, freq, P, q_weight=w[0], k_weight=w[1], interleaved=interleaved)
+    for got, x, weight in ((qo, q, w[0]), (ko, k, w[1])):
+        with np.errstate(invalid="ignore"):
+            want, _ = ref.norm_rope(f64(x), f64(weight), 1e-6, ref.angles(place, freq.cpu().numpy()), interleaved)
+        got, bad = f64(got), np.isinf(f64(x)).any(-1)
+        assert bad.sum() == np.isinf(f64(x)).sum() > 0        # one to a row
+        assert np.array_equal(got[bad], want[bad], equal_nan=True) and not np.nan_to_num(got[bad]).any()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_frequencies_that_are_not_finite_leave_infinities_alone(interleaved):
+    q, k, _, _, freq = make(31, 1, 5, 2, 1, 64, 48)
+    q = q.clone()
+    freq[2], freq[7], freq[23] = torch.inf, torch.nan, -torch.inf
+    pair = lambda j: (2 * j, 2 * j + 1) if interleaved else (j, j + 24)
+    q[0, 1, 0, pair(2)[0]], q[0, 2, 1, pair(7)[1]], q[0, 3, 0, pair(23)[1]] = torch.inf, -torch.inf, torch.nan
+    qo, _, _ = das.das_qk_norm_rope(q, k, None, freq, dev_i32([9]), eps=None, interleaved=interleaved)
+    still = [e for j in (2, 7, 23) for e in pair(j)] + list(range(48, 64))
+    assert np.array_equal(f64(qo)[..., still], f64(q)[..., still], equal_nan=True)
+    rest = [e for e in range(48) if e not in still]
+    assert qo[..., rest].isfinite().all()
