@@ -324,8 +324,8 @@ typedef struct {
  * finite turns nothing.
  *   q, k, v      any strides that are multiples of 4 elements, 8-byte aligned; v (and
  *                v_out) may be NULL
- *   q_weight, k_weight  device [head_dim], fp32 or bf16, or NULL for ones (with eps < 0
- *                they are not read)
+ *   q_weight, k_weight  device [head_dim], fp32 (16-byte aligned) or bf16 (8-byte
+ *                aligned), or NULL for ones (with eps < 0 they are not read)
  *   inv_freq     device fp32 [rotary_dim / 2] (NULL with rotary_dim 0); rotary_dim a
  *                multiple of 8 from 0 to head_dim
  *   prefix_len   device int32 [batch], or NULL for zeros; negative counts as 0

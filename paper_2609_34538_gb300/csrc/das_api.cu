@@ -663,6 +663,7 @@ das_status das_qk_norm_rope(const das_head_rows *q, const das_head_rows *k, cons
         (weight_type != DAS_WEIGHTS_F32 && weight_type != DAS_WEIGHTS_BF16))
         return DAS_ERR_INVALID_ARG;
     if (head_dim != 64 && head_dim != 128) return DAS_ERR_UNSUPPORTED;
+    if (eps < 0.f) q_weight = k_weight = nullptr;
     const uintptr_t wide = weight_type == DAS_WEIGHTS_BF16 ? 8 : 16;
     if (reinterpret_cast<uintptr_t>(q_weight) % wide || reinterpret_cast<uintptr_t>(k_weight) % wide)
         return DAS_ERR_INVALID_ARG;

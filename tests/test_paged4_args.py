@@ -197,3 +197,14 @@ def test_a_cache_has_matching_tensors_on_one_gpu(fake):
         dt = f32 if name == "k_unit" else u8
         with pytest.raises(ValueError, match="pages must have 64" if name == "k" else name):
             das.PagedKVCache4(**{n: fake(dt, *shape) if n == name else fake(*s) for n, s in shapes.items()})
+
+
+def test_weights_that_are_not_read_are_not_looked_at():
+    """Without a norm the weights are not read, so their addresses do not matter either; with one they have to be aligned."""
+    r = ctypes.byref(das.das_head_rows(0, 0, 0, 0))
+    call = lambda qw, kw, wt, eps: L.das_qk_norm_rope(r, r, None, 0, 3, 4, 2, 64, ctypes.c_void_p(qw), ctypes.c_void_p(kw), wt,
+                                                      eps, A, 64, 0, NULL, NULL, NULL, NULL, NULL, NULL)
+    for qw, kw in ((1, 256), (256, 1), (1, 1)):
+        for wt in (0, 1):
+            assert call(qw, kw, wt, -1.0) == OK
+            assert call(qw, kw, wt, 0.0) == BAD
