@@ -119,7 +119,8 @@ __device__ __forceinline__ int block_of(const Paged4AttnParams &p, int b) {
     return clamp_to(__ldcg(p.block_len + b), p.max_block);
 }
 // a sequence without rows has nothing but its outputs to clear
-__device__ __forceinline__ int tiles_of(int P, int T) { return T > 0 ? (P + kKeys - 1) / kKeys + 1 : 1; }
+// (P may be 2^31 - 64)
+__device__ __forceinline__ int tiles_of(int P, int T) { return T > 0 ? (int)((P + (unsigned)kKeys - 1) / kKeys) + 1 : 1; }
 
 struct Walk {
     int b, h, t, nt, P, T;

@@ -584,3 +584,22 @@ def test_attention_offsets_past_32_bits():
     out, lse = das.das_mature_v_attention_paged4(cache, 0, 1, 1, dev_i32([ids]), dev_i32([P]), dev_i32([4]), q, kb, vb, ws)
     o, l, dev = ref.attention(K, V, np.array([[0, 1, 2, 3]]), [P], [4], f64(q), f64(kb), f64(vb))
     assert_close(f64(out), o, lse.cpu().numpy(), l, dev, where="far pages")
+
+
+def test_attention_over_the_longest_table():
+    """Prefixes of up to 2^31 - 64 tokens, all on one page: keys are 0 and values 1, so that weights are equal powers of two whose
+    sums are exact (a segment has fewer than 2^24 keys), outputs 1 and the lse the logarithm of the number of keys seen."""
+    D, rows = 64, (1 << 25) - 1
+    z = lambda *s: np.zeros((1, 1, 1, 1) + s, np.uint8)
+    one = 8 * 15                                            # the scale byte of 1
+    cache = das.PagedKVCache4(u8(z(PAGE, D // 2) + 0x88), u8(z(8, D, 4) + 0x99), u8(z(PAGE, D // GROUP) + one),
+                              u8(z(D // GROUP, PAGE) + one))
+    ws = das.new_workspace_paged4(cache, 1, 2, 2)
+    table = torch.zeros((1, rows), dtype=torch.int32, device="cuda")
+    q = bf16(np.random.default_rng(22).normal(0, 1, (1, 2, 2, D)))
+    kb, vb = bf16(np.zeros((1, 2, 1, D))), bf16(np.ones((1, 2, 1, D)))
+    for P in (rows * PAGE, rows * PAGE - 64, 2 ** 31 - 127, 2 ** 31 - 300, 1 << 30):
+        out, lse = das.das_mature_v_attention_paged4(cache, 0, 1, 1, table, dev_i32([P]), dev_i32([2]), q, kb, vb, ws)
+        want = np.log(P + np.array([1.0, 2.0]))
+        assert (out == 1).all() and np.abs(lse[0].cpu().numpy() - want).max() <= LSE_ABS, P
+    assert das.workspace_status(ws) == 0
