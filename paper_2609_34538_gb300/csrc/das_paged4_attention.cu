@@ -69,7 +69,7 @@ struct Roles {
     static constexpr int kProducerWarp = kValueWarp0 + 4 * kValueSets, kSWarp = kProducerWarp + 1;
     static constexpr int kPvWarp = kSWarp + 1, kThreads = (kPvWarp + 1) * 32;
 };
-constexpr float kBelow = 60.f;
+constexpr float kBelow = 60.f, kMost = 1e38f;
 // Tensor memory: keys [2], values [2], S [2], O, the sums of P.
 constexpr int kKCol = 0, kVCol = 128, kSCol = 256, kOCol = 384, kSumCol = 448, kCols = 512;
 constexpr int kInfos = 64;  // ring of the tiles' visible keys
@@ -871,7 +871,8 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
 #pragma unroll
                             for (int j = 0; j < kChunk; ++j) {
                                 const float m = __uint_as_float(a[j]) * sc;
-                                off[row0 + c + j] = (fabsf(m) < INFINITY ? -m : 0.f) - kBelow;
+                                // (of one of -inf, below all others, so that the reference moves)
+                                off[row0 + c + j] = fmaxf(fminf(-m, kMost), -kMost) - kBelow;
                             }
                     }
                     group_sync();

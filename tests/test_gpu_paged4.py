@@ -603,3 +603,41 @@ def test_attention_over_the_longest_table():
         want = np.log(P + np.array([1.0, 2.0]))
         assert (out == 1).all() and np.abs(lse[0].cpu().numpy() - want).max() <= LSE_ABS, P
     assert das.workspace_status(ws) == 0
+
+
+def test_attention_first_key_without_weight():
+    """A key with a score of -inf at the head of a block, or of what a group of warps has of a prefix, while all others lie far
+    below 0: the others are the row's weights.  Scores are of up to 2^9 binary orders, whose sum, product and difference are off
+    by 3 * 2^-13 orders together (as in assert_close), and the lse is their size: 2^-11 more than for small ones."""
+    rng = np.random.default_rng(23)
+
+    def check(c, rows, where):
+        B, Tm, Hq, _ = c["q"].shape
+        cache = cache_of(c)
+        ws = das.new_workspace_paged4(cache, B, Hq, Tm)
+        out, lse = das.das_mature_v_attention_paged4(cache, 0, 1, 2, dev_i32(c["table"]), dev_i32(c["P"]), dev_i32(c["T"]),
+                                                     bf16(c["q"]), bf16(c["kb"]), bf16(c["vb"]), ws, softmax_scale=1.0)
+        with np.errstate(invalid="ignore"):
+            o, l, dev = reference(c, *(f64(bf16(c[n])) for n in ("q", "kb", "vb")), c["P"], c["T"], scale=1.0)
+        o, l, dev, out, lse = o[:, rows], l[..., rows], dev[:, rows], f64(out)[:, rows], lse.cpu().numpy()[..., rows]
+        assert_close(out, o, l, l, dev, where=where)
+        inf = np.isneginf(l)
+        assert np.array_equal(np.isneginf(lse), inf) and np.abs(lse[~inf] - l[~inf]).max() <= LSE_ABS + 2.0 ** -11, where
+        assert das.workspace_status(ws) == 0
+
+    for D, Hq, Tm, T in ((64, 2, 5, 5), (128, 8, 8, 7)):
+        c = attention_case(rng, D, Hq, 1, Tm, [0, 0], [T, T - 1], poison=False)
+        c["q"][..., 0], c["q"][..., 1] = 1.0, 20.0
+        c["kb"][..., 0], c["kb"][..., 1] = 0.0, -16.0          # scores about -320
+        c["kb"][:, 0, 0, 0] = -np.inf
+        check(c, slice(1, None), "block")                       # (the first row sees that key alone)
+    for Hq, Tm in ((1, 1), (8, 8)):
+        c = attention_case(rng, 64, Hq, 1, Tm, [900, 129], [Tm, Tm], poison=False)
+        c["q"][..., 0], c["q"][..., 1] = -2.0 ** 126, 1.0
+        c["kb"][..., 0], c["kb"][..., 1] = 0.0, -300.0
+        c["ku"], c["ks"][..., 0], c["k"][..., :16] = np.ones(1), 0xa7, 0x88   # elements 0 to 31: scale 60, but for two 0
+        c["k"][..., 0] = 3 << 4 | 8                             # elements 0 and 1: 0 and -5 steps, -300
+        for b in range(2):
+            for t in range(0, int(c["P"][b]), 128):             # the first key of every tile: 7 steps times -2^126
+                c["k"][c["table"][b, t // PAGE], 0, t % PAGE, 0] = 3 << 4 | 15
+        check(c, slice(None), "prefix")
