@@ -534,7 +534,9 @@ size_t das_workspace_size_paged4(const das_kv_cache_paged4 *cache, int batch, in
  * here, and the value scales, which need no limits.  All products run in bf16, which
  * queries and stored keys and values are; a weight is rounded to it, off by 2^-8 of itself at most, or
  * by 2^-65 of the row's sum.  Sums and outputs before their rounding are in fp32.  A
- * value of the block's own that is not finite makes that element of the rows that see it NaN.
+ * value of the block's own that is not finite makes that element of the rows that see it NaN; one
+ * of 2^128 of its head's v_units or more in size counts as that many at most, or as infinite, to
+ * those rows alone (a commit would cut it at 420 units), and one below 2^-126 units as 0.
  */
 das_status das_mature_v_attention_paged4(const das_kv_cache_paged4 *cache, int layer, int key_depth,
                                          int value_depth, const int32_t *block_table, int max_pages,

@@ -670,7 +670,7 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
                     __syncwarp();
                     if (lane == 0) mbar_arrive(b_empty + 8 * st);
                     ++kp;
-                } else {  // the block's own, in units of the stored ones'
+                } else {  // the block's own, in units of the stored ones' (exact, but for what is past bf16's range)
                     if (k >= 2) ok = waits(b_pvdone + 8 * s, half_of(k) ^ 1);
                     if (!ok) break;
                     fence_after();
@@ -696,7 +696,7 @@ __global__ void __launch_bounds__(Roles<N>::kThreads, 1)
                                         x[j] = 0.f;
                                     }
 #pragma unroll
-                                for (int j = 0; j < 4; ++j) r[4 * o + j] = pack_bf16(x[j] * unit, x[j + 4] * unit);
+                                for (int j = 0; j < 4; ++j) r[4 * o + j] = pack_bf16_finite(x[j] * unit, x[j + 4] * unit);
                             }
                             st_lanes(dst + 64 * s + 8 * c, r);
                         }

@@ -641,3 +641,31 @@ def test_attention_first_key_without_weight():
             for t in range(0, int(c["P"][b]), 128):             # the first key of every tile: 7 steps times -2^126
                 c["k"][c["table"][b, t // PAGE], 0, t % PAGE, 0] = 3 << 4 | 15
         check(c, slice(None), "prefix")
+
+
+def test_attention_block_values_past_the_units():
+    """A value of the block's own whose quotient by a small unit is past bf16 counts as the most units that there are, or as
+    infinite, to the rows that see it, one that is not finite as NaN, and either as nothing to the rows that do not."""
+    rng = np.random.default_rng(24)
+    for D, Hq, Tm, T, big in ((64, 2, 6, 6, 2.0 ** 100), (128, 8, 8, 7, -2.0 ** 89), (64, 1, 4, 4, np.inf)):
+        c = attention_case(rng, D, Hq, 1, Tm, [140, 0], [T, T], poison=False)
+        c["vu"] = np.array([2.0 ** -40])
+        c["vb"] = c["vb"] * 2.0 ** -40
+        clean = c["vb"].copy()
+        c["vb"][:, 2, 0, 5] = big
+        cache = cache_of(c)
+        ws = das.new_workspace_paged4(cache, 2, Hq, Tm)
+        out, lse = das.das_mature_v_attention_paged4(cache, 0, 1, 2, dev_i32(c["table"]), dev_i32(c["P"]), dev_i32(c["T"]),
+                                                     bf16(c["q"]), bf16(c["kb"]), bf16(c["vb"]), ws)
+        o, l, dev = reference(c, *(f64(bf16(x)) for x in (c["q"], c["kb"], clean)), c["P"], c["T"])
+        out, bad = f64(out), np.zeros(o.shape, bool)
+        bad[:, 2:T, :, 5] = True
+        if np.isinf(big):
+            assert np.isnan(out[bad]).all()
+        else:                                               # (weights of the 150 keys are some thousandths or more)
+            assert (out[bad] * np.sign(big) > 2.0 ** 70).all()
+        # (values are of the size of 2^-40: what is lost of them is as much less)
+        err = np.abs(np.where(bad, 0.0, out - o))
+        off = (2.0 ** -8 + 2.0 ** -11) * (1 + 2.0 ** -6) * dev
+        assert (err <= off + half_ulp_bf16(np.abs(o) + off) + 2.0 ** -85).all()
+        assert np.abs(lse.cpu().numpy()[:, :, :T] - l[:, :, :T]).max() <= LSE_ABS
