@@ -319,9 +319,10 @@ typedef struct {
  *   (y_a, y_c) -> (y_a cos t - y_c sin t, y_c cos t + y_a sin t),  t = n inv_freq[j],
  * for j < rotary_dim / 2, where (a, c) is (j, j + rotary_dim / 2), or (2 j, 2 j + 1) with
  * `interleaved`; the elements from rotary_dim on, and values, are not rotated.
- * Computed in binary32 and rounded once, to bf16; t is reduced exactly (the product n
- * inv_freq is not rounded to 32 bits), so far positions lose nothing.  A frequency that is not
- * finite turns nothing.
+ * Computed in binary32 and rounded once, to bf16; t is reduced modulo 2 pi in whole numbers,
+ * off by n (|inv_freq[j]| 2^-66 + 2^-64) turns at most before it is rounded to binary32: less than
+ * 2^-32 turns at every position with a frequency of up to 1.  A pair whose frequency is not finite
+ * is not rotated.
  *   q, k, v      any strides that are multiples of 4 elements, 8-byte aligned; v (and
  *                v_out) may be NULL
  *   q_weight, k_weight  device [head_dim], fp32 (16-byte aligned) or bf16 (8-byte

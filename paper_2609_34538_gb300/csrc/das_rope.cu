@@ -5,8 +5,9 @@
 // lane 8 of its elements: the two elements of every rotated pair are the same lane's, so
 // rows need no exchange but the sum of squares, and any output may overwrite its
 // input.  The angle n f_j is taken in turns as a 64-bit fraction: n times f_j / (2 pi)
-// modulo 1 is an integer product whose overflow is what is not wanted.  The lane's
-// four angles serve all of the token's heads.
+// modulo 1 is an integer product whose overflow is what is not wanted.  (f_j / (2 pi) is
+// cut to 2^-64, 1 / (2 pi) to 2^-66, so n f_j is off by n (f_j 2^-66 + 2^-64) turns at most.)
+// The lane's four angles serve all of the token's heads.
 //
 // Bound by memory, reads and writes of 2 bytes an element each.  4 x 2001 tokens of prompts of 500
 // to 2001, 48 heads of 128, take 24.9 us, 70% of the measured copy rate; in a loop on the same rows 23.8,

@@ -286,14 +286,6 @@ __device__ __forceinline__ void ld_lanes(uint32_t a, uint32_t (&r)[16]) {
         : "r"(a)
         : "memory");
 }
-__device__ __forceinline__ void ld_lanes(uint32_t a, uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
-        "%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : DAS_R8(r, 0), DAS_R8(r, 8), DAS_R8(r, 16), DAS_R8(r, 24)
-        : "r"(a)
-        : "memory");
-}
 __device__ __forceinline__ void st_lanes(uint32_t a, const uint32_t (&r)[8]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(a),
                  DAS_I8(r, 0)
@@ -306,7 +298,6 @@ __device__ __forceinline__ void st_lanes(uint32_t a, const uint32_t (&r)[16]) {
         DAS_I8(r, 0), DAS_I8(r, 8)
         : "memory");
 }
-__device__ __forceinline__ void st_lanes(uint32_t a, const uint32_t (&r)[32]) { st_lanes32(a, r); }
 #undef DAS_I8
 #undef DAS_R8
 
