@@ -709,7 +709,8 @@ def das_kv_append_paged4(cache, k_new, v_new, slots, slot_start, error_flag, str
 
 
 def new_workspace_paged4(cache, batch, num_q_heads, max_block, device=None):
-    """Zeroed workspace for das_mature_v_attention_paged4."""
+    """Zeroed workspace for das_mature_v_attention_paged4 alone: calls of other shapes may share it one after the
+    other if it is large enough for them, other functions may not."""
     n = int(LIB.das_workspace_size_paged4(ctypes.byref(cache.desc), batch, num_q_heads, max_block))
     if n == 0:
         raise DasError(DAS_ERR_UNSUPPORTED, "das_workspace_size_paged4")

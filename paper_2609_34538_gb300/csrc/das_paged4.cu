@@ -18,7 +18,7 @@
 //
 // Bound by memory for long appends: 4 sequences of 501 to 1001 tokens at 8 depths and 4 layers,
 // 8 heads of 128, take 96.8 us, 5.5 TB/s (81% of the copy rate); 8 of 8 to 16 tokens at 32 depths
-// 23.5 us, instructions of passes of eight tokens that are partly there and the chain of
+// 23.6 us, instructions of passes of eight tokens that are partly there and the chain of
 // look-ups before them.  64 registers and 32 warps to an SM are the best of both: with 80
 // the long one takes 102 us.  Loads of the next pass ahead of this one's work made that 95 us, but the
 // short one 25; several pieces of work to a warp in turn 98 and 23.

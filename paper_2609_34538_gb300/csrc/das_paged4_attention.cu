@@ -15,7 +15,9 @@
 // row's reference set again, to the tile's largest, and O and l are rescaled.  The output
 // is divided by the sum of the rounded weights, taken by the tensor core with a row of
 // ones, and is so a mean of the values with the very weights in use; the lse is from the
-// unrounded ones.
+// unrounded ones.  Weights are rounded to bf16 as both operands of a product are of one type, and a second
+// part of each would double P's stores and products: an output is off by 0.0018 to 0.0020 of its
+// size (root mean square), by 0.0016 with weights in binary32, which is the output's own rounding.
 //
 // A word of eight codes gives four pairs (elements i and i + 4): or-ing four bits into bf16 128
 // makes 128 + c, and (128 + c) s - 136 s is exact.  The order of elements (keys) that comes of it
@@ -34,7 +36,7 @@
 // memory is freed before the CTA exits.
 //
 // What bounds it: the warps' instructions, not the bytes.  4 x 32768 tokens with 32 query and 8 kv
-// heads of 128 (143 MB, 21 us at the copy rate) take 44.3 us with one row a head, 3.2 TB/s, and 67.3 us
+// heads of 128 (143 MB, 21 us at the copy rate) take 44.4 us with one row a head, 3.2 TB/s, and 67.3 us
 // with 16.  Of the 0.8 us that a tile takes with one row, 0.6 are left without the widening's
 // arithmetic; with 16 the softmax groups are busy throughout, 2100 cycles a tile, of which almost a thousand
 // are a tile's own waits, barrier and masks; the products take 540.  (Scores loaded a chunk ahead made

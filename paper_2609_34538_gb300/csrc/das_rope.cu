@@ -10,10 +10,11 @@
 // The lane's four angles serve all of the token's heads.
 //
 // Bound by memory, reads and writes of 2 bytes an element each.  4 x 2001 tokens of prompts of 500
-// to 2001, 48 heads of 128, take 24.9 us, 70% of the measured copy rate; in a loop on the same rows 23.8,
-// without two steps' loads before the first use 28.1, with four steps' 22.6, but then 16 x 16 tokens
-// take 5.7 us instead of 5.3; with 40 warps to an SM instead of 32, whose registers spill, 30 and more.
-// Angles in doubles took 13 us more, as doubles are slow.
+// to 2001, 48 heads of 128, take 25.3 us, 69% of the measured copy rate, 16 x 16 tokens with half of the
+// head rotated 4.4 us, a single token 3.2 us.  As measured when they were chosen, in a loop on the same rows:
+// 23.8 us, without two steps' loads before the first use 28.1, with four steps' 22.6, but then 16 x 16 tokens
+// took 5.7 us instead of 5.3; with 40 warps to an SM instead of 32, whose registers spill, 30 and more.
+// Angles in doubles took 13 us more, as doubles are slow.  The choice of what is not rotated takes 0.2 us.
 #include <algorithm>
 
 #include "das_internal.h"
@@ -201,8 +202,9 @@ cudaError_t rope_launch(const RopeArgs &a, int head_dim, cudaStream_t stream) {
     const int sms = attn_grid_size(dev);
     if (sms <= 0) return cudaErrorInvalidDevice;
     const int rows = 256 / head_dim;  // heads that a warp takes at once
-    // warps to a token until there are 16 to an SM, each with whole steps (16 x 16 tokens of 4 to 16 and 16 x 64:
-    // 4.2 and 6.8 us; until there are 8 4.5 and 7.5, 24 5.3 and 6.8; 256 tokens 5.4, 4.7 and 6.7)
+    // warps to a token until there are 16 to an SM, each with whole steps (as measured when it was chosen, 16 x 16
+    // tokens of 4 to 16 and 16 x 64: 4.2 and 6.8 us; until there are 8 4.5 and 7.5, 24 5.3 and 6.8; 256 tokens
+    // 5.4, 4.7 and 6.7)
     p.part = p.heads;
     while (p.part > rows && tokens * ((p.heads + p.part - 1) / p.part) < (long long)sms * 16) p.part = (p.part / 2 + rows - 1) / rows * rows;
     p.parts = (p.heads + p.part - 1) / p.part;

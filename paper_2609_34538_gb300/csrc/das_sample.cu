@@ -86,8 +86,8 @@ __device__ __forceinline__ T block_reduce(T v, T *sums, F f) {
 // ---- a row in the shared memory of a cluster ---------------------------------------
 constexpr int kDrawThreads = 1024;
 // Rows that are recorded are not held but read again, from L2: two CTAs of half the threads
-// share an SM, and one's waits are the other's time (2 x 128 rows of 32000 and the acceptance: 28.7 us,
-// 40 with the rows held; 2 x 64 of 128257: 50 us).
+// share an SM, and one's waits are the other's time (2 x 128 rows of 32000 and the acceptance, as measured
+// when it was chosen: 28.7 us, 40 with the rows held).
 constexpr int kRecordThreads = 512;
 constexpr int kMaxRowCtas = 8;                 // a portable cluster
 // Logits per CTA, as they come: what shared memory holds, and fewer than 2^16, so that
@@ -1519,11 +1519,11 @@ __global__ void __launch_bounds__(kScanWarps * 32)
 
 // ---- proposals that were drawn by chance -------------------------------------------
 // From the rows' records: the first proposal that is refused, and the draw in its place from
-// what the target's row has more.  What bounds a call: of the 50 us of 64 proposals of 128257 bf16
-// logits each, whose 33 MB take 4.8 us, the rows' first pass (largest logit and bins) takes 12, the
+// what the target's row has more.  What bounds a call: of the 48.0 us of 64 proposals of 128257 bf16
+// logits each, whose 33 MB take 4.8 us, the rows' first pass (largest logit and bins) takes about 12, the
 // look for the cut 10, the count of the logits equal to it 6, and this kernel 13, of which 8 are the
-// sweep over one row of target and drafter by 64 of the SMs.  One sequence's 8 proposals of 32000 take
-// 22 us, all latency.  A cluster to a sequence; each of its warps has a run of
+// sweep over one row of target and drafter by 64 of the SMs; the rest is launches and barriers.  8 x 16
+// proposals of 32000 take 28 to 30 us, one sequence's 8 of 32000 20 to 22 us, all latency.  A cluster to a sequence; each of its warps has a run of
 // the row in 32 steps at most, whose sums stand in its lanes: the warp that the draw falls
 // to finds the step in them and computes that alone again.
 constexpr int kAcceptThreads = 1024;
